@@ -97,6 +97,8 @@ extern "C" {
 #define ANS_U8   0   /* decoded symbols, one byte each             */
 #define ANS_F32  1   /* dequantised weights, IEEE single           */
 #define ANS_BF16 2   /* dequantised weights, bfloat16 (RNE of F32) */
+#define ANS_E4M3 3   /* 8-bit floats (4 exponent, 3 mantissa bits, largest 448); operands and outputs of the
+                        norm and the product only, no out_dtype of the decode calls */
 
 #define ANS_LAYOUT_INTERLEAVED 0
 #define ANS_LAYOUT_PRIVATE     1
@@ -118,6 +120,8 @@ extern "C" {
 #define ANS_STATUS_COPY_TIMEOUT    8u   /* an asynchronous copy of compressed bytes into shared memory
                                            did not complete within the kernel's bounded wait; the
                                            warp that waited decoded nothing further            */
+#define ANS_STATUS_BAD_PAGE        16u  /* cache calls: a slot, page number or row range lies outside the
+                                           cache; nothing was written there, what was read is zeros */
 
 /*
  * One layer of a decode call.  For the *_batch call an array of these lives in device
@@ -410,6 +414,115 @@ int ans_encode_layer_device(const uint8_t* d_symbols, uint64_t n_symbols, const 
  * ------------------------------------------------------------------------------------ */
 int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, int N, int K, float* d_y,
                          uint32_t* d_status, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * The operators around a product with decoded weights.
+ * All three take strides in ELEMENTS, enqueue one kernel on `stream` and return without
+ * waiting; they need no workspace and keep nothing from one call for the next.  Sizes of
+ * zero are fine (nothing is launched).  Unless said otherwise, outputs do not overlap inputs.
+ * ------------------------------------------------------------------------------------ */
+
+/*
+ * Root-mean-square norm of every row, with the residual's addition before it:
+ *   h = x + residual (in fp32),   y = h * 1/sqrt(mean(h^2) + eps) * weight.
+ * out_dtype ANS_BF16 or ANS_F32: d_out holds y, rounded once.  ANS_E4M3: d_out holds
+ * q = e4m3(y / s) (to nearest even), d_scales the row's s = max(max|y| / 448, 2^-126).
+ * A row with a NaN in it gets NaN everywhere, its scale too.
+ * d_sum receives h, rounded once to x's type; it may be the same buffer as d_x or d_residual
+ * (same stride).  width <= 32768.  Any alignment and any strides >= width; the fast path needs
+ * the rows of all four matrices to start equally far from a multiple of 16 bytes (8 for 8-bit
+ * rows), in elements, and d_weight on a multiple of 16 bytes.
+ */
+typedef struct ans_norm_desc {
+  const void* d_x;                /* rows x width, x_dtype                                   */
+  const void* d_residual;         /* rows x width, x_dtype; NULL: none                       */
+  const void* d_weight;           /* [width], weight_dtype; NULL: ones                       */
+  void*       d_out;              /* rows x width, out_dtype                                 */
+  float*      d_scales;           /* [rows]; used with ANS_E4M3 only                         */
+  void*       d_sum;              /* rows x width, x_dtype; NULL: not stored                 */
+  uint64_t    rows;
+  uint64_t    x_stride, residual_stride, out_stride, sum_stride;
+  uint32_t    width;
+  float       eps;                /* >= 0                                                    */
+  int32_t     x_dtype;            /* ANS_BF16 or ANS_F32                                     */
+  int32_t     weight_dtype;       /* ANS_BF16 or ANS_F32                                     */
+  int32_t     out_dtype;          /* ANS_BF16, ANS_F32 or ANS_E4M3                           */
+} ans_norm_desc;
+int ans_rms_norm(const ans_norm_desc* h_desc, void* stream);
+
+#define ANS_ACT_NONE      0
+#define ANS_ACT_RELU      1
+#define ANS_ACT_GELU      2   /* v/2 (1 + erf(v / sqrt 2))                                    */
+#define ANS_ACT_GELU_TANH 3   /* v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3)))                */
+#define ANS_ACT_SILU      4   /* v / (1 + exp(-v))                                            */
+
+/*
+ * Matrix product with its epilogue, on the tensor cores with sums in fp32:
+ *   Y[m][n] = act( x_scale[m] * w_scale[n] * sum_k X[m][k] W[n][k] + bias[n] ) + residual[m][n].
+ * X and W are both ANS_BF16 (weights as the decode calls write them) or both ANS_E4M3 (rows of
+ * ans_rms_norm; symbols q - zero_point of weights of up to 4 bits are integers of at most 15 and
+ * exact in e4m3).  The epilogue works in fp32 and rounds once.
+ * d_x and d_w 16-byte aligned, their strides multiples of 16 bytes; columns from k on are never
+ * used.  y and residual of any alignment; d_residual may be d_y (same stride).
+ * d_status as for the decode calls (ANS_STATUS_COPY_TIMEOUT).
+ */
+typedef struct ans_product_desc {
+  const void*  d_x;               /* m x k, dtype                                            */
+  const void*  d_w;               /* n x k, dtype: row = output feature                      */
+  const float* d_x_scales;        /* [m]; NULL: ones                                         */
+  const float* d_w_scales;        /* [n]; NULL: ones                                         */
+  const float* d_bias;            /* [n]; NULL: none                                         */
+  const void*  d_residual;        /* m x n, y_dtype; NULL: none                              */
+  void*        d_y;               /* m x n, y_dtype                                          */
+  uint64_t     x_stride, w_stride, residual_stride, y_stride;
+  uint32_t     m, n, k;           /* m and n up to 2^30, k up to 2^22                        */
+  int32_t      dtype;             /* ANS_BF16 or ANS_E4M3                                    */
+  int32_t      y_dtype;           /* ANS_BF16 or ANS_F32                                     */
+  int32_t      activation;        /* ANS_ACT_*                                               */
+} ans_product_desc;
+int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
+
+/*
+ * A paged cache of keys and values, quantised as it is written.  Every group of `group` values of
+ * one (token, head) is quantised by itself (Section II-B's uniform quantiser with a zero-point, zero
+ * always representable).  With L = 2^bitwidth - 1, u = 1 / L, lo = min(values, 0), hi = max(values, 0),
+ * every operation rounded to fp32:
+ *   scale = max(hi * u - lo * u, 2^-126),  zero = rint(-lo / scale),
+ *   code  = clamp(rint(x / scale) + zero, 0, L),     read back as  scale * (code - zero),
+ * rounded to nearest even where bf16 is asked for (what passes the type's largest finite value reads as
+ * that value).  A group that holds a NaN or an infinity is
+ * stored with scale NaN and reads back as NaN.
+ * Arrays, all contiguous (token slot = page * page_size + offset in the page):
+ *   codes  uint8_t[n_pages][page_size][heads][head_dim * bitwidth / 8]; 4 bits: value 2i in the low
+ *          half of byte i, value 2i + 1 in the high half;
+ *   scales float[n_pages][page_size][heads][head_dim / group], zeros uint8_t of the same shape.
+ */
+typedef struct ans_cache_desc {
+  uint8_t* d_k_codes;  float* d_k_scales;  uint8_t* d_k_zeros;    /* codes and scales 16-byte aligned */
+  uint8_t* d_v_codes;  float* d_v_scales;  uint8_t* d_v_zeros;
+  uint32_t n_pages, page_size;
+  uint32_t heads, head_dim;       /* head_dim a multiple of group                            */
+  uint32_t group;                 /* a multiple of 16, up to 256                             */
+  int32_t  bitwidth;              /* 8 or 4                                                  */
+} ans_cache_desc;
+
+/* Quantise tokens x heads x head_dim keys and values (dtype ANS_BF16 or ANS_F32; the values of one
+ * head contiguous, tokens and heads `*_token_stride` and `*_head_stride` elements apart, any
+ * alignment) into the slots d_slots[tokens].  A negative slot skips its token; a slot past the end
+ * is skipped and flagged ANS_STATUS_BAD_PAGE.  No slot may be named twice in one call. */
+int ans_cache_write(const ans_cache_desc* h_desc, const void* d_k, const void* d_v, int dtype, uint64_t tokens,
+                    uint64_t k_token_stride, uint64_t k_head_stride, uint64_t v_token_stride,
+                    uint64_t v_head_stride, const int64_t* d_slots, uint32_t* d_status, void* stream);
+
+/* Read sequences back: row d_starts[s] + i of d_k_out and d_v_out, i < d_starts[s + 1] - d_starts[s],
+ * is token i of sequence s, found in page d_tables[s * table_stride + i / page_size]; the table of a
+ * sequence has table_pages <= table_stride entries (one sequence: any stride).  The outputs are rows x heads x head_dim, contiguous, 16-byte aligned, out_dtype ANS_BF16 or ANS_F32; d_starts
+ * [n_seqs + 1] starts at 0 and does not decrease.  Rows past d_starts[n_seqs] are not written; a page
+ * number outside the cache, or a token past table_pages pages, reads as zeros and is flagged
+ * ANS_STATUS_BAD_PAGE, as is d_starts[n_seqs] > rows (the rows that fit are read). */
+int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tables, uint64_t table_stride, uint32_t table_pages,
+                   uint32_t n_seqs, const int32_t* d_starts, uint64_t rows, void* d_k_out, void* d_v_out,
+                   int out_dtype, uint32_t* d_status, void* stream);
 
 #ifdef __cplusplus
 }

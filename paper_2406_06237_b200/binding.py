@@ -19,8 +19,13 @@ ANS_ERR_BUFFER_TOO_SMALL, ANS_ERR_CUDA, ANS_ERR_CORRUPT = -4, -5, -6
 ANS_U8, ANS_F32, ANS_BF16 = 0, 1, 2
 ANS_LAYOUT_INTERLEAVED, ANS_LAYOUT_PRIVATE, ANS_LAYOUT_QUADS, ANS_LAYOUT_STRIPS, ANS_LAYOUT_CHANNELS = 0, 1, 2, 3, 4
 ANS_DESC_INPUTS_SETTLED, ANS_DESC_OUTPUT_IDLE = 1, 2
+ANS_E4M3 = 3
 DTYPES = {"u8": ANS_U8, "f32": ANS_F32, "bf16": ANS_BF16}
 ELEM_SIZE = {ANS_U8: 1, ANS_F32: 4, ANS_BF16: 2}
+ANS_STATUS_BAD_PAGE = 16
+ANS_ACT_NONE, ANS_ACT_RELU, ANS_ACT_GELU, ANS_ACT_GELU_TANH, ANS_ACT_SILU = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": ANS_ACT_NONE, "relu": ANS_ACT_RELU, "gelu": ANS_ACT_GELU, "gelu_tanh": ANS_ACT_GELU_TANH,
+               "silu": ANS_ACT_SILU}
 
 EXPORTS = [
     "ans_version", "ans_strerror", "ans_last_cuda_error", "ans_table_bytes", "ans_build_decode_tables",
@@ -31,6 +36,7 @@ EXPORTS = [
     "ans_histogram_device", "ans_entropy_device", "ans_normalize_freqs_device",
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
+    "ans_rms_norm", "ans_product", "ans_cache_write", "ans_cache_read",
 ]
 
 
@@ -43,6 +49,37 @@ class ans_layer_desc(ctypes.Structure):
         ("scale", ctypes.c_float), ("out_dtype", ctypes.c_int32), ("layout", ctypes.c_int32),
         ("work_begin", ctypes.c_uint32), ("work_count", ctypes.c_uint32),
         ("piece_symbols", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+    ]
+
+
+class ans_norm_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_x", ctypes.c_void_p), ("d_residual", ctypes.c_void_p), ("d_weight", ctypes.c_void_p),
+        ("d_out", ctypes.c_void_p), ("d_scales", ctypes.c_void_p), ("d_sum", ctypes.c_void_p),
+        ("rows", ctypes.c_uint64), ("x_stride", ctypes.c_uint64), ("residual_stride", ctypes.c_uint64),
+        ("out_stride", ctypes.c_uint64), ("sum_stride", ctypes.c_uint64), ("width", ctypes.c_uint32),
+        ("eps", ctypes.c_float), ("x_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+    ]
+
+
+class ans_product_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_x", ctypes.c_void_p), ("d_w", ctypes.c_void_p), ("d_x_scales", ctypes.c_void_p),
+        ("d_w_scales", ctypes.c_void_p), ("d_bias", ctypes.c_void_p), ("d_residual", ctypes.c_void_p),
+        ("d_y", ctypes.c_void_p), ("x_stride", ctypes.c_uint64), ("w_stride", ctypes.c_uint64),
+        ("residual_stride", ctypes.c_uint64), ("y_stride", ctypes.c_uint64), ("m", ctypes.c_uint32),
+        ("n", ctypes.c_uint32), ("k", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+    ]
+
+
+class ans_cache_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_k_codes", ctypes.c_void_p), ("d_k_scales", ctypes.c_void_p), ("d_k_zeros", ctypes.c_void_p),
+        ("d_v_codes", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p), ("d_v_zeros", ctypes.c_void_p),
+        ("n_pages", ctypes.c_uint32), ("page_size", ctypes.c_uint32), ("heads", ctypes.c_uint32),
+        ("head_dim", ctypes.c_uint32), ("group", ctypes.c_uint32), ("bitwidth", ctypes.c_int32),
     ]
 
 
@@ -97,6 +134,10 @@ def lib():
         L.ans_encode_layer_device.argtypes = [vp, u64, vp, i32, u32, u32, i32, vp, u64, vp, vp, sz, vp, vp]
         L.ans_encode_channels_device.argtypes = [vp, u64, vp, i32, u32, u32, u32, vp, u64, vp, vp, sz, vp, vp]
         L.ans_encode_quads_device.argtypes = [vp, u64, vp, i32, u32, u32, vp, u64, vp, vp, vp, sz, vp, vp]
+        L.ans_rms_norm.argtypes = [P(ans_norm_desc), vp]
+        L.ans_product.argtypes = [P(ans_product_desc), vp, vp]
+        L.ans_cache_write.argtypes = [P(ans_cache_desc), vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, vp]
+        L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
         _LIB = L
     return _LIB
 
@@ -310,3 +351,24 @@ def ans_host_pack_channels(symbols: np.ndarray, freqs: np.ndarray, alphabet: int
 def ans_decode_gemm_bf16(h_desc: ans_layer_desc, d_x: int, M: int, N: int, K: int, d_y: int, d_status: int,
                          stream: int = 0) -> None:
     _check(lib().ans_decode_gemm_bf16(ctypes.byref(h_desc), d_x, M, N, K, d_y, d_status, stream), "ans_decode_gemm_bf16")
+
+
+def ans_rms_norm(h_desc: ans_norm_desc, stream: int = 0) -> None:
+    _check(lib().ans_rms_norm(h_desc, stream), "ans_rms_norm")
+
+
+def ans_product(h_desc: ans_product_desc, d_status: int, stream: int = 0) -> None:
+    _check(lib().ans_product(h_desc, d_status, stream), "ans_product")
+
+
+def ans_cache_write(h_desc: ans_cache_desc, d_k: int, d_v: int, dtype: int, tokens: int, k_strides, v_strides,
+                    d_slots: int, d_status: int, stream: int = 0) -> None:
+    """k_strides, v_strides: (token stride, head stride) in elements."""
+    _check(lib().ans_cache_write(h_desc, d_k, d_v, dtype, tokens, k_strides[0], k_strides[1], v_strides[0], v_strides[1],
+                                 d_slots, d_status, stream), "ans_cache_write")
+
+
+def ans_cache_read(h_desc: ans_cache_desc, d_tables: int, table_stride: int, table_pages: int, n_seqs: int, d_starts: int,
+                   rows: int, d_k_out: int, d_v_out: int, out_dtype: int, d_status: int, stream: int = 0) -> None:
+    _check(lib().ans_cache_read(h_desc, d_tables, table_stride, table_pages, n_seqs, d_starts, rows, d_k_out, d_v_out,
+                                out_dtype, d_status, stream), "ans_cache_read")

@@ -1,0 +1,313 @@
+"""The operators around a product with decoded weights, on torch tensors: torch supplies memory and the
+stream, the library's kernels compute.  A handle keeps what does not change between calls (weights and
+a call descriptor), never an input or an output, and is used by one thread at a time.  Every call
+enqueues on the current stream of its tensors' device and returns without waiting."""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+_ELEMENT = {torch.bfloat16: B.ANS_BF16, torch.float32: B.ANS_F32, torch.float8_e4m3fn: B.ANS_E4M3}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _on_device(t: torch.Tensor, device: torch.device, what: str) -> None:
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the handle on {device}")
+
+
+def _cuda_device(device) -> torch.device:
+    d = torch.device(device)
+    if d.type != "cuda":
+        raise RuntimeError("the operators need a CUDA device: there is no CPU path")
+    return torch.device("cuda", torch.cuda.current_device() if d.index is None else d.index)
+
+
+class _Handle:
+    """A device, and the status word its calls report to."""
+
+    def __init__(self, device):
+        self.device = _cuda_device(device)
+        self._index = self.device.index
+        self.status = torch.zeros(64, dtype=torch.int32, device=self.device)
+        self._status = self.status.data_ptr()
+
+    def _enter(self) -> int:
+        """The current stream; the library launches on the current device."""
+        if torch.cuda.current_device() != self._index:
+            raise RuntimeError(f"the handle is on {self.device}, which is not the current device")
+        return torch.cuda.current_stream(self._index).cuda_stream
+
+    def read_status(self) -> int:
+        """Waits for the stream; ANS_STATUS_* bits that calls have set since the last look (0: all sound)."""
+        return B.ans_read_status(self._status, self._enter())
+
+
+def _rows(t: torch.Tensor, what: str) -> int:
+    """Row stride of a matrix whose rows are contiguous."""
+    _need(t.dim() == 2, f"{what} must be a matrix")
+    rows, width = t.shape
+    stride, one = t.stride()
+    _need(one == 1 or width <= 1, f"the rows of {what} must be contiguous")
+    if stride < width:
+        _need(rows <= 1, f"the rows of {what} overlap")
+        return width
+    return stride
+
+
+class RmsNorm(_Handle):
+    """y = h / sqrt(mean(h^2) + eps) * weight with h = x + residual, rows of `x` by themselves.
+
+    weight: [width], bf16 or fp32, or None (ones; `device` must then be given).  out_dtype: bf16,
+    fp32, or float8_e4m3fn: then y is returned as q with one fp32 scale a row, y ~ scale * q."""
+
+    def __init__(self, weight: torch.Tensor | None, eps: float = 1e-6, out_dtype: torch.dtype = torch.bfloat16, device=None):
+        super().__init__(weight.device if weight is not None else device or "cuda")
+        _need(out_dtype in _ELEMENT, f"out_dtype {out_dtype} is not supported")
+        if weight is not None:
+            _need(weight.dim() == 1 and weight.is_contiguous(), "weight must be a contiguous vector")
+            _need(weight.dtype in (torch.bfloat16, torch.float32), "weight must be bf16 or fp32")
+        self.weight, self.eps, self.out_dtype = weight, float(eps), out_dtype
+        self._desc = d = B.ans_norm_desc()
+        d.d_weight = weight.data_ptr() if weight is not None and weight.numel() else None
+        d.weight_dtype = _ELEMENT[weight.dtype] if weight is not None else B.ANS_F32
+        d.eps, d.out_dtype = self.eps, _ELEMENT[out_dtype]
+
+    def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                 scales: torch.Tensor | None = None, summed: torch.Tensor | None = None):
+        """x, residual: [rows, width] of one type, bf16 or fp32.  Returns (out, scales, summed): scales
+        ([rows] fp32) only with an 8-bit output, summed (x + residual in x's type) only with a residual;
+        None otherwise.  Buffers given for them are written and returned; summed may be x or residual."""
+        st, d = self._enter(), self._desc
+        xs = _rows(x, "x")
+        rows, width = x.shape
+        dt = x.dtype
+        _need(dt is torch.bfloat16 or dt is torch.float32, "x must be bf16 or fp32")
+        _on_device(x, self.device, "x")
+        _need(self.weight is None or self.weight.shape[0] == width, "weight and x differ in width")
+        if out is None:
+            out = torch.empty(rows, width, dtype=self.out_dtype, device=self.device)
+        else:
+            _need(out.dtype is self.out_dtype and out.shape == x.shape, "out has the wrong type or shape")
+            _on_device(out, self.device, "out")
+        if self.out_dtype is torch.float8_e4m3fn:
+            if scales is None:
+                scales = torch.empty(rows, dtype=torch.float32, device=self.device)
+            else:
+                _need(scales.dtype is torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales must be fp32 [rows]")
+                _on_device(scales, self.device, "scales")
+            d.d_scales = scales.data_ptr()
+        else:
+            _need(scales is None, "scales belong to an 8-bit output")
+        if residual is not None:
+            _need(residual.dtype is dt and residual.shape == x.shape, "residual and x differ")
+            _on_device(residual, self.device, "residual")
+            if summed is None:
+                summed = torch.empty(rows, width, dtype=dt, device=self.device)
+            else:
+                _need(summed.dtype is dt and summed.shape == x.shape, "summed has the wrong type or shape")
+                _on_device(summed, self.device, "summed")
+            d.d_residual, d.residual_stride = residual.data_ptr(), _rows(residual, "residual")
+            d.d_sum, d.sum_stride = summed.data_ptr(), _rows(summed, "summed")
+        else:
+            _need(summed is None, "summed belongs to a residual")
+            d.d_residual = d.d_sum = None
+        d.d_x, d.x_stride, d.x_dtype, d.rows, d.width = x.data_ptr(), xs, _ELEMENT[dt], rows, width
+        d.d_out, d.out_stride = out.data_ptr(), _rows(out, "out")
+        B.ans_rms_norm(d, st)
+        return out, scales, summed
+
+
+def symbols_to_e4m3(symbols: torch.Tensor, zero_point: int) -> torch.Tensor:
+    """Decoded symbols (uint8, any shape) as e4m3 values q - zero_point: the weights of a Linear in 8 bits,
+    whose `scales` is then the layer's scale.  Raises if a difference in use is not exact in e4m3 (those
+    of up to 4 bits always are)."""
+    table = (torch.arange(256, dtype=torch.float32) - zero_point)
+    exact = table.to(torch.float8_e4m3fn).float() == table
+    used = torch.bincount(symbols.reshape(-1), minlength=256).cpu() > 0 if symbols.numel() else torch.zeros(256, dtype=torch.bool)
+    _need(bool(exact[used].all()), "a symbol minus the zero-point is not exact in e4m3")
+    return table.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).to(symbols.device)[symbols.long()].view(torch.float8_e4m3fn)
+
+
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy of it, with contiguous rows that start on 16 bytes."""
+    size = t.element_size()
+    if t.data_ptr() % 16 == 0 and (t.stride(1) == 1 or t.shape[1] <= 1) and (t.shape[0] <= 1 or t.stride(0) * size % 16 == 0 and t.stride(0) >= t.shape[1]):
+        return t
+    pad = 16 // size
+    room = torch.empty(t.shape[0], (t.shape[1] + pad - 1) // pad * pad, dtype=t.dtype, device=t.device)
+    room = room[:, :t.shape[1]]
+    room.copy_(t)
+    return room
+
+
+class Linear(_Handle):
+    """Y = act(x_scales * scales * X W^T + bias) + residual with W [out features, in features].
+
+    weight: bf16 (as decoded) or float8_e4m3fn (see symbols_to_e4m3).  scales: fp32, one for each
+    output feature or one for all (a float or one element), or None.  bias: [out features] or None.
+    activation: "none", "relu", "gelu", "gelu_tanh" or "silu".  A weight whose rows do not start on 16
+    bytes is copied once into rows that do."""
+
+    def __init__(self, weight: torch.Tensor, scales=None, bias: torch.Tensor | None = None, activation: str = "none"):
+        super().__init__(weight.device)
+        _need(weight.dim() == 2, "weight must be a matrix")
+        _need(weight.dtype in (torch.bfloat16, torch.float8_e4m3fn), "weight must be bf16 or float8_e4m3fn")
+        _need(activation in B.ACTIVATIONS, f"activation {activation!r} is not one of {', '.join(B.ACTIVATIONS)}")
+        n, k = weight.shape
+        self.weight = _aligned(weight)
+        if scales is not None:
+            scales = torch.as_tensor(scales, dtype=torch.float32, device=self.device).reshape(-1)
+            _need(scales.numel() in (1, n), "scales must be one or one for each output feature")
+            scales = scales.expand(n).contiguous()
+        if bias is not None:
+            _need(bias.shape == (n,), "bias must have one value for each output feature")
+            bias = bias.to(device=self.device, dtype=torch.float32).contiguous()
+        self.scales, self.bias, self.activation = scales, bias, activation
+        self.in_features, self.out_features = k, n
+        self._desc = d = B.ans_product_desc()
+        d.d_w, d.w_stride = self.weight.data_ptr() or None, max(self.weight.stride(0), k)
+        d.d_w_scales = scales.data_ptr() if scales is not None else None
+        d.d_bias = bias.data_ptr() if bias is not None else None
+        d.n, d.k, d.dtype, d.activation = n, k, _ELEMENT[weight.dtype], B.ACTIVATIONS[activation]
+
+    def __call__(self, x: torch.Tensor, x_scales: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                 out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """x: [rows, in features] of the weight's type; x_scales: [rows] fp32.  Returns out (bf16 or fp32,
+        [rows, out features]), the given buffer if there is one; residual is of its type and may be out
+        itself.  An x whose rows do not start on 16 bytes is copied first."""
+        st, d = self._enter(), self._desc
+        _need(x.dim() == 2 and x.shape[1] == self.in_features, "x must be [rows, in features]")
+        _need(x.dtype is self.weight.dtype, f"x is {x.dtype}, the weight {self.weight.dtype}")
+        _on_device(x, self.device, "x")
+        rows = x.shape[0]
+        x = _aligned(x)
+        shape = (rows, self.out_features)
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype, device=self.device)
+        else:
+            _need(out.shape == shape, "out has the wrong shape")
+            _on_device(out, self.device, "out")
+        dt = out.dtype
+        _need(dt is torch.bfloat16 or dt is torch.float32, "the output is bf16 or fp32")
+        if x_scales is not None:
+            _need(x_scales.dtype is torch.float32 and x_scales.shape == (rows,) and x_scales.is_contiguous(), "x_scales must be fp32 [rows]")
+            _on_device(x_scales, self.device, "x_scales")
+            d.d_x_scales = x_scales.data_ptr()
+        else:
+            d.d_x_scales = None
+        if residual is not None:
+            _need(residual.dtype is dt and residual.shape == shape, "residual and out differ")
+            _on_device(residual, self.device, "residual")
+            d.d_residual, d.residual_stride = residual.data_ptr(), _rows(residual, "residual")
+        else:
+            d.d_residual = None
+        d.d_x, d.x_stride, d.m = x.data_ptr(), max(x.stride(0), self.in_features), rows
+        d.d_y, d.y_stride, d.y_dtype = out.data_ptr(), _rows(out, "out"), _ELEMENT[dt]
+        B.ans_product(d, self._status, st)
+        return out
+
+
+class PagedCache(_Handle):
+    """A paged cache of keys and values in 8 or 4 bits, quantised with a scale and a zero-point for every
+    `group` values of a (token, head) as they are written (see ans_cache_desc in the header).
+
+    Pages are the caller's to assign: token i of a sequence lies in slot
+    table[i // page_size] * page_size + i % page_size."""
+
+    def __init__(self, n_pages: int, page_size: int, heads: int, head_dim: int, bitwidth: int = 8, group: int | None = None, device="cuda"):
+        group = head_dim if group is None else group
+        _need(bitwidth in (4, 8), "bitwidth must be 8 or 4")
+        _need(min(n_pages, page_size, heads, head_dim, group) > 0, "sizes must be positive")
+        _need(head_dim % group == 0 and head_dim % 2 == 0, "head_dim must be a multiple of group")
+        device = _cuda_device(device)
+
+        def make(last, dtype):
+            return torch.zeros(n_pages, page_size, heads, last, dtype=dtype, device=device)
+
+        codes, groups = head_dim * bitwidth // 8, head_dim // group
+        self._hold(make(codes, torch.uint8), make(groups, torch.float32), make(groups, torch.uint8),
+                   make(codes, torch.uint8), make(groups, torch.float32), make(groups, torch.uint8), bitwidth)
+
+    @classmethod
+    def wrap(cls, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth: int) -> "PagedCache":
+        """A cache on existing arrays (shapes as in ans_cache_desc), which are used in place."""
+        self = cls.__new__(cls)
+        self._hold(k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth)
+        return self
+
+    def _hold(self, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth):
+        _Handle.__init__(self, k_codes.device)
+        _need(bitwidth in (4, 8), "bitwidth must be 8 or 4")
+        _need(k_codes.dim() == 4 and k_scales.dim() == 4, "codes, scales and zeros have four dimensions")
+        dim = k_codes.shape[3] * 8 // bitwidth
+        groups = k_scales.shape[3]
+        _need(groups > 0 and dim % groups == 0, "codes and scales do not fit together")
+        params = (*k_codes.shape[:3], groups)
+        for t, dtype, shape, what in ((k_codes, torch.uint8, k_codes.shape, "k_codes"), (v_codes, torch.uint8, k_codes.shape, "v_codes"),
+                                      (k_scales, torch.float32, params, "k_scales"), (v_scales, torch.float32, params, "v_scales"),
+                                      (k_zeros, torch.uint8, params, "k_zeros"), (v_zeros, torch.uint8, params, "v_zeros")):
+            _need(t.dtype is dtype and t.shape == shape and t.is_contiguous(), f"{what} must be a contiguous {dtype} tensor of {tuple(shape)}")
+            _on_device(t, self.device, what)
+        self.k_codes, self.k_scales, self.k_zeros = k_codes, k_scales, k_zeros
+        self.v_codes, self.v_scales, self.v_zeros = v_codes, v_scales, v_zeros
+        self.n_pages, self.page_size, self.heads = k_codes.shape[:3]
+        self.head_dim, self.group, self.bitwidth = dim, dim // groups, bitwidth
+        self._desc = d = B.ans_cache_desc()
+        d.d_k_codes, d.d_k_scales, d.d_k_zeros = k_codes.data_ptr(), k_scales.data_ptr(), k_zeros.data_ptr()
+        d.d_v_codes, d.d_v_scales, d.d_v_zeros = v_codes.data_ptr(), v_scales.data_ptr(), v_zeros.data_ptr()
+        d.n_pages, d.page_size, d.heads, d.head_dim = self.n_pages, self.page_size, self.heads, dim
+        d.group, d.bitwidth = self.group, bitwidth
+
+    def _strides(self, t: torch.Tensor, what: str):
+        _need(t.dim() == 3 and t.shape[1:] == (self.heads, self.head_dim), f"{what} must be [tokens, heads, head_dim]")
+        _need(t.stride(2) == 1, f"the values of a head of {what} must be contiguous")
+        _on_device(t, self.device, what)
+        return t.stride(0), t.stride(1)
+
+    def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+        """k, v: [tokens, heads, head_dim], bf16 or fp32, tokens and heads at any stride; slots: [tokens]
+        int64, a negative one skips its token."""
+        st = self._enter()
+        ks, vs = self._strides(k, "k"), self._strides(v, "v")
+        dt, tokens = k.dtype, k.shape[0]
+        _need(dt is torch.bfloat16 or dt is torch.float32, "k and v must be bf16 or fp32")
+        _need(v.dtype is dt and v.shape[0] == tokens, "k and v differ")
+        _need(slots.dtype is torch.int64 and slots.shape == (tokens,) and slots.is_contiguous(), "slots must be int64 [tokens]")
+        _on_device(slots, self.device, "slots")
+        B.ans_cache_write(self._desc, k.data_ptr(), v.data_ptr(), _ELEMENT[dt], tokens, ks, vs, slots.data_ptr(), self._status, st)
+
+    def read(self, tables: torch.Tensor, starts: torch.Tensor, rows: int | None = None, k_out: torch.Tensor | None = None,
+             v_out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16):
+        """The keys and values of whole sequences, one after the other: [rows, heads, head_dim] each.
+        tables: [sequences, pages] int32; starts: [sequences + 1] int32, sequence s is rows starts[s] to
+        starts[s + 1].  rows = starts[-1] as a number (the call does not read it from the device), or
+        k_out and v_out of that many rows are given.  Returns (k, v)."""
+        st = self._enter()
+        _need((k_out is None) == (v_out is None), "give both of k_out and v_out or none")
+        if k_out is None:
+            _need(rows is not None, "rows is needed where no buffers are given")
+            k_out = torch.empty(rows, self.heads, self.head_dim, dtype=out_dtype, device=self.device)
+            v_out = torch.empty_like(k_out)
+        else:
+            rows = k_out.shape[0] if rows is None else rows
+            for t in (k_out, v_out):
+                _need(t.dim() == 3 and t.shape[0] >= rows and t.shape[1:] == (self.heads, self.head_dim) and t.is_contiguous(),
+                      "k_out and v_out must be contiguous [rows, heads, head_dim]")
+                _on_device(t, self.device, "an output")
+            _need(v_out.dtype is k_out.dtype, "k_out and v_out differ")
+        dt = k_out.dtype
+        _need(dt is torch.bfloat16 or dt is torch.float32, "the outputs are bf16 or fp32")
+        _need(tables.dtype is torch.int32 and tables.dim() == 2 and (tables.stride(1) == 1 or tables.shape[1] <= 1), "tables must be int32 [sequences, pages]")
+        n = tables.shape[0]
+        _need(starts.dtype is torch.int32 and starts.shape == (n + 1,) and starts.is_contiguous(), "starts must be int32 [sequences + 1]")
+        _on_device(tables, self.device, "tables")
+        _on_device(starts, self.device, "starts")
+        B.ans_cache_read(self._desc, tables.data_ptr(), tables.stride(0), tables.shape[1], n, starts.data_ptr(), rows,
+                         k_out.data_ptr(), v_out.data_ptr(), _ELEMENT[dt], self._status, st)
+        return k_out, v_out

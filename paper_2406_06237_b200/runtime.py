@@ -215,3 +215,6 @@ class DeviceBatch:
 
     def output(self, i: int, out_set: int = 0) -> torch.Tensor:
         return self.out_sets[out_set][i][:self.layers[i].n_symbols]
+
+
+from .operators import Linear, PagedCache, RmsNorm, symbols_to_e4m3  # noqa: E402,F401
