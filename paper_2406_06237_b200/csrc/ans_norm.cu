@@ -19,18 +19,32 @@ struct NormArgs {
   uint32_t width;
   float eps;
   uint32_t together;      // the rows of all matrices start equally far from a 16-byte boundary
+  uint32_t shift;         // the most that a row starts past such a boundary, in elements
   uint32_t w_f32;         // type of w
   uint32_t w_vec;         // w on a 16-byte boundary
 };
 
+// Elements of a type one by one and eight at a time.  Eight are loaded as they lie (Raw), so that all of a
+// thread's loads are under way before the first value is used; they bypass L1, which is left to the weight.
 template <typename T> struct Elem;
+template <int N> struct Raw { uint4 q[N]; };
+template <int N>
+__device__ __forceinline__ Raw<N> load_once(const void* p) {
+  Raw<N> r;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r.q[i].x), "=r"(r.q[i].y), "=r"(r.q[i].z), "=r"(r.q[i].w) : "l"(static_cast<const uint4*>(p) + i) : "memory");
+  return r;
+}
 template <> struct Elem<__nv_bfloat16> {
+  using Eight = Raw<1>;
   static __device__ __forceinline__ float one(const void* p, uint64_t i) {
     return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
   }
-  static __device__ __forceinline__ void eight(const void* p, uint64_t i, float (&v)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + i);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  static __device__ __forceinline__ const void* at(const void* p, uint64_t i) { return static_cast<const __nv_bfloat16*>(p) + i; }
+  static __device__ __forceinline__ void open(const Eight& u, float (&v)[8]) {
+    const uint32_t w[4] = {u.q[0].x, u.q[0].y, u.q[0].z, u.q[0].w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[2 * j] = __uint_as_float(w[j] << 16);
@@ -51,11 +65,17 @@ template <> struct Elem<__nv_bfloat16> {
   }
 };
 template <> struct Elem<float> {
+  using Eight = Raw<2>;
   static __device__ __forceinline__ float one(const void* p, uint64_t i) { return static_cast<const float*>(p)[i]; }
-  static __device__ __forceinline__ void eight(const void* p, uint64_t i, float (&v)[8]) {
-    const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-    const float4 a = f[0], b = f[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  static __device__ __forceinline__ const void* at(const void* p, uint64_t i) { return static_cast<const float*>(p) + i; }
+  static __device__ __forceinline__ void open(const Eight& u, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      v[4 * j] = __uint_as_float(u.q[j].x);
+      v[4 * j + 1] = __uint_as_float(u.q[j].y);
+      v[4 * j + 2] = __uint_as_float(u.q[j].z);
+      v[4 * j + 3] = __uint_as_float(u.q[j].w);
+    }
   }
   static __device__ __forceinline__ void put(void* p, uint64_t i, float v) { static_cast<float*>(p)[i] = v; }
   static __device__ __forceinline__ void put8(void* p, uint64_t i, const float (&v)[8]) {
@@ -80,45 +100,101 @@ template <> struct Elem<__nv_fp8_e4m3> {
   }
 };
 
+// Elements i .. i + 7 of w, i any number in 0 .. width - 8.
+__device__ __forceinline__ void weight8(const NormArgs& a, int i, float (&w)[8]) {
+  if (!a.w) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = 1.f;
+    return;
+  }
+  if (a.w_vec && !(i & 7)) {
+    if (a.w_f32) {
+      const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + i);
+      const float4 p = *f, q = f[1];
+      w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w; w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
+    } else {
+      Raw<1> u;
+      u.q[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + i);
+      Elem<__nv_bfloat16>::open(u, w);
+    }
+    return;
+  }
+  const int i0 = i & ~7, by = i & 7;
+  if (a.w_vec && !a.w_f32 && i0 + 16 <= static_cast<int>(a.width)) {
+    // the two aligned vectors around it, moved down by `by` elements (the same for the whole row)
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + i0);
+    const uint4 lo = p[0], hi = p[1];
+    uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (by & 4) {
+#pragma unroll
+      for (int j = 0; j < 6; ++j) c[j] = c[j + 2];
+    }
+    if (by & 2) {
+#pragma unroll
+      for (int j = 0; j < 6; ++j) c[j] = c[j + 1];
+    }
+    if (by & 1) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = __funnelshift_r(c[j], c[j + 1], 16);
+    }
+    Raw<1> u;
+    u.q[0] = make_uint4(c[0], c[1], c[2], c[3]);
+    Elem<__nv_bfloat16>::open(u, w);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = a.w_f32 ? Elem<float>::one(a.w, i + j) : Elem<__nv_bfloat16>::one(a.w, i + j);
+}
+
 constexpr uint32_t kNormWarps = 32;
 
 // blockDim = (threads of a row, rows of a block); a row of at most one warp needs no barrier.
-// Thread t of a row holds the vectors of 8 elements t, t + T, ...  Where rows start `phase` elements
+// Thread t of a row holds the V vectors of 8 elements t, t + T, ...  Where rows start `phase` elements
 // past a 16-byte boundary, vector 0 starts `phase` elements before the row, so that every vector is
 // aligned; the first and the last, and all of them where the matrices' rows are not equally aligned,
 // are read and written element by element.
-template <typename TX, typename TO, int V>
-__global__ void __launch_bounds__(1024) ans_rms_norm_kernel(const NormArgs a) {
+template <typename TX, typename TO, int V, int MOST>
+__global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
   __shared__ float s_sum[kNormWarps];
   __shared__ uint32_t s_top[kNormWarps];
+  ten::let_next_start();
   const uint64_t row = uint64_t(blockIdx.x) * blockDim.y + threadIdx.y;
   const uint32_t T = blockDim.x, t = threadIdx.x;
   const bool live = row < a.rows;
   const uint64_t xo = row * a.x_stride, ro = row * a.r_stride, oo = row * a.out_stride, so = row * a.sum_stride;
   const int width = static_cast<int>(a.width);
   const int phase = a.together ? static_cast<int>((reinterpret_cast<uintptr_t>(a.x) / sizeof(TX) + xo) & 7u) : 0;
+  auto first = [&](int j) { return static_cast<int>(t + j * T) * 8 - phase; };             // the vector's first element
+  auto whole = [&](int j) { return a.together && first(j) >= 0 && first(j) + 8 <= width; };
+  ten::wait_for_previous();
 
+  typename Elem<TX>::Eight x[V], r[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    x[j] = {}; r[j] = {};
+    if (live && whole(j)) {
+      x[j] = load_once<sizeof(TX) / 2>(Elem<TX>::at(a.x, xo + first(j)));
+      if (a.r) r[j] = load_once<sizeof(TX) / 2>(Elem<TX>::at(a.r, ro + first(j)));
+    }
+  }
   float h[V][8];
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int at = static_cast<int>(t + j * T) * 8 - phase;      // the vector's first element
-    const bool whole = live && a.together && at >= 0 && at + 8 <= width;
-    if (whole) {
-      Elem<TX>::eight(a.x, xo + at, h[j]);
-      if (a.r) {
-        float r[8];
-        Elem<TX>::eight(a.r, ro + at, r);
+    float u[8];
+    Elem<TX>::open(x[j], h[j]);
+    Elem<TX>::open(r[j], u);
+    if (a.r) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[j][i] += r[i];
-      }
-      if (a.sum) Elem<TX>::put8(a.sum, so + at, h[j]);
-    } else {
+      for (int i = 0; i < 8; ++i) h[j][i] += u[i];
+    }
+    if (live && whole(j)) {
+      if (a.sum) Elem<TX>::put8(a.sum, so + first(j), h[j]);
+    } else if (live && first(j) < width) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[j][i] = 0.f;
-        const int e = at + i;
-        if (live && e >= 0 && e < width) {
+        const int e = first(j) + i;
+        if (e >= 0 && e < width) {
           h[j][i] = Elem<TX>::one(a.x, xo + e);
           if (a.r) h[j][i] += Elem<TX>::one(a.r, ro + e);
           if (a.sum) Elem<TX>::put(a.sum, so + e, h[j][i]);
@@ -133,19 +209,15 @@ __global__ void __launch_bounds__(1024) ans_rms_norm_kernel(const NormArgs a) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int at = static_cast<int>(t + j * T) * 8 - phase;
     float w[8];
-    if (!a.w) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = 1.f;
-    } else if (a.w_vec && !(at & 7) && at >= 0 && at + 8 <= width) {
-      if (a.w_f32) Elem<float>::eight(a.w, at, w); else Elem<__nv_bfloat16>::eight(a.w, at, w);
+    if (whole(j)) {
+      weight8(a, first(j), w);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int e = at + i;
-        w[i] = 0.f;
-        if (e >= 0 && e < width) w[i] = a.w_f32 ? Elem<float>::one(a.w, e) : Elem<__nv_bfloat16>::one(a.w, e);
+        const int e = first(j) + i;
+        w[i] = 1.f;
+        if (a.w && e >= 0 && e < width) w[i] = a.w_f32 ? Elem<float>::one(a.w, e) : Elem<__nv_bfloat16>::one(a.w, e);
       }
     }
 #pragma unroll
@@ -168,7 +240,7 @@ __global__ void __launch_bounds__(1024) ans_rms_norm_kernel(const NormArgs a) {
     top = __reduce_max_sync(ten::kAll, top);
   }
   if (!live) return;
-  float f = 1.f / sqrtf(sum / static_cast<float>(width) + a.eps);
+  const float f = 1.f / sqrtf(sum / static_cast<float>(width) + a.eps);
   float back = 1.f;
   constexpr bool k8 = std::is_same<TO, __nv_fp8_e4m3>::value;
   if constexpr (k8) {
@@ -179,15 +251,14 @@ __global__ void __launch_bounds__(1024) ans_rms_norm_kernel(const NormArgs a) {
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int at = static_cast<int>(t + j * T) * 8 - phase;
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[j][i] = k8 ? h[j][i] * f * back : h[j][i] * f;
-    if (a.together && at >= 0 && at + 8 <= width) {
-      Elem<TO>::put8(a.out, oo + at, h[j]);
-    } else {
+    if (whole(j)) {
+      Elem<TO>::put8(a.out, oo + first(j), h[j]);
+    } else if (first(j) < width) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int e = at + i;
+        const int e = first(j) + i;
         if (e >= 0 && e < width) Elem<TO>::put(a.out, oo + e, h[j][i]);
       }
     }
@@ -195,36 +266,32 @@ __global__ void __launch_bounds__(1024) ans_rms_norm_kernel(const NormArgs a) {
 }
 
 template <typename TX, typename TO>
-static int launch_norm(const NormArgs& a, cudaStream_t st) {
-  const uint32_t vectors = (a.width + (a.together ? 7u : 0u) + 7u) / 8u;
-  // a warp a row up to 128 vectors, then a block a row
-  dim3 block;
-  int v;
-  if (vectors <= 128) {
-    v = vectors <= 32 ? 1 : vectors <= 64 ? 2 : 4;
-    block = dim3(32, 8);
-  } else {
-    v = vectors <= 1024 ? 1 : vectors <= 2048 ? 2 : 4;
-    block = dim3(((vectors + v - 1) / v + 31) / 32 * 32, 1);
-    if (block.x > 1024) { v = 5; block.x = 1024; }              // 32768 elements and a phase
+static int launch_norm(const NormArgs& a, int sms, cudaStream_t st) {
+  const uint32_t vectors = (a.width + a.shift + 7u) / 8u;
+  constexpr uint32_t kWide = sizeof(TX) == 2 ? 4 : 2;             // vectors a thread: 64 bytes of x
+  if (vectors <= 128) {                                           // a warp a row
+    const uint64_t blocks = (a.rows + 7) / 8;
+    if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+    const dim3 grid(static_cast<unsigned>(blocks)), block(32, 8);
+    if (vectors <= 32) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 256>, grid, block, 0, st, 1, a);
+    if (vectors <= 64) return ten::launch(ans_rms_norm_kernel<TX, TO, 2, 256>, grid, block, 0, st, 1, a);
+    return ten::launch(ans_rms_norm_kernel<TX, TO, 4, 256>, grid, block, 0, st, 1, a);
   }
-  const uint64_t blocks = (a.rows + block.y - 1) / block.y;
-  if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  switch (v) {
-    case 1: ans_rms_norm_kernel<TX, TO, 1><<<unsigned(blocks), block, 0, st>>>(a); break;
-    case 2: ans_rms_norm_kernel<TX, TO, 2><<<unsigned(blocks), block, 0, st>>>(a); break;
-    case 4: ans_rms_norm_kernel<TX, TO, 4><<<unsigned(blocks), block, 0, st>>>(a); break;
-    default: ans_rms_norm_kernel<TX, TO, 5><<<unsigned(blocks), block, 0, st>>>(a); break;
-  }
-  ANSB_CUDA(cudaGetLastError());
-  return ANS_OK;
+  if (a.rows > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(a.rows));
+  auto threads = [&](uint32_t v) { return dim3(((vectors + v - 1) / v + 31) / 32 * 32); };
+  // Few rows: as many threads as a row has vectors; many: as many loads a thread as registers hold.
+  if (vectors <= 1024 && a.rows <= 2ull * sms) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 1024>, grid, threads(1), 0, st, 1, a);
+  if (vectors <= 512 * kWide) return ten::launch(ans_rms_norm_kernel<TX, TO, kWide, 512>, grid, threads(kWide), 0, st, 1, a);
+  if (vectors <= 2048) return ten::launch(ans_rms_norm_kernel<TX, TO, 4, 512>, grid, threads(4), 0, st, 1, a);
+  return ten::launch(ans_rms_norm_kernel<TX, TO, 8, 576>, grid, threads(8), 0, st, 1, a);
 }
 
 template <typename TX>
-static int launch_norm_out(const NormArgs& a, int out_dtype, cudaStream_t st) {
-  if (out_dtype == ANS_E4M3) return launch_norm<TX, __nv_fp8_e4m3>(a, st);
-  if (out_dtype == ANS_F32) return launch_norm<TX, float>(a, st);
-  return launch_norm<TX, __nv_bfloat16>(a, st);
+static int launch_norm_out(const NormArgs& a, int out_dtype, int sms, cudaStream_t st) {
+  if (out_dtype == ANS_E4M3) return launch_norm<TX, __nv_fp8_e4m3>(a, sms, st);
+  if (out_dtype == ANS_F32) return launch_norm<TX, float>(a, sms, st);
+  return launch_norm<TX, __nv_bfloat16>(a, sms, st);
 }
 
 }  // namespace ansb
@@ -262,8 +329,12 @@ ANS_EXPORT int ans_rms_norm(const ans_norm_desc* h_desc, void* stream) {
   a.rows = d.rows; a.width = d.width; a.eps = d.eps;
   a.x_stride = d.x_stride; a.r_stride = d.residual_stride; a.out_stride = d.out_stride; a.sum_stride = d.sum_stride;
   a.together = same(d.d_residual, xs, d.residual_stride) && same(d.d_out, os, d.out_stride) && same(d.d_sum, xs, d.sum_stride);
+  a.shift = a.together && (at || (d.rows > 1 && d.x_stride % 8)) ? 7u : 0u;
   a.w_f32 = d.weight_dtype == ANS_F32;
   a.w_vec = !(reinterpret_cast<uintptr_t>(d.d_weight) & 15);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return d.x_dtype == ANS_F32 ? launch_norm_out<float>(a, d.out_dtype, st) : launch_norm_out<__nv_bfloat16>(a, d.out_dtype, st);
+  int dev = 0, sms = 0;
+  ANSB_CUDA(cudaGetDevice(&dev));
+  ANSB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  return d.x_dtype == ANS_F32 ? launch_norm_out<float>(a, d.out_dtype, sms, st) : launch_norm_out<__nv_bfloat16>(a, d.out_dtype, sms, st);
 }

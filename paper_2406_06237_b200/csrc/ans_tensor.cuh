@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
+#include <utility>
+
 #include "ans_common.cuh"
 
 namespace ansb {
@@ -13,6 +15,31 @@ constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+
+// ---- launches that overlap their ends ------------------------------------------------------
+// Every kernel lets the next one on its stream be set up while it runs, and touches no global memory
+// before the work queued ahead of it is complete.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+inline int launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, uint32_t cluster, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+  return e == cudaSuccess ? ANS_OK : cuda_fail(e);
 }
 
 // ---- mbarriers ---------------------------------------------------------------------------
@@ -47,9 +74,9 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t
   for (;;) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        : "=r"(done) : "r"(bar), "r"(parity), "r"(20000u) : "memory");   // asleep for up to 20 us
     if (done) return true;
     if (bad || clock64() - t0 > 200000000ll) { bad = 1; return false; }
   }
@@ -94,25 +121,25 @@ template <bool F8>
 __host__ __device__ constexpr uint32_t instruction(uint32_t m, uint32_t n) {
   return (1u << 4) | (F8 ? 0u : (1u << 7) | (1u << 10)) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
-template <uint32_t CG, bool F8>
+// D += A B.  REUSE: 0: A is read for this instruction alone; 1: and kept for the next one; 2: the kept A is used, the last time
+#define ANSB_MMA(GROUP, KIND, COLLECT)                                                                    \
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"                                          \
+               "tcgen05.mma.cta_group::" GROUP ".kind::" KIND COLLECT " [%0], %1, %2, %3, p;\n\t}"        \
+               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory")
+template <uint32_t CG, bool F8, int REUSE = 0>
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (CG == 1 && !F8)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-  else if constexpr (CG == 1 && F8)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-  else if constexpr (CG == 2 && !F8)
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-  else
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+  if constexpr (CG == 1) {
+    static_assert(REUSE == 0, "");
+    if constexpr (F8) ANSB_MMA("1", "f8f6f4", ""); else ANSB_MMA("1", "f16", "");
+  } else if constexpr (REUSE == 0) {
+    if constexpr (F8) ANSB_MMA("2", "f8f6f4", ""); else ANSB_MMA("2", "f16", "");
+  } else if constexpr (REUSE == 1) {
+    if constexpr (F8) ANSB_MMA("2", "f8f6f4", ".collector::a::fill"); else ANSB_MMA("2", "f16", ".collector::a::fill");
+  } else {
+    if constexpr (F8) ANSB_MMA("2", "f8f6f4", ".collector::a::lastuse"); else ANSB_MMA("2", "f16", ".collector::a::lastuse");
+  }
 }
+#undef ANSB_MMA
 // arrive on `bar` (CG = 2: on it in both CTAs of the pair) when the matrix instructions issued so far are done
 template <uint32_t CG>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
