@@ -2,10 +2,10 @@
 //
 // Per group of values of one (token, head), L = 2^b - 1, u = 1 / L, lo = min(x, 0), hi = max(x, 0):
 //   scale = max(hi * u - lo * u, 2^-126),  zero = rint(-lo / scale),  code = clamp(rint(x / scale) + zero, 0, L)
-// and back  scale * (code - zero).  Divisions are IEEE divisions, so codes are a function of the
+// and back  scale * (code - zero).  The results are those of IEEE divisions, so codes are a function of the
 // values alone and equal on every device and in any IEEE restatement.
 //
-// Both directions are bound by memory: eight values a thread, 16 bytes of bf16.
+// Both directions are bound by memory.  Writing takes eight values a thread (16 bytes of bf16), reading sixteen.
 #include <cmath>
 #include <initializer_list>
 
@@ -34,6 +34,7 @@ struct WriteArgs {
 // LANES (a power of two) lanes per group, eight values each, lanes past group / 8 idle.  blockIdx.y: keys or values.
 template <typename T, int BITS, int LANES>
 __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a) {
+  ten::let_next_start();
   const uint32_t which = blockIdx.y;
   const uint32_t lane = threadIdx.x % LANES;
   const uint32_t per_head = a.c.head_dim / a.c.group, per_token = a.c.heads * per_head;
@@ -41,6 +42,7 @@ __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a)
   const uint64_t token = unit / per_token;
   const uint32_t in_token = static_cast<uint32_t>(unit - token * per_token);
   int64_t slot = -1;
+  ten::wait_for_previous();
   if (token < a.tokens) {
     slot = a.slot[token];
     if (slot >= 0 && static_cast<uint64_t>(slot) >= a.c.slots) {
@@ -92,10 +94,18 @@ __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a)
   const uint64_t param = (uint64_t(slot) * a.c.heads + head) * per_head + g;
   float scale = fmaxf(hi * (1.f / L) - lo * (1.f / L), 1.17549435e-38f);
   float zero = fminf(rintf(-lo / scale), L);
+  const float inverse = 1.f / scale;
   uint32_t code[8];
   if (hi < INFINITY) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = static_cast<uint32_t>(fminf(fmaxf(rintf(v[i] / scale) + zero, 0.f), L));
+    for (int i = 0; i < 8; ++i) {
+      // v * (1 / scale) is within 2^-14 of v / scale, whose magnitude is at most 255: only near a tie between two codes
+      // is the division itself needed
+      const float q = v[i] * inverse;
+      float n = rintf(q);
+      if (fabsf(fabsf(q - n) - 0.5f) < 0.0001f) n = rintf(v[i] / scale);
+      code[i] = static_cast<uint32_t>(fminf(fmaxf(n + zero, 0.f), L));
+    }
   } else {
     scale = __uint_as_float(0x7FC00000u);
     zero = 0.f;
@@ -132,88 +142,136 @@ struct ReadArgs {
   uint32_t* status;
 };
 
-constexpr uint32_t kReadRows = 16;
+constexpr uint32_t kReadRows = 64;    // rows of a block at most
 
 // scale * (code - zero).  The ends of a group's range lie up to half a step outside its values, so that with
 // values near the type's largest the product can pass it: such a result is that largest value.  A NaN stays.
+// raised: 2^23 + code as a float; below: 2^23 + zero.  Their difference is exact.
 template <typename T>
-__device__ __forceinline__ float value_of(uint32_t code, int zero, float scale) {
-  const float v = scale * static_cast<float>(static_cast<int>(code) - zero);
+__device__ __forceinline__ float value_of(uint32_t raised, float below, float scale) {
+  const float v = scale * (__uint_as_float(raised) - below);
   const float most = __uint_as_float(sizeof(T) == 2 ? 0x7F7F0000u : 0x7F7FFFFFu);
   float r;
   asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(most));   // the smaller magnitude, v's sign
   return r;
 }
 
-// A block reads kReadRows output rows of keys or of values (blockIdx.y): first their slots, then eight values a thread.
+// The last s in 0 .. n - 1 with starts[s] <= row (0 if there is none): a warp looks at 32 places at a time.
+__device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t n, int64_t row, uint32_t lane) {
+  uint32_t lo = 0, hi = n;                                // the answer lies in [lo, hi)
+  while (hi - lo > 1) {
+    const uint32_t step = (hi - lo + 31u) / 32u, at = lo + lane * step;
+    const uint32_t below = __ballot_sync(ten::kAll, at < hi && static_cast<int64_t>(starts[at]) <= row);
+    const uint32_t last = below ? 31u - __clz(below) : 0u;
+    lo += last * step;
+    hi = min(hi, lo + step);
+  }
+  return lo;
+}
+
+// A block reads `some` output rows of keys or of values (blockIdx.y).  First the slots of its rows: two warps find the
+// sequences of the first and the last row, between which, most often nowhere, the others' lie.  Then
+// sixteen values a thread, four of them under way at a time.
 template <typename T, int BITS>
-__global__ void __launch_bounds__(256) ans_cache_read_kernel(const ReadArgs a) {
+__global__ void __launch_bounds__(256) ans_cache_read_kernel(const ReadArgs a, const uint32_t some) {
   __shared__ int64_t s_slot[kReadRows];                   // -1: zeros, -2: not written
-  const uint32_t which = blockIdx.y;
-  const uint64_t row0 = uint64_t(blockIdx.x) * kReadRows;
-  if (threadIdx.x < kReadRows) {
-    const uint64_t row = row0 + threadIdx.x;
+  __shared__ uint32_t s_seq[2];
+  ten::let_next_start();
+  const uint32_t which = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  const uint64_t row0 = uint64_t(blockIdx.x) * some;
+  ten::wait_for_previous();
+  const int64_t last = min(static_cast<int64_t>(a.starts[a.n_seqs]), static_cast<int64_t>(a.rows));   // rows to write
+  if (warp < 2) {
+    const uint32_t s = sequence_of(a.starts, a.n_seqs, static_cast<int64_t>(row0) + (warp ? some - 1 : 0), lane);
+    if (lane == 0) s_seq[warp] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < some) {
+    const int64_t row = static_cast<int64_t>(row0 + threadIdx.x);
     int64_t slot = -2;
-    const int32_t last = a.starts[a.n_seqs];
-    if (last > 0 && static_cast<uint64_t>(last) > a.rows && row == 0 && which == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-    if (row < a.rows && static_cast<int64_t>(row) < last) {
-      uint32_t lo = 0, hi = a.n_seqs;                     // the last s with starts[s] <= row
+    if (row < last) {
+      uint32_t lo = s_seq[0], hi = max(s_seq[0], s_seq[1]) + 1;
       while (hi - lo > 1) {
         const uint32_t mid = (lo + hi) / 2;
-        if (static_cast<int64_t>(a.starts[mid]) <= static_cast<int64_t>(row)) lo = mid; else hi = mid;
+        if (static_cast<int64_t>(a.starts[mid]) <= row) lo = mid; else hi = mid;
       }
-      const int64_t pos = static_cast<int64_t>(row) - a.starts[lo];
+      const int64_t pos = row - a.starts[lo];
       slot = -1;
-      if (pos >= 0 && static_cast<uint64_t>(pos) / a.c.page_size < a.table_pages) {
-        const uint64_t in = static_cast<uint64_t>(pos) / a.c.page_size;
-        const int32_t page = a.tables[lo * a.table_stride + in];
-        if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages)
-          slot = int64_t(page) * a.c.page_size + (pos - int64_t(in) * a.c.page_size);
+      if (pos >= 0) {
+        const uint32_t in = static_cast<uint32_t>(pos) / a.c.page_size;
+        if (in < a.table_pages) {
+          const int32_t page = a.tables[lo * a.table_stride + in];
+          if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages)
+            slot = int64_t(page) * a.c.page_size + (static_cast<uint32_t>(pos) - in * a.c.page_size);
+        }
       }
       if (slot < 0 && which == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
     }
+    if (row == 0 && which == 0 && static_cast<int64_t>(a.starts[a.n_seqs]) > static_cast<int64_t>(a.rows)) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
     s_slot[threadIdx.x] = slot;
   }
   __syncthreads();
-  const uint32_t width = a.c.heads * a.c.head_dim, eights = width / 8u;
-  for (uint32_t i = threadIdx.x; i < kReadRows * eights; i += 256u) {
-    const uint32_t r = i / eights, e = (i - r * eights) * 8u;
-    const int64_t slot = s_slot[r];
-    if (slot == -2) break;
-    float v[8];
-    if (slot >= 0) {
-      const uint64_t at = uint64_t(slot) * width + e, param = uint64_t(slot) * (width / a.c.group) + e / a.c.group;
-      const float scale = a.c.scales[which][param];
-      const int zero = a.c.zeros[which][param];
-      if constexpr (BITS == 8) {
-        const uint2 w = *reinterpret_cast<const uint2*>(a.c.codes[which] + at);
+  const uint32_t width = a.c.heads * a.c.head_dim, units = width / 16u, per_row = width / a.c.group;
+  constexpr uint32_t kAhead = 4;
+  for (uint32_t i0 = threadIdx.x; i0 < some * units; i0 += 256u * kAhead) {
+    uint32_t w[kAhead][BITS / 2];
+    float scale[kAhead];
+    uint32_t zero[kAhead];
+    int64_t slot[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[j] = value_of<T>((w.x >> (8 * j)) & 255u, zero, scale);
-          v[4 + j] = value_of<T>((w.y >> (8 * j)) & 255u, zero, scale);
+    for (uint32_t j = 0; j < kAhead; ++j) {
+      const uint32_t i = i0 + j * 256u;
+      slot[j] = -2;
+      if (i < some * units) {
+        const uint32_t r = i / units, e = (i - r * units) * 16u;
+        slot[j] = s_slot[r];
+        if (slot[j] >= 0) {
+          const uint64_t at = uint64_t(slot[j]) * width + e, param = uint64_t(slot[j]) * per_row + e / a.c.group;
+          if constexpr (BITS == 8) {
+            const uint4 u = *reinterpret_cast<const uint4*>(a.c.codes[which] + at);
+            w[j][0] = u.x; w[j][1] = u.y; w[j][2] = u.z; w[j][3] = u.w;
+          } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(a.c.codes[which] + at / 2);
+            w[j][0] = u.x; w[j][1] = u.y;
+          }
+          scale[j] = *(a.c.scales[which] + param);
+          zero[j] = *(a.c.zeros[which] + param);
+        }
+      }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kAhead; ++j) {
+      if (slot[j] == -2) continue;
+      const uint32_t i = i0 + j * 256u, r = i / units, e = (i - r * units) * 16u;
+      float v[16];
+      if (slot[j] >= 0) {
+        const float below = 8388608.f + static_cast<float>(zero[j]);
+#pragma unroll
+        for (uint32_t n = 0; n < 16; ++n) {
+          const uint32_t raised = BITS == 8 ? __byte_perm(w[j][n / 4], 0x4B000000u, 0x7540u + n % 4)
+                                            : ((w[j][n / 8] >> (4 * (n % 8))) & 15u) | 0x4B000000u;
+          v[n] = value_of<T>(raised, below, scale[j]);
         }
       } else {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(a.c.codes[which] + at / 2);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = value_of<T>((w >> (4 * j)) & 15u, zero, scale);
+        for (uint32_t n = 0; n < 16; ++n) v[n] = 0.f;
       }
-    } else {
+      const uint64_t to = (row0 + r) * width + e;
+      if constexpr (sizeof(T) == 2) {
+        uint32_t o[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-    }
-    const uint64_t to = (row0 + r) * width + e;
-    if constexpr (sizeof(T) == 2) {
-      uint32_t w[4];
+        for (uint32_t n = 0; n < 8; ++n) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * n], v[2 * n + 1]);
+          o[n] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        uint4* p = reinterpret_cast<uint4*>(static_cast<T*>(a.out[which]) + to);
+        p[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        p[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      } else {
+        float4* p = reinterpret_cast<float4*>(static_cast<T*>(a.out[which]) + to);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-        w[j] = *reinterpret_cast<const uint32_t*>(&b);
+        for (uint32_t n = 0; n < 4; ++n) p[n] = make_float4(v[4 * n], v[4 * n + 1], v[4 * n + 2], v[4 * n + 3]);
       }
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.out[which]) + to) = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-      float4* f = reinterpret_cast<float4*>(static_cast<T*>(a.out[which]) + to);
-      f[0] = make_float4(v[0], v[1], v[2], v[3]);
-      f[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
   }
 }
@@ -244,14 +302,12 @@ static int launch_write(const WriteArgs& a, cudaStream_t st) {
   if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(blocks), 2);
   switch (lanes) {
-    case 2: ans_cache_write_kernel<T, BITS, 2><<<grid, 256, 0, st>>>(a); break;
-    case 4: ans_cache_write_kernel<T, BITS, 4><<<grid, 256, 0, st>>>(a); break;
-    case 8: ans_cache_write_kernel<T, BITS, 8><<<grid, 256, 0, st>>>(a); break;
-    case 16: ans_cache_write_kernel<T, BITS, 16><<<grid, 256, 0, st>>>(a); break;
-    default: ans_cache_write_kernel<T, BITS, 32><<<grid, 256, 0, st>>>(a); break;
+    case 2: return ten::launch(ans_cache_write_kernel<T, BITS, 2>, grid, dim3(256), 0, st, 1, a);
+    case 4: return ten::launch(ans_cache_write_kernel<T, BITS, 4>, grid, dim3(256), 0, st, 1, a);
+    case 8: return ten::launch(ans_cache_write_kernel<T, BITS, 8>, grid, dim3(256), 0, st, 1, a);
+    case 16: return ten::launch(ans_cache_write_kernel<T, BITS, 16>, grid, dim3(256), 0, st, 1, a);
+    default: return ten::launch(ans_cache_write_kernel<T, BITS, 32>, grid, dim3(256), 0, st, 1, a);
   }
-  ANSB_CUDA(cudaGetLastError());
-  return ANS_OK;
 }
 
 }  // namespace ansb
@@ -303,14 +359,16 @@ ANS_EXPORT int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tab
   a.tables = d_tables; a.table_stride = table_stride; a.table_pages = table_pages; a.starts = d_starts; a.n_seqs = n_seqs; a.rows = rows;
   a.out[0] = d_k_out; a.out[1] = d_v_out; a.status = d_status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 grid(static_cast<unsigned>((rows + kReadRows - 1) / kReadRows), 2);
-  if (out_dtype == ANS_BF16) {
-    if (h_desc->bitwidth == 8) ans_cache_read_kernel<__nv_bfloat16, 8><<<grid, 256, 0, st>>>(a);
-    else ans_cache_read_kernel<__nv_bfloat16, 4><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (h_desc->bitwidth == 8) ans_cache_read_kernel<float, 8><<<grid, 256, 0, st>>>(a);
-    else ans_cache_read_kernel<float, 4><<<grid, 256, 0, st>>>(a);
-  }
-  ANSB_CUDA(cudaGetLastError());
-  return ANS_OK;
+  // rows of a block: enough blocks for eight on each SM, up to 64 rows each, over which a block's look-up is spread
+  int dev = 0, sms = 0;
+  ANSB_CUDA(cudaGetDevice(&dev));
+  ANSB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const uint64_t share = rows / (4u * static_cast<uint64_t>(sms));
+  const uint32_t some = share < 4 ? 4u : share > kReadRows ? kReadRows : static_cast<uint32_t>(share);
+  const dim3 grid(static_cast<unsigned>((rows + some - 1) / some), 2);
+  if (out_dtype == ANS_BF16)
+    return h_desc->bitwidth == 8 ? ten::launch(ans_cache_read_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, st, 1, a, some)
+                                 : ten::launch(ans_cache_read_kernel<__nv_bfloat16, 4>, grid, dim3(256), 0, st, 1, a, some);
+  return h_desc->bitwidth == 8 ? ten::launch(ans_cache_read_kernel<float, 8>, grid, dim3(256), 0, st, 1, a, some)
+                               : ten::launch(ans_cache_read_kernel<float, 4>, grid, dim3(256), 0, st, 1, a, some);
 }
