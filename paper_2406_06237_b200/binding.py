@@ -354,21 +354,28 @@ def ans_decode_gemm_bf16(h_desc: ans_layer_desc, d_x: int, M: int, N: int, K: in
 
 
 def ans_rms_norm(h_desc: ans_norm_desc, stream: int = 0) -> None:
-    _check(lib().ans_rms_norm(h_desc, stream), "ans_rms_norm")
+    rc = (_LIB or lib()).ans_rms_norm(h_desc, stream)
+    if rc:
+        _check(rc, "ans_rms_norm")
 
 
 def ans_product(h_desc: ans_product_desc, d_status: int, stream: int = 0) -> None:
-    _check(lib().ans_product(h_desc, d_status, stream), "ans_product")
+    rc = (_LIB or lib()).ans_product(h_desc, d_status, stream)
+    if rc:
+        _check(rc, "ans_product")
 
 
 def ans_cache_write(h_desc: ans_cache_desc, d_k: int, d_v: int, dtype: int, tokens: int, k_strides, v_strides,
                     d_slots: int, d_status: int, stream: int = 0) -> None:
     """k_strides, v_strides: (token stride, head stride) in elements."""
-    _check(lib().ans_cache_write(h_desc, d_k, d_v, dtype, tokens, k_strides[0], k_strides[1], v_strides[0], v_strides[1],
-                                 d_slots, d_status, stream), "ans_cache_write")
+    rc = (_LIB or lib()).ans_cache_write(h_desc, d_k, d_v, dtype, tokens, *k_strides, *v_strides, d_slots, d_status, stream)
+    if rc:
+        _check(rc, "ans_cache_write")
 
 
 def ans_cache_read(h_desc: ans_cache_desc, d_tables: int, table_stride: int, table_pages: int, n_seqs: int, d_starts: int,
                    rows: int, d_k_out: int, d_v_out: int, out_dtype: int, d_status: int, stream: int = 0) -> None:
-    _check(lib().ans_cache_read(h_desc, d_tables, table_stride, table_pages, n_seqs, d_starts, rows, d_k_out, d_v_out,
-                                out_dtype, d_status, stream), "ans_cache_read")
+    rc = (_LIB or lib()).ans_cache_read(h_desc, d_tables, table_stride, table_pages, n_seqs, d_starts, rows, d_k_out, d_v_out,
+                                        out_dtype, d_status, stream)
+    if rc:
+        _check(rc, "ans_cache_read")

@@ -28,8 +28,16 @@ def _cuda_device(device) -> torch.device:
     return torch.device("cuda", torch.cuda.current_device() if d.index is None else d.index)
 
 
+# the current device and its current stream, as plain numbers
+_current_device = torch._C._cuda_getDevice
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
 class _Handle:
-    """A device, and the status word its calls report to."""
+    """A device, and the status word its calls report to.
+
+    A call checks its tensors' types, shapes, strides and devices; where all of them are those of the
+    handle's last call the checks' result is known and only the pointers change."""
 
     def __init__(self, device):
         self.device = _cuda_device(device)
@@ -39,13 +47,18 @@ class _Handle:
 
     def _enter(self) -> int:
         """The current stream; the library launches on the current device."""
-        if torch.cuda.current_device() != self._index:
+        if _current_device() != self._index:
             raise RuntimeError(f"the handle is on {self.device}, which is not the current device")
-        return torch.cuda.current_stream(self._index).cuda_stream
+        return _current_stream(self._index)
 
     def read_status(self) -> int:
         """Waits for the stream; ANS_STATUS_* bits that calls have set since the last look (0: all sound)."""
         return B.ans_read_status(self._status, self._enter())
+
+
+def _form(t: torch.Tensor | None):
+    """All of a tensor that checks look at."""
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.device)
 
 
 def _rows(t: torch.Tensor, what: str) -> int:
@@ -73,6 +86,8 @@ class RmsNorm(_Handle):
             _need(weight.dim() == 1 and weight.is_contiguous(), "weight must be a contiguous vector")
             _need(weight.dtype in (torch.bfloat16, torch.float32), "weight must be bf16 or fp32")
         self.weight, self.eps, self.out_dtype = weight, float(eps), out_dtype
+        self._8bit = out_dtype is torch.float8_e4m3fn
+        self._last = None
         self._desc = d = B.ans_norm_desc()
         d.d_weight = weight.data_ptr() if weight is not None and weight.numel() else None
         d.weight_dtype = _ELEMENT[weight.dtype] if weight is not None else B.ANS_F32
@@ -84,43 +99,58 @@ class RmsNorm(_Handle):
         ([rows] fp32) only with an 8-bit output, summed (x + residual in x's type) only with a residual;
         None otherwise.  Buffers given for them are written and returned; summed may be x or residual."""
         st, d = self._enter(), self._desc
+        if out is None or (scales is None and self._8bit) or (summed is None and residual is not None):
+            out, scales, summed = self._buffers(x, residual, out, scales, summed)
+        form = (_form(x), _form(residual), _form(out), _form(scales), _form(summed))
+        if form != self._last:
+            self._last = None
+            self._check(x, residual, out, scales, summed)
+            self._last = form
+        d.d_x, d.d_out = x.data_ptr(), out.data_ptr()
+        if scales is not None:
+            d.d_scales = scales.data_ptr()
+        if residual is not None:
+            d.d_residual, d.d_sum = residual.data_ptr(), summed.data_ptr()
+        B.ans_rms_norm(d, st)
+        return out, scales, summed
+
+    def _buffers(self, x, residual, out, scales, summed):
+        _need(x.dim() == 2, "x must be a matrix")
+        _on_device(x, self.device, "x")
+        if out is None:
+            out = torch.empty(x.shape, dtype=self.out_dtype, device=self.device)
+        if scales is None and self._8bit:
+            scales = torch.empty(x.shape[0], dtype=torch.float32, device=self.device)
+        if summed is None and residual is not None:
+            summed = torch.empty(x.shape, dtype=x.dtype, device=self.device)
+        return out, scales, summed
+
+    def _check(self, x, residual, out, scales, summed):
+        """Checks one call's tensors and writes all but their places into the descriptor."""
+        d, dt = self._desc, x.dtype
         xs = _rows(x, "x")
         rows, width = x.shape
-        dt = x.dtype
-        _need(dt is torch.bfloat16 or dt is torch.float32, "x must be bf16 or fp32")
+        _need(dt in (torch.bfloat16, torch.float32), "x must be bf16 or fp32")
         _on_device(x, self.device, "x")
         _need(self.weight is None or self.weight.shape[0] == width, "weight and x differ in width")
-        if out is None:
-            out = torch.empty(rows, width, dtype=self.out_dtype, device=self.device)
-        else:
-            _need(out.dtype is self.out_dtype and out.shape == x.shape, "out has the wrong type or shape")
-            _on_device(out, self.device, "out")
-        if self.out_dtype is torch.float8_e4m3fn:
-            if scales is None:
-                scales = torch.empty(rows, dtype=torch.float32, device=self.device)
-            else:
-                _need(scales.dtype is torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales must be fp32 [rows]")
-                _on_device(scales, self.device, "scales")
-            d.d_scales = scales.data_ptr()
+        _need(out.dtype is self.out_dtype and out.shape == x.shape, "out has the wrong type or shape")
+        _on_device(out, self.device, "out")
+        if self._8bit:
+            _need(scales.dtype is torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales must be fp32 [rows]")
+            _on_device(scales, self.device, "scales")
         else:
             _need(scales is None, "scales belong to an 8-bit output")
         if residual is not None:
             _need(residual.dtype is dt and residual.shape == x.shape, "residual and x differ")
             _on_device(residual, self.device, "residual")
-            if summed is None:
-                summed = torch.empty(rows, width, dtype=dt, device=self.device)
-            else:
-                _need(summed.dtype is dt and summed.shape == x.shape, "summed has the wrong type or shape")
-                _on_device(summed, self.device, "summed")
-            d.d_residual, d.residual_stride = residual.data_ptr(), _rows(residual, "residual")
-            d.d_sum, d.sum_stride = summed.data_ptr(), _rows(summed, "summed")
+            _need(summed.dtype is dt and summed.shape == x.shape, "summed has the wrong type or shape")
+            _on_device(summed, self.device, "summed")
+            d.residual_stride, d.sum_stride = _rows(residual, "residual"), _rows(summed, "summed")
         else:
             _need(summed is None, "summed belongs to a residual")
             d.d_residual = d.d_sum = None
-        d.d_x, d.x_stride, d.x_dtype, d.rows, d.width = x.data_ptr(), xs, _ELEMENT[dt], rows, width
-        d.d_out, d.out_stride = out.data_ptr(), _rows(out, "out")
-        B.ans_rms_norm(d, st)
-        return out, scales, summed
+        d.x_stride, d.x_dtype, d.rows, d.width = xs, _ELEMENT[dt], rows, width
+        d.out_stride = _rows(out, "out")
 
 
 def symbols_to_e4m3(symbols: torch.Tensor, zero_point: int) -> torch.Tensor:
@@ -134,12 +164,17 @@ def symbols_to_e4m3(symbols: torch.Tensor, zero_point: int) -> torch.Tensor:
     return table.clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).to(symbols.device)[symbols.long()].view(torch.float8_e4m3fn)
 
 
+def _fits(t: torch.Tensor) -> bool:
+    """Whether rows are contiguous and, if the first one does, start on 16 bytes."""
+    (rows, width), (stride, one) = t.shape, t.stride()
+    return (one == 1 or width <= 1) and (rows <= 1 or stride >= width and stride * t.element_size() % 16 == 0)
+
+
 def _aligned(t: torch.Tensor) -> torch.Tensor:
     """t, or a copy of it, with contiguous rows that start on 16 bytes."""
-    size = t.element_size()
-    if t.data_ptr() % 16 == 0 and (t.stride(1) == 1 or t.shape[1] <= 1) and (t.shape[0] <= 1 or t.stride(0) * size % 16 == 0 and t.stride(0) >= t.shape[1]):
+    if t.data_ptr() % 16 == 0 and _fits(t):
         return t
-    pad = 16 // size
+    pad = 16 // t.element_size()
     room = torch.empty(t.shape[0], (t.shape[1] + pad - 1) // pad * pad, dtype=t.dtype, device=t.device)
     room = room[:, :t.shape[1]]
     room.copy_(t)
@@ -170,6 +205,7 @@ class Linear(_Handle):
             bias = bias.to(device=self.device, dtype=torch.float32).contiguous()
         self.scales, self.bias, self.activation = scales, bias, activation
         self.in_features, self.out_features = k, n
+        self._last, self._copies = None, False
         self._desc = d = B.ans_product_desc()
         d.d_w, d.w_stride = self.weight.data_ptr() or None, max(self.weight.stride(0), k)
         d.d_w_scales = scales.data_ptr() if scales is not None else None
@@ -182,35 +218,48 @@ class Linear(_Handle):
         [rows, out features]), the given buffer if there is one; residual is of its type and may be out
         itself.  An x whose rows do not start on 16 bytes is copied first."""
         st, d = self._enter(), self._desc
+        if out is None:
+            _need(x.dim() == 2, "x must be [rows, in features]")
+            out = torch.empty(x.shape[0], self.out_features, dtype=out_dtype, device=self.device)
+        form = (_form(x), _form(x_scales), _form(residual), _form(out))
+        if form != self._last:
+            self._last = None
+            self._check(x, x_scales, residual, out)
+            self._last = form
+        at = x.data_ptr()
+        if at % 16 or self._copies:
+            x = _aligned(x)
+            at, d.x_stride = x.data_ptr(), max(x.stride(0), self.in_features)
+            self._last = None
+        d.d_x, d.d_y = at, out.data_ptr()
+        if x_scales is not None:
+            d.d_x_scales = x_scales.data_ptr()
+        if residual is not None:
+            d.d_residual = residual.data_ptr()
+        B.ans_product(d, self._status, st)
+        return out
+
+    def _check(self, x, x_scales, residual, out):
+        """Checks one call's tensors and writes all but their places into the descriptor."""
+        d, dt = self._desc, out.dtype
         _need(x.dim() == 2 and x.shape[1] == self.in_features, "x must be [rows, in features]")
         _need(x.dtype is self.weight.dtype, f"x is {x.dtype}, the weight {self.weight.dtype}")
         _on_device(x, self.device, "x")
-        rows = x.shape[0]
-        x = _aligned(x)
-        shape = (rows, self.out_features)
-        if out is None:
-            out = torch.empty(shape, dtype=out_dtype, device=self.device)
-        else:
-            _need(out.shape == shape, "out has the wrong shape")
-            _on_device(out, self.device, "out")
-        dt = out.dtype
-        _need(dt is torch.bfloat16 or dt is torch.float32, "the output is bf16 or fp32")
+        shape = (x.shape[0], self.out_features)
+        _need(out.shape == shape, "out has the wrong shape")
+        _need(dt in (torch.bfloat16, torch.float32), "the output is bf16 or fp32")
+        _on_device(out, self.device, "out")
+        d.d_x_scales = d.d_residual = None
         if x_scales is not None:
-            _need(x_scales.dtype is torch.float32 and x_scales.shape == (rows,) and x_scales.is_contiguous(), "x_scales must be fp32 [rows]")
+            _need(x_scales.dtype is torch.float32 and x_scales.shape == shape[:1] and x_scales.is_contiguous(), "x_scales must be fp32 [rows]")
             _on_device(x_scales, self.device, "x_scales")
-            d.d_x_scales = x_scales.data_ptr()
-        else:
-            d.d_x_scales = None
         if residual is not None:
             _need(residual.dtype is dt and residual.shape == shape, "residual and out differ")
             _on_device(residual, self.device, "residual")
-            d.d_residual, d.residual_stride = residual.data_ptr(), _rows(residual, "residual")
-        else:
-            d.d_residual = None
-        d.d_x, d.x_stride, d.m = x.data_ptr(), max(x.stride(0), self.in_features), rows
-        d.d_y, d.y_stride, d.y_dtype = out.data_ptr(), _rows(out, "out"), _ELEMENT[dt]
-        B.ans_product(d, self._status, st)
-        return out
+            d.residual_stride = _rows(residual, "residual")
+        self._copies = not _fits(x)
+        d.x_stride, d.m = max(x.stride(0), self.in_features), shape[0]
+        d.y_stride, d.y_dtype = _rows(out, "out"), _ELEMENT[dt]
 
 
 class PagedCache(_Handle):
@@ -258,29 +307,38 @@ class PagedCache(_Handle):
         self.v_codes, self.v_scales, self.v_zeros = v_codes, v_scales, v_zeros
         self.n_pages, self.page_size, self.heads = k_codes.shape[:3]
         self.head_dim, self.group, self.bitwidth = dim, dim // groups, bitwidth
+        self._wrote = self._read = None
         self._desc = d = B.ans_cache_desc()
         d.d_k_codes, d.d_k_scales, d.d_k_zeros = k_codes.data_ptr(), k_scales.data_ptr(), k_zeros.data_ptr()
         d.d_v_codes, d.d_v_scales, d.d_v_zeros = v_codes.data_ptr(), v_scales.data_ptr(), v_zeros.data_ptr()
         d.n_pages, d.page_size, d.heads, d.head_dim = self.n_pages, self.page_size, self.heads, dim
         d.group, d.bitwidth = self.group, bitwidth
 
-    def _strides(self, t: torch.Tensor, what: str):
-        _need(t.dim() == 3 and t.shape[1:] == (self.heads, self.head_dim), f"{what} must be [tokens, heads, head_dim]")
-        _need(t.stride(2) == 1, f"the values of a head of {what} must be contiguous")
-        _on_device(t, self.device, what)
-        return t.stride(0), t.stride(1)
-
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """k, v: [tokens, heads, head_dim], bf16 or fp32, tokens and heads at any stride; slots: [tokens]
         int64, a negative one skips its token."""
         st = self._enter()
-        ks, vs = self._strides(k, "k"), self._strides(v, "v")
+        form = (_form(k), _form(v), _form(slots))
+        if form != self._wrote:
+            self._wrote = None
+            self._check_write(k, v, slots)
+            self._wrote = form
+        B.ans_cache_write(self._desc, k.data_ptr(), v.data_ptr(), *self._write_args, slots.data_ptr(), self._status, st)
+
+    def _check_write(self, k, v, slots):
+        def strides(t, what):
+            _need(t.dim() == 3 and t.shape[1:] == (self.heads, self.head_dim), f"{what} must be [tokens, heads, head_dim]")
+            _need(t.stride(2) == 1, f"the values of a head of {what} must be contiguous")
+            _on_device(t, self.device, what)
+            return t.stride()[:2]
+
+        ks, vs = strides(k, "k"), strides(v, "v")
         dt, tokens = k.dtype, k.shape[0]
-        _need(dt is torch.bfloat16 or dt is torch.float32, "k and v must be bf16 or fp32")
+        _need(dt in (torch.bfloat16, torch.float32), "k and v must be bf16 or fp32")
         _need(v.dtype is dt and v.shape[0] == tokens, "k and v differ")
         _need(slots.dtype is torch.int64 and slots.shape == (tokens,) and slots.is_contiguous(), "slots must be int64 [tokens]")
         _on_device(slots, self.device, "slots")
-        B.ans_cache_write(self._desc, k.data_ptr(), v.data_ptr(), _ELEMENT[dt], tokens, ks, vs, slots.data_ptr(), self._status, st)
+        self._write_args = (_ELEMENT[dt], tokens, ks, vs)
 
     def read(self, tables: torch.Tensor, starts: torch.Tensor, rows: int | None = None, k_out: torch.Tensor | None = None,
              v_out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16):
@@ -289,25 +347,35 @@ class PagedCache(_Handle):
         starts[s + 1].  rows = starts[-1] as a number (the call does not read it from the device), or
         k_out and v_out of that many rows are given.  Returns (k, v)."""
         st = self._enter()
-        _need((k_out is None) == (v_out is None), "give both of k_out and v_out or none")
+        if (k_out is None) != (v_out is None):
+            raise ValueError("give both of k_out and v_out or none")
         if k_out is None:
             _need(rows is not None, "rows is needed where no buffers are given")
             k_out = torch.empty(rows, self.heads, self.head_dim, dtype=out_dtype, device=self.device)
             v_out = torch.empty_like(k_out)
-        else:
-            rows = k_out.shape[0] if rows is None else rows
-            for t in (k_out, v_out):
-                _need(t.dim() == 3 and t.shape[0] >= rows and t.shape[1:] == (self.heads, self.head_dim) and t.is_contiguous(),
-                      "k_out and v_out must be contiguous [rows, heads, head_dim]")
-                _on_device(t, self.device, "an output")
-            _need(v_out.dtype is k_out.dtype, "k_out and v_out differ")
+        form = (_form(tables), _form(starts), rows, _form(k_out), _form(v_out))
+        if form != self._read:
+            self._read = None
+            self._check_read(tables, starts, rows, k_out, v_out)
+            self._read = form
+        (stride, pages, n), (count, dtype) = self._read_args
+        B.ans_cache_read(self._desc, tables.data_ptr(), stride, pages, n, starts.data_ptr(), count, k_out.data_ptr(), v_out.data_ptr(),
+                         dtype, self._status, st)
+        return k_out, v_out
+
+    def _check_read(self, tables, starts, rows, k_out, v_out):
+        rows = k_out.shape[0] if rows is None else rows
+        for t in (k_out, v_out):
+            _need(t.dim() == 3 and t.shape[0] >= rows >= 0 and t.shape[1:] == (self.heads, self.head_dim) and t.is_contiguous(),
+                  "k_out and v_out must be contiguous [rows, heads, head_dim]")
+            _on_device(t, self.device, "an output")
         dt = k_out.dtype
-        _need(dt is torch.bfloat16 or dt is torch.float32, "the outputs are bf16 or fp32")
+        _need(v_out.dtype is dt, "k_out and v_out differ")
+        _need(dt in (torch.bfloat16, torch.float32), "the outputs are bf16 or fp32")
         _need(tables.dtype is torch.int32 and tables.dim() == 2 and (tables.stride(1) == 1 or tables.shape[1] <= 1), "tables must be int32 [sequences, pages]")
-        n = tables.shape[0]
+        n, pages = tables.shape
+        _need(n <= 1 or tables.stride(0) >= pages, "the rows of tables overlap")
         _need(starts.dtype is torch.int32 and starts.shape == (n + 1,) and starts.is_contiguous(), "starts must be int32 [sequences + 1]")
         _on_device(tables, self.device, "tables")
         _on_device(starts, self.device, "starts")
-        B.ans_cache_read(self._desc, tables.data_ptr(), tables.stride(0), tables.shape[1], n, starts.data_ptr(), rows,
-                         k_out.data_ptr(), v_out.data_ptr(), _ELEMENT[dt], self._status, st)
-        return k_out, v_out
+        self._read_args = (tables.stride(0), pages, n), (rows, _ELEMENT[dt])
