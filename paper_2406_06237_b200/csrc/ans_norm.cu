@@ -13,285 +13,530 @@
 namespace ansb {
 
 struct NormArgs {
-  const void* x; const void* r; const void* w;
-  void* out; float* scales; void* sum;
-  uint64_t rows, x_stride, r_stride, out_stride, sum_stride;
+  const char* x; const char* r; const void* w;
+  char* out; float* scales; char* sum;
+  const char* x_end; const char* r_end;        // the ends of the last rows
+  uint64_t rows;
+  uint64_t x_step, r_step, out_step, sum_step; // bytes from a row to the next
   uint32_t width;
-  float eps;
+  float eps, part;        // part: 1 / width
   uint32_t together;      // the rows of all matrices start equally far from a 16-byte boundary
   uint32_t shift;         // the most that a row starts past such a boundary, in elements
   uint32_t w_f32;         // type of w
   uint32_t w_vec;         // w on a 16-byte boundary
 };
 
-// Elements of a type one by one and eight at a time.  Eight are loaded as they lie (Raw), so that all of a
-// thread's loads are under way before the first value is used; they bypass L1, which is left to the weight.
-template <typename T> struct Elem;
-template <int N> struct Raw { uint4 q[N]; };
-template <int N>
-__device__ __forceinline__ Raw<N> load_once(const void* p) {
-  Raw<N> r;
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r.q[i].x), "=r"(r.q[i].y), "=r"(r.q[i].z), "=r"(r.q[i].w) : "l"(static_cast<const uint4*>(p) + i) : "memory");
+// ---- two floats at a time ------------------------------------------------------------------
+using Two = unsigned long long;
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
   return r;
 }
-template <> struct Elem<__nv_bfloat16> {
-  using Eight = Raw<1>;
-  static __device__ __forceinline__ float one(const void* p, uint64_t i) {
-    return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-  }
-  static __device__ __forceinline__ const void* at(const void* p, uint64_t i) { return static_cast<const __nv_bfloat16*>(p) + i; }
-  static __device__ __forceinline__ void open(const Eight& u, float (&v)[8]) {
-    const uint32_t w[4] = {u.q[0].x, u.q[0].y, u.q[0].z, u.q[0].w};
+__device__ __forceinline__ float low(Two v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float high(Two v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+__device__ __forceinline__ Two add2(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Two mul2(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// the largest magnitude, NaN above all
+__device__ __forceinline__ float larger(float top, Two v) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(top), "f"(low(v)), "f"(high(v)));
+  return r;
+}
+
+// ---- elements of a type, one by one and a vector at a time -------------------------------------
+// A vector is 16 bytes of x: E = 8 elements of bf16, 4 of fp32.
+__device__ __forceinline__ uint4 load_once(const void* p) {        // past L1, which is left to the weight
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+  return r;
+}
+__device__ __forceinline__ Two open(uint32_t w) { return two(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ void open(const uint4& u, Two (&v)[4]) {            // bf16
+  v[0] = open(u.x); v[1] = open(u.y); v[2] = open(u.z); v[3] = open(u.w);
+}
+__device__ __forceinline__ void open(const uint4& u, Two (&v)[2]) {            // fp32
+  v[0] = two(__uint_as_float(u.x), __uint_as_float(u.y));
+  v[1] = two(__uint_as_float(u.z), __uint_as_float(u.w));
+}
+template <typename T>
+__device__ __forceinline__ float one(const void* p, int i) { return static_cast<float>(static_cast<const T*>(p)[i]); }
+template <typename T>
+__device__ __forceinline__ void put1(void* p, int i, float v) {
+  if constexpr (sizeof(T) == 1) static_cast<uint8_t*>(p)[i] = static_cast<uint8_t>(__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3));
+  else if constexpr (sizeof(T) == 2) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+  else static_cast<float*>(p)[i] = v;
+}
+template <typename T, int H>
+__device__ __forceinline__ void put_all(void* p, int i, const Two (&v)[H]) {
+  if constexpr (sizeof(T) == 4) {
+    float4* f = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[2 * j] = __uint_as_float(w[j] << 16);
-      v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
-  }
-  static __device__ __forceinline__ void put(void* p, uint64_t i, float v) {
-    static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-  }
-  static __device__ __forceinline__ void put8(void* p, uint64_t i, const float (&v)[8]) {
-    uint32_t w[4];
+    for (int j = 0; j < H / 2; ++j) f[j] = make_float4(low(v[2 * j]), high(v[2 * j]), low(v[2 * j + 1]), high(v[2 * j + 1]));
+  } else if constexpr (sizeof(T) == 2) {
+    uint32_t w[H];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    for (int j = 0; j < H; ++j) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(low(v[j]), high(v[j]));
       w[j] = *reinterpret_cast<const uint32_t*>(&b);
     }
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-};
-template <> struct Elem<float> {
-  using Eight = Raw<2>;
-  static __device__ __forceinline__ float one(const void* p, uint64_t i) { return static_cast<const float*>(p)[i]; }
-  static __device__ __forceinline__ const void* at(const void* p, uint64_t i) { return static_cast<const float*>(p) + i; }
-  static __device__ __forceinline__ void open(const Eight& u, float (&v)[8]) {
+    if constexpr (H == 4) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + i) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p) + i) = make_uint2(w[0], w[1]);
+  } else {
+    uint32_t w[H / 2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      v[4 * j] = __uint_as_float(u.q[j].x);
-      v[4 * j + 1] = __uint_as_float(u.q[j].y);
-      v[4 * j + 2] = __uint_as_float(u.q[j].z);
-      v[4 * j + 3] = __uint_as_float(u.q[j].w);
-    }
-  }
-  static __device__ __forceinline__ void put(void* p, uint64_t i, float v) { static_cast<float*>(p)[i] = v; }
-  static __device__ __forceinline__ void put8(void* p, uint64_t i, const float (&v)[8]) {
-    float4* f = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
-    f[0] = make_float4(v[0], v[1], v[2], v[3]);
-    f[1] = make_float4(v[4], v[5], v[6], v[7]);
-  }
-};
-template <> struct Elem<__nv_fp8_e4m3> {
-  static __device__ __forceinline__ void put(void* p, uint64_t i, float v) {
-    static_cast<uint8_t*>(p)[i] = static_cast<uint8_t>(__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3));
-  }
-  static __device__ __forceinline__ void put8(void* p, uint64_t i, const float (&v)[8]) {
-    uint32_t w[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j], v[4 * j + 1]), __NV_SATFINITE, __NV_E4M3);
-      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * j + 2], v[4 * j + 3]), __NV_SATFINITE, __NV_E4M3);
+    for (int j = 0; j < H / 2; ++j) {
+      const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(low(v[2 * j]), high(v[2 * j])), __NV_SATFINITE, __NV_E4M3);
+      const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(low(v[2 * j + 1]), high(v[2 * j + 1])), __NV_SATFINITE, __NV_E4M3);
       w[j] = lo | (hi << 16);
     }
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p) + i) = make_uint2(w[0], w[1]);
+    if constexpr (H == 4) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p) + i) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = w[0];
   }
-};
+}
 
-// Elements i .. i + 7 of w, i any number in 0 .. width - 8.
-__device__ __forceinline__ void weight8(const NormArgs& a, int i, float (&w)[8]) {
+// The vectors at a row's ends, and all vectors where the matrices' rows are not equally aligned: element by
+// element, elements e .. e + 2 H - 1 of a row of `width`, those outside it as zeros.  Not inlined: rare, and long.
+template <int H> struct Pairs { Two v[H]; };
+template <typename T, int H>
+__device__ __noinline__ Pairs<H> gather(const void* row, int e, int width) {
+  float f[2 * H];
+#pragma unroll
+  for (int i = 0; i < 2 * H; ++i) f[i] = static_cast<unsigned>(e + i) < static_cast<unsigned>(width) ? one<T>(row, e + i) : 0.f;
+  Pairs<H> p;
+#pragma unroll
+  for (int i = 0; i < H; ++i) p.v[i] = two(f[2 * i], f[2 * i + 1]);
+  return p;
+}
+template <typename T, int H>
+__device__ __noinline__ void scatter(void* row, int e, int width, Pairs<H> f) {
+#pragma unroll
+  for (int i = 0; i < 2 * H; ++i)
+    if (static_cast<unsigned>(e + i) < static_cast<unsigned>(width)) put1<T>(row, e + i, i & 1 ? high(f.v[i / 2]) : low(f.v[i / 2]));
+}
+
+// The weights e .. e + 2 H - 1.  aligned: e is a multiple of 2 H and all of them lie in the row.
+template <int H>
+__device__ __forceinline__ Pairs<H> weights(const NormArgs& a, int e, bool aligned) {
+  Pairs<H> p;
   if (!a.w) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = 1.f;
-    return;
-  }
-  if (a.w_vec && !(i & 7)) {
-    if (a.w_f32) {
-      const float4* f = reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + i);
-      const float4 p = *f, q = f[1];
-      w[0] = p.x; w[1] = p.y; w[2] = p.z; w[3] = p.w; w[4] = q.x; w[5] = q.y; w[6] = q.z; w[7] = q.w;
-    } else {
-      Raw<1> u;
-      u.q[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + i);
-      Elem<__nv_bfloat16>::open(u, w);
-    }
-    return;
-  }
-  const int i0 = i & ~7, by = i & 7;
-  if (a.w_vec && !a.w_f32 && i0 + 16 <= static_cast<int>(a.width)) {
-    // the two aligned vectors around it, moved down by `by` elements (the same for the whole row)
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + i0);
-    const uint4 lo = p[0], hi = p[1];
+    for (int i = 0; i < H; ++i) p.v[i] = two(1.f, 1.f);
+  } else if (!a.w_vec || !aligned) {
+    if (a.w_f32) return gather<float, H>(a.w, e, static_cast<int>(a.width));
+    const int e0 = e & ~7, by = e & 7;
+    if (!a.w_vec || e < 0 || e0 + 16 > static_cast<int>(a.width)) return gather<__nv_bfloat16, H>(a.w, e, static_cast<int>(a.width));
+    // the two aligned vectors around them, moved down by `by` elements
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + e0);
+    const uint4 lo = q[0], hi = q[1];
     uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    if (by & 4) {
 #pragma unroll
-      for (int j = 0; j < 6; ++j) c[j] = c[j + 2];
-    }
-    if (by & 2) {
+    for (int j = 0; j < 6; ++j) c[j] = by & 4 ? c[j + 2] : c[j];
 #pragma unroll
-      for (int j = 0; j < 6; ++j) c[j] = c[j + 1];
-    }
-    if (by & 1) {
+    for (int j = 0; j < 5; ++j) c[j] = by & 2 ? c[j + 1] : c[j];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c[j] = __funnelshift_r(c[j], c[j + 1], 16);
+    for (int i = 0; i < H; ++i) p.v[i] = open(by & 1 ? __funnelshift_r(c[i], c[i + 1], 16) : c[i]);
+  } else if (a.w_f32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(a.w) + e);
+#pragma unroll
+    for (int i = 0; i < H / 2; ++i) {
+      const float4 u = q[i];
+      p.v[2 * i] = two(u.x, u.y);
+      p.v[2 * i + 1] = two(u.z, u.w);
     }
-    Raw<1> u;
-    u.q[0] = make_uint4(c[0], c[1], c[2], c[3]);
-    Elem<__nv_bfloat16>::open(u, w);
-    return;
+  } else if constexpr (H == 4) {
+    open(*reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.w) + e), p.v);
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.w) + e);
+    p.v[0] = open(u.x);
+    p.v[1] = open(u.y);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) w[j] = a.w_f32 ? Elem<float>::one(a.w, i + j) : Elem<__nv_bfloat16>::one(a.w, i + j);
+  return p;
 }
 
 constexpr uint32_t kNormWarps = 32;
+constexpr size_t kNormRing = 216 * 1024;         // bytes of an SM's rings
 
-// blockDim = (threads of a row, rows of a block); a row of at most one warp needs no barrier.
-// Thread t of a row holds the V vectors of 8 elements t, t + T, ...  Where rows start `phase` elements
-// past a 16-byte boundary, vector 0 starts `phase` elements before the row, so that every vector is
-// aligned; the first and the last, and all of them where the matrices' rows are not equally aligned,
-// are read and written element by element.
-template <typename TX, typename TO, int V, int MOST>
-__global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
-  __shared__ float s_sum[kNormWarps];
-  __shared__ uint32_t s_top[kNormWarps];
-  ten::let_next_start();
-  const uint64_t row = uint64_t(blockIdx.x) * blockDim.y + threadIdx.y;
-  const uint32_t T = blockDim.x, t = threadIdx.x;
-  const bool live = row < a.rows;
-  const uint64_t xo = row * a.x_stride, ro = row * a.r_stride, oo = row * a.out_stride, so = row * a.sum_stride;
-  const int width = static_cast<int>(a.width);
-  const int phase = a.together ? static_cast<int>((reinterpret_cast<uintptr_t>(a.x) / sizeof(TX) + xo) & 7u) : 0;
-  auto first = [&](int j) { return static_cast<int>(t + j * T) * 8 - phase; };             // the vector's first element
-  auto whole = [&](int j) { return a.together && first(j) >= 0 && first(j) + 8 <= width; };
-  ten::wait_for_previous();
-
-  typename Elem<TX>::Eight x[V], r[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-    x[j] = {}; r[j] = {};
-    if (live && whole(j)) {
-      x[j] = load_once<sizeof(TX) / 2>(Elem<TX>::at(a.x, xo + first(j)));
-      if (a.r) r[j] = load_once<sizeof(TX) / 2>(Elem<TX>::at(a.r, ro + first(j)));
+// What the kernels share of a row: thread t of its T threads holds the V vectors of E elements t, t + T, ...
+// Where rows start `phase` elements past a 16-byte boundary, vector 0 starts `phase` elements before the
+// row, so that every vector is aligned.  EVEN: all rows start on a boundary and are whole vectors.
+template <typename TX, typename TO, int V, bool EVEN>
+struct NormRow {
+  static constexpr int E = 16 / sizeof(TX), H = E / 2;
+  const NormArgs& a;
+  int t, T, width, phase;
+  bool edge;                       // among the first or last rows, whose end vectors can reach past the matrices
+  const char* x; const char* r; char* out; char* sum;
+  __device__ __forceinline__ NormRow(const NormArgs& args, uint32_t thread, uint32_t threads)
+      : a(args), t(static_cast<int>(thread)), T(static_cast<int>(threads)), width(static_cast<int>(args.width)), phase(0), edge(true) {}
+  __device__ __forceinline__ void at(uint64_t row) {
+    x = a.x + row * a.x_step;
+    r = a.r + row * a.r_step;
+    out = a.out + row * a.out_step;
+    sum = a.sum + row * a.sum_step;
+    settle(row);
+  }
+  __device__ __forceinline__ void settle(uint64_t row) {
+    if constexpr (!EVEN) {
+      phase = a.shift ? static_cast<int>((reinterpret_cast<uintptr_t>(x) / sizeof(TX)) & (E - 1u)) : 0;
+      edge = row < E || row + E >= a.rows;
     }
   }
-  float h[V][8];
-  float sum = 0.f;
+  __device__ __forceinline__ int first(int j) const { return (t + j * T) * E - phase; }   // a vector's first element
+  __device__ __forceinline__ bool some(int j) const { return first(j) < width; }
+  __device__ __forceinline__ bool whole(int j) const { return EVEN ? some(j) : a.together && first(j) >= 0 && first(j) + E <= width; }
+  __device__ __forceinline__ const char* place(const char* row, int j) const { return row + int64_t(first(j)) * int(sizeof(TX)); }
+  // Whether vector j can be loaded as one: it holds some of the row, and nothing from before the matrices' first
+  // element or past their last one (what belongs to the rows next to this one is dropped).
+  __device__ __forceinline__ bool loads(int j) const {
+    if constexpr (EVEN) return some(j);
+    if (!a.together || !some(j)) return false;
+    return !edge || loads_at_edge(j);
+  }
+  __device__ __forceinline__ bool loads_at_edge(int j) const {
+    return place(x, j) >= a.x && place(x, j) + 16 <= a.x_end && (!a.r || (place(r, j) >= a.r && place(r, j) + 16 <= a.r_end));
+  }
+  // h = x + r from the loaded vectors; h stored; its sum of squares
+  __device__ __forceinline__ float add(const uint4 (&xs)[V], const uint4 (&rs)[V], Two (&h)[V][H]) const {
+    Two total = two(0.f, 0.f);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    float u[8];
-    Elem<TX>::open(x[j], h[j]);
-    Elem<TX>::open(r[j], u);
-    if (a.r) {
+    for (int j = 0; j < V; ++j) {
+      if (EVEN || loads(j)) {
+        open(xs[j], h[j]);
+        if (a.r) {
+          Two u[H];
+          open(rs[j], u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) h[j][i] += u[i];
-    }
-    if (live && whole(j)) {
-      if (a.sum) Elem<TX>::put8(a.sum, so + first(j), h[j]);
-    } else if (live && first(j) < width) {
+          for (int i = 0; i < H; ++i) h[j][i] = add2(h[j][i], u[i]);
+        }
+        if constexpr (!EVEN) {
+          if (!whole(j)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = first(j) + i;
-        if (e >= 0 && e < width) {
-          h[j][i] = Elem<TX>::one(a.x, xo + e);
-          if (a.r) h[j][i] += Elem<TX>::one(a.r, ro + e);
-          if (a.sum) Elem<TX>::put(a.sum, so + e, h[j][i]);
+            for (int i = 0; i < H; ++i)
+              h[j][i] = two(static_cast<unsigned>(first(j) + 2 * i) < static_cast<unsigned>(width) ? low(h[j][i]) : 0.f,
+                            static_cast<unsigned>(first(j) + 2 * i + 1) < static_cast<unsigned>(width) ? high(h[j][i]) : 0.f);
+          }
+        }
+      } else {
+        Pairs<H> f{};
+        if (some(j)) f = gather<TX, H>(x, first(j), width);
+#pragma unroll
+        for (int i = 0; i < H; ++i) h[j][i] = f.v[i];
+        if (a.r && some(j)) {
+          const Pairs<H> g = gather<TX, H>(r, first(j), width);
+#pragma unroll
+          for (int i = 0; i < H; ++i) h[j][i] = add2(h[j][i], g.v[i]);
         }
       }
-    }
+      if (a.sum) put<TX>(sum, j, h[j]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fmaf(h[j][i], h[j][i], sum);
+      for (int i = 0; i < H; ++i) total = fma2(h[j][i], h[j][i], total);
+    }
+    return low(total) + high(total);
+  }
+  template <typename T2>
+  __device__ __forceinline__ void put(char* row, int j, const Two (&v)[H]) const {
+    if (whole(j)) {
+      put_all<T2, H>(row, first(j), v);
+    } else if (!EVEN && some(j)) {
+      Pairs<H> f;
+#pragma unroll
+      for (int i = 0; i < H; ++i) f.v[i] = v[i];
+      scatter<T2, H>(row, first(j), width, f);
+    }
+  }
+  // h * w in place of h, and for an 8-bit output the largest of |h w|
+  static __device__ __forceinline__ float scale(Two (&h)[H], const Two (&w)[H], float top) {
+#pragma unroll
+    for (int i = 0; i < H; ++i) {
+      h[i] = mul2(h[i], w[i]);
+      if constexpr (sizeof(TO) == 1) top = larger(top, h[i]);
+    }
+    return top;
+  }
+  // over a row's threads; s_*: a place for each warp, free when this is called.  Magnitudes compare like their bits, NaN above all.
+  __device__ __forceinline__ void reduce(float& total, float& top, float* s_sum, float* s_top) const {
+    constexpr bool k8 = sizeof(TO) == 1;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(ten::kAll, total, d);
+    if (k8) top = __uint_as_float(__reduce_max_sync(ten::kAll, __float_as_uint(top)));
+    if (T > 32) {
+      const int warps = T >> 5, lane = t & 31;
+      if (lane == 0) {
+        s_sum[t >> 5] = total;
+        if (k8) s_top[t >> 5] = top;
+      }
+      __syncthreads();
+      if (warps <= 8) {                                           // the same few words for every thread: no second round of shuffles
+        total = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (i >= warps) break;
+          total += s_sum[i];
+          if (k8) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(s_top[i])));
+        }
+      } else {
+        total = lane < warps ? s_sum[lane] : 0.f;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(ten::kAll, total, d);
+        if (k8) top = __uint_as_float(__reduce_max_sync(ten::kAll, lane < warps ? __float_as_uint(s_top[lane]) : 0u));
+      }
+    }
+  }
+  __device__ __forceinline__ void store(uint64_t row, Two (&h)[V][H], float total, float top) const {
+    float f = rsqrtf(fmaf(total, a.part, a.eps));
+    if constexpr (sizeof(TO) == 1) {
+      const float amax = f * top;
+      const float s = amax != amax ? amax : fmaxf(amax * (1.f / 448.f), 1.17549435e-38f);   // fmaxf alone would drop a NaN
+      if (t == 0) a.scales[row] = s;
+      const float back = __frcp_rn(s);                            // at most 2^126
+      if (!(f * back < INFINITY) && back < INFINITY) {            // tiny rows: not in one factor
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+          for (int i = 0; i < H; ++i) h[j][i] = mul2(h[j][i], two(f, f));
+        f = 1.f;
+      }
+      f *= back;
+    }
+    const Two ff = two(f, f);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+#pragma unroll
+      for (int i = 0; i < H; ++i) h[j][i] = mul2(h[j][i], ff);
+      put<TO>(out, j, h[j]);
+    }
+  }
+};
+
+// A block a row: for few rows, where a row's own latency counts, and for rows that the rings below do not fit.
+template <typename TX, typename TO, int V, int MOST>
+__global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
+  __shared__ float s_sum[kNormWarps], s_top[kNormWarps];
+  ten::let_next_start();
+  using Row = NormRow<TX, TO, V, false>;
+  Row n(a, threadIdx.x, blockDim.x);
+  n.at(blockIdx.x);
+  ten::wait_for_previous();
+  uint4 x[V], r[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    x[j] = r[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (n.loads(j)) {
+      x[j] = load_once(n.place(n.x, j));
+      if (a.r) r[j] = load_once(n.place(n.r, j));
+    }
+  }
+  auto weight = [&](int j) { return n.some(j) ? weights<Row::H>(a, n.first(j), !n.phase && n.whole(j)) : Pairs<Row::H>{}; };
+  Two h[V][Row::H];
+  float total, top = 0.f;
+  if constexpr (V == 1) {                                         // its load is under way with the row's
+    const Pairs<Row::H> w = weight(0);
+    total = n.add(x, r, h);
+    top = n.scale(h[0], w.v, top);
+  } else {
+    total = n.add(x, r, h);
+#pragma unroll
+    for (int j = 0; j < V; ++j) top = n.scale(h[j], weight(j).v, top);
+  }
+  n.reduce(total, top, s_sum, s_top);
+  n.store(blockIdx.x, h, total, top);
+}
+
+// Persistent: blockDim = (threads of a row, rows of a block); a block takes row after row.  Every thread copies its
+// own vectors of the rows to come into a ring of `depth` rows in shared memory (cp.async), so memory is
+// read on while a row is reduced and written; a thread reads only what it copied, and a row of one warp needs no
+// barrier at all.  Even rows: a weight in bf16 stays in registers.  Others, whose vectors start at any element: the
+// weight lies in shared memory, element e at [e % E][e / E], where a warp's reads of any alignment meet no conflict.
+template <typename TX, typename TO, int V, int MOST, bool EVEN>
+__global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs a, const uint32_t depth) {
+  extern __shared__ uint4 ring[];
+  __shared__ float s_sum[2][kNormWarps], s_top[2][kNormWarps];
+  ten::let_next_start();
+  using Row = NormRow<TX, TO, V, EVEN>;
+  constexpr int E = Row::E, H = Row::H;
+  const uint32_t t = threadIdx.x, T = blockDim.x, y = threadIdx.y, Y = blockDim.y;
+  const uint32_t per_row = (a.r ? 2u : 1u) * V * T;               // vectors of a row in the ring
+  const uint32_t mine = ten::smem_addr(ring + size_t(y) * depth * per_row + t), ring_end = mine + depth * per_row * 16u;
+  float* const s_w = reinterpret_cast<float*>(ring + size_t(Y) * depth * per_row);
+  const uint32_t w_pitch = a.width / E + 3u;                      // elements -E .. width + E and more
+  const uint64_t step = uint64_t(gridDim.x) * Y;
+  uint64_t row = uint64_t(blockIdx.x) * Y + y;
+  ten::wait_for_previous();
+
+  Row ahead(a, t, T), n(a, t, T);                                 // the row that is fetched next, the row at hand
+  ahead.at(row);
+  n.at(row);
+  uint64_t ahead_row = row;
+  auto fetch = [&](uint32_t to) {
+    if (ahead_row < a.rows) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (!ahead.loads(j)) continue;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + j * T * 16u), "l"(ahead.place(ahead.x, j)) : "memory");
+        if (a.r) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V + j) * T * 16u), "l"(ahead.place(ahead.r, j)) : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ahead_row += step;
+    ahead.x += step * a.x_step;
+    ahead.r += step * a.r_step;
+    ahead.settle(ahead_row);
+  };
+  uint32_t spare = mine;                                          // the place for the next fetch
+  for (uint32_t i = 0; i + 1 < depth; ++i, spare += per_row * 16u) fetch(spare);
+
+  const bool keep = EVEN && a.w && !a.w_f32;
+  uint2 kept[V][H / 2];
+  if constexpr (EVEN) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (keep && n.some(j)) {
+#pragma unroll
+        for (int i = 0; i < H / 2; ++i) kept[j][i] = reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.w) + n.first(j))[i];
+      }
+  } else {
+    for (uint32_t i = y * T + t; i < E * w_pitch; i += T * Y) {
+      const int e = static_cast<int>(i) - E;
+      float w = 0.f;
+      if (static_cast<unsigned>(e) < a.width) w = !a.w ? 1.f : a.w_f32 ? one<float>(a.w, e) : one<__nv_bfloat16>(a.w, e);
+      s_w[(i % E) * w_pitch + i / E] = w;
+    }
+    __syncthreads();
   }
 
-  // h * w in place of h; the largest of |h w| as bits: of two non-negative floats the larger has the larger bits, NaN above all
-  uint32_t top = 0;
+  uint32_t from = mine, odd = 0;
+  for (uint64_t base = uint64_t(blockIdx.x) * Y; base < a.rows; base += step) {   // the same trips for all of the block
+    fetch(spare);
+    spare += per_row * 16u;
+    if (spare == ring_end) spare = mine;
+    switch (depth) {                                              // all but the last depth - 1 copies are there
+      case 2: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+      case 3: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+      case 4: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+      case 5: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+      default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+    }
+    const bool live = row < a.rows;
+    Two h[V][H];
+    float total = 0.f, top = 0.f;
+    if (live) {
+      uint4 x[V], r[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    float w[8];
-    if (whole(j)) {
-      weight8(a, first(j), w);
-    } else {
+      for (int j = 0; j < V; ++j) {
+        x[j] = r[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (n.loads(j)) {
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[j].x), "=r"(x[j].y), "=r"(x[j].z), "=r"(x[j].w)
+                       : "r"(from + j * T * 16u) : "memory");
+          if (a.r)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[j].x), "=r"(r[j].y), "=r"(r[j].z), "=r"(r[j].w)
+                         : "r"(from + (V + j) * T * 16u) : "memory");
+        }
+      }
+      total = n.add(x, r, h);
+      const float* w_at[E];                                       // element i of a vector at [(i - phase) % E][vector + 1 + (i - phase) / E]
+      if constexpr (!EVEN) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = first(j) + i;
-        w[i] = 1.f;
-        if (a.w && e >= 0 && e < width) w[i] = a.w_f32 ? Elem<float>::one(a.w, e) : Elem<__nv_bfloat16>::one(a.w, e);
+        for (int i = 0; i < E; ++i) w_at[i] = s_w + ((i - n.phase) & (E - 1)) * w_pitch + 1 + (i < n.phase ? -1 : 0) + t;
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (!n.some(j)) continue;
+        Pairs<H> w;
+        if constexpr (EVEN) {
+          if (keep) {
+#pragma unroll
+            for (int i = 0; i < H / 2; ++i) { w.v[2 * i] = open(kept[j][i].x); w.v[2 * i + 1] = open(kept[j][i].y); }
+          } else {
+            w = weights<H>(a, n.first(j), true);
+          }
+        } else {
+          float f[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) f[i] = w_at[i][j * T];
+#pragma unroll
+          for (uint32_t i = 0; i < H; ++i) w.v[i] = two(f[2 * i], f[2 * i + 1]);
+        }
+        top = n.scale(h[j], w.v, top);
       }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      h[j][i] *= w[i];
-      top = max(top, __float_as_uint(h[j][i]) & 0x7FFFFFFFu);
-    }
-  }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(ten::kAll, sum, d);
-  top = __reduce_max_sync(ten::kAll, top);
-  if (T > 32) {
-    const uint32_t warps = T >> 5, lane = t & 31u;
-    if (lane == 0) { s_sum[t >> 5] = sum; s_top[t >> 5] = top; }
-    __syncthreads();
-    sum = lane < warps ? s_sum[lane] : 0.f;
-    top = lane < warps ? s_top[lane] : 0u;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(ten::kAll, sum, d);
-    top = __reduce_max_sync(ten::kAll, top);
-  }
-  if (!live) return;
-  const float f = 1.f / sqrtf(sum / static_cast<float>(width) + a.eps);
-  float back = 1.f;
-  constexpr bool k8 = std::is_same<TO, __nv_fp8_e4m3>::value;
-  if constexpr (k8) {
-    const float amax = f * __uint_as_float(top);
-    const float s = amax != amax ? amax : fmaxf(amax / 448.f, 1.17549435e-38f);   // fmaxf alone would drop a NaN
-    if (t == 0) a.scales[row] = s;
-    back = 1.f / s;                                               // at most 2^126: f / s at once could overflow
-  }
-#pragma unroll
-  for (int j = 0; j < V; ++j) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) h[j][i] = k8 ? h[j][i] * f * back : h[j][i] * f;
-    if (whole(j)) {
-      Elem<TO>::put8(a.out, oo + first(j), h[j]);
-    } else if (first(j) < width) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int e = first(j) + i;
-        if (e >= 0 && e < width) Elem<TO>::put(a.out, oo + e, h[j][i]);
-      }
-    }
+    n.reduce(total, top, s_sum[odd], s_top[odd]);
+    if (live) n.store(row, h, total, top);
+    from += per_row * 16u;
+    if (from == ring_end) from = mine;
+    odd ^= 1u;
+    row += step;
+    n.x += step * a.x_step;
+    n.r += step * a.r_step;
+    n.out += step * a.out_step;
+    n.sum += step * a.sum_step;
+    n.settle(row);
   }
 }
 
-template <typename TX, typename TO>
+// `blocks` blocks an SM split its shared memory; a ring of two to six rows
+template <typename TX>
+static size_t weight_bytes(const NormArgs& a) { return size_t(a.width / (16 / sizeof(TX)) + 3) * (16 / sizeof(TX)) * 4; }
+template <typename TX, typename TO, int V, int MOST, bool EVEN>
+static int launch_ring(const NormArgs& a, dim3 block, uint32_t blocks, int sms, cudaStream_t st) {
+  const size_t row = size_t(a.r ? 2 : 1) * V * 16 * block.x * block.y;
+  const size_t rest = EVEN ? 0 : weight_bytes<TX>(a);
+  auto* kernel = ans_rms_norm_ring_kernel<TX, TO, V, MOST, EVEN>;
+  while (blocks > 1 && blocks * (2 * row + rest) > kNormRing) --blocks;
+  uint32_t depth = static_cast<uint32_t>((kNormRing / blocks - rest) / row);
+  if (depth > 6) depth = 6;
+  const size_t smem = depth * row + rest;
+  ANSB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+  const uint64_t need = (a.rows + block.y - 1) / block.y, have = uint64_t(sms) * blocks;
+  return ten::launch(kernel, dim3(static_cast<unsigned>(need < have ? need : have)), block, smem, st, 1, a, depth);
+}
+
+template <typename TX, typename TO, bool EVEN>
 static int launch_norm(const NormArgs& a, int sms, cudaStream_t st) {
-  const uint32_t vectors = (a.width + a.shift + 7u) / 8u;
-  constexpr uint32_t kWide = sizeof(TX) == 2 ? 4 : 2;             // vectors a thread: 64 bytes of x
+  constexpr uint32_t E = 16 / sizeof(TX), kTwice = sizeof(TX) / 2;   // fp32: twice the vectors for a row
+  const uint32_t vectors = (a.width + a.shift + E - 1) / E;
   if (vectors <= 128) {                                           // a warp a row
-    const uint64_t blocks = (a.rows + 7) / 8;
-    if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-    const dim3 grid(static_cast<unsigned>(blocks)), block(32, 8);
-    if (vectors <= 32) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 256>, grid, block, 0, st, 1, a);
-    if (vectors <= 64) return ten::launch(ans_rms_norm_kernel<TX, TO, 2, 256>, grid, block, 0, st, 1, a);
-    return ten::launch(ans_rms_norm_kernel<TX, TO, 4, 256>, grid, block, 0, st, 1, a);
+    const dim3 block(32, 8);
+    if (vectors <= 32) return launch_ring<TX, TO, 1, 256, EVEN>(a, block, EVEN ? 4 : 3, sms, st);
+    if (vectors <= 64) return launch_ring<TX, TO, 2, 256, EVEN>(a, block, 3, sms, st);
+    return launch_ring<TX, TO, 4, 256, EVEN>(a, block, kTwice == 2 && EVEN ? 3 : 2, sms, st);
   }
-  if (a.rows > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(a.rows));
   auto threads = [&](uint32_t v) { return dim3(((vectors + v - 1) / v + 31) / 32 * 32); };
-  // Few rows: as many threads as a row has vectors; many: as many loads a thread as registers hold.
-  if (vectors <= 1024 && a.rows <= 2ull * sms) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 1024>, grid, threads(1), 0, st, 1, a);
-  if (vectors <= 512 * kWide) return ten::launch(ans_rms_norm_kernel<TX, TO, kWide, 512>, grid, threads(kWide), 0, st, 1, a);
-  if (vectors <= 2048) return ten::launch(ans_rms_norm_kernel<TX, TO, 4, 512>, grid, threads(4), 0, st, 1, a);
-  return ten::launch(ans_rms_norm_kernel<TX, TO, 8, 576>, grid, threads(8), 0, st, 1, a);
+  const dim3 rows(static_cast<unsigned>(a.rows < 0x7FFFFFFFull ? a.rows : 0x7FFFFFFFull));
+  // A ring pays where a block has some rows to read ahead: six and more.  With fewer a block takes one row, with as
+  // many threads as it has vectors where a block can have them.
+  constexpr int V = 4 * kTwice;
+  const dim3 block = threads(V);
+  const uint32_t blocks = 512 / block.x;
+  const size_t bytes = size_t(vectors + 256) * 16 * (a.r ? 2 : 1);   // of a row in the ring, at most
+  const size_t rest = EVEN ? 0 : weight_bytes<TX>(a);
+  if (vectors <= 2048 * kTwice && a.rows >= 6ull * sms * blocks && 2 * bytes + rest <= kNormRing)
+    return launch_ring<TX, TO, V, 512, EVEN>(a, block, blocks, sms, st);
+  if (vectors <= 1024) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 1024>, rows, threads(1), 0, st, 1, a);
+  if (a.rows > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+  if (vectors <= 2048 * kTwice) return ten::launch(ans_rms_norm_kernel<TX, TO, 4 * kTwice, 512>, rows, threads(4 * kTwice), 0, st, 1, a);
+  return ten::launch(ans_rms_norm_kernel<TX, TO, 8 * kTwice, 576>, rows, threads(8 * kTwice), 0, st, 1, a);
 }
 
 template <typename TX>
 static int launch_norm_out(const NormArgs& a, int out_dtype, int sms, cudaStream_t st) {
-  if (out_dtype == ANS_E4M3) return launch_norm<TX, __nv_fp8_e4m3>(a, sms, st);
-  if (out_dtype == ANS_F32) return launch_norm<TX, float>(a, sms, st);
-  return launch_norm<TX, __nv_bfloat16>(a, sms, st);
+  const bool even = a.together && !a.shift && a.width % (16 / sizeof(TX)) == 0 && (!a.w || a.w_vec);
+  if (out_dtype == ANS_E4M3) return even ? launch_norm<TX, __nv_fp8_e4m3, true>(a, sms, st) : launch_norm<TX, __nv_fp8_e4m3, false>(a, sms, st);
+  if (out_dtype == ANS_F32) return even ? launch_norm<TX, float, true>(a, sms, st) : launch_norm<TX, float, false>(a, sms, st);
+  return even ? launch_norm<TX, __nv_bfloat16, true>(a, sms, st) : launch_norm<TX, __nv_bfloat16, false>(a, sms, st);
 }
 
 }  // namespace ansb
@@ -315,21 +560,28 @@ ANS_EXPORT int ans_rms_norm(const ans_norm_desc* h_desc, void* stream) {
   for (uint64_t s : strides)
     if (d.rows > 1 && (s < d.width || s > kMost)) return ANS_ERR_INVALID_ARG;
   const int xs = d.x_dtype == ANS_F32 ? 4 : 2, os = d.out_dtype == ANS_F32 ? 4 : d.out_dtype == ANS_BF16 ? 2 : 1;
-  // the place of a matrix's first row past a multiple of 8 elements, and its rows' step modulo 8; 99: not even on an element
-  auto place = [](const void* p, int size) { const uintptr_t u = reinterpret_cast<uintptr_t>(p); return u % size ? 99u : unsigned(u / size % 8); };
+  // the place of a matrix's first row past a whole vector, in elements, and its rows' step; 99: not even on an element
+  const unsigned E = 16 / xs;
+  auto place = [&](const void* p, int size) { const uintptr_t u = reinterpret_cast<uintptr_t>(p); return u % size ? 99u : unsigned(u / size % E); };
   const unsigned at = place(d.d_x, xs);
   if (at == 99 || place(d.d_out, os) == 99 || (d.d_residual && place(d.d_residual, xs) == 99) || (d.d_sum && place(d.d_sum, xs) == 99))
     return ANS_ERR_INVALID_ARG;
   if (d.d_weight && place(d.d_weight, d.weight_dtype == ANS_F32 ? 4 : 2) == 99) return ANS_ERR_INVALID_ARG;
   auto same = [&](const void* p, int size, uint64_t stride) {
-    return !p || (place(p, size) == at && (d.rows == 1 || stride % 8 == d.x_stride % 8));
+    return !p || (place(p, size) == at && (d.rows == 1 || stride % E == d.x_stride % E));
   };
   NormArgs a{};
-  a.x = d.d_x; a.r = d.d_residual; a.w = d.d_weight; a.out = d.d_out; a.scales = d.d_scales; a.sum = d.d_sum;
+  a.x = static_cast<const char*>(d.d_x); a.r = static_cast<const char*>(d.d_residual); a.w = d.d_weight;
+  a.out = static_cast<char*>(d.d_out); a.scales = d.d_scales; a.sum = static_cast<char*>(d.d_sum);
   a.rows = d.rows; a.width = d.width; a.eps = d.eps;
-  a.x_stride = d.x_stride; a.r_stride = d.residual_stride; a.out_stride = d.out_stride; a.sum_stride = d.sum_stride;
+  a.x_step = d.x_stride * xs; a.out_step = d.out_stride * os;
+  if (a.r) a.r_step = d.residual_stride * xs;
+  if (a.sum) a.sum_step = d.sum_stride * xs;
+  a.x_end = a.x + (d.rows - 1) * a.x_step + uint64_t(d.width) * xs;
+  a.r_end = a.r + (d.rows - 1) * a.r_step + uint64_t(d.width) * xs;
+  a.part = 1.f / static_cast<float>(d.width);
   a.together = same(d.d_residual, xs, d.residual_stride) && same(d.d_out, os, d.out_stride) && same(d.d_sum, xs, d.sum_stride);
-  a.shift = a.together && (at || (d.rows > 1 && d.x_stride % 8)) ? 7u : 0u;
+  a.shift = a.together && (at || (d.rows > 1 && d.x_stride % E)) ? E - 1 : 0u;
   a.w_f32 = d.weight_dtype == ANS_F32;
   a.w_vec = !(reinterpret_cast<uintptr_t>(d.d_weight) & 15);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
