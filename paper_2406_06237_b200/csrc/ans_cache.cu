@@ -13,6 +13,8 @@
 
 namespace ansb {
 
+using namespace ten;
+
 struct CacheArgs {
   uint8_t* codes[2];                 // [0]: keys, [1]: values
   float* scales[2];
@@ -31,102 +33,109 @@ struct WriteArgs {
   uint32_t wide[2];                  // every run of 8 values starts on 16 bytes
 };
 
-// LANES (a power of two) lanes per group, eight values each, lanes past group / 8 idle.  blockIdx.y: keys or values.
+// LANES (a power of two) lanes per group, eight values each, lanes past group / 8 idle.  A block takes
+// blockDim.y tokens, or the parts of one after another where a token has more threads' work than a block; blockIdx.y:
+// keys or values.
 template <typename T, int BITS, int LANES>
 __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a) {
-  ten::let_next_start();
+  let_next_start();
   const uint32_t which = blockIdx.y;
-  const uint32_t lane = threadIdx.x % LANES;
+  const uint64_t token = uint64_t(blockIdx.x) * blockDim.y + threadIdx.y;
   const uint32_t per_head = a.c.head_dim / a.c.group, per_token = a.c.heads * per_head;
-  const uint64_t unit = (uint64_t(blockIdx.x) * 256u + threadIdx.x) / LANES;      // (token, head, group)
-  const uint64_t token = unit / per_token;
-  const uint32_t in_token = static_cast<uint32_t>(unit - token * per_token);
-  int64_t slot = -1;
-  ten::wait_for_previous();
-  if (token < a.tokens) {
-    slot = a.slot[token];
-    if (slot >= 0 && static_cast<uint64_t>(slot) >= a.c.slots) {
-      if (lane == 0 && in_token == 0 && which == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-      slot = -1;
-    }
+  const uint32_t lane = threadIdx.x % LANES;
+  constexpr float L = static_cast<float>((1 << BITS) - 1);
+  wait_for_previous();
+  int64_t slot = token < a.tokens ? a.slot[token] : -1;
+  if (slot >= 0 && static_cast<uint64_t>(slot) >= a.c.slots) {
+    if (threadIdx.x == 0 && which == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+    slot = -1;
   }
-  const uint32_t head = in_token / per_head, g = in_token - head * per_head;
-  const bool live = slot >= 0 && lane * 8u < a.c.group;
-  float v[8];
+  for (uint32_t base = 0; base < per_token * LANES; base += blockDim.x) {    // the same trips for all of the block
+    const uint32_t unit = (base + threadIdx.x) / LANES;                      // (head, group)
+    const uint32_t head = unit / per_head, g = unit - head * per_head;
+    const bool live = token < a.tokens && unit < per_token && lane * 8u < a.c.group;
+    Two v[4] = {0, 0, 0, 0};
+    if (live) {
+      const T* p = static_cast<const T*>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which] + g * a.c.group + lane * 8u;
+      if (a.wide[which]) {
+        if constexpr (sizeof(T) == 2) {
+          const uint4 u = *reinterpret_cast<const uint4*>(p);
+          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = 0.f;
-  if (live) {
-    const T* p = static_cast<const T*>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which] + g * a.c.group + lane * 8u;
-    if (a.wide[which]) {
-      if constexpr (sizeof(T) == 2) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          v[2 * j] = __uint_as_float(w[j] << 16);
-          v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+          for (int j = 0; j < 4; ++j) v[j] = two(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+        } else {
+          const float4 q0 = reinterpret_cast<const float4*>(p)[0], q1 = reinterpret_cast<const float4*>(p)[1];
+          v[0] = two(q0.x, q0.y); v[1] = two(q0.z, q0.w); v[2] = two(q1.x, q1.y); v[3] = two(q1.z, q1.w);
         }
       } else {
-        const float4 q0 = reinterpret_cast<const float4*>(p)[0], q1 = reinterpret_cast<const float4*>(p)[1];
-        v[0] = q0.x; v[1] = q0.y; v[2] = q0.z; v[3] = q0.w; v[4] = q1.x; v[5] = q1.y; v[6] = q1.z; v[7] = q1.w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = two(static_cast<float>(p[2 * i]), static_cast<float>(p[2 * i + 1]));
       }
+    }
+    float lo = 0.f, hi = 0.f, top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo = fminf(lo, fminf(low(v[i]), high(v[i])));
+      hi = fmaxf(hi, fmaxf(low(v[i]), high(v[i])));
+      top = larger(top, v[i]);
+    }
+    if (!(top < INFINITY)) hi = INFINITY;                 // an infinity or a NaN
+#pragma unroll
+    for (int d = LANES / 2; d; d >>= 1) {
+      lo = fminf(lo, __shfl_xor_sync(kAll, lo, d));
+      hi = fmaxf(hi, __shfl_xor_sync(kAll, hi, d));
+    }
+    if (!live || slot < 0) continue;
+    const uint64_t param = (uint64_t(slot) * a.c.heads + head) * per_head + g;
+    float scale = fmaxf(hi * (1.f / L) - lo * (1.f / L), 1.17549435e-38f);
+    float zero = fminf(rintf(-lo / scale), L);
+    // v * (1 / scale) is within 2^-14 of v / scale, whose magnitude is at most 255: only near a tie between two codes
+    // is the division itself needed.  Adding 1.5 * 2^23 rounds to a whole number, in the sum's low bits.
+    const float inverse = __frcp_rn(scale);
+    constexpr float kWhole = 12582912.f;
+    Two m[4];
+    float tie = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Two q = mul2(v[i], two(inverse, inverse));
+      m[i] = add2(q, two(kWhole, kWhole));
+      const Two n = add2(m[i], two(-kWhole, -kWhole));
+      tie = larger(tie, add2(q, mul2(n, two(-1.f, -1.f))));
+    }
+    if (tie > 0.4999f) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = add2(two(rintf(low(v[i]) / scale), rintf(high(v[i]) / scale)), two(kWhole, kWhole));
+    }
+    // no code is under 0: values are at least lo, and zero is what lo rounds to
+    const int raise = static_cast<int>(zero) - __float_as_int(kWhole);
+    uint32_t code[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      code[2 * i] = min(__float_as_int(low(m[i])) + raise, (1 << BITS) - 1);
+      code[2 * i + 1] = min(__float_as_int(high(m[i])) + raise, (1 << BITS) - 1);
+    }
+    if (!(hi < INFINITY)) {
+      scale = __uint_as_float(0x7FC00000u);
+      zero = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) code[i] = 0;
+    }
+    const uint64_t at = param * a.c.group + lane * 8u;    // the first code's number in the whole array
+    if constexpr (BITS == 8) {
+      uint2 w;
+      w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+      w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+      *reinterpret_cast<uint2*>(a.c.codes[which] + at) = w;
     } else {
+      uint32_t w = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(p[i]);
+      for (int i = 0; i < 8; ++i) w |= code[i] << (4 * i);
+      *reinterpret_cast<uint32_t*>(a.c.codes[which] + at / 2) = w;
     }
-  }
-  float lo = 0.f, hi = 0.f;
-  bool odd = false;                                       // an infinity or a NaN
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    lo = fminf(lo, v[i]);
-    hi = fmaxf(hi, v[i]);
-    odd |= !(fabsf(v[i]) < INFINITY);
-  }
-  if (odd) hi = INFINITY;
-#pragma unroll
-  for (int d = LANES / 2; d; d >>= 1) {
-    lo = fminf(lo, __shfl_xor_sync(ten::kAll, lo, d));
-    hi = fmaxf(hi, __shfl_xor_sync(ten::kAll, hi, d));
-  }
-  if (!live) return;
-  constexpr float L = static_cast<float>((1 << BITS) - 1);
-  const uint64_t param = (uint64_t(slot) * a.c.heads + head) * per_head + g;
-  float scale = fmaxf(hi * (1.f / L) - lo * (1.f / L), 1.17549435e-38f);
-  float zero = fminf(rintf(-lo / scale), L);
-  const float inverse = 1.f / scale;
-  uint32_t code[8];
-  if (hi < INFINITY) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // v * (1 / scale) is within 2^-14 of v / scale, whose magnitude is at most 255: only near a tie between two codes
-      // is the division itself needed
-      const float q = v[i] * inverse;
-      float n = rintf(q);
-      if (fabsf(fabsf(q - n) - 0.5f) < 0.0001f) n = rintf(v[i] / scale);
-      code[i] = static_cast<uint32_t>(fminf(fmaxf(n + zero, 0.f), L));
+    if (lane == 0) {
+      a.c.scales[which][param] = scale;
+      a.c.zeros[which][param] = static_cast<uint8_t>(zero);
     }
-  } else {
-    scale = __uint_as_float(0x7FC00000u);
-    zero = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = 0;
-  }
-  const uint64_t at = param * a.c.group + lane * 8u;      // the first code's number in the whole array
-  if constexpr (BITS == 8) {
-    uint2 w;
-    w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-    w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-    *reinterpret_cast<uint2*>(a.c.codes[which] + at) = w;
-  } else {
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w |= code[i] << (4 * i);
-    *reinterpret_cast<uint32_t*>(a.c.codes[which] + at / 2) = w;
-  }
-  if (lane == 0) {
-    a.c.scales[which][param] = scale;
-    a.c.zeros[which][param] = static_cast<uint8_t>(zero);
   }
 }
 
@@ -140,20 +149,52 @@ struct ReadArgs {
   uint64_t rows;
   void* out[2];
   uint32_t* status;
+  uint32_t wide;                     // outputs on 32 bytes
 };
 
 constexpr uint32_t kReadRows = 64;    // rows of a block at most
 
-// scale * (code - zero).  The ends of a group's range lie up to half a step outside its values, so that with
-// values near the type's largest the product can pass it: such a result is that largest value.  A NaN stays.
-// raised: 2^23 + code as a float; below: 2^23 + zero.  Their difference is exact.
-template <typename T>
-__device__ __forceinline__ float value_of(uint32_t raised, float below, float scale) {
-  const float v = scale * (__uint_as_float(raised) - below);
+// Sixteen codes in w to scale * (code - zero), two at a time: a code set under the exponent of 2^23 is 2^23 + code * 16^k
+// (k: its place among the four nibbles of a half word; 0 for whole bytes), from which 2^23 + zero * 16^k is
+// subtracted without error, and scale / 16^k, exact too where it is no subnormal number, gives the product's one rounding.
+template <int BITS>
+__device__ __forceinline__ void open_codes(const uint32_t (&w)[BITS / 2], uint32_t zero, float scale, Two (&v)[8]) {
+  constexpr float kRaise = 8388608.f;
+  const float z = static_cast<float>(zero);
+  if constexpr (BITS == 8) {
+    const Two below = two(-kRaise - z, -kRaise - z), s = two(scale, scale);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const Two raised = two(__uint_as_float(__byte_perm(w[n / 2], 0x4B000000u, 0x7540u + (2 * n) % 4)),
+                             __uint_as_float(__byte_perm(w[n / 2], 0x4B000000u, 0x7540u + (2 * n + 1) % 4)));
+      v[n] = mul2(add2(raised, below), s);
+    }
+  } else {
+    const Two below[2] = {two(-kRaise - z, -kRaise - 16.f * z), two(-kRaise - 256.f * z, -kRaise - 4096.f * z)};
+    const Two s[2] = {two(scale, scale * 0.0625f), two(scale * 0.00390625f, scale * 0.000244140625f)};
+#pragma unroll
+    for (int n = 0; n < 8; ++n) {
+      const uint32_t h = n & 2 ? w[n / 4] >> 16 : w[n / 4];
+      const uint32_t mask = n & 1 ? 0xF00u : 0xFu;
+      const Two raised = two(__uint_as_float((h & mask) | 0x4B000000u), __uint_as_float((h & (mask << 4)) | 0x4B000000u));
+      v[n] = mul2(add2(raised, below[n & 1]), s[n & 1]);
+    }
+  }
+}
+// The same for scales of any size.  The ends of a group's range lie up to half a step outside its values, so that
+// with values near the type's largest the product can pass it: such a result is that largest value.  A NaN stays.
+template <typename T, int BITS>
+__device__ __forceinline__ void open_any(const uint32_t (&w)[BITS / 2], uint32_t zero, float scale, Two (&v)[8]) {
   const float most = __uint_as_float(sizeof(T) == 2 ? 0x7F7F0000u : 0x7F7FFFFFu);
-  float r;
-  asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(most));   // the smaller magnitude, v's sign
-  return r;
+  float f[16];
+#pragma unroll
+  for (int n = 0; n < 16; ++n) {
+    const uint32_t code = BITS == 8 ? (w[n / 4] >> (8 * (n % 4))) & 255u : (w[n / 8] >> (4 * (n % 8))) & 15u;
+    f[n] = scale * static_cast<float>(static_cast<int>(code) - static_cast<int>(zero));
+    asm("min.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(f[n]) : "f"(f[n]), "f"(most));   // the smaller magnitude, the value's sign
+  }
+#pragma unroll
+  for (int n = 0; n < 8; ++n) v[n] = two(f[2 * n], f[2 * n + 1]);
 }
 
 // The last s in 0 .. n - 1 with starts[s] <= row (0 if there is none): a warp looks at 32 places at a time.
@@ -171,7 +212,7 @@ __device__ __forceinline__ uint32_t sequence_of(const int32_t* starts, uint32_t 
 
 // A block reads `some` output rows of keys or of values (blockIdx.y).  First the slots of its rows: two warps find the
 // sequences of the first and the last row, between which, most often nowhere, the others' lie.  Then
-// sixteen values a thread, four of them under way at a time.
+// sixteen values a thread, always of the same columns, four rows under way at a time.
 template <typename T, int BITS>
 __global__ void __launch_bounds__(256) ans_cache_read_kernel(const ReadArgs a, const uint32_t some) {
   __shared__ int64_t s_slot[kReadRows];                   // -1: zeros, -2: not written
@@ -212,65 +253,68 @@ __global__ void __launch_bounds__(256) ans_cache_read_kernel(const ReadArgs a, c
   }
   __syncthreads();
   const uint32_t width = a.c.heads * a.c.head_dim, units = width / 16u, per_row = width / a.c.group;
+  const uint32_t across = min(units, 256u), down = 256u / across;        // threads over a row, rows at a time
+  const uint32_t r0 = threadIdx.x / across;
+  if (r0 >= down) return;
   constexpr uint32_t kAhead = 4;
-  for (uint32_t i0 = threadIdx.x; i0 < some * units; i0 += 256u * kAhead) {
-    uint32_t w[kAhead][BITS / 2];
-    float scale[kAhead];
-    uint32_t zero[kAhead];
-    int64_t slot[kAhead];
+  for (uint32_t c = threadIdx.x - r0 * across; c < units; c += across) {
+    const uint32_t e = c * 16u, group = e / a.c.group;
+    const uint8_t* const codes = a.c.codes[which] + (BITS == 8 ? e : e / 2);
+    const float* const scales = a.c.scales[which] + group;
+    const uint8_t* const zeros = a.c.zeros[which] + group;
+    T* const out = static_cast<T*>(a.out[which]) + row0 * width + e;
+    for (uint32_t r = r0; r < some; r += kAhead * down) {
+      uint32_t w[kAhead][BITS / 2], zero[kAhead];
+      float scale[kAhead];
+      bool to[kAhead];
 #pragma unroll
-    for (uint32_t j = 0; j < kAhead; ++j) {
-      const uint32_t i = i0 + j * 256u;
-      slot[j] = -2;
-      if (i < some * units) {
-        const uint32_t r = i / units, e = (i - r * units) * 16u;
-        slot[j] = s_slot[r];
-        if (slot[j] >= 0) {
-          const uint64_t at = uint64_t(slot[j]) * width + e, param = uint64_t(slot[j]) * per_row + e / a.c.group;
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        const uint32_t at = r + j * down;
+        const int64_t slot = at < some ? s_slot[at] : -2;
+        to[j] = slot != -2;
+        scale[j] = 0.f;                                   // no page: zeros
+        zero[j] = 0;
+#pragma unroll
+        for (int i = 0; i < BITS / 2; ++i) w[j][i] = 0;
+        if (slot >= 0) {
+          const uint8_t* const p = codes + uint64_t(slot) * (BITS == 8 ? width : width / 2);
           if constexpr (BITS == 8) {
-            const uint4 u = *reinterpret_cast<const uint4*>(a.c.codes[which] + at);
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
             w[j][0] = u.x; w[j][1] = u.y; w[j][2] = u.z; w[j][3] = u.w;
           } else {
-            const uint2 u = *reinterpret_cast<const uint2*>(a.c.codes[which] + at / 2);
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
             w[j][0] = u.x; w[j][1] = u.y;
           }
-          scale[j] = *(a.c.scales[which] + param);
-          zero[j] = *(a.c.zeros[which] + param);
+          scale[j] = scales[uint64_t(slot) * per_row];
+          zero[j] = zeros[uint64_t(slot) * per_row];
         }
       }
-    }
 #pragma unroll
-    for (uint32_t j = 0; j < kAhead; ++j) {
-      if (slot[j] == -2) continue;
-      const uint32_t i = i0 + j * 256u, r = i / units, e = (i - r * units) * 16u;
-      float v[16];
-      if (slot[j] >= 0) {
-        const float below = 8388608.f + static_cast<float>(zero[j]);
+      for (uint32_t j = 0; j < kAhead; ++j) {
+        if (!to[j]) continue;
+        Two v[8];
+        if (scale[j] == 0.f || (scale[j] > 1e-33f && scale[j] < 1e36f)) open_codes<BITS>(w[j], zero[j], scale[j], v);
+        else open_any<T, BITS>(w[j], zero[j], scale[j], v);
+        T* const p = out + uint64_t(r + j * down) * width;
+        if constexpr (sizeof(T) == 2) {
+          uint32_t o[8];
 #pragma unroll
-        for (uint32_t n = 0; n < 16; ++n) {
-          const uint32_t raised = BITS == 8 ? __byte_perm(w[j][n / 4], 0x4B000000u, 0x7540u + n % 4)
-                                            : ((w[j][n / 8] >> (4 * (n % 8))) & 15u) | 0x4B000000u;
-          v[n] = value_of<T>(raised, below, scale[j]);
+          for (uint32_t n = 0; n < 8; ++n) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(low(v[n]), high(v[n]));
+            o[n] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+          if (a.wide) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                         :: "l"(p), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]) : "memory");
+          } else {
+            reinterpret_cast<uint4*>(p)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            reinterpret_cast<uint4*>(p)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+          }
+        } else {
+#pragma unroll
+          for (uint32_t n = 0; n < 4; ++n)
+            reinterpret_cast<float4*>(p)[n] = make_float4(low(v[2 * n]), high(v[2 * n]), low(v[2 * n + 1]), high(v[2 * n + 1]));
         }
-      } else {
-#pragma unroll
-        for (uint32_t n = 0; n < 16; ++n) v[n] = 0.f;
-      }
-      const uint64_t to = (row0 + r) * width + e;
-      if constexpr (sizeof(T) == 2) {
-        uint32_t o[8];
-#pragma unroll
-        for (uint32_t n = 0; n < 8; ++n) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * n], v[2 * n + 1]);
-          o[n] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        uint4* p = reinterpret_cast<uint4*>(static_cast<T*>(a.out[which]) + to);
-        p[0] = make_uint4(o[0], o[1], o[2], o[3]);
-        p[1] = make_uint4(o[4], o[5], o[6], o[7]);
-      } else {
-        float4* p = reinterpret_cast<float4*>(static_cast<T*>(a.out[which]) + to);
-#pragma unroll
-        for (uint32_t n = 0; n < 4; ++n) p[n] = make_float4(v[4 * n], v[4 * n + 1], v[4 * n + 2], v[4 * n + 3]);
       }
     }
   }
@@ -297,16 +341,17 @@ template <typename T, int BITS>
 static int launch_write(const WriteArgs& a, cudaStream_t st) {
   const uint32_t need = a.c.group / 8u;
   const uint32_t lanes = need <= 2 ? 2 : need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : 32;
-  const uint64_t units = a.tokens * a.c.heads * (a.c.head_dim / a.c.group);
-  const uint64_t blocks = (units * lanes + 255) / 256;
+  const uint32_t threads = a.c.heads * (a.c.head_dim / a.c.group) * lanes;        // of a token
+  const dim3 block(threads < 256 ? (threads + 31) / 32 * 32 : 256, threads < 256 ? 256 / ((threads + 31) / 32 * 32) : 1);
+  const uint64_t blocks = (a.tokens + block.y - 1) / block.y;
   if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(blocks), 2);
   switch (lanes) {
-    case 2: return ten::launch(ans_cache_write_kernel<T, BITS, 2>, grid, dim3(256), 0, st, 1, a);
-    case 4: return ten::launch(ans_cache_write_kernel<T, BITS, 4>, grid, dim3(256), 0, st, 1, a);
-    case 8: return ten::launch(ans_cache_write_kernel<T, BITS, 8>, grid, dim3(256), 0, st, 1, a);
-    case 16: return ten::launch(ans_cache_write_kernel<T, BITS, 16>, grid, dim3(256), 0, st, 1, a);
-    default: return ten::launch(ans_cache_write_kernel<T, BITS, 32>, grid, dim3(256), 0, st, 1, a);
+    case 2: return ten::launch(ans_cache_write_kernel<T, BITS, 2>, grid, block, 0, st, 1, a);
+    case 4: return ten::launch(ans_cache_write_kernel<T, BITS, 4>, grid, block, 0, st, 1, a);
+    case 8: return ten::launch(ans_cache_write_kernel<T, BITS, 8>, grid, block, 0, st, 1, a);
+    case 16: return ten::launch(ans_cache_write_kernel<T, BITS, 16>, grid, block, 0, st, 1, a);
+    default: return ten::launch(ans_cache_write_kernel<T, BITS, 32>, grid, block, 0, st, 1, a);
   }
 }
 
@@ -358,6 +403,7 @@ ANS_EXPORT int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tab
   if (rows > 0x7FFFFFFFull || n_seqs > 0x7FFFFFFFu || table_stride > (uint64_t(1) << 40)) return ANS_ERR_UNSUPPORTED;
   a.tables = d_tables; a.table_stride = table_stride; a.table_pages = table_pages; a.starts = d_starts; a.n_seqs = n_seqs; a.rows = rows;
   a.out[0] = d_k_out; a.out[1] = d_v_out; a.status = d_status;
+  a.wide = !((reinterpret_cast<uintptr_t>(d_k_out) | reinterpret_cast<uintptr_t>(d_v_out)) & 31);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   // rows of a block: enough blocks for eight on each SM, up to 64 rows each, over which a block's look-up is spread
   int dev = 0, sms = 0;

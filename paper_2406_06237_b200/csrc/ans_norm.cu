@@ -26,36 +26,7 @@ struct NormArgs {
   uint32_t w_vec;         // w on a 16-byte boundary
 };
 
-// ---- two floats at a time ------------------------------------------------------------------
-using Two = unsigned long long;
-__device__ __forceinline__ Two two(float a, float b) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float low(Two v) { return __uint_as_float(static_cast<uint32_t>(v)); }
-__device__ __forceinline__ float high(Two v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
-__device__ __forceinline__ Two add2(Two a, Two b) {
-  Two r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ Two mul2(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-// the largest magnitude, NaN above all
-__device__ __forceinline__ float larger(float top, Two v) {
-  float r;
-  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(top), "f"(low(v)), "f"(high(v)));
-  return r;
-}
+using namespace ten;
 
 // ---- elements of a type, one by one and a vector at a time -------------------------------------
 // A vector is 16 bytes of x: E = 8 elements of bf16, 4 of fp32.
