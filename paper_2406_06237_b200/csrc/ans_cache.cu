@@ -5,7 +5,7 @@
 // and back  scale * (code - zero).  The results are those of IEEE divisions, so codes are a function of the
 // values alone and equal on every device and in any IEEE restatement.
 //
-// Both directions are bound by memory.  Writing takes eight values a thread (16 bytes of bf16), reading sixteen.
+// Both directions are bound by memory.  A thread has sixteen values of one group.
 #include <cmath>
 #include <initializer_list>
 
@@ -30,10 +30,50 @@ struct WriteArgs {
   const int64_t* slot;
   uint64_t tokens;
   uint32_t* status;
-  uint32_t wide[2];                  // every run of 8 values starts on 16 bytes
+  uint32_t wide[2];                  // every run of 16 values starts on 32 bytes: 2; on 16: 1
 };
 
-// LANES (a power of two) lanes per group, eight values each, lanes past group / 8 idle.  A block takes
+// the least and the largest of three, NaN if one of them is
+__device__ __forceinline__ float least(float a, Two b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(low(b)), "f"(high(b)));
+  return r;
+}
+__device__ __forceinline__ float largest(float a, Two b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(low(b)), "f"(high(b)));
+  return r;
+}
+
+// Sixteen values from p on.  wide: 2: on 32 bytes, 1: on 16, 0: on a value.
+template <typename T>
+__device__ __forceinline__ void load16(const T* p, uint32_t wide, Two (&v)[8]) {
+  if (wide == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = two(static_cast<float>(p[2 * i]), static_cast<float>(p[2 * i + 1]));
+    return;
+  }
+  constexpr int kParts = sizeof(T) / 2;                   // 32 bytes each
+#pragma unroll
+  for (int h = 0; h < kParts; ++h) {
+    uint32_t w[8];
+    const uint4* q = reinterpret_cast<const uint4*>(p) + 2 * h;
+    if (wide == 2) {
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(q) : "memory");
+    } else {
+      const uint4 a = q[0], b = q[1];
+      w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (kParts == 1) v[i] = two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+      else if (!(i & 1)) v[4 * h + i / 2] = two(__uint_as_float(w[i]), __uint_as_float(w[i + 1]));
+    }
+  }
+}
+
+// LANES (a power of two) lanes per group, sixteen values each, lanes past group / 16 idle.  A block takes
 // blockDim.y tokens, or the parts of one after another where a token has more threads' work than a block; blockIdx.y:
 // keys or values.
 template <typename T, int BITS, int LANES>
@@ -53,85 +93,70 @@ __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a)
   for (uint32_t base = 0; base < per_token * LANES; base += blockDim.x) {    // the same trips for all of the block
     const uint32_t unit = (base + threadIdx.x) / LANES;                      // (head, group)
     const uint32_t head = unit / per_head, g = unit - head * per_head;
-    const bool live = token < a.tokens && unit < per_token && lane * 8u < a.c.group;
-    Two v[4] = {0, 0, 0, 0};
-    if (live) {
-      const T* p = static_cast<const T*>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which] + g * a.c.group + lane * 8u;
-      if (a.wide[which]) {
-        if constexpr (sizeof(T) == 2) {
-          const uint4 u = *reinterpret_cast<const uint4*>(p);
-          const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    const bool live = token < a.tokens && unit < per_token && lane * 16u < a.c.group;
+    Two v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (live)
+      load16(static_cast<const T*>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which] + (g * a.c.group + lane * 16u), a.wide[which], v);
+    float lo = 0.f, hi = 0.f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[j] = two(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
-        } else {
-          const float4 q0 = reinterpret_cast<const float4*>(p)[0], q1 = reinterpret_cast<const float4*>(p)[1];
-          v[0] = two(q0.x, q0.y); v[1] = two(q0.z, q0.w); v[2] = two(q1.x, q1.y); v[3] = two(q1.z, q1.w);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = two(static_cast<float>(p[2 * i]), static_cast<float>(p[2 * i + 1]));
-      }
+    for (int i = 0; i < 8; ++i) {
+      lo = least(lo, v[i]);
+      hi = largest(hi, v[i]);
     }
-    float lo = 0.f, hi = 0.f, top = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo = fminf(lo, fminf(low(v[i]), high(v[i])));
-      hi = fmaxf(hi, fmaxf(low(v[i]), high(v[i])));
-      top = larger(top, v[i]);
-    }
-    if (!(top < INFINITY)) hi = INFINITY;                 // an infinity or a NaN
 #pragma unroll
     for (int d = LANES / 2; d; d >>= 1) {
-      lo = fminf(lo, __shfl_xor_sync(kAll, lo, d));
-      hi = fmaxf(hi, __shfl_xor_sync(kAll, hi, d));
+      const float l = __shfl_xor_sync(kAll, lo, d), h = __shfl_xor_sync(kAll, hi, d);
+      lo = least(lo, two(l, l));
+      hi = largest(hi, two(h, h));
     }
     if (!live || slot < 0) continue;
-    const uint64_t param = (uint64_t(slot) * a.c.heads + head) * per_head + g;
+    const bool finite = lo > -INFINITY && hi < INFINITY;  // neither infinite nor NaN
     float scale = fmaxf(hi * (1.f / L) - lo * (1.f / L), 1.17549435e-38f);
-    float zero = fminf(rintf(-lo / scale), L);
-    // v * (1 / scale) is within 2^-14 of v / scale, whose magnitude is at most 255: only near a tie between two codes
-    // is the division itself needed.  Adding 1.5 * 2^23 rounds to a whole number, in the sum's low bits.
+    // The quotients x / scale, correctly rounded (Markstein, 1990): with the correctly rounded reciprocal y of the
+    // divisor, q = x y is at most a unit off, its remainder r = x - q * scale is exact, and q + r y rounds to the
+    // quotient, as long as r is no subnormal number.  Ties between codes are common (bf16 values, few levels), so
+    // a product by y alone would not do.  Adding 1.5 * 2^23 rounds to a whole number, in the sum's low bits.
     const float inverse = __frcp_rn(scale);
     constexpr float kWhole = 12582912.f;
-    Two m[4];
-    float tie = 0.f;
+    const Two y = two(inverse, inverse), s = two(-scale, -scale), up = two(kWhole, kWhole);
+    auto quotient = [&](Two x) {
+      const Two q = mul2(x, y);
+      return fma2(fma2(q, s, x), y, q);
+    };
+    float zero = rintf(low(quotient(two(-lo, -lo))));
+    Two m[8];
+    if (scale > 1e-27f) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const Two q = mul2(v[i], two(inverse, inverse));
-      m[i] = add2(q, two(kWhole, kWhole));
-      const Two n = add2(m[i], two(-kWhole, -kWhole));
-      tie = larger(tie, add2(q, mul2(n, two(-1.f, -1.f))));
-    }
-    if (tie > 0.4999f) {
+      for (int i = 0; i < 8; ++i) m[i] = add2(quotient(v[i]), up);
+    } else {
+      zero = rintf(-lo / scale);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) m[i] = add2(two(rintf(low(v[i]) / scale), rintf(high(v[i]) / scale)), two(kWhole, kWhole));
+      for (int i = 0; i < 8; ++i) m[i] = add2(two(rintf(low(v[i]) / scale), rintf(high(v[i]) / scale)), up);
     }
-    // no code is under 0: values are at least lo, and zero is what lo rounds to
+    zero = fminf(zero, L);
+    // no code is under 0: values are at least lo, and zero is what -lo rounds to
     const int raise = static_cast<int>(zero) - __float_as_int(kWhole);
-    uint32_t code[8];
+    uint32_t w[BITS / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      code[2 * i] = min(__float_as_int(low(m[i])) + raise, (1 << BITS) - 1);
-      code[2 * i + 1] = min(__float_as_int(high(m[i])) + raise, (1 << BITS) - 1);
+    for (int i = 0; i < BITS / 2; ++i) {
+      w[i] = 0;
+#pragma unroll
+      for (int j = 0; j < 32 / BITS; ++j) {
+        const Two pair = m[(i * (32 / BITS) + j) / 2];
+        const int code = min(__float_as_int(j & 1 ? high(pair) : low(pair)) + raise, (1 << BITS) - 1);
+        w[i] |= static_cast<uint32_t>(code) << (BITS * j);
+      }
     }
-    if (!(hi < INFINITY)) {
+    if (!finite) {
       scale = __uint_as_float(0x7FC00000u);
       zero = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) code[i] = 0;
+      for (int i = 0; i < BITS / 2; ++i) w[i] = 0;
     }
-    const uint64_t at = param * a.c.group + lane * 8u;    // the first code's number in the whole array
-    if constexpr (BITS == 8) {
-      uint2 w;
-      w.x = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-      w.y = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-      *reinterpret_cast<uint2*>(a.c.codes[which] + at) = w;
-    } else {
-      uint32_t w = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w |= code[i] << (4 * i);
-      *reinterpret_cast<uint32_t*>(a.c.codes[which] + at / 2) = w;
-    }
+    const uint64_t param = uint64_t(slot) * per_token + unit;
+    const uint64_t at = param * a.c.group + lane * 16u;   // the first code's number in the whole array
+    if constexpr (BITS == 8) *reinterpret_cast<uint4*>(a.c.codes[which] + at) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(a.c.codes[which] + at / 2) = make_uint2(w[0], w[1]);
     if (lane == 0) {
       a.c.scales[which][param] = scale;
       a.c.zeros[which][param] = static_cast<uint8_t>(zero);
@@ -339,19 +364,19 @@ static int check_cache(const ans_cache_desc& d, CacheArgs& c) {
 
 template <typename T, int BITS>
 static int launch_write(const WriteArgs& a, cudaStream_t st) {
-  const uint32_t need = a.c.group / 8u;
-  const uint32_t lanes = need <= 2 ? 2 : need <= 4 ? 4 : need <= 8 ? 8 : need <= 16 ? 16 : 32;
+  const uint32_t need = a.c.group / 16u;
+  const uint32_t lanes = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : need <= 8 ? 8 : 16;
   const uint32_t threads = a.c.heads * (a.c.head_dim / a.c.group) * lanes;        // of a token
   const dim3 block(threads < 256 ? (threads + 31) / 32 * 32 : 256, threads < 256 ? 256 / ((threads + 31) / 32 * 32) : 1);
   const uint64_t blocks = (a.tokens + block.y - 1) / block.y;
   if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(blocks), 2);
   switch (lanes) {
+    case 1: return ten::launch(ans_cache_write_kernel<T, BITS, 1>, grid, block, 0, st, 1, a);
     case 2: return ten::launch(ans_cache_write_kernel<T, BITS, 2>, grid, block, 0, st, 1, a);
     case 4: return ten::launch(ans_cache_write_kernel<T, BITS, 4>, grid, block, 0, st, 1, a);
     case 8: return ten::launch(ans_cache_write_kernel<T, BITS, 8>, grid, block, 0, st, 1, a);
-    case 16: return ten::launch(ans_cache_write_kernel<T, BITS, 16>, grid, block, 0, st, 1, a);
-    default: return ten::launch(ans_cache_write_kernel<T, BITS, 32>, grid, block, 0, st, 1, a);
+    default: return ten::launch(ans_cache_write_kernel<T, BITS, 16>, grid, block, 0, st, 1, a);
   }
 }
 
@@ -380,7 +405,10 @@ ANS_EXPORT int ans_cache_write(const ans_cache_desc* h_desc, const void* d_k, co
   a.head_stride[0] = k_head_stride; a.head_stride[1] = v_head_stride;
   a.slot = d_slots; a.tokens = tokens; a.status = d_status;
   for (int w = 0; w < 2; ++w)
-    a.wide[w] = !((reinterpret_cast<uintptr_t>(a.x[w]) | (a.token_stride[w] * size) | (a.head_stride[w] * size)) & 15);
+    {
+      const uint64_t places = reinterpret_cast<uintptr_t>(a.x[w]) | (a.token_stride[w] * size) | (a.head_stride[w] * size);
+      a.wide[w] = !(places & 31) ? 2 : !(places & 15) ? 1 : 0;
+    }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (dtype == ANS_BF16) return h_desc->bitwidth == 8 ? launch_write<__nv_bfloat16, 8>(a, st) : launch_write<__nv_bfloat16, 4>(a, st);
   return h_desc->bitwidth == 8 ? launch_write<float, 8>(a, st) : launch_write<float, 4>(a, st);
