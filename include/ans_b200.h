@@ -479,7 +479,11 @@ typedef struct ans_product_desc {
   int32_t      dtype;             /* ANS_BF16 or ANS_E4M3                                    */
   int32_t      y_dtype;           /* ANS_BF16 or ANS_F32                                     */
   int32_t      activation;        /* ANS_ACT_*                                               */
+  uint32_t     flags;             /* ANS_PRODUCT_*, or 0                                     */
 } ans_product_desc;
+/* The caller knows that d_w was on the device before the work queued ahead of this call began, and that
+ * that work does not write it: the call may then read W before that work is done. */
+#define ANS_PRODUCT_WEIGHTS_SETTLED 1u
 int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
 
 /*

@@ -5,21 +5,23 @@
 // (rows of X) the columns, so that a call with few tokens uses matrix instructions with few columns
 // and reads W, which is what such a call is made of, in full tiles.  Both operands come by TMA in
 // 128-byte rows (64 bf16 or 128 e4m3) into a ring of stages; one thread issues tcgen05.mma; sums
-// stay in tensor memory in fp32.  Teams of four warps take them out: a thread holds one feature, so a block of
-// tokens goes through shared memory (fp32, token-major) and leaves in rows of 128 features, where
-// the epilogue's operands (bias, scales of W) are constants of a thread and residual and Y are
-// read and written in whole sectors.
+// stay in tensor memory in fp32.  Teams of four warps take them out: a thread holds one feature, so a warp's
+// block of 32 tokens goes through its own 4 KB of shared memory (fp32, token-major) and leaves in rows of 32
+// features, where the epilogue's operands (bias, scales of W) are constants of a thread and residual and
+// Y are read and written in whole sectors.
 //
 // Two forms:
-//   split:  one tile of 128 features x BN tokens a cluster of S CTAs; each sums a part of K, then each
-//           takes some of the tokens and adds the S partial sums out of the others' shared memory, in
-//           the order of the ranks: no workspace, no atomics, results do not vary from run to run.
+//   split:  one tile of 128 features x BN tokens a cluster of S CTAs; each sums a part of K and writes its sums of
+//           every token into the shared memory of the CTA that finishes the token, which adds the S parts in the
+//           order of the ranks: no workspace, no atomics, results do not vary from run to run.  Weights
+//           that the caller calls settled are fetched before the work queued ahead is done.
 //   whole:  persistent; a CTA (or a pair of CTAs on one tile of 256 features, cta_group::2) takes tile after
 //           tile, the accumulators are double-buffered so that one tile's epilogue runs under the next one's products.
 // Every wait is bounded; one that runs out sets ANS_STATUS_COPY_TIMEOUT and the kernel runs to its end.
 #include <cuda.h>
 
 #include <initializer_list>
+#include <type_traits>
 
 #include "ans_tensor.cuh"
 
@@ -29,8 +31,8 @@ using namespace ten;
 
 constexpr uint32_t kPrRow = 128;                      // bytes of K per stage and row
 constexpr uint32_t kPrFeatures = 128;                 // features of a CTA's tile
-constexpr uint32_t kPrBlock = 32;                     // tokens of an epilogue block
-constexpr uint32_t kPrStaging = kPrBlock * kPrFeatures * 4;
+constexpr uint32_t kPrBlock = 32;                     // tokens that an epilogue warp takes out at a time, of its 32 features
+constexpr uint32_t kPrScratch = kPrBlock * 32 * 4;
 
 struct PrArgs {
   const float* x_scales; const float* w_scales; const float* bias;
@@ -39,7 +41,7 @@ struct PrArgs {
   uint32_t M, N, steps;                               // steps: stages of K
   uint32_t tiles_f, tiles_t;
   int32_t activation;
-  uint32_t y_f32;
+  uint32_t settled;                                   // W may be read before the work queued ahead is done
   uint32_t wide;                                      // four features of Y (and residual) can be accessed at once
   uint32_t* status;
 };
@@ -52,16 +54,19 @@ struct PrShape {
   static constexpr uint32_t kBlockX = BN / CG * kPrRow;  // a pair's CTAs hold half of the tokens each
   static constexpr uint32_t kX = NT * kBlockX;
   static constexpr uint32_t kStage = kW + kX;
-  static constexpr uint32_t kTeams = SPLIT ? 1u : 2u; // teams of four epilogue warps, each with its part of the tokens
+  static constexpr uint32_t kTeams = SPLIT && BN <= 64u ? 1u : 2u;    // teams of four epilogue warps, each with its part of the tokens
   static constexpr uint32_t kTma = 4u * kTeams, kMma = kTma + 1u;     // the warps after them: copies, matrix instructions
   static constexpr uint32_t kThreads = 32u * (kMma + 1u);
-  static constexpr uint32_t kStagingBytes = SPLIT ? 0u : kTeams * kPrStaging;
-  static constexpr uint32_t kFit = (227u * 1024u - 1024u - 512u - kStagingBytes) / kStage;
+  // whole: a block for each epilogue warp; split: what the cluster's CTAs send to this one
+  static constexpr uint32_t kStagingBytes = SPLIT ? BN * kPrFeatures * 4u : 4u * kTeams * kPrScratch;
+  // Up to 64 tokens a CTA takes half of an SM's shared memory at most, so that the next call's CTAs can start
+  // beside it and fetch their weights; with more the ring has to be long enough for the matrix instructions' pace.
+  static constexpr uint32_t kRoom = SPLIT && BN <= 64u ? 112u * 1024u : 227u * 1024u;
+  static constexpr uint32_t kFit = (kRoom - 1024u - 512u - kStagingBytes) / kStage;
   static constexpr uint32_t kStages = kFit > 8u ? 8u : kFit;
   static constexpr uint32_t kAccs = SPLIT || kTokens > 256u ? 1u : 2u;  // tiles' accumulators in tensor memory
   static constexpr uint32_t kCols = kAccs * kTokens < 32u ? 32u : kAccs * kTokens;
   static constexpr uint32_t kSmem = 1024u + kStages * kStage + kStagingBytes + 512u;
-  static_assert(!SPLIT || BN * kPrFeatures * 4u <= kStages * kStage, "partial sums fit the ring");
 };
 
 // 2^x and 1/x to about 2^-22, subnormal results as zero
@@ -130,73 +135,88 @@ struct PrColumns {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Features f .. f + 3 of the T tokens m, m + step, ..., sums in v (four a token): scales, bias, activation,
-// residual, one rounding, store.  Tokens from `end` on are left alone.  Where four features can be accessed at
-// once the T tokens' loads and stores are in flight together.
-template <uint32_t T>
-__device__ __forceinline__ void finish(const PrArgs& a, const PrColumns& c, uint32_t m, uint32_t step, uint32_t end, uint32_t f, float (&v)[4 * T]) {
-  const bool whole = a.wide && f + 4 <= a.N;
-  uint4 r[T];
-  if (whole && a.residual) {
+// What the epilogue reads for features f .. f + 3 of the T tokens m, m + step, ... before `end`: the tokens' scales, and
+// the residual where four features can be accessed at once.  Fetched ahead of the sums, without a branch between the
+// loads (a token past the end stands for the last one).
+template <uint32_t T, bool YF32>
+struct PrAhead {
+  uint4 r[T];                                          // bf16: x and y
+  float xs[T];
+  __device__ __forceinline__ void fetch(const PrArgs& a, uint32_t m, uint32_t step, uint32_t end, uint32_t f) {
 #pragma unroll
-    for (uint32_t j = 0; j < T; ++j) {
-      r[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (m + j * step >= end) continue;
-      const uint64_t at = uint64_t(m + j * step) * a.residual_stride + f;
-      if (a.y_f32) {
-        r[j] = *reinterpret_cast<const uint4*>(static_cast<const float*>(a.residual) + at);
-      } else {
-        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.residual) + at);
-        r[j] = make_uint4(q.x << 16, q.x & 0xFFFF0000u, q.y << 16, q.y & 0xFFFF0000u);
+    for (uint32_t j = 0; j < T; ++j) xs[j] = 1.f;
+    if (m >= end) return;
+    if (a.x_scales) {
+#pragma unroll
+      for (uint32_t j = 0; j < T; ++j) xs[j] = a.x_scales[min(m + j * step, end - 1u)];
+    }
+    if (a.residual && a.wide && f + 4 <= a.N) {
+#pragma unroll
+      for (uint32_t j = 0; j < T; ++j) {
+        const uint64_t at = uint64_t(min(m + j * step, end - 1u)) * a.residual_stride + f;
+        if constexpr (YF32) {
+          r[j] = *reinterpret_cast<const uint4*>(static_cast<const float*>(a.residual) + at);
+        } else {
+          const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(a.residual) + at);
+          r[j].x = q.x;
+          r[j].y = q.y;
+        }
       }
     }
   }
+};
+
+// Features f .. f + 3 of the T tokens m, m + step, ..., sums in v (four a token): scales, bias, activation,
+// residual, one rounding, store.  Tokens from `end` on are left alone.
+template <uint32_t T, bool YF32>
+__device__ __forceinline__ void finish(const PrArgs& a, const PrColumns& c, const PrAhead<T, YF32>& p, uint32_t m, uint32_t step, uint32_t end,
+                                       uint32_t f, float (&v)[4 * T]) {
+  using Y = std::conditional_t<YF32, float, __nv_bfloat16>;
+  if (f >= a.N || m >= end) return;
 #pragma unroll
   for (uint32_t j = 0; j < T; ++j) {
-    const float xs = a.x_scales && m + j * step < end ? *(a.x_scales + m + j * step) : 1.f;
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) v[4 * j + i] = fmaf(v[4 * j + i], xs * c.scale[i], c.bias[i]);
+    for (uint32_t i = 0; i < 4; ++i) v[4 * j + i] = fmaf(v[4 * j + i], p.xs[j] * c.scale[i], c.bias[i]);
   }
   activate<4 * T>(v, a.activation);
-  if (whole) {
+  Y* const y = static_cast<Y*>(a.y) + uint64_t(m) * a.y_stride + f;
+  const uint64_t down = uint64_t(step) * a.y_stride;
+  if (a.wide && f + 4 <= a.N) {
     if (a.residual) {
 #pragma unroll
       for (uint32_t j = 0; j < T; ++j) {
-        v[4 * j] += __uint_as_float(r[j].x);
-        v[4 * j + 1] += __uint_as_float(r[j].y);
-        v[4 * j + 2] += __uint_as_float(r[j].z);
-        v[4 * j + 3] += __uint_as_float(r[j].w);
+        v[4 * j] += YF32 ? __uint_as_float(p.r[j].x) : bf16_lo(p.r[j].x);
+        v[4 * j + 1] += YF32 ? __uint_as_float(p.r[j].y) : bf16_hi(p.r[j].x);
+        v[4 * j + 2] += YF32 ? __uint_as_float(p.r[j].z) : bf16_lo(p.r[j].y);
+        v[4 * j + 3] += YF32 ? __uint_as_float(p.r[j].w) : bf16_hi(p.r[j].y);
       }
     }
 #pragma unroll
     for (uint32_t j = 0; j < T; ++j) {
-      if (m + j * step >= end) continue;
-      const uint64_t at = uint64_t(m + j * step) * a.y_stride + f;
-      if (a.y_f32) {
-        *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      uint4 u;
+      if constexpr (YF32) {
+        u = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
       } else {
         const __nv_bfloat162 lo = __floats2bfloat162_rn(v[4 * j], v[4 * j + 1]), hi = __floats2bfloat162_rn(v[4 * j + 2], v[4 * j + 3]);
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + at) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        u.x = *reinterpret_cast<const uint32_t*>(&lo);
+        u.y = *reinterpret_cast<const uint32_t*>(&hi);
+      }
+      if (m + j * step < end) {
+        if constexpr (YF32) *reinterpret_cast<uint4*>(y + j * down) = u;
+        else *reinterpret_cast<uint2*>(y + j * down) = make_uint2(u.x, u.y);
       }
     }
   } else {
+    const Y* const r = static_cast<const Y*>(a.residual) + uint64_t(m) * a.residual_stride + f;
+    const uint64_t r_down = uint64_t(step) * a.residual_stride;
 #pragma unroll
     for (uint32_t j = 0; j < T; ++j) {
-      const uint32_t t = m + j * step;
-      if (t >= end) continue;
-      const uint64_t at = uint64_t(t) * a.y_stride + f, rat = uint64_t(t) * a.residual_stride + f;
+      if (m + j * step >= end) break;
 #pragma unroll
       for (uint32_t i = 0; i < 4; ++i) {
-        if (f + i >= a.N) continue;
-        float u = v[4 * j + i];
-        if (a.y_f32) {
-          if (a.residual) u += static_cast<const float*>(a.residual)[rat + i];
-          static_cast<float*>(a.y)[at + i] = u;
-        } else {
-          if (a.residual) u += __bfloat162float(static_cast<const __nv_bfloat16*>(a.residual)[rat + i]);
-          static_cast<__nv_bfloat16*>(a.y)[at + i] = __float2bfloat16_rn(u);
-        }
+        if (f + i >= a.N) break;
+        const float u = a.residual ? v[4 * j + i] + static_cast<float>(r[j * r_down + i]) : v[4 * j + i];
+        if constexpr (YF32) y[j * down + i] = u; else y[j * down + i] = __float2bfloat16_rn(u);
       }
     }
   }
@@ -211,7 +231,7 @@ __device__ __forceinline__ void tile_at(const PrArgs& a, uint32_t tile, uint32_t
   tf = g * 8u + (in - tt * wide);
 }
 
-template <uint32_t BN, uint32_t NT, uint32_t CG, bool F8, bool SPLIT>
+template <uint32_t BN, uint32_t NT, uint32_t CG, bool F8, bool SPLIT, bool YF32>
 __global__ void __launch_bounds__(PrShape<BN, NT, CG, SPLIT>::kThreads, 1)
 ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const PrArgs a) {
   using S = PrShape<BN, NT, CG, SPLIT>;
@@ -227,8 +247,9 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   const uint32_t rank = SPLIT || CG == 2 ? cluster_rank() : 0u;
   uint32_t ranks = 1;
   if constexpr (SPLIT) asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+  const uint32_t share = BN / ranks;                                   // split: tokens that a rank finishes; powers of two all
   uint32_t bad = 0;
-  let_next_start();
+  if constexpr (!SPLIT) let_next_start();
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < S::kStages; ++s) { bar_init(full + 8u * s, 1); bar_init(empty + 8u * s, 1); }
@@ -239,6 +260,7 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   if (threadIdx.x == 32u * S::kTma && a.steps) { map_prefetch(&w_map); map_prefetch(&x_map); }
   fence_before();
   if constexpr (CG == 2) cluster_sync(); else __syncthreads();
+  if (SPLIT && ranks > 1) cluster_arrive();                            // waited for before the first store into another CTA
   fence_after();
   uint32_t tmem;
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
@@ -249,15 +271,39 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   const uint32_t k0 = SPLIT ? static_cast<uint32_t>(uint64_t(a.steps) * rank / ranks) : 0u;
   const uint32_t k1 = SPLIT ? static_cast<uint32_t>(uint64_t(a.steps) * (rank + 1u) / ranks) : a.steps;
 
+  // split: the tokens that this CTA finishes, and the first of a warp's
+  constexpr uint32_t kEach = BN < 64u ? 2u : 4u;                       // tokens of a warp at a time
+  uint32_t f_mine = 0, first = 0, here = 0;
+  PrColumns own;
+  PrAhead<kEach, YF32> mine;
+  if constexpr (SPLIT) {
+    uint32_t tf, tt;
+    tile_at(a, team, tf, tt);
+    const uint32_t live = min(BN, a.M - tt * BN);
+    f_mine = tf * kPrFeatures + 4u * lane;
+    first = tt * BN + rank * share;
+    here = live > rank * share ? min(share, live - rank * share) : 0u;
+  }
+
   if (warp == S::kTma) {
     if (lane == 0) {
+      uint32_t n = 0, early = 0;                                       // stages filled so far; those with W alone
+      if (SPLIT && a.settled) {
+        uint32_t tf, tt;
+        tile_at(a, team, tf, tt);
+        early = min(S::kStages, k1 - k0);
+        for (uint32_t s = 0; s < early; ++s) {
+          bar_expect(full + 8u * s, S::kStage);
+          tile_load<false>(base + s * S::kStage, &w_map, full + 8u * s, (k0 + s) * kPerRow, tf * kPrFeatures);
+        }
+      }
       wait_for_previous();
-      uint32_t n = 0;                                                  // stages filled so far
       for (uint32_t tile = team; tile < tiles; tile += teams) {
         uint32_t tf, tt;
         tile_at(a, tile, tf, tt);
         const uint32_t f = (tf * CG + (CG == 2 ? rank : 0u)) * kPrFeatures, t = tt * S::kTokens + (CG == 2 ? rank * (BN / 2u) : 0u);
-        for (uint32_t k = k0; k < k1; ++k, ++n) {
+        for (; n < early; ++n) tile_load<false>(base + n * S::kStage + S::kW, &x_map, full + 8u * n, (k0 + n) * kPerRow, t);
+        for (uint32_t k = k0 + early; k < k1; ++k, ++n) {
           const uint32_t s = n % S::kStages, round = n / S::kStages;
           if (round && !bar_wait(empty + 8u * s, (round - 1u) & 1u, bad)) break;
           if (CG == 1 || rank == 0) bar_expect(full + 8u * s, CG * S::kStage);
@@ -269,6 +315,9 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
         }
         if (bad) break;
       }
+      // The next call's CTAs come up while the last stages are worked on and the parts are added; earlier they would fetch
+      // settled weights against this call's own and be idle at its end.
+      if constexpr (SPLIT) let_next_start();
       // no copy may be in flight when the CTA ends: every filled stage has to be seen full or free
       for (uint32_t i = n > S::kStages ? n - S::kStages : 0u; i < n; ++i)
         bar_wait(empty + 8u * (i % S::kStages), (i / S::kStages) & 1u, bad);
@@ -302,12 +351,16 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
     }
   } else {
     wait_for_previous();
+    if constexpr (SPLIT) {                                             // under way while the sums are made
+      own.load(a, f_mine);
+      mine.fetch(a, first + warp, 4u * S::kTeams, first + here, f_mine);
+    }
     const uint32_t part = warp >> 2, quarter = warp & 3u;              // which tokens, which features
     uint32_t it = 0;
     for (uint32_t tile = team; tile < tiles; tile += teams, ++it) {
       uint32_t tf, tt;
       tile_at(a, tile, tf, tt);
-      const uint32_t f = (tf * CG + (CG == 2 ? rank : 0u)) * kPrFeatures + 4u * lane, t0 = tt * S::kTokens;
+      const uint32_t f = (tf * CG + (CG == 2 ? rank : 0u)) * kPrFeatures + quarter * 32u + 4u * (lane & 7u), t0 = tt * S::kTokens;
       const uint32_t live = min(S::kTokens, a.M - t0);                         // tokens of the tile
       const uint32_t acc = it % S::kAccs;
       PrColumns columns;
@@ -315,37 +368,49 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
       if (lane == 0) bar_wait(acc_full + 8u * acc, (it / S::kAccs) & 1u, bad);   // one lane polls
       __syncwarp();
       fence_after();
+      if (SPLIT && ranks > 1) cluster_wait();
       const uint32_t from = tmem + ((quarter * 32u) << 16) + acc * S::kTokens;
       constexpr uint32_t kStep = BN < kPrBlock ? BN : kPrBlock;        // tokens taken out at a time
+      // a warp's block goes through its own scratch (split: in the ring, which is done with) into rows of 32 features:
+      // lane: four features of token 4 i + lane / 8
+      const uint32_t scratch = SPLIT ? base + warp * kPrScratch : staging + warp * kPrScratch;
+      const uint32_t row = lane >> 3;
 #pragma unroll 1
       for (uint32_t c = part * kStep; c < live; c += S::kTeams * kStep) {
-        uint32_t v[kStep / 16][16];
-#pragma unroll
-        for (uint32_t h = 0; h < kStep / 16u; ++h) tmem_load16(from + c + 16u * h, v[h]);
+        uint32_t v[kStep];
+        PrAhead<kStep / 4u, YF32> ahead;
+        if constexpr (!SPLIT) ahead.fetch(a, t0 + c + row, 4u, t0 + live, f);
+        __syncwarp();
+        tmem_load(from + c, v);
         tmem_wait();
         if (k1 == k0) {                                                // K = 0: nothing was accumulated
 #pragma unroll
-          for (uint32_t h = 0; h < kStep / 16u; ++h)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) v[h][i] = 0u;
+          for (uint32_t i = 0; i < kStep; ++i) v[i] = 0u;
         }
-        const uint32_t to = SPLIT ? base + c * (kPrFeatures * 4u) : staging + part * kPrStaging;
-        if constexpr (!SPLIT) asm volatile("bar.sync %0, 128;" :: "r"(1u + part) : "memory");   // the block before is read
+        __syncwarp();                                                  // the block before is read
 #pragma unroll
-        for (uint32_t h = 0; h < kStep / 16u; ++h)
+        for (uint32_t i = 0; i < kStep; ++i)
+          asm volatile("st.shared.u32 [%0], %1;" :: "r"(scratch + i * 128u + lane * 4u), "r"(v[i]) : "memory");
+        __syncwarp();
+        float q[kStep];
 #pragma unroll
-          for (uint32_t i = 0; i < 16; ++i)
-            asm volatile("st.shared.u32 [%0], %1;" :: "r"(to + ((16u * h + i) * kPrFeatures + quarter * 32u + lane) * 4u), "r"(v[h][i]) : "memory");
-        if constexpr (!SPLIT) {
-          asm volatile("bar.sync %0, 128;" :: "r"(1u + part) : "memory");
-          constexpr uint32_t kEach = kStep / 4u;                       // tokens of a warp
-          float q[4 * kEach];
+        for (uint32_t i = 0; i < kStep / 4u; ++i)
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q[4 * i]), "=f"(q[4 * i + 1]), "=f"(q[4 * i + 2]), "=f"(q[4 * i + 3])
+                       : "r"(scratch + i * 512u + lane * 16u));
+        if constexpr (SPLIT) {                                         // to the tokens' ranks
 #pragma unroll
-          for (uint32_t i = 0; i < kEach; ++i)
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(q[4 * i]), "=f"(q[4 * i + 1]), "=f"(q[4 * i + 2]), "=f"(q[4 * i + 3])
-                         : "r"(to + ((quarter + 4u * i) * kPrFeatures + 4u * lane) * 4u));
-          if (f < a.N) finish<kEach>(a, columns, t0 + c + quarter, 4u, t0 + live, f, q);
+          for (uint32_t i = 0; i < kStep / 4u; ++i) {
+            const uint32_t t = c + 4u * i + row;
+            if (t < live)
+              asm volatile(
+                  "{\n\t.reg .b32 p;\n\t"
+                  "mapa.shared::cluster.u32 p, %0, %1;\n\t"
+                  "st.shared::cluster.v4.f32 [p], {%2, %3, %4, %5};\n\t}"
+                  :: "r"(staging + ((rank * share + (t & (share - 1u))) * kPrFeatures + quarter * 32u + (lane & 7u) * 4u) * 4u), "r"(t / share),
+                     "f"(q[4 * i]), "f"(q[4 * i + 1]), "f"(q[4 * i + 2]), "f"(q[4 * i + 3]) : "memory");
+          }
+        } else {
+          finish<kStep / 4u, YF32>(a, columns, ahead, t0 + c + row, 4u, t0 + live, f, q);
         }
       }
       if constexpr (!SPLIT) {
@@ -358,43 +423,32 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   __syncwarp();
 
   if constexpr (SPLIT) {
-    cluster_sync();                                                    // the partial sums of all ranks are in place
-    if (warp < 4) {
-      uint32_t tf, tt;
-      tile_at(a, team, tf, tt);
-      const uint32_t f = tf * kPrFeatures + 4u * lane, t0 = tt * BN, live = min(BN, a.M - t0);
-      PrColumns columns;
-      columns.load(a, f);
-      constexpr uint32_t kEach = BN < 64u ? 2u : 4u;                   // tokens of a warp at a time
-      const uint32_t step = 4u * ranks;
-      for (uint32_t t = rank * 4u + warp; t < live; t += kEach * step) {
+    if (warp >= S::kTma && ranks > 1) cluster_wait();
+    if (ranks > 1) cluster_sync(); else __syncthreads();               // all parts are in place
+    if (warp < S::kTma) {
+      constexpr uint32_t kWarps = 4u * S::kTeams;
+      for (uint32_t l = warp; l < here; l += kWarps * kEach) {
         float v[4 * kEach];
 #pragma unroll
         for (uint32_t i = 0; i < 4 * kEach; ++i) v[i] = 0.f;
-        for (uint32_t r = 0; r < ranks; r += 2) {                      // two ranks' parts under way together, added in order
-          float q[2][4 * kEach];
+        for (uint32_t r = 0; r < ranks; ++r) {
+          float q[4 * kEach];
 #pragma unroll
-          for (uint32_t p = 0; p < 2; ++p)
+          for (uint32_t j = 0; j < kEach; ++j)
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(q[4 * j]), "=f"(q[4 * j + 1]), "=f"(q[4 * j + 2]), "=f"(q[4 * j + 3])
+                         : "r"(staging + ((r * share + min(l + kWarps * j, here - 1u)) * kPrFeatures + 4u * lane) * 4u));
 #pragma unroll
-            for (uint32_t j = 0; j < kEach; ++j)
-              asm volatile(
-                  "{\n\t.reg .b32 p;\n\t"
-                  "mapa.shared::cluster.u32 p, %4, %5;\n\t"
-                  "ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [p];\n\t}"
-                  : "=f"(q[p][4 * j]), "=f"(q[p][4 * j + 1]), "=f"(q[p][4 * j + 2]), "=f"(q[p][4 * j + 3])
-                  : "r"(base + (min(t + j * step, BN - 1u) * kPrFeatures + 4u * lane) * 4u), "r"(min(r + p, ranks - 1u)) : "memory");
-#pragma unroll
-          for (uint32_t i = 0; i < 4 * kEach; ++i) {
-            v[i] += q[0][i];
-            if (r + 1 < ranks) v[i] += q[1][i];
-          }
+          for (uint32_t i = 0; i < 4 * kEach; ++i) v[i] += q[i];
         }
-        if (f < a.N) finish<kEach>(a, columns, t0 + t, step, t0 + live, f, v);
+        const PrAhead<kEach, YF32> now = mine;
+        mine.fetch(a, first + l + kWarps * kEach, kWarps, first + here, f_mine);
+        finish<kEach, YF32>(a, own, now, first + l, kWarps, first + here, f_mine, v);
       }
     }
   }
   fence_before();
-  if constexpr (SPLIT || CG == 2) cluster_sync(); else __syncthreads();   // others' shared memory is read, theirs signals ours
+  if constexpr (CG == 2) cluster_sync(); else __syncthreads();         // nothing of the pair's other CTA is under way any more
   if (warp == S::kMma) {
     fence_after();
     tmem_free<CG>(tmem, S::kCols);
@@ -434,8 +488,8 @@ static int make_map(CUtensorMap* map, const void* p, uint32_t rows, uint32_t k, 
   return rc == CUDA_SUCCESS ? ANS_OK : cuda_fail(cudaErrorInvalidValue);
 }
 
-template <uint32_t BN, uint32_t NT, uint32_t CG, bool F8, bool SPLIT>
-static int launch_product(const ans_product_desc& d, PrArgs a, uint32_t cluster, int sms, cudaStream_t st) {
+template <uint32_t BN, uint32_t NT, uint32_t CG, bool F8, bool SPLIT, bool YF32>
+static int launch_form(const ans_product_desc& d, PrArgs a, uint32_t cluster, int sms, cudaStream_t st) {
   using S = PrShape<BN, NT, CG, SPLIT>;
   CUtensorMap w_map{}, x_map{};                       // k = 0: not used
   if (d.k) {
@@ -449,10 +503,16 @@ static int launch_product(const ans_product_desc& d, PrArgs a, uint32_t cluster,
   if (tiles * cluster > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const uint32_t teams = SPLIT ? static_cast<uint32_t>(tiles)
                                : static_cast<uint32_t>(tiles < uint64_t(sms) / CG ? tiles : uint64_t(sms) / CG);
-  auto* kernel = ans_product_kernel<BN, NT, CG, F8, SPLIT>;
+  auto* kernel = ans_product_kernel<BN, NT, CG, F8, SPLIT, YF32>;
   ANSB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem)));
   const uint32_t together = SPLIT ? cluster : CG;
   return launch(kernel, dim3(teams * together), dim3(S::kThreads), S::kSmem, st, together, w_map, x_map, a);
+}
+
+template <uint32_t BN, uint32_t NT, uint32_t CG, bool F8, bool SPLIT>
+static int launch_product(const ans_product_desc& d, const PrArgs& a, uint32_t cluster, int sms, cudaStream_t st) {
+  return d.y_dtype == ANS_F32 ? launch_form<BN, NT, CG, F8, SPLIT, true>(d, a, cluster, sms, st)
+                              : launch_form<BN, NT, CG, F8, SPLIT, false>(d, a, cluster, sms, st);
 }
 
 template <bool F8>
@@ -487,6 +547,7 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   const ans_product_desc& d = *h_desc;
   if (d.dtype != ANS_BF16 && d.dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
   if (d.y_dtype != ANS_BF16 && d.y_dtype != ANS_F32) return ANS_ERR_UNSUPPORTED;
+  if (d.flags & ~ANS_PRODUCT_WEIGHTS_SETTLED) return ANS_ERR_UNSUPPORTED;
   if (d.activation < ANS_ACT_NONE || d.activation > ANS_ACT_SILU) return ANS_ERR_UNSUPPORTED;
   constexpr uint32_t kMost = 1u << 30;
   if (d.m > kMost || d.n > kMost || d.k > (1u << 22)) return ANS_ERR_UNSUPPORTED;
@@ -510,7 +571,7 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   a.residual = d.d_residual; a.y = d.d_y; a.residual_stride = d.residual_stride; a.y_stride = d.y_stride;
   a.M = d.m; a.N = d.n; a.steps = static_cast<uint32_t>((d.k * es + kPrRow - 1) / kPrRow);
   a.activation = d.activation;
-  a.y_f32 = d.y_dtype == ANS_F32;
+  a.settled = (d.flags & ANS_PRODUCT_WEIGHTS_SETTLED) != 0;
   auto four = [&](const void* p, uint64_t stride) { return !p || !((reinterpret_cast<uintptr_t>(p) | (d.m > 1 ? stride * ys : 0)) & (4 * ys - 1)); };
   a.wide = four(d.d_y, d.y_stride) && four(d.d_residual, d.residual_stride);
   a.status = d_status;

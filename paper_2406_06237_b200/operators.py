@@ -187,9 +187,15 @@ class Linear(_Handle):
     weight: bf16 (as decoded) or float8_e4m3fn (see symbols_to_e4m3).  scales: fp32, one for each
     output feature or one for all (a float or one element), or None.  bias: [out features] or None.
     activation: "none", "relu", "gelu", "gelu_tanh" or "silu".  A weight whose rows do not start on 16
-    bytes is copied once into rows that do."""
+    bytes is copied once into rows that do.
 
-    def __init__(self, weight: torch.Tensor, scales=None, bias: torch.Tensor | None = None, activation: str = "none"):
+    settled: the weight does not change any more.  The device is synchronised here, and calls may read the
+    weight before the work queued ahead of them is done (ANS_PRODUCT_WEIGHTS_SETTLED).  Leave it
+    out where the weight's buffer is decoded into again.
+    """
+
+    def __init__(self, weight: torch.Tensor, scales=None, bias: torch.Tensor | None = None, activation: str = "none",
+                 settled: bool = False):
         super().__init__(weight.device)
         _need(weight.dim() == 2, "weight must be a matrix")
         _need(weight.dtype in (torch.bfloat16, torch.float8_e4m3fn), "weight must be bf16 or float8_e4m3fn")
@@ -211,6 +217,9 @@ class Linear(_Handle):
         d.d_w_scales = scales.data_ptr() if scales is not None else None
         d.d_bias = bias.data_ptr() if bias is not None else None
         d.n, d.k, d.dtype, d.activation = n, k, _ELEMENT[weight.dtype], B.ACTIVATIONS[activation]
+        if settled:
+            torch.cuda.synchronize(self.device)
+            d.flags = B.ANS_PRODUCT_WEIGHTS_SETTLED
 
     def __call__(self, x: torch.Tensor, x_scales: torch.Tensor | None = None, residual: torch.Tensor | None = None,
                  out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
