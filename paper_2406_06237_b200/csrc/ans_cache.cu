@@ -434,9 +434,9 @@ ANS_EXPORT int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tab
   a.wide = !((reinterpret_cast<uintptr_t>(d_k_out) | reinterpret_cast<uintptr_t>(d_v_out)) & 31);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   // rows of a block: enough blocks for eight on each SM, up to 64 rows each, over which a block's look-up is spread
-  int dev = 0, sms = 0;
-  ANSB_CUDA(cudaGetDevice(&dev));
-  ANSB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  int sms = 0;
+  const int asked = ten::sm_count(&sms);
+  if (asked != ANS_OK) return asked;
   const uint64_t share = rows / (4u * static_cast<uint64_t>(sms));
   const uint32_t some = share < 4 ? 4u : share > kReadRows ? kReadRows : static_cast<uint32_t>(share);
   const dim3 grid(static_cast<unsigned>((rows + some - 1) / some), 2);

@@ -465,12 +465,13 @@ template <typename TX, typename TO, int V, int MOST, bool EVEN>
 static int launch_ring(const NormArgs& a, dim3 block, uint32_t blocks, int sms, cudaStream_t st) {
   const size_t row = size_t(a.r ? 2 : 1) * V * 16 * block.x * block.y;
   const size_t rest = EVEN ? 0 : weight_bytes<TX>(a);
-  auto* kernel = ans_rms_norm_ring_kernel<TX, TO, V, MOST, EVEN>;
+  constexpr auto kernel = ans_rms_norm_ring_kernel<TX, TO, V, MOST, EVEN>;
   while (blocks > 1 && blocks * (2 * row + rest) > kNormRing) --blocks;
   uint32_t depth = static_cast<uint32_t>((kNormRing / blocks - rest) / row);
   if (depth > 6) depth = 6;
   const size_t smem = depth * row + rest;
-  ANSB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+  const int rc = ten::allow_smem<kernel>(kNormRing);
+  if (rc != ANS_OK) return rc;
   const uint64_t need = (a.rows + block.y - 1) / block.y, have = uint64_t(sms) * blocks;
   return ten::launch(kernel, dim3(static_cast<unsigned>(need < have ? need : have)), block, smem, st, 1, a, depth);
 }
@@ -556,8 +557,8 @@ ANS_EXPORT int ans_rms_norm(const ans_norm_desc* h_desc, void* stream) {
   a.w_f32 = d.weight_dtype == ANS_F32;
   a.w_vec = !(reinterpret_cast<uintptr_t>(d.d_weight) & 15);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int dev = 0, sms = 0;
-  ANSB_CUDA(cudaGetDevice(&dev));
-  ANSB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  int sms = 0;
+  const int rc = ten::sm_count(&sms);
+  if (rc != ANS_OK) return rc;
   return d.x_dtype == ANS_F32 ? launch_norm_out<float>(a, d.out_dtype, sms, st) : launch_norm_out<__nv_bfloat16>(a, d.out_dtype, sms, st);
 }

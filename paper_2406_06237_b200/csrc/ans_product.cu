@@ -503,8 +503,9 @@ static int launch_form(const ans_product_desc& d, PrArgs a, uint32_t cluster, in
   if (tiles * cluster > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const uint32_t teams = SPLIT ? static_cast<uint32_t>(tiles)
                                : static_cast<uint32_t>(tiles < uint64_t(sms) / CG ? tiles : uint64_t(sms) / CG);
-  auto* kernel = ans_product_kernel<BN, NT, CG, F8, SPLIT, YF32>;
-  ANSB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem)));
+  constexpr auto kernel = ans_product_kernel<BN, NT, CG, F8, SPLIT, YF32>;
+  const int allowed = allow_smem<kernel>(S::kSmem);
+  if (allowed != ANS_OK) return allowed;
   const uint32_t together = SPLIT ? cluster : CG;
   return launch(kernel, dim3(teams * together), dim3(S::kThreads), S::kSmem, st, together, w_map, x_map, a);
 }
@@ -563,9 +564,9 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   if (d.k && d.n > 1 && (d.w_stride < d.k || (d.w_stride * es) % 16 || d.w_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && (d.y_stride < d.n || d.y_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && d.d_residual && (d.residual_stride < d.n || d.residual_stride > kFar)) return ANS_ERR_INVALID_ARG;
-  int dev = 0, sms = 0;
-  ANSB_CUDA(cudaGetDevice(&dev));
-  ANSB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc != ANS_OK) return rc;
   PrArgs a{};
   a.x_scales = d.d_x_scales; a.w_scales = d.d_w_scales; a.bias = d.d_bias;
   a.residual = d.d_residual; a.y = d.d_y; a.residual_stride = d.residual_stride; a.y_stride = d.y_stride;

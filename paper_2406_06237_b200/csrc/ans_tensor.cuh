@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 
+#include <atomic>
 #include <utility>
 
 #include "ans_common.cuh"
@@ -22,6 +23,31 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
 // before the work queued ahead of it is complete.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// What a launch needs to know of the current device, asked once: both are properties of the device or of the kernel on
+// it for as long as the process lives.
+constexpr int kDevices = 64;
+inline int sm_count(int* sms) {
+  static std::atomic<int> known[kDevices];
+  int dev = 0;
+  ANSB_CUDA(cudaGetDevice(&dev));
+  const bool keep = dev >= 0 && dev < kDevices;
+  if (keep && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return ANS_OK;
+  ANSB_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  if (keep) known[dev].store(*sms, std::memory_order_relaxed);
+  return ANS_OK;
+}
+template <auto KERNEL>
+inline int allow_smem(size_t most) {
+  static std::atomic<bool> done[kDevices];
+  int dev = 0;
+  ANSB_CUDA(cudaGetDevice(&dev));
+  const bool keep = dev >= 0 && dev < kDevices;
+  if (keep && done[dev].load(std::memory_order_relaxed)) return ANS_OK;
+  ANSB_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most)));
+  if (keep) done[dev].store(true, std::memory_order_relaxed);
+  return ANS_OK;
+}
 
 template <typename... P, typename... A>
 inline int launch(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, uint32_t cluster, A&&... args) {

@@ -37,9 +37,11 @@ class _Handle:
     """A device, and the status word its calls report to.
 
     A call checks its tensors' types, shapes, strides and devices; where all of them are those of the
-    handle's last call the checks' result is known and only the pointers change."""
+    handle's last call (Form in csrc/torch) the checks' result is known and only the pointers change."""
 
     def __init__(self, device):
+        from ._ans_form import Form                        # built in-tree with the library
+        self._new_form = Form
         self.device = _cuda_device(device)
         self._index = self.device.index
         self.status = torch.zeros(64, dtype=torch.int32, device=self.device)
@@ -54,11 +56,6 @@ class _Handle:
     def read_status(self) -> int:
         """Waits for the stream; ANS_STATUS_* bits that calls have set since the last look (0: all sound)."""
         return B.ans_read_status(self._status, self._enter())
-
-
-def _form(t: torch.Tensor | None):
-    """All of a tensor that checks look at."""
-    return None if t is None else (t.dtype, t.shape, t.stride(), t.device)
 
 
 def _rows(t: torch.Tensor, what: str) -> int:
@@ -87,7 +84,7 @@ class RmsNorm(_Handle):
             _need(weight.dtype in (torch.bfloat16, torch.float32), "weight must be bf16 or fp32")
         self.weight, self.eps, self.out_dtype = weight, float(eps), out_dtype
         self._8bit = out_dtype is torch.float8_e4m3fn
-        self._last = None
+        self._form = self._new_form()
         self._desc = d = B.ans_norm_desc()
         d.d_weight = weight.data_ptr() if weight is not None and weight.numel() else None
         d.weight_dtype = _ELEMENT[weight.dtype] if weight is not None else B.ANS_F32
@@ -101,16 +98,13 @@ class RmsNorm(_Handle):
         st, d = self._enter(), self._desc
         if out is None or (scales is None and self._8bit) or (summed is None and residual is not None):
             out, scales, summed = self._buffers(x, residual, out, scales, summed)
-        form = (_form(x), _form(residual), _form(out), _form(scales), _form(summed))
-        if form != self._last:
-            self._last = None
+        at = self._form.places(x, residual, out, scales, summed)
+        if at is None:
+            self._form.keep()
             self._check(x, residual, out, scales, summed)
-            self._last = form
-        d.d_x, d.d_out = x.data_ptr(), out.data_ptr()
-        if scales is not None:
-            d.d_scales = scales.data_ptr()
-        if residual is not None:
-            d.d_residual, d.d_sum = residual.data_ptr(), summed.data_ptr()
+            self._form.keep(x, residual, out, scales, summed)
+            at = self._form.places(x, residual, out, scales, summed)
+        d.d_x, d.d_residual, d.d_out, d.d_scales, d.d_sum = at
         B.ans_rms_norm(d, st)
         return out, scales, summed
 
@@ -148,7 +142,6 @@ class RmsNorm(_Handle):
             d.residual_stride, d.sum_stride = _rows(residual, "residual"), _rows(summed, "summed")
         else:
             _need(summed is None, "summed belongs to a residual")
-            d.d_residual = d.d_sum = None
         d.x_stride, d.x_dtype, d.rows, d.width = xs, _ELEMENT[dt], rows, width
         d.out_stride = _rows(out, "out")
 
@@ -211,7 +204,7 @@ class Linear(_Handle):
             bias = bias.to(device=self.device, dtype=torch.float32).contiguous()
         self.scales, self.bias, self.activation = scales, bias, activation
         self.in_features, self.out_features = k, n
-        self._last, self._copies = None, False
+        self._form, self._copies = self._new_form(), False
         self._desc = d = B.ans_product_desc()
         d.d_w, d.w_stride = self.weight.data_ptr() or None, max(self.weight.stride(0), k)
         d.d_w_scales = scales.data_ptr() if scales is not None else None
@@ -230,21 +223,17 @@ class Linear(_Handle):
         if out is None:
             _need(x.dim() == 2, "x must be [rows, in features]")
             out = torch.empty(x.shape[0], self.out_features, dtype=out_dtype, device=self.device)
-        form = (_form(x), _form(x_scales), _form(residual), _form(out))
-        if form != self._last:
-            self._last = None
+        at = self._form.places(x, x_scales, residual, out)
+        if at is None:
+            self._form.keep()
             self._check(x, x_scales, residual, out)
-            self._last = form
-        at = x.data_ptr()
-        if at % 16 or self._copies:
+            self._form.keep(x, x_scales, residual, out)
+            at = self._form.places(x, x_scales, residual, out)
+        d.d_x, d.d_x_scales, d.d_residual, d.d_y = at
+        if self._copies or at[0] % 16:
             x = _aligned(x)
-            at, d.x_stride = x.data_ptr(), max(x.stride(0), self.in_features)
-            self._last = None
-        d.d_x, d.d_y = at, out.data_ptr()
-        if x_scales is not None:
-            d.d_x_scales = x_scales.data_ptr()
-        if residual is not None:
-            d.d_residual = residual.data_ptr()
+            d.d_x, d.x_stride = x.data_ptr(), max(x.stride(0), self.in_features)
+            self._form.keep()                              # x_stride is the copy's
         B.ans_product(d, self._status, st)
         return out
 
@@ -258,7 +247,6 @@ class Linear(_Handle):
         _need(out.shape == shape, "out has the wrong shape")
         _need(dt in (torch.bfloat16, torch.float32), "the output is bf16 or fp32")
         _on_device(out, self.device, "out")
-        d.d_x_scales = d.d_residual = None
         if x_scales is not None:
             _need(x_scales.dtype is torch.float32 and x_scales.shape == shape[:1] and x_scales.is_contiguous(), "x_scales must be fp32 [rows]")
             _on_device(x_scales, self.device, "x_scales")
@@ -316,7 +304,7 @@ class PagedCache(_Handle):
         self.v_codes, self.v_scales, self.v_zeros = v_codes, v_scales, v_zeros
         self.n_pages, self.page_size, self.heads = k_codes.shape[:3]
         self.head_dim, self.group, self.bitwidth = dim, dim // groups, bitwidth
-        self._wrote = self._read = None
+        self._wrote, self._read = self._new_form(), self._new_form()
         self._desc = d = B.ans_cache_desc()
         d.d_k_codes, d.d_k_scales, d.d_k_zeros = k_codes.data_ptr(), k_scales.data_ptr(), k_zeros.data_ptr()
         d.d_v_codes, d.d_v_scales, d.d_v_zeros = v_codes.data_ptr(), v_scales.data_ptr(), v_zeros.data_ptr()
@@ -327,12 +315,14 @@ class PagedCache(_Handle):
         """k, v: [tokens, heads, head_dim], bf16 or fp32, tokens and heads at any stride; slots: [tokens]
         int64, a negative one skips its token."""
         st = self._enter()
-        form = (_form(k), _form(v), _form(slots))
-        if form != self._wrote:
-            self._wrote = None
+        at = self._wrote.places(k, v, slots)
+        if at is None:
+            self._wrote.keep()
             self._check_write(k, v, slots)
-            self._wrote = form
-        B.ans_cache_write(self._desc, k.data_ptr(), v.data_ptr(), *self._write_args, slots.data_ptr(), self._status, st)
+            self._wrote.keep(k, v, slots)
+            at = self._wrote.places(k, v, slots)
+        dtype, tokens, ks, vs = self._write_args
+        B.ans_cache_write(self._desc, at[0], at[1], dtype, tokens, ks, vs, at[2], self._status, st)
 
     def _check_write(self, k, v, slots):
         def strides(t, what):
@@ -362,18 +352,18 @@ class PagedCache(_Handle):
             _need(rows is not None, "rows is needed where no buffers are given")
             k_out = torch.empty(rows, self.heads, self.head_dim, dtype=out_dtype, device=self.device)
             v_out = torch.empty_like(k_out)
-        form = (_form(tables), _form(starts), rows, _form(k_out), _form(v_out))
-        if form != self._read:
-            self._read = None
+        at = self._read.places(tables, starts, k_out, v_out)
+        if at is None or rows != self._read_args[0]:
+            self._read.keep()
             self._check_read(tables, starts, rows, k_out, v_out)
-            self._read = form
-        (stride, pages, n), (count, dtype) = self._read_args
-        B.ans_cache_read(self._desc, tables.data_ptr(), stride, pages, n, starts.data_ptr(), count, k_out.data_ptr(), v_out.data_ptr(),
-                         dtype, self._status, st)
+            self._read.keep(tables, starts, k_out, v_out)
+            at = self._read.places(tables, starts, k_out, v_out)
+        _, stride, pages, n, count, dtype = self._read_args
+        B.ans_cache_read(self._desc, at[0], stride, pages, n, at[1], count, at[2], at[3], dtype, self._status, st)
         return k_out, v_out
 
     def _check_read(self, tables, starts, rows, k_out, v_out):
-        rows = k_out.shape[0] if rows is None else rows
+        given, rows = rows, k_out.shape[0] if rows is None else rows
         for t in (k_out, v_out):
             _need(t.dim() == 3 and t.shape[0] >= rows >= 0 and t.shape[1:] == (self.heads, self.head_dim) and t.is_contiguous(),
                   "k_out and v_out must be contiguous [rows, heads, head_dim]")
@@ -387,4 +377,4 @@ class PagedCache(_Handle):
         _need(starts.dtype is torch.int32 and starts.shape == (n + 1,) and starts.is_contiguous(), "starts must be int32 [sequences + 1]")
         _on_device(tables, self.device, "tables")
         _on_device(starts, self.device, "starts")
-        self._read_args = (tables.stride(0), pages, n), (rows, _ELEMENT[dt])
+        self._read_args = given, tables.stride(0), pages, n, rows, _ELEMENT[dt]
