@@ -20,6 +20,8 @@
 // Every wait is bounded; one that runs out sets ANS_STATUS_COPY_TIMEOUT and the kernel runs to its end.
 #include <cuda.h>
 
+#include <cmath>
+
 #include <initializer_list>
 #include <type_traits>
 
@@ -31,8 +33,6 @@ using namespace ten;
 
 constexpr uint32_t kPrRow = 128;                      // bytes of K per stage and row
 constexpr uint32_t kPrFeatures = 128;                 // features of a CTA's tile
-constexpr uint32_t kPrBlock = 32;                     // tokens that an epilogue warp takes out at a time, of its 32 features
-constexpr uint32_t kPrScratch = kPrBlock * 32 * 4;
 
 struct PrArgs {
   const float* x_scales; const float* w_scales; const float* bias;
@@ -54,11 +54,14 @@ struct PrShape {
   static constexpr uint32_t kBlockX = BN / CG * kPrRow;  // a pair's CTAs hold half of the tokens each
   static constexpr uint32_t kX = NT * kBlockX;
   static constexpr uint32_t kStage = kW + kX;
-  static constexpr uint32_t kTeams = SPLIT && BN <= 64u ? 1u : 2u;    // teams of four epilogue warps, each with its part of the tokens
+  static constexpr uint32_t kTeams = !SPLIT ? 4u : BN <= 64u ? 1u : 2u;    // teams of four epilogue warps, each with its part of the tokens
+  // tokens that an epilogue warp takes out at a time, of its 32 features, and the bytes of such a block
+  static constexpr uint32_t kBlock = !SPLIT || BN < 32u ? 16u : 32u;
+  static constexpr uint32_t kScratch = kBlock * 32u * 4u;
   static constexpr uint32_t kTma = 4u * kTeams, kMma = kTma + 1u;     // the warps after them: copies, matrix instructions
   static constexpr uint32_t kThreads = 32u * (kMma + 1u);
   // whole: a block for each epilogue warp; split: what the cluster's CTAs send to this one
-  static constexpr uint32_t kStagingBytes = SPLIT ? BN * kPrFeatures * 4u : 4u * kTeams * kPrScratch;
+  static constexpr uint32_t kStagingBytes = SPLIT ? BN * kPrFeatures * 4u : 4u * kTeams * kScratch;
   // Up to 64 tokens a CTA takes half of an SM's shared memory at most, so that the next call's CTAs can start
   // beside it and fetch their weights; with more the ring has to be long enough for the matrix instructions' pace.
   static constexpr uint32_t kRoom = SPLIT && BN <= 64u ? 112u * 1024u : 227u * 1024u;
@@ -363,25 +366,29 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
       const uint32_t f = (tf * CG + (CG == 2 ? rank : 0u)) * kPrFeatures + quarter * 32u + 4u * (lane & 7u), t0 = tt * S::kTokens;
       const uint32_t live = min(S::kTokens, a.M - t0);                         // tokens of the tile
       const uint32_t acc = it % S::kAccs;
+      constexpr uint32_t kStep = S::kBlock;
+      const uint32_t row = lane >> 3;
       PrColumns columns;
-      if constexpr (!SPLIT) columns.load(a, f);
+      PrAhead<kStep / 4u, YF32> next;                                  // a block ahead of the sums
+      if constexpr (!SPLIT) {
+        columns.load(a, f);
+        next.fetch(a, t0 + part * kStep + row, 4u, t0 + live, f);
+      }
       if (lane == 0) bar_wait(acc_full + 8u * acc, (it / S::kAccs) & 1u, bad);   // one lane polls
       __syncwarp();
       fence_after();
       if (SPLIT && ranks > 1) cluster_wait();
       const uint32_t from = tmem + ((quarter * 32u) << 16) + acc * S::kTokens;
-      constexpr uint32_t kStep = BN < kPrBlock ? BN : kPrBlock;        // tokens taken out at a time
       // a warp's block goes through its own scratch (split: in the ring, which is done with) into rows of 32 features:
       // lane: four features of token 4 i + lane / 8
-      const uint32_t scratch = SPLIT ? base + warp * kPrScratch : staging + warp * kPrScratch;
-      const uint32_t row = lane >> 3;
+      const uint32_t scratch = SPLIT ? base + warp * S::kScratch : staging + warp * S::kScratch;
 #pragma unroll 1
       for (uint32_t c = part * kStep; c < live; c += S::kTeams * kStep) {
         uint32_t v[kStep];
-        PrAhead<kStep / 4u, YF32> ahead;
-        if constexpr (!SPLIT) ahead.fetch(a, t0 + c + row, 4u, t0 + live, f);
         __syncwarp();
         tmem_load(from + c, v);
+        const PrAhead<kStep / 4u, YF32> now = next;
+        if constexpr (!SPLIT) next.fetch(a, t0 + c + S::kTeams * kStep + row, 4u, t0 + live, f);
         tmem_wait();
         if (k1 == k0) {                                                // K = 0: nothing was accumulated
 #pragma unroll
@@ -410,7 +417,7 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
                      "f"(q[4 * i]), "f"(q[4 * i + 1]), "f"(q[4 * i + 2]), "f"(q[4 * i + 3]) : "memory");
           }
         } else {
-          finish<kStep / 4u, YF32>(a, columns, ahead, t0 + c + row, 4u, t0 + live, f, q);
+          finish<kStep / 4u, YF32>(a, columns, now, t0 + c + row, 4u, t0 + live, f, q);
         }
       }
       if constexpr (!SPLIT) {
@@ -516,26 +523,58 @@ static int launch_product(const ans_product_desc& d, const PrArgs& a, uint32_t c
                               : launch_form<BN, NT, CG, F8, SPLIT, false>(d, a, cluster, sms, st);
 }
 
+// What a form takes, in us, by a model fitted to sweeps on a B200 (both types, 1 to 4096 tokens, 1000 to 8192
+// features, K of 512 to 8192; within a fifth of most of what was measured, and the order of the forms is what counts):
+// about 2 us for the launch and its way to the first stage, the stages at the rate at which a CTA takes them in, and the
+// tile's end.  A CTA takes in its ring every 1.36 us, the way from memory, and an SM 118 GB/s at most.
+struct PrChoice {
+  float us = 1e30f;
+  uint32_t tokens = 0, split = 0;                      // split = 0: the whole form
+};
+
+// The split form: every CTA one part of one tile; two CTAs an SM up to 64 tokens.
+template <uint32_t BN>
+static void weigh_split(const ans_product_desc& d, const PrArgs& a, int sms, PrChoice& best) {
+  using S = PrShape<BN, 1, 1, true>;
+  constexpr float kEnd = BN == 16 ? 1.2f : BN == 32 ? 1.5f : BN == 64 ? 2.8f : 3.5f;
+  constexpr float kRing = S::kStages * S::kStage / 1.36e3f;           // GB/s
+  const uint64_t tiles = uint64_t((d.n + 127) / 128) * ((d.m + BN - 1) / BN), slots = uint64_t(sms) * (BN <= 64 ? 2 : 1);
+  // Clusters of 8 with an SM for each CTA do not all fit the GPU's groups of SMs at once: 100 x 2048 x 8192 24 us against
+  // 15 in fours.
+  for (uint32_t split = 1; split <= (BN <= 64 ? 8u : 4u) && (split == 1 || split <= a.steps); split *= 2) {
+    const uint64_t ctas = tiles * split, waves = (ctas + slots - 1) / slots;
+    const uint64_t beside = waves > 1 ? slots / sms : (ctas + sms - 1) / sms;   // CTAs of an SM
+    const float rate = fminf(kRing, 118.f / beside);
+    const float us = 2.f + waves * (kEnd + (a.steps + split - 1) / split * (S::kStage / 1e3f) / rate);
+    if (us < best.us) best = {us, BN, split};
+  }
+}
+
 template <bool F8>
 static int choose_product(const ans_product_desc& d, const PrArgs& a, int sms, cudaStream_t st) {
-  // Few tiles: K is split so that all SMs have a part of the work, at least two stages each.
-  auto split_of = [&](uint32_t bn) {
-    const uint64_t tiles = uint64_t((d.n + 127) / 128) * ((d.m + bn - 1) / bn);
-    uint32_t s = 1;
-    while (s < 8 && tiles * s * 2 <= uint64_t(sms) && a.steps >= 4 * s) s *= 2;
-    return s;
-  };
-  if (d.m <= 16) return launch_product<16, 1, 1, F8, true>(d, a, split_of(16), sms, st);
-  if (d.m <= 32) return launch_product<32, 1, 1, F8, true>(d, a, split_of(32), sms, st);
-  if (d.m <= 64) return launch_product<64, 1, 1, F8, true>(d, a, split_of(64), sms, st);
-  const uint64_t tiles = uint64_t((d.n + 127) / 128) * ((d.m + 127) / 128);
-  if (tiles <= uint64_t(sms)) return launch_product<128, 1, 1, F8, true>(d, a, split_of(128), sms, st);
-  // Tiles of 512 tokens read W once for both halves and move a quarter less into shared memory: 8192^3 in bf16 860 us,
-  // 895 with 256.  They are taken where they need no more rounds over the pairs of SMs (counted in 256s).
-  const uint64_t pairs = sms / 2, wide_f = (d.n + 255) / 256;
-  auto rounds = [&](uint32_t tokens) { return (wide_f * ((d.m + tokens - 1) / tokens) + pairs - 1) / pairs; };
-  if (2 * rounds(512) <= rounds(256)) return launch_product<256, 2, 2, F8, false>(d, a, 1, sms, st);
-  return launch_product<256, 1, 2, F8, false>(d, a, 1, sms, st);
+  PrChoice best;
+  weigh_split<16>(d, a, sms, best);
+  if (d.m > 16) weigh_split<32>(d, a, sms, best);
+  if (d.m > 32) weigh_split<64>(d, a, sms, best);
+  if (d.m > 64) weigh_split<128>(d, a, sms, best);
+  if (d.m > 64) {
+    // The whole forms on pairs of SMs: a stage of 256 tokens 0.31 us, of 512 tokens 0.55 us (they read W once for both
+    // halves and move a quarter less into shared memory, but nothing runs under a tile's end): 8192^3 in bf16 power-
+    // capped 830 us in 512s, 900 in 256s; 4096 x 4096 x 1024 43 and 38.
+    const uint64_t pairs = sms / 2, wide_f = (d.n + 255) / 256;
+    auto rounds = [&](uint32_t tokens) { return static_cast<float>((wide_f * ((d.m + tokens - 1) / tokens) + pairs - 1) / pairs); };
+    const float us256 = 6.5f + rounds(256) * a.steps * 0.31f, us512 = 3.5f + rounds(512) * (a.steps * 0.55f + 5.f);
+    if (us256 < best.us) best = {us256, 256, 0};
+    if (us512 < best.us) best = {us512, 512, 0};
+  }
+  switch (best.tokens) {
+    case 16: return launch_product<16, 1, 1, F8, true>(d, a, best.split, sms, st);
+    case 32: return launch_product<32, 1, 1, F8, true>(d, a, best.split, sms, st);
+    case 64: return launch_product<64, 1, 1, F8, true>(d, a, best.split, sms, st);
+    case 128: return launch_product<128, 1, 1, F8, true>(d, a, best.split, sms, st);
+    case 256: return launch_product<256, 1, 2, F8, false>(d, a, 1, sms, st);
+    default: return launch_product<256, 2, 2, F8, false>(d, a, 1, sms, st);
+  }
 }
 
 }  // namespace ansb

@@ -20,7 +20,7 @@ def integers(shape, most, dtype, seed):
 # every tile form, its edges, and lengths of K around a stage (64 bf16 or 128 e4m3) and a split of it
 SIZES = [(1, 1, 1), (1, 128, 64), (2, 130, 65), (16, 257, 512), (17, 64, 1000), (31, 1000, 2048), (33, 129, 130), (64, 128, 4096),
          (65, 300, 200), (100, 1000, 2048), (128, 256, 128), (129, 128, 256), (333, 1000, 2048), (500, 2500, 72), (777, 3001, 264),
-         (1100, 2048, 640), (2047, 1025, 1024)]
+         (1100, 2048, 640), (2047, 1025, 1024), (1030, 8200, 4096), (4100, 600, 128), (100, 2048, 8192)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, E4M3])
