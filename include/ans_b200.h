@@ -417,8 +417,8 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
 
 /* ------------------------------------------------------------------------------------
  * The operators around a product with decoded weights.
- * All three take strides in ELEMENTS, enqueue one kernel on `stream` and return without
- * waiting; they need no workspace and keep nothing from one call for the next.  Sizes of
+ * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where X's rows
+ * start off 16 bytes) and return without waiting; they keep nothing from one call for the next.  Sizes of
  * zero are fine (nothing is launched).  Unless said otherwise, outputs do not overlap inputs.
  * ------------------------------------------------------------------------------------ */
 
@@ -462,8 +462,9 @@ int ans_rms_norm(const ans_norm_desc* h_desc, void* stream);
  * X and W are both ANS_BF16 (weights as the decode calls write them) or both ANS_E4M3 (rows of
  * ans_rms_norm; symbols q - zero_point of weights of up to 4 bits are integers of at most 15 and
  * exact in e4m3).  The epilogue works in fp32 and rounds once.
- * d_x and d_w 16-byte aligned, their strides multiples of 16 bytes; columns from k on are never
- * used.  y and residual of any alignment; d_residual may be d_y (same stride).
+ * d_w 16-byte aligned, its stride a multiple of 16 bytes; columns from k on are never used.  Where d_x or
+ * its stride are not so, the rows of X are first copied (a second kernel) into d_room, 16-byte aligned, of
+ * ans_product_room_bytes() bytes, which is free again when the call's work is done.  y and residual of any alignment; d_residual may be d_y (same stride).
  * d_status as for the decode calls (ANS_STATUS_COPY_TIMEOUT).
  */
 typedef struct ans_product_desc {
@@ -480,11 +481,15 @@ typedef struct ans_product_desc {
   int32_t      y_dtype;           /* ANS_BF16 or ANS_F32                                     */
   int32_t      activation;        /* ANS_ACT_*                                               */
   uint32_t     flags;             /* ANS_PRODUCT_*, or 0                                     */
+  void*        d_room;            /* see above; NULL where X's rows start on 16 bytes        */
+  uint64_t     room_bytes;
 } ans_product_desc;
 /* The caller knows that d_w was on the device before the work queued ahead of this call began, and that
  * that work does not write it: the call may then read W before that work is done. */
 #define ANS_PRODUCT_WEIGHTS_SETTLED 1u
 int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
+/* Bytes of d_room that a call with this X needs (from d_x, x_stride, m, k and dtype); 0: none. */
+int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out);
 
 /*
  * A paged cache of keys and values, quantised as it is written.  Every group of `group` values of

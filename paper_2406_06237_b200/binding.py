@@ -37,7 +37,7 @@ EXPORTS = [
     "ans_histogram_device", "ans_entropy_device", "ans_normalize_freqs_device",
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
-    "ans_rms_norm", "ans_product", "ans_cache_write", "ans_cache_read",
+    "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_cache_write", "ans_cache_read",
 ]
 
 
@@ -72,6 +72,7 @@ class ans_product_desc(ctypes.Structure):
         ("residual_stride", ctypes.c_uint64), ("y_stride", ctypes.c_uint64), ("m", ctypes.c_uint32),
         ("n", ctypes.c_uint32), ("k", ctypes.c_uint32), ("dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
         ("activation", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("d_room", ctypes.c_void_p), ("room_bytes", ctypes.c_uint64),
     ]
 
 
@@ -137,6 +138,7 @@ def lib():
         L.ans_encode_quads_device.argtypes = [vp, u64, vp, i32, u32, u32, vp, u64, vp, vp, vp, sz, vp, vp]
         L.ans_rms_norm.argtypes = [P(ans_norm_desc), vp]
         L.ans_product.argtypes = [P(ans_product_desc), vp, vp]
+        L.ans_product_room_bytes.argtypes = [P(ans_product_desc), P(sz)]
         L.ans_cache_write.argtypes = [P(ans_cache_desc), vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, vp]
         L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
         _LIB = L
@@ -364,6 +366,12 @@ def ans_product(h_desc: ans_product_desc, d_status: int, stream: int = 0) -> Non
     rc = (_LIB or lib()).ans_product(h_desc, d_status, stream)
     if rc:
         _check(rc, "ans_product")
+
+
+def ans_product_room_bytes(h_desc: ans_product_desc) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ans_product_room_bytes(h_desc, ctypes.byref(out)), "ans_product_room_bytes")
+    return out.value
 
 
 def ans_cache_write(h_desc: ans_cache_desc, d_k: int, d_v: int, dtype: int, tokens: int, k_strides, v_strides,

@@ -464,6 +464,32 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   if (lane == 0 && bad) atomicOr(a.status, ANS_STATUS_COPY_TIMEOUT);
 }
 
+// Rows of X that start anywhere into rows that start on 16 bytes: 16 bytes of a row a thread, element by element (the
+// elements' neighbours come out of L1).  T: an element's bits.
+template <typename T>
+__global__ void __launch_bounds__(256) ans_product_rows_kernel(const T* x, uint64_t x_stride, uint4* room, uint32_t m, uint32_t k, uint32_t pieces) {
+  constexpr uint32_t kIn = 16 / sizeof(T);
+  let_next_start();
+  const uint64_t i = uint64_t(blockIdx.x) * 256u + threadIdx.x;
+  wait_for_previous();
+  const uint64_t row = i / pieces;
+  if (row >= m) return;
+  const uint32_t e = static_cast<uint32_t>(i - row * pieces) * kIn;
+  const T* const p = x + row * x_stride + e;
+  T v[kIn];
+#pragma unroll
+  for (uint32_t j = 0; j < kIn; ++j) v[j] = e + j < k ? p[j] : T(0);
+  uint4 out;
+  uint32_t* const w = &out.x;
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j) {
+    w[j] = 0;
+#pragma unroll
+    for (uint32_t b = 0; b < kIn / 4; ++b) w[j] |= uint32_t(v[j * (kIn / 4) + b]) << (8 * sizeof(T) * b);
+  }
+  room[i] = out;
+}
+
 // ---- host side -----------------------------------------------------------------------------
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -581,10 +607,24 @@ static int choose_product(const ans_product_desc& d, const PrArgs& a, int sms, c
 
 using namespace ansb;
 
+// whether TMA can read X's rows
+static bool rows_fit(const ans_product_desc& d, uint64_t es) {
+  return !(reinterpret_cast<uintptr_t>(d.d_x) & 15) && (d.m <= 1 || !((d.x_stride * es) & 15));
+}
+static uint64_t room_row(const ans_product_desc& d, uint64_t es) { return (d.k * es + 15) & ~uint64_t(15); }
+
+ANS_EXPORT int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out) {
+  if (!h_desc || !h_bytes_out) return ANS_ERR_INVALID_ARG;
+  if (h_desc->dtype != ANS_BF16 && h_desc->dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
+  const uint64_t es = h_desc->dtype == ANS_E4M3 ? 1 : 2;
+  *h_bytes_out = rows_fit(*h_desc, es) ? 0 : h_desc->m * room_row(*h_desc, es);
+  return ANS_OK;
+}
+
 ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream) {
   ApiRange range("ans_product");
   if (!h_desc || !d_status) return ANS_ERR_INVALID_ARG;
-  const ans_product_desc& d = *h_desc;
+  ans_product_desc d = *h_desc;
   if (d.dtype != ANS_BF16 && d.dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
   if (d.y_dtype != ANS_BF16 && d.y_dtype != ANS_F32) return ANS_ERR_UNSUPPORTED;
   if (d.flags & ~ANS_PRODUCT_WEIGHTS_SETTLED) return ANS_ERR_UNSUPPORTED;
@@ -594,15 +634,31 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   if (d.m == 0 || d.n == 0) return ANS_OK;
   if (!d.d_y || (d.k && (!d.d_x || !d.d_w))) return ANS_ERR_INVALID_ARG;
   const uint64_t es = d.dtype == ANS_E4M3 ? 1 : 2, ys = d.y_dtype == ANS_F32 ? 4 : 2;
-  if ((reinterpret_cast<uintptr_t>(d.d_x) | reinterpret_cast<uintptr_t>(d.d_w)) & 15) return ANS_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(d.d_w) & 15) || (reinterpret_cast<uintptr_t>(d.d_x) & (es - 1))) return ANS_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_residual)) & (ys - 1)) return ANS_ERR_INVALID_ARG;
   for (const float* p : {d.d_x_scales, d.d_w_scales, d.d_bias})
     if (reinterpret_cast<uintptr_t>(p) & 3) return ANS_ERR_INVALID_ARG;
   constexpr uint64_t kFar = uint64_t(1) << 36;
-  if (d.k && d.m > 1 && (d.x_stride < d.k || (d.x_stride * es) % 16 || d.x_stride > kFar)) return ANS_ERR_INVALID_ARG;
+  if (d.k && d.m > 1 && (d.x_stride < d.k || d.x_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.k && d.n > 1 && (d.w_stride < d.k || (d.w_stride * es) % 16 || d.w_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && (d.y_stride < d.n || d.y_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && d.d_residual && (d.residual_stride < d.n || d.residual_stride > kFar)) return ANS_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (d.k && !rows_fit(d, es)) {
+    const uint64_t row = room_row(d, es);
+    if (!d.d_room || d.room_bytes < d.m * row) return ANS_ERR_BUFFER_TOO_SMALL;
+    if (reinterpret_cast<uintptr_t>(d.d_room) & 15) return ANS_ERR_INVALID_ARG;
+    const uint64_t blocks = (d.m * (row / 16) + 255) / 256;
+    if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+    const uint32_t pieces = static_cast<uint32_t>(row / 16);
+    uint4* const room = static_cast<uint4*>(d.d_room);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    const int rc = es == 1 ? launch(ans_product_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, static_cast<const uint8_t*>(d.d_x), d.x_stride, room, d.m, d.k, pieces)
+                           : launch(ans_product_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, static_cast<const uint16_t*>(d.d_x), d.x_stride, room, d.m, d.k, pieces);
+    if (rc != ANS_OK) return rc;
+    d.d_x = room;
+    d.x_stride = row / es;
+  }
   int sms = 0;
   const int rc = sm_count(&sms);
   if (rc != ANS_OK) return rc;
@@ -615,6 +671,5 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   auto four = [&](const void* p, uint64_t stride) { return !p || !((reinterpret_cast<uintptr_t>(p) | (d.m > 1 ? stride * ys : 0)) & (4 * ys - 1)); };
   a.wide = four(d.d_y, d.y_stride) && four(d.d_residual, d.residual_stride);
   a.status = d_status;
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   return d.dtype == ANS_E4M3 ? choose_product<true>(d, a, sms, st) : choose_product<false>(d, a, sms, st);
 }

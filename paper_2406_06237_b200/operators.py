@@ -163,15 +163,13 @@ def _fits(t: torch.Tensor) -> bool:
     return (one == 1 or width <= 1) and (rows <= 1 or stride >= width and stride * t.element_size() % 16 == 0)
 
 
-def _aligned(t: torch.Tensor) -> torch.Tensor:
-    """t, or a copy of it, with contiguous rows that start on 16 bytes."""
-    if t.data_ptr() % 16 == 0 and _fits(t):
-        return t
+def _padded(t: torch.Tensor) -> torch.Tensor:
+    """A copy of t with rows that start on 16 bytes."""
+    rows, width = t.shape
     pad = 16 // t.element_size()
-    room = torch.empty(t.shape[0], (t.shape[1] + pad - 1) // pad * pad, dtype=t.dtype, device=t.device)
-    room = room[:, :t.shape[1]]
-    room.copy_(t)
-    return room
+    room = torch.empty((rows, max(width + pad - 1, 1) // pad * pad), dtype=t.dtype, device=t.device)
+    room = room.as_strided((rows, width), (room.shape[1], 1))
+    return room.copy_(t)
 
 
 class Linear(_Handle):
@@ -194,7 +192,7 @@ class Linear(_Handle):
         _need(weight.dtype in (torch.bfloat16, torch.float8_e4m3fn), "weight must be bf16 or float8_e4m3fn")
         _need(activation in B.ACTIVATIONS, f"activation {activation!r} is not one of {', '.join(B.ACTIVATIONS)}")
         n, k = weight.shape
-        self.weight = _aligned(weight)
+        self.weight = weight if _fits(weight) and weight.data_ptr() % 16 == 0 else _padded(weight)
         if scales is not None:
             scales = torch.as_tensor(scales, dtype=torch.float32, device=self.device).reshape(-1)
             _need(scales.numel() in (1, n), "scales must be one or one for each output feature")
@@ -204,7 +202,7 @@ class Linear(_Handle):
             bias = bias.to(device=self.device, dtype=torch.float32).contiguous()
         self.scales, self.bias, self.activation = scales, bias, activation
         self.in_features, self.out_features = k, n
-        self._form, self._copies = self._new_form(), False
+        self._form, self._lies_off = self._new_form(), False
         self._desc = d = B.ans_product_desc()
         d.d_w, d.w_stride = self.weight.data_ptr() or None, max(self.weight.stride(0), k)
         d.d_w_scales = scales.data_ptr() if scales is not None else None
@@ -218,7 +216,7 @@ class Linear(_Handle):
                  out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """x: [rows, in features] of the weight's type; x_scales: [rows] fp32.  Returns out (bf16 or fp32,
         [rows, out features]), the given buffer if there is one; residual is of its type and may be out
-        itself.  An x whose rows do not start on 16 bytes is copied first."""
+        itself.  An x whose rows do not start on 16 bytes is laid out in fresh memory first."""
         st, d = self._enter(), self._desc
         if out is None:
             _need(x.dim() == 2, "x must be [rows, in features]")
@@ -230,10 +228,9 @@ class Linear(_Handle):
             self._form.keep(x, x_scales, residual, out)
             at = self._form.places(x, x_scales, residual, out)
         d.d_x, d.d_x_scales, d.d_residual, d.d_y = at
-        if self._copies or at[0] % 16:
-            x = _aligned(x)
-            d.d_x, d.x_stride = x.data_ptr(), max(x.stride(0), self.in_features)
-            self._form.keep()                              # x_stride is the copy's
+        if self._lies_off or at[0] % 16:
+            room = torch.empty(B.ans_product_room_bytes(d), dtype=torch.uint8, device=self.device)
+            d.d_room, d.room_bytes = room.data_ptr(), room.numel()
         B.ans_product(d, self._status, st)
         return out
 
@@ -254,8 +251,8 @@ class Linear(_Handle):
             _need(residual.dtype is dt and residual.shape == shape, "residual and out differ")
             _on_device(residual, self.device, "residual")
             d.residual_stride = _rows(residual, "residual")
-        self._copies = not _fits(x)
-        d.x_stride, d.m = max(x.stride(0), self.in_features), shape[0]
+        d.x_stride, d.m = _rows(x, "x"), shape[0]
+        self._lies_off = not _fits(x)
         d.y_stride, d.y_dtype = _rows(out, "out"), _ELEMENT[dt]
 
 

@@ -89,6 +89,11 @@ def test_strides_and_places(m, n, k, dtype):
             assert f(x, residual=y, out=y) is y
             assert torch.equal(y, expect)
             assert int(whole.isnan().sum()) == m * pad
+    # x at an odd place, and with rows that do not start on 16 bytes
+    for off, cols in ((1, k), (8, k), (0, k - 3), (5, k - 7)):
+        odd = torch.full((m, k + 21), float("nan"), device="cuda").to(dtype)[:, off:off + cols]
+        odd.copy_(x[:, :cols])
+        assert torch.equal(Linear(w[:, :cols])(odd, out_dtype=F32), (odd.double() @ w[:, :cols].double().T).float())
     # a K that is no multiple of 16 bytes, contiguous: copied
     x2, w2 = integers((m, k + 1), 4, dtype, 4), integers((n, k + 1), 4, dtype, 5)
     assert torch.equal(Linear(w2)(x2, out_dtype=F32), (x2.double() @ w2.double().T).float())
@@ -167,7 +172,7 @@ def test_refusals():
     y = torch.empty(4, 64, device="cuda")
     d.d_x, d.x_stride, d.m, d.d_y, d.y_stride, d.y_dtype = x.data_ptr(), 128, 4, y.data_ptr(), 64, ans.ANS_F32
     ans.binding.ans_product(d, f.status.data_ptr())
-    for field, value in (("d_x", x.data_ptr() + 2), ("x_stride", 127), ("x_stride", 132), ("w_stride", 0), ("y_stride", 63), ("d_y", None),
+    for field, value in (("d_x", x.data_ptr() + 2), ("d_x", x.data_ptr() + 1), ("x_stride", 127), ("x_stride", 132), ("w_stride", 0), ("y_stride", 63), ("d_y", None),
                          ("d_y", y.data_ptr() + 2), ("dtype", ans.ANS_F32), ("y_dtype", ans.ANS_E4M3), ("activation", 5), ("k", 1 << 23), ("m", 1 << 31)):
         e = ans.binding.ans_product_desc.from_buffer_copy(d)
         setattr(e, field, value)

@@ -6,7 +6,7 @@ import pytest
 import paper_2406_06237_b200 as ans
 from paper_2406_06237_b200 import binding as B
 
-INVALID, UNSUPPORTED = ans.ANS_ERR_INVALID_ARG, ans.ANS_ERR_UNSUPPORTED
+INVALID, UNSUPPORTED, TOO_SMALL = ans.ANS_ERR_INVALID_ARG, ans.ANS_ERR_UNSUPPORTED, ans.ANS_ERR_BUFFER_TOO_SMALL
 P = 1 << 20                                              # an address on every boundary asked for
 
 
@@ -38,13 +38,27 @@ def product(status=P, **kw):
 
 
 @pytest.mark.parametrize("kw,rc", [
-    (dict(d_x=None), INVALID), (dict(d_w=None), INVALID), (dict(d_y=None), INVALID), (dict(status=None), INVALID), (dict(d_x=P + 8), INVALID),
+    (dict(d_x=None), INVALID), (dict(d_w=None), INVALID), (dict(d_y=None), INVALID), (dict(status=None), INVALID), (dict(d_x=P + 8), TOO_SMALL), (dict(d_x=P + 1), INVALID),
     (dict(d_w=P + 2), INVALID), (dict(d_y=P + 1), INVALID), (dict(d_residual=P + 1), INVALID), (dict(d_bias=P + 2), INVALID), (dict(x_stride=63), INVALID),
-    (dict(x_stride=68), INVALID), (dict(w_stride=0), INVALID), (dict(y_stride=31), INVALID), (dict(d_residual=P, residual_stride=5), INVALID),
+    (dict(x_stride=68), TOO_SMALL), (dict(x_stride=68, d_room=P, room_bytes=4 * 128 - 1), TOO_SMALL), (dict(x_stride=68, d_room=P + 8, room_bytes=512), INVALID), (dict(w_stride=0), INVALID), (dict(y_stride=31), INVALID), (dict(d_residual=P, residual_stride=5), INVALID),
     (dict(dtype=ans.ANS_F32), UNSUPPORTED), (dict(y_dtype=ans.ANS_E4M3), UNSUPPORTED), (dict(activation=5), UNSUPPORTED), (dict(activation=-1), UNSUPPORTED),
     (dict(flags=2), UNSUPPORTED), (dict(k=(1 << 22) + 1), UNSUPPORTED), (dict(m=(1 << 30) + 1), UNSUPPORTED), (dict(m=0, d_x=None), 0), (dict(n=0, d_w=None), 0)])
 def test_product(kw, rc):
     assert product(**kw) == rc
+
+
+def test_product_room():
+    def room(**kw):
+        d = B.ans_product_desc(d_x=P, x_stride=64, m=4, k=64, dtype=ans.ANS_BF16)
+        for k, v in kw.items():
+            setattr(d, k, v)
+        return ans.binding.ans_product_room_bytes(d)
+    assert room() == room(m=1, x_stride=3) == room(dtype=ans.ANS_E4M3) == 0
+    assert room(x_stride=65) == room(d_x=P + 2) == 4 * 128 and room(x_stride=65, k=61) == 4 * 128 and room(x_stride=65, k=56) == 4 * 112
+    assert room(dtype=ans.ANS_E4M3, x_stride=65, k=33) == 4 * 48
+    with pytest.raises(ans.AnsError):
+        room(dtype=ans.ANS_U8)
+    assert ans.lib().ans_product_room_bytes(None, None) == INVALID
 
 
 def cache_desc(**kw):
@@ -90,11 +104,11 @@ def test_descriptors_have_the_header_layout(tmp_path):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     c = tmp_path / "sizes.c"
     c.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "ans_b200.h"\nint main(void) { printf("%zu %zu %zu %zu %zu %zu\\n", sizeof(ans_norm_desc), '
-                 "offsetof(ans_norm_desc, out_dtype), sizeof(ans_product_desc), offsetof(ans_product_desc, flags), sizeof(ans_cache_desc), "
+                 "offsetof(ans_norm_desc, out_dtype), sizeof(ans_product_desc), offsetof(ans_product_desc, room_bytes), sizeof(ans_cache_desc), "
                  "offsetof(ans_cache_desc, bitwidth)); return 0; }\n")
     subprocess.check_call(["gcc", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "sizes"), str(c)])
     got = [int(v) for v in subprocess.check_output([str(tmp_path / "sizes")]).split()]
-    assert got == [ctypes.sizeof(B.ans_norm_desc), B.ans_norm_desc.out_dtype.offset, ctypes.sizeof(B.ans_product_desc), B.ans_product_desc.flags.offset,
+    assert got == [ctypes.sizeof(B.ans_norm_desc), B.ans_norm_desc.out_dtype.offset, ctypes.sizeof(B.ans_product_desc), B.ans_product_desc.room_bytes.offset,
                    ctypes.sizeof(B.ans_cache_desc), B.ans_cache_desc.bitwidth.offset]
 
 
