@@ -51,6 +51,11 @@ __device__ __forceinline__ void put1(void* p, int i, float v) {
   else if constexpr (sizeof(T) == 2) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
   else static_cast<float*>(p)[i] = v;
 }
+template <typename T>
+__device__ __forceinline__ void copy1(void* to, int i, const void* from, int j) {
+  using Bits = std::conditional_t<sizeof(T) == 1, uint8_t, std::conditional_t<sizeof(T) == 2, uint16_t, uint32_t>>;
+  static_cast<Bits*>(to)[i] = static_cast<const Bits*>(from)[j];
+}
 template <typename T, int H>
 __device__ __forceinline__ void put_all(void* p, int i, const Two (&v)[H]) {
   if constexpr (sizeof(T) == 4) {
@@ -150,14 +155,22 @@ struct NormRow {
   const NormArgs& a;
   int t, T, width, phase;
   bool edge;                       // among the first or last rows, whose end vectors can reach past the matrices
-  const char* x; const char* r; char* out; char* sum;
-  __device__ __forceinline__ NormRow(const NormArgs& args, uint32_t thread, uint32_t threads)
-      : a(args), t(static_cast<int>(thread)), T(static_cast<int>(threads)), width(static_cast<int>(args.width)), phase(0), edge(true) {}
+  const char* x; const char* r; char* out; char* sum;          // the row
+  const char* x0; const char* r0; char* out0; char* sum0;      // the thread's vector 0 of it
+  char* ends;                      // this warp's 128 bytes of shared memory for the row's end vectors: two of h, two of y
+  __device__ __forceinline__ NormRow(const NormArgs& args, uint32_t thread, uint32_t threads, char* scratch)
+      : a(args), t(static_cast<int>(thread)), T(static_cast<int>(threads)), width(static_cast<int>(args.width)), phase(0), edge(true), ends(scratch) {}
   __device__ __forceinline__ void at(uint64_t row) {
     x = a.x + row * a.x_step;
     r = a.r + row * a.r_step;
     out = a.out + row * a.out_step;
     sum = a.sum + row * a.sum_step;
+    if constexpr (EVEN) {                                         // these are the thread's vector 0 from here on
+      x += t * 16;
+      r += t * 16;
+      sum += t * 16;
+      out += t * E * int(sizeof(TO));
+    }
     settle(row);
   }
   __device__ __forceinline__ void settle(uint64_t row) {
@@ -165,11 +178,16 @@ struct NormRow {
       phase = a.shift ? static_cast<int>((reinterpret_cast<uintptr_t>(x) / sizeof(TX)) & (E - 1u)) : 0;
       edge = row < E || row + E >= a.rows;
     }
+    const int at0 = EVEN ? 0 : first(0);
+    x0 = x + at0 * int(sizeof(TX));
+    r0 = r + at0 * int(sizeof(TX));
+    sum0 = sum + at0 * int(sizeof(TX));
+    out0 = out + at0 * int(sizeof(TO));
   }
   __device__ __forceinline__ int first(int j) const { return (t + j * T) * E - phase; }   // a vector's first element
   __device__ __forceinline__ bool some(int j) const { return first(j) < width; }
   __device__ __forceinline__ bool whole(int j) const { return EVEN ? some(j) : a.together && first(j) >= 0 && first(j) + E <= width; }
-  __device__ __forceinline__ const char* place(const char* row, int j) const { return row + int64_t(first(j)) * int(sizeof(TX)); }
+  __device__ __forceinline__ const char* place(const char* row0, int j) const { return row0 + j * T * 16; }
   // Whether vector j can be loaded as one: it holds some of the row, and nothing from before the matrices' first
   // element or past their last one (what belongs to the rows next to this one is dropped).
   __device__ __forceinline__ bool loads(int j) const {
@@ -178,7 +196,7 @@ struct NormRow {
     return !edge || loads_at_edge(j);
   }
   __device__ __forceinline__ bool loads_at_edge(int j) const {
-    return place(x, j) >= a.x && place(x, j) + 16 <= a.x_end && (!a.r || (place(r, j) >= a.r && place(r, j) + 16 <= a.r_end));
+    return place(x0, j) >= a.x && place(x0, j) + 16 <= a.x_end && (!a.r || (place(r0, j) >= a.r && place(r0, j) + 16 <= a.r_end));
   }
   // h = x + r from the loaded vectors; h stored; its sum of squares
   __device__ __forceinline__ float add(const uint4 (&xs)[V], const uint4 (&rs)[V], Two (&h)[V][H]) const {
@@ -194,7 +212,7 @@ struct NormRow {
           for (int i = 0; i < H; ++i) h[j][i] = add2(h[j][i], u[i]);
         }
         if constexpr (!EVEN) {
-          if (!whole(j)) {
+          if (some(j) && !whole(j)) {
 #pragma unroll
             for (int i = 0; i < H; ++i)
               h[j][i] = two(static_cast<unsigned>(first(j) + 2 * i) < static_cast<unsigned>(width) ? low(h[j][i]) : 0.f,
@@ -212,21 +230,52 @@ struct NormRow {
           for (int i = 0; i < H; ++i) h[j][i] = add2(h[j][i], g.v[i]);
         }
       }
-      if (a.sum) put<TX>(sum, j, h[j]);
+      if (a.sum) put<TX, 0>(sum, sum0, j, h[j]);
 #pragma unroll
       for (int i = 0; i < H; ++i) total = fma2(h[j][i], h[j][i], total);
     }
     return low(total) + high(total);
   }
-  template <typename T2>
-  __device__ __forceinline__ void put(char* row, int j, const Two (&v)[H]) const {
+  // Vector j of a matrix; an end vector waits in slot SLOT (or the one after it) of the warp's scratch.
+  template <typename T2, int SLOT>
+  __device__ __forceinline__ void put(char* row, char* row0, int j, const Two (&v)[H]) const {
     if (whole(j)) {
-      put_all<T2, H>(row, first(j), v);
+      put_all<T2, H>(row0 + j * T * (E * int(sizeof(T2))), 0, v);
     } else if (!EVEN && some(j)) {
-      Pairs<H> f;
+      if (a.together) {
+        put_all<T2, H>(ends + 32 * (SLOT + (first(j) < 0 ? 0 : 1)), 0, v);
+      } else {
+        Pairs<H> f;
 #pragma unroll
-      for (int i = 0; i < H; ++i) f.v[i] = v[i];
-      scatter<T2, H>(row, first(j), width, f);
+        for (int i = 0; i < H; ++i) f.v[i] = v[i];
+        scatter<T2, H>(row, first(j), width, f);
+      }
+    }
+  }
+  // The end vectors out of the scratch, an element a lane: lanes 0-7 h's first, 8-15 h's last, 16-23 y's first, 24-31 y's last.
+  __device__ __forceinline__ void put_ends() const {
+    if constexpr (!EVEN) {
+      if (!a.together) return;
+      bool head = false, tail = false;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const bool part = some(j) && !whole(j);
+        head |= part && first(j) < 0;
+        tail |= part && first(j) >= 0;
+      }
+      head = __any_sync(ten::kAll, head);
+      tail = __any_sync(ten::kAll, tail);
+      if (head || tail) {
+        __syncwarp();
+        const int lane = t & 31, i = lane & 7, last = lane & 8;
+        const int e = (last ? (width + phase - 1) & ~(E - 1) : 0) - phase + i;
+        const char* const from = ends + 32 * (lane >> 3);
+        if (i < E && static_cast<unsigned>(e) < static_cast<unsigned>(width) && (last ? tail : head)) {
+          if (lane >= 16) copy1<TO>(out, e, from, i);
+          else if (a.sum) copy1<TX>(sum, e, from, i);
+        }
+        __syncwarp();
+      }
     }
   }
   // h * w in place of h, and for an 8-bit output the largest of |h w|
@@ -288,7 +337,7 @@ struct NormRow {
     for (int j = 0; j < V; ++j) {
 #pragma unroll
       for (int i = 0; i < H; ++i) h[j][i] = mul2(h[j][i], ff);
-      put<TO>(out, j, h[j]);
+      put<TO, 2>(out, out0, j, h[j]);
     }
   }
 };
@@ -297,9 +346,10 @@ struct NormRow {
 template <typename TX, typename TO, int V, int MOST>
 __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
   __shared__ float s_sum[kNormWarps], s_top[kNormWarps];
+  __shared__ uint4 s_ends[kNormWarps][8];
   ten::let_next_start();
   using Row = NormRow<TX, TO, V, false>;
-  Row n(a, threadIdx.x, blockDim.x);
+  Row n(a, threadIdx.x, blockDim.x, reinterpret_cast<char*>(s_ends[threadIdx.x >> 5]));
   n.at(blockIdx.x);
   ten::wait_for_previous();
   uint4 x[V], r[V];
@@ -307,8 +357,8 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
   for (int j = 0; j < V; ++j) {
     x[j] = r[j] = make_uint4(0u, 0u, 0u, 0u);
     if (n.loads(j)) {
-      x[j] = load_once(n.place(n.x, j));
-      if (a.r) r[j] = load_once(n.place(n.r, j));
+      x[j] = load_once(n.place(n.x0, j));
+      if (a.r) r[j] = load_once(n.place(n.r0, j));
     }
   }
   auto weight = [&](int j) { return n.some(j) ? weights<Row::H>(a, n.first(j), !n.phase && n.whole(j)) : Pairs<Row::H>{}; };
@@ -325,6 +375,7 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
   }
   n.reduce(total, top, s_sum, s_top);
   n.store(blockIdx.x, h, total, top);
+  n.put_ends();
 }
 
 // Persistent: blockDim = (threads of a row, rows of a block); a block takes row after row.  Every thread copies its
@@ -336,6 +387,7 @@ template <typename TX, typename TO, int V, int MOST, bool EVEN>
 __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs a, const uint32_t depth) {
   extern __shared__ uint4 ring[];
   __shared__ float s_sum[2][kNormWarps], s_top[2][kNormWarps];
+  __shared__ uint4 s_ends[EVEN ? 1 : kNormWarps][8];
   ten::let_next_start();
   using Row = NormRow<TX, TO, V, EVEN>;
   constexpr int E = Row::E, H = Row::H;
@@ -343,12 +395,14 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
   const uint32_t per_row = (a.r ? 2u : 1u) * V * T;               // vectors of a row in the ring
   const uint32_t mine = ten::smem_addr(ring + size_t(y) * depth * per_row + t), ring_end = mine + depth * per_row * 16u;
   float* const s_w = reinterpret_cast<float*>(ring + size_t(Y) * depth * per_row);
+  const uint32_t w_base = ten::smem_addr(s_w);
   const uint32_t w_pitch = a.width / E + 3u;                      // elements -E .. width + E and more
   const uint64_t step = uint64_t(gridDim.x) * Y;
   uint64_t row = uint64_t(blockIdx.x) * Y + y;
   ten::wait_for_previous();
 
-  Row ahead(a, t, T), n(a, t, T);                                 // the row that is fetched next, the row at hand
+  char* const scratch = reinterpret_cast<char*>(s_ends[EVEN ? 0 : (y * T + t) >> 5]);
+  Row ahead(a, t, T, scratch), n(a, t, T, scratch);               // the row that is fetched next, the row at hand
   ahead.at(row);
   n.at(row);
   uint64_t ahead_row = row;
@@ -357,8 +411,8 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (!ahead.loads(j)) continue;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + j * T * 16u), "l"(ahead.place(ahead.x, j)) : "memory");
-        if (a.r) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V + j) * T * 16u), "l"(ahead.place(ahead.r, j)) : "memory");
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + j * T * 16u), "l"(ahead.place(ahead.x0, j)) : "memory");
+        if (a.r) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + (V + j) * T * 16u), "l"(ahead.place(ahead.r0, j)) : "memory");
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -418,10 +472,10 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
         }
       }
       total = n.add(x, r, h);
-      const float* w_at[E];                                       // element i of a vector at [(i - phase) % E][vector + 1 + (i - phase) / E]
+      uint32_t w_at[E];                                           // element i of a vector at [(i - phase) % E][vector + 1 + (i - phase) / E]
       if constexpr (!EVEN) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) w_at[i] = s_w + ((i - n.phase) & (E - 1)) * w_pitch + 1 + (i < n.phase ? -1 : 0) + t;
+        for (int i = 0; i < E; ++i) w_at[i] = w_base + (((i - n.phase) & (E - 1)) * w_pitch + (i < n.phase ? 0u : 1u) + t) * 4u;
       }
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -437,7 +491,7 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
         } else {
           float f[E];
 #pragma unroll
-          for (int i = 0; i < E; ++i) f[i] = w_at[i][j * T];
+          for (int i = 0; i < E; ++i) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[i]) : "r"(w_at[i] + j * T * 4u));
 #pragma unroll
           for (uint32_t i = 0; i < H; ++i) w.v[i] = two(f[2 * i], f[2 * i + 1]);
         }
@@ -445,7 +499,10 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
       }
     }
     n.reduce(total, top, s_sum[odd], s_top[odd]);
-    if (live) n.store(row, h, total, top);
+    if (live) {
+      n.store(row, h, total, top);
+      n.put_ends();
+    }
     from += per_row * 16u;
     if (from == ring_end) from = mine;
     odd ^= 1u;
@@ -483,7 +540,7 @@ static int launch_norm(const NormArgs& a, int sms, cudaStream_t st) {
   if (vectors <= 128) {                                           // a warp a row
     const dim3 block(32, 8);
     if (vectors <= 32) return launch_ring<TX, TO, 1, 256, EVEN>(a, block, EVEN ? 4 : 3, sms, st);
-    if (vectors <= 64) return launch_ring<TX, TO, 2, 256, EVEN>(a, block, 3, sms, st);
+    if (vectors <= 64) return launch_ring<TX, TO, 2, 256, EVEN>(a, block, EVEN ? 3 : 2, sms, st);
     return launch_ring<TX, TO, 4, 256, EVEN>(a, block, kTwice == 2 && EVEN ? 3 : 2, sms, st);
   }
   auto threads = [&](uint32_t v) { return dim3(((vectors + v - 1) / v + 31) / 32 * 32); };
