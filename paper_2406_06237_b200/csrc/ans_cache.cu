@@ -45,58 +45,99 @@ __device__ __forceinline__ float largest(float a, Two b) {
   return r;
 }
 
-// Sixteen values from p on.  wide: 2: on 32 bytes, 1: on 16, 0: on a value.
+// Sixteen values from p on, as they lie, and opened.  wide: 2: on 32 bytes, 1: on 16, 0: on a value.
+template <typename T> struct Sixteen { uint32_t w[4 * sizeof(T)]; };
 template <typename T>
-__device__ __forceinline__ void load16(const T* p, uint32_t wide, Two (&v)[8]) {
-  if (wide == 0) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = two(static_cast<float>(p[2 * i]), static_cast<float>(p[2 * i + 1]));
-    return;
-  }
+__device__ __forceinline__ Sixteen<T> load16(const T* p, uint32_t wide) {
+  Sixteen<T> s;
   constexpr int kParts = sizeof(T) / 2;                   // 32 bytes each
 #pragma unroll
   for (int h = 0; h < kParts; ++h) {
-    uint32_t w[8];
+    uint32_t* const w = s.w + 8 * h;
     const uint4* q = reinterpret_cast<const uint4*>(p) + 2 * h;
     if (wide == 2) {
       asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(q) : "memory");
-    } else {
+    } else if (wide == 1) {
       const uint4 a = q[0], b = q[1];
       w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-    }
+    } else {
+      const uint16_t* e = reinterpret_cast<const uint16_t*>(p) + 16 * h;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (kParts == 1) v[i] = two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
-      else if (!(i & 1)) v[4 * h + i / 2] = two(__uint_as_float(w[i]), __uint_as_float(w[i + 1]));
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (kParts == 1) w[i] = e[2 * i] | static_cast<uint32_t>(e[2 * i + 1]) << 16;
+        else w[i] = reinterpret_cast<const uint32_t*>(p)[8 * h + i];
+      }
     }
+  }
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ void open16(const Sixteen<T>& s, Two (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (sizeof(T) == 2) v[i] = two(__uint_as_float(s.w[i] << 16), __uint_as_float(s.w[i] & 0xFFFF0000u));
+    else v[i] = two(__uint_as_float(s.w[2 * i]), __uint_as_float(s.w[2 * i + 1]));
   }
 }
 
-// LANES (a power of two) lanes per group, sixteen values each, lanes past group / 16 idle.  A block takes
-// blockDim.y tokens, or the parts of one after another where a token has more threads' work than a block; blockIdx.y:
-// keys or values.
+// LANES (a power of two) lanes per group, sixteen values each, lanes past group / 16 idle.  blockIdx.y: keys or values.
+// A block's piece of work is blockDim.y tokens, or a part of one token that has more threads' work than a block; it takes
+// piece after piece and loads the next one's values before it quantises one's.
 template <typename T, int BITS, int LANES>
 __global__ void __launch_bounds__(256) ans_cache_write_kernel(const WriteArgs a) {
   let_next_start();
   const uint32_t which = blockIdx.y;
-  const uint64_t token = uint64_t(blockIdx.x) * blockDim.y + threadIdx.y;
   const uint32_t per_head = a.c.head_dim / a.c.group, per_token = a.c.heads * per_head;
   const uint32_t lane = threadIdx.x % LANES;
   constexpr float L = static_cast<float>((1 << BITS) - 1);
+  const uint32_t parts = (per_token * LANES + blockDim.x - 1) / blockDim.x;   // of a token
+  const uint64_t pieces = (a.tokens + blockDim.y - 1) / blockDim.y * parts;
   wait_for_previous();
-  int64_t slot = token < a.tokens ? a.slot[token] : -1;
-  if (slot >= 0 && static_cast<uint64_t>(slot) >= a.c.slots) {
-    if (threadIdx.x == 0 && which == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-    slot = -1;
-  }
-  for (uint32_t base = 0; base < per_token * LANES; base += blockDim.x) {    // the same trips for all of the block
-    const uint32_t unit = (base + threadIdx.x) / LANES;                      // (head, group)
+  struct Piece { Sixteen<T> s; int64_t slot; uint32_t unit; bool live; };
+  // a (head, group)'s values within a token; the same for all pieces where a piece is whole tokens
+  auto inside = [&](uint32_t unit) {
     const uint32_t head = unit / per_head, g = unit - head * per_head;
-    const bool live = token < a.tokens && unit < per_token && lane * 16u < a.c.group;
-    Two v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (live)
-      load16(static_cast<const T*>(a.x[which]) + token * a.token_stride[which] + head * a.head_stride[which] + (g * a.c.group + lane * 16u), a.wide[which], v);
+    return head * a.head_stride[which] + (g * a.c.group + lane * 16u);
+  };
+  const uint32_t unit0 = threadIdx.x / LANES;
+  const bool live0 = unit0 < per_token && lane * 16u < a.c.group;
+  const T* const x0 = static_cast<const T*>(a.x[which]) + inside(unit0);
+  auto fetch = [&](uint64_t piece) {
+    Piece p;
+    uint64_t token = piece * blockDim.y + threadIdx.y;
+    const T* from = x0;
+    p.unit = unit0;
+    p.live = live0;
+    if (parts > 1) {
+      const uint64_t tokens = piece / parts;
+      token = tokens * blockDim.y + threadIdx.y;
+      p.unit = (static_cast<uint32_t>(piece - tokens * parts) * blockDim.x + threadIdx.x) / LANES;
+      p.live = p.unit < per_token && lane * 16u < a.c.group;
+      from = static_cast<const T*>(a.x[which]) + inside(p.unit);
+    }
+    p.slot = -1;
+    p.live = p.live && token < a.tokens;
+    p.s = Sixteen<T>{};
+    if (p.live) {
+      p.slot = a.slot[token];
+      p.s = load16(from + token * a.token_stride[which], a.wide[which]);
+    }
+    return p;
+  };
+  Piece next = fetch(blockIdx.x);
+  for (uint64_t piece = blockIdx.x; piece < pieces; piece += gridDim.x) {     // the same trips for all of the block
+    const Piece now = next;
+    next = fetch(piece + gridDim.x);
+    int64_t slot = now.slot;
+    const bool live = now.live;
+    const uint32_t unit = now.unit;
+    if (slot >= 0 && static_cast<uint64_t>(slot) >= a.c.slots) {
+      if (which == 0 && unit == 0 && lane == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+      slot = -1;
+    }
+    Two v[8];
+    open16(now.s, v);
     float lo = 0.f, hi = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -177,7 +218,7 @@ struct ReadArgs {
   uint32_t wide;                     // outputs on 32 bytes
 };
 
-constexpr uint32_t kReadRows = 64;    // rows of a block at most
+constexpr uint32_t kReadRows = 256;   // rows of a block at most
 
 // Sixteen codes in w to scale * (code - zero), two at a time: a code set under the exponent of 2^23 is 2^23 + code * 16^k
 // (k: its place among the four nibbles of a half word; 0 for whole bytes), from which 2^23 + zero * 16^k is
@@ -367,10 +408,15 @@ static int launch_write(const WriteArgs& a, cudaStream_t st) {
   const uint32_t need = a.c.group / 16u;
   const uint32_t lanes = need <= 1 ? 1 : need <= 2 ? 2 : need <= 4 ? 4 : need <= 8 ? 8 : 16;
   const uint32_t threads = a.c.heads * (a.c.head_dim / a.c.group) * lanes;        // of a token
-  const dim3 block(threads < 256 ? (threads + 31) / 32 * 32 : 256, threads < 256 ? 256 / ((threads + 31) / 32 * 32) : 1);
-  const uint64_t blocks = (a.tokens + block.y - 1) / block.y;
-  if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(blocks), 2);
+  const uint32_t across = threads >= 256 ? 256u : 32u % threads == 0 ? threads : (threads + 31u) / 32u * 32u;
+  const dim3 block(across, 256u / across);
+  const uint64_t pieces = (a.tokens + block.y - 1) / block.y * ((threads + block.x - 1) / block.x);
+  int sms = 0;
+  const int asked = ten::sm_count(&sms);
+  if (asked != ANS_OK) return asked;
+  // up to five blocks an SM, keys and values together (what registers hold)
+  const uint64_t most = 5ull * sms / 2;
+  const dim3 grid(static_cast<unsigned>(pieces < most ? pieces : most), 2);
   switch (lanes) {
     case 1: return ten::launch(ans_cache_write_kernel<T, BITS, 1>, grid, block, 0, st, 1, a);
     case 2: return ten::launch(ans_cache_write_kernel<T, BITS, 2>, grid, block, 0, st, 1, a);
@@ -433,12 +479,17 @@ ANS_EXPORT int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tab
   a.out[0] = d_k_out; a.out[1] = d_v_out; a.status = d_status;
   a.wide = !((reinterpret_cast<uintptr_t>(d_k_out) | reinterpret_cast<uintptr_t>(d_v_out)) & 31);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // rows of a block: enough blocks for eight on each SM, up to 64 rows each, over which a block's look-up is spread
+  // Rows of a block: enough blocks for eight on each SM, up to 64 rows each, over which a block's look-up is spread; of
+  // narrow rows as many as give its threads four pieces each.
   int sms = 0;
   const int asked = ten::sm_count(&sms);
   if (asked != ANS_OK) return asked;
   const uint64_t share = rows / (4u * static_cast<uint64_t>(sms));
-  const uint32_t some = share < 4 ? 4u : share > kReadRows ? kReadRows : static_cast<uint32_t>(share);
+  uint32_t some = share < 4 ? 4u : share > 64 ? 64u : static_cast<uint32_t>(share);
+  const uint32_t units = a.c.heads * a.c.head_dim / 16u;
+  uint64_t full = 1024u / units < kReadRows ? 1024u / units : kReadRows;
+  if (full > 2 * rows / sms) full = 2 * rows / sms;                   // but not fewer blocks than SMs
+  if (some < full) some = static_cast<uint32_t>(full);
   const dim3 grid(static_cast<unsigned>((rows + some - 1) / some), 2);
   if (out_dtype == ANS_BF16)
     return h_desc->bitwidth == 8 ? ten::launch(ans_cache_read_kernel<__nv_bfloat16, 8>, grid, dim3(256), 0, st, 1, a, some)

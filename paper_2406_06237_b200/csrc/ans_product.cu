@@ -54,9 +54,9 @@ struct PrShape {
   static constexpr uint32_t kBlockX = BN / CG * kPrRow;  // a pair's CTAs hold half of the tokens each
   static constexpr uint32_t kX = NT * kBlockX;
   static constexpr uint32_t kStage = kW + kX;
-  static constexpr uint32_t kTeams = !SPLIT ? 4u : BN <= 64u ? 1u : 2u;    // teams of four epilogue warps, each with its part of the tokens
+  static constexpr uint32_t kTeams = NT == 2u ? 4u : SPLIT && BN <= 64u ? 1u : 2u;    // teams of four epilogue warps, each with its part of the tokens
   // tokens that an epilogue warp takes out at a time, of its 32 features, and the bytes of such a block
-  static constexpr uint32_t kBlock = !SPLIT || BN < 32u ? 16u : 32u;
+  static constexpr uint32_t kBlock = NT == 2u || BN < 32u ? 16u : 32u;
   static constexpr uint32_t kScratch = kBlock * 32u * 4u;
   static constexpr uint32_t kTma = 4u * kTeams, kMma = kTma + 1u;     // the warps after them: copies, matrix instructions
   static constexpr uint32_t kThreads = 32u * (kMma + 1u);
