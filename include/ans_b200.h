@@ -418,8 +418,10 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
 /* ------------------------------------------------------------------------------------
  * The operators around a product with decoded weights.
  * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where X's rows
- * start off 16 bytes) and return without waiting; they keep nothing from one call for the next.  Sizes of
- * zero are fine (nothing is launched).  Unless said otherwise, outputs do not overlap inputs.
+ * start off 16 bytes) and return without waiting; they keep nothing from one call for the next.  The
+ * kernels may take their place while the work queued ahead drains; they touch memory only once it is
+ * complete (weights that the caller calls settled apart).  Calls with no rows, tokens or features do
+ * nothing.  Unless said otherwise, outputs do not overlap inputs.
  * ------------------------------------------------------------------------------------ */
 
 /*

@@ -340,7 +340,9 @@ __global__ void __launch_bounds__(MANY ? 896 : 512, 1) ans_decode_kernel(const L
     cursor = stop;
   }
   bad = __reduce_or_sync(kFull, bad);
-  if (args.early && bad) asm volatile("griddepcontrol.wait;" ::: "memory");
+  // A launch that waits for nothing still does not end before the work ahead of it: a later launch that waits for this
+  // one alone (as overlapping launches do) is then behind all of it.  One warp is enough.
+  if ((args.early && bad) || (args.early == 2u && blockIdx.x == 0 && warp == 0)) asm volatile("griddepcontrol.wait;" ::: "memory");
   if (lane == 0 && bad && args.d_status) atomicOr(args.d_status, bad);
 }
 

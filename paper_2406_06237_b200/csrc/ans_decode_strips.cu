@@ -417,7 +417,9 @@ __global__ void __launch_bounds__(kStripWarps * 32) ans_decode_strips_kernel(con
     }
   }
   bad = __reduce_or_sync(kFull, bad);
-  if (args.early && bad) asm volatile("griddepcontrol.wait;" ::: "memory");   // (a warp that wrote nothing has not waited yet)
+  // (a warp that wrote nothing has not waited yet.)  A launch that waits for nothing still does not end before the work
+  // ahead of it: a later launch that waits for this one alone is then behind all of it.  One warp is enough.
+  if ((args.early && bad) || (args.early == 2u && blockIdx.x == 0 && warp == 0)) asm volatile("griddepcontrol.wait;" ::: "memory");
   if (lane == 0 && bad && args.d_status) atomicOr(args.d_status, bad);
 }
 
