@@ -5,7 +5,10 @@
 // and back  scale * (code - zero).  The results are those of IEEE divisions, so codes are a function of the
 // values alone and equal on every device and in any IEEE restatement.
 //
-// Both directions are bound by memory.  A thread has sixteen values of one group.
+// A thread has sixteen values of one group.  Reading is bound by memory: 64 sequences of about 1500 tokens (8 heads of 128, 8 bits)
+// 72 us, 91 % of the rate of a copy with the step's write before it.  Writing is bound by instruction issue: 10240 tokens
+// of the same heads in 4 bits, groups of 32, 17 us where the bytes take 8; two 16-byte loads a lane, the next piece's under way
+// while one is quantised.
 #include <cmath>
 #include <initializer_list>
 
