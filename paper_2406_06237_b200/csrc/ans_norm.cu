@@ -303,14 +303,17 @@ struct NormRow {
         s_sum[t >> 5] = total;
         if (k8) s_top[t >> 5] = top;
       }
+      if (t >= warps && t < 8) {
+        s_sum[t] = 0.f;
+        if (k8) s_top[t] = 0.f;
+      }
       __syncthreads();
-      if (warps <= 8) {                                           // the same few words for every thread: no second round of shuffles
-        total = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (i >= warps) break;
-          total += s_sum[i];
-          if (k8) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(s_top[i])));
+      if (warps <= 8) {                                           // the same eight words for every thread: no second round of shuffles
+        const float4 p = reinterpret_cast<const float4*>(s_sum)[0], q = reinterpret_cast<const float4*>(s_sum)[1];
+        total = ((p.x + p.y) + (p.z + p.w)) + ((q.x + q.y) + (q.z + q.w));
+        if (k8) {
+          const uint4 u = reinterpret_cast<const uint4*>(s_top)[0], v = reinterpret_cast<const uint4*>(s_top)[1];
+          top = __uint_as_float(max(max(max(u.x, u.y), max(u.z, u.w)), max(max(v.x, v.y), max(v.z, v.w))));
         }
       } else {
         total = lane < warps ? s_sum[lane] : 0.f;
@@ -349,7 +352,7 @@ struct NormRow {
 // A block a row: for few rows, where a row's own latency counts, and for rows that the rings below do not fit.
 template <typename TX, typename TO, int V, int MOST>
 __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
-  __shared__ float s_sum[kNormWarps], s_top[kNormWarps];
+  __shared__ __align__(16) float s_sum[kNormWarps], s_top[kNormWarps];
   __shared__ uint4 s_ends[kNormWarps][8];
   ten::let_next_start();
   using Row = NormRow<TX, TO, V, false>;
@@ -390,7 +393,7 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
 template <typename TX, typename TO, int V, int MOST, bool EVEN>
 __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs a, const uint32_t depth) {
   extern __shared__ uint4 ring[];
-  __shared__ float s_sum[2][kNormWarps], s_top[2][kNormWarps];
+  __shared__ __align__(16) float s_sum[2][kNormWarps], s_top[2][kNormWarps];
   __shared__ uint4 s_ends[EVEN ? 1 : kNormWarps][8];
   ten::let_next_start();
   using Row = NormRow<TX, TO, V, EVEN>;
@@ -401,7 +404,8 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
   float* const s_w = reinterpret_cast<float*>(ring + size_t(Y) * depth * per_row);
   const uint32_t w_base = ten::smem_addr(s_w);
   const uint32_t w_pitch = a.width / E + 3u;                      // elements -E .. width + E and more
-  const uint64_t step = uint64_t(gridDim.x) * Y;
+  const uint64_t step = uint64_t(gridDim.x) * Y;                  // rows from a block's row to its next, and their bytes
+  const uint64_t x_on = step * a.x_step, r_on = step * a.r_step, out_on = step * a.out_step, sum_on = step * a.sum_step;
   uint64_t row = uint64_t(blockIdx.x) * Y + y;
   ten::wait_for_previous();
 
@@ -421,8 +425,8 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     ahead_row += step;
-    ahead.x += step * a.x_step;
-    ahead.r += step * a.r_step;
+    ahead.x += x_on;
+    ahead.r += r_on;
     ahead.settle(ahead_row);
   };
   uint32_t spare = mine;                                          // the place for the next fetch
@@ -511,10 +515,10 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
     if (from == ring_end) from = mine;
     odd ^= 1u;
     row += step;
-    n.x += step * a.x_step;
-    n.r += step * a.r_step;
-    n.out += step * a.out_step;
-    n.sum += step * a.sum_step;
+    n.x += x_on;
+    n.r += r_on;
+    n.out += out_on;
+    n.sum += sum_on;
     n.settle(row);
   }
 }

@@ -328,6 +328,7 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   } else if (warp == S::kMma) {
     if (lane == 0 && (CG == 1 || rank == 0)) {
       constexpr uint32_t idesc = instruction<F8>(kPrFeatures * CG, BN);
+      wait_for_previous();                                             // the limits of the waits below are for this call's own work
       uint32_t n = 0, it = 0;
       for (uint32_t tile = team; tile < tiles; tile += teams, ++it) {
         const uint32_t acc = it % S::kAccs, round = it / S::kAccs;
@@ -342,7 +343,7 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
           for (uint32_t j = 0; j < 4; ++j)                             // 32 bytes of K an instruction
             if constexpr (NT == 1) {
               mma<CG, F8>(tmem + acc * S::kTokens, dw + 2u * j, dx + 2u * j, idesc, (k > k0 || j) ? 1u : 0u);
-            } else {                                                   // both halves of the tokens against one read of W
+            } else {                                                   // both halves of the tokens against one read of W (1 % at 8192^3)
               mma<CG, F8, 1>(tmem, dw + 2u * j, dx + 2u * j, idesc, (k > k0 || j) ? 1u : 0u);
               mma<CG, F8, 2>(tmem + BN, dw + 2u * j, dx + (S::kBlockX >> 4) + 2u * j, idesc, (k > k0 || j) ? 1u : 0u);
             }
