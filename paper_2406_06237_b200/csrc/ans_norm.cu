@@ -8,7 +8,7 @@
 //
 // Bound by memory for all but few or unaligned rows: 16384 x 8192 in bf16 with residual to e4m3 168 us, 5.6 TB/s, 85 % of the
 // rate of a copy; 8192 x 4096 from fp32 to bf16 33 us, 93 %; one row of 8192 2.8 us, its own latency; 5000 x 7777 in bf16
-// (rows off 16 bytes) 69 us, 69 %.
+// (rows off 16 bytes) 65 us, 73 %.
 #include <cmath>
 #include <type_traits>
 
@@ -545,25 +545,30 @@ template <typename TX, typename TO, bool EVEN>
 static int launch_norm(const NormArgs& a, int sms, cudaStream_t st) {
   constexpr uint32_t E = 16 / sizeof(TX), kTwice = sizeof(TX) / 2;   // fp32: twice the vectors for a row
   const uint32_t vectors = (a.width + a.shift + E - 1) / E;
-  if (vectors <= 128) {                                           // a warp a row
-    const dim3 block(32, 8);
-    if (vectors <= 32) return launch_ring<TX, TO, 1, 256, EVEN>(a, block, EVEN ? 4 : 3, sms, st);
-    if (vectors <= 64) return launch_ring<TX, TO, 2, 256, EVEN>(a, block, EVEN ? 3 : 2, sms, st);
-    return launch_ring<TX, TO, 4, 256, EVEN>(a, block, kTwice == 2 && EVEN ? 3 : 2, sms, st);
-  }
   auto threads = [&](uint32_t v) { return dim3(((vectors + v - 1) / v + 31) / 32 * 32); };
-  const dim3 rows(static_cast<unsigned>(a.rows < 0x7FFFFFFFull ? a.rows : 0x7FFFFFFFull));
-  // A ring pays where a block has some rows to read ahead: six and more.  With fewer a block takes one row, with as
-  // many threads as it has vectors where a block can have them.
+  // The ring.  Even rows: a warp a row up to 128 vectors; a block a row where a block has at least two of them to read ahead:
+  // 1100 x 8192 13 us, 16 without, 400 x 8192 6.8 with and without.  Rows off 16 bytes spend their time on their ends and
+  // on the weight's place, which the ring's few threads make longer: it takes the narrowest (100000 x 111 52 us, 104 with a
+  // block a row; but 20000 x 333 28 and 22) and the widest (3000 x 16001 86 and 100 us; but 16000 x 2047 74 and 55).
+  const dim3 warps(32, 8);
+  if (vectors <= 32) return launch_ring<TX, TO, 1, 256, EVEN>(a, warps, EVEN ? 4 : 3, sms, st);
+  if constexpr (EVEN) {
+    if (vectors <= 64) return launch_ring<TX, TO, 2, 256, true>(a, warps, 3, sms, st);
+    if (vectors <= 128) return launch_ring<TX, TO, 4, 256, true>(a, warps, kTwice == 2 ? 3 : 2, sms, st);
+  }
   constexpr int V = 4 * kTwice;
   const dim3 block = threads(V);
   const uint32_t blocks = 512 / block.x;
   const size_t bytes = size_t(vectors + 256) * 16 * (a.r ? 2 : 1);   // of a row in the ring, at most
   const size_t rest = EVEN ? 0 : weight_bytes<TX>(a);
-  if (vectors <= 2048 * kTwice && a.rows >= 6ull * sms * blocks && 2 * bytes + rest <= kNormRing)
+  if (vectors <= 2048 * kTwice && (EVEN || vectors > 1024) && a.rows >= (EVEN ? 2u : 6u) * uint64_t(sms) * blocks && 2 * bytes + rest <= kNormRing)
     return launch_ring<TX, TO, V, 512, EVEN>(a, block, blocks, sms, st);
-  if (vectors <= 1024) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 1024>, rows, threads(1), 0, st, 1, a);
   if (a.rows > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+  const dim3 rows(static_cast<unsigned>(a.rows));
+  // One vector a thread while all rows' blocks are on the SMs at once (1344 threads of it an SM), else two: 500 x 2047 3.2 and
+  // 4.2 us, 1537 x 2047 7.7 and 6.7, 1500 x 8192 28 and 21.
+  if (vectors <= 1024 && a.rows > uint64_t(sms) * (1344u / threads(1).x)) return ten::launch(ans_rms_norm_kernel<TX, TO, 2, 512>, rows, threads(2), 0, st, 1, a);
+  if (vectors <= 1024) return ten::launch(ans_rms_norm_kernel<TX, TO, 1, 1024>, rows, threads(1), 0, st, 1, a);
   if (vectors <= 2048 * kTwice) return ten::launch(ans_rms_norm_kernel<TX, TO, 4 * kTwice, 512>, rows, threads(4 * kTwice), 0, st, 1, a);
   return ten::launch(ans_rms_norm_kernel<TX, TO, 8 * kTwice, 576>, rows, threads(8 * kTwice), 0, st, 1, a);
 }

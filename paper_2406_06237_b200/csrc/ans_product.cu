@@ -584,7 +584,7 @@ static int choose_product(const ans_product_desc& d, const PrArgs& a, int sms, c
   if (d.m > 16) weigh_split<32>(d, a, sms, best);
   if (d.m > 32) weigh_split<64>(d, a, sms, best);
   if (d.m > 64) weigh_split<128>(d, a, sms, best);
-  if (d.m > 64) {
+  if (d.m > 64 && sms > 1) {
     // The whole forms on pairs of SMs: a stage of 256 tokens 0.31 us, of 512 tokens 0.55 us (they read W once for both
     // halves and move a quarter less into shared memory, but nothing runs under a tile's end): 8192^3 in bf16 power-
     // capped 830 us in 512s, 900 in 256s; 4096 x 4096 x 1024 43 and 38.

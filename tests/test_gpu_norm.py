@@ -51,6 +51,21 @@ def test_rows(rows, width, x_dtype, out_dtype):
         check(x, residual, weight, 1e-5, *got, out_dtype)
 
 
+@pytest.mark.parametrize("out_dtype", [BF16, F32, E4M3])
+@pytest.mark.parametrize("x_dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,width", [(9000, 64), (9001, 250), (7000, 500), (5003, 1024), (3000, 2048), (2001, 4096), (1201, 8192), (701, 12000),
+                                        (701, 16384), (1000, 8201), (901, 16381), (3001, 2047), (700, 1111)])
+def test_many_rows(rows, width, x_dtype, out_dtype):
+    """Row counts at which blocks take row after row, some of them one more than others."""
+    g = torch.Generator(device="cuda").manual_seed(rows + width)
+    x = (3 * torch.randn(rows, width, device="cuda", generator=g)).to(x_dtype)
+    r = torch.randn(rows, width, device="cuda", generator=g).to(x_dtype)
+    w = torch.randn(width, device="cuda", generator=g).to(F32 if rows % 2 else BF16)
+    f = RmsNorm(w, 1e-5, out_dtype)
+    for residual in (r, None):
+        check(x, residual, w, 1e-5, *f(x, residual), out_dtype)
+
+
 @pytest.mark.parametrize("out_dtype", [BF16, E4M3])
 @pytest.mark.parametrize("offset,stride", [(0, 520), (3, 515), (8, 513), (5, 700)])
 @pytest.mark.parametrize("width", [513, 512, 40])
