@@ -492,6 +492,10 @@ typedef struct ans_product_desc {
 int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
 /* Bytes of d_room that a call with this X needs (from d_x, x_stride, m, k and dtype); 0: none. */
 int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out);
+/* A matrix that lies anywhere (element (r, c) at d_from[r * stride + c * step], dtype ANS_BF16 or ANS_E4M3) laid out in rows
+ * as ans_product reads them: d_to on 16 bytes, a row every k elements rounded up to whole 16 bytes, zeros behind
+ * its end.  For a W that does not start, or whose rows do not all start, on 16 bytes.  rows <= 2^30, k <= 2^22. */
+int ans_product_rows(const void* d_from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, int dtype, void* d_to, void* stream);
 
 /*
  * A paged cache of keys and values, quantised as it is written.  Every group of `group` values of

@@ -37,7 +37,7 @@ EXPORTS = [
     "ans_histogram_device", "ans_entropy_device", "ans_normalize_freqs_device",
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
-    "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_cache_write", "ans_cache_read",
+    "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_product_rows", "ans_cache_write", "ans_cache_read",
 ]
 
 
@@ -139,6 +139,7 @@ def lib():
         L.ans_rms_norm.argtypes = [P(ans_norm_desc), vp]
         L.ans_product.argtypes = [P(ans_product_desc), vp, vp]
         L.ans_product_room_bytes.argtypes = [P(ans_product_desc), P(sz)]
+        L.ans_product_rows.argtypes = [vp, u64, u64, u32, u32, i32, vp, vp]
         L.ans_cache_write.argtypes = [P(ans_cache_desc), vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, vp]
         L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
         _LIB = L
@@ -372,6 +373,12 @@ def ans_product_room_bytes(h_desc: ans_product_desc) -> int:
     out = ctypes.c_size_t()
     _check(lib().ans_product_room_bytes(h_desc, ctypes.byref(out)), "ans_product_room_bytes")
     return out.value
+
+
+def ans_product_rows(d_from: int, stride: int, step: int, rows: int, k: int, dtype: int, d_to: int, stream: int = 0) -> None:
+    rc = (_LIB or lib()).ans_product_rows(d_from, stride, step, rows, k, dtype, d_to, stream)
+    if rc:
+        _check(rc, "ans_product_rows")
 
 
 def ans_cache_write(h_desc: ans_cache_desc, d_k: int, d_v: int, dtype: int, tokens: int, k_strides, v_strides,

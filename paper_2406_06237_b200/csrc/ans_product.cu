@@ -465,21 +465,21 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   if (lane == 0 && bad) atomicOr(a.status, ANS_STATUS_COPY_TIMEOUT);
 }
 
-// Rows of X that start anywhere into rows that start on 16 bytes: 16 bytes of a row a thread, element by element (the
-// elements' neighbours come out of L1).  T: an element's bits.
+// Rows that start anywhere, elements `step` apart, into rows that start on 16 bytes, zeros behind their ends: 16 bytes of a row
+// a thread, element by element (the elements' neighbours come out of L1).  T: an element's bits.
 template <typename T>
-__global__ void __launch_bounds__(256) ans_product_rows_kernel(const T* x, uint64_t x_stride, uint4* room, uint32_t m, uint32_t k, uint32_t pieces) {
+__global__ void __launch_bounds__(256) ans_product_rows_kernel(const T* x, uint64_t stride, uint64_t step, uint4* room, uint32_t rows, uint32_t k, uint32_t pieces) {
   constexpr uint32_t kIn = 16 / sizeof(T);
   let_next_start();
   const uint64_t i = uint64_t(blockIdx.x) * 256u + threadIdx.x;
   wait_for_previous();
   const uint64_t row = i / pieces;
-  if (row >= m) return;
+  if (row >= rows) return;
   const uint32_t e = static_cast<uint32_t>(i - row * pieces) * kIn;
-  const T* const p = x + row * x_stride + e;
+  const T* const p = x + row * stride + e * step;
   T v[kIn];
 #pragma unroll
-  for (uint32_t j = 0; j < kIn; ++j) v[j] = e + j < k ? p[j] : T(0);
+  for (uint32_t j = 0; j < kIn; ++j) v[j] = e + j < k ? p[j * step] : T(0);
   uint4 out;
   uint32_t* const w = &out.x;
 #pragma unroll
@@ -612,13 +612,35 @@ using namespace ansb;
 static bool rows_fit(const ans_product_desc& d, uint64_t es) {
   return !(reinterpret_cast<uintptr_t>(d.d_x) & 15) && (d.m <= 1 || !((d.x_stride * es) & 15));
 }
-static uint64_t room_row(const ans_product_desc& d, uint64_t es) { return (d.k * es + 15) & ~uint64_t(15); }
+static uint64_t room_row(uint32_t k, uint64_t es) { return (k * es + 15) & ~uint64_t(15); }
+
+static int lay_out(const void* from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, uint64_t es, void* to, cudaStream_t st) {
+  const uint64_t pieces = room_row(k, es) / 16, blocks = (rows * pieces + 255) / 256;
+  if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  uint4* const room = static_cast<uint4*>(to);
+  return es == 1 ? launch(ans_product_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, static_cast<const uint8_t*>(from), stride, step, room, rows, k,
+                          static_cast<uint32_t>(pieces))
+                 : launch(ans_product_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, static_cast<const uint16_t*>(from), stride, step, room, rows, k,
+                          static_cast<uint32_t>(pieces));
+}
+
+ANS_EXPORT int ans_product_rows(const void* d_from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, int dtype, void* d_to, void* stream) {
+  ApiRange range("ans_product_rows");
+  if (dtype != ANS_BF16 && dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
+  constexpr uint64_t kFar = uint64_t(1) << 36;
+  if (rows > (1u << 30) || k > (1u << 22) || stride > kFar || step > kFar) return ANS_ERR_UNSUPPORTED;
+  if (rows == 0 || k == 0) return ANS_OK;
+  const uint64_t es = dtype == ANS_E4M3 ? 1 : 2;
+  if (!d_from || !d_to || (reinterpret_cast<uintptr_t>(d_from) & (es - 1)) || (reinterpret_cast<uintptr_t>(d_to) & 15)) return ANS_ERR_INVALID_ARG;
+  return lay_out(d_from, stride, step, rows, k, es, d_to, static_cast<cudaStream_t>(stream));
+}
 
 ANS_EXPORT int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out) {
   if (!h_desc || !h_bytes_out) return ANS_ERR_INVALID_ARG;
   if (h_desc->dtype != ANS_BF16 && h_desc->dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
   const uint64_t es = h_desc->dtype == ANS_E4M3 ? 1 : 2;
-  *h_bytes_out = rows_fit(*h_desc, es) ? 0 : h_desc->m * room_row(*h_desc, es);
+  *h_bytes_out = rows_fit(*h_desc, es) ? 0 : h_desc->m * room_row(h_desc->k, es);
   return ANS_OK;
 }
 
@@ -646,18 +668,12 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   if (d.m > 1 && d.d_residual && (d.residual_stride < d.n || d.residual_stride > kFar)) return ANS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (d.k && !rows_fit(d, es)) {
-    const uint64_t row = room_row(d, es);
+    const uint64_t row = room_row(d.k, es);
     if (!d.d_room || d.room_bytes < d.m * row) return ANS_ERR_BUFFER_TOO_SMALL;
     if (reinterpret_cast<uintptr_t>(d.d_room) & 15) return ANS_ERR_INVALID_ARG;
-    const uint64_t blocks = (d.m * (row / 16) + 255) / 256;
-    if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-    const uint32_t pieces = static_cast<uint32_t>(row / 16);
-    uint4* const room = static_cast<uint4*>(d.d_room);
-    const dim3 grid(static_cast<unsigned>(blocks));
-    const int rc = es == 1 ? launch(ans_product_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, static_cast<const uint8_t*>(d.d_x), d.x_stride, room, d.m, d.k, pieces)
-                           : launch(ans_product_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, static_cast<const uint16_t*>(d.d_x), d.x_stride, room, d.m, d.k, pieces);
+    const int rc = lay_out(d.d_x, d.x_stride, 1, d.m, d.k, es, d.d_room, st);
     if (rc != ANS_OK) return rc;
-    d.d_x = room;
+    d.d_x = d.d_room;
     d.x_stride = row / es;
   }
   int sms = 0;

@@ -163,26 +163,20 @@ def _fits(t: torch.Tensor) -> bool:
     return (one == 1 or width <= 1) and (rows <= 1 or stride >= width and stride * t.element_size() % 16 == 0)
 
 
-def _padded(t: torch.Tensor) -> torch.Tensor:
-    """A copy of t with rows that start on 16 bytes."""
-    rows, width = t.shape
-    pad = 16 // t.element_size()
-    room = torch.empty((rows, max(width + pad - 1, 1) // pad * pad), dtype=t.dtype, device=t.device)
-    room = room.as_strided((rows, width), (room.shape[1], 1))
-    return room.copy_(t)
-
-
 class Linear(_Handle):
     """Y = act(x_scales * scales * X W^T + bias) + residual with W [out features, in features].
 
     weight: bf16 (as decoded) or float8_e4m3fn (see symbols_to_e4m3).  scales: fp32, one for each
     output feature or one for all (a float or one element), or None.  bias: [out features] or None.
-    activation: "none", "relu", "gelu", "gelu_tanh" or "silu".  A weight whose rows do not start on 16
-    bytes is copied once into rows that do.
+    activation: "none", "relu", "gelu", "gelu_tanh" or "silu".
 
-    settled: the weight does not change any more.  The device is synchronised here, and calls may read the
-    weight before the work queued ahead of them is done (ANS_PRODUCT_WEIGHTS_SETTLED).  Leave it
-    out where the weight's buffer is decoded into again.
+    The weight is read where it lies, at each call, so that its buffer may be decoded into again.  Where it or its
+    rows do not start on 16 bytes, each call lays it out in fresh memory first (a kernel that reads and writes
+    the whole weight), unless it is settled.
+
+    settled: the weight does not change any more.  The device is synchronised here, a weight off 16 bytes is laid
+    out here once, and calls may read the weight before the work queued ahead of them is done
+    (ANS_PRODUCT_WEIGHTS_SETTLED).  Leave it out where the weight's buffer is decoded into again.
     """
 
     def __init__(self, weight: torch.Tensor, scales=None, bias: torch.Tensor | None = None, activation: str = "none",
@@ -192,7 +186,7 @@ class Linear(_Handle):
         _need(weight.dtype in (torch.bfloat16, torch.float8_e4m3fn), "weight must be bf16 or float8_e4m3fn")
         _need(activation in B.ACTIVATIONS, f"activation {activation!r} is not one of {', '.join(B.ACTIVATIONS)}")
         n, k = weight.shape
-        self.weight = weight if _fits(weight) and weight.data_ptr() % 16 == 0 else _padded(weight)
+        self.weight = weight
         if scales is not None:
             scales = torch.as_tensor(scales, dtype=torch.float32, device=self.device).reshape(-1)
             _need(scales.numel() in (1, n), "scales must be one or one for each output feature")
@@ -204,11 +198,15 @@ class Linear(_Handle):
         self.in_features, self.out_features = k, n
         self._form, self._lies_off = self._new_form(), False
         self._desc = d = B.ans_product_desc()
-        d.d_w, d.w_stride = self.weight.data_ptr() or None, max(self.weight.stride(0), k)
+        d.d_w, d.w_stride = weight.data_ptr() or None, max(weight.stride(0), k)
         d.d_w_scales = scales.data_ptr() if scales is not None else None
         d.d_bias = bias.data_ptr() if bias is not None else None
         d.n, d.k, d.dtype, d.activation = n, k, _ELEMENT[weight.dtype], B.ACTIVATIONS[activation]
+        self._weight_off = n > 0 and k > 0 and not (_fits(weight) and weight.data_ptr() % 16 == 0)
         if settled:
+            if self._weight_off:
+                with torch.cuda.device(self.device):
+                    self._laid, self._weight_off = self._lay_out(_current_stream(self._index)), False
             torch.cuda.synchronize(self.device)
             d.flags = B.ANS_PRODUCT_WEIGHTS_SETTLED
 
@@ -228,11 +226,23 @@ class Linear(_Handle):
             self._form.keep(x, x_scales, residual, out)
             at = self._form.places(x, x_scales, residual, out)
         d.d_x, d.d_x_scales, d.d_residual, d.d_y = at
+        if self._weight_off:
+            laid = self._lay_out(st)                       # kept until the call is queued  # noqa: F841
         if self._lies_off or at[0] % 16:
             room = torch.empty(B.ans_product_room_bytes(d), dtype=torch.uint8, device=self.device)
             d.d_room, d.room_bytes = room.data_ptr(), room.numel()
         B.ans_product(d, self._status, st)
         return out
+
+    def _lay_out(self, stream: int) -> torch.Tensor:
+        """The weight as it is when the stream gets there, in rows that start on 16 bytes; the descriptor names them."""
+        d, w = self._desc, self.weight
+        pad = 16 // w.element_size()
+        d.w_stride = (d.k + pad - 1) // pad * pad
+        laid = torch.empty(d.n * d.w_stride, dtype=w.dtype, device=self.device)
+        d.d_w = laid.data_ptr()
+        B.ans_product_rows(w.data_ptr(), *w.stride(), d.n, d.k, d.dtype, d.d_w, stream)
+        return laid
 
     def _check(self, x, x_scales, residual, out):
         """Checks one call's tensors and writes all but their places into the descriptor."""

@@ -1,0 +1,73 @@
+"""What a handle keeps between calls, and what it reads anew."""
+import pytest
+import torch
+
+from paper_2406_06237_b200.runtime import Linear
+
+pytestmark = pytest.mark.gpu
+BF16, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+def integers(shape, most, dtype, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randint(-most, most + 1, shape, device="cuda", generator=g).float().to(dtype)
+
+
+def product(x, w):
+    """Whole numbers with sums under 2^24: exact in fp32."""
+    return (x.double() @ w.double().T).float()
+
+
+# n, k, the weight's first element in its buffer, its rows' distance (0: k)
+PLACES = [(128, 256, 0, 0), (128, 256, 1, 0), (65, 131, 0, 0), (300, 2047, 0, 0), (1, 33, 3, 0), (1000, 64, 8, 0), (200, 100, 0, 104), (200, 100, 5, 203),
+          (3001, 520, 0, 521)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("n,k,off,stride", PLACES)
+def test_a_weight_written_again_is_read_again(n, k, off, stride, dtype):
+    """Wherever the weight lies: a call multiplies by what its buffer holds when the stream gets there."""
+    stride = stride or k
+    room = torch.full((off + n * stride,), 9.0, device="cuda").to(dtype)
+    w = room.as_strided((n, k), (stride, 1), off)
+    for m in (1, 70):
+        x = integers((m, k), 4, dtype, m)
+        f = Linear(w)
+        for seed in range(3):
+            w.copy_(integers((n, k), 4, dtype, seed))
+            assert torch.equal(f(x, out_dtype=F32), product(x, w))
+        assert f.read_status() == 0
+
+
+def test_a_transposed_weight_is_read_again():
+    base = torch.empty(300, 77, device="cuda", dtype=BF16)
+    f, x = Linear(base.t()), integers((5, 300), 4, BF16, 1)
+    for seed in range(2):
+        base.copy_(integers((300, 77), 4, BF16, seed))
+        assert torch.equal(f(x, out_dtype=F32), product(x, base.t()))
+
+
+@pytest.mark.parametrize("k", [64, 67])
+def test_a_weight_written_between_replays(k):
+    w, x, y = integers((130, k), 4, BF16, 1), integers((20, k), 4, BF16, 2), torch.empty(20, 130, device="cuda")
+    f = Linear(w)
+    f(x, out=y)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f(x, out=y)
+    for seed in (5, 6):
+        w.copy_(integers((130, k), 4, BF16, seed))
+        g.replay()
+        assert torch.equal(y, product(x, w))
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("n,k,off,stride", PLACES)
+def test_a_settled_weight_anywhere(n, k, off, stride, dtype):
+    stride = stride or k
+    w = torch.empty(off + n * stride, device="cuda").to(dtype).as_strided((n, k), (stride, 1), off)
+    w.copy_(integers((n, k), 4, dtype, 1))
+    f = Linear(w, settled=True)
+    for m in (1, 70):
+        x = integers((m, k), 4, dtype, m)
+        assert torch.equal(f(x, out_dtype=F32), product(x, w))
