@@ -163,6 +163,11 @@ def _fits(t: torch.Tensor) -> bool:
     return (one == 1 or width <= 1) and (rows <= 1 or stride >= width and stride * t.element_size() % 16 == 0)
 
 
+def _vector(t: torch.Tensor, n: int, device) -> torch.Tensor:
+    """One value or n as n fp32 values."""
+    return t.to(device=device, dtype=torch.float32).reshape(-1).expand(n).contiguous()
+
+
 class Linear(_Handle):
     """Y = act(x_scales * scales * X W^T + bias) + residual with W [out features, in features].
 
@@ -172,10 +177,12 @@ class Linear(_Handle):
 
     The weight is read where it lies, at each call, so that its buffer may be decoded into again.  Where it or its
     rows do not start on 16 bytes, each call lays it out in fresh memory first (a kernel that reads and writes
-    the whole weight), unless it is settled.
+    the whole weight), unless it is settled.  Scales and bias on the weight's device are read anew in the same way: contiguous fp32
+    vectors where they lie, others converted by each call.  What lies on another device, and a plain
+    number, is taken once, here.
 
-    settled: the weight does not change any more.  The device is synchronised here, a weight off 16 bytes is laid
-    out here once, and calls may read the weight before the work queued ahead of them is done
+    settled: weight, scales and bias do not change any more.  The device is synchronised here, what has to be laid out or
+    converted is so here once, and calls may read the weight before the work queued ahead of them is done
     (ANS_PRODUCT_WEIGHTS_SETTLED).  Leave it out where the weight's buffer is decoded into again.
     """
 
@@ -188,19 +195,26 @@ class Linear(_Handle):
         n, k = weight.shape
         self.weight = weight
         if scales is not None:
-            scales = torch.as_tensor(scales, dtype=torch.float32, device=self.device).reshape(-1)
+            scales = torch.as_tensor(scales, dtype=None if isinstance(scales, torch.Tensor) else torch.float32)
             _need(scales.numel() in (1, n), "scales must be one or one for each output feature")
-            scales = scales.expand(n).contiguous()
         if bias is not None:
             _need(bias.shape == (n,), "bias must have one value for each output feature")
-            bias = bias.to(device=self.device, dtype=torch.float32).contiguous()
         self.scales, self.bias, self.activation = scales, bias, activation
         self.in_features, self.out_features = k, n
         self._form, self._lies_off = self._new_form(), False
         self._desc = d = B.ans_product_desc()
         d.d_w, d.w_stride = weight.data_ptr() or None, max(weight.stride(0), k)
-        d.d_w_scales = scales.data_ptr() if scales is not None else None
-        d.d_bias = bias.data_ptr() if bias is not None else None
+        self._anew, self._taken = [], []
+        for field, t in (("d_w_scales", scales), ("d_bias", bias)):
+            if t is None:
+                continue
+            if t.device == self.device and t.dtype is torch.float32 and t.is_contiguous() and t.numel() == n:
+                setattr(d, field, t.data_ptr() or None)
+            elif t.device == self.device and not settled:
+                self._anew.append((field, t.detach()))
+            else:
+                self._taken.append(_vector(t.detach(), n, self.device))
+                setattr(d, field, self._taken[-1].data_ptr() or None)
         d.n, d.k, d.dtype, d.activation = n, k, _ELEMENT[weight.dtype], B.ACTIVATIONS[activation]
         self._weight_off = n > 0 and k > 0 and not (_fits(weight) and weight.data_ptr() % 16 == 0)
         if settled:
@@ -226,6 +240,10 @@ class Linear(_Handle):
             self._form.keep(x, x_scales, residual, out)
             at = self._form.places(x, x_scales, residual, out)
         d.d_x, d.d_x_scales, d.d_residual, d.d_y = at
+        if self._anew:
+            taken = [(field, _vector(t, d.n, self.device)) for field, t in self._anew]     # kept until the call is queued
+            for field, t in taken:
+                setattr(d, field, t.data_ptr())
         if self._weight_off:
             laid = self._lay_out(st)                       # kept until the call is queued  # noqa: F841
         if self._lies_off or at[0] % 16:

@@ -71,3 +71,38 @@ def test_a_settled_weight_anywhere(n, k, off, stride, dtype):
     for m in (1, 70):
         x = integers((m, k), 4, dtype, m)
         assert torch.equal(f(x, out_dtype=F32), product(x, w))
+
+
+def vectors(n):
+    """Tensors of n values in every form that is not the one the kernel reads."""
+    return {"fp32": torch.empty(n, device="cuda"), "bf16": torch.empty(n, device="cuda", dtype=BF16), "double": torch.empty(n, device="cuda", dtype=torch.float64),
+            "strided": torch.empty(n, 3, device="cuda")[:, 1]}
+
+
+@pytest.mark.parametrize("form", ["fp32", "bf16", "double", "strided"])
+def test_bias_and_scales_written_again_are_read_again(form):
+    n, k = 203, 64
+    w, x = integers((n, k), 4, BF16, 1), integers((9, k), 4, BF16, 2)
+    bias, scales = vectors(n)[form], vectors(n)[form]
+    f = Linear(w, scales=scales, bias=bias)
+    for seed in range(3):
+        bias.copy_(integers((n,), 9, F32, seed))
+        scales.copy_(2.0 ** integers((n,), 3, F32, seed + 7))
+        assert torch.equal(f(x, out_dtype=F32), product(x, w) * scales.float() + bias.float())
+    settled = Linear(w, scales=scales, bias=bias, settled=True)
+    assert torch.equal(settled(x, out_dtype=F32), product(x, w) * scales.float() + bias.float())
+
+
+def test_one_scale_for_all():
+    n, k = 130, 64
+    w, x = integers((n, k), 4, BF16, 1), integers((9, k), 4, BF16, 2)
+    scale = torch.full((1,), 0.5, device="cuda")
+    f = Linear(w, scales=scale)
+    for value in (0.25, 4.0):
+        scale.fill_(value)
+        assert torch.equal(f(x, out_dtype=F32), product(x, w) * value)
+    # numbers and tensors of another device are taken when the handle is made
+    there = torch.full((n,), 2.0)
+    by_number, by_host = Linear(w, scales=0.5, bias=there), Linear(w, scales=there, bias=torch.ones(n, dtype=torch.int32))
+    there.zero_()
+    assert torch.equal(by_number(x, out_dtype=F32), product(x, w) * 0.5 + 2) and torch.equal(by_host(x, out_dtype=F32), product(x, w) * 2 + 1)
