@@ -37,7 +37,11 @@ class _Handle:
     """A device, and the status word its calls report to.
 
     A call checks its tensors' types, shapes, strides and devices; where all of them are those of the
-    handle's last call (Form in csrc/torch) the checks' result is known and only the pointers change."""
+    handle's last call (Form in csrc/torch) the checks' result is known and only the pointers change.
+
+    Streams: making a handle waits for its stream, so that what the handle made of its own is complete for a call on
+    any other.  What a handle holds is marked as used by each stream it is called on (record_stream), so that a handle may be
+    dropped while its calls run.  A graph that holds calls needs the handle for as long as it is replayed."""
 
     def __init__(self, device):
         from ._ans_form import Form                        # built in-tree with the library
@@ -47,11 +51,24 @@ class _Handle:
         self.status = torch.zeros(64, dtype=torch.int32, device=self.device)
         self._status = self.status.data_ptr()
 
+    def _hold(self, *tensors) -> None:
+        """The end of making a handle: the tensors that its calls use besides those they are given."""
+        self._held = [t for t in (self.status, *tensors) if t is not None and t.device == self.device]
+        self._streams = {_current_stream(self._index)}
+        with torch.cuda.device(self.device):
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream().synchronize()
+
     def _enter(self) -> int:
         """The current stream; the library launches on the current device."""
         if _current_device() != self._index:
             raise RuntimeError(f"the handle is on {self.device}, which is not the current device")
-        return _current_stream(self._index)
+        stream = _current_stream(self._index)
+        if stream not in self._streams:
+            for t in self._held:
+                t.record_stream(torch.cuda.current_stream())
+            self._streams.add(stream)
+        return stream
 
     def read_status(self) -> int:
         """Waits for the stream; ANS_STATUS_* bits that calls have set since the last look (0: all sound)."""
@@ -89,6 +106,7 @@ class RmsNorm(_Handle):
         d.d_weight = weight.data_ptr() if weight is not None and weight.numel() else None
         d.weight_dtype = _ELEMENT[weight.dtype] if weight is not None else B.ANS_F32
         d.eps, d.out_dtype = self.eps, _ELEMENT[out_dtype]
+        self._hold(weight)
 
     def __call__(self, x: torch.Tensor, residual: torch.Tensor | None = None, out: torch.Tensor | None = None,
                  scales: torch.Tensor | None = None, summed: torch.Tensor | None = None):
@@ -220,9 +238,11 @@ class Linear(_Handle):
         if settled:
             if self._weight_off:
                 with torch.cuda.device(self.device):
-                    self._laid, self._weight_off = self._lay_out(_current_stream(self._index)), False
+                    self._taken.append(self._lay_out(_current_stream(self._index)))
+                self._weight_off = False
             torch.cuda.synchronize(self.device)
             d.flags = B.ANS_PRODUCT_WEIGHTS_SETTLED
+        self._hold(weight, scales, bias, *self._taken)
 
     def __call__(self, x: torch.Tensor, x_scales: torch.Tensor | None = None, residual: torch.Tensor | None = None,
                  out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
@@ -302,17 +322,17 @@ class PagedCache(_Handle):
             return torch.zeros(n_pages, page_size, heads, last, dtype=dtype, device=device)
 
         codes, groups = head_dim * bitwidth // 8, head_dim // group
-        self._hold(make(codes, torch.uint8), make(groups, torch.float32), make(groups, torch.uint8),
+        self._take(make(codes, torch.uint8), make(groups, torch.float32), make(groups, torch.uint8),
                    make(codes, torch.uint8), make(groups, torch.float32), make(groups, torch.uint8), bitwidth)
 
     @classmethod
     def wrap(cls, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth: int) -> "PagedCache":
         """A cache on existing arrays (shapes as in ans_cache_desc), which are used in place."""
         self = cls.__new__(cls)
-        self._hold(k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth)
+        self._take(k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth)
         return self
 
-    def _hold(self, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth):
+    def _take(self, k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros, bitwidth):
         _Handle.__init__(self, k_codes.device)
         _need(bitwidth in (4, 8), "bitwidth must be 8 or 4")
         _need(k_codes.dim() == 4 and k_scales.dim() == 4, "codes, scales and zeros have four dimensions")
@@ -335,6 +355,7 @@ class PagedCache(_Handle):
         d.d_v_codes, d.d_v_scales, d.d_v_zeros = v_codes.data_ptr(), v_scales.data_ptr(), v_zeros.data_ptr()
         d.n_pages, d.page_size, d.heads, d.head_dim = self.n_pages, self.page_size, self.heads, dim
         d.group, d.bitwidth = self.group, bitwidth
+        self._hold(k_codes, k_scales, k_zeros, v_codes, v_scales, v_zeros)
 
     def write(self, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
         """k, v: [tokens, heads, head_dim], bf16 or fp32, tokens and heads at any stride; slots: [tokens]
