@@ -429,7 +429,9 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
  *   h = x + residual (in fp32),   y = h * 1/sqrt(mean(h^2) + eps) * weight.
  * out_dtype ANS_BF16 or ANS_F32: d_out holds y, rounded once.  ANS_E4M3: d_out holds
  * q = e4m3(y / s) (to nearest even), d_scales the row's s = max(max|y| / 448, 2^-126).
- * A row with a NaN in it gets NaN everywhere, its scale too.
+ * A row with a NaN in it gets NaN everywhere, its scale too.  Finite rows of any size are computed: where the squares' sum
+ * leaves fp32's range (values above about 1e19, or under 1e-15 with eps < 2^-100) in scaled units.  Such a row in bf16 whose
+ * sum is stored over d_x or d_residual is computed from the sum as it is stored.
  * d_sum receives h, rounded once to x's type; it may be the same buffer as d_x or d_residual
  * (same stride).  width <= 32768.  Any alignment and any strides >= width; the fast path needs
  * the rows of all four matrices to start equally far from a multiple of 16 bytes (8 for 8-bit

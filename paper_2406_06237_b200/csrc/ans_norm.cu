@@ -6,6 +6,11 @@
 // second pass over the row: it is rsqrt(...) times the largest |h w|, so the sum of squares and the
 // maximum are reduced together, behind one barrier.
 //
+// Squares leave fp32's range long before the values do.  A row whose sum of squares is infinite, or (where eps is too
+// small to matter) next to nothing, is noted, and the threads that had it compute it again at their end, element by
+// element in units of 2^76 or 2^-76 (powers of two change no rounding).  The note costs other rows 0 to 2 %, narrow ones more (60000 x
+// 128: 16.1 to 18.4 us); the same in the middle of their work cost 1 to 6 %, and 20.2 us.
+//
 // Bound by memory for all but few or unaligned rows: 16384 x 8192 in bf16 with residual to e4m3 168 us, 5.6 TB/s, 85 % of the
 // rate of a copy; 8192 x 4096 from fp32 to bf16 33 us, 93 %; one row of 8192 2.8 us, its own latency; 5000 x 7777 in bf16
 // (rows off 16 bytes) 65 us, 73 %.
@@ -24,6 +29,8 @@ struct NormArgs {
   uint64_t x_step, r_step, out_step, sum_step; // bytes from a row to the next
   uint32_t width;
   float eps, part;        // part: 1 / width
+  float low;              // a sum of squares under this is taken again in smaller units; 0: none is, eps covers them
+  uint32_t in_place;      // the sum is stored over x or r
   uint32_t together;      // the rows of all matrices start equally far from a 16-byte boundary
   uint32_t shift;         // the most that a row starts past such a boundary, in elements
   uint32_t w_f32;         // type of w
@@ -148,7 +155,13 @@ __device__ __forceinline__ Pairs<H> weights(const NormArgs& a, int e, bool align
 }
 
 constexpr uint32_t kNormWarps = 32;
+constexpr float kUp = 75557863725914323419136.f, kDown = 1.f / kUp;      // 2^76, 2^-76
 constexpr size_t kNormRing = 216 * 1024;         // bytes of an SM's rings
+
+// an 8-bit row's scale from its largest magnitude
+__device__ __forceinline__ float scale_of(float amax) {
+  return amax != amax ? amax : fmaxf(amax * (1.f / 448.f), 1.17549435e-38f);                 // fmaxf alone would drop a NaN
+}
 
 // What the kernels share of a row: thread t of its T threads holds the V vectors of E elements t, t + T, ...
 // Where rows start `phase` elements past a 16-byte boundary, vector 0 starts `phase` elements before the
@@ -326,8 +339,7 @@ struct NormRow {
   __device__ __forceinline__ void store(uint64_t row, Two (&h)[V][H], float total, float top) const {
     float f = rsqrtf(fmaf(total, a.part, a.eps));
     if constexpr (sizeof(TO) == 1) {
-      const float amax = f * top;
-      const float s = amax != amax ? amax : fmaxf(amax * (1.f / 448.f), 1.17549435e-38f);   // fmaxf alone would drop a NaN
+      const float s = scale_of(f * top);
       if (t == 0) a.scales[row] = s;
       const float back = __frcp_rn(s);                            // at most 2^126
       if (!(f * back < INFINITY) && back < INFINITY) {            // tiny rows: not in one factor
@@ -349,9 +361,54 @@ struct NormRow {
   }
 };
 
+// Whether a row's sum of squares is out of range.  A NaN is not: its row is NaN whatever the units.
+__device__ __forceinline__ bool out_of_range(const NormArgs& a, float total) { return total == INFINITY || total < a.low; }
+
+// A row again if its sum of squares is out of range (or within 1 %: the sums' order differs here, and values may be
+// the stored ones), by the threads that had it.  Values are x + r, or the stored sum where that is exact (fp32) or lies over one of them.
+template <typename TX, typename TO>
+__device__ __noinline__ void redo(const NormArgs& a, uint64_t row, int t, int T, float* s_sum, float* s_top) {
+  using Row = NormRow<TX, TO, 1, false>;
+  const Row n(a, t, T, nullptr);
+  const char* const x = a.x + row * a.x_step;
+  const char* const r = a.r + row * a.r_step;
+  const char* const sum = a.sum + row * a.sum_step;
+  char* const out = a.out + row * a.out_step;
+  const int width = static_cast<int>(a.width);
+  const bool stored = a.sum && (sizeof(TX) == 4 || a.in_place);
+  auto value = [&](int e) { return stored ? one<TX>(sum, e) : a.r ? one<TX>(x, e) + one<TX>(r, e) : one<TX>(x, e); };
+  auto sync = [&] { if (T > 32) __syncthreads(); else __syncwarp(); };
+  sync();                                                         // what the row's threads stored is seen; the places are free
+  float total = 0.f, top = 0.f;
+  for (int e = t; e < width; e += T) { const float v = value(e); total = fmaf(v, v, total); }
+  n.reduce(total, top, s_sum, s_top);
+  if (!(total > 3.37e38f || total < 1.01f * a.low)) return;
+  const float unit = total < 1.f ? kUp : kDown;
+  auto weighed = [&](int e) {
+    const float w = !a.w ? 1.f : a.w_f32 ? one<float>(a.w, e) : one<__nv_bfloat16>(a.w, e);
+    return value(e) * unit * w;
+  };
+  total = 0.f;
+  for (int e = t; e < width; e += T) {
+    const float v = value(e) * unit;
+    total = fmaf(v, v, total);
+    if constexpr (sizeof(TO) == 1) { const float u = weighed(e); top = larger(top, two(u, u)); }
+  }
+  sync();
+  n.reduce(total, top, s_sum, s_top);
+  float f = rsqrtf(fmaf(total, a.part, a.eps * unit * unit)), back = 1.f;
+  if constexpr (sizeof(TO) == 1) {
+    const float s = scale_of(f * top);
+    if (t == 0) a.scales[row] = s;
+    back = __frcp_rn(s);
+  }
+  for (int e = t; e < width; e += T) put1<TO>(out, e, weighed(e) * f * back);
+  sync();
+}
+
 // A block a row: for few rows, where a row's own latency counts, and for rows that the rings below do not fit.
 template <typename TX, typename TO, int V, int MOST>
-__global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ __align__(16) float s_sum[kNormWarps], s_top[kNormWarps];
   __shared__ uint4 s_ends[kNormWarps][8];
   ten::let_next_start();
@@ -383,6 +440,7 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
   n.reduce(total, top, s_sum, s_top);
   n.store(blockIdx.x, h, total, top);
   n.put_ends();
+  if (out_of_range(a, total)) redo<TX, TO>(a, blockIdx.x, threadIdx.x, blockDim.x, s_sum, s_top);
 }
 
 // Persistent: blockDim = (threads of a row, rows of a block); a block takes row after row.  Every thread copies its
@@ -391,10 +449,11 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_kernel(const NormArgs a) {
 // barrier at all.  Even rows: a weight in bf16 stays in registers.  Others, whose vectors start at any element: the
 // weight lies in shared memory, element e at [e % E][e / E], where a warp's reads of any alignment meet no conflict.
 template <typename TX, typename TO, int V, int MOST, bool EVEN>
-__global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs a, const uint32_t depth) {
+__global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const __grid_constant__ NormArgs a, const uint32_t depth) {
   extern __shared__ uint4 ring[];
   __shared__ __align__(16) float s_sum[2][kNormWarps], s_top[2][kNormWarps];
   __shared__ uint4 s_ends[EVEN ? 1 : kNormWarps][8];
+  __shared__ uint32_t s_again[kNormWarps];
   ten::let_next_start();
   using Row = NormRow<TX, TO, V, EVEN>;
   constexpr int E = Row::E, H = Row::H;
@@ -452,6 +511,9 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
   }
 
   uint32_t from = mine, odd = 0;
+  uint32_t* const again = &s_again[(y * T + t) >> 5];
+  *again = 0u;
+  __syncwarp();
   for (uint64_t base = uint64_t(blockIdx.x) * Y; base < a.rows; base += step) {   // the same trips for all of the block
     fetch(spare);
     spare += per_row * 16u;
@@ -510,6 +572,7 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
     if (live) {
       n.store(row, h, total, top);
       n.put_ends();
+      if (out_of_range(a, total)) *again = 1u;
     }
     from += per_row * 16u;
     if (from == ring_end) from = mine;
@@ -521,6 +584,9 @@ __global__ void __launch_bounds__(MOST) ans_rms_norm_ring_kernel(const NormArgs 
     n.sum += sum_on;
     n.settle(row);
   }
+  __syncwarp();
+  if (*again)                                                      // the row's threads alike
+    for (row = uint64_t(blockIdx.x) * Y + y; row < a.rows; row += step) redo<TX, TO>(a, row, t, T, s_sum[0], s_top[0]);
 }
 
 // `blocks` blocks an SM split its shared memory; a ring of two to six rows
@@ -622,6 +688,9 @@ ANS_EXPORT int ans_rms_norm(const ans_norm_desc* h_desc, void* stream) {
   a.x_end = a.x + (d.rows - 1) * a.x_step + uint64_t(d.width) * xs;
   a.r_end = a.r + (d.rows - 1) * a.r_step + uint64_t(d.width) * xs;
   a.part = 1.f / static_cast<float>(d.width);
+  constexpr float kLittle = 7.8886091e-31f;                         // 2^-100: squares that vanish (2^-149 each) are nothing beside it
+  a.low = d.eps < kLittle ? kLittle : 0.f;
+  a.in_place = a.sum && (a.sum == a.x || a.sum == a.r);
   a.together = same(d.d_residual, xs, d.residual_stride) && same(d.d_out, os, d.out_stride) && same(d.d_sum, xs, d.sum_stride);
   a.shift = a.together && (at || (d.rows > 1 && d.x_stride % E)) ? E - 1 : 0u;
   a.w_f32 = d.weight_dtype == ANS_F32;
