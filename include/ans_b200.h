@@ -494,6 +494,9 @@ typedef struct ans_product_desc {
 int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
 /* Bytes of d_room that a call with this X needs (from d_x, x_stride, m, k and dtype); 0: none. */
 int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out);
+/* The form that a call with these sizes (m, n, k and dtype) takes on the current device: rows of X a tile, and the number of
+ * CTAs that share a tile's K (0: pairs of SMs take tile after tile). */
+int ans_product_form(const ans_product_desc* h_desc, uint32_t* h_tokens, uint32_t* h_parts);
 /* A matrix that lies anywhere (element (r, c) at d_from[r * stride + c * step], dtype ANS_BF16 or ANS_E4M3) laid out in rows
  * as ans_product reads them: d_to on 16 bytes, a row every k elements rounded up to whole 16 bytes, zeros behind
  * its end.  For a W that does not start, or whose rows do not all start, on 16 bytes.  rows <= 2^30, k <= 2^22. */

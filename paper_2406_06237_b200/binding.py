@@ -37,7 +37,7 @@ EXPORTS = [
     "ans_histogram_device", "ans_entropy_device", "ans_normalize_freqs_device",
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
-    "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_product_rows", "ans_cache_write", "ans_cache_read",
+    "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_product_rows", "ans_product_form", "ans_cache_write", "ans_cache_read",
 ]
 
 
@@ -139,6 +139,7 @@ def lib():
         L.ans_rms_norm.argtypes = [P(ans_norm_desc), vp]
         L.ans_product.argtypes = [P(ans_product_desc), vp, vp]
         L.ans_product_room_bytes.argtypes = [P(ans_product_desc), P(sz)]
+        L.ans_product_form.argtypes = [P(ans_product_desc), P(u32), P(u32)]
         L.ans_product_rows.argtypes = [vp, u64, u64, u32, u32, i32, vp, vp]
         L.ans_cache_write.argtypes = [P(ans_cache_desc), vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, vp]
         L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
@@ -373,6 +374,13 @@ def ans_product_room_bytes(h_desc: ans_product_desc) -> int:
     out = ctypes.c_size_t()
     _check(lib().ans_product_room_bytes(h_desc, ctypes.byref(out)), "ans_product_room_bytes")
     return out.value
+
+
+def ans_product_form(m: int, n: int, k: int, dtype: int):
+    """(rows of X a tile, CTAs that share a tile's K or 0)."""
+    tokens, parts = ctypes.c_uint32(), ctypes.c_uint32()
+    _check(lib().ans_product_form(ans_product_desc(m=m, n=n, k=k, dtype=dtype), ctypes.byref(tokens), ctypes.byref(parts)), "ans_product_form")
+    return tokens.value, parts.value
 
 
 def ans_product_rows(d_from: int, stride: int, step: int, rows: int, k: int, dtype: int, d_to: int, stream: int = 0) -> None:

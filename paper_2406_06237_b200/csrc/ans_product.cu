@@ -559,41 +559,49 @@ struct PrChoice {
   uint32_t tokens = 0, split = 0;                      // split = 0: the whole form
 };
 
+static uint32_t stages_of(const ans_product_desc& d) { return static_cast<uint32_t>((uint64_t(d.k) * (d.dtype == ANS_E4M3 ? 1 : 2) + kPrRow - 1) / kPrRow); }
+
 // The split form: every CTA one part of one tile; two CTAs an SM up to 64 tokens.
 template <uint32_t BN>
-static void weigh_split(const ans_product_desc& d, const PrArgs& a, int sms, PrChoice& best) {
+static void weigh_split(const ans_product_desc& d, uint32_t steps, int sms, PrChoice& best) {
   using S = PrShape<BN, 1, 1, true>;
   constexpr float kEnd = BN == 16 ? 1.2f : BN == 32 ? 1.5f : BN == 64 ? 2.8f : 3.5f;
   constexpr float kRing = S::kStages * S::kStage / 1.36e3f;           // GB/s
   const uint64_t tiles = uint64_t((d.n + 127) / 128) * ((d.m + BN - 1) / BN), slots = uint64_t(sms) * (BN <= 64 ? 2 : 1);
   // Clusters of 8 with an SM for each CTA do not all fit the GPU's groups of SMs at once: 100 x 2048 x 8192 24 us against
   // 15 in fours.
-  for (uint32_t split = 1; split <= (BN <= 64 ? 8u : 4u) && (split == 1 || split <= a.steps); split *= 2) {
+  for (uint32_t split = 1; split <= (BN <= 64 ? 8u : 4u) && (split == 1 || split <= steps); split *= 2) {
     const uint64_t ctas = tiles * split, waves = (ctas + slots - 1) / slots;
     const uint64_t beside = waves > 1 ? slots / sms : (ctas + sms - 1) / sms;   // CTAs of an SM
     const float rate = fminf(kRing, 118.f / beside);
-    const float us = 2.f + waves * (kEnd + (a.steps + split - 1) / split * (S::kStage / 1e3f) / rate);
+    const float us = 2.f + waves * (kEnd + (steps + split - 1) / split * (S::kStage / 1e3f) / rate);
     if (us < best.us) best = {us, BN, split};
   }
 }
 
-template <bool F8>
-static int choose_product(const ans_product_desc& d, const PrArgs& a, int sms, cudaStream_t st) {
+static PrChoice choose(const ans_product_desc& d, int sms) {
+  const uint32_t steps = stages_of(d);
   PrChoice best;
-  weigh_split<16>(d, a, sms, best);
-  if (d.m > 16) weigh_split<32>(d, a, sms, best);
-  if (d.m > 32) weigh_split<64>(d, a, sms, best);
-  if (d.m > 64) weigh_split<128>(d, a, sms, best);
+  weigh_split<16>(d, steps, sms, best);
+  if (d.m > 16) weigh_split<32>(d, steps, sms, best);
+  if (d.m > 32) weigh_split<64>(d, steps, sms, best);
+  if (d.m > 64) weigh_split<128>(d, steps, sms, best);
   if (d.m > 64 && sms > 1) {
     // The whole forms on pairs of SMs: a stage of 256 tokens 0.31 us, of 512 tokens 0.55 us (they read W once for both
     // halves and move a quarter less into shared memory, but nothing runs under a tile's end): 8192^3 in bf16 power-
     // capped 830 us in 512s, 900 in 256s; 4096 x 4096 x 1024 43 and 38.
     const uint64_t pairs = sms / 2, wide_f = (d.n + 255) / 256;
     auto rounds = [&](uint32_t tokens) { return static_cast<float>((wide_f * ((d.m + tokens - 1) / tokens) + pairs - 1) / pairs); };
-    const float us256 = 6.5f + rounds(256) * a.steps * 0.31f, us512 = 3.5f + rounds(512) * (a.steps * 0.55f + 5.f);
+    const float us256 = 6.5f + rounds(256) * steps * 0.31f, us512 = 3.5f + rounds(512) * (steps * 0.55f + 5.f);
     if (us256 < best.us) best = {us256, 256, 0};
     if (us512 < best.us) best = {us512, 512, 0};
   }
+  return best;
+}
+
+template <bool F8>
+static int launch_choice(const ans_product_desc& d, const PrArgs& a, int sms, cudaStream_t st) {
+  const PrChoice best = choose(d, sms);
   switch (best.tokens) {
     case 16: return launch_product<16, 1, 1, F8, true>(d, a, best.split, sms, st);
     case 32: return launch_product<32, 1, 1, F8, true>(d, a, best.split, sms, st);
@@ -644,6 +652,20 @@ ANS_EXPORT int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_
   return ANS_OK;
 }
 
+ANS_EXPORT int ans_product_form(const ans_product_desc* h_desc, uint32_t* h_tokens, uint32_t* h_parts) {
+  if (!h_desc || !h_tokens || !h_parts) return ANS_ERR_INVALID_ARG;
+  if (h_desc->dtype != ANS_BF16 && h_desc->dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
+  *h_tokens = *h_parts = 0;
+  if (h_desc->m == 0 || h_desc->n == 0) return ANS_OK;
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc != ANS_OK) return rc;
+  const PrChoice best = choose(*h_desc, sms);
+  *h_tokens = best.tokens;
+  *h_parts = best.split;
+  return ANS_OK;
+}
+
 ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream) {
   ApiRange range("ans_product");
   if (!h_desc || !d_status) return ANS_ERR_INVALID_ARG;
@@ -682,11 +704,11 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   PrArgs a{};
   a.x_scales = d.d_x_scales; a.w_scales = d.d_w_scales; a.bias = d.d_bias;
   a.residual = d.d_residual; a.y = d.d_y; a.residual_stride = d.residual_stride; a.y_stride = d.y_stride;
-  a.M = d.m; a.N = d.n; a.steps = static_cast<uint32_t>((d.k * es + kPrRow - 1) / kPrRow);
+  a.M = d.m; a.N = d.n; a.steps = stages_of(d);
   a.activation = d.activation;
   a.settled = (d.flags & ANS_PRODUCT_WEIGHTS_SETTLED) != 0;
   auto four = [&](const void* p, uint64_t stride) { return !p || !((reinterpret_cast<uintptr_t>(p) | (d.m > 1 ? stride * ys : 0)) & (4 * ys - 1)); };
   a.wide = four(d.d_y, d.y_stride) && four(d.d_residual, d.residual_stride);
   a.status = d_status;
-  return d.dtype == ANS_E4M3 ? choose_product<true>(d, a, sms, st) : choose_product<false>(d, a, sms, st);
+  return d.dtype == ANS_E4M3 ? launch_choice<true>(d, a, sms, st) : launch_choice<false>(d, a, sms, st);
 }

@@ -15,3 +15,14 @@ P = 1 << 20                                              # an address on every b
 def test_product_rows(kw, rc):
     a = {**dict(d_from=P, stride=65, step=1, rows=4, k=65, dtype=ans.ANS_BF16, d_to=P), **kw}
     assert ans.lib().ans_product_rows(*(a[f] for f in ("d_from", "stride", "step", "rows", "k", "dtype", "d_to")), None) == rc
+
+
+def test_product_form():
+    import ctypes
+    d, t, p = ans.binding.ans_product_desc(m=3, n=4, k=5, dtype=ans.ANS_BF16), ctypes.c_uint32(), ctypes.c_uint32()
+    f = ans.lib().ans_product_form
+    assert f(None, ctypes.byref(t), ctypes.byref(p)) == f(d, None, ctypes.byref(p)) == f(d, ctypes.byref(t), None) == INVALID
+    d.dtype = ans.ANS_F32
+    assert f(d, ctypes.byref(t), ctypes.byref(p)) == UNSUPPORTED
+    d.dtype, d.m = ans.ANS_E4M3, 0
+    assert f(d, ctypes.byref(t), ctypes.byref(p)) == 0 and t.value == p.value == 0
