@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
+#include <memory>
 #include <vector>
 
 namespace {
@@ -126,6 +127,10 @@ PyMODINIT_FUNC PyInit__ans_form() {
   Py_INCREF(&kType);
   if (PyModule_AddObject(m, "Form", reinterpret_cast<PyObject*>(&kType)) < 0) {
     Py_DECREF(&kType);
+    Py_DECREF(m);
+    return nullptr;
+  }
+  if (PyModule_AddStringConstant(m, "MADE_FOR", ANS_MADE_FOR) < 0) {
     Py_DECREF(m);
     return nullptr;
   }

@@ -7,6 +7,7 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
+from . import build as _build
 
 _ELEMENT = {torch.bfloat16: B.ANS_BF16, torch.float32: B.ANS_F32, torch.float8_e4m3fn: B.ANS_E4M3}
 
@@ -33,6 +34,18 @@ _current_device = torch._C._cuda_getDevice
 _current_stream = torch._C._cuda_getCurrentRawStream
 
 
+def _form_type():
+    """The type that compares tensors' forms, out of the module built in-tree with the library."""
+    again = "run paper_2406_06237_b200.build.build() (needs g++ and torch's headers); there is no fallback path"
+    try:
+        from . import _ans_form
+    except ImportError as e:
+        raise ImportError(f"{_build.FORM} is missing or does not load: {again}") from e
+    if _ans_form.MADE_FOR != _build.form_interface():
+        raise ImportError(f"{_build.FORM} was built for {_ans_form.MADE_FOR}, this is {_build.form_interface()}: {again}")
+    return _ans_form.Form
+
+
 class _Handle:
     """A device, and the status word its calls report to.
 
@@ -44,8 +57,7 @@ class _Handle:
     dropped while its calls run.  A graph that holds calls needs the handle for as long as it is replayed."""
 
     def __init__(self, device):
-        from ._ans_form import Form                        # built in-tree with the library
-        self._new_form = Form
+        self._new_form = _form_type()
         self.device = _cuda_device(device)
         self._index = self.device.index
         self.status = torch.zeros(64, dtype=torch.int32, device=self.device)

@@ -26,3 +26,48 @@ def test_product_form():
     assert f(d, ctypes.byref(t), ctypes.byref(p)) == UNSUPPORTED
     d.dtype, d.m = ans.ANS_E4M3, 0
     assert f(d, ctypes.byref(t), ctypes.byref(p)) == 0 and t.value == p.value == 0
+
+
+def test_a_missing_or_foreign_module_says_what_to_run(monkeypatch):
+    """Without the module of tensor forms, or with one of another torch or Python, a handle says so; nothing is guessed."""
+    import sys
+    import types
+
+    import paper_2406_06237_b200 as package
+    from paper_2406_06237_b200 import operators
+    name = "paper_2406_06237_b200._ans_form"
+    monkeypatch.delattr(package, "_ans_form", raising=False)
+    monkeypatch.setitem(sys.modules, name, None)
+    with pytest.raises(ImportError, match=r"build\.build\(\)"):
+        operators._form_type()
+    other = types.ModuleType(name)
+    other.MADE_FOR, other.Form = "torch 1.0, cpython-27", object
+    monkeypatch.setitem(sys.modules, name, other)
+    with pytest.raises(ImportError, match=r"torch 1\.0.*build\.build\(\)"):
+        operators._form_type()
+    monkeypatch.undo()
+    assert operators._form_type()().places() is None
+
+
+def test_the_module_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
+    from paper_2406_06237_b200 import build
+    binary, noted = tmp_path / "form.so", tmp_path / "made_for"
+    monkeypatch.setattr(build, "FORM", str(binary))
+    monkeypatch.setattr(build, "FORM_MADE_FOR", str(noted))
+    assert not build.form_is_current()
+    binary.write_bytes(b"")
+    assert not build.form_is_current()                   # built by something that noted nothing
+    noted.write_text("torch 1.0, cpython-27")
+    assert not build.form_is_current()
+    noted.write_text(build.form_interface())
+    assert build.form_is_current()
+
+
+def test_build_builds_both(monkeypatch):
+    from paper_2406_06237_b200 import build
+    asked = []
+    monkeypatch.setattr(build, "build_form", lambda force=False: asked.append(force))
+    monkeypatch.setattr(build, "sources", lambda: [])
+    monkeypatch.setattr(build.subprocess, "check_call", lambda cmd: asked.append("nvcc"))
+    build.build(force=True)
+    assert asked == [True, "nvcc"]
