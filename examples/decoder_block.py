@@ -8,7 +8,8 @@ q - zero_point; the others are decoded to bf16.  The attention itself is plain t
 
     python examples/decoder_block.py [--width 1024] [--heads 8] [--prompt 200] [--tokens 16] [--bits 8]
 
-prints the largest deviation from the same block in fp32 (unquantised activations and cache) and the time of a token.
+prints the norm of the deviation from the same block in fp32 (unquantised activations and cache), relative to the norm of its
+output, and the time of a token.
 """
 import argparse
 import os
@@ -33,7 +34,7 @@ def draw_symbols(rng, n, k, bits):
 
 
 class Weights:
-    """Six matrices, packed, put on the GPU in compressed form and decoded by one launch."""
+    """Four matrices, packed, put on the GPU in compressed form and decoded by one launch."""
 
     def __init__(self, width, hidden, seed):
         rng = np.random.default_rng(seed)

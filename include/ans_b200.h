@@ -417,7 +417,7 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
 
 /* ------------------------------------------------------------------------------------
  * The operators around a product with decoded weights.
- * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where X's rows
+ * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where X or its rows
  * start off 16 bytes) and return without waiting; they keep nothing from one call for the next.  The
  * kernels may take their place while the work queued ahead drains; they touch memory only once it is
  * complete (weights that the caller calls settled apart).  Calls with no rows, tokens or features do
@@ -428,7 +428,10 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
  * Root-mean-square norm of every row, with the residual's addition before it:
  *   h = x + residual (in fp32),   y = h * 1/sqrt(mean(h^2) + eps) * weight.
  * out_dtype ANS_BF16 or ANS_F32: d_out holds y, rounded once.  ANS_E4M3: d_out holds
- * q = e4m3(y / s) (to nearest even), d_scales the row's s = max(max|y| / 448, 2^-126).
+ * q = e4m3(y / s) (to nearest even), d_scales the row's s = max(max|y| / 448, 2^-126).  In fp32 as
+ *   f = rsqrtf(sum of h^2 * (1 / width) + eps),  y = (h * weight) * f,  s = max(f * max|h weight| * (1 / 448), 2^-126),
+ *   q = e4m3((h * weight) * (f * (1 / s))),
+ * every constant and reciprocal rounded: s is within 2^-18 of the formula's, and a q near the middle of two codes may be the other one.
  * A row with a NaN in it gets NaN everywhere, its scale too.  Finite rows of any size are computed: where the squares' sum
  * leaves fp32's range (values above about 1e19, or under 1e-15 with eps < 2^-100) in scaled units.  Such a row in bf16 whose
  * sum is stored over d_x or d_residual is computed from the sum as it is stored.
@@ -465,7 +468,9 @@ int ans_rms_norm(const ans_norm_desc* h_desc, void* stream);
  *   Y[m][n] = act( x_scale[m] * w_scale[n] * sum_k X[m][k] W[n][k] + bias[n] ) + residual[m][n].
  * X and W are both ANS_BF16 (weights as the decode calls write them) or both ANS_E4M3 (rows of
  * ans_rms_norm; symbols q - zero_point of weights of up to 4 bits are integers of at most 15 and
- * exact in e4m3).  The epilogue works in fp32 and rounds once.
+ * exact in e4m3).  The epilogue works in fp32 and rounds once; exponentials and reciprocals are the hardware's approximations and the
+ * error function is a polynomial's, so that the three smooth activations are within 2^-20 of |v|, not of their own value: gelu(-4) in
+ * fp32 has a relative error of 5e-4.
  * d_w 16-byte aligned, its stride a multiple of 16 bytes; columns from k on are never used.  Where d_x or
  * its stride are not so, the rows of X are first copied (a second kernel) into d_room, 16-byte aligned, of
  * ans_product_room_bytes() bytes, which is free again when the call's work is done.  y and residual of any alignment; d_residual may be d_y (same stride).

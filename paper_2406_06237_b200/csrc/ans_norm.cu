@@ -8,11 +8,11 @@
 //
 // Squares leave fp32's range long before the values do.  A row whose sum of squares is infinite, or (where eps is too
 // small to matter) next to nothing, is noted, and the threads that had it compute it again at their end, element by
-// element in units of 2^76 or 2^-76 (powers of two change no rounding).  The note costs other rows 0 to 2 %, narrow ones more (60000 x
+// element in units of 2^76 or 2^-76 (powers of two change no rounding).  The note costs other rows 0 to 3 %, narrow ones more (60000 x
 // 128: 16.1 to 18.4 us); the same in the middle of their work cost 1 to 6 %, and 20.2 us.
 //
-// Bound by memory for all but few or unaligned rows: 16384 x 8192 in bf16 with residual to e4m3 168 us, 5.6 TB/s, 85 % of the
-// rate of a copy; 8192 x 4096 from fp32 to bf16 33 us, 93 %; one row of 8192 2.8 us, its own latency; 5000 x 7777 in bf16
+// Bound by memory for all but few or unaligned rows: 16384 x 8192 in bf16 with residual to e4m3 169 us, 5.6 TB/s, 85 % of the
+// rate of a copy; 8192 x 4096 from fp32 to bf16 32 us, 95 %; one row of 8192 2.8 us, its own latency; 5000 x 7777 in bf16
 // (rows off 16 bytes) 65 us, 73 %.
 #include <cmath>
 #include <type_traits>

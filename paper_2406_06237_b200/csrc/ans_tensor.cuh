@@ -20,7 +20,7 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
 
 // ---- launches that overlap their ends ------------------------------------------------------
 // Every kernel lets the next one on its stream be set up while it runs, and touches no global memory
-// before the work queued ahead of it is complete.
+// before the work queued ahead of it is complete, but for weights that the caller calls settled.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

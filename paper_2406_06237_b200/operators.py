@@ -1,7 +1,9 @@
 """The operators around a product with decoded weights, on torch tensors: torch supplies memory and the
 stream, the library's kernels compute.  A handle keeps what does not change between calls (weights and
 a call descriptor), never an input or an output, and is used by one thread at a time.  Every call
-enqueues on the current stream of its tensors' device and returns without waiting."""
+enqueues on the current stream of its tensors' device and returns without waiting.
+
+For inference: results carry no graph, and a tensor that requires a gradient is taken by its values."""
 from __future__ import annotations
 
 import torch
@@ -321,7 +323,11 @@ class PagedCache(_Handle):
     `group` values of a (token, head) as they are written (see ans_cache_desc in the header).
 
     Pages are the caller's to assign: token i of a sequence lies in slot
-    table[i // page_size] * page_size + i % page_size."""
+    table[i // page_size] * page_size + i % page_size.
+
+    group: a multiple of 16 up to 256, head_dim unless given; a cache of other groups can be made, its calls are refused.  The
+    cache saves room, not traffic: a step that reads it back moves the codes, writes 2 or 4 bytes a value and reads
+    those again."""
 
     def __init__(self, n_pages: int, page_size: int, heads: int, head_dim: int, bitwidth: int = 8, group: int | None = None, device="cuda"):
         group = head_dim if group is None else group
@@ -402,7 +408,10 @@ class PagedCache(_Handle):
         """The keys and values of whole sequences, one after the other: [rows, heads, head_dim] each.
         tables: [sequences, pages] int32; starts: [sequences + 1] int32, sequence s is rows starts[s] to
         starts[s + 1].  rows = starts[-1] as a number (the call does not read it from the device), or
-        k_out and v_out of that many rows are given.  Returns (k, v)."""
+        k_out and v_out of that many rows are given.  Returns (k, v).
+
+        A loop whose sequences grow gives the same buffers, long enough for all its steps, and no rows: the
+        form of its calls is then the same each time, and their checks' result is known."""
         st = self._enter()
         if (k_out is None) != (v_out is None):
             raise ValueError("give both of k_out and v_out or none")

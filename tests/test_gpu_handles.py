@@ -106,3 +106,11 @@ def test_one_scale_for_all():
     by_number, by_host = Linear(w, scales=0.5, bias=there), Linear(w, scales=there, bias=torch.ones(n, dtype=torch.int32))
     there.zero_()
     assert torch.equal(by_number(x, out_dtype=F32), product(x, w) * 0.5 + 2) and torch.equal(by_host(x, out_dtype=F32), product(x, w) * 2 + 1)
+
+
+@pytest.mark.parametrize("k", [64, 67])
+def test_tensors_that_require_a_gradient_are_taken_by_their_values(k):
+    w, x, bias = integers((130, k), 4, BF16, 1), integers((9, k), 4, BF16, 2), integers((130,), 4, BF16, 3)
+    want = product(x, w) + bias.float()
+    y = Linear(w.requires_grad_(), bias=bias.requires_grad_())(x.requires_grad_(), out_dtype=F32)
+    assert torch.equal(y, want) and not y.requires_grad
