@@ -417,7 +417,7 @@ int ans_decode_gemm_bf16(const ans_layer_desc* h_desc, const void* d_x, int M, i
 
 /* ------------------------------------------------------------------------------------
  * The operators around a product with decoded weights.
- * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where X or its rows
+ * All take strides in ELEMENTS, enqueue one kernel on `stream` (ans_product two where rows
  * start off 16 bytes) and return without waiting; they keep nothing from one call for the next.  The
  * kernels may take their place while the work queued ahead drains; they touch memory only once it is
  * complete (weights that the caller calls settled apart).  Calls with no rows, tokens or features do
@@ -471,8 +471,8 @@ int ans_rms_norm(const ans_norm_desc* h_desc, void* stream);
  * exact in e4m3).  The epilogue works in fp32 and rounds once; exponentials and reciprocals are the hardware's approximations and the
  * error function is a polynomial's, so that the three smooth activations are within 2^-20 of |v|, not of their own value: gelu(-4) in
  * fp32 has a relative error of 5e-4.
- * d_w 16-byte aligned, its stride a multiple of 16 bytes; columns from k on are never used.  Where d_x or
- * its stride are not so, the rows of X are first copied (a second kernel) into d_room, 16-byte aligned, of
+ * d_w 16-byte aligned, its stride a multiple of 16 bytes (but see ANS_PRODUCT_WEIGHTS_ANYWHERE); columns from k on are never used.
+ * Where d_x or its stride are not so, the rows of X are first copied (a second kernel) into d_room, 16-byte aligned, of
  * ans_product_room_bytes() bytes, which is free again when the call's work is done.  y and residual of any alignment; d_residual may be d_y (same stride).
  * d_status as for the decode calls (ANS_STATUS_COPY_TIMEOUT).
  */
@@ -490,21 +490,25 @@ typedef struct ans_product_desc {
   int32_t      y_dtype;           /* ANS_BF16 or ANS_F32                                     */
   int32_t      activation;        /* ANS_ACT_*                                               */
   uint32_t     flags;             /* ANS_PRODUCT_*, or 0                                     */
-  void*        d_room;            /* see above; NULL where X's rows start on 16 bytes        */
+  void*        d_room;            /* see above; NULL where all rows start on 16 bytes        */
   uint64_t     room_bytes;
 } ans_product_desc;
 /* The caller knows that d_w was on the device before the work queued ahead of this call began, and that
  * that work does not write it: the call may then read W before that work is done. */
 #define ANS_PRODUCT_WEIGHTS_SETTLED 1u
+/* d_w and its rows may start anywhere: where they do not on 16 bytes, W is copied into d_room as well, by the same kernel as X
+ * and in front of it, and counts as not settled. */
+#define ANS_PRODUCT_WEIGHTS_ANYWHERE 4u
 int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, void* stream);
-/* Bytes of d_room that a call with this X needs (from d_x, x_stride, m, k and dtype); 0: none. */
+/* Bytes of d_room that a call with this X needs (from d_x, x_stride, m, k and dtype; with ANS_PRODUCT_WEIGHTS_ANYWHERE in flags from
+ * d_w, w_stride and n too); 0: none. */
 int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out);
 /* The form that a call with these sizes (m, n, k and dtype) takes on the current device: rows of X a tile, and the number of
  * CTAs that share a tile's K (0: pairs of SMs take tile after tile). */
 int ans_product_form(const ans_product_desc* h_desc, uint32_t* h_tokens, uint32_t* h_parts);
 /* A matrix that lies anywhere (element (r, c) at d_from[r * stride + c * step], dtype ANS_BF16 or ANS_E4M3) laid out in rows
  * as ans_product reads them: d_to on 16 bytes, a row every k elements rounded up to whole 16 bytes, zeros behind
- * its end.  For a W that does not start, or whose rows do not all start, on 16 bytes.  rows <= 2^30, k <= 2^22. */
+ * its end.  For a W that is laid out once, or whose columns are not contiguous.  rows <= 2^30, k <= 2^22. */
 int ans_product_rows(const void* d_from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, int dtype, void* d_to, void* stream);
 
 /*

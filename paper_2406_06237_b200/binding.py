@@ -23,7 +23,7 @@ ANS_E4M3 = 3
 DTYPES = {"u8": ANS_U8, "f32": ANS_F32, "bf16": ANS_BF16}
 ELEM_SIZE = {ANS_U8: 1, ANS_F32: 4, ANS_BF16: 2}
 ANS_STATUS_BAD_PAGE = 16
-ANS_PRODUCT_WEIGHTS_SETTLED = 1
+ANS_PRODUCT_WEIGHTS_SETTLED, ANS_PRODUCT_WEIGHTS_ANYWHERE = 1, 4
 ANS_ACT_NONE, ANS_ACT_RELU, ANS_ACT_GELU, ANS_ACT_GELU_TANH, ANS_ACT_SILU = 0, 1, 2, 3, 4
 ACTIVATIONS = {"none": ANS_ACT_NONE, "relu": ANS_ACT_RELU, "gelu": ANS_ACT_GELU, "gelu_tanh": ANS_ACT_GELU_TANH,
                "silu": ANS_ACT_SILU}

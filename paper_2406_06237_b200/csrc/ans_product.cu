@@ -465,21 +465,29 @@ ans_product_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_const
   if (lane == 0 && bad) atomicOr(a.status, ANS_STATUS_COPY_TIMEOUT);
 }
 
-// Rows that start anywhere, elements `step` apart, into rows that start on 16 bytes, zeros behind their ends: 16 bytes of a row
-// a thread, element by element (the elements' neighbours come out of L1).  T: an element's bits.
-template <typename T>
-__global__ void __launch_bounds__(256) ans_product_rows_kernel(const T* x, uint64_t stride, uint64_t step, uint4* room, uint32_t rows, uint32_t k, uint32_t pieces) {
+// Rows that start anywhere, elements `step` apart, into rows that start on 16 bytes, zeros behind their ends, of one matrix or of
+// two in one launch: 16 bytes of a row a thread, element by element (the elements' neighbours come out of L1).  5 TB/s read and
+// written at 8192 x 8191 in bf16.  T: an element's bits; UNIT: all steps are 1.
+struct PrRows {
+  const void* from; uint64_t stride, step;
+  uint4* to;
+  uint32_t rows, blocks;
+};
+template <typename T, bool UNIT>
+__global__ void __launch_bounds__(256) ans_product_rows_kernel(const PrRows first, const PrRows second, uint32_t k, uint32_t pieces) {
   constexpr uint32_t kIn = 16 / sizeof(T);
   let_next_start();
-  const uint64_t i = uint64_t(blockIdx.x) * 256u + threadIdx.x;
+  const bool one = blockIdx.x < first.blocks;
+  const PrRows& a = one ? first : second;
+  const uint64_t i = uint64_t(blockIdx.x - (one ? 0u : first.blocks)) * 256u + threadIdx.x;
   wait_for_previous();
   const uint64_t row = i / pieces;
-  if (row >= rows) return;
+  if (row >= a.rows) return;
   const uint32_t e = static_cast<uint32_t>(i - row * pieces) * kIn;
-  const T* const p = x + row * stride + e * step;
+  const T* const p = static_cast<const T*>(a.from) + row * a.stride + (UNIT ? e : e * a.step);
   T v[kIn];
 #pragma unroll
-  for (uint32_t j = 0; j < kIn; ++j) v[j] = e + j < k ? p[j * step] : T(0);
+  for (uint32_t j = 0; j < kIn; ++j) v[j] = e + j < k ? p[UNIT ? j : j * a.step] : T(0);
   uint4 out;
   uint32_t* const w = &out.x;
 #pragma unroll
@@ -488,7 +496,7 @@ __global__ void __launch_bounds__(256) ans_product_rows_kernel(const T* x, uint6
 #pragma unroll
     for (uint32_t b = 0; b < kIn / 4; ++b) w[j] |= uint32_t(v[j * (kIn / 4) + b]) << (8 * sizeof(T) * b);
   }
-  room[i] = out;
+  a.to[i] = out;
 }
 
 // ---- host side -----------------------------------------------------------------------------
@@ -617,21 +625,32 @@ static int launch_choice(const ans_product_desc& d, const PrArgs& a, int sms, cu
 
 using namespace ansb;
 
-// whether TMA can read X's rows
-static bool rows_fit(const ans_product_desc& d, uint64_t es) {
-  return !(reinterpret_cast<uintptr_t>(d.d_x) & 15) && (d.m <= 1 || !((d.x_stride * es) & 15));
+// whether TMA can read a matrix's rows
+static bool rows_fit(const void* p, uint64_t stride, uint32_t rows, uint64_t es) {
+  return !(reinterpret_cast<uintptr_t>(p) & 15) && (rows <= 1 || !((stride * es) & 15));
 }
 static uint64_t room_row(uint32_t k, uint64_t es) { return (k * es + 15) & ~uint64_t(15); }
+// bytes of the room for W, which comes first, and for X
+static uint64_t room_w(const ans_product_desc& d, uint64_t es) {
+  return !(d.flags & ANS_PRODUCT_WEIGHTS_ANYWHERE) || rows_fit(d.d_w, d.w_stride, d.n, es) ? 0 : d.n * room_row(d.k, es);
+}
+static uint64_t room_x(const ans_product_desc& d, uint64_t es) {
+  return rows_fit(d.d_x, d.x_stride, d.m, es) ? 0 : d.m * room_row(d.k, es);
+}
 
-static int lay_out(const void* from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, uint64_t es, void* to, cudaStream_t st) {
-  const uint64_t pieces = room_row(k, es) / 16, blocks = (rows * pieces + 255) / 256;
-  if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(blocks));
-  uint4* const room = static_cast<uint4*>(to);
-  return es == 1 ? launch(ans_product_rows_kernel<uint8_t>, grid, dim3(256), 0, st, 1, static_cast<const uint8_t*>(from), stride, step, room, rows, k,
-                          static_cast<uint32_t>(pieces))
-                 : launch(ans_product_rows_kernel<uint16_t>, grid, dim3(256), 0, st, 1, static_cast<const uint16_t*>(from), stride, step, room, rows, k,
-                          static_cast<uint32_t>(pieces));
+static int lay_out(PrRows first, PrRows second, uint32_t k, uint64_t es, cudaStream_t st) {
+  const uint64_t pieces = room_row(k, es) / 16;
+  uint64_t blocks = 0;
+  for (PrRows* r : {&first, &second}) {
+    const uint64_t own = (r->rows * pieces + 255) / 256;
+    blocks += own;
+    if (blocks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+    r->blocks = static_cast<uint32_t>(own);
+  }
+  const bool unit = first.step == 1 && (second.step == 1 || !second.rows);
+  auto* const kernel = es == 1 ? (unit ? ans_product_rows_kernel<uint8_t, true> : ans_product_rows_kernel<uint8_t, false>)
+                               : (unit ? ans_product_rows_kernel<uint16_t, true> : ans_product_rows_kernel<uint16_t, false>);
+  return launch(kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, 1, first, second, k, static_cast<uint32_t>(pieces));
 }
 
 ANS_EXPORT int ans_product_rows(const void* d_from, uint64_t stride, uint64_t step, uint32_t rows, uint32_t k, int dtype, void* d_to, void* stream) {
@@ -642,14 +661,14 @@ ANS_EXPORT int ans_product_rows(const void* d_from, uint64_t stride, uint64_t st
   if (rows == 0 || k == 0) return ANS_OK;
   const uint64_t es = dtype == ANS_E4M3 ? 1 : 2;
   if (!d_from || !d_to || (reinterpret_cast<uintptr_t>(d_from) & (es - 1)) || (reinterpret_cast<uintptr_t>(d_to) & 15)) return ANS_ERR_INVALID_ARG;
-  return lay_out(d_from, stride, step, rows, k, es, d_to, static_cast<cudaStream_t>(stream));
+  return lay_out({d_from, stride, step, static_cast<uint4*>(d_to), rows, 0}, {}, k, es, static_cast<cudaStream_t>(stream));
 }
 
 ANS_EXPORT int ans_product_room_bytes(const ans_product_desc* h_desc, size_t* h_bytes_out) {
   if (!h_desc || !h_bytes_out) return ANS_ERR_INVALID_ARG;
   if (h_desc->dtype != ANS_BF16 && h_desc->dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
   const uint64_t es = h_desc->dtype == ANS_E4M3 ? 1 : 2;
-  *h_bytes_out = rows_fit(*h_desc, es) ? 0 : h_desc->m * room_row(h_desc->k, es);
+  *h_bytes_out = room_w(*h_desc, es) + room_x(*h_desc, es);
   return ANS_OK;
 }
 
@@ -673,31 +692,36 @@ ANS_EXPORT int ans_product(const ans_product_desc* h_desc, uint32_t* d_status, v
   ans_product_desc d = *h_desc;
   if (d.dtype != ANS_BF16 && d.dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
   if (d.y_dtype != ANS_BF16 && d.y_dtype != ANS_F32) return ANS_ERR_UNSUPPORTED;
-  if (d.flags & ~ANS_PRODUCT_WEIGHTS_SETTLED) return ANS_ERR_UNSUPPORTED;
+  if (d.flags & ~(ANS_PRODUCT_WEIGHTS_SETTLED | ANS_PRODUCT_WEIGHTS_ANYWHERE)) return ANS_ERR_UNSUPPORTED;
   if (d.activation < ANS_ACT_NONE || d.activation > ANS_ACT_SILU) return ANS_ERR_UNSUPPORTED;
   constexpr uint32_t kMost = 1u << 30;
   if (d.m > kMost || d.n > kMost || d.k > (1u << 22)) return ANS_ERR_UNSUPPORTED;
   if (d.m == 0 || d.n == 0) return ANS_OK;
   if (!d.d_y || (d.k && (!d.d_x || !d.d_w))) return ANS_ERR_INVALID_ARG;
   const uint64_t es = d.dtype == ANS_E4M3 ? 1 : 2, ys = d.y_dtype == ANS_F32 ? 4 : 2;
-  if ((reinterpret_cast<uintptr_t>(d.d_w) & 15) || (reinterpret_cast<uintptr_t>(d.d_x) & (es - 1))) return ANS_ERR_INVALID_ARG;
+  const bool anywhere = d.flags & ANS_PRODUCT_WEIGHTS_ANYWHERE;
+  if ((reinterpret_cast<uintptr_t>(d.d_w) & (anywhere ? es - 1 : 15)) || (reinterpret_cast<uintptr_t>(d.d_x) & (es - 1))) return ANS_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_residual)) & (ys - 1)) return ANS_ERR_INVALID_ARG;
   for (const float* p : {d.d_x_scales, d.d_w_scales, d.d_bias})
     if (reinterpret_cast<uintptr_t>(p) & 3) return ANS_ERR_INVALID_ARG;
   constexpr uint64_t kFar = uint64_t(1) << 36;
   if (d.k && d.m > 1 && (d.x_stride < d.k || d.x_stride > kFar)) return ANS_ERR_INVALID_ARG;
-  if (d.k && d.n > 1 && (d.w_stride < d.k || (d.w_stride * es) % 16 || d.w_stride > kFar)) return ANS_ERR_INVALID_ARG;
+  if (d.k && d.n > 1 && (d.w_stride < d.k || (!anywhere && (d.w_stride * es) % 16) || d.w_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && (d.y_stride < d.n || d.y_stride > kFar)) return ANS_ERR_INVALID_ARG;
   if (d.m > 1 && d.d_residual && (d.residual_stride < d.n || d.residual_stride > kFar)) return ANS_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (d.k && !rows_fit(d, es)) {
-    const uint64_t row = room_row(d.k, es);
-    if (!d.d_room || d.room_bytes < d.m * row) return ANS_ERR_BUFFER_TOO_SMALL;
+  const uint64_t for_w = d.k ? room_w(d, es) : 0, for_x = d.k ? room_x(d, es) : 0;
+  if (for_w + for_x) {
+    if (!d.d_room || d.room_bytes < for_w + for_x) return ANS_ERR_BUFFER_TOO_SMALL;
     if (reinterpret_cast<uintptr_t>(d.d_room) & 15) return ANS_ERR_INVALID_ARG;
-    const int rc = lay_out(d.d_x, d.x_stride, 1, d.m, d.k, es, d.d_room, st);
+    PrRows w{}, x{};
+    if (for_w) w = {d.d_w, d.w_stride, 1, static_cast<uint4*>(d.d_room), d.n, 0};
+    if (for_x) x = {d.d_x, d.x_stride, 1, reinterpret_cast<uint4*>(static_cast<char*>(d.d_room) + for_w), d.m, 0};
+    const int rc = for_w ? lay_out(w, x, d.k, es, st) : lay_out(x, w, d.k, es, st);
     if (rc != ANS_OK) return rc;
-    d.d_x = d.d_room;
-    d.x_stride = row / es;
+    const uint64_t stride = room_row(d.k, es) / es;
+    if (for_w) { d.d_w = w.to; d.w_stride = stride; d.flags &= ~ANS_PRODUCT_WEIGHTS_SETTLED; }      // written just ahead
+    if (for_x) { d.d_x = x.to; d.x_stride = stride; }
   }
   int sms = 0;
   const int rc = sm_count(&sms);

@@ -248,14 +248,18 @@ class Linear(_Handle):
                 self._taken.append(_vector(t.detach(), n, self.device))
                 setattr(d, field, self._taken[-1].data_ptr() or None)
         d.n, d.k, d.dtype, d.activation = n, k, _ELEMENT[weight.dtype], B.ACTIVATIONS[activation]
-        self._weight_off = n > 0 and k > 0 and not (_fits(weight) and weight.data_ptr() % 16 == 0)
+        off = n > 0 and k > 0 and not (_fits(weight) and weight.data_ptr() % 16 == 0)
+        strided = off and (k > 1 and weight.stride(1) != 1 or n > 1 and weight.stride(0) < k)
         if settled:
-            if self._weight_off:
+            if off:
                 with torch.cuda.device(self.device):
                     self._taken.append(self._lay_out(_current_stream(self._index)))
-                self._weight_off = False
             torch.cuda.synchronize(self.device)
             d.flags = B.ANS_PRODUCT_WEIGHTS_SETTLED
+        elif off and not strided:
+            d.flags = B.ANS_PRODUCT_WEIGHTS_ANYWHERE
+        # what each call does: lay the weight out by a call of its own; have the product lay it out
+        self._weight_strided, self._weight_off = strided and not settled, off and not strided and not settled
         self._hold(weight, scales, bias, *self._taken)
 
     def __call__(self, x: torch.Tensor, x_scales: torch.Tensor | None = None, residual: torch.Tensor | None = None,
@@ -278,9 +282,9 @@ class Linear(_Handle):
             taken = [(field, _vector(t, d.n, self.device)) for field, t in self._anew]     # kept until the call is queued
             for field, t in taken:
                 setattr(d, field, t.data_ptr())
-        if self._weight_off:
+        if self._weight_strided:
             laid = self._lay_out(st)                       # kept until the call is queued  # noqa: F841
-        if self._lies_off or at[0] % 16:
+        if self._weight_off or self._lies_off or at[0] % 16:
             room = torch.empty(B.ans_product_room_bytes(d), dtype=torch.uint8, device=self.device)
             d.d_room, d.room_bytes = room.data_ptr(), room.numel()
         B.ans_product(d, self._status, st)

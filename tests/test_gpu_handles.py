@@ -1,8 +1,10 @@
 """What a handle keeps between calls, and what it reads anew."""
+import numpy as np
 import pytest
 import torch
 
-from paper_2406_06237_b200.runtime import Linear
+import paper_2406_06237_b200 as ans
+from paper_2406_06237_b200.runtime import DeviceBatch, Linear, pack_layer
 
 pytestmark = pytest.mark.gpu
 BF16, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
@@ -45,6 +47,14 @@ def test_a_transposed_weight_is_read_again():
     for seed in range(2):
         base.copy_(integers((300, 77), 4, BF16, seed))
         assert torch.equal(f(x, out_dtype=F32), product(x, base.t()))
+
+
+def test_a_broadcast_weight():
+    """Strides of zero: one column for all, one row for all."""
+    x = integers((5, 300), 4, BF16, 1)
+    for w in (integers((77, 1), 4, BF16, 2).expand(77, 300), integers((1, 300), 4, BF16, 2).expand(77, 300)):
+        for settled in (False, True):
+            assert torch.equal(Linear(w, settled=settled)(x, out_dtype=F32), product(x, w))
 
 
 @pytest.mark.parametrize("k", [64, 67])
@@ -114,3 +124,39 @@ def test_tensors_that_require_a_gradient_are_taken_by_their_values(k):
     want = product(x, w) + bias.float()
     y = Linear(w.requires_grad_(), bias=bias.requires_grad_())(x.requires_grad_(), out_dtype=F32)
     assert torch.equal(y, want) and not y.requires_grad
+
+
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+@pytest.mark.parametrize("n,k,off,stride", PLACES)
+def test_rows_and_weight_off_16_bytes_together(n, k, off, stride, dtype):
+    """Both are laid out by one launch, X behind W; what lies between the rows is never used."""
+    stride = stride or k
+    w = torch.full((off + n * stride + 40,), float("nan"), device="cuda").to(dtype).as_strided((n, k), (stride, 1), off)
+    w.copy_(integers((n, k), 4, dtype, 1))
+    f = Linear(w)
+    for m in (1, 2, 33, 300):
+        for x_off, x_stride in ((0, k + (-k) % 16), (1, k + 3), (0, k)):
+            x = torch.full((x_off + m * x_stride,), float("nan"), device="cuda").to(dtype).as_strided((m, k), (x_stride, 1), x_off)
+            x.copy_(integers((m, k), 4, dtype, m))
+            assert torch.equal(f(x, out_dtype=F32), product(x, w))
+    assert f.read_status() == 0
+
+
+@pytest.mark.parametrize("n,k", [(130, 256), (130, 255), (64, 2047)])
+def test_a_weight_decoded_again_behind_its_handle(n, k):
+    """The handle is made before the weight is decoded; every decode into the buffer is multiplied by."""
+    symbols = [np.random.default_rng(seed).integers(0, 16, n * k).astype(np.uint8) for seed in range(3)]
+    batches = [DeviceBatch([pack_layer(s, 16, 8, 4096, 32, ans.ANS_LAYOUT_QUADS, 4, 8, 0.25, ans.ANS_BF16)]) for s in symbols]
+    weight = torch.zeros(n * k, device="cuda", dtype=BF16)
+    f, x = Linear(weight.view(n, k)), integers((40, k), 4, BF16, 1)
+    for s, b in zip(symbols, batches):
+        b.decode()
+        weight.copy_(b.output(0))
+        y = f(x, out_dtype=F32)
+        want = torch.from_numpy((s.astype(np.float32) - 8) * 0.25).cuda().view(n, k)
+        assert torch.equal(y, product(x, want)) and b.read_status() == 0
+    own = Linear(batches[0].output(0).view(n, k))           # and in the decoder's own buffer
+    batches[0].out_sets[0][0].zero_()
+    assert not own(x, out_dtype=F32).any()
+    batches[0].decode()
+    assert torch.equal(own(x, out_dtype=F32), product(x, torch.from_numpy((symbols[0].astype(np.float32) - 8) * 0.25).cuda().view(n, k)))

@@ -3,7 +3,7 @@ import pytest
 
 import paper_2406_06237_b200 as ans
 
-INVALID, UNSUPPORTED = ans.ANS_ERR_INVALID_ARG, ans.ANS_ERR_UNSUPPORTED
+INVALID, UNSUPPORTED, TOO_SMALL = ans.ANS_ERR_INVALID_ARG, ans.ANS_ERR_UNSUPPORTED, ans.ANS_ERR_BUFFER_TOO_SMALL
 P = 1 << 20                                              # an address on every boundary asked for; never read
 
 
@@ -15,6 +15,33 @@ P = 1 << 20                                              # an address on every b
 def test_product_rows(kw, rc):
     a = {**dict(d_from=P, stride=65, step=1, rows=4, k=65, dtype=ans.ANS_BF16, d_to=P), **kw}
     assert ans.lib().ans_product_rows(*(a[f] for f in ("d_from", "stride", "step", "rows", "k", "dtype", "d_to")), None) == rc
+
+
+ANYWHERE = ans.binding.ANS_PRODUCT_WEIGHTS_ANYWHERE
+
+
+@pytest.mark.parametrize("kw,rc", [
+    (dict(d_w=P + 2), TOO_SMALL), (dict(w_stride=65), TOO_SMALL), (dict(w_stride=65, d_room=P, room_bytes=32 * 128 - 1), TOO_SMALL),
+    (dict(w_stride=65, d_room=P + 8, room_bytes=1 << 20), INVALID), (dict(d_w=P + 1), INVALID), (dict(w_stride=63), INVALID),
+    (dict(d_w=P + 2, x_stride=65, d_room=P, room_bytes=36 * 128 - 1), TOO_SMALL), (dict(flags=ANYWHERE | 2), UNSUPPORTED),
+    (dict(d_w=P + 2, n=1 << 30, y_stride=1 << 30, k=1 << 22, x_stride=1 << 22, w_stride=1 << 22, d_room=P, room_bytes=1 << 62), UNSUPPORTED)])
+def test_weights_anywhere(kw, rc):
+    d = ans.binding.ans_product_desc(d_x=P, d_w=P, d_y=P, x_stride=64, w_stride=64, residual_stride=32, y_stride=32, m=4, n=32, k=64, dtype=ans.ANS_BF16,
+                                     y_dtype=ans.ANS_BF16, flags=ANYWHERE)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    assert ans.lib().ans_product(d, P, None) == rc
+
+
+def test_room_for_weights_anywhere():
+    def room(**kw):
+        d = ans.binding.ans_product_desc(d_x=P, d_w=P, x_stride=64, w_stride=64, m=4, n=32, k=64, dtype=ans.ANS_BF16, flags=ANYWHERE)
+        for k, v in kw.items():
+            setattr(d, k, v)
+        return ans.binding.ans_product_room_bytes(d)
+    assert room() == room(n=1, w_stride=65) == room(flags=0, d_w=P + 2) == 0
+    assert room(d_w=P + 2) == room(w_stride=65) == 32 * 128 and room(w_stride=65, x_stride=65) == 36 * 128 and room(x_stride=65) == 4 * 128
+    assert room(dtype=ans.ANS_E4M3, w_stride=65, k=33) == 32 * 48
 
 
 def test_product_form():
