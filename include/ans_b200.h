@@ -553,6 +553,119 @@ int ans_cache_read(const ans_cache_desc* h_desc, const int32_t* d_tables, uint64
                    uint32_t n_seqs, const int32_t* d_starts, uint64_t rows, void* d_k_out, void* d_v_out,
                    int out_dtype, uint32_t* d_status, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Many requests at once.  A batch is a row of n_seqs sequences (requests); sequence s has
+ * d_lengths[s] tokens, of which the last d_starts[s + 1] - d_starts[s] are new and have the rows
+ * d_starts[s] ... of the batch's matrices (queries, keys, ...).  Token i lies in page
+ * d_tables[s * table_stride + i / page_size] at i % page_size.  d_starts [n_seqs + 1] starts at 0 and
+ * does not decrease; rows from d_starts[n_seqs] on are padding: not read, not written.  All of these
+ * are int32 on the device and are not looked at by the host, so that a captured call serves batches of other lengths.
+ * n_seqs <= ANS_MAX_SEQS.  The calls below enqueue on `stream` and return without waiting, as those above.
+ * ------------------------------------------------------------------------------------ */
+#define ANS_MAX_SEQS 4096
+
+/*
+ * Block tables, slot maps and row ranges of a batch from its requests' lengths, in one kernel.
+ * Request s has d_cached[s] tokens in its pages and gets d_new[s] more.  The pages that it lacks are taken from
+ * d_free[*d_taken], d_free[*d_taken + 1], ..., request by request, and written into its row of d_tables behind those
+ * that it has; entries past them are left as they are.  Written besides:
+ *   d_starts[n_seqs + 1]  sums of d_new;      d_lengths[n_seqs]  d_cached + d_new (may be d_cached itself);
+ *   d_ends[n_seqs + 1]    sums of d_lengths (what ans_cache_read calls d_starts);
+ *   d_slots[rows]         each new token's slot, page * page_size + offset (for ans_cache_write); -1 behind the last one;
+ *   d_positions[rows]     each new token's position in its sequence; 0 behind the last one;
+ *   d_taken_out[1]        *d_taken plus the pages taken (may be d_taken itself).
+ * A batch that does not fit (free pages, table_pages, rows, a negative number, sums past 2^31 - 1) is flagged
+ * ANS_STATUS_BAD_PAGE and left as it was: no page is taken, d_starts is all 0 and d_slots all -1, d_lengths is d_cached.
+ * A page number outside 0 .. 2^31 / page_size among those that get tokens gives slots of -1 and the flag.
+ */
+typedef struct ans_pages_desc {
+  const int32_t* d_cached; const int32_t* d_new;                  /* [n_seqs] each                     */
+  const int32_t* d_free; const int32_t* d_taken;                  /* [n_free], [1]                     */
+  int32_t* d_tables; uint64_t table_stride; uint32_t table_pages;
+  uint32_t n_seqs, n_free, page_size, rows;
+  int32_t* d_starts; int32_t* d_lengths; int32_t* d_ends;
+  int64_t* d_slots; int32_t* d_positions; int32_t* d_taken_out;
+} ans_pages_desc;
+int ans_page_tables(const ans_pages_desc* h_desc, uint32_t* d_status, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a projection that they share:
+ *   out[t][:] = y[t][:] + scales[i] * x_scales[t] * (x[t][:] A_i^T) B_i^T,   i = d_which[s] of row t's request s,
+ * A_i = d_a[i] (rank x n_in), B_i = d_b[i] (n_out x rank), bf16, contiguous.  i < 0: no adapter, out = y; i >= count: the same, and
+ * flagged ANS_STATUS_BAD_PAGE.  Sums in fp32; x A^T meets B as a sum of two bf16 numbers (2^-17 of it); one rounding at the end.
+ * d_out may be d_y (same stride).  x: ANS_BF16, or ANS_E4M3 with d_x_scales (or NULL: ones).  rank <= 128.  Any alignment;
+ * the fast path wants d_x, d_a and their rows on 16 bytes.
+ */
+typedef struct ans_adapters_desc {
+  const void* d_x; const float* d_x_scales; const void* d_y; void* d_out;
+  const void* d_a; const void* d_b; const float* d_scales;        /* d_scales [count]; NULL: ones      */
+  const int32_t* d_which; const int32_t* d_starts;
+  uint64_t x_stride, y_stride, out_stride;
+  uint32_t rows, n_seqs, count, rank, n_in, n_out;
+  int32_t x_dtype, y_dtype;                                       /* y: ANS_BF16 or ANS_F32            */
+} ans_adapters_desc;
+int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status, void* stream);
+
+/*
+ * A paged cache of keys and values in 8 bits with one scale for each block (page) and head, made for the attention
+ * that reads it.  A value is code * scale, code in -127 .. 127.  Arrays, contiguous, 16-byte aligned:
+ *   codes  int8_t[n_pages][heads][page_size][head_dim],  scales float[n_pages][heads]  (keys and values each).
+ * page_size a multiple of 16 up to 256, head_dim a multiple of 16 up to 256.
+ */
+typedef struct ans_block_cache_desc {
+  int8_t* d_k_codes; float* d_k_scales;
+  int8_t* d_v_codes; float* d_v_scales;
+  uint32_t n_pages, page_size, heads, head_dim;
+} ans_block_cache_desc;
+typedef struct ans_batch_desc {
+  const int32_t* d_tables; uint64_t table_stride; uint32_t table_pages;
+  uint32_t n_seqs, rows;
+  const int32_t* d_lengths; const int32_t* d_starts;
+} ans_batch_desc;
+
+/*
+ * Write the batch's new keys and values (rows x heads x head_dim, dtype ANS_BF16 or ANS_F32, the values of a head
+ * contiguous, any alignment).  A block's scale is the least power of two, and at least 2^-40, that holds the largest
+ * magnitude written to it in 127 steps, so that every code is a function of the values alone:
+ *   code = rint(x / scale)  (to nearest even).
+ * A block begins anew when its first token is written.  Where tokens are added behind others and need a larger scale,
+ * the codes before them are rounded to it, code' = rint(code * old / new).  Codes of the block's other places stay.
+ * A NaN or an infinity makes its block's scale NaN (and the block's values of that head read as NaN) until it begins anew.
+ * No two sequences may get new tokens in the same page.  A page number outside the cache, a sequence longer than its
+ * table, or rows that do not fit are left out and flagged ANS_STATUS_BAD_PAGE.
+ */
+int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_desc* h_batch, const void* d_k, const void* d_v,
+                          int dtype, uint64_t k_token_stride, uint64_t k_head_stride, uint64_t v_token_stride,
+                          uint64_t v_head_stride, uint32_t* d_status, void* stream);
+
+/*
+ * Attention of the batch's new tokens over the cache (which holds them already):
+ *   out[t][j] = sum_i p_i v_i / sum_i p_i,   p_i = exp(scale * q[t][j] . k_i),   k, v of head j / (q_heads / heads),
+ * over the tokens i that row t sees: with `causal` those up to its own position, with `window` > 0 only the last `window`
+ * of these; without `causal` all of the sequence's tokens (the states of an encoder; window = 0).  A row that sees nothing is 0.
+ * q and out bf16, rows x q_heads x head_dim, the values of a head contiguous; d_q and its strides on 16 bytes, d_out on 4.
+ * d_out may be d_q (same strides).  Sums and the softmax's maximum and sum are in fp32; p meets the codes as an
+ * fp16 number scaled by a power of two (p_i times the scale of its block of values is off by 2^-11 of itself, or by 2^-39 of the largest such
+ * product of the row where that is more), q as fp16 scaled likewise, row by row (exact, but for values
+ * under 2^-14 of the row's largest, which are off by at most 2^-25 of it).
+ * Scales are taken as they are if they are at least 2^-40 (less counts as 2^-40).  Logits of about 1e38 and more are not supported.
+ * `longest`: the most new tokens of a sequence, if the caller knows it (0: no knowledge): choosing the kernels by it
+ * saves time, results do not depend on its being right.
+ * Pages outside the cache, or tokens past table_pages pages, count as not there and are flagged ANS_STATUS_BAD_PAGE.
+ * d_room: 16-byte aligned, ans_attend_room_bytes() bytes, free again when the call's work is done.
+ */
+typedef struct ans_attend_desc {
+  const void* d_q; void* d_out;
+  uint64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+  uint32_t q_heads;               /* a multiple of the cache's heads, up to 128 times them   */
+  uint32_t longest, window;
+  int32_t causal;
+  float scale;                    /* finite                                                  */
+  void* d_room; uint64_t room_bytes;
+} ans_attend_desc;
+int ans_attend(const ans_block_cache_desc* h_cache, const ans_batch_desc* h_batch, const ans_attend_desc* h_desc, uint32_t* d_status, void* stream);
+int ans_attend_room_bytes(const ans_block_cache_desc* h_cache, const ans_batch_desc* h_batch, const ans_attend_desc* h_desc, size_t* h_bytes_out);
+
 #ifdef __cplusplus
 }
 #endif

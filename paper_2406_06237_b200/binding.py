@@ -38,6 +38,7 @@ EXPORTS = [
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
     "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_product_rows", "ans_product_form", "ans_cache_write", "ans_cache_read",
+    "ans_page_tables", "ans_adapters", "ans_block_cache_write", "ans_attend", "ans_attend_room_bytes",
 ]
 
 
@@ -82,6 +83,50 @@ class ans_cache_desc(ctypes.Structure):
         ("d_v_codes", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p), ("d_v_zeros", ctypes.c_void_p),
         ("n_pages", ctypes.c_uint32), ("page_size", ctypes.c_uint32), ("heads", ctypes.c_uint32),
         ("head_dim", ctypes.c_uint32), ("group", ctypes.c_uint32), ("bitwidth", ctypes.c_int32),
+    ]
+
+
+class ans_pages_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_cached", ctypes.c_void_p), ("d_new", ctypes.c_void_p), ("d_free", ctypes.c_void_p), ("d_taken", ctypes.c_void_p),
+        ("d_tables", ctypes.c_void_p), ("table_stride", ctypes.c_uint64), ("table_pages", ctypes.c_uint32),
+        ("n_seqs", ctypes.c_uint32), ("n_free", ctypes.c_uint32), ("page_size", ctypes.c_uint32), ("rows", ctypes.c_uint32),
+        ("d_starts", ctypes.c_void_p), ("d_lengths", ctypes.c_void_p), ("d_ends", ctypes.c_void_p),
+        ("d_slots", ctypes.c_void_p), ("d_positions", ctypes.c_void_p), ("d_taken_out", ctypes.c_void_p),
+    ]
+
+
+class ans_adapters_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_x", ctypes.c_void_p), ("d_x_scales", ctypes.c_void_p), ("d_y", ctypes.c_void_p), ("d_out", ctypes.c_void_p),
+        ("d_a", ctypes.c_void_p), ("d_b", ctypes.c_void_p), ("d_scales", ctypes.c_void_p),
+        ("d_which", ctypes.c_void_p), ("d_starts", ctypes.c_void_p),
+        ("x_stride", ctypes.c_uint64), ("y_stride", ctypes.c_uint64), ("out_stride", ctypes.c_uint64),
+        ("rows", ctypes.c_uint32), ("n_seqs", ctypes.c_uint32), ("count", ctypes.c_uint32), ("rank", ctypes.c_uint32),
+        ("n_in", ctypes.c_uint32), ("n_out", ctypes.c_uint32), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
+    ]
+
+
+class ans_block_cache_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_k_codes", ctypes.c_void_p), ("d_k_scales", ctypes.c_void_p), ("d_v_codes", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p),
+        ("n_pages", ctypes.c_uint32), ("page_size", ctypes.c_uint32), ("heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32),
+    ]
+
+
+class ans_batch_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_tables", ctypes.c_void_p), ("table_stride", ctypes.c_uint64), ("table_pages", ctypes.c_uint32),
+        ("n_seqs", ctypes.c_uint32), ("rows", ctypes.c_uint32), ("d_lengths", ctypes.c_void_p), ("d_starts", ctypes.c_void_p),
+    ]
+
+
+class ans_attend_desc(ctypes.Structure):
+    _fields_ = [
+        ("d_q", ctypes.c_void_p), ("d_out", ctypes.c_void_p), ("q_token_stride", ctypes.c_uint64), ("q_head_stride", ctypes.c_uint64),
+        ("out_token_stride", ctypes.c_uint64), ("out_head_stride", ctypes.c_uint64), ("q_heads", ctypes.c_uint32),
+        ("longest", ctypes.c_uint32), ("window", ctypes.c_uint32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("d_room", ctypes.c_void_p), ("room_bytes", ctypes.c_uint64),
     ]
 
 
@@ -143,6 +188,11 @@ def lib():
         L.ans_product_rows.argtypes = [vp, u64, u64, u32, u32, i32, vp, vp]
         L.ans_cache_write.argtypes = [P(ans_cache_desc), vp, vp, i32, u64, u64, u64, u64, u64, vp, vp, vp]
         L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
+        L.ans_page_tables.argtypes = [P(ans_pages_desc), vp, vp]
+        L.ans_adapters.argtypes = [P(ans_adapters_desc), vp, vp]
+        L.ans_block_cache_write.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), vp, vp, i32, u64, u64, u64, u64, vp, vp]
+        L.ans_attend.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), P(ans_attend_desc), vp, vp]
+        L.ans_attend_room_bytes.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), P(ans_attend_desc), P(sz)]
         _LIB = L
     return _LIB
 
@@ -403,3 +453,35 @@ def ans_cache_read(h_desc: ans_cache_desc, d_tables: int, table_stride: int, tab
                                         out_dtype, d_status, stream)
     if rc:
         _check(rc, "ans_cache_read")
+
+
+def ans_page_tables(h_desc: ans_pages_desc, d_status: int, stream: int = 0) -> None:
+    rc = (_LIB or lib()).ans_page_tables(h_desc, d_status, stream)
+    if rc:
+        _check(rc, "ans_page_tables")
+
+
+def ans_adapters(h_desc: ans_adapters_desc, d_status: int, stream: int = 0) -> None:
+    rc = (_LIB or lib()).ans_adapters(h_desc, d_status, stream)
+    if rc:
+        _check(rc, "ans_adapters")
+
+
+def ans_block_cache_write(h_cache: ans_block_cache_desc, h_batch: ans_batch_desc, d_k: int, d_v: int, dtype: int, k_strides, v_strides,
+                          d_status: int, stream: int = 0) -> None:
+    """k_strides, v_strides: (token stride, head stride) in elements."""
+    rc = (_LIB or lib()).ans_block_cache_write(h_cache, h_batch, d_k, d_v, dtype, *k_strides, *v_strides, d_status, stream)
+    if rc:
+        _check(rc, "ans_block_cache_write")
+
+
+def ans_attend(h_cache: ans_block_cache_desc, h_batch: ans_batch_desc, h_desc: ans_attend_desc, d_status: int, stream: int = 0) -> None:
+    rc = (_LIB or lib()).ans_attend(h_cache, h_batch, h_desc, d_status, stream)
+    if rc:
+        _check(rc, "ans_attend")
+
+
+def ans_attend_room_bytes(h_cache: ans_block_cache_desc, h_batch: ans_batch_desc, h_desc: ans_attend_desc) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ans_attend_room_bytes(h_cache, h_batch, h_desc, ctypes.byref(out)), "ans_attend_room_bytes")
+    return out.value

@@ -1,0 +1,409 @@
+// Low-rank adapters of many requests beside a projection that they share:
+//   out[t] = y[t] + scales[i] * x_scales[t] * (x[t] A_i^T) B_i^T,   i the adapter of row t's request.
+//
+// A cluster of blocks has a tile of rows of one request.  Each block sums its part of the inputs, h = x A^T (rows x rank, mma.sync,
+// fp32), the blocks exchange their sums through distributed shared memory, added in the order of the ranks, and each goes on with
+// its part of the outputs: one launch, no workspace, A, B, x and y read once.  B's first rows are under way while A's are summed.
+// With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64 rows: bound by the bytes, so the plain
+// matrix instructions are enough.  h meets B as the sum of two bf16 numbers, h = hi + lo, |h - hi - lo| <= 2^-17 |h|: a second
+// product, which costs less than the rounding of h to 8 bits would lose.
+//
+// The order of the inputs in a product is free, so a lane takes 16 bytes of a row at once; the columns of a product with B stand
+// for outputs such that a lane has 8 neighbouring ones.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+#include <initializer_list>
+
+#include "ans_blocks.cuh"
+
+namespace ansb {
+namespace blk {
+
+struct AdArgs {
+  const uint8_t* x; const float* x_scales; const void* y; void* out;
+  const __nv_bfloat16* a; const __nv_bfloat16* b; const float* scales;
+  const int32_t* which; const int32_t* starts;
+  uint64_t x_stride, y_stride, out_stride;
+  uint32_t rows, n_seqs, count, rank, n_in, n_out;
+  uint32_t b_wide, y_wide;           // four elements of B, eight of y and out can be accessed at once
+  uint32_t* status;
+};
+
+constexpr uint32_t kAdWarps = 8, kAdThreads = 32 * kAdWarps;
+
+template <int R, int MT>
+struct AdShape {
+  static constexpr uint32_t kRows = 16 * MT;
+  static constexpr uint32_t kSums = kRows * R;                       // of h
+  static constexpr uint32_t kHRow = R + 8;                           // bf16 elements
+  static constexpr uint32_t kSmem = (kAdWarps + 1) * kSums * 4 + 2 * kRows * kHRow * 2;
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// two e4m3 values as bf16 (exact)
+__device__ __forceinline__ uint32_t open_e4m3(uint32_t two) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  return pack_bf16(f.x, f.y);
+}
+// 16 bytes of a row of bf16 or e4m3 elements from element e on; zeros from element n on.  VEC: the row starts on 16 bytes and n is a
+// multiple of 16 bytes.
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, bool live) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (!live) return v;
+  if constexpr (VEC) {
+    if (e < n) v = *reinterpret_cast<const uint4*>(row + e);
+  } else {
+    constexpr uint32_t kIn = 16 / sizeof(T);
+    uint32_t* const w = &v.x;
+#pragma unroll
+    for (uint32_t i = 0; i < kIn; ++i)
+      if (e + i < n) w[i / (kIn / 4)] |= static_cast<uint32_t>(row[e + i]) << (8 * sizeof(T) * (i % (kIn / 4)));
+  }
+  return v;
+}
+
+// R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each.
+template <int R, int MT, bool F8, bool YF32, bool VEC>
+__global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a) {
+  using S = AdShape<R, MT>;
+  using X = std::conditional_t<F8, uint8_t, uint16_t>;
+  using Y = std::conditional_t<YF32, float, __nv_bfloat16>;
+  constexpr uint32_t kUnit = F8 ? 64 : 32, kLane = kUnit / 4, kSteps = kUnit / 16;     // inputs of a unit, of a lane, products
+  constexpr int NT = R / 8, KT = R / 16;
+  constexpr int kAhead = MT * R <= 16 ? 4 : MT * R <= 64 ? 2 : 1;   // units whose loads are under way together
+  constexpr int kOuts = R == 16 ? 4 : R == 32 ? 2 : 1;               // groups of 32 outputs whose rows of B are loaded ahead
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* const parts = reinterpret_cast<float*>(smem);               // [warp][row][R]
+  float* const mine = parts + kAdWarps * S::kSums;                   // [row][R], this block's part of the inputs
+  __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(mine + S::kSums);
+  __nv_bfloat16* const low = high + S::kRows * S::kHRow;
+  __shared__ uint32_t s_seq;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
+  uint32_t ranks;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
+  const uint32_t rank = cluster_rank(), tile = blockIdx.x / ranks;
+  let_next_start();
+  wait_for_previous();
+  // tiles: request s has starts[s] / rows + s and on, at least as many as it needs
+  if (warp == 0) {
+    const uint32_t found = sequence_at(a.starts, a.n_seqs, S::kRows, 1u, tile);
+    if (lane == 0) s_seq = found;
+  }
+  __syncthreads();
+  const uint32_t s = s_seq;
+  const int32_t r0 = a.starts[s], r1 = a.starts[s + 1];
+  const bool fits = r0 >= 0 && r1 >= r0 && static_cast<uint32_t>(r1) <= a.rows;
+  if (!fits && rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+  const uint32_t place = static_cast<uint32_t>(max(r0, 0)) / S::kRows + s;
+  if (!fits || tile < place) return;                                 // the same for the whole cluster
+  const uint64_t begin = uint64_t(r0) + uint64_t(tile - place) * S::kRows;
+  if (begin >= static_cast<uint32_t>(r1)) return;
+  const uint32_t live = static_cast<uint32_t>(min(uint64_t(S::kRows), r1 - begin));
+  int32_t i = a.which[s];
+  if (i >= 0 && static_cast<uint32_t>(i) >= a.count) {
+    if (rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+    i = -1;
+  }
+  const bool none = i < 0;
+  if (none && a.out == a.y) return;
+
+  const uint32_t groups = (a.n_out + 31u) / 32u;
+  const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * rank / ranks), o1 = static_cast<uint32_t>(uint64_t(groups) * (rank + 1u) / ranks);
+  // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
+  // elements t R / 4 + 4 k and on of a row
+  auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) {
+      const uint32_t out = 32u * o + 8u * (g >> 1) + 2u * j + (g & 1u);
+      const __nv_bfloat16* const row = a.b + (uint64_t(max(i, 0)) * a.n_out + min(out, a.n_out - 1u)) * a.rank;
+#pragma unroll
+      for (uint32_t k = 0; k < KT; ++k) {
+        const uint32_t e = t * (R / 4) + 4u * k;
+        f[j][k][0] = f[j][k][1] = 0u;
+        if (none || o >= o1 || out >= a.n_out) continue;
+        if (a.b_wide) {
+          if (e < a.rank) {
+            const uint2 u = *reinterpret_cast<const uint2*>(row + e);
+            f[j][k][0] = u.x; f[j][k][1] = u.y;
+          }
+        } else {
+#pragma unroll
+          for (uint32_t h = 0; h < 4; ++h)
+            if (e + h < a.rank) f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[e + h]) << (16 * (h % 2));
+        }
+      }
+    }
+  };
+  uint32_t bf[kOuts][4][KT][2];
+#pragma unroll
+  for (int n = 0; n < kOuts; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
+
+  if (!none) {
+    float c[MT][NT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
+    const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
+    const uint32_t u0 = static_cast<uint32_t>(uint64_t(units) * rank / ranks), u1 = static_cast<uint32_t>(uint64_t(units) * (rank + 1u) / ranks);
+    const X* const x = reinterpret_cast<const X*>(a.x) + begin * a.x_stride;
+    const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + uint64_t(i) * a.rank * a.n_in;
+    for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
+      uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t now = u + kAdWarps * k, e = now * kUnit + t * kLane;
+        const bool in = now < u1;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (uint32_t h = 0; h < kLane / 8; ++h)
+            af[k][n][h] = piece_of<uint16_t, VEC>(down + uint64_t(min(8u * n + g, a.rank - 1u)) * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (uint32_t h = 0; h < 2; ++h) {
+            const uint32_t r = 16u * m + 8u * h + g;
+            xf[k][m][h] = piece_of<X, VEC>(x + min(r, live - 1u) * a.x_stride, e, a.n_in, in && r < live);
+          }
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (uint32_t j = 0; j < kSteps; ++j) {
+          uint32_t xw[MT][4];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t* const w = &xf[k][m][h].x;
+              if constexpr (F8) {
+                xw[m][h] = open_e4m3(w[j] & 0xFFFFu);
+                xw[m][h + 2] = open_e4m3(w[j] >> 16);
+              } else {
+                xw[m][h] = w[2 * j];
+                xw[m][h + 2] = w[2 * j + 1];
+              }
+            }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint32_t* const w = &af[k][n][j / 2].x;
+            const uint32_t b0 = w[2 * (j % 2)], b1 = w[2 * (j % 2) + 1];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma_bf16(c[m][n], xw[m][0], xw[m][1], xw[m][2], xw[m][3], b0, b1);
+          }
+        }
+    }
+    float* const to = parts + warp * S::kSums;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        *reinterpret_cast<float2*>(to + (16 * m + g) * R + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
+        *reinterpret_cast<float2*>(to + (16 * m + g + 8) * R + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
+      }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < S::kSums; e += kAdThreads) {
+      float sum = 0.f;
+#pragma unroll
+      for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kSums + e];
+      mine[e] = sum;
+    }
+    if (ranks > 1) cluster_sync(); else __syncthreads();
+    const float scale = a.scales ? a.scales[i] : 1.f;
+    const uint32_t from = smem_addr(mine);
+    for (uint32_t e = threadIdx.x; e < live * R; e += kAdThreads) {
+      float sum = 0.f;
+      for (uint32_t r = 0; r < ranks; ++r) {
+        float v;
+        asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
+                     : "=f"(v) : "r"(from + 4u * e), "r"(r) : "memory");
+        sum += v;
+      }
+      const uint32_t row = e / R, k = e % R;
+      sum *= a.x_scales ? a.x_scales[begin + row] * scale : scale;
+      const __nv_bfloat16 h = __float2bfloat16_rn(sum);
+      const float rest = sum - __bfloat162float(h);
+      high[row * S::kHRow + k] = h;
+      low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
+    }
+    for (uint32_t e = live * R + threadIdx.x; e < S::kSums; e += kAdThreads) {
+      high[(e / R) * S::kHRow + e % R] = __float2bfloat16_rn(0.f);
+      low[(e / R) * S::kHRow + e % R] = __float2bfloat16_rn(0.f);
+    }
+    __syncthreads();
+    if (ranks > 1) cluster_arrive();                                 // this block has read the others' sums
+  }
+
+  const Y* const y = static_cast<const Y*>(a.y) + begin * a.y_stride;
+  Y* const out = static_cast<Y*>(a.out) + begin * a.out_stride;
+  for (uint32_t o = o0 + warp; o < o1; o += kAdWarps * kOuts) {
+#pragma unroll
+    for (int n = 0; n < kOuts; ++n) {
+      const uint32_t now = o + kAdWarps * n;
+      if (now >= o1) break;
+      const uint32_t at = 32u * now + 8u * t;                        // the lane's outputs: at .. at + 7
+      const bool wide = a.y_wide && at + 8 <= a.n_out;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (16u * m >= live) break;
+        float v[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t r = 16u * m + 8u * h + g;
+          const Y* const p = y + uint64_t(r) * a.y_stride + at;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[h][k] = 0.f;
+          if (r >= live) continue;
+          if (wide) {
+            if constexpr (YF32) {
+              const float4 q = reinterpret_cast<const float4*>(p)[0], z = reinterpret_cast<const float4*>(p)[1];
+              v[h][0] = q.x; v[h][1] = q.y; v[h][2] = q.z; v[h][3] = q.w; v[h][4] = z.x; v[h][5] = z.y; v[h][6] = z.z; v[h][7] = z.w;
+            } else {
+              const uint4 q = *reinterpret_cast<const uint4*>(p);
+              const uint32_t* const w = &q.x;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                v[h][2 * k] = __uint_as_float(w[k] << 16);
+                v[h][2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (at + k < a.n_out) v[h][k] = static_cast<float>(p[k]);
+          }
+        }
+        if (!none) {
+          float d[4][4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+#pragma unroll
+          for (int k = 0; k < KT; ++k) {
+            const uint32_t e = t * (R / 4) + 4u * k, up = (16u * m + g) * S::kHRow + e, dn = up + 8u * S::kHRow;
+            const uint2 lu = *reinterpret_cast<const uint2*>(low + up), ld = *reinterpret_cast<const uint2*>(low + dn);
+            const uint2 hu = *reinterpret_cast<const uint2*>(high + up), hd = *reinterpret_cast<const uint2*>(high + dn);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              mma_bf16(d[j], lu.x, ld.x, lu.y, ld.y, bf[n][j][k][0], bf[n][j][k][1]);
+              mma_bf16(d[j], hu.x, hd.x, hu.y, hd.y, bf[n][j][k][0], bf[n][j][k][1]);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[0][2 * j] += d[j][0]; v[0][2 * j + 1] += d[j][1];
+            v[1][2 * j] += d[j][2]; v[1][2 * j + 1] += d[j][3];
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t r = 16u * m + 8u * h + g;
+          Y* const p = out + uint64_t(r) * a.out_stride + at;
+          if (r >= live) continue;
+          if (wide) {
+            if constexpr (YF32) {
+              reinterpret_cast<float4*>(p)[0] = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+              reinterpret_cast<float4*>(p)[1] = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
+            } else {
+              *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[h][0], v[h][1]), pack_bf16(v[h][2], v[h][3]), pack_bf16(v[h][4], v[h][5]),
+                                                        pack_bf16(v[h][6], v[h][7]));
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (at + k < a.n_out) {
+                if constexpr (YF32) p[k] = v[h][k]; else p[k] = __float2bfloat16_rn(v[h][k]);
+              }
+          }
+        }
+      }
+      load_b(now + kAdWarps * kOuts, bf[n]);
+    }
+  }
+  if (!none && ranks > 1) cluster_wait();                            // nobody reads this block's sums any more
+}
+
+template <int R, int MT, bool F8, bool YF32>
+static int launch_adapters(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
+  using S = AdShape<R, MT>;
+  const uint64_t tiles = a.rows / S::kRows + a.n_seqs;
+  if (tiles * ranks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
+  const dim3 grid(static_cast<unsigned>(tiles * ranks));
+  if (vec) {
+    constexpr auto kernel = ans_adapters_kernel<R, MT, F8, YF32, true>;
+    const int rc = allow_smem<kernel>(S::kSmem);
+    return rc == ANS_OK ? launch(kernel, grid, dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
+  }
+  constexpr auto kernel = ans_adapters_kernel<R, MT, F8, YF32, false>;
+  const int rc = allow_smem<kernel>(S::kSmem);
+  return rc == ANS_OK ? launch(kernel, grid, dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
+}
+
+// Tiles of 16 rows where requests have about as many, else as many as registers hold the sums of.
+template <int R, bool F8, bool YF32>
+static int launch_rank(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
+  constexpr int kMost = R <= 32 ? 4 : R == 64 ? 2 : 1;
+  return uint64_t(a.rows) <= 16ull * a.n_seqs ? launch_adapters<R, 1, F8, YF32>(a, vec, ranks, st) : launch_adapters<R, kMost, F8, YF32>(a, vec, ranks, st);
+}
+template <bool F8, bool YF32>
+static int launch_types(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
+  if (a.rank <= 16) return launch_rank<16, F8, YF32>(a, vec, ranks, st);
+  if (a.rank <= 32) return launch_rank<32, F8, YF32>(a, vec, ranks, st);
+  if (a.rank <= 64) return launch_rank<64, F8, YF32>(a, vec, ranks, st);
+  return launch_rank<128, F8, YF32>(a, vec, ranks, st);
+}
+
+}  // namespace blk
+}  // namespace ansb
+
+using namespace ansb;
+using namespace ansb::blk;
+
+ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status, void* stream) {
+  ApiRange range("ans_adapters");
+  if (!h_desc || !d_status) return ANS_ERR_INVALID_ARG;
+  const ans_adapters_desc& d = *h_desc;
+  if (d.x_dtype != ANS_BF16 && d.x_dtype != ANS_E4M3) return ANS_ERR_UNSUPPORTED;
+  if (d.y_dtype != ANS_BF16 && d.y_dtype != ANS_F32) return ANS_ERR_UNSUPPORTED;
+  if (d.rank == 0 || d.n_in == 0) return ANS_ERR_INVALID_ARG;
+  if (d.rank > 128 || d.n_seqs > ANS_MAX_SEQS || d.rows > 0x7FFFFFFFu || d.n_in > (1u << 22) || d.n_out > (1u << 30) || d.count > 0x7FFFFFFFu) return ANS_ERR_UNSUPPORTED;
+  if (d.rows == 0 || d.n_seqs == 0 || d.n_out == 0) return ANS_OK;
+  if (!d.d_x || !d.d_y || !d.d_out || !d.d_which || !d.d_starts || (d.count && (!d.d_a || !d.d_b))) return ANS_ERR_INVALID_ARG;
+  const uint64_t xs = d.x_dtype == ANS_E4M3 ? 1 : 2, ys = d.y_dtype == ANS_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(d.d_x) & (xs - 1) || (reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_out)) & (ys - 1) ||
+      (reinterpret_cast<uintptr_t>(d.d_a) | reinterpret_cast<uintptr_t>(d.d_b)) & 1)
+    return ANS_ERR_INVALID_ARG;
+  for (const void* p : {static_cast<const void*>(d.d_x_scales), static_cast<const void*>(d.d_scales), static_cast<const void*>(d.d_which),
+                        static_cast<const void*>(d.d_starts)})
+    if (reinterpret_cast<uintptr_t>(p) & 3) return ANS_ERR_INVALID_ARG;
+  constexpr uint64_t kFar = uint64_t(1) << 36;
+  if (d.rows > 1 && (d.x_stride < d.n_in || d.y_stride < d.n_out || d.out_stride < d.n_out)) return ANS_ERR_INVALID_ARG;
+  if (d.rows > 1 && d.d_y == d.d_out && d.y_stride != d.out_stride) return ANS_ERR_INVALID_ARG;
+  if (d.x_stride > kFar || d.y_stride > kFar || d.out_stride > kFar) return ANS_ERR_UNSUPPORTED;
+  AdArgs a{};
+  a.x = static_cast<const uint8_t*>(d.d_x); a.x_scales = d.d_x_scales; a.y = d.d_y; a.out = d.d_out;
+  a.a = static_cast<const __nv_bfloat16*>(d.d_a); a.b = static_cast<const __nv_bfloat16*>(d.d_b); a.scales = d.d_scales;
+  a.which = d.d_which; a.starts = d.d_starts;
+  a.x_stride = d.x_stride; a.y_stride = d.y_stride; a.out_stride = d.out_stride;
+  a.rows = d.rows; a.n_seqs = d.n_seqs; a.count = d.count; a.rank = d.rank; a.n_in = d.n_in; a.n_out = d.n_out;
+  a.status = d_status;
+  const uint64_t many = d.rows > 1;
+  const bool vec = !((reinterpret_cast<uintptr_t>(d.d_x) | (many * d.x_stride * xs) | reinterpret_cast<uintptr_t>(d.d_a) | (uint64_t(d.n_in) * 2) |
+                      (uint64_t(d.n_in) * xs)) & 15);
+  a.b_wide = d.rank % 4 == 0 && !(reinterpret_cast<uintptr_t>(d.d_b) & 7);
+  a.y_wide = !((reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_out) | (many * d.y_stride * ys) | (many * d.out_stride * ys)) & 15);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  constexpr uint32_t ranks = 8;
+  if (d.x_dtype == ANS_E4M3) return ys == 4 ? launch_types<true, true>(a, vec, ranks, st) : launch_types<true, false>(a, vec, ranks, st);
+  return ys == 4 ? launch_types<false, true>(a, vec, ranks, st) : launch_types<false, false>(a, vec, ranks, st);
+}

@@ -218,3 +218,4 @@ class DeviceBatch:
 
 
 from .operators import Linear, PagedCache, RmsNorm, symbols_to_e4m3  # noqa: E402,F401
+from .batches import Adapters, Batch, BlockCache, PageTables  # noqa: E402,F401

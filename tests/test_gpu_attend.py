@@ -1,0 +1,192 @@
+"""Attention over the block-scaled cache against its definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from batch_helpers import BF16, attention, fill_cache, ints, sums, tables_for
+from operator_helpers import rounds_from
+from paper_2406_06237_b200 import binding as B
+from paper_2406_06237_b200.runtime import BlockCache
+
+pytestmark = pytest.mark.gpu
+
+
+def queries(rows, heads, dim, seed=2, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (size * torch.randn(rows, heads, dim, device="cuda", generator=g)).to(BF16)
+
+
+def check(arrays, q, tables, lengths, starts, **kw):
+    cache = BlockCache.wrap(*arrays)
+    longest = kw.pop("longest", None)
+    out = torch.full_like(q, 7.0)
+    got = cache.attend(q, tables, ints(lengths), ints(starts), longest=longest, out=out, **kw)
+    assert got is out and cache.read_status() == 0
+    want, slack = attention(q, arrays, tables, lengths, starts, **kw)
+    n = starts[-1]
+    ok = rounds_from(out[:n], want[:n], slack[:n])
+    assert ok.all(), (int((~ok).sum()), ok.numel(), float(((out[:n].double() - want[:n]).abs() / slack[:n].clamp(min=1e-30)).max()))
+    assert (out[n:] == 7.0).all()
+    return out
+
+
+CASES = [                                                # heads, share, dim, page, cached, new
+    (8, 4, 128, 16, [100], [1]), (1, 1, 64, 16, [0], [1]), (2, 1, 128, 64, [700], [1]), (1, 8, 128, 64, [5000], [1]), (2, 7, 80, 48, [300, 15, 16, 0], [1, 1, 1, 1]),
+    (1, 16, 128, 16, [130, 127, 128], [1, 1, 1]), (2, 3, 256, 32, [400, 33], [1, 2]), (1, 5, 16, 16, [20], [3]), (4, 2, 112, 128, [1000, 0, 250], [1, 5, 0]),
+    (2, 4, 128, 16, [0, 200, 31], [70, 33, 17]), (1, 8, 64, 32, [90], [100]), (3, 1, 128, 64, [0], [300]), (2, 2, 256, 16, [10, 600], [150, 129]),
+    (1, 128, 128, 16, [60], [1]), (1, 40, 64, 16, [260], [2]), (2, 4, 96, 256, [2000] * 3, [1, 260, 3]), (8, 4, 128, 16, [int(700 / (i + 1)) for i in range(30)], [1] * 30),
+    (1, 4, 128, 64, [0], [1025]), (2, 8, 128, 64, [3000], [64]),
+]
+
+
+@pytest.mark.parametrize("heads,share,dim,page,cached,new", CASES)
+@pytest.mark.parametrize("how", [dict(), dict(window=1), dict(window=100), dict(causal=False)])
+def test_against_the_definition(heads, share, dim, page, cached, new, how):
+    lengths, starts = [b + m for b, m in zip(cached, new)], sums(new)
+    tables, n_pages = tables_for(lengths, page)
+    arrays = fill_cache(n_pages, heads, page, dim)
+    q = queries(starts[-1] + 2, heads * share, dim)
+    longest = max(new) if len(new) % 2 else None
+    check(arrays, q, tables, lengths, starts, longest=longest, **how)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_longest_that_is_wrong_changes_nothing(new):
+    tables, n_pages = tables_for([300 + new, 20 + new], 16)
+    arrays = fill_cache(n_pages, 2, 16, 64)
+    q = queries(2 * new, 8, 64)
+    for longest in (1, 3, 2 * new, 100000):
+        check(arrays, q, tables, [300 + new, 20 + new], [0, new, 2 * new], longest=longest)
+
+
+@pytest.mark.parametrize("new", [1, 50])
+def test_rows_that_see_nothing_are_zero(new):
+    arrays = fill_cache(9, 2, 16, 64)
+    tables = ints([[0, 1, 2, 3], [4, 5, 6, 7]])
+    out = check(arrays, queries(2 * new, 4, 64), tables, [0, 5], [0, new, 2 * new])          # fewer tokens than new ones
+    assert (out[:new] == 0).all() and (out[new:2 * new - 5] == 0).all()
+    out = check(arrays, queries(2 * new, 4, 64), tables, [0, 5], [0, new, 2 * new], causal=False)
+    assert (out[:new] == 0).all() and (out[new:] != 0).any()
+
+
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("low,high", [(-20, 20), (-40, -30), (60, 100)])
+def test_scales_of_very_different_blocks(new, low, high):
+    lengths = [700 + new]
+    tables, n_pages = tables_for(lengths, 16)
+    arrays = fill_cache(n_pages, 2, 16, 128)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    arrays[3].copy_(torch.exp2(torch.randint(low, high, arrays[3].shape, device="cuda", generator=g).float()))
+    check(arrays, queries(new, 4, 128), tables, lengths, [0, new])
+    arrays[3].mul_(1.37)                                 # and of no powers of two
+    check(arrays, queries(new, 4, 128), tables, lengths, [0, new])
+
+
+@pytest.mark.parametrize("new", [1, 90])
+def test_sharp_and_flat_rows(new):
+    lengths = [2000 + new]
+    tables, n_pages = tables_for(lengths, 64)
+    arrays = fill_cache(n_pages, 1, 64, 128)
+    for size, scale in ((30.0, None), (1e-3, None), (2.0 ** 100, 2.0 ** -103), (2.0 ** -110, 2.0 ** 109), (1.0, 0.0), (1.0, -0.1), (3.0, 2.0)):
+        q = queries(new, 4, 128, size=size)
+        q[:, 1] = 0
+        check(arrays, q, tables, lengths, [0, new], scale=scale)
+
+
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("which", [1, 3])
+def test_a_nan_block_is_seen_only_by_rows_that_see_it(new, which):
+    page, lengths = 16, [200 + new]
+    tables, n_pages = tables_for(lengths, page)
+    arrays = fill_cache(n_pages, 2, page, 64)
+    cache, q = BlockCache.wrap(*arrays), queries(new, 4, 64)
+    clean = cache.attend(q, tables, ints(lengths), ints([0, new]), window=20)
+    last = (200 + new - 1) // page                       # the last page: hidden from none but the rows before it
+    arrays[which][int(tables[0, 0]), :] = math.nan       # hidden by the window
+    arrays[which][int(tables[0, last]), 1] = math.nan
+    got = cache.attend(q, tables, ints(lengths), ints([0, new]), window=20)
+    sees = torch.arange(200, 200 + new, device="cuda") >= last * page
+    assert got[sees][:, 2:].isnan().all() and torch.equal(got[:, :2], clean[:, :2]) and torch.equal(got[~sees], clean[~sees])
+
+
+def test_strides_alignment_and_in_place():
+    lengths, starts = [70, 300], [0, 5, 40]
+    tables, n_pages = tables_for(lengths, 16)
+    arrays = fill_cache(n_pages, 2, 16, 64)
+    cache = BlockCache.wrap(*arrays)
+    packed = queries(40, 24, 64).unflatten(1, (3, 8))
+    want = check(arrays, packed[:, 1].contiguous(), tables, lengths, starts)
+    assert torch.equal(cache.attend(packed[:, 1], tables, ints(lengths), ints(starts)), want)
+    flat = torch.zeros(40 * 8 * 64 + 3, dtype=BF16, device="cuda")
+    off = flat[3:].view(40, 8, 64)
+    off.copy_(packed[:, 1])
+    assert torch.equal(cache.attend(off, tables, ints(lengths), ints(starts)), want)
+    wide = torch.zeros(40, 8, 66, dtype=BF16, device="cuda")[:, :, :64]
+    assert torch.equal(cache.attend(packed[:, 1], tables, ints(lengths), ints(starts), out=wide), want)
+    own = packed[:, 1].clone()
+    assert cache.attend(own, tables, ints(lengths), ints(starts), out=own) is own and torch.equal(own, want)
+    assert cache.read_status() == 0
+
+
+def test_results_do_not_vary_and_a_graph_serves_other_lengths():
+    page, n = 16, 12
+    tables, n_pages = tables_for([900] * n, page)
+    arrays = fill_cache(n_pages, 4, page, 128)
+    cache, q = BlockCache.wrap(*arrays), queries(n, 16, 128)
+    lengths, starts = ints([900 - 70 * i for i in range(n)]), ints(range(n + 1))
+    want = cache.attend(q, tables, lengths, starts, longest=1)
+    for _ in range(5):
+        assert torch.equal(cache.attend(q, tables, lengths, starts, longest=1), want)
+    out = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attend(q, tables, lengths, starts, longest=1, out=out)
+    graph.replay()
+    assert torch.equal(out, want)
+    lengths.copy_(ints([1 + 80 * i for i in range(n)]))
+    graph.replay()
+    assert torch.equal(out, cache.attend(q, tables, lengths, starts, longest=1))
+    want, slack = attention(q, arrays, tables, lengths.tolist(), list(range(n + 1)))
+    assert rounds_from(out, want, slack).all() and cache.read_status() == 0
+
+
+def test_pages_outside_the_cache_count_as_not_there():
+    arrays = fill_cache(6, 2, 16, 64)
+    cache, q = BlockCache.wrap(*arrays), queries(41, 4, 64)
+    for new in (1, 41):
+        good = cache.attend(q[:new], ints([[0, 1, 2, 3]]), ints([48]), ints([0, new]), causal=False)
+        assert cache.read_status() == 0
+        got = cache.attend(q[:new], ints([[0, 1, 2, 6]]), ints([64]), ints([0, new]), causal=False)
+        assert cache.read_status() == B.ANS_STATUS_BAD_PAGE and torch.equal(got, good)
+        got = cache.attend(q[:new], ints([[0, 1, 2]]), ints([64]), ints([0, new]), causal=False)
+        assert cache.read_status() == B.ANS_STATUS_BAD_PAGE and torch.equal(got, good)
+        got = cache.attend(q[:new], ints([[-1, -1, -1, 9]]), ints([64]), ints([0, new]), causal=False)
+        assert cache.read_status() == B.ANS_STATUS_BAD_PAGE and (got == 0).all()
+
+
+def test_nothing_to_do():
+    cache = BlockCache(4, 16, 2, 64)
+    q = queries(3, 4, 64)
+    out = torch.full_like(q, 3.0)
+    cache.attend(q, ints([[0]]), ints([5]), ints([0, 0]), out=out)
+    assert (out == 3).all()
+    assert cache.attend(q[:0], ints([[0]]), ints([5]), ints([0, 0])).shape == (0, 4, 64)
+    assert cache.attend(q, torch.zeros(0, 3, dtype=torch.int32, device="cuda"), ints([]), ints([0]), out=out) is out and (out == 3).all()
+    cache.write(q[:, :2], q[:, 2:], ints([[0]]), ints([5]), ints([0, 0]))
+    assert cache.read_status() == 0
+
+
+def test_another_stream():
+    tables, n_pages = tables_for([400, 90], 16)
+    arrays = fill_cache(n_pages, 2, 16, 128)
+    q = queries(2, 8, 128)
+    cache = BlockCache.wrap(*arrays)
+    want = cache.attend(q, tables, ints([400, 90]), ints([0, 1, 2]))
+    side = torch.cuda.Stream()
+    lengths, starts = ints([400, 90]), ints([0, 1, 2])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = cache.attend(q, tables, lengths, starts)
+    side.synchronize()
+    assert torch.equal(got, want)
