@@ -645,7 +645,7 @@ int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_d
  * of these; without `causal` all of the sequence's tokens (the states of an encoder; window = 0).  A row that sees nothing is 0.
  * q and out bf16, rows x q_heads x head_dim, the values of a head contiguous; d_q and its strides on 16 bytes, d_out on 4.
  * d_out may be d_q (same strides).  Sums and the softmax's maximum and sum are in fp32; p meets the codes as an
- * fp16 number scaled by a power of two (p_i times the scale of its block of values is off by 2^-11 of itself, or by 2^-39 of the largest such
+ * fp16 number scaled by a power of two (p_i times the scale of its block of values is off by 2^-11 of itself, or by 2^-32 of the largest such
  * product of the row where that is more), q as fp16 scaled likewise, row by row (exact, but for values
  * under 2^-14 of the row's largest, which are off by at most 2^-25 of it).
  * Scales are taken as they are if they are at least 2^-40 (less counts as 2^-40).  Logits of about 1e38 and more are not supported.

@@ -18,6 +18,7 @@
 #include <algorithm>
 
 #include "ans_attend.cuh"
+#include "ans_attend_tiles.cuh"
 
 namespace ansb {
 namespace blk {
@@ -73,8 +74,6 @@ template <int D> __device__ __forceinline__ uint32_t v_piece(uint32_t row, uint3
   return row * D + (D >= 128 ? c ^ (row & 7u) : c ^ ((row >> 1) & 3u)) * 16u;
 }
 
-constexpr uint32_t kArLongest = 1u << 30;              // tokens of a sequence
-
 // A sequence's units and chunks.
 struct ArSeq {
   uint32_t row, fresh;
@@ -87,7 +86,7 @@ __device__ __forceinline__ ArSeq ar_sequence(const AttendArgs& a, uint32_t s, bo
   ArSeq q;
   q.row = r.row;
   q.fresh = r.fresh;
-  const uint64_t held = min(uint64_t(a.b.table_pages) * a.c.page_size, uint64_t(kArLongest));
+  const uint64_t held = min(uint64_t(a.b.table_pages) * a.c.page_size, uint64_t(kAtLongest));
   bad |= !r.fits || (r.fresh && r.length > held);
   q.length = static_cast<int32_t>(min(uint64_t(max(static_cast<int32_t>(r.length), 0)), held));
   q.old = static_cast<int32_t>(r.length) - static_cast<int32_t>(r.fresh);
@@ -575,8 +574,15 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   return ANS_OK;
 }
 
-// What a call launches.
-struct AttendPlan { ArPlan rows; };
+// What a call launches: the kernel of this file for sequences of up to `border` rows (new tokens x share), the tiles for
+// the others; one of them alone where the caller's numbers say that no sequence needs the other.
+constexpr uint32_t kBorder = 32;
+struct AttendPlan {
+  bool with_rows, with_tiles;
+  ArPlan rows;
+  AtPlan tiles;
+  size_t room;
+};
 template <typename F>
 static int for_shape(uint32_t dim, uint32_t tiles, F&& f) {
   if (dim <= 64) return tiles == 1 ? f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{}) : f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
@@ -585,14 +591,20 @@ static int for_shape(uint32_t dim, uint32_t tiles, F&& f) {
 }
 static int plan_attend(const AttendArgs& a, uint32_t longest, AttendPlan& p) {
   int sms = 0;
-  const int rc = sm_count(&sms);
+  int rc = sm_count(&sms);
   if (rc != ANS_OK) return rc;
   if (longest == 0 || longest > a.b.rows) longest = a.b.rows;
   const uint64_t most = uint64_t(longest) * a.share;
-  return for_shape(a.c.dim, most <= 8 ? 1 : 2, [&](auto d, auto nt) {
-    plan_shape<d(), nt()>(a, longest, sms, p.rows);
-    return int(ANS_OK);
-  });
+  p.with_tiles = most > kBorder;
+  p.with_rows = !p.with_tiles || a.b.n_seqs > 1;
+  if (p.with_rows)                                     // beside the tiles, most others are single tokens
+    rc = for_shape(a.c.dim, (p.with_tiles ? a.share : most) <= 8 ? 1 : 2, [&](auto d, auto nt) {
+      plan_shape<d(), nt()>(a, p.with_tiles ? std::max(kBorder / a.share, 1u) : longest, sms, p.rows);
+      return int(ANS_OK);
+    });
+  if (p.with_tiles) plan_tiles(a, sms, p.tiles);
+  p.room = std::max(p.rows.room, p.tiles.room);        // the two kernels follow each other
+  return rc;
 }
 
 }  // namespace blk
@@ -611,7 +623,7 @@ ANS_EXPORT int ans_attend_room_bytes(const ans_block_cache_desc* h_cache, const 
   if (a.b.n_seqs == 0 || a.b.rows == 0) return ANS_OK;
   AttendPlan p{};
   rc = plan_attend(a, h_desc->longest, p);
-  if (rc == ANS_OK) *h_bytes_out = p.rows.room;
+  if (rc == ANS_OK) *h_bytes_out = p.room;
   return rc;
 }
 
@@ -626,13 +638,19 @@ ANS_EXPORT int ans_attend(const ans_block_cache_desc* h_cache, const ans_batch_d
   AttendPlan p{};
   rc = plan_attend(a, h_desc->longest, p);
   if (rc != ANS_OK) return rc;
-  if (p.rows.room) {
-    if (!h_desc->d_room || h_desc->room_bytes < p.rows.room) return ANS_ERR_BUFFER_TOO_SMALL;
+  if (p.room) {
+    if (!h_desc->d_room || h_desc->room_bytes < p.room) return ANS_ERR_BUFFER_TOO_SMALL;
     if (reinterpret_cast<uintptr_t>(h_desc->d_room) & 15) return ANS_ERR_INVALID_ARG;
     a.parts = static_cast<float*>(h_desc->d_room);
   }
-  a.least = 1;
-  a.most = 0xFFFFFFFFu;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (p.with_tiles) {
+    a.least = p.with_rows ? kBorder + 1 : 1;
+    a.most = 0xFFFFFFFFu;
+    rc = launch_tiles(a, p.tiles, st);
+    if (rc != ANS_OK || !p.with_rows) return rc;
+  }
+  a.least = 1;
+  a.most = p.with_tiles ? kBorder : 0xFFFFFFFFu;
   return for_shape(a.c.dim, p.rows.tiles, [&](auto d, auto nt) { return launch_rows<d(), nt()>(a, p.rows, st); });
 }

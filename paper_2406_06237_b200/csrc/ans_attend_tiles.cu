@@ -1,0 +1,550 @@
+// Attention over the block-scaled cache for many queries a head of the cache (prompts, chunks of prompts), on the
+// fifth-generation tensor cores.
+//
+// A block of threads has a tile of rows (new tokens x query heads of one head of the cache), one or two halves of 128, and goes over
+// the tokens that they see, BN at a time.  Its warps:
+//   4 converters:   codes from global memory, opened to fp16, into shared memory as operands (two stages of K and V);
+//   1 issuer:       S = Q K^T into tensor memory, then O += P V with P out of tensor memory;
+//   4 a half:       the softmax of a row a thread: S out of tensor memory, P over it as fp16, O rescaled there when the row's maximum
+//                   has grown by more than 2^kSlack since it was last.
+// While one half's softmax runs, the other half's products do: per BN = 128 tokens of D = 128 the two halves' four
+// products take 2048 clocks, their 32768 exponentials the same (16 a clock), the arithmetic around them 900 issue
+// slots of each of the four schedulers, and opening the codes 320.
+// V is the operand as it lies in the cache, tokens x dimensions ("MN-major"), so nothing is transposed.
+//
+// S of the next block goes over P of this one: the products of one issuer are done in order, and P's was issued before.  For the same
+// reason O may be rescaled by whoever has seen S of the next block.  Where there are fewer tiles than SMs, several blocks have parts
+// of a tile's tokens and a second kernel joins them.
+#include <algorithm>
+
+#include "ans_attend.cuh"
+#include "ans_attend_tiles.cuh"
+
+namespace ansb {
+namespace blk {
+
+constexpr float kUpTile = 7.f, kSlack = 8.f;           // P <= 2^15
+constexpr uint32_t kAtSoft = 8, kAtOpen = 4, kAtIssue = kAtSoft + kAtOpen;       // warps: softmax, converters, issuer and three idle
+constexpr uint32_t kAtThreads = 32 * (kAtSoft + kAtOpen + 4);
+
+template <int D>
+struct AtShape {
+  static constexpr uint32_t kHalves = D <= 128 ? 2 : 1;
+  static constexpr uint32_t kRows = 128 * kHalves;
+  static constexpr uint32_t kTokens = D <= 128 ? 128 : 64;             // of a block
+  static constexpr uint32_t kPanels = D / 64;                          // of 64 dimensions, 128 bytes
+  static constexpr uint32_t kQPanel = 128 * 128, kPanel = kTokens * 128;
+  static constexpr uint32_t kQ = kHalves * kPanels * kQPanel;
+  static constexpr uint32_t kTile = kPanels * kPanel;                  // K or V of a block
+  static constexpr uint32_t kStages = 2;
+  static constexpr uint32_t kSubs = kTokens / 16;                      // runs of 16 tokens, each in one page
+  static constexpr uint32_t kMeta = kStages * kSubs * 16;
+  static constexpr uint32_t kBars = 8 * (4 * kStages + 2 * kHalves + 2);
+  static constexpr uint32_t kSmem = 1024 + kQ + 2 * kStages * kTile + kMeta + kBars + 16;
+  static constexpr uint32_t kPieces = kTokens * (D / 16) / (32 * kAtOpen);       // of 16 codes, of a converter's thread, of K or of V
+  static constexpr uint32_t kDown = 32 * kAtOpen / (D / 16);           // tokens between a thread's pieces
+  static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory; halves 128 and D apart
+};
+
+__device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 184;"); }
+__device__ __forceinline__ void regs_open() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
+__device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 24;"); }
+static_assert(256 * 184 + 128 * 104 + 128 * 24 <= kAtThreads * 128, "what the launch brings");
+
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+               "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+               :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+                  "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+                  "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
+__device__ __forceinline__ uint64_t operand_across(uint32_t addr, uint32_t panel) {
+  return uint64_t((addr & 0x3FFFFu) >> 4) | (uint64_t(panel >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// fp16 operands, sums in fp32; B across: its N contiguous
+__host__ __device__ constexpr uint32_t instruction_half(uint32_t n, bool across) {
+  return (1u << 4) | (across ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// A tile: rows [r0, r0 + live) of a sequence's new tokens x share, and the blocks of tokens that they see.
+struct AtTile {
+  uint32_t row, fresh, r0, live;
+  int32_t old, length;
+  uint32_t b0, b1;                                     // blocks of kTokens
+};
+
+template <int D>
+__global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const AttendArgs a, const uint32_t splits) {
+  using S = AtShape<D>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base, k_at = q_at + S::kQ, v_at = k_at + S::kStages * S::kTile, meta = v_at + S::kStages * S::kTile;
+  const uint32_t bars = meta + S::kMeta;
+  const uint32_t k_full = bars, k_empty = k_full + 8 * S::kStages, v_full = k_empty + 8 * S::kStages, v_empty = v_full + 8 * S::kStages;
+  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 8 * S::kHalves, q_full = p_full + 8 * S::kHalves, o_full = q_full + 8;
+  const uint32_t slot = o_full + 8;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  uint32_t bad = 0;
+  __shared__ uint32_t s_seq;
+
+  if (threadIdx.x == 0) {
+    for (uint32_t s = 0; s < S::kStages; ++s) {
+      bar_init(k_full + 8 * s, kAtOpen); bar_init(k_empty + 8 * s, 1);
+      bar_init(v_full + 8 * s, kAtOpen); bar_init(v_empty + 8 * s, 1);
+    }
+    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 8 * h, 1); bar_init(p_full + 8 * h, 4); }
+    bar_init(q_full, 4 * S::kHalves);
+    bar_init(o_full, 1);
+    bar_init_fence();
+  }
+  if (warp == kAtIssue) tmem_alloc<1>(slot, 512);
+  let_next_start();
+  wait_for_previous();
+  // tiles: sequence s has starts[s] * share / rows + s and on; those that see most come first
+  const uint32_t x = gridDim.x - 1u - blockIdx.x, head = blockIdx.y;
+  if (warp == 0) {
+    uint32_t lo = 0, span = a.b.n_seqs;
+    while (span > 1) {
+      const uint32_t step = (span + 31u) / 32u, s = lo + lane * step, end = lo + span;
+      const bool before = s < end && static_cast<uint32_t>(max(a.b.starts[s], 0)) * uint64_t(a.share) / S::kRows + s <= x;
+      const uint32_t hits = __ballot_sync(kAll, before);
+      lo += (hits ? 31u - __clz(hits) : 0u) * step;
+      span = min(step, end - lo);
+    }
+    if (lane == 0) s_seq = lo;
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  uint32_t tmem;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+  const uint32_t s = s_seq;
+  AtTile T;
+  const Range r = range_of(a.b, s);
+  const uint32_t rows = r.fresh * a.share;
+  uint32_t blocks = 0;                                 // of this block of threads
+  uint32_t first = 0;
+  bool mine = false;
+  {
+    const uint32_t place = static_cast<uint32_t>(uint64_t(r.row) * a.share / S::kRows) + s;
+    const uint64_t held = min(uint64_t(a.b.table_pages) * a.c.page_size, uint64_t(kAtLongest));
+    T.row = r.row; T.fresh = r.fresh;
+    T.length = static_cast<int32_t>(min(uint64_t(max(static_cast<int32_t>(r.length), 0)), held));
+    T.old = static_cast<int32_t>(r.length) - static_cast<int32_t>(r.fresh);
+    const uint64_t r0 = uint64_t(x - place) * S::kRows;
+    mine = r.fits && x >= place && rows >= a.least && rows <= a.most && r0 < rows;
+    if (x == 0 && head == 0 && blockIdx.z == 0) {      // what does not fit is found by one block
+      bool wrong = false;
+      for (uint32_t i = threadIdx.x; i < a.b.n_seqs; i += kAtThreads) {
+        const Range o = range_of(a.b, i);
+        wrong |= !o.fits || (o.fresh && o.length > held);
+      }
+      if (wrong) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+    }
+    if (mine) {
+      T.r0 = static_cast<uint32_t>(r0);
+      T.live = min(S::kRows, rows - T.r0);
+      const Seen top = seen_by(a, T.old, T.length, T.r0 / a.share), end = seen_by(a, T.old, T.length, (T.r0 + T.live - 1u) / a.share);
+      T.b0 = static_cast<uint32_t>(top.first) / S::kTokens;
+      T.b1 = (static_cast<uint32_t>(end.end) + S::kTokens - 1) / S::kTokens;
+      if (T.b1 < T.b0) T.b1 = T.b0;
+      const uint32_t all = T.b1 - T.b0;
+      first = T.b0 + static_cast<uint32_t>(uint64_t(all) * blockIdx.z / splits);
+      blocks = T.b0 + static_cast<uint32_t>(uint64_t(all) * (blockIdx.z + 1u) / splits) - first;
+    }
+  }
+  const uint32_t halves = mine && T.live > 128u ? S::kHalves : 1u;
+  const int32_t* const table = a.b.tables + s * a.b.table_stride;
+
+  if (mine && warp < kAtSoft) {
+    // ---- softmax: a row a thread
+    regs_more();
+    const uint32_t half = warp >> 2, in = threadIdx.x & 127u, row = T.r0 + threadIdx.x;
+    if (half < halves) {
+      const bool live = threadIdx.x < T.live;
+      const uint32_t i = (live ? row : T.r0) / a.share, j = (live ? row : T.r0) - i * a.share;
+      float factor;
+      {
+        const __nv_bfloat16* const from = a.q + (T.row + i) * a.q_token + (head * a.share + j) * a.q_head;
+        uint32_t top = 0;
+#pragma unroll 4
+        for (uint32_t d = 0; d < D; d += 8) {
+          if (d >= a.c.dim || !live) break;
+          const uint4 w = *reinterpret_cast<const uint4*>(from + d);
+          const uint32_t* const e = &w.x;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top = max(top, max((e[k] << 16) & 0x7FFFFFFFu, e[k] & 0x7FFF0000u));
+        }
+        const int32_t up = exponent_of(top);
+        const float down = power_of(-up);
+        factor = a.scale2 * power_of(up);
+#pragma unroll 4
+        for (uint32_t d = 0; d < D; d += 8) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (d < a.c.dim && live) w = *reinterpret_cast<const uint4*>(from + d);
+          uint32_t* const e = &w.x;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) e[k] = pack_half(__uint_as_float(e[k] << 16) * down, __uint_as_float(e[k] & 0xFFFF0000u) * down);
+          const uint32_t to = q_at + (half * S::kPanels + d / 64u) * S::kQPanel + in * 128u + (((d / 8u) & 7u) ^ (in & 7u)) * 16u;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+        }
+      }
+      fence_operands();
+      __syncwarp();
+      if (lane == 0) arrive(q_full);
+      const Seen seen = seen_by(a, T.old, T.length, i);
+      const int32_t all_lo = __reduce_max_sync(kAll, seen.first), all_hi = __reduce_min_sync(kAll, seen.end);
+      const uint32_t lanes = (warp & 3u) << 21;        // this warp's 32 lanes of tensor memory
+      const uint32_t s_at = tmem + lanes + S::kS + half * 128u, o_at = tmem + lanes + S::kO + half * D;
+      float top = kLowest, sum = 0.f;
+      for (uint32_t n = 0; n < blocks; ++n) {
+        const uint32_t stage = n % S::kStages;
+        bar_wait(s_full + 8 * half, n & 1u, bad);
+        bar_wait(v_full + 8 * stage, (n / S::kStages) & 1u, bad);      // the scales
+        __syncwarp();
+        fence_after();
+        uint32_t v[S::kTokens];
+#pragma unroll
+        for (uint32_t c = 0; c < S::kTokens; c += 32) tmem_load(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+        tmem_wait();
+        const int32_t t0 = static_cast<int32_t>((first + n) * S::kTokens);
+        const uint32_t from = meta + stage * S::kSubs * 16u;
+        float best = kLowest;
+        const bool inside = t0 >= all_lo && t0 + static_cast<int32_t>(S::kTokens) <= all_hi;
+#pragma unroll
+        for (uint32_t b = 0; b < S::kSubs; ++b) {
+          float ks, e;
+          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(e) : "r"(from + 16u * b));
+          const float f = factor * ks;
+          const Two ff = two(f, f), ee = two(e, e);
+#pragma unroll
+          for (uint32_t c = 16 * b; c < 16 * b + 16; c += 2) {
+            const Two y = fma2(two(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), ff, ee);
+            v[c] = __float_as_uint(low(y));
+            v[c + 1] = __float_as_uint(high(y));
+          }
+        }
+        if (!inside) {
+          const int32_t lo = seen.first - t0, hi = seen.end - t0;
+#pragma unroll
+          for (int32_t c = 0; c < static_cast<int32_t>(S::kTokens); ++c)
+            if (c < lo || c >= hi) v[c] = 0xFF800000u;
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < S::kTokens; c += 2) best = largest3(best, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+        if (__any_sync(kAll, best > top + kSlack)) {
+          const float now = fmaxf(top, best), shrink = exp2_near(top - now);
+          top = now;
+          sum *= shrink;
+          if (n) {
+#pragma unroll 1
+            for (uint32_t c = 0; c < D; c += 32) {
+              uint32_t o[32];
+              tmem_load(o_at + c, o);
+              tmem_wait();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * shrink);
+              tmem_store(o_at + c, o);
+            }
+          }
+        }
+        const float less = kUpTile - top;
+        const Two ll = two(less, less);
+#pragma unroll
+        for (uint32_t b = 0; b < S::kSubs; ++b) {
+          float back;
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(back) : "r"(from + 16u * b + 8u));
+          Two part = 0;
+#pragma unroll
+          for (uint32_t c = 16 * b; c < 16 * b + 16; c += 2) {
+            const Two y = add2(two(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), ll);
+            const float p0 = exp2_near(low(y)), p1 = exp2_near(high(y));
+            part = add2(part, two(p0, p1));
+            v[c / 2] = pack_half(p0, p1);
+          }
+          sum = fmaf(low(part) + high(part), back, sum);
+        }
+#pragma unroll
+        for (uint32_t c = 0; c < S::kTokens / 2; c += 32) tmem_store(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+        tmem_stored();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(p_full + 8 * half);
+      }
+      bar_wait(o_full, 0u, bad);
+      __syncwarp();
+      fence_after();
+      const float f = sum == 0.f ? 0.f : exp2_near(-kUpTile) / sum;
+      __nv_bfloat16* const to = a.out + (T.row + i) * a.out_token + (head * a.share + j) * a.out_head;
+      const uint64_t part = (uint64_t(blockIdx.z) * a.b.rows + T.row + i) * (a.share * a.c.heads) + head * a.share + j;
+      float* const sums = a.parts + part * D;
+      if (splits > 1 && live) reinterpret_cast<float2*>(a.parts + uint64_t(splits) * a.b.rows * (a.share * a.c.heads) * D)[part] = make_float2(top, sum);
+#pragma unroll 1
+      for (uint32_t c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        tmem_load(o_at + c, o);
+        tmem_wait();
+        if (!blocks) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) o[k] = 0u;
+        }
+        if (!live) continue;
+        if (splits > 1) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4*>(sums + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; k += 2)
+            if (c + k < a.c.dim)
+              *reinterpret_cast<__nv_bfloat162*>(to + c + k) = __floats2bfloat162_rn(__uint_as_float(o[k]) * f, __uint_as_float(o[k + 1]) * f);
+        }
+      }
+    }
+  } else if (mine && warp < kAtIssue) {
+    // ---- converters
+    regs_open();
+    const uint32_t t = threadIdx.x - 32 * kAtSoft, row0 = t / (D / 16), c = t % (D / 16);
+    // piece c of a token: chunks 2 c and 2 c + 1 of 8 dimensions; those of the second four pieces the other way round, so
+    // that eight lanes write to different banks
+    const uint32_t odd = (c >> 2) & 1u, panel = c / 4u;
+    const uint32_t warp_row = (t & ~31u) / (D / 16);   // a warp's pieces lie in one run of 16 tokens
+    const uint32_t in = c * 16u < a.c.dim ? 1u : 0u;
+    uint64_t where = 0;                                // lane b: run b of 16 tokens
+    float ks = 0.f, e = 0.f, back = 0.f;
+    uint32_t used = 0;
+    auto look = [&](uint32_t block) {                  // the pages of a block's runs
+      const uint32_t token = block * S::kTokens + lane * 16u;
+      used = 0;
+      ks = 0.f; e = -INFINITY; back = 0.f;
+      if (lane < S::kSubs && block < first + blocks && token < static_cast<uint32_t>(T.length)) {
+        const uint32_t p_in = token / a.c.page_size;
+        const int32_t page = table[p_in];
+        if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {
+          const uint64_t at = uint64_t(page) * a.c.heads + head;
+          where = (at * a.c.page_size + (token - p_in * a.c.page_size)) * a.c.dim;
+          ks = usable(a.c.scales[0][at]);
+          e = log2_near(usable(a.c.scales[1][at]));
+          back = isnan(e) ? 1.f : exp2_near(-e - kUpTile);             // where e is NaN, so is what is summed
+          used = 1;
+        } else {
+          atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+        }
+      }
+    };
+    uint4 codes[2][S::kPieces];
+    auto load = [&](uint32_t which) {
+#pragma unroll
+      for (uint32_t i = 0; i < S::kPieces; ++i) {
+        const uint32_t sub = (warp_row + i * S::kDown) / 16u;
+        const uint64_t p = __shfl_sync(kAll, where, sub);
+        const uint32_t u = __shfl_sync(kAll, used, sub);
+        codes[which][i] = make_uint4(0, 0, 0, 0);
+        const uint32_t row = row0 + i * S::kDown;
+        if (u && in) codes[which][i] = *reinterpret_cast<const uint4*>(a.c.codes[which] + p + (row % 16u) * a.c.dim + c * 16u);
+      }
+    };
+    auto open = [&](uint32_t which, uint32_t to) {
+#pragma unroll
+      for (uint32_t i = 0; i < S::kPieces; ++i) {
+        const uint32_t row = row0 + i * S::kDown;
+        const uint32_t* const w = &codes[which][i].x;
+        uint32_t h[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t u = w[k] ^ 0x80808080u;
+          h[2 * k] = open_low(u);
+          h[2 * k + 1] = open_high(u);
+        }
+        const uint32_t line = to + panel * S::kPanel + row * 128u, chunk = (2u * c) & 7u;
+        const uint32_t at0 = line + ((chunk + odd) ^ (row & 7u)) * 16u, at1 = line + ((chunk + 1u - odd) ^ (row & 7u)) * 16u;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at0), "r"(odd ? h[4] : h[0]), "r"(odd ? h[5] : h[1]),
+                     "r"(odd ? h[6] : h[2]), "r"(odd ? h[7] : h[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at1), "r"(odd ? h[0] : h[4]), "r"(odd ? h[1] : h[5]),
+                     "r"(odd ? h[2] : h[6]), "r"(odd ? h[3] : h[7]) : "memory");
+      }
+    };
+    look(first);
+    load(0);
+    load(1);
+    for (uint32_t n = 0; n < blocks; ++n) {
+      const uint32_t stage = n % S::kStages, round = n / S::kStages;
+      const float now_ks = ks, now_e = e, now_back = back;             // of this block's runs
+      look(first + n + 1);
+      if (round) bar_wait(k_empty + 8 * stage, (round - 1u) & 1u, bad);
+      open(0, k_at + stage * S::kTile);
+      fence_operands();
+      __syncwarp();
+      if (lane == 0) arrive(k_full + 8 * stage);
+      load(0);
+      if (round) bar_wait(v_empty + 8 * stage, (round - 1u) & 1u, bad);
+      open(1, v_at + stage * S::kTile);
+      if (warp == kAtSoft && lane < S::kSubs)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(meta + (stage * S::kSubs + lane) * 16u), "f"(now_ks), "f"(now_e), "f"(now_back), "f"(0.f) : "memory");
+      fence_operands();
+      __syncwarp();
+      if (lane == 0) arrive(v_full + 8 * stage);
+      load(1);
+    }
+  } else if (mine) {
+    regs_few();
+    if (warp == kAtIssue && lane == 0) {
+      // ---- issuer
+      constexpr uint32_t is = instruction_half(S::kTokens, false), io = instruction_half(D, true);
+      auto scores = [&](uint32_t h, uint32_t stage) {
+#pragma unroll
+        for (uint32_t p = 0; p < S::kPanels; ++p) {
+          const uint64_t dq = operand(q_at + (h * S::kPanels + p) * S::kQPanel), dk = operand(k_at + stage * S::kTile + p * S::kPanel);
+#pragma unroll
+          for (uint32_t k = 0; k < 4; ++k) mma_smem(tmem + S::kS + h * 128u, dq + 2u * k, dk + 2u * k, is, p || k);
+        }
+        mma_commit<1>(s_full + 8 * h);
+      };
+      auto outputs = [&](uint32_t h, uint32_t stage, bool more) {
+        const uint64_t dv = operand_across(v_at + stage * S::kTile, S::kPanel);
+#pragma unroll
+        for (uint32_t k = 0; k < S::kTokens / 16; ++k)
+          mma_tmem(tmem + S::kO + h * D, tmem + S::kS + h * 128u + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || k);
+      };
+      for (uint32_t h = 0; h < S::kHalves; ++h)
+        if (h >= halves) for (uint32_t i = 0; i < 4; ++i) arrive(q_full);            // a half without rows
+      bar_wait(q_full, 0u, bad);
+      for (uint32_t n = 0; n < blocks; ++n) {
+        const uint32_t stage = n % S::kStages, parity = (n / S::kStages) & 1u;
+        if (n == 0) {
+          bar_wait(k_full, 0u, bad);
+          fence_after();
+          for (uint32_t h = 0; h < halves; ++h) scores(h, 0);
+          mma_commit<1>(k_empty);
+        }
+        bar_wait(v_full + 8 * stage, parity, bad);
+        const uint32_t next = (n + 1) % S::kStages;
+        for (uint32_t h = 0; h < halves; ++h) {
+          bar_wait(p_full + 8 * h, n & 1u, bad);
+          fence_after();
+          outputs(h, stage, n > 0);
+          if (h + 1 == halves) mma_commit<1>(v_empty + 8 * stage);
+          if (n + 1 < blocks) {
+            if (h == 0) bar_wait(k_full + 8 * next, ((n + 1) / S::kStages) & 1u, bad);
+            fence_after();
+            scores(h, next);
+            if (h + 1 == halves) mma_commit<1>(k_empty + 8 * next);
+          }
+        }
+      }
+      mma_commit<1>(o_full);
+      bar_wait(o_full, 0u, bad);                       // nothing is under way any more
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kAtIssue) {
+    fence_after();
+    tmem_free<1>(tmem, 512);
+  }
+  bad = __any_sync(kAll, bad);
+  if (lane == 0 && bad) atomicOr(a.status, ANS_STATUS_COPY_TIMEOUT);
+}
+
+// Joins the parts of every row of the sequences that the tiles kernel had: a warp a row and head.
+template <int D>
+__global__ void __launch_bounds__(256) ans_attend_tiles_join_kernel(const AttendArgs a, const uint32_t splits) {
+  let_next_start();
+  wait_for_previous();
+  const uint32_t lane = threadIdx.x & 31u, heads = a.share * a.c.heads;
+  const uint64_t at = uint64_t(blockIdx.x) * 8u + (threadIdx.x >> 5);
+  if (at >= uint64_t(a.b.rows) * heads) return;
+  const uint32_t row = static_cast<uint32_t>(at / heads), head = static_cast<uint32_t>(at - uint64_t(row) * heads);
+  uint32_t lo = 0, hi = a.b.n_seqs;                    // the last sequence that does not start behind the row
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (a.b.starts[mid] <= static_cast<int32_t>(row)) lo = mid; else hi = mid;
+  }
+  const Range r = range_of(a.b, lo);
+  const uint64_t rows = uint64_t(r.fresh) * a.share;
+  if (!r.fits || row < r.row || row - r.row >= r.fresh || rows < a.least || rows > a.most) return;
+  const uint64_t all = uint64_t(a.b.rows) * heads;
+  const float2* const ml = reinterpret_cast<const float2*>(a.parts + splits * all * D);
+  float most = kLowest, sum = 0.f;
+  for (uint32_t z = 0; z < splits; ++z) most = fmaxf(most, ml[z * all + at].x);
+  float x[D / 32];
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
+#pragma unroll 2
+  for (uint32_t z = 0; z < splits; ++z) {
+    const float2 m = ml[z * all + at];
+    const float f = exp2_near(m.x - most);
+    sum = fmaf(f, m.y, sum);
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) {
+      const float2 v = *reinterpret_cast<const float2*>(a.parts + (z * all + at) * D + 64 * k + 2 * lane);
+      x[2 * k] = fmaf(f, v.x, x[2 * k]);
+      x[2 * k + 1] = fmaf(f, v.y, x[2 * k + 1]);
+    }
+  }
+  const float f = sum == 0.f ? 0.f : exp2_near(-kUpTile) / sum;
+  __nv_bfloat16* const to = a.out + row * a.out_token + head * a.out_head;
+#pragma unroll
+  for (int k = 0; k < D / 64; ++k) {
+    const uint32_t d = 64u * k + 2u * lane;
+    if (d < a.c.dim) *reinterpret_cast<__nv_bfloat162*>(to + d) = __floats2bfloat162_rn(x[2 * k] * f, x[2 * k + 1] * f);
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------
+template <int D>
+static void plan_tiles_shape(const AttendArgs& a, int sms, AtPlan& p) {
+  using S = AtShape<D>;
+  const uint64_t rows = uint64_t(a.b.rows) * a.share;
+  p.tiles = static_cast<uint32_t>(rows / S::kRows + a.b.n_seqs);
+  // parts: as many as there are SMs for, of 512 tokens at least
+  const uint64_t units = std::max<uint64_t>((rows + S::kRows - 1) / S::kRows * a.c.heads, 1);
+  const uint64_t most = uint64_t(a.b.table_pages) * a.c.page_size / 512;
+  p.splits = static_cast<uint32_t>(std::max<uint64_t>(std::min<uint64_t>({uint64_t(sms) / units, most, 16}), 1));
+  p.room = p.splits > 1 ? size_t(p.splits) * a.b.rows * a.share * a.c.heads * (D + 2) * sizeof(float) : 0;
+}
+void plan_tiles(const AttendArgs& a, int sms, AtPlan& p) {
+  if (a.c.dim <= 64) plan_tiles_shape<64>(a, sms, p);
+  else if (a.c.dim <= 128) plan_tiles_shape<128>(a, sms, p);
+  else plan_tiles_shape<256>(a, sms, p);
+}
+
+template <int D>
+static int launch_tiles_shape(const AttendArgs& a, const AtPlan& p, cudaStream_t st) {
+  using S = AtShape<D>;
+  constexpr auto kernel = ans_attend_tiles_kernel<D>;
+  static_assert(S::kSmem <= 227 * 1024, "");
+  int rc = allow_smem<kernel>(S::kSmem);
+  if (rc == ANS_OK) rc = launch(kernel, dim3(p.tiles, a.c.heads, p.splits), dim3(kAtThreads), S::kSmem, st, 1, a, p.splits);
+  if (rc == ANS_OK && p.splits > 1) {
+    const uint64_t blocks = (uint64_t(a.b.rows) * a.share * a.c.heads + 7) / 8;
+    rc = launch(ans_attend_tiles_join_kernel<D>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, 1, a, p.splits);
+  }
+  return rc;
+}
+int launch_tiles(const AttendArgs& a, const AtPlan& p, cudaStream_t st) {
+  if (a.c.dim <= 64) return launch_tiles_shape<64>(a, p, st);
+  if (a.c.dim <= 128) return launch_tiles_shape<128>(a, p, st);
+  return launch_tiles_shape<256>(a, p, st);
+}
+
+}  // namespace blk
+}  // namespace ansb

@@ -54,9 +54,9 @@ def attention(q, arrays, tables, lengths, starts, scale=None, causal=True, windo
     a sum of up to 256 products in groups of 16 whose additions may each be off by 2^-22 of the sum of magnitudes B (17 of them),
     three roundings of factors follow and an exponential within 2^-22: under 2^-17 (1 + B) in all, which moves p_i and the sum
     of p by that share each.
-    fp16 ends at steps of 2^-24: what is rounded is P_i = 2^14 p_i c_i / T, c_i the scale of v_i's block and T the largest p_j c_j, so that a
-    P_i under 2^-14 is off by up to 2^-25, half a step, and p_i v_i = P_i code_i T / 2^14 by 2^-25 * 127 * T / 2^14: 127 * 2^-39 T a token,
-    which counts where the tokens with large p_i have a v_i of 0."""
+    fp16 ends at steps of 2^-24: what is rounded is P_i = 2^u p_i c_i / T, u = 7 at least, c_i the scale of v_i's block and T the largest
+    p_j c_j, so that a P_i under 2^-14 is off by up to 2^-25, half a step, and p_i v_i = P_i code_i T / 2^u by 2^-25 * 127 * T / 2^7:
+    127 * 2^-32 T a token, which counts where the tokens with large p_i have a v_i of 0."""
     kc, ks, vc, vs = arrays
     heads, dim = kc.shape[1], kc.shape[3]
     share = q.shape[1] // heads
@@ -88,7 +88,7 @@ def attention(q, arrays, tables, lengths, starts, scale=None, causal=True, windo
         off = torch.einsum("hgts,hsd->thgd", p, v0.abs()) * (2.0 ** -11 + 2 * 2.0 ** -17 * (1 + big.permute(2, 0, 1)[..., None]))
         held = torch.nan_to_num(vs[tables[s][:-(-length // vc.shape[2])].long()].to(F64)).T.repeat_interleave(vc.shape[2], 1)[:, :length]
         top = (p * held[:, None, None, :]).amax(3).permute(2, 0, 1)[..., None]           # T
-        off = off + seen.sum(1)[:, None, None, None] * 127 * 2.0 ** -39 * top
+        off = off + seen.sum(1)[:, None, None, None] * 127 * 2.0 ** -32 * top
         out[r0:r1], slack[r0:r1] = at.flatten(1, 2), off.flatten(1, 2)
     return out, slack
 
