@@ -4,6 +4,7 @@
 // A block of threads has a tile of rows (new tokens x query heads of one head of the cache), one or two halves of 128, and goes over
 // the tokens that they see, BN at a time.  Its warps:
 //   4 converters:   codes from global memory, opened to fp16, into shared memory as operands (two stages of K and V);
+//   1 for scales:   of the runs of 16 tokens, as the softmax uses them;
 //   1 issuer:       S = Q K^T into tensor memory, then O += P V with P out of tensor memory;
 //   4 a half:       the softmax of a row a thread: S out of tensor memory, P over it as fp16, O rescaled there when the row's maximum
 //                   has grown by more than 2^kSlack since it was last.
@@ -24,8 +25,9 @@ namespace ansb {
 namespace blk {
 
 constexpr float kUpTile = 7.f, kSlack = 8.f;           // P <= 2^15
-constexpr uint32_t kAtSoft = 8, kAtOpen = 4, kAtIssue = kAtSoft + kAtOpen;       // warps: softmax, converters, issuer and three idle
-constexpr uint32_t kAtThreads = 32 * (kAtSoft + kAtOpen + 4);
+constexpr float kLeastFactor = 1e-38f;                 // of S, so that -inf times it is -inf
+constexpr uint32_t kAtSoft = 8, kAtOpen = 4, kAtIssue = kAtSoft + kAtOpen, kAtScales = kAtIssue + 1;   // warps: softmax, converters, issuer, scales
+constexpr uint32_t kAtThreads = 32 * (kAtScales + 1);
 
 template <int D>
 struct AtShape {
@@ -41,15 +43,11 @@ struct AtShape {
   static constexpr uint32_t kMeta = kStages * kSubs * 16;
   static constexpr uint32_t kBars = 8 * (4 * kStages + 2 * kHalves + 2);
   static constexpr uint32_t kSmem = 1024 + kQ + 2 * kStages * kTile + kMeta + kBars + 16;
-  static constexpr uint32_t kPieces = kTokens * (D / 16) / (32 * kAtOpen);       // of 16 codes, of a converter's thread, of K or of V
-  static constexpr uint32_t kDown = 32 * kAtOpen / (D / 16);           // tokens between a thread's pieces
+  static constexpr uint32_t kOwn = kTokens / kAtOpen, kRuns = kOwn / 16;         // tokens and runs of a converter's warp
+  static constexpr uint32_t kDown = 32 / (D / 16);                     // tokens between a thread's pieces of 16 codes
+  static constexpr uint32_t kPieces = kOwn / kDown;
   static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory; halves 128 and D apart
 };
-
-__device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 184;"); }
-__device__ __forceinline__ void regs_open() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
-__device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 24;"); }
-static_assert(256 * 184 + 128 * 104 + 128 * 24 <= kAtThreads * 128, "what the launch brings");
 
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -60,6 +58,11 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
@@ -82,6 +85,14 @@ __device__ __forceinline__ float largest3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+
+// columns outside [lo, hi) as tokens that are not seen
+template <uint32_t N>
+__device__ __forceinline__ void hide(uint32_t (&v)[N], int32_t lo, int32_t hi) {
+#pragma unroll
+  for (int32_t c = 0; c < static_cast<int32_t>(N); ++c)
+    if (c < lo || c >= hi) v[c] = 0xFF800000u;
 }
 
 // A tile: rows [r0, r0 + live) of a sequence's new tokens x share, and the blocks of tokens that they see.
@@ -108,7 +119,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < S::kStages; ++s) {
       bar_init(k_full + 8 * s, kAtOpen); bar_init(k_empty + 8 * s, 1);
-      bar_init(v_full + 8 * s, kAtOpen); bar_init(v_empty + 8 * s, 1);
+      bar_init(v_full + 8 * s, kAtOpen + 1); bar_init(v_empty + 8 * s, 1);
     }
     for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 8 * h, 1); bar_init(p_full + 8 * h, 4); }
     bar_init(q_full, 4 * S::kHalves);
@@ -177,7 +188,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
 
   if (mine && warp < kAtSoft) {
     // ---- softmax: a row a thread
-    regs_more();
     const uint32_t half = warp >> 2, in = threadIdx.x & 127u, row = T.r0 + threadIdx.x;
     if (half < halves) {
       const bool live = threadIdx.x < T.live;
@@ -195,8 +205,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           for (int k = 0; k < 4; ++k) top = max(top, max((e[k] << 16) & 0x7FFFFFFFu, e[k] & 0x7FFF0000u));
         }
         const int32_t up = exponent_of(top);
-        const float down = power_of(-up);
-        factor = a.scale2 * power_of(up);
+        const float down = a.scale2 < 0.f ? -power_of(-up) : power_of(-up);
+        factor = fabsf(a.scale2) * power_of(up);       // the scale's sign goes to the queries
 #pragma unroll 4
         for (uint32_t d = 0; d < D; d += 8) {
           uint4 w = make_uint4(0, 0, 0, 0);
@@ -222,35 +232,34 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
         bar_wait(v_full + 8 * stage, (n / S::kStages) & 1u, bad);      // the scales
         __syncwarp();
         fence_after();
-        uint32_t v[S::kTokens];
-#pragma unroll
-        for (uint32_t c = 0; c < S::kTokens; c += 32) tmem_load(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
-        tmem_wait();
-        const int32_t t0 = static_cast<int32_t>((first + n) * S::kTokens);
+        const int32_t t0 = static_cast<int32_t>((first + n) * S::kTokens), lo = seen.first - t0, hi = seen.end - t0;
         const uint32_t from = meta + stage * S::kSubs * 16u;
-        float best = kLowest;
         const bool inside = t0 >= all_lo && t0 + static_cast<int32_t>(S::kTokens) <= all_hi;
+        // the runs of 16 tokens: s_i + e_i = S_i f + e
+        auto run = [&](uint32_t b, float& f, float& e, float& back) {
+          float rest;
+          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f), "=f"(e), "=f"(back), "=f"(rest) : "r"(from + 16u * b));
+          f = fmaxf(factor * f, kLeastFactor);
+        };
+        // the maximum: of S by runs, as f is positive; S is read again below, which costs less than the registers to hold it
+        float best = kLowest;
+        uint32_t v[2][32];
+        tmem_load(s_at, v[0]);
 #pragma unroll
-        for (uint32_t b = 0; b < S::kSubs; ++b) {
-          float ks, e;
-          asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(e) : "r"(from + 16u * b));
-          const float f = factor * ks;
-          const Two ff = two(f, f), ee = two(e, e);
+        for (uint32_t c = 0; c < S::kTokens; c += 32) {
+          uint32_t (&now)[32] = v[(c / 32) % 2];
+          tmem_wait();
+          tmem_load(s_at + (c + 32) % S::kTokens, v[(c / 32 + 1) % 2]);          // at the end the first again
+          if (!inside) hide(now, lo - static_cast<int32_t>(c), hi - static_cast<int32_t>(c));
 #pragma unroll
-          for (uint32_t c = 16 * b; c < 16 * b + 16; c += 2) {
-            const Two y = fma2(two(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), ff, ee);
-            v[c] = __float_as_uint(low(y));
-            v[c + 1] = __float_as_uint(high(y));
+          for (uint32_t h = 0; h < 2; ++h) {
+            float m = __uint_as_float(now[16 * h]), f, e, back;
+            run(c / 16 + h, f, e, back);
+#pragma unroll
+            for (uint32_t k = 1; k < 15; k += 2) m = largest3(m, __uint_as_float(now[16 * h + k]), __uint_as_float(now[16 * h + k + 1]));
+            best = fmaxf(best, fmaf(fmaxf(m, __uint_as_float(now[16 * h + 15])), f, e));
           }
         }
-        if (!inside) {
-          const int32_t lo = seen.first - t0, hi = seen.end - t0;
-#pragma unroll
-          for (int32_t c = 0; c < static_cast<int32_t>(S::kTokens); ++c)
-            if (c < lo || c >= hi) v[c] = 0xFF800000u;
-        }
-#pragma unroll
-        for (uint32_t c = 0; c < S::kTokens; c += 2) best = largest3(best, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
         if (__any_sync(kAll, best > top + kSlack)) {
           const float now = fmaxf(top, best), shrink = exp2_near(top - now);
           top = now;
@@ -268,23 +277,41 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           }
         }
         const float less = kUpTile - top;
-        const Two ll = two(less, less);
 #pragma unroll
-        for (uint32_t b = 0; b < S::kSubs; ++b) {
-          float back;
-          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(back) : "r"(from + 16u * b + 8u));
-          Two part = 0;
+        for (uint32_t c = 0; c < S::kTokens; c += 32) {
+          uint32_t (&now)[32] = v[(c / 32) % 2];
+          tmem_wait();
+          if (c + 32 < S::kTokens) tmem_load(s_at + c + 32, v[(c / 32 + 1) % 2]);
+          float back[2];
 #pragma unroll
-          for (uint32_t c = 16 * b; c < 16 * b + 16; c += 2) {
-            const Two y = add2(two(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), ll);
-            const float p0 = exp2_near(low(y)), p1 = exp2_near(high(y));
-            part = add2(part, two(p0, p1));
-            v[c / 2] = pack_half(p0, p1);
+          for (uint32_t h = 0; h < 2; ++h) {
+            float f, e;
+            run(c / 16 + h, f, e, back[h]);
+            const float add = e + less;
+            const Two ff = two(f, f), aa = two(add, add);
+#pragma unroll
+            for (uint32_t k = 16 * h; k < 16 * h + 16; k += 2) {
+              const Two y = fma2(two(__uint_as_float(now[k]), __uint_as_float(now[k + 1])), ff, aa);
+              now[k] = __float_as_uint(low(y));
+              now[k + 1] = __float_as_uint(high(y));
+            }
           }
-          sum = fmaf(low(part) + high(part), back, sum);
-        }
+          // what is not seen is hidden here, also from a scale that is NaN
+          if (!inside) hide(now, lo - static_cast<int32_t>(c), hi - static_cast<int32_t>(c));
+          uint32_t packed[16];
 #pragma unroll
-        for (uint32_t c = 0; c < S::kTokens / 2; c += 32) tmem_store(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+          for (uint32_t h = 0; h < 2; ++h) {
+            Two part = 0;
+#pragma unroll
+            for (uint32_t k = 16 * h; k < 16 * h + 16; k += 2) {
+              const float p0 = exp2_near(__uint_as_float(now[k])), p1 = exp2_near(__uint_as_float(now[k + 1]));
+              part = add2(part, two(p0, p1));
+              packed[k / 2] = pack_half(p0, p1);
+            }
+            sum = fmaf(low(part) + high(part), back[h], sum);
+          }
+          tmem_store16(s_at + c / 2, packed);          // over what has been read
+        }
         tmem_stored();
         fence_before();
         __syncwarp();
@@ -320,57 +347,52 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       }
     }
   } else if (mine && warp < kAtIssue) {
-    // ---- converters
-    regs_open();
-    const uint32_t t = threadIdx.x - 32 * kAtSoft, row0 = t / (D / 16), c = t % (D / 16);
+    // ---- converters: a warp has kOwn tokens of every block, one or two runs of 16
+    const uint32_t w = warp - kAtSoft, row0 = lane / (D / 16), c = lane % (D / 16);
     // piece c of a token: chunks 2 c and 2 c + 1 of 8 dimensions; those of the second four pieces the other way round, so
     // that eight lanes write to different banks
     const uint32_t odd = (c >> 2) & 1u, panel = c / 4u;
-    const uint32_t warp_row = (t & ~31u) / (D / 16);   // a warp's pieces lie in one run of 16 tokens
-    const uint32_t in = c * 16u < a.c.dim ? 1u : 0u;
-    uint64_t where = 0;                                // lane b: run b of 16 tokens
-    float ks = 0.f, e = 0.f, back = 0.f;
-    uint32_t used = 0;
-    auto look = [&](uint32_t block) {                  // the pages of a block's runs
-      const uint32_t token = block * S::kTokens + lane * 16u;
-      used = 0;
-      ks = 0.f; e = -INFINITY; back = 0.f;
-      if (lane < S::kSubs && block < first + blocks && token < static_cast<uint32_t>(T.length)) {
-        const uint32_t p_in = token / a.c.page_size;
-        const int32_t page = table[p_in];
-        if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {
-          const uint64_t at = uint64_t(page) * a.c.heads + head;
-          where = (at * a.c.page_size + (token - p_in * a.c.page_size)) * a.c.dim;
-          ks = usable(a.c.scales[0][at]);
-          e = log2_near(usable(a.c.scales[1][at]));
-          back = isnan(e) ? 1.f : exp2_near(-e - kUpTile);             // where e is NaN, so is what is summed
-          used = 1;
-        } else {
-          atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-        }
+    const bool in = c * 16u < a.c.dim;
+    const uint64_t from = uint64_t(row0) * a.c.dim + c * 16u;
+    // page numbers are asked for a block ahead of their codes, those a block ahead of their use
+    int32_t page[S::kRuns];
+    uint32_t offset[S::kRuns];                         // of a run in its page
+    auto ask = [&](uint32_t block) {
+#pragma unroll
+      for (uint32_t r = 0; r < S::kRuns; ++r) {
+        const uint32_t token = block * S::kTokens + w * S::kOwn + 16u * r, p_in = token / a.c.page_size;
+        offset[r] = token - p_in * a.c.page_size;
+        page[r] = -1;
+        if (block < first + blocks && token < static_cast<uint32_t>(T.length)) page[r] = table[p_in];
+      }
+    };
+    uint64_t where[S::kRuns];
+    bool used[S::kRuns];
+    auto take = [&]() {
+#pragma unroll
+      for (uint32_t r = 0; r < S::kRuns; ++r) {
+        used[r] = in && page[r] >= 0 && static_cast<uint32_t>(page[r]) < a.c.n_pages;
+        where[r] = from + ((uint64_t(max(page[r], 0)) * a.c.heads + head) * a.c.page_size + offset[r]) * a.c.dim;
       }
     };
     uint4 codes[2][S::kPieces];
     auto load = [&](uint32_t which) {
 #pragma unroll
       for (uint32_t i = 0; i < S::kPieces; ++i) {
-        const uint32_t sub = (warp_row + i * S::kDown) / 16u;
-        const uint64_t p = __shfl_sync(kAll, where, sub);
-        const uint32_t u = __shfl_sync(kAll, used, sub);
+        const uint32_t r = i * S::kDown / 16u;
         codes[which][i] = make_uint4(0, 0, 0, 0);
-        const uint32_t row = row0 + i * S::kDown;
-        if (u && in) codes[which][i] = *reinterpret_cast<const uint4*>(a.c.codes[which] + p + (row % 16u) * a.c.dim + c * 16u);
+        if (used[r]) codes[which][i] = *reinterpret_cast<const uint4*>(a.c.codes[which] + where[r] + (i * S::kDown % 16u) * a.c.dim);
       }
     };
     auto open = [&](uint32_t which, uint32_t to) {
 #pragma unroll
       for (uint32_t i = 0; i < S::kPieces; ++i) {
-        const uint32_t row = row0 + i * S::kDown;
-        const uint32_t* const w = &codes[which][i].x;
+        const uint32_t row = w * S::kOwn + row0 + i * S::kDown;
+        const uint32_t* const x = &codes[which][i].x;
         uint32_t h[8];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t u = w[k] ^ 0x80808080u;
+          const uint32_t u = x[k] ^ 0x80808080u;
           h[2 * k] = open_low(u);
           h[2 * k + 1] = open_high(u);
         }
@@ -382,13 +404,15 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
                      "r"(odd ? h[2] : h[6]), "r"(odd ? h[3] : h[7]) : "memory");
       }
     };
-    look(first);
+    ask(first);
+    take();
     load(0);
     load(1);
+    ask(first + 1);
     for (uint32_t n = 0; n < blocks; ++n) {
       const uint32_t stage = n % S::kStages, round = n / S::kStages;
-      const float now_ks = ks, now_e = e, now_back = back;             // of this block's runs
-      look(first + n + 1);
+      take();
+      ask(first + n + 2);
       if (round) bar_wait(k_empty + 8 * stage, (round - 1u) & 1u, bad);
       open(0, k_at + stage * S::kTile);
       fence_operands();
@@ -397,15 +421,40 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       load(0);
       if (round) bar_wait(v_empty + 8 * stage, (round - 1u) & 1u, bad);
       open(1, v_at + stage * S::kTile);
-      if (warp == kAtSoft && lane < S::kSubs)
-        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(meta + (stage * S::kSubs + lane) * 16u), "f"(now_ks), "f"(now_e), "f"(now_back), "f"(0.f) : "memory");
       fence_operands();
       __syncwarp();
       if (lane == 0) arrive(v_full + 8 * stage);
       load(1);
     }
+  } else if (mine && warp == kAtScales) {
+    // ---- scales: lane b has run b of every block
+    float ks, e, back;
+    auto look = [&](uint32_t block) {
+      const uint32_t token = block * S::kTokens + lane * 16u;
+      ks = 1.f; e = -INFINITY; back = 0.f;             // not there: not seen
+      if (lane < S::kSubs && block < first + blocks && token < static_cast<uint32_t>(T.length)) {
+        const int32_t page = table[token / a.c.page_size];
+        if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {
+          const uint64_t at = uint64_t(page) * a.c.heads + head;
+          ks = usable(a.c.scales[0][at]);
+          e = log2_near(usable(a.c.scales[1][at]));
+          if (isnan(ks)) e = ks;
+          back = isnan(e) ? 1.f : exp2_near(-e - kUpTile);             // where e is NaN, so is what is summed
+        } else {
+          atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+        }
+      }
+    };
+    for (uint32_t n = 0; n < blocks; ++n) {
+      const uint32_t stage = n % S::kStages, round = n / S::kStages;
+      look(first + n);
+      if (round) bar_wait(v_empty + 8 * stage, (round - 1u) & 1u, bad);
+      if (lane < S::kSubs)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(meta + (stage * S::kSubs + lane) * 16u), "f"(ks), "f"(e), "f"(back), "f"(0.f) : "memory");
+      __syncwarp();
+      if (lane == 0) arrive(v_full + 8 * stage);
+    }
   } else if (mine) {
-    regs_few();
     if (warp == kAtIssue && lane == 0) {
       // ---- issuer
       constexpr uint32_t is = instruction_half(S::kTokens, false), io = instruction_half(D, true);
