@@ -570,6 +570,7 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   a.share = d.q_heads / a.c.heads;
   a.window = std::min<uint32_t>(d.window, 0x7FFFFFFFu);
   a.causal = d.causal != 0;
+  a.out_wide = !((reinterpret_cast<uintptr_t>(d.d_out) | (d.out_token_stride | d.out_head_stride) * 2) & 15);
   a.scale2 = static_cast<float>(d.scale * 1.4426950408889634);
   return ANS_OK;
 }

@@ -24,6 +24,7 @@ struct AttendArgs {
   const __nv_bfloat16* q; __nv_bfloat16* out;
   uint64_t q_token, q_head, out_token, out_head;       // strides, elements
   uint32_t share, window, causal;
+  uint32_t out_wide;                                   // eight values of out can be stored at once
   float scale2;                                        // scale * log2(e)
   uint32_t least, most;                                // a kernel takes sequences of least .. most rows (new tokens * share)
   float* parts;                                        // partial results: see the kernels

@@ -17,6 +17,7 @@
 // reason O may be rescaled by whoever has seen S of the next block.  Where there are fewer tiles than SMs, several blocks have parts
 // of a tile's tokens and a second kernel joins them.
 #include <algorithm>
+#include <type_traits>
 
 #include "ans_attend.cuh"
 #include "ans_attend_tiles.cuh"
@@ -27,7 +28,7 @@ namespace blk {
 constexpr float kUpTile = 7.f, kSlack = 8.f;           // P <= 2^15
 constexpr float kLeastFactor = 1e-38f;                 // of S, so that -inf times it is -inf
 constexpr uint32_t kAtSoft = 8, kAtOpen = 4, kAtIssue = kAtSoft + kAtOpen, kAtScales = kAtIssue + 1;   // warps: softmax, converters, issuer, scales
-constexpr uint32_t kAtThreads = 32 * (kAtScales + 1);
+constexpr uint32_t kAtThreads = 32 * (kAtScales + 3);       // and two idle, as registers move by four warps
 
 template <int D>
 struct AtShape {
@@ -49,6 +50,12 @@ struct AtShape {
   static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory; halves 128 and D apart
 };
 
+// Registers a thread: the launch brings 128 for 512 threads.
+__device__ __forceinline__ void regs_soft() { asm volatile("setmaxnreg.inc.sync.aligned.u32 176;"); }
+__device__ __forceinline__ void regs_open() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
+__device__ __forceinline__ void regs_issue() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
+static_assert(256 * 176 + 128 * 104 + 128 * 56 <= kAtThreads * 128, "");
+
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) {
@@ -57,12 +64,7 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
                :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-                  "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-               :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+                  "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
@@ -73,13 +75,26 @@ __device__ __forceinline__ uint64_t operand_across(uint32_t addr, uint32_t panel
 __host__ __device__ constexpr uint32_t instruction_half(uint32_t n, bool across) {
   return (1u << 4) | (across ? 1u << 16 : 0u) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
-__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+// One lane of a warp that runs together issues: so the operands stay in uniform registers, and an instruction costs a few
+// clocks of issue where a single lane's branch costs 130, twice what the instruction takes on the tensor pipe.
+__device__ __forceinline__ uint32_t elect() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r;
 }
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_smem(uint32_t chosen, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(chosen) : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t chosen, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+               "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(chosen) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t chosen, uint32_t bar) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+               "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" :: "r"(bar), "r"(chosen) : "memory");
 }
 __device__ __forceinline__ float largest3(float a, float b, float c) {
   float r;
@@ -115,6 +130,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   uint32_t bad = 0;
   __shared__ uint32_t s_seq;
+  const float4* const scales = reinterpret_cast<const float4*>(smem_raw + (meta - smem_addr(smem_raw)));
 
   if (threadIdx.x == 0) {
     for (uint32_t s = 0; s < S::kStages; ++s) {
@@ -130,7 +146,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   let_next_start();
   wait_for_previous();
   // tiles: sequence s has starts[s] * share / rows + s and on; those that see most come first
-  const uint32_t x = gridDim.x - 1u - blockIdx.x, head = blockIdx.y;
+  const uint32_t behind = blockIdx.x / a.c.heads, head = blockIdx.x - behind * a.c.heads, x = gridDim.x / a.c.heads - 1u - behind;
   if (warp == 0) {
     uint32_t lo = 0, span = a.b.n_seqs;
     while (span > 1) {
@@ -188,36 +204,44 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
 
   if (mine && warp < kAtSoft) {
     // ---- softmax: a row a thread
-    const uint32_t half = warp >> 2, in = threadIdx.x & 127u, row = T.r0 + threadIdx.x;
+    regs_soft();
+    const uint32_t half = warp >> 2, row = T.r0 + threadIdx.x;
     if (half < halves) {
       const bool live = threadIdx.x < T.live;
       const uint32_t i = (live ? row : T.r0) / a.share, j = (live ? row : T.r0) - i * a.share;
-      float factor;
+      // the queries of this warp's 32 rows, kPer lanes a row
+      constexpr uint32_t kPer = D / 8 < 32 ? D / 8 : 32, kAtOnce = 32 / kPer;
+      uint32_t my_top = 0;
       {
-        const __nv_bfloat16* const from = a.q + (T.row + i) * a.q_token + (head * a.share + j) * a.q_head;
-        uint32_t top = 0;
+        const uint32_t d = (lane % kPer) * 8u;
 #pragma unroll 4
-        for (uint32_t d = 0; d < D; d += 8) {
-          if (d >= a.c.dim || !live) break;
-          const uint4 w = *reinterpret_cast<const uint4*>(from + d);
-          const uint32_t* const e = &w.x;
+        for (uint32_t r = 0; r < 32; r += kAtOnce) {
+          const uint32_t in_tile = warp * 32u + r + lane / kPer;
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (in_tile < T.live && d < a.c.dim) {
+            const uint32_t at = T.r0 + in_tile, token = at / a.share;
+            w = *reinterpret_cast<const uint4*>(a.q + (T.row + token) * a.q_token + (head * a.share + (at - token * a.share)) * a.q_head + d);
+          }
+          uint32_t* const e = &w.x;
+          uint32_t top = 0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) top = max(top, max((e[k] << 16) & 0x7FFFFFFFu, e[k] & 0x7FFF0000u));
-        }
-        const int32_t up = exponent_of(top);
-        const float down = a.scale2 < 0.f ? -power_of(-up) : power_of(-up);
-        factor = fabsf(a.scale2) * power_of(up);       // the scale's sign goes to the queries
-#pragma unroll 4
-        for (uint32_t d = 0; d < D; d += 8) {
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (d < a.c.dim && live) w = *reinterpret_cast<const uint4*>(from + d);
-          uint32_t* const e = &w.x;
+#pragma unroll
+          for (uint32_t step = 1; step < kPer; step *= 2) top = max(top, __shfl_xor_sync(kAll, top, step));
+#pragma unroll
+          for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t of = __shfl_sync(kAll, top, k * kPer);
+            if (lane == r + k) my_top = of;
+          }
+          const float down = power_of(-exponent_of(top)) * (a.scale2 < 0.f ? -1.f : 1.f);      // the scale's sign goes to the queries
 #pragma unroll
           for (int k = 0; k < 4; ++k) e[k] = pack_half(__uint_as_float(e[k] << 16) * down, __uint_as_float(e[k] & 0xFFFF0000u) * down);
-          const uint32_t to = q_at + (half * S::kPanels + d / 64u) * S::kQPanel + in * 128u + (((d / 8u) & 7u) ^ (in & 7u)) * 16u;
+          const uint32_t in_half = in_tile & 127u;
+          const uint32_t to = q_at + (half * S::kPanels + d / 64u) * S::kQPanel + in_half * 128u + (((d / 8u) & 7u) ^ (in_half & 7u)) * 16u;
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
         }
       }
+      const float factor = fabsf(a.scale2) * power_of(exponent_of(my_top));
       fence_operands();
       __syncwarp();
       if (lane == 0) arrive(q_full);
@@ -233,32 +257,28 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
         __syncwarp();
         fence_after();
         const int32_t t0 = static_cast<int32_t>((first + n) * S::kTokens), lo = seen.first - t0, hi = seen.end - t0;
-        const uint32_t from = meta + stage * S::kSubs * 16u;
         const bool inside = t0 >= all_lo && t0 + static_cast<int32_t>(S::kTokens) <= all_hi;
-        // the runs of 16 tokens: s_i + e_i = S_i f + e
+        // of a run of 16 tokens: s_i + e_i = S_i f + e, and what p_i counts for in the sum
         auto run = [&](uint32_t b, float& f, float& e, float& back) {
-          float rest;
-          asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f), "=f"(e), "=f"(back), "=f"(rest) : "r"(from + 16u * b));
-          f = fmaxf(factor * f, kLeastFactor);
+          const float4 m = scales[stage * S::kSubs + b];
+          f = fmaxf(factor * m.x, kLeastFactor);
+          e = m.y;
+          back = m.z;
         };
-        // the maximum: of S by runs, as f is positive; S is read again below, which costs less than the registers to hold it
+        uint32_t v[S::kTokens];
+#pragma unroll
+        for (uint32_t c = 0; c < S::kTokens; c += 32) tmem_load(s_at + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+        tmem_wait();
+        if (!inside) hide(v, lo, hi);
+        // the maximum, of S by runs, as f is positive
         float best = kLowest;
-        uint32_t v[2][32];
-        tmem_load(s_at, v[0]);
 #pragma unroll
-        for (uint32_t c = 0; c < S::kTokens; c += 32) {
-          uint32_t (&now)[32] = v[(c / 32) % 2];
-          tmem_wait();
-          tmem_load(s_at + (c + 32) % S::kTokens, v[(c / 32 + 1) % 2]);          // at the end the first again
-          if (!inside) hide(now, lo - static_cast<int32_t>(c), hi - static_cast<int32_t>(c));
+        for (uint32_t b = 0; b < S::kSubs; ++b) {
+          float m = __uint_as_float(v[16 * b]), f, e, back;
+          run(b, f, e, back);
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            float m = __uint_as_float(now[16 * h]), f, e, back;
-            run(c / 16 + h, f, e, back);
-#pragma unroll
-            for (uint32_t k = 1; k < 15; k += 2) m = largest3(m, __uint_as_float(now[16 * h + k]), __uint_as_float(now[16 * h + k + 1]));
-            best = fmaxf(best, fmaf(fmaxf(m, __uint_as_float(now[16 * h + 15])), f, e));
-          }
+          for (uint32_t k = 1; k < 15; k += 2) m = largest3(m, __uint_as_float(v[16 * b + k]), __uint_as_float(v[16 * b + k + 1]));
+          best = fmaxf(best, fmaf(fmaxf(m, __uint_as_float(v[16 * b + 15])), f, e));
         }
         if (__any_sync(kAll, best > top + kSlack)) {
           const float now = fmaxf(top, best), shrink = exp2_near(top - now);
@@ -276,42 +296,37 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
             }
           }
         }
-        const float less = kUpTile - top;
+        // one stretch of code without branches, so that the runs' chains of instructions run beside each other
+        auto weigh = [&](auto all_seen) {
+          const float less = kUpTile - top;
 #pragma unroll
-        for (uint32_t c = 0; c < S::kTokens; c += 32) {
-          uint32_t (&now)[32] = v[(c / 32) % 2];
-          tmem_wait();
-          if (c + 32 < S::kTokens) tmem_load(s_at + c + 32, v[(c / 32 + 1) % 2]);
-          float back[2];
-#pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            float f, e;
-            run(c / 16 + h, f, e, back[h]);
+          for (uint32_t b = 0; b < S::kSubs; ++b) {
+            float f, e, back;
+            run(b, f, e, back);
             const float add = e + less;
             const Two ff = two(f, f), aa = two(add, add);
+            uint32_t (&now)[16] = *reinterpret_cast<uint32_t(*)[16]>(v + 16 * b);
 #pragma unroll
-            for (uint32_t k = 16 * h; k < 16 * h + 16; k += 2) {
+            for (uint32_t k = 0; k < 16; k += 2) {
               const Two y = fma2(two(__uint_as_float(now[k]), __uint_as_float(now[k + 1])), ff, aa);
               now[k] = __float_as_uint(low(y));
               now[k + 1] = __float_as_uint(high(y));
             }
-          }
-          // what is not seen is hidden here, also from a scale that is NaN
-          if (!inside) hide(now, lo - static_cast<int32_t>(c), hi - static_cast<int32_t>(c));
-          uint32_t packed[16];
+            // what is not seen is hidden again, also from a scale that is NaN
+            if constexpr (!decltype(all_seen)::value) hide(now, lo - static_cast<int32_t>(16 * b), hi - static_cast<int32_t>(16 * b));
+            Two part[2] = {0, 0};
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            Two part = 0;
-#pragma unroll
-            for (uint32_t k = 16 * h; k < 16 * h + 16; k += 2) {
+            for (uint32_t k = 0; k < 16; k += 2) {
               const float p0 = exp2_near(__uint_as_float(now[k])), p1 = exp2_near(__uint_as_float(now[k + 1]));
-              part = add2(part, two(p0, p1));
-              packed[k / 2] = pack_half(p0, p1);
+              part[(k / 2) % 2] = add2(part[(k / 2) % 2], two(p0, p1));
+              v[8 * b + k / 2] = pack_half(p0, p1);
             }
-            sum = fmaf(low(part) + high(part), back[h], sum);
+            const Two both = add2(part[0], part[1]);
+            sum = fmaf(low(both) + high(both), back, sum);
+            if (b % 4 == 3) tmem_store(s_at + 8 * (b - 3), *reinterpret_cast<uint32_t(*)[32]>(v + 8 * (b - 3)));
           }
-          tmem_store16(s_at + c / 2, packed);          // over what has been read
-        }
+        };
+        if (inside) weigh(std::true_type{}); else weigh(std::false_type{});
         tmem_stored();
         fence_before();
         __syncwarp();
@@ -321,32 +336,69 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       __syncwarp();
       fence_after();
       const float f = sum == 0.f ? 0.f : exp2_near(-kUpTile) / sum;
-      __nv_bfloat16* const to = a.out + (T.row + i) * a.out_token + (head * a.share + j) * a.out_head;
-      const uint64_t part = (uint64_t(blockIdx.z) * a.b.rows + T.row + i) * (a.share * a.c.heads) + head * a.share + j;
-      float* const sums = a.parts + part * D;
-      if (splits > 1 && live) reinterpret_cast<float2*>(a.parts + uint64_t(splits) * a.b.rows * (a.share * a.c.heads) * D)[part] = make_float2(top, sum);
+      const uint32_t heads = a.share * a.c.heads;
+      const uint64_t part = (uint64_t(blockIdx.z) * a.b.rows + T.row + i) * heads + head * a.share + j;
+      if (splits > 1 && live) reinterpret_cast<float2*>(a.parts + uint64_t(splits) * a.b.rows * heads * D)[part] = make_float2(top, sum);
+      // Rows leave through the stages of K and V, which are done with, 8 KB a warp: 128 bytes of a row a step, its 16-byte pieces
+      // in the places where eight rows meet different banks.
+      const uint32_t own = k_at + warp * 8192u;
+      static_assert(2 * S::kStages * S::kTile >= 8 * 8192, "");
+      constexpr uint32_t kStep = 64;                   // dimensions: as bf16 128 bytes, or as fp32 two lines of 128
 #pragma unroll 1
-      for (uint32_t c = 0; c < D; c += 32) {
-        uint32_t o[32];
-        tmem_load(o_at + c, o);
+      for (uint32_t c = 0; c < D; c += kStep) {
+        uint32_t o[64];
+        tmem_load(o_at + c, *reinterpret_cast<uint32_t(*)[32]>(o));
+        tmem_load(o_at + c + 32, *reinterpret_cast<uint32_t(*)[32]>(o + 32));
         tmem_wait();
         if (!blocks) {
 #pragma unroll
-          for (int k = 0; k < 32; ++k) o[k] = 0u;
+          for (int k = 0; k < 64; ++k) o[k] = 0u;
         }
-        if (!live) continue;
         if (splits > 1) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) *reinterpret_cast<uint4*>(sums + c + k) = make_uint4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          for (uint32_t k = 0; k < 16; ++k)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(own + (k / 8) * 4096u + lane * 128u + ((k ^ lane) & 7u) * 16u), "r"(o[4 * k]),
+                         "r"(o[4 * k + 1]), "r"(o[4 * k + 2]), "r"(o[4 * k + 3]) : "memory");
         } else {
 #pragma unroll
-          for (int k = 0; k < 32; k += 2)
-            if (c + k < a.c.dim)
-              *reinterpret_cast<__nv_bfloat162*>(to + c + k) = __floats2bfloat162_rn(__uint_as_float(o[k]) * f, __uint_as_float(o[k + 1]) * f);
+          for (uint32_t k = 0; k < 8; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (uint32_t x = 0; x < 4; ++x) {
+              const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(o[8 * k + 2 * x]) * f, __uint_as_float(o[8 * k + 2 * x + 1]) * f);
+              w[x] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(own + lane * 128u + ((k ^ lane) & 7u) * 16u), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                         "r"(w[3]) : "memory");
+          }
         }
+        __syncwarp();
+        const uint32_t lines = splits > 1 ? 2u : 1u;
+#pragma unroll 4
+        for (uint32_t r = lane / 8u; r < 32u * lines; r += 4) {          // eight lanes a line
+          const uint32_t line = r / 32u, in_warp = r % 32u, in_tile = warp * 32u + in_warp, k = lane & 7u;
+          uint4 w;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
+                       : "r"(own + line * 4096u + in_warp * 128u + ((k ^ in_warp) & 7u) * 16u) : "memory");
+          if (in_tile >= T.live) continue;
+          const uint32_t at = T.r0 + in_tile, token = at / a.share, h = head * a.share + (at - token * a.share);
+          if (splits > 1) {
+            *reinterpret_cast<uint4*>(a.parts + ((uint64_t(blockIdx.z) * a.b.rows + T.row + token) * heads + h) * D + c + line * 32u + 4u * k) = w;
+          } else if (c + 8u * k < a.c.dim) {
+            __nv_bfloat16* const to = a.out + (T.row + token) * a.out_token + h * a.out_head + c + 8u * k;
+            if (a.out_wide) {
+              *reinterpret_cast<uint4*>(to) = w;
+            } else {
+              uint32_t* const p = reinterpret_cast<uint32_t*>(to);
+              p[0] = w.x; p[1] = w.y; p[2] = w.z; p[3] = w.w;
+            }
+          }
+        }
+        __syncwarp();
       }
     }
   } else if (mine && warp < kAtIssue) {
+    regs_open();
     // ---- converters: a warp has kOwn tokens of every block, one or two runs of 16
     const uint32_t w = warp - kAtSoft, row0 = lane / (D / 16), c = lane % (D / 16);
     // piece c of a token: chunks 2 c and 2 c + 1 of 8 dimensions; those of the second four pieces the other way round, so
@@ -428,6 +480,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     }
   } else if (mine && warp == kAtScales) {
     // ---- scales: lane b has run b of every block
+    regs_issue();
     float ks, e, back;
     auto look = [&](uint32_t block) {
       const uint32_t token = block * S::kTokens + lane * 16u;
@@ -455,26 +508,28 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       if (lane == 0) arrive(v_full + 8 * stage);
     }
   } else if (mine) {
-    if (warp == kAtIssue && lane == 0) {
-      // ---- issuer
+    regs_issue();
+    if (warp == kAtIssue) {
+      // ---- issuer: the whole warp waits, one lane issues
+      const uint32_t me = elect();
       constexpr uint32_t is = instruction_half(S::kTokens, false), io = instruction_half(D, true);
       auto scores = [&](uint32_t h, uint32_t stage) {
 #pragma unroll
         for (uint32_t p = 0; p < S::kPanels; ++p) {
           const uint64_t dq = operand(q_at + (h * S::kPanels + p) * S::kQPanel), dk = operand(k_at + stage * S::kTile + p * S::kPanel);
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) mma_smem(tmem + S::kS + h * 128u, dq + 2u * k, dk + 2u * k, is, p || k);
+          for (uint32_t k = 0; k < 4; ++k) mma_smem(me, tmem + S::kS + h * 128u, dq + 2u * k, dk + 2u * k, is, p || k);
         }
-        mma_commit<1>(s_full + 8 * h);
+        commit(me, s_full + 8 * h);
       };
       auto outputs = [&](uint32_t h, uint32_t stage, bool more) {
         const uint64_t dv = operand_across(v_at + stage * S::kTile, S::kPanel);
 #pragma unroll
         for (uint32_t k = 0; k < S::kTokens / 16; ++k)
-          mma_tmem(tmem + S::kO + h * D, tmem + S::kS + h * 128u + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || k);
+          mma_tmem(me, tmem + S::kO + h * D, tmem + S::kS + h * 128u + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || k);
       };
       for (uint32_t h = 0; h < S::kHalves; ++h)
-        if (h >= halves) for (uint32_t i = 0; i < 4; ++i) arrive(q_full);            // a half without rows
+        if (h >= halves) for (uint32_t i = 0; i < 4; ++i) { if (lane == 0) arrive(q_full); }            // a half without rows
       bar_wait(q_full, 0u, bad);
       for (uint32_t n = 0; n < blocks; ++n) {
         const uint32_t stage = n % S::kStages, parity = (n / S::kStages) & 1u;
@@ -482,7 +537,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           bar_wait(k_full, 0u, bad);
           fence_after();
           for (uint32_t h = 0; h < halves; ++h) scores(h, 0);
-          mma_commit<1>(k_empty);
+          commit(me, k_empty);
         }
         bar_wait(v_full + 8 * stage, parity, bad);
         const uint32_t next = (n + 1) % S::kStages;
@@ -490,16 +545,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           bar_wait(p_full + 8 * h, n & 1u, bad);
           fence_after();
           outputs(h, stage, n > 0);
-          if (h + 1 == halves) mma_commit<1>(v_empty + 8 * stage);
+          if (h + 1 == halves) commit(me, v_empty + 8 * stage);
           if (n + 1 < blocks) {
             if (h == 0) bar_wait(k_full + 8 * next, ((n + 1) / S::kStages) & 1u, bad);
             fence_after();
             scores(h, next);
-            if (h + 1 == halves) mma_commit<1>(k_empty + 8 * next);
+            if (h + 1 == halves) commit(me, k_empty + 8 * next);
           }
         }
       }
-      mma_commit<1>(o_full);
+      commit(me, o_full);
       bar_wait(o_full, 0u, bad);                       // nothing is under way any more
     }
   }
@@ -582,7 +637,7 @@ static int launch_tiles_shape(const AttendArgs& a, const AtPlan& p, cudaStream_t
   constexpr auto kernel = ans_attend_tiles_kernel<D>;
   static_assert(S::kSmem <= 227 * 1024, "");
   int rc = allow_smem<kernel>(S::kSmem);
-  if (rc == ANS_OK) rc = launch(kernel, dim3(p.tiles, a.c.heads, p.splits), dim3(kAtThreads), S::kSmem, st, 1, a, p.splits);
+  if (rc == ANS_OK) rc = launch(kernel, dim3(a.c.heads * p.tiles, 1, p.splits), dim3(kAtThreads), S::kSmem, st, 1, a, p.splits);
   if (rc == ANS_OK && p.splits > 1) {
     const uint64_t blocks = (uint64_t(a.b.rows) * a.share * a.c.heads + 7) / 8;
     rc = launch(ans_attend_tiles_join_kernel<D>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, st, 1, a, p.splits);
