@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       const uint32_t r = 8u * m + g;
       uint4 w[D / 32];
       uint32_t top = 0;
-      const uint32_t i = (r0 + min(r, live - 1u)) / a.share, j = (r0 + min(r, live - 1u)) - i * a.share;
+      const uint32_t i = token_of(a, r0 + min(r, live - 1u)), j = (r0 + min(r, live - 1u)) - i * a.share;
       const __nv_bfloat16* const from = a.q + (q.row + i) * a.q_token + (head * a.share + j) * a.q_head;
 #pragma unroll
       for (uint32_t x = 0; x < D / 32; ++x) {          // 8 values: half x % 2 of dims 64 (x / 2) + 16 t
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       for (int e = 0; e < 2; ++e) {
         factor[m][e] = a.scale2 * power_of(__shfl_sync(kAll, up, (2u * t + e) * 4u));
         const uint32_t col = 8u * m + 2u * t + e;
-        const Seen v = seen_by(a, q.old, q.length, (r0 + min(col, live - 1u)) / a.share);
+        const Seen v = seen_by(a, q.old, q.length, token_of(a, r0 + min(col, live - 1u)));
         lo[m][e] = v.first;
         hi[m][e] = v.end;
         all_lo = max(all_lo, v.first);
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       if (whole) {
         if (d < a.c.dim) {
           const float l = total_ml[r].y, f = l == 0.f ? 0.f : exp2_near(-kUp) / l;
-          const uint32_t row = (r0 + r) / a.share, j = (r0 + r) - row * a.share;
+          const uint32_t row = token_of(a, r0 + r), j = (r0 + r) - row * a.share;
           __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.out + (q.row + row) * a.out_token + (head * a.share + j) * a.out_head + d);
           to[0] = __floats2bfloat162_rn(x.x * f, x.y * f);
           to[1] = __floats2bfloat162_rn(x.z * f, x.w * f);
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(128) ans_attend_join_kernel(const AttendArgs a
       }
     }
     const float f = all == 0.f ? 0.f : exp2_near(-kUp) / all;
-    const uint32_t row = (r0 + r) / a.share, j = (r0 + r) - row * a.share;
+    const uint32_t row = token_of(a, r0 + r), j = (r0 + r) - row * a.share;
     __nv_bfloat16* const to = a.out + (q.row + row) * a.out_token + (head * a.share + j) * a.out_head;
 #pragma unroll
     for (int k = 0; k < D / 64; ++k) {
@@ -568,6 +568,10 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   a.q_token = d.q_token_stride; a.q_head = d.q_head_stride; a.out_token = d.out_token_stride; a.out_head = d.out_head_stride;
   if (d.d_q == d.d_out && (d.q_token_stride != d.out_token_stride || d.q_head_stride != d.out_head_stride)) return ANS_ERR_INVALID_ARG;
   a.share = d.q_heads / a.c.heads;
+  uint32_t bits = 0;
+  while ((1u << bits) < a.share) ++bits;
+  a.share_shift = 31 + bits;
+  a.share_by = static_cast<uint32_t>(((uint64_t(1) << a.share_shift) + a.share - 1) / a.share);
   a.window = std::min<uint32_t>(d.window, 0x7FFFFFFFu);
   a.causal = d.causal != 0;
   a.out_wide = !((reinterpret_cast<uintptr_t>(d.d_out) | (d.out_token_stride | d.out_head_stride) * 2) & 15);

@@ -24,12 +24,19 @@ struct AttendArgs {
   const __nv_bfloat16* q; __nv_bfloat16* out;
   uint64_t q_token, q_head, out_token, out_head;       // strides, elements
   uint32_t share, window, causal;
+  uint32_t share_by, share_shift;                      // x / share = x * share_by >> share_shift, x < 2^31
   uint32_t out_wide;                                   // eight values of out can be stored at once
   float scale2;                                        // scale * log2(e)
   uint32_t least, most;                                // a kernel takes sequences of least .. most rows (new tokens * share)
   float* parts;                                        // partial results: see the kernels
   uint32_t* status;
 };
+
+// A row of a sequence (new token * share + query of the head): its token.  With k the bits of share - 1, share_by = ceil(2^(31 + k) / share) and
+// share_shift = 31 + k the quotient is exact: the product is off by x * (less than share) < 2^(31 + k).
+__device__ __forceinline__ uint32_t token_of(const AttendArgs& a, uint32_t row) {
+  return static_cast<uint32_t>(uint64_t(row) * a.share_by >> a.share_shift);
+}
 
 // The tokens that new token i of a sequence sees are [first, end).
 struct Seen { int32_t first, end; };

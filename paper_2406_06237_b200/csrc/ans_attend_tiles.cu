@@ -42,11 +42,10 @@ struct AtShape {
   static constexpr uint32_t kStages = 2;
   static constexpr uint32_t kSubs = kTokens / 16;                      // runs of 16 tokens, each in one page
   static constexpr uint32_t kMeta = kStages * kSubs * 16;
-  static constexpr uint32_t kBars = 8 * (4 * kStages + 2 * kHalves + 2);
+  static constexpr uint32_t kBars = 8 * (4 * kStages + 3 * kHalves + 2);
   static constexpr uint32_t kSmem = 1024 + kQ + 2 * kStages * kTile + kMeta + kBars + 16;
   static constexpr uint32_t kOwn = kTokens / kAtOpen, kRuns = kOwn / 16;         // tokens and runs of a converter's warp
-  static constexpr uint32_t kDown = 32 / (D / 16);                     // tokens between a thread's pieces of 16 codes
-  static constexpr uint32_t kPieces = kOwn / kDown;
+  static constexpr uint32_t kPieces = kOwn / 8 * kPanels;              // of 16 codes, of a converter's lane
   static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory; halves 128 and D apart
 };
 
@@ -65,6 +64,11 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]));
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
@@ -125,7 +129,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   const uint32_t q_at = base, k_at = q_at + S::kQ, v_at = k_at + S::kStages * S::kTile, meta = v_at + S::kStages * S::kTile;
   const uint32_t bars = meta + S::kMeta;
   const uint32_t k_full = bars, k_empty = k_full + 8 * S::kStages, v_full = k_empty + 8 * S::kStages, v_empty = v_full + 8 * S::kStages;
-  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 8 * S::kHalves, q_full = p_full + 8 * S::kHalves, o_full = q_full + 8;
+  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 8 * S::kHalves, q_full = p_full + 16 * S::kHalves, o_full = q_full + 8;
   const uint32_t slot = o_full + 8;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   uint32_t bad = 0;
@@ -137,7 +141,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       bar_init(k_full + 8 * s, kAtOpen); bar_init(k_empty + 8 * s, 1);
       bar_init(v_full + 8 * s, kAtOpen + 1); bar_init(v_empty + 8 * s, 1);
     }
-    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 8 * h, 1); bar_init(p_full + 8 * h, 4); }
+    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 8 * h, 1); bar_init(p_full + 16 * h, 4); bar_init(p_full + 16 * h + 8, 4); }
     bar_init(q_full, 4 * S::kHalves);
     bar_init(o_full, 1);
     bar_init_fence();
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     if (mine) {
       T.r0 = static_cast<uint32_t>(r0);
       T.live = min(S::kRows, rows - T.r0);
-      const Seen top = seen_by(a, T.old, T.length, T.r0 / a.share), end = seen_by(a, T.old, T.length, (T.r0 + T.live - 1u) / a.share);
+      const Seen top = seen_by(a, T.old, T.length, token_of(a, T.r0)), end = seen_by(a, T.old, T.length, token_of(a, T.r0 + T.live - 1u));
       T.b0 = static_cast<uint32_t>(top.first) / S::kTokens;
       T.b1 = (static_cast<uint32_t>(end.end) + S::kTokens - 1) / S::kTokens;
       if (T.b1 < T.b0) T.b1 = T.b0;
@@ -208,21 +212,25 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     const uint32_t half = warp >> 2, row = T.r0 + threadIdx.x;
     if (half < halves) {
       const bool live = threadIdx.x < T.live;
-      const uint32_t i = (live ? row : T.r0) / a.share, j = (live ? row : T.r0) - i * a.share;
+      const uint32_t i = token_of(a, live ? row : T.r0), j = (live ? row : T.r0) - i * a.share;
       // the queries of this warp's 32 rows, kPer lanes a row
       constexpr uint32_t kPer = D / 8 < 32 ? D / 8 : 32, kAtOnce = 32 / kPer;
       uint32_t my_top = 0;
       {
         const uint32_t d = (lane % kPer) * 8u;
-#pragma unroll 4
-        for (uint32_t r = 0; r < 32; r += kAtOnce) {
-          const uint32_t in_tile = warp * 32u + r + lane / kPer;
-          uint4 w = make_uint4(0, 0, 0, 0);
+        uint4 w[32 / kAtOnce];                         // all under way together
+#pragma unroll
+        for (uint32_t n = 0; n < 32 / kAtOnce; ++n) {
+          const uint32_t in_tile = warp * 32u + n * kAtOnce + lane / kPer;
+          w[n] = make_uint4(0, 0, 0, 0);
           if (in_tile < T.live && d < a.c.dim) {
-            const uint32_t at = T.r0 + in_tile, token = at / a.share;
-            w = *reinterpret_cast<const uint4*>(a.q + (T.row + token) * a.q_token + (head * a.share + (at - token * a.share)) * a.q_head + d);
+            const uint32_t at = T.r0 + in_tile, token = token_of(a, at);
+            w[n] = *reinterpret_cast<const uint4*>(a.q + (T.row + token) * a.q_token + (head * a.share + (at - token * a.share)) * a.q_head + d);
           }
-          uint32_t* const e = &w.x;
+        }
+#pragma unroll
+        for (uint32_t n = 0; n < 32 / kAtOnce; ++n) {
+          uint32_t* const e = &w[n].x;
           uint32_t top = 0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) top = max(top, max((e[k] << 16) & 0x7FFFFFFFu, e[k] & 0x7FFF0000u));
@@ -231,14 +239,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
 #pragma unroll
           for (uint32_t k = 0; k < kAtOnce; ++k) {
             const uint32_t of = __shfl_sync(kAll, top, k * kPer);
-            if (lane == r + k) my_top = of;
+            if (lane == n * kAtOnce + k) my_top = of;
           }
           const float down = power_of(-exponent_of(top)) * (a.scale2 < 0.f ? -1.f : 1.f);      // the scale's sign goes to the queries
 #pragma unroll
           for (int k = 0; k < 4; ++k) e[k] = pack_half(__uint_as_float(e[k] << 16) * down, __uint_as_float(e[k] & 0xFFFF0000u) * down);
-          const uint32_t in_half = in_tile & 127u;
+          const uint32_t in_half = (warp * 32u + n * kAtOnce + lane / kPer) & 127u;
           const uint32_t to = q_at + (half * S::kPanels + d / 64u) * S::kQPanel + in_half * 128u + (((d / 8u) & 7u) ^ (in_half & 7u)) * 16u;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(e[0]), "r"(e[1]), "r"(e[2]), "r"(e[3]) : "memory");
         }
       }
       const float factor = fabsf(a.scale2) * power_of(exponent_of(my_top));
@@ -323,14 +331,18 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
             }
             const Two both = add2(part[0], part[1]);
             sum = fmaf(low(both) + high(both), back, sum);
-            if (b % 4 == 3) tmem_store(s_at + 8 * (b - 3), *reinterpret_cast<uint32_t(*)[32]>(v + 8 * (b - 3)));
+            if (b % (S::kSubs / 2) == S::kSubs / 2 - 1) {              // half of P is ready
+              constexpr uint32_t kHalf = S::kTokens / 4;               // columns of it
+              const uint32_t h = b / (S::kSubs / 2);
+              tmem_store(s_at + h * kHalf, *reinterpret_cast<uint32_t(*)[kHalf]>(v + h * kHalf));
+              tmem_stored();
+              fence_before();
+              __syncwarp();
+              if (lane == 0) arrive(p_full + 16 * half + 8 * h);
+            }
           }
         };
         if (inside) weigh(std::true_type{}); else weigh(std::false_type{});
-        tmem_stored();
-        fence_before();
-        __syncwarp();
-        if (lane == 0) arrive(p_full + 8 * half);
       }
       bar_wait(o_full, 0u, bad);
       __syncwarp();
@@ -344,6 +356,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       const uint32_t own = k_at + warp * 8192u;
       static_assert(2 * S::kStages * S::kTile >= 8 * 8192, "");
       constexpr uint32_t kStep = 64;                   // dimensions: as bf16 128 bytes, or as fp32 two lines of 128
+      const uint8_t* const own_p = smem_raw + (own - smem_addr(smem_raw));
+      // eight lanes a row, rows lane / 8, lane / 8 + 4, ...
+      const uint32_t piece = lane & 7u;
+      uint64_t goes[8];                                // elements from the start of out or of the parts
+#pragma unroll
+      for (uint32_t k = 0; k < 8; ++k) {
+        const uint32_t at = T.r0 + min(warp * 32u + 4u * k + lane / 8u, T.live - 1u), token = token_of(a, at), h = head * a.share + (at - token * a.share);
+        goes[k] = splits > 1 ? ((uint64_t(blockIdx.z) * a.b.rows + T.row + token) * heads + h) * D + 4u * piece
+                             : (T.row + token) * a.out_token + h * a.out_head + 8u * piece;
+      }
 #pragma unroll 1
       for (uint32_t c = 0; c < D; c += kStep) {
         uint32_t o[64];
@@ -373,24 +395,26 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           }
         }
         __syncwarp();
-        const uint32_t lines = splits > 1 ? 2u : 1u;
-#pragma unroll 4
-        for (uint32_t r = lane / 8u; r < 32u * lines; r += 4) {          // eight lanes a line
-          const uint32_t line = r / 32u, in_warp = r % 32u, in_tile = warp * 32u + in_warp, k = lane & 7u;
-          uint4 w;
-          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w)
-                       : "r"(own + line * 4096u + in_warp * 128u + ((k ^ in_warp) & 7u) * 16u) : "memory");
-          if (in_tile >= T.live) continue;
-          const uint32_t at = T.r0 + in_tile, token = at / a.share, h = head * a.share + (at - token * a.share);
-          if (splits > 1) {
-            *reinterpret_cast<uint4*>(a.parts + ((uint64_t(blockIdx.z) * a.b.rows + T.row + token) * heads + h) * D + c + line * 32u + 4u * k) = w;
-          } else if (c + 8u * k < a.c.dim) {
-            __nv_bfloat16* const to = a.out + (T.row + token) * a.out_token + h * a.out_head + c + 8u * k;
-            if (a.out_wide) {
-              *reinterpret_cast<uint4*>(to) = w;
-            } else {
-              uint32_t* const p = reinterpret_cast<uint32_t*>(to);
-              p[0] = w.x; p[1] = w.y; p[2] = w.z; p[3] = w.w;
+        for (uint32_t line = 0; line < (splits > 1 ? 2u : 1u); ++line) {
+          uint4 w[8];
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k) {
+            const uint32_t r = 4u * k + lane / 8u;
+            w[k] = *reinterpret_cast<const uint4*>(own_p + line * 4096u + r * 128u + ((piece ^ r) & 7u) * 16u);
+          }
+#pragma unroll
+          for (uint32_t k = 0; k < 8; ++k) {
+            if (warp * 32u + 4u * k + lane / 8u >= T.live) continue;
+            if (splits > 1) {
+              *reinterpret_cast<uint4*>(a.parts + goes[k] + c + line * 32u) = w[k];
+            } else if (c + 8u * piece < a.c.dim) {
+              __nv_bfloat16* const to = a.out + goes[k] + c;
+              if (a.out_wide) {
+                *reinterpret_cast<uint4*>(to) = w[k];
+              } else {
+                uint32_t* const p = reinterpret_cast<uint32_t*>(to);
+                p[0] = w[k].x; p[1] = w[k].y; p[2] = w[k].z; p[3] = w[k].w;
+              }
             }
           }
         }
@@ -398,13 +422,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       }
     }
   } else if (mine && warp < kAtIssue) {
-    regs_open();
     // ---- converters: a warp has kOwn tokens of every block, one or two runs of 16
-    const uint32_t w = warp - kAtSoft, row0 = lane / (D / 16), c = lane % (D / 16);
-    // piece c of a token: chunks 2 c and 2 c + 1 of 8 dimensions; those of the second four pieces the other way round, so
-    // that eight lanes write to different banks
-    const uint32_t odd = (c >> 2) & 1u, panel = c / 4u;
-    const bool in = c * 16u < a.c.dim;
+    regs_open();
+    // A lane has piece lane % 4 (16 codes) of each panel of every eighth token: the two chunks of 8 dimensions that it becomes have the
+    // same places in every panel and every eight tokens, and four lanes by two tokens write to different banks.
+    const uint32_t w = warp - kAtSoft, row0 = lane / 4u, c = lane % 4u;
+    const uint32_t line = (w * S::kOwn + row0) * 128u, place0 = line + ((2u * c) ^ (row0 & 7u)) * 16u, place1 = line + ((2u * c + 1u) ^ (row0 & 7u)) * 16u;
     const uint64_t from = uint64_t(row0) * a.c.dim + c * 16u;
     // page numbers are asked for a block ahead of their codes, those a block ahead of their use
     int32_t page[S::kRuns];
@@ -423,23 +446,23 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     auto take = [&]() {
 #pragma unroll
       for (uint32_t r = 0; r < S::kRuns; ++r) {
-        used[r] = in && page[r] >= 0 && static_cast<uint32_t>(page[r]) < a.c.n_pages;
+        used[r] = page[r] >= 0 && static_cast<uint32_t>(page[r]) < a.c.n_pages;
         where[r] = from + ((uint64_t(max(page[r], 0)) * a.c.heads + head) * a.c.page_size + offset[r]) * a.c.dim;
       }
     };
-    uint4 codes[2][S::kPieces];
+    uint4 codes[2][S::kPieces];                        // piece i: panel i % kPanels, tokens row0 + 8 (i / kPanels)
     auto load = [&](uint32_t which) {
 #pragma unroll
       for (uint32_t i = 0; i < S::kPieces; ++i) {
-        const uint32_t r = i * S::kDown / 16u;
+        const uint32_t down = 8u * (i / S::kPanels), p = i % S::kPanels, r = down / 16u;
         codes[which][i] = make_uint4(0, 0, 0, 0);
-        if (used[r]) codes[which][i] = *reinterpret_cast<const uint4*>(a.c.codes[which] + where[r] + (i * S::kDown % 16u) * a.c.dim);
+        if (used[r] && p * 64u + c * 16u < a.c.dim)
+          codes[which][i] = *reinterpret_cast<const uint4*>(a.c.codes[which] + where[r] + (down % 16u) * a.c.dim + p * 64u);
       }
     };
     auto open = [&](uint32_t which, uint32_t to) {
 #pragma unroll
       for (uint32_t i = 0; i < S::kPieces; ++i) {
-        const uint32_t row = w * S::kOwn + row0 + i * S::kDown;
         const uint32_t* const x = &codes[which][i].x;
         uint32_t h[8];
 #pragma unroll
@@ -448,12 +471,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           h[2 * k] = open_low(u);
           h[2 * k + 1] = open_high(u);
         }
-        const uint32_t line = to + panel * S::kPanel + row * 128u, chunk = (2u * c) & 7u;
-        const uint32_t at0 = line + ((chunk + odd) ^ (row & 7u)) * 16u, at1 = line + ((chunk + 1u - odd) ^ (row & 7u)) * 16u;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at0), "r"(odd ? h[4] : h[0]), "r"(odd ? h[5] : h[1]),
-                     "r"(odd ? h[6] : h[2]), "r"(odd ? h[7] : h[3]) : "memory");
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at1), "r"(odd ? h[0] : h[4]), "r"(odd ? h[1] : h[5]),
-                     "r"(odd ? h[2] : h[6]), "r"(odd ? h[3] : h[7]) : "memory");
+        const uint32_t at = to + (i % S::kPanels) * S::kPanel + 8u * (i / S::kPanels) * 128u;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at + place0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(at + place1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
       }
     };
     ask(first);
@@ -522,11 +542,13 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
         }
         commit(me, s_full + 8 * h);
       };
-      auto outputs = [&](uint32_t h, uint32_t stage, bool more) {
-        const uint64_t dv = operand_across(v_at + stage * S::kTile, S::kPanel);
+      auto outputs = [&](uint32_t h, uint32_t part, uint32_t stage, bool more) {      // of half of the block's tokens
+        constexpr uint32_t kSteps = S::kTokens / 32;
+        const uint64_t dv = operand_across(v_at + stage * S::kTile, S::kPanel) + uint64_t(part * kSteps * 2048u >> 4);
+        const uint32_t p = tmem + S::kS + h * 128u + 8u * kSteps * part;
 #pragma unroll
-        for (uint32_t k = 0; k < S::kTokens / 16; ++k)
-          mma_tmem(me, tmem + S::kO + h * D, tmem + S::kS + h * 128u + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || k);
+        for (uint32_t k = 0; k < kSteps; ++k)
+          mma_tmem(me, tmem + S::kO + h * D, p + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || part || k);
       };
       for (uint32_t h = 0; h < S::kHalves; ++h)
         if (h >= halves) for (uint32_t i = 0; i < 4; ++i) { if (lane == 0) arrive(q_full); }            // a half without rows
@@ -542,9 +564,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
         bar_wait(v_full + 8 * stage, parity, bad);
         const uint32_t next = (n + 1) % S::kStages;
         for (uint32_t h = 0; h < halves; ++h) {
-          bar_wait(p_full + 8 * h, n & 1u, bad);
-          fence_after();
-          outputs(h, stage, n > 0);
+#pragma unroll
+          for (uint32_t part = 0; part < 2; ++part) {
+            bar_wait(p_full + 16 * h + 8 * part, n & 1u, bad);
+            fence_after();
+            outputs(h, part, stage, n > 0);
+          }
           if (h + 1 == halves) commit(me, v_empty + 8 * stage);
           if (n + 1 < blocks) {
             if (h == 0) bar_wait(k_full + 8 * next, ((n + 1) / S::kStages) & 1u, bad);
