@@ -27,6 +27,7 @@ struct AdArgs {
   uint64_t x_stride, y_stride, out_stride;
   uint32_t rows, n_seqs, count, rank, n_in, n_out;
   uint32_t b_wide, y_wide;           // four elements of B, eight of y and out can be accessed at once
+  uint32_t y_f32;                    // y and out in fp32, else bf16
   uint32_t* status;
 };
 
@@ -37,7 +38,9 @@ struct AdShape {
   static constexpr uint32_t kRows = 16 * MT;
   static constexpr uint32_t kSums = kRows * R;                       // of h
   static constexpr uint32_t kHRow = R + 8;                           // bf16 elements
-  static constexpr uint32_t kSmem = (kAdWarps + 1) * kSums * 4 + 2 * kRows * kHRow * 2;
+  // a warp's ring of groups of 32 outputs of y, on their way while h is made: four groups in bf16, two in fp32
+  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = (R == 64 && MT == 2 ? 2 : 4) * kGroup;
+  static constexpr uint32_t kSmem = (kAdWarps + 1) * kSums * 4 + 2 * kRows * kHRow * 2 + kAdWarps * kRing;
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -73,20 +76,20 @@ __device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, 
 }
 
 // R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each.
-template <int R, int MT, bool F8, bool YF32, bool VEC>
-__global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a) {
+template <int R, int MT, bool F8, bool VEC>
+__global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kernel(const AdArgs a) {
   using S = AdShape<R, MT>;
   using X = std::conditional_t<F8, uint8_t, uint16_t>;
-  using Y = std::conditional_t<YF32, float, __nv_bfloat16>;
   constexpr uint32_t kUnit = F8 ? 64 : 32, kLane = kUnit / 4, kSteps = kUnit / 16;     // inputs of a unit, of a lane, products
   constexpr int NT = R / 8, KT = R / 16;
-  constexpr int kAhead = MT * R <= 16 ? 4 : MT * R <= 64 ? 2 : 1;   // units whose loads are under way together
-  constexpr int kOuts = R == 16 ? 4 : R == 32 ? 2 : 1;               // groups of 32 outputs whose rows of B are loaded ahead
+  constexpr int kAhead = MT * R <= 16 ? (F8 ? 2 : 4) : MT * R <= 32 && !F8 ? 2 : 1;      // units whose loads are under way together
+  constexpr int kOuts = R == 16 ? (MT == 1 && !F8 ? 4 : 2) : 1;      // groups of 32 outputs whose rows of B are loaded ahead
   extern __shared__ __align__(16) uint8_t smem[];
   float* const parts = reinterpret_cast<float*>(smem);               // [warp][row][R]
   float* const mine = parts + kAdWarps * S::kSums;                   // [row][R], this block's part of the inputs
   __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(mine + S::kSums);
   __nv_bfloat16* const low = high + S::kRows * S::kHRow;
+  uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + (threadIdx.x >> 5) * S::kRing;
   __shared__ uint32_t s_seq;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
   uint32_t ranks;
@@ -96,12 +99,13 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
   wait_for_previous();
   // tiles: request s has starts[s] / rows + s and on, at least as many as it needs
   if (warp == 0) {
-    const uint32_t found = sequence_at(a.starts, a.n_seqs, S::kRows, 1u, tile);
+    const uint32_t found = sequence_at(a.starts, a.n_seqs, 1u, S::kRows, 1u, tile);
     if (lane == 0) s_seq = found;
   }
   __syncthreads();
   const uint32_t s = s_seq;
   const int32_t r0 = a.starts[s], r1 = a.starts[s + 1];
+  int32_t i = a.which[s];
   const bool fits = r0 >= 0 && r1 >= r0 && static_cast<uint32_t>(r1) <= a.rows;
   if (!fits && rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
   const uint32_t place = static_cast<uint32_t>(max(r0, 0)) / S::kRows + s;
@@ -109,7 +113,6 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
   const uint64_t begin = uint64_t(r0) + uint64_t(tile - place) * S::kRows;
   if (begin >= static_cast<uint32_t>(r1)) return;
   const uint32_t live = static_cast<uint32_t>(min(uint64_t(S::kRows), r1 - begin));
-  int32_t i = a.which[s];
   if (i >= 0 && static_cast<uint32_t>(i) >= a.count) {
     if (rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
     i = -1;
@@ -144,6 +147,22 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
       }
     }
   };
+  // groups of y: 16 bytes a lane and copy, a group ring slot a commit
+  const uint32_t y_size = a.y_f32 ? 4u : 2u, slots = S::kRing / (S::kGroup / 2 * y_size), in_row = 2u * y_size;       // pieces of a row
+  const uint8_t* const y = static_cast<const uint8_t*>(a.y) + begin * a.y_stride * y_size;
+  uint8_t* const out = static_cast<uint8_t*>(a.out) + begin * a.out_stride * y_size;
+  auto fetch_y = [&](uint32_t o, uint32_t slot) {
+    if (a.y_wide && o < o1)
+      for (uint32_t e = lane; e < live * in_row; e += 32) {
+        const uint32_t row = e / in_row, at = 32u * y_size * o + 16u * (e % in_row);
+        if (at + 16u <= a.n_out * y_size)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(smem_addr(ring) + slot * (S::kGroup / 2 * y_size) + e * 16u),
+                       "l"(y + row * a.y_stride * y_size + at) : "memory");
+      }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
+  const float scale = a.scales && !none ? a.scales[i] : 1.f;
   uint32_t bf[kOuts][4][KT][2];
 #pragma unroll
   for (int n = 0; n < kOuts; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
@@ -220,16 +239,17 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
       mine[e] = sum;
     }
     if (ranks > 1) cluster_sync(); else __syncthreads();
-    const float scale = a.scales ? a.scales[i] : 1.f;
     const uint32_t from = smem_addr(mine);
     for (uint32_t e = threadIdx.x; e < live * R; e += kAdThreads) {
-      float sum = 0.f;
-      for (uint32_t r = 0; r < ranks; ++r) {
-        float v;
-        asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
-                     : "=f"(v) : "r"(from + 4u * e), "r"(r) : "memory");
-        sum += v;
-      }
+      float v[8], sum = 0.f;                                         // of all blocks, at most 8, under way together
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r)
+        if (r < ranks)
+          asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
+                       : "=f"(v[r]) : "r"(from + 4u * e), "r"(r));
+#pragma unroll
+      for (uint32_t r = 0; r < 8; ++r)
+        if (r < ranks) sum += v[r];
       const uint32_t row = e / R, k = e % R;
       sum *= a.x_scales ? a.x_scales[begin + row] * scale : scale;
       const __nv_bfloat16 h = __float2bfloat16_rn(sum);
@@ -245,8 +265,7 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
     if (ranks > 1) cluster_arrive();                                 // this block has read the others' sums
   }
 
-  const Y* const y = static_cast<const Y*>(a.y) + begin * a.y_stride;
-  Y* const out = static_cast<Y*>(a.out) + begin * a.out_stride;
+  uint32_t slot = 0;
   for (uint32_t o = o0 + warp; o < o1; o += kAdWarps * kOuts) {
 #pragma unroll
     for (int n = 0; n < kOuts; ++n) {
@@ -254,6 +273,11 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
       if (now >= o1) break;
       const uint32_t at = 32u * now + 8u * t;                        // the lane's outputs: at .. at + 7
       const bool wide = a.y_wide && at + 8 <= a.n_out;
+      if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+      const uint8_t* const staged = ring + slot * (S::kGroup / 2 * y_size);
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         if (16u * m >= live) break;
@@ -261,16 +285,17 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t r = 16u * m + 8u * h + g;
-          const Y* const p = y + uint64_t(r) * a.y_stride + at;
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[h][k] = 0.f;
           if (r >= live) continue;
           if (wide) {
-            if constexpr (YF32) {
-              const float4 q = reinterpret_cast<const float4*>(p)[0], z = reinterpret_cast<const float4*>(p)[1];
-              v[h][0] = q.x; v[h][1] = q.y; v[h][2] = q.z; v[h][3] = q.w; v[h][4] = z.x; v[h][5] = z.y; v[h][6] = z.z; v[h][7] = z.w;
+            const uint4* const p = reinterpret_cast<const uint4*>(staged) + r * in_row + t * (in_row / 4u);
+            const uint4 q = p[0];
+            if (a.y_f32) {
+              const uint4 z = p[1];
+              v[h][0] = __uint_as_float(q.x); v[h][1] = __uint_as_float(q.y); v[h][2] = __uint_as_float(q.z); v[h][3] = __uint_as_float(q.w);
+              v[h][4] = __uint_as_float(z.x); v[h][5] = __uint_as_float(z.y); v[h][6] = __uint_as_float(z.z); v[h][7] = __uint_as_float(z.w);
             } else {
-              const uint4 q = *reinterpret_cast<const uint4*>(p);
               const uint32_t* const w = &q.x;
 #pragma unroll
               for (int k = 0; k < 4; ++k) {
@@ -279,9 +304,11 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
               }
             }
           } else {
+            const uint8_t* const p = y + (r * a.y_stride + at) * y_size;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              if (at + k < a.n_out) v[h][k] = static_cast<float>(p[k]);
+              if (at + k < a.n_out)
+                v[h][k] = a.y_f32 ? reinterpret_cast<const float*>(p)[k] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[k]);
           }
         }
         if (!none) {
@@ -308,10 +335,10 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t r = 16u * m + 8u * h + g;
-          Y* const p = out + uint64_t(r) * a.out_stride + at;
+          uint8_t* const p = out + (r * a.out_stride + at) * y_size;
           if (r >= live) continue;
           if (wide) {
-            if constexpr (YF32) {
+            if (a.y_f32) {
               reinterpret_cast<float4*>(p)[0] = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
               reinterpret_cast<float4*>(p)[1] = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
             } else {
@@ -322,45 +349,43 @@ __global__ void __launch_bounds__(kAdThreads) ans_adapters_kernel(const AdArgs a
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               if (at + k < a.n_out) {
-                if constexpr (YF32) p[k] = v[h][k]; else p[k] = __float2bfloat16_rn(v[h][k]);
+                if (a.y_f32) reinterpret_cast<float*>(p)[k] = v[h][k];
+                else reinterpret_cast<__nv_bfloat16*>(p)[k] = __float2bfloat16_rn(v[h][k]);
               }
           }
         }
       }
+      __syncwarp();
       load_b(now + kAdWarps * kOuts, bf[n]);
+      fetch_y(now + kAdWarps * slots, slot);
+      slot = slot + 1u == slots ? 0u : slot + 1u;
     }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
   if (!none && ranks > 1) cluster_wait();                            // nobody reads this block's sums any more
 }
 
-template <int R, int MT, bool F8, bool YF32>
-static int launch_adapters(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
+template <int R, int MT, bool F8, bool VEC>
+static int launch_adapters(const AdArgs& a, int sms, cudaStream_t st) {
   using S = AdShape<R, MT>;
   const uint64_t tiles = a.rows / S::kRows + a.n_seqs;
+  // Blocks of a tile: 8, but for single rows as many as have their places on the GPU at once, two an SM.
+  uint32_t ranks = 8;
+  while (MT == 1 && ranks > 1 && tiles * ranks > 2ull * sms) ranks /= 2;
   if (tiles * ranks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  const dim3 grid(static_cast<unsigned>(tiles * ranks));
-  if (vec) {
-    constexpr auto kernel = ans_adapters_kernel<R, MT, F8, YF32, true>;
-    const int rc = allow_smem<kernel>(S::kSmem);
-    return rc == ANS_OK ? launch(kernel, grid, dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
-  }
-  constexpr auto kernel = ans_adapters_kernel<R, MT, F8, YF32, false>;
+  constexpr auto kernel = ans_adapters_kernel<R, MT, F8, VEC>;
   const int rc = allow_smem<kernel>(S::kSmem);
-  return rc == ANS_OK ? launch(kernel, grid, dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
+  return rc == ANS_OK ? launch(kernel, dim3(static_cast<unsigned>(tiles * ranks)), dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
 }
 
-// Tiles of 16 rows where requests have about as many, else as many as registers hold the sums of.
-template <int R, bool F8, bool YF32>
-static int launch_rank(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
-  constexpr int kMost = R <= 32 ? 4 : R == 64 ? 2 : 1;
-  return uint64_t(a.rows) <= 16ull * a.n_seqs ? launch_adapters<R, 1, F8, YF32>(a, vec, ranks, st) : launch_adapters<R, kMost, F8, YF32>(a, vec, ranks, st);
-}
-template <bool F8, bool YF32>
-static int launch_types(const AdArgs& a, bool vec, uint32_t ranks, cudaStream_t st) {
-  if (a.rank <= 16) return launch_rank<16, F8, YF32>(a, vec, ranks, st);
-  if (a.rank <= 32) return launch_rank<32, F8, YF32>(a, vec, ranks, st);
-  if (a.rank <= 64) return launch_rank<64, F8, YF32>(a, vec, ranks, st);
-  return launch_rank<128, F8, YF32>(a, vec, ranks, st);
+// Tiles of 16 rows where requests have about as many, else of 32, if registers hold their sums.
+template <bool F8, bool VEC>
+static int launch_rank(const AdArgs& a, int sms, cudaStream_t st) {
+  const bool few = uint64_t(a.rows) <= 16ull * a.n_seqs;
+  if (a.rank <= 16) return few ? launch_adapters<16, 1, F8, VEC>(a, sms, st) : launch_adapters<16, 2, F8, VEC>(a, sms, st);
+  if (a.rank <= 32) return few ? launch_adapters<32, 1, F8, VEC>(a, sms, st) : launch_adapters<32, 2, F8, VEC>(a, sms, st);
+  if (a.rank <= 64) return few ? launch_adapters<64, 1, F8, VEC>(a, sms, st) : launch_adapters<64, 2, F8, VEC>(a, sms, st);
+  return launch_adapters<128, 1, F8, VEC>(a, sms, st);
 }
 
 }  // namespace blk
@@ -402,8 +427,11 @@ ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status,
                       (uint64_t(d.n_in) * xs)) & 15);
   a.b_wide = d.rank % 4 == 0 && !(reinterpret_cast<uintptr_t>(d.d_b) & 7);
   a.y_wide = !((reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_out) | (many * d.y_stride * ys) | (many * d.out_stride * ys)) & 15);
+  a.y_f32 = ys == 4;
+  int sms = 0;
+  const int asked = sm_count(&sms);
+  if (asked != ANS_OK) return asked;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  constexpr uint32_t ranks = 8;
-  if (d.x_dtype == ANS_E4M3) return ys == 4 ? launch_types<true, true>(a, vec, ranks, st) : launch_types<true, false>(a, vec, ranks, st);
-  return ys == 4 ? launch_types<false, true>(a, vec, ranks, st) : launch_types<false, false>(a, vec, ranks, st);
+  if (d.x_dtype == ANS_E4M3) return vec ? launch_rank<true, true>(a, sms, st) : launch_rank<true, false>(a, sms, st);
+  return vec ? launch_rank<false, true>(a, sms, st) : launch_rank<false, false>(a, sms, st);
 }

@@ -152,15 +152,8 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   // tiles: sequence s has starts[s] * share / rows + s and on; those that see most come first
   const uint32_t behind = blockIdx.x / a.c.heads, head = blockIdx.x - behind * a.c.heads, x = gridDim.x / a.c.heads - 1u - behind;
   if (warp == 0) {
-    uint32_t lo = 0, span = a.b.n_seqs;
-    while (span > 1) {
-      const uint32_t step = (span + 31u) / 32u, s = lo + lane * step, end = lo + span;
-      const bool before = s < end && static_cast<uint32_t>(max(a.b.starts[s], 0)) * uint64_t(a.share) / S::kRows + s <= x;
-      const uint32_t hits = __ballot_sync(kAll, before);
-      lo += (hits ? 31u - __clz(hits) : 0u) * step;
-      span = min(step, end - lo);
-    }
-    if (lane == 0) s_seq = lo;
+    const uint32_t found = sequence_at(a.b.starts, a.b.n_seqs, a.share, S::kRows, 1u, x);
+    if (lane == 0) s_seq = found;
   }
   fence_before();
   __syncthreads();

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   const uint32_t P = a.c.page_size, head = blockIdx.y, which = blockIdx.z, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   wait_for_previous();
   if (warp == 0) {
-    const uint32_t found = sequence_at(a.b.starts, a.b.n_seqs, P, 2u, blockIdx.x);
+    const uint32_t found = sequence_at(a.b.starts, a.b.n_seqs, 1u, P, 2u, blockIdx.x);
     if (lane == 0) s_seq = found;
   }
   __syncthreads();

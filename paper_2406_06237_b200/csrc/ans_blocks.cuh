@@ -38,18 +38,21 @@ __device__ __forceinline__ Range range_of(const Batch& b, uint32_t s) {
   return r;
 }
 
-// Of places dealt out so that sequence s has starts[s] / per + each * s and on: the sequence of place `at`, for a whole warp.
-__device__ __forceinline__ uint32_t sequence_at(const int32_t* starts, uint32_t n, uint32_t per, uint32_t each, uint32_t at) {
+// Of places dealt out so that sequence s has starts[s] / per + each * s and on (times `share` first): the sequence of place `at`, for a
+// whole warp.  All starts of up to 1024 sequences are asked for together: one trip to memory, where halving would take one a step.
+__device__ __forceinline__ uint32_t sequence_at(const int32_t* starts, uint32_t n, uint32_t share, uint32_t per, uint32_t each, uint32_t at) {
   const uint32_t lane = threadIdx.x & 31u;
-  uint32_t lo = 0, span = n;
-  while (span > 1) {                                   // 32 at a time
-    const uint32_t step = (span + 31u) / 32u, s = lo + lane * step, end = lo + span;
-    const bool before = s < end && static_cast<uint32_t>(max(starts[s], 0)) / per + each * s <= at;
-    const uint32_t hits = __ballot_sync(kAll, before);
-    lo += (hits ? 31u - __clz(hits) : 0u) * step;
-    span = min(step, end - lo);
+  uint32_t count = 0;                                  // of sequences that begin at or before the place: they come first
+  for (uint32_t s0 = 0; s0 < n; s0 += 1024) {
+    uint32_t here = 0;
+#pragma unroll 8
+    for (uint32_t s = s0 + lane; s < min(s0 + 1024u, n); s += 32)
+      here += static_cast<uint32_t>(uint64_t(max(starts[s], 0)) * share / per) + each * s <= at ? 1u : 0u;
+    here = __reduce_add_sync(kAll, here);
+    count += here;
+    if (here < min(1024u, n - s0)) break;
   }
-  return lo;
+  return count ? count - 1u : 0u;
 }
 
 // Four codes in a word, opened to two pairs of fp16: 0x6400 | u is 1024 + u, u = code + 128.
