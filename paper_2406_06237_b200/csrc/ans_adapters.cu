@@ -15,32 +15,19 @@
 #include <algorithm>
 #include <initializer_list>
 
-#include "ans_blocks.cuh"
+#include "ans_adapters.cuh"
 
 namespace ansb {
 namespace blk {
-
-struct AdArgs {
-  const uint8_t* x; const float* x_scales; const void* y; void* out;
-  const __nv_bfloat16* a; const __nv_bfloat16* b; const float* scales;
-  const int32_t* which; const int32_t* starts;
-  uint64_t x_stride, y_stride, out_stride;
-  uint32_t rows, n_seqs, count, rank, n_in, n_out;
-  uint32_t b_wide, y_wide;           // four elements of B, eight of y and out can be accessed at once
-  uint32_t y_f32;                    // y and out in fp32, else bf16
-  uint32_t* status;
-};
-
-constexpr uint32_t kAdWarps = 8, kAdThreads = 32 * kAdWarps;
 
 template <int R, int MT>
 struct AdShape {
   static constexpr uint32_t kRows = 16 * MT;
   static constexpr uint32_t kSums = kRows * R;                       // of h
-  static constexpr uint32_t kHRow = R + 8;                           // bf16 elements
-  // a warp's ring of groups of 32 outputs of y, on their way while h is made: four groups in bf16, two in fp32
-  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = (R == 64 && MT == 2 ? 2 : 4) * kGroup;
-  static constexpr uint32_t kSmem = (kAdWarps + 1) * kSums * 4 + 2 * kRows * kHRow * 2 + kAdWarps * kRing;
+  static constexpr uint32_t kHRow = R + 8, kPart = kRows * (R + 8);  // elements of a row of h, of a warp's sums; + 8: eight rows in different banks
+  // a warp's ring of groups of 32 outputs of y, on their way while h is made: up to four groups in bf16, half as many in fp32
+  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = (MT == 1 ? 4 : R == 64 ? 2 : 3) * kGroup;
+  static constexpr uint32_t kSmem = (kAdWarps * kPart + kSums + kRows) * 4 + 2 * kRows * kHRow * 2 + kAdWarps * kRing;
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -86,8 +73,9 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
   constexpr int kOuts = R == 16 ? (MT == 1 && !F8 ? 4 : 2) : 1;      // groups of 32 outputs whose rows of B are loaded ahead
   extern __shared__ __align__(16) uint8_t smem[];
   float* const parts = reinterpret_cast<float*>(smem);               // [warp][row][R]
-  float* const mine = parts + kAdWarps * S::kSums;                   // [row][R], this block's part of the inputs
-  __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(mine + S::kSums);
+  float* const mine = parts + kAdWarps * S::kPart;                   // [row][R], this block's part of the inputs
+  float* const factor = mine + S::kSums;                             // [row]
+  __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(factor + S::kRows);
   __nv_bfloat16* const low = high + S::kRows * S::kHRow;
   uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + (threadIdx.x >> 5) * S::kRing;
   __shared__ uint32_t s_seq;
@@ -124,45 +112,54 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
   const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * rank / ranks), o1 = static_cast<uint32_t>(uint64_t(groups) * (rank + 1u) / ranks);
   // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
   // elements t R / 4 + 4 k and on of a row
+  const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4);
+  const __nv_bfloat16* const b_lane = a.b + (uint64_t(max(i, 0)) * a.n_out + b_out) * a.rank + b_in;
   auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
+    const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * a.rank);
+    const uint32_t left = o < o1 && !none ? a.n_out - 32u * o : 0u;  // outputs from the group's first on
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) {
-      const uint32_t out = 32u * o + 8u * (g >> 1) + 2u * j + (g & 1u);
-      const __nv_bfloat16* const row = a.b + (uint64_t(max(i, 0)) * a.n_out + min(out, a.n_out - 1u)) * a.rank;
+      const __nv_bfloat16* const row = rows + 2u * j * a.rank;
+      const bool in = b_out + 2u * j < left;
 #pragma unroll
       for (uint32_t k = 0; k < KT; ++k) {
-        const uint32_t e = t * (R / 4) + 4u * k;
         f[j][k][0] = f[j][k][1] = 0u;
-        if (none || o >= o1 || out >= a.n_out) continue;
         if (a.b_wide) {
-          if (e < a.rank) {
-            const uint2 u = *reinterpret_cast<const uint2*>(row + e);
+          if (in && b_in + 4u * k < a.rank) {
+            const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
             f[j][k][0] = u.x; f[j][k][1] = u.y;
           }
         } else {
 #pragma unroll
           for (uint32_t h = 0; h < 4; ++h)
-            if (e + h < a.rank) f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[e + h]) << (16 * (h % 2));
+            if (in && b_in + 4u * k + h < a.rank)
+              f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[4u * k + h]) << (16 * (h % 2));
         }
       }
     }
   };
   // groups of y: 16 bytes a lane and copy, a group ring slot a commit
-  const uint32_t y_size = a.y_f32 ? 4u : 2u, slots = S::kRing / (S::kGroup / 2 * y_size), in_row = 2u * y_size;       // pieces of a row
+  const uint32_t y_shift = a.y_f32 ? 3u : 2u, y_size = a.y_f32 ? 4u : 2u;        // 2^y_shift pieces of 16 bytes a row
+  const uint32_t slot_bytes = S::kRows << (y_shift + 4u), slots = S::kRing / slot_bytes;
   const uint8_t* const y = static_cast<const uint8_t*>(a.y) + begin * a.y_stride * y_size;
   uint8_t* const out = static_cast<uint8_t*>(a.out) + begin * a.out_stride * y_size;
+  const uint32_t y_row = lane >> y_shift, y_at = 16u * (lane & ((1u << y_shift) - 1u)), y_down = 32u >> y_shift;
+  const uint8_t* const y_lane = y + y_row * a.y_stride * y_size + y_at;
+  const uint32_t ring_lane = smem_addr(ring) + lane * 16u;
   auto fetch_y = [&](uint32_t o, uint32_t slot) {
-    if (a.y_wide && o < o1)
-      for (uint32_t e = lane; e < live * in_row; e += 32) {
-        const uint32_t row = e / in_row, at = 32u * y_size * o + 16u * (e % in_row);
-        if (at + 16u <= a.n_out * y_size)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(smem_addr(ring) + slot * (S::kGroup / 2 * y_size) + e * 16u),
-                       "l"(y + row * a.y_stride * y_size + at) : "memory");
-      }
+    if (a.y_wide && o < o1 && uint64_t(32u * y_size) * o + y_at + 16u <= uint64_t(a.n_out) * y_size) {
+      const uint8_t* from = y_lane + uint64_t(32u * y_size) * o;
+      uint32_t to = ring_lane + slot * slot_bytes;
+      for (uint32_t row = y_row; row < live; row += y_down, from += y_down * a.y_stride * y_size, to += 512u)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+    }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  if (threadIdx.x < S::kRows && !none) {
+    const float scale = a.scales ? a.scales[i] : 1.f;
+    factor[threadIdx.x] = a.x_scales && threadIdx.x < live ? a.x_scales[begin + threadIdx.x] * scale : scale;
+  }
   for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
-  const float scale = a.scales && !none ? a.scales[i] : 1.f;
   uint32_t bf[kOuts][4][KT][2];
 #pragma unroll
   for (int n = 0; n < kOuts; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
@@ -175,8 +172,12 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
       for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
     const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
     const uint32_t u0 = static_cast<uint32_t>(uint64_t(units) * rank / ranks), u1 = static_cast<uint32_t>(uint64_t(units) * (rank + 1u) / ranks);
-    const X* const x = reinterpret_cast<const X*>(a.x) + begin * a.x_stride;
-    const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + uint64_t(i) * a.rank * a.n_in;
+    const X* x[MT][2];                                               // the lane's rows
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (uint32_t h = 0; h < 2; ++h) x[m][h] = reinterpret_cast<const X*>(a.x) + (begin + min(16u * m + 8u * h + g, live - 1u)) * a.x_stride;
+    const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + (uint64_t(i) * a.rank + min(g, a.rank - 1u)) * a.n_in;
     for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
       uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
 #pragma unroll
@@ -187,14 +188,11 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (uint32_t h = 0; h < kLane / 8; ++h)
-            af[k][n][h] = piece_of<uint16_t, VEC>(down + uint64_t(min(8u * n + g, a.rank - 1u)) * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
+            af[k][n][h] = piece_of<uint16_t, VEC>(down + 8u * n * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) {
-            const uint32_t r = 16u * m + 8u * h + g;
-            xf[k][m][h] = piece_of<X, VEC>(x + min(r, live - 1u) * a.x_stride, e, a.n_in, in && r < live);
-          }
+          for (uint32_t h = 0; h < 2; ++h) xf[k][m][h] = piece_of<X, VEC>(x[m][h], e, a.n_in, in && 16u * m + 8u * h + g < live);
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k)
@@ -223,43 +221,51 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
           }
         }
     }
-    float* const to = parts + warp * S::kSums;
+    float* const to = parts + warp * S::kPart;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        *reinterpret_cast<float2*>(to + (16 * m + g) * R + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
-        *reinterpret_cast<float2*>(to + (16 * m + g + 8) * R + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
+        *reinterpret_cast<float2*>(to + (16 * m + g) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
+        *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
       }
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < S::kSums; e += kAdThreads) {
+    constexpr uint32_t kEach = S::kSums / kAdThreads;                // sums of a thread
+    static_assert(S::kSums % kAdThreads == 0, "");
+#pragma unroll
+    for (uint32_t n = 0; n < kEach; ++n) {
+      const uint32_t e = threadIdx.x + n * kAdThreads;
       float sum = 0.f;
 #pragma unroll
-      for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kSums + e];
+      for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
       mine[e] = sum;
     }
     if (ranks > 1) cluster_sync(); else __syncthreads();
-    const uint32_t from = smem_addr(mine);
-    for (uint32_t e = threadIdx.x; e < live * R; e += kAdThreads) {
-      float v[8], sum = 0.f;                                         // of all blocks, at most 8, under way together
+    const uint32_t from = smem_addr(mine) + 4u * threadIdx.x;
+    constexpr uint32_t kBatch = kEach < 4 ? kEach : 4;
+#pragma unroll 1
+    for (uint32_t n0 = 0; n0 < kEach; n0 += kBatch) {
+      float v[kBatch][8];                                            // of all blocks, at most 8, under way together
 #pragma unroll
       for (uint32_t r = 0; r < 8; ++r)
-        if (r < ranks)
-          asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
-                       : "=f"(v[r]) : "r"(from + 4u * e), "r"(r));
 #pragma unroll
-      for (uint32_t r = 0; r < 8; ++r)
-        if (r < ranks) sum += v[r];
-      const uint32_t row = e / R, k = e % R;
-      sum *= a.x_scales ? a.x_scales[begin + row] * scale : scale;
-      const __nv_bfloat16 h = __float2bfloat16_rn(sum);
-      const float rest = sum - __bfloat162float(h);
-      high[row * S::kHRow + k] = h;
-      low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
-    }
-    for (uint32_t e = live * R + threadIdx.x; e < S::kSums; e += kAdThreads) {
-      high[(e / R) * S::kHRow + e % R] = __float2bfloat16_rn(0.f);
-      low[(e / R) * S::kHRow + e % R] = __float2bfloat16_rn(0.f);
+        for (uint32_t n = 0; n < kBatch; ++n)
+          if (r < ranks)
+            asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
+                         : "=f"(v[n][r]) : "r"(from + (n0 + n) * (4u * kAdThreads)), "r"(r));
+#pragma unroll
+      for (uint32_t n = 0; n < kBatch; ++n) {
+        const uint32_t e = threadIdx.x + (n0 + n) * kAdThreads, row = e / R, k = e % R;
+        float sum = 0.f;
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r)
+          if (r < ranks) sum += v[n][r];
+        sum = row < live ? sum * factor[row] : 0.f;
+        const __nv_bfloat16 h = __float2bfloat16_rn(sum);
+        const float rest = sum - __bfloat162float(h);
+        high[row * S::kHRow + k] = h;
+        low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
+      }
     }
     __syncthreads();
     if (ranks > 1) cluster_arrive();                                 // this block has read the others' sums
@@ -274,10 +280,11 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
       const uint32_t at = 32u * now + 8u * t;                        // the lane's outputs: at .. at + 7
       const bool wide = a.y_wide && at + 8 <= a.n_out;
       if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (slots == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
       else if (slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
       else asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncwarp();
-      const uint8_t* const staged = ring + slot * (S::kGroup / 2 * y_size);
+      const uint8_t* const staged = ring + slot * slot_bytes;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         if (16u * m >= live) break;
@@ -289,7 +296,7 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
           for (int k = 0; k < 8; ++k) v[h][k] = 0.f;
           if (r >= live) continue;
           if (wide) {
-            const uint4* const p = reinterpret_cast<const uint4*>(staged) + r * in_row + t * (in_row / 4u);
+            const uint4* const p = reinterpret_cast<const uint4*>(staged) + ((r * 4u + t) << (y_shift - 2u));
             const uint4 q = p[0];
             if (a.y_f32) {
               const uint4 z = p[1];
@@ -425,6 +432,7 @@ ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status,
   const uint64_t many = d.rows > 1;
   const bool vec = !((reinterpret_cast<uintptr_t>(d.d_x) | (many * d.x_stride * xs) | reinterpret_cast<uintptr_t>(d.d_a) | (uint64_t(d.n_in) * 2) |
                       (uint64_t(d.n_in) * xs)) & 15);
+  a.b_run = !((reinterpret_cast<uintptr_t>(d.d_b) | (uint64_t(d.n_out) * d.rank * 2)) & 15);
   a.b_wide = d.rank % 4 == 0 && !(reinterpret_cast<uintptr_t>(d.d_b) & 7);
   a.y_wide = !((reinterpret_cast<uintptr_t>(d.d_y) | reinterpret_cast<uintptr_t>(d.d_out) | (many * d.y_stride * ys) | (many * d.out_stride * ys)) & 15);
   a.y_f32 = ys == 4;
@@ -432,6 +440,7 @@ ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status,
   const int asked = sm_count(&sms);
   if (asked != ANS_OK) return asked;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (d.rows <= d.n_seqs) return launch_adapters_rows(a, d.x_dtype == ANS_E4M3, vec, sms, st);
   if (d.x_dtype == ANS_E4M3) return vec ? launch_rank<true, true>(a, sms, st) : launch_rank<true, false>(a, sms, st);
   return vec ? launch_rank<false, true>(a, sms, st) : launch_rank<false, false>(a, sms, st);
 }
