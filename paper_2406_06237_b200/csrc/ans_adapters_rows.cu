@@ -35,12 +35,43 @@ __device__ __forceinline__ uint4 eight_of(const uint16_t* p, uint32_t e, uint32_
   return w;
 }
 
+// The lane's output of a group of 32: rows of B of P pieces of 16 bytes lie one after the other, a lane takes piece lane % P of the rows
+// lane / P + 32 / P j, in the order in which they lie, and the P lanes of a row exchange their sums until each has a row's.
+template <uint32_t P>
+__device__ __forceinline__ float across(const uint8_t* rows, uint32_t lane, const float (&hp)[8]) {
+  float sum[P];
+#pragma unroll
+  for (uint32_t j = 0; j < P; ++j) {
+    float z[8];
+    open8(*reinterpret_cast<const uint4*>(rows + lane * 16u + j * 512u), z);
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; n += 2) {
+      s = fmaf(hp[n], z[n], s);
+      u = fmaf(hp[n + 1], z[n + 1], u);
+    }
+    sum[j] = s + u;
+  }
+#pragma unroll
+  for (uint32_t n = P / 2; n >= 1; n /= 2)             // lane bit n: which half of the rows it goes on with
+#pragma unroll
+    for (uint32_t k = 0; k < n; ++k) {
+      const bool up = lane & n;
+      const float give = up ? sum[k] : sum[k + n], keep = up ? sum[k + n] : sum[k];
+      sum[k] = keep + __shfl_xor_sync(kAll, give, n);
+    }
+  // lane l has row l / P + 32 / P (l % P): its own output's is with lane (l % (32 / P)) P + l / (32 / P)
+  return P == 1 ? sum[0] : __shfl_sync(kAll, sum[0], (lane % (32u / P)) * P + lane / (32u / P));
+}
+
 template <bool F8, bool VEC>
 __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_rows_kernel(const AdArgs a) {
   constexpr uint32_t kUnit = 256, kRows = 16;          // inputs of a warp, rows of A at a time
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float parts[kAdWarps][128], mine[128];
   __shared__ __align__(16) float h[128];
+  constexpr uint32_t kYs = 8;
+  __shared__ uint32_t ahead[kYs][kAdThreads];          // y of a warp's next groups, of each lane its own
   __shared__ uint32_t s_seq;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   uint32_t ranks;
@@ -95,6 +126,18 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_rows_kernel(const 
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   for (uint32_t n = 0; n < slots; ++n) fetch(o0 + warp + kAdWarps * n, n);
+  // y of the lane's output in a warp's next kYs groups
+  const uint32_t size = a.y_f32 ? 4u : 2u;
+  const uint8_t* const y = static_cast<const uint8_t*>(a.y) + row * a.y_stride * size;
+  uint8_t* const out = static_cast<uint8_t*>(a.out) + row * a.out_stride * size;
+  uint32_t ys[kYs];
+  auto y_of = [&](uint32_t o) {
+    const uint32_t at = 32u * o + lane;
+    if (o >= o1 || at >= a.n_out) return 0u;
+    return a.y_f32 ? reinterpret_cast<const uint32_t*>(y)[at] : static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(y)[at]);
+  };
+#pragma unroll
+  for (uint32_t n = 0; n < kYs; ++n) ys[n] = y_of(o0 + warp + kAdWarps * n);
 
   if (!none) {
     const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
@@ -181,45 +224,53 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_rows_kernel(const 
     if (ranks > 1) cluster_arrive();                                 // this block has read the others' sums
   }
 
-  const uint32_t size = a.y_f32 ? 4u : 2u;
-  const uint8_t* const y = static_cast<const uint8_t*>(a.y) + row * a.y_stride * size;
-  uint8_t* const out = static_cast<uint8_t*>(a.out) + row * a.out_stride * size;
+  const uint32_t pieces = a.rank % 8 == 0 ? a.rank / 8u : 0u;
+  float hp[8];                                         // of the lane's piece
+#pragma unroll
+  for (uint32_t k = 0; k < 8; ++k) hp[k] = none || !pieces ? 0.f : h[(lane % pieces) * 8u + k];
   uint32_t slot = 0;
-  for (uint32_t o = o0 + warp; o < o1; o += kAdWarps) {
-    const uint32_t at = 32u * o + lane;
-    const bool in = at < a.n_out;
-    float v = 0.f;
-    if (in) v = a.y_f32 ? reinterpret_cast<const float*>(y)[at] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(y)[at]);
-    // all but the slots behind this one may be on their way: waits for a few are kinds of instruction
-    if (slots >= 8) asm volatile("cp.async.wait_group 7;" ::: "memory");
-    else if (slots >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-    else if (slots >= 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncwarp();
-    if (!none && in) {
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-      const uint16_t* const p = staged ? reinterpret_cast<const uint16_t*>(ring + slot * bytes) + lane * a.rank
-                                       : reinterpret_cast<const uint16_t*>(b) + uint64_t(at) * a.rank;
-      if (staged && a.rank % 8 == 0) {
-        for (uint32_t k = 0; k < a.rank; k += 8) {
-          float z[8];
-          open8(*reinterpret_cast<const uint4*>(p + k), z);
-          const float4 ha = *reinterpret_cast<const float4*>(h + k), hb = *reinterpret_cast<const float4*>(h + k + 4);
-          sum[0] = fmaf(ha.x, z[0], sum[0]); sum[1] = fmaf(ha.y, z[1], sum[1]); sum[2] = fmaf(ha.z, z[2], sum[2]); sum[3] = fmaf(ha.w, z[3], sum[3]);
-          sum[0] = fmaf(hb.x, z[4], sum[0]); sum[1] = fmaf(hb.y, z[5], sum[1]); sum[2] = fmaf(hb.z, z[6], sum[2]); sum[3] = fmaf(hb.w, z[7], sum[3]);
-        }
-      } else {
-        for (uint32_t k = 0; k < a.rank; ++k) sum[0] = fmaf(h[k], __uint_as_float(static_cast<uint32_t>(p[k]) << 16), sum[0]);
+  for (uint32_t first = o0 + warp; first < o1; first += kAdWarps * kYs) {
+#pragma unroll
+    for (uint32_t n = 0; n < kYs; ++n) ahead[n][threadIdx.x] = ys[n];
+#pragma unroll
+    for (uint32_t n = 0; n < kYs; ++n) ys[n] = y_of(first + kAdWarps * (kYs + n));
+#pragma unroll 1                                                     // short code: most of it runs once a block, out of a cold instruction cache
+    for (uint32_t n = 0; n < kYs; ++n) {
+      const uint32_t o = first + kAdWarps * n, at = 32u * o + lane;
+      if (o >= o1) break;
+      const bool in = at < a.n_out;
+      float v = a.y_f32 ? __uint_as_float(ahead[n][threadIdx.x]) : __uint_as_float(ahead[n][threadIdx.x] << 16);
+      // all but the slots behind this one may be on their way: waits for a few are kinds of instruction
+      if (slots >= 8) asm volatile("cp.async.wait_group 7;" ::: "memory");
+      else if (slots >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (slots >= 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+      const uint8_t* const rows = ring + slot * bytes;
+      if (none) {
+      } else if (staged && pieces == 1) {
+        v += across<1>(rows, lane, hp);
+      } else if (staged && pieces == 2) {
+        v += across<2>(rows, lane, hp);
+      } else if (staged && pieces == 4) {
+        v += across<4>(rows, lane, hp);
+      } else if (staged && pieces == 8) {
+        v += across<8>(rows, lane, hp);
+      } else if (in) {
+        const uint16_t* const far = reinterpret_cast<const uint16_t*>(b) + uint64_t(at) * a.rank;
+        const uint16_t* const near = reinterpret_cast<const uint16_t*>(rows) + lane * a.rank;
+        float sum = 0.f;
+        for (uint32_t k = 0; k < a.rank; ++k) sum = fmaf(h[k], __uint_as_float(static_cast<uint32_t>(staged ? near[k] : far[k]) << 16), sum);
+        v += sum;
       }
-      v += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (in) {
+        if (a.y_f32) reinterpret_cast<float*>(out)[at] = v;
+        else reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
+      }
+      __syncwarp();
+      fetch(o + kAdWarps * slots, slot);
+      slot = slot + 1u == slots ? 0u : slot + 1u;
     }
-    if (in) {
-      if (a.y_f32) reinterpret_cast<float*>(out)[at] = v;
-      else reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
-    }
-    __syncwarp();
-    fetch(o + kAdWarps * slots, slot);
-    slot = slot + 1u == slots ? 0u : slot + 1u;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   if (!none && ranks > 1) cluster_wait();                            // nobody reads this block's sums any more
