@@ -592,7 +592,8 @@ int ans_page_tables(const ans_pages_desc* h_desc, uint32_t* d_status, void* stre
  * Low-rank adapters of many requests beside a projection that they share:
  *   out[t][:] = y[t][:] + scales[i] * x_scales[t] * (x[t][:] A_i^T) B_i^T,   i = d_which[s] of row t's request s,
  * A_i = d_a[i] (rank x n_in), B_i = d_b[i] (n_out x rank), bf16, contiguous.  i < 0: no adapter, out = y; i >= count: the same, and
- * flagged ANS_STATUS_BAD_PAGE.  Sums in fp32; x A^T meets B as a sum of two bf16 numbers (2^-17 of it); one rounding at the end.
+ * flagged ANS_STATUS_BAD_PAGE, as are rows that do not fit.  Sums in fp32; with more rows than requests x A^T meets B as a sum of two bf16
+ * numbers (within 2^-17 of it); one rounding at the end.
  * d_out may be d_y (same stride).  x: ANS_BF16, or ANS_E4M3 with d_x_scales (or NULL: ones).  rank <= 128.  Any alignment;
  * the fast path wants d_x, d_a and their rows on 16 bytes.
  */
@@ -603,7 +604,9 @@ typedef struct ans_adapters_desc {
   uint64_t x_stride, y_stride, out_stride;
   uint32_t rows, n_seqs, count, rank, n_in, n_out;
   int32_t x_dtype, y_dtype;                                       /* y: ANS_BF16 or ANS_F32            */
+  void* d_room; uint64_t room_bytes;                              /* 16-byte aligned, ans_adapters_room_bytes() (0: none), free again after the call's work */
 } ans_adapters_desc;
+int ans_adapters_room_bytes(const ans_adapters_desc* h_desc, size_t* h_bytes_out);
 int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status, void* stream);
 
 /*

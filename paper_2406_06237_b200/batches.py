@@ -134,8 +134,12 @@ class Adapters(_Handle):
         if at is None:
             self._form.keep()
             self._check(x, x_scales, y, out, which, starts)
+            d.d_room, d.room_bytes = None, B.ans_adapters_room_bytes(d)
             self._form.keep(x, x_scales, y, out, which, starts)
             at = self._form.places(x, x_scales, y, out, which, starts)
+        if d.room_bytes:
+            room = torch.empty(d.room_bytes, dtype=torch.uint8, device=self.device)        # kept until the call is queued
+            d.d_room = room.data_ptr()
         d.d_x, d.d_x_scales, d.d_y, d.d_out, d.d_which, d.d_starts = at
         B.ans_adapters(d, self._status, st)
         return out

@@ -38,7 +38,7 @@ EXPORTS = [
     "ans_encode_scratch_bytes", "ans_encode_layer_device", "ans_encode_channels_device", "ans_encode_quads_device",
     "ans_decode_gemm_bf16",
     "ans_rms_norm", "ans_product", "ans_product_room_bytes", "ans_product_rows", "ans_product_form", "ans_cache_write", "ans_cache_read",
-    "ans_page_tables", "ans_adapters", "ans_block_cache_write", "ans_attend", "ans_attend_room_bytes",
+    "ans_page_tables", "ans_adapters", "ans_adapters_room_bytes", "ans_block_cache_write", "ans_attend", "ans_attend_room_bytes",
 ]
 
 
@@ -104,6 +104,7 @@ class ans_adapters_desc(ctypes.Structure):
         ("x_stride", ctypes.c_uint64), ("y_stride", ctypes.c_uint64), ("out_stride", ctypes.c_uint64),
         ("rows", ctypes.c_uint32), ("n_seqs", ctypes.c_uint32), ("count", ctypes.c_uint32), ("rank", ctypes.c_uint32),
         ("n_in", ctypes.c_uint32), ("n_out", ctypes.c_uint32), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
+        ("d_room", ctypes.c_void_p), ("room_bytes", ctypes.c_uint64),
     ]
 
 
@@ -190,6 +191,7 @@ def lib():
         L.ans_cache_read.argtypes = [P(ans_cache_desc), vp, u64, u32, u32, vp, u64, vp, vp, i32, vp, vp]
         L.ans_page_tables.argtypes = [P(ans_pages_desc), vp, vp]
         L.ans_adapters.argtypes = [P(ans_adapters_desc), vp, vp]
+        L.ans_adapters_room_bytes.argtypes = [P(ans_adapters_desc), P(sz)]
         L.ans_block_cache_write.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), vp, vp, i32, u64, u64, u64, u64, vp, vp]
         L.ans_attend.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), P(ans_attend_desc), vp, vp]
         L.ans_attend_room_bytes.argtypes = [P(ans_block_cache_desc), P(ans_batch_desc), P(ans_attend_desc), P(sz)]
@@ -465,6 +467,12 @@ def ans_adapters(h_desc: ans_adapters_desc, d_status: int, stream: int = 0) -> N
     rc = (_LIB or lib()).ans_adapters(h_desc, d_status, stream)
     if rc:
         _check(rc, "ans_adapters")
+
+
+def ans_adapters_room_bytes(h_desc: ans_adapters_desc) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().ans_adapters_room_bytes(h_desc, ctypes.byref(out)), "ans_adapters_room_bytes")
+    return out.value
 
 
 def ans_block_cache_write(h_cache: ans_block_cache_desc, h_batch: ans_batch_desc, d_k: int, d_v: int, dtype: int, k_strides, v_strides,

@@ -1,12 +1,13 @@
 // Low-rank adapters of many requests beside a projection that they share:
 //   out[t] = y[t] + scales[i] * x_scales[t] * (x[t] A_i^T) B_i^T,   i the adapter of row t's request.
 //
-// A cluster of blocks has a tile of rows of one request.  Each block sums its part of the inputs, h = x A^T (rows x rank, mma.sync,
-// fp32), the blocks exchange their sums through distributed shared memory, added in the order of the ranks, and each goes on with
-// its part of the outputs: one launch, no workspace, A, B, x and y read once.  B's first rows are under way while A's are summed.
-// With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64 rows: bound by the bytes, so the plain
+// For more rows than requests two kernels, both over tiles of 16 or 32 rows of one request: the first sums h = x A^T (mma.sync, fp32) over a
+// part of the inputs, up to eight parts a tile, into the caller's room; the second adds the parts in their order and streams y through the product
+// with B.  With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64 rows: bound by the bytes, so the plain
 // matrix instructions are enough.  h meets B as the sum of two bf16 numbers, h = hi + lo, |h - hi - lo| <= 2^-17 |h|: a second
-// product, which costs less than the rounding of h to 8 bits would lose.
+// product, which costs less than the rounding of h to 8 bits would lose.  One kernel with a cluster a tile, whose blocks exchange h
+// through shared memory, took 118 us where these take 91 (5005 rows of 8192 in e4m3, rank 32, 8192 outputs): 54 us of it were the
+// blocks' starts, barriers and exchanges, eight times as many as there are tiles.
 //
 // The order of the inputs in a product is free, so a lane takes 16 bytes of a row at once; the columns of a product with B stand
 // for outputs such that a lane has 8 neighbouring ones.
@@ -25,9 +26,10 @@ struct AdShape {
   static constexpr uint32_t kRows = 16 * MT;
   static constexpr uint32_t kSums = kRows * R;                       // of h
   static constexpr uint32_t kHRow = R + 8, kPart = kRows * (R + 8);  // elements of a row of h, of a warp's sums; + 8: eight rows in different banks
-  // a warp's ring of groups of 32 outputs of y, on their way while h is made: up to four groups in bf16, half as many in fp32
-  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = (MT == 1 ? 4 : R == 64 ? 2 : 3) * kGroup;
-  static constexpr uint32_t kSmem = (kAdWarps * kPart + kSums + kRows) * 4 + 2 * kRows * kHRow * 2 + kAdWarps * kRing;
+  static constexpr uint32_t kDownSmem = kAdWarps * kPart * 4;
+  // a warp's ring of groups of 32 outputs of y: four groups in bf16, two in fp32
+  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = 4 * kGroup;
+  static constexpr uint32_t kUpSmem = 2 * kRows * kHRow * 2 + kAdWarps * kRing;
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -62,54 +64,155 @@ __device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, 
   return v;
 }
 
-// R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each.
-template <int R, int MT, bool F8, bool VEC>
-__global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kernel(const AdArgs a) {
-  using S = AdShape<R, MT>;
-  using X = std::conditional_t<F8, uint8_t, uint16_t>;
-  constexpr uint32_t kUnit = F8 ? 64 : 32, kLane = kUnit / 4, kSteps = kUnit / 16;     // inputs of a unit, of a lane, products
-  constexpr int NT = R / 8, KT = R / 16;
-  constexpr int kAhead = MT * R <= 16 ? (F8 ? 2 : 4) : MT * R <= 32 && !F8 ? 2 : 1;      // units whose loads are under way together
-  constexpr int kOuts = R == 16 ? (MT == 1 && !F8 ? 4 : 2) : 1;      // groups of 32 outputs whose rows of B are loaded ahead
-  extern __shared__ __align__(16) uint8_t smem[];
-  float* const parts = reinterpret_cast<float*>(smem);               // [warp][row][R]
-  float* const mine = parts + kAdWarps * S::kPart;                   // [row][R], this block's part of the inputs
-  float* const factor = mine + S::kSums;                             // [row]
-  __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(factor + S::kRows);
-  __nv_bfloat16* const low = high + S::kRows * S::kHRow;
-  uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + (threadIdx.x >> 5) * S::kRing;
+// A tile of rows: tile numbers are dealt so that request s has starts[s] / rows + s and on, at least as many as it needs.
+struct AdTile {
+  uint64_t begin;                    // first row
+  uint32_t live;                     // rows; 0: none
+  int32_t which;                     // adapter, negative: none
+};
+template <uint32_t ROWS>
+__device__ __forceinline__ AdTile ad_tile(const AdArgs& a, uint32_t tile, bool tell) {
   __shared__ uint32_t s_seq;
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
-  uint32_t ranks;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
-  const uint32_t rank = cluster_rank(), tile = blockIdx.x / ranks;
-  let_next_start();
-  wait_for_previous();
-  // tiles: request s has starts[s] / rows + s and on, at least as many as it needs
-  if (warp == 0) {
-    const uint32_t found = sequence_at(a.starts, a.n_seqs, 1u, S::kRows, 1u, tile);
-    if (lane == 0) s_seq = found;
+  if (threadIdx.x < 32) {
+    const uint32_t found = sequence_at(a.starts, a.n_seqs, 1u, ROWS, 1u, tile);
+    if (threadIdx.x == 0) s_seq = found;
   }
   __syncthreads();
   const uint32_t s = s_seq;
   const int32_t r0 = a.starts[s], r1 = a.starts[s + 1];
-  int32_t i = a.which[s];
-  const bool fits = r0 >= 0 && r1 >= r0 && static_cast<uint32_t>(r1) <= a.rows;
-  if (!fits && rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-  const uint32_t place = static_cast<uint32_t>(max(r0, 0)) / S::kRows + s;
-  if (!fits || tile < place) return;                                 // the same for the whole cluster
-  const uint64_t begin = uint64_t(r0) + uint64_t(tile - place) * S::kRows;
-  if (begin >= static_cast<uint32_t>(r1)) return;
-  const uint32_t live = static_cast<uint32_t>(min(uint64_t(S::kRows), r1 - begin));
-  if (i >= 0 && static_cast<uint32_t>(i) >= a.count) {
-    if (rank == 0 && threadIdx.x == 0) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
-    i = -1;
+  AdTile T{0, 0, a.which[s]};
+  if (tell) {                                          // what does not fit is found by one block
+    bool bad = false;
+    for (uint32_t k = threadIdx.x; k < a.n_seqs; k += kAdThreads)
+      bad |= a.starts[k] < 0 || a.starts[k + 1] < a.starts[k] || static_cast<uint32_t>(a.starts[k + 1]) > a.rows ||
+             (a.starts[k + 1] > a.starts[k] && a.which[k] >= 0 && static_cast<uint32_t>(a.which[k]) >= a.count);
+    if (bad) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
   }
+  const uint32_t place = static_cast<uint32_t>(max(r0, 0)) / ROWS + s;
+  if (r0 < 0 || r1 < r0 || static_cast<uint32_t>(r1) > a.rows || tile < place) return T;
+  T.begin = uint64_t(r0) + uint64_t(tile - place) * ROWS;
+  if (T.begin < static_cast<uint32_t>(r1)) T.live = static_cast<uint32_t>(min(uint64_t(ROWS), r1 - T.begin));
+  if (T.which >= 0 && static_cast<uint32_t>(T.which) >= a.count) T.which = -1;
+  return T;
+}
+
+// R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each.  blockIdx.y: the part of the inputs.
+template <int R, int MT, bool F8, bool VEC>
+__global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapters_down_kernel(const AdArgs a) {
+  using S = AdShape<R, MT>;
+  using X = std::conditional_t<F8, uint8_t, uint16_t>;
+  constexpr uint32_t kUnit = F8 ? 64 : 32, kLane = kUnit / 4, kSteps = kUnit / 16;     // inputs of a unit, of a lane, products
+  constexpr int NT = R / 8;
+  constexpr int kAhead = MT * R <= 16 ? (F8 ? 2 : 4) : MT * R <= 64 && !F8 ? 2 : 1;    // units whose loads are under way together
+  extern __shared__ __align__(16) uint8_t smem[];
+  float* const parts = reinterpret_cast<float*>(smem);               // [warp][row][R + 8]
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
+  let_next_start();
+  wait_for_previous();
+  const AdTile T = ad_tile<S::kRows>(a, blockIdx.x, blockIdx.x == 0 && blockIdx.y == 0);
+  if (T.live == 0 || T.which < 0) return;
+  const uint32_t live = T.live, i = T.which;
+  const uint64_t begin = T.begin;
+
+  float c[MT][NT][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
+  const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
+  const uint32_t u0 = static_cast<uint32_t>(uint64_t(units) * blockIdx.y / gridDim.y), u1 = static_cast<uint32_t>(uint64_t(units) * (blockIdx.y + 1u) / gridDim.y);
+  const X* x[MT][2];                                               // the lane's rows
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (uint32_t h = 0; h < 2; ++h) x[m][h] = reinterpret_cast<const X*>(a.x) + (begin + min(16u * m + 8u * h + g, live - 1u)) * a.x_stride;
+  const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + (uint64_t(i) * a.rank + min(g, a.rank - 1u)) * a.n_in;
+  for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
+    uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t now = u + kAdWarps * k, e = now * kUnit + t * kLane;
+      const bool in = now < u1;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (uint32_t h = 0; h < kLane / 8; ++h)
+          af[k][n][h] = piece_of<uint16_t, VEC>(down + 8u * n * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) xf[k][m][h] = piece_of<X, VEC>(x[m][h], e, a.n_in, in && 16u * m + 8u * h + g < live);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (uint32_t j = 0; j < kSteps; ++j) {
+        uint32_t xw[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t* const w = &xf[k][m][h].x;
+            if constexpr (F8) {
+              xw[m][h] = open_e4m3(w[j] & 0xFFFFu);
+              xw[m][h + 2] = open_e4m3(w[j] >> 16);
+            } else {
+              xw[m][h] = w[2 * j];
+              xw[m][h + 2] = w[2 * j + 1];
+            }
+          }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          const uint32_t* const w = &af[k][n][j / 2].x;
+          const uint32_t b0 = w[2 * (j % 2)], b1 = w[2 * (j % 2) + 1];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) mma_bf16(c[m][n], xw[m][0], xw[m][1], xw[m][2], xw[m][3], b0, b1);
+        }
+      }
+  }
+  float* const to = parts + warp * S::kPart;
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      *reinterpret_cast<float2*>(to + (16 * m + g) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
+      *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
+    }
+  __syncthreads();
+  float* const h = a.room + (uint64_t(blockIdx.y) * a.rows + begin) * R;
+#pragma unroll
+  for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
+    const uint32_t e = threadIdx.x + n * kAdThreads;
+    if (e / R >= live) break;
+    float sum = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
+    h[e] = sum;
+  }
+}
+
+// blockIdx.y: the part of the outputs; `sums`: parts of the inputs.
+template <int R, int MT>
+__global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_up_kernel(const AdArgs a, uint32_t sums) {
+  using S = AdShape<R, MT>;
+  constexpr int KT = R / 16;
+  constexpr int kOuts = R <= 32 ? 2 : 1;                             // groups of 32 outputs whose rows of B are loaded ahead
+  extern __shared__ __align__(16) uint8_t smem[];
+  __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(smem);
+  __nv_bfloat16* const low = high + S::kRows * S::kHRow;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
+  uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + warp * S::kRing;
+  let_next_start();
+  wait_for_previous();
+  const AdTile T = ad_tile<S::kRows>(a, blockIdx.x, false);
+  const uint32_t live = T.live;
+  const int32_t i = T.which;
+  const uint64_t begin = T.begin;
   const bool none = i < 0;
-  if (none && a.out == a.y) return;
+  if (live == 0 || (none && a.out == a.y)) return;
 
   const uint32_t groups = (a.n_out + 31u) / 32u;
-  const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * rank / ranks), o1 = static_cast<uint32_t>(uint64_t(groups) * (rank + 1u) / ranks);
+  const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * blockIdx.y / gridDim.y), o1 = static_cast<uint32_t>(uint64_t(groups) * (blockIdx.y + 1u) / gridDim.y);
   // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
   // elements t R / 4 + 4 k and on of a row
   const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4);
@@ -155,120 +258,29 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (threadIdx.x < S::kRows && !none) {
-    const float scale = a.scales ? a.scales[i] : 1.f;
-    factor[threadIdx.x] = a.x_scales && threadIdx.x < live ? a.x_scales[begin + threadIdx.x] * scale : scale;
-  }
   for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
   uint32_t bf[kOuts][4][KT][2];
 #pragma unroll
   for (int n = 0; n < kOuts; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
 
   if (!none) {
-    float c[MT][NT][4];
+    const float scale = a.scales ? a.scales[i] : 1.f;
+    const float* const h = a.room + begin * R;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
+      const uint32_t e = threadIdx.x + n * kAdThreads, row = e / R, k = e % R;
+      float v[8], sum = 0.f;                                         // of all parts, under way together
 #pragma unroll
-      for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
-    const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
-    const uint32_t u0 = static_cast<uint32_t>(uint64_t(units) * rank / ranks), u1 = static_cast<uint32_t>(uint64_t(units) * (rank + 1u) / ranks);
-    const X* x[MT][2];                                               // the lane's rows
+      for (uint32_t p = 0; p < 8; ++p) v[p] = p < sums && row < live ? h[uint64_t(p) * a.rows * R + e] : 0.f;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (uint32_t h = 0; h < 2; ++h) x[m][h] = reinterpret_cast<const X*>(a.x) + (begin + min(16u * m + 8u * h + g, live - 1u)) * a.x_stride;
-    const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + (uint64_t(i) * a.rank + min(g, a.rank - 1u)) * a.n_in;
-    for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
-      uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const uint32_t now = u + kAdWarps * k, e = now * kUnit + t * kLane;
-        const bool in = now < u1;
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (uint32_t h = 0; h < kLane / 8; ++h)
-            af[k][n][h] = piece_of<uint16_t, VEC>(down + 8u * n * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (uint32_t h = 0; h < 2; ++h) xf[k][m][h] = piece_of<X, VEC>(x[m][h], e, a.n_in, in && 16u * m + 8u * h + g < live);
-      }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-#pragma unroll
-        for (uint32_t j = 0; j < kSteps; ++j) {
-          uint32_t xw[MT][4];
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const uint32_t* const w = &xf[k][m][h].x;
-              if constexpr (F8) {
-                xw[m][h] = open_e4m3(w[j] & 0xFFFFu);
-                xw[m][h + 2] = open_e4m3(w[j] >> 16);
-              } else {
-                xw[m][h] = w[2 * j];
-                xw[m][h + 2] = w[2 * j + 1];
-              }
-            }
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const uint32_t* const w = &af[k][n][j / 2].x;
-            const uint32_t b0 = w[2 * (j % 2)], b1 = w[2 * (j % 2) + 1];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) mma_bf16(c[m][n], xw[m][0], xw[m][1], xw[m][2], xw[m][3], b0, b1);
-          }
-        }
-    }
-    float* const to = parts + warp * S::kPart;
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        *reinterpret_cast<float2*>(to + (16 * m + g) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
-        *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
-      }
-    __syncthreads();
-    constexpr uint32_t kEach = S::kSums / kAdThreads;                // sums of a thread
-    static_assert(S::kSums % kAdThreads == 0, "");
-#pragma unroll
-    for (uint32_t n = 0; n < kEach; ++n) {
-      const uint32_t e = threadIdx.x + n * kAdThreads;
-      float sum = 0.f;
-#pragma unroll
-      for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
-      mine[e] = sum;
-    }
-    if (ranks > 1) cluster_sync(); else __syncthreads();
-    const uint32_t from = smem_addr(mine) + 4u * threadIdx.x;
-    constexpr uint32_t kBatch = kEach < 4 ? kEach : 4;
-#pragma unroll 1
-    for (uint32_t n0 = 0; n0 < kEach; n0 += kBatch) {
-      float v[kBatch][8];                                            // of all blocks, at most 8, under way together
-#pragma unroll
-      for (uint32_t r = 0; r < 8; ++r)
-#pragma unroll
-        for (uint32_t n = 0; n < kBatch; ++n)
-          if (r < ranks)
-            asm volatile("{\n\t.reg .b32 p;\n\tmapa.shared::cluster.u32 p, %1, %2;\n\tld.shared::cluster.f32 %0, [p];\n\t}"
-                         : "=f"(v[n][r]) : "r"(from + (n0 + n) * (4u * kAdThreads)), "r"(r));
-#pragma unroll
-      for (uint32_t n = 0; n < kBatch; ++n) {
-        const uint32_t e = threadIdx.x + (n0 + n) * kAdThreads, row = e / R, k = e % R;
-        float sum = 0.f;
-#pragma unroll
-        for (uint32_t r = 0; r < 8; ++r)
-          if (r < ranks) sum += v[n][r];
-        sum = row < live ? sum * factor[row] : 0.f;
-        const __nv_bfloat16 h = __float2bfloat16_rn(sum);
-        const float rest = sum - __bfloat162float(h);
-        high[row * S::kHRow + k] = h;
-        low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
-      }
+      for (uint32_t p = 0; p < 8; ++p) sum += v[p];
+      sum *= a.x_scales && row < live ? a.x_scales[begin + row] * scale : scale;
+      const __nv_bfloat16 hi = __float2bfloat16_rn(sum);
+      const float rest = sum - __bfloat162float(hi);
+      high[row * S::kHRow + k] = hi;
+      low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
     }
     __syncthreads();
-    if (ranks > 1) cluster_arrive();                                 // this block has read the others' sums
   }
 
   uint32_t slot = 0;
@@ -369,30 +381,53 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_kern
     }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
-  if (!none && ranks > 1) cluster_wait();                            // nobody reads this block's sums any more
+}
+
+// What a call with more rows than requests launches.
+struct AdPlan {
+  int r, mt;                         // the rank as the kernels have it, and 16 rows each
+  uint32_t tiles, sums, parts;       // parts of the inputs and of the outputs
+  size_t room;
+};
+static AdPlan plan_adapters(const ans_adapters_desc& d, int sms) {
+  AdPlan p{};
+  p.r = d.rank <= 16 ? 16 : d.rank <= 32 ? 32 : d.rank <= 64 ? 64 : 128;
+  // tiles of 16 rows where requests have about as many, else of 32, if registers hold their sums
+  p.mt = p.r == 128 || uint64_t(d.rows) <= 16ull * d.n_seqs ? 1 : 2;
+  p.tiles = d.rows / (16u * p.mt) + d.n_seqs;
+  // enough blocks for four an SM, as long as each warp has a unit of inputs, and four groups of outputs, to itself
+  const uint32_t units = (d.n_in + 63) / 64, groups = (d.n_out + 31) / 32, enough = 4u * sms;
+  p.sums = 1;
+  while (p.sums < 8 && uint64_t(p.tiles) * p.sums < enough && 2 * p.sums * kAdWarps <= units) p.sums *= 2;
+  p.parts = 1;
+  while (p.parts < 64 && uint64_t(p.tiles) * p.parts < enough && 2 * p.parts * kAdWarps <= groups) p.parts *= 2;
+  p.room = size_t(p.sums) * d.rows * p.r * sizeof(float);
+  return p;
 }
 
 template <int R, int MT, bool F8, bool VEC>
-static int launch_adapters(const AdArgs& a, int sms, cudaStream_t st) {
+static int launch_down(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
   using S = AdShape<R, MT>;
-  const uint64_t tiles = a.rows / S::kRows + a.n_seqs;
-  // Blocks of a tile: 8, but for single rows as many as have their places on the GPU at once, two an SM.
-  uint32_t ranks = 8;
-  while (MT == 1 && ranks > 1 && tiles * ranks > 2ull * sms) ranks /= 2;
-  if (tiles * ranks > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  constexpr auto kernel = ans_adapters_kernel<R, MT, F8, VEC>;
-  const int rc = allow_smem<kernel>(S::kSmem);
-  return rc == ANS_OK ? launch(kernel, dim3(static_cast<unsigned>(tiles * ranks)), dim3(kAdThreads), S::kSmem, st, ranks, a) : rc;
+  constexpr auto kernel = ans_adapters_down_kernel<R, MT, F8, VEC>;
+  const int rc = allow_smem<kernel>(S::kDownSmem);
+  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.sums), dim3(kAdThreads), S::kDownSmem, st, 1, a) : rc;
 }
-
-// Tiles of 16 rows where requests have about as many, else of 32, if registers hold their sums.
-template <bool F8, bool VEC>
-static int launch_rank(const AdArgs& a, int sms, cudaStream_t st) {
-  const bool few = uint64_t(a.rows) <= 16ull * a.n_seqs;
-  if (a.rank <= 16) return few ? launch_adapters<16, 1, F8, VEC>(a, sms, st) : launch_adapters<16, 2, F8, VEC>(a, sms, st);
-  if (a.rank <= 32) return few ? launch_adapters<32, 1, F8, VEC>(a, sms, st) : launch_adapters<32, 2, F8, VEC>(a, sms, st);
-  if (a.rank <= 64) return few ? launch_adapters<64, 1, F8, VEC>(a, sms, st) : launch_adapters<64, 2, F8, VEC>(a, sms, st);
-  return launch_adapters<128, 1, F8, VEC>(a, sms, st);
+template <int R, int MT>
+static int launch_both(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
+  using S = AdShape<R, MT>;
+  int rc = f8 ? (vec ? launch_down<R, MT, true, true>(a, p, st) : launch_down<R, MT, true, false>(a, p, st))
+              : (vec ? launch_down<R, MT, false, true>(a, p, st) : launch_down<R, MT, false, false>(a, p, st));
+  constexpr auto kernel = ans_adapters_up_kernel<R, MT>;
+  if (rc == ANS_OK) rc = allow_smem<kernel>(S::kUpSmem);
+  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.parts), dim3(kAdThreads), S::kUpSmem, st, 1, a, p.sums) : rc;
+}
+static int launch_tiles_of(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
+  switch (p.r) {
+    case 16: return p.mt == 1 ? launch_both<16, 1>(a, p, f8, vec, st) : launch_both<16, 2>(a, p, f8, vec, st);
+    case 32: return p.mt == 1 ? launch_both<32, 1>(a, p, f8, vec, st) : launch_both<32, 2>(a, p, f8, vec, st);
+    case 64: return p.mt == 1 ? launch_both<64, 1>(a, p, f8, vec, st) : launch_both<64, 2>(a, p, f8, vec, st);
+    default: return launch_both<128, 1>(a, p, f8, vec, st);
+  }
 }
 
 }  // namespace blk
@@ -400,6 +435,18 @@ static int launch_rank(const AdArgs& a, int sms, cudaStream_t st) {
 
 using namespace ansb;
 using namespace ansb::blk;
+
+ANS_EXPORT int ans_adapters_room_bytes(const ans_adapters_desc* h_desc, size_t* h_bytes_out) {
+  if (!h_desc || !h_bytes_out) return ANS_ERR_INVALID_ARG;
+  if (h_desc->rank == 0 || h_desc->n_in == 0) return ANS_ERR_INVALID_ARG;
+  if (h_desc->rank > 128 || h_desc->n_seqs > ANS_MAX_SEQS || h_desc->rows > 0x7FFFFFFFu || h_desc->n_in > (1u << 22) || h_desc->n_out > (1u << 30)) return ANS_ERR_UNSUPPORTED;
+  *h_bytes_out = 0;
+  if (h_desc->rows <= h_desc->n_seqs || h_desc->n_seqs == 0 || h_desc->n_out == 0) return ANS_OK;
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc == ANS_OK) *h_bytes_out = plan_adapters(*h_desc, sms).room;
+  return rc;
+}
 
 ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status, void* stream) {
   ApiRange range("ans_adapters");
@@ -441,6 +488,9 @@ ANS_EXPORT int ans_adapters(const ans_adapters_desc* h_desc, uint32_t* d_status,
   if (asked != ANS_OK) return asked;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (d.rows <= d.n_seqs) return launch_adapters_rows(a, d.x_dtype == ANS_E4M3, vec, sms, st);
-  if (d.x_dtype == ANS_E4M3) return vec ? launch_rank<true, true>(a, sms, st) : launch_rank<true, false>(a, sms, st);
-  return vec ? launch_rank<false, true>(a, sms, st) : launch_rank<false, false>(a, sms, st);
+  const AdPlan p = plan_adapters(d, sms);
+  if (!d.d_room || d.room_bytes < p.room) return ANS_ERR_BUFFER_TOO_SMALL;
+  if (reinterpret_cast<uintptr_t>(d.d_room) & 15) return ANS_ERR_INVALID_ARG;
+  a.room = static_cast<float*>(d.d_room);
+  return launch_tiles_of(a, p, d.x_dtype == ANS_E4M3, vec, st);
 }

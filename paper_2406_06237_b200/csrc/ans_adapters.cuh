@@ -15,6 +15,7 @@ struct AdArgs {
   uint32_t b_run;                    // runs of 32 rows of B start on 16 bytes
   uint32_t b_wide, y_wide;           // four elements of B, eight of y and out can be accessed at once
   uint32_t y_f32;                    // y and out in fp32, else bf16
+  float* room;                       // [part of the inputs][row][rank as the kernels have it]
   uint32_t* status;
 };
 
