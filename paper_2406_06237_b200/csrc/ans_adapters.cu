@@ -27,8 +27,8 @@ struct AdShape {
   static constexpr uint32_t kSums = kRows * R;                       // of h
   static constexpr uint32_t kHRow = R + 8, kPart = kRows * (R + 8);  // elements of a row of h, of a warp's sums; + 8: eight rows in different banks
   static constexpr uint32_t kDownSmem = kAdWarps * kPart * 4;
-  // a warp's ring of groups of 32 outputs of y: four groups in bf16, two in fp32
-  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = 4 * kGroup;
+  // a warp's ring of groups of 32 outputs of y: two groups in bf16, one in fp32
+  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = 2 * kGroup;
   static constexpr uint32_t kUpSmem = 2 * kRows * kHRow * 2 + kAdWarps * kRing;
 };
 
@@ -191,12 +191,13 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   }
 }
 
-// blockIdx.y: the part of the outputs; `sums`: parts of the inputs.
-template <int R, int MT>
-__global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_up_kernel(const AdArgs a, uint32_t sums) {
+// blockIdx.y: the part of the outputs; `sums`: parts of the inputs.  EXACT: the rank is R, outputs come in whole groups of 32, and B, y
+// and out can be accessed 8 and 16 bytes at a time: addresses are then constants apart and nothing is asked (180 instructions a group
+// of 32 rows by 32 outputs where the general form takes 600).
+template <int R, int MT, bool EXACT>
+__global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_kernel(const AdArgs a, uint32_t sums) {
   using S = AdShape<R, MT>;
   constexpr int KT = R / 16;
-  constexpr int kOuts = R <= 32 ? 2 : 1;                             // groups of 32 outputs whose rows of B are loaded ahead
   extern __shared__ __align__(16) uint8_t smem[];
   __nv_bfloat16* const high = reinterpret_cast<__nv_bfloat16*>(smem);
   __nv_bfloat16* const low = high + S::kRows * S::kHRow;
@@ -215,28 +216,36 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_up_k
   const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * blockIdx.y / gridDim.y), o1 = static_cast<uint32_t>(uint64_t(groups) * (blockIdx.y + 1u) / gridDim.y);
   // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
   // elements t R / 4 + 4 k and on of a row
-  const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4);
-  const __nv_bfloat16* const b_lane = a.b + (uint64_t(max(i, 0)) * a.n_out + b_out) * a.rank + b_in;
+  const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4), b_row = EXACT ? R : a.rank;
+  const __nv_bfloat16* const b_lane = a.b + (uint64_t(max(i, 0)) * a.n_out + b_out) * b_row + b_in;
   auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
-    const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * a.rank);
-    const uint32_t left = o < o1 && !none ? a.n_out - 32u * o : 0u;  // outputs from the group's first on
+    const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * b_row);
+    const bool ours = o < o1 && !none;
+    const uint32_t left = ours ? a.n_out - 32u * o : 0u;             // outputs from the group's first on
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) {
-      const __nv_bfloat16* const row = rows + 2u * j * a.rank;
-      const bool in = b_out + 2u * j < left;
+      const __nv_bfloat16* const row = rows + 2u * j * b_row;
 #pragma unroll
       for (uint32_t k = 0; k < KT; ++k) {
-        f[j][k][0] = f[j][k][1] = 0u;
-        if (a.b_wide) {
-          if (in && b_in + 4u * k < a.rank) {
+        if constexpr (EXACT) {
+          if (ours) {
             const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
             f[j][k][0] = u.x; f[j][k][1] = u.y;
           }
         } else {
+          const bool in = b_out + 2u * j < left;
+          f[j][k][0] = f[j][k][1] = 0u;
+          if (a.b_wide) {
+            if (in && b_in + 4u * k < a.rank) {
+              const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
+              f[j][k][0] = u.x; f[j][k][1] = u.y;
+            }
+          } else {
 #pragma unroll
-          for (uint32_t h = 0; h < 4; ++h)
-            if (in && b_in + 4u * k + h < a.rank)
-              f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[4u * k + h]) << (16 * (h % 2));
+            for (uint32_t h = 0; h < 4; ++h)
+              if (in && b_in + 4u * k + h < a.rank)
+                f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[4u * k + h]) << (16 * (h % 2));
+          }
         }
       }
     }
@@ -246,22 +255,32 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_up_k
   const uint32_t slot_bytes = S::kRows << (y_shift + 4u), slots = S::kRing / slot_bytes;
   const uint8_t* const y = static_cast<const uint8_t*>(a.y) + begin * a.y_stride * y_size;
   uint8_t* const out = static_cast<uint8_t*>(a.out) + begin * a.out_stride * y_size;
-  const uint32_t y_row = lane >> y_shift, y_at = 16u * (lane & ((1u << y_shift) - 1u)), y_down = 32u >> y_shift;
+  const uint32_t y_row = lane >> y_shift, y_at = 16u * (lane & ((1u << y_shift) - 1u)), y_rows = 32u >> y_shift;
+  const uint64_t y_down = y_rows * a.y_stride * y_size;
   const uint8_t* const y_lane = y + y_row * a.y_stride * y_size + y_at;
   const uint32_t ring_lane = smem_addr(ring) + lane * 16u;
+  const bool whole = live == S::kRows;
   auto fetch_y = [&](uint32_t o, uint32_t slot) {
-    if (a.y_wide && o < o1 && uint64_t(32u * y_size) * o + y_at + 16u <= uint64_t(a.n_out) * y_size) {
-      const uint8_t* from = y_lane + uint64_t(32u * y_size) * o;
+    const uint64_t across = uint64_t(32u * y_size) * o;
+    if ((EXACT || a.y_wide) && o < o1 && (EXACT || across + y_at + 16u <= uint64_t(a.n_out) * y_size)) {
+      const uint8_t* from = y_lane + across;
       uint32_t to = ring_lane + slot * slot_bytes;
-      for (uint32_t row = y_row; row < live; row += y_down, from += y_down * a.y_stride * y_size, to += 512u)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+      if (EXACT && whole && y_shift == 2) {
+#pragma unroll
+        for (uint32_t n = 0; n < S::kRows / 8; ++n, from += y_down, to += 512u)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+      } else {
+        for (uint32_t row = y_row; row < live; row += y_rows, from += y_down, to += 512u)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
-  uint32_t bf[kOuts][4][KT][2];
+  constexpr uint32_t kBs = R <= 32 ? 2 : 1;                          // groups whose rows of B are loaded ahead
+  uint32_t bf[kBs][4][KT][2];
 #pragma unroll
-  for (int n = 0; n < kOuts; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
+  for (uint32_t n = 0; n < kBs; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
 
   if (!none) {
     const float scale = a.scales ? a.scales[i] : 1.f;
@@ -284,99 +303,86 @@ __global__ void __launch_bounds__(kAdThreads, R >= 64 ? 1 : 2) ans_adapters_up_k
   }
 
   uint32_t slot = 0;
-  for (uint32_t o = o0 + warp; o < o1; o += kAdWarps * kOuts) {
+  uint8_t* out_lane = out + (g * a.out_stride + 8u * t) * y_size + uint64_t(32u * y_size) * (o0 + warp);
+  const uint64_t out_down = 8u * a.out_stride * y_size;
+#pragma unroll 1
+  for (uint32_t first = o0 + warp; first < o1; first += kAdWarps * kBs) {
 #pragma unroll
-    for (int n = 0; n < kOuts; ++n) {
-      const uint32_t now = o + kAdWarps * n;
-      if (now >= o1) break;
-      const uint32_t at = 32u * now + 8u * t;                        // the lane's outputs: at .. at + 7
-      const bool wide = a.y_wide && at + 8 <= a.n_out;
-      if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-      else if (slots == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
-      else if (slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    for (uint32_t n = 0; n < kBs; ++n, out_lane += 32u * y_size * kAdWarps) {
+      const uint32_t o = first + kAdWarps * n;
+      if (o >= o1) break;
+      const uint32_t at = 32u * o + 8u * t;                          // the lane's outputs: at .. at + 7
+      const bool wide = EXACT || (a.y_wide && at + 8 <= a.n_out);
+      if (slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
       else asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncwarp();
       const uint8_t* const staged = ring + slot * slot_bytes;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if (16u * m >= live) break;
-        float v[2][8];
+        float d[4][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t r = 16u * m + 8u * h + g;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[h][k] = 0.f;
-          if (r >= live) continue;
-          if (wide) {
-            const uint4* const p = reinterpret_cast<const uint4*>(staged) + ((r * 4u + t) << (y_shift - 2u));
-            const uint4 q = p[0];
-            if (a.y_f32) {
-              const uint4 z = p[1];
-              v[h][0] = __uint_as_float(q.x); v[h][1] = __uint_as_float(q.y); v[h][2] = __uint_as_float(q.z); v[h][3] = __uint_as_float(q.w);
-              v[h][4] = __uint_as_float(z.x); v[h][5] = __uint_as_float(z.y); v[h][6] = __uint_as_float(z.z); v[h][7] = __uint_as_float(z.w);
-            } else {
-              const uint32_t* const w = &q.x;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                v[h][2 * k] = __uint_as_float(w[k] << 16);
-                v[h][2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-              }
-            }
-          } else {
-            const uint8_t* const p = y + (r * a.y_stride + at) * y_size;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (at + k < a.n_out)
-                v[h][k] = a.y_f32 ? reinterpret_cast<const float*>(p)[k] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[k]);
-          }
-        }
+        for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
         if (!none) {
-          float d[4][4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
-#pragma unroll
-          for (int k = 0; k < KT; ++k) {
+          for (uint32_t k = 0; k < KT; ++k) {
             const uint32_t e = t * (R / 4) + 4u * k, up = (16u * m + g) * S::kHRow + e, dn = up + 8u * S::kHRow;
             const uint2 lu = *reinterpret_cast<const uint2*>(low + up), ld = *reinterpret_cast<const uint2*>(low + dn);
             const uint2 hu = *reinterpret_cast<const uint2*>(high + up), hd = *reinterpret_cast<const uint2*>(high + dn);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              mma_bf16(d[j], lu.x, ld.x, lu.y, ld.y, bf[n][j][k][0], bf[n][j][k][1]);
-              mma_bf16(d[j], hu.x, hd.x, hu.y, hd.y, bf[n][j][k][0], bf[n][j][k][1]);
-            }
-          }
+            for (int j = 0; j < 4; ++j) mma_bf16(d[j], lu.x, ld.x, lu.y, ld.y, bf[n][j][k][0], bf[n][j][k][1]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v[0][2 * j] += d[j][0]; v[0][2 * j + 1] += d[j][1];
-            v[1][2 * j] += d[j][2]; v[1][2 * j + 1] += d[j][3];
+            for (int j = 0; j < 4; ++j) mma_bf16(d[j], hu.x, hd.x, hu.y, hd.y, bf[n][j][k][0], bf[n][j][k][1]);
           }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t r = 16u * m + 8u * h + g;
-          uint8_t* const p = out + (r * a.out_stride + at) * y_size;
           if (r >= live) continue;
+          float v[8];
+          uint8_t* const p = out_lane + (2 * m + h) * out_down;
           if (wide) {
+            const uint4* const q = reinterpret_cast<const uint4*>(staged) + ((r * 4u + t) << (y_shift - 2u));
             if (a.y_f32) {
-              reinterpret_cast<float4*>(p)[0] = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
-              reinterpret_cast<float4*>(p)[1] = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
+              const uint4 w = q[0], z = q[1];
+              v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+              v[4] = __uint_as_float(z.x); v[5] = __uint_as_float(z.y); v[6] = __uint_as_float(z.z); v[7] = __uint_as_float(z.w);
             } else {
-              *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[h][0], v[h][1]), pack_bf16(v[h][2], v[h][3]), pack_bf16(v[h][4], v[h][5]),
-                                                        pack_bf16(v[h][6], v[h][7]));
+              const uint4 u = q[0];
+              const uint32_t* const w = &u.x;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                v[2 * k] = __uint_as_float(w[k] << 16);
+                v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+              }
+            }
+            if (!none)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                v[2 * j] += d[j][2 * h];
+                v[2 * j + 1] += d[j][2 * h + 1];
+              }
+            if (a.y_f32) {
+              reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+              reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+              *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
             }
           } else {
+            const uint8_t* const q = y + (r * a.y_stride + at) * y_size;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               if (at + k < a.n_out) {
-                if (a.y_f32) reinterpret_cast<float*>(p)[k] = v[h][k];
-                else reinterpret_cast<__nv_bfloat16*>(p)[k] = __float2bfloat16_rn(v[h][k]);
+                float u = a.y_f32 ? reinterpret_cast<const float*>(q)[k] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[k]);
+                if (!none) u += d[k / 2][2 * h + k % 2];
+                if (a.y_f32) reinterpret_cast<float*>(p)[k] = u;
+                else reinterpret_cast<__nv_bfloat16*>(p)[k] = __float2bfloat16_rn(u);
               }
           }
         }
       }
       __syncwarp();
-      load_b(now + kAdWarps * kOuts, bf[n]);
-      fetch_y(now + kAdWarps * slots, slot);
+      load_b(o + kAdWarps * kBs, bf[n]);
+      fetch_y(o + kAdWarps * slots, slot);
       slot = slot + 1u == slots ? 0u : slot + 1u;
     }
   }
@@ -412,14 +418,19 @@ static int launch_down(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
   const int rc = allow_smem<kernel>(S::kDownSmem);
   return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.sums), dim3(kAdThreads), S::kDownSmem, st, 1, a) : rc;
 }
+template <int R, int MT, bool EXACT>
+static int launch_up(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
+  using S = AdShape<R, MT>;
+  constexpr auto kernel = ans_adapters_up_kernel<R, MT, EXACT>;
+  const int rc = allow_smem<kernel>(S::kUpSmem);
+  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.parts), dim3(kAdThreads), S::kUpSmem, st, 1, a, p.sums) : rc;
+}
 template <int R, int MT>
 static int launch_both(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
-  using S = AdShape<R, MT>;
-  int rc = f8 ? (vec ? launch_down<R, MT, true, true>(a, p, st) : launch_down<R, MT, true, false>(a, p, st))
+  const int rc = f8 ? (vec ? launch_down<R, MT, true, true>(a, p, st) : launch_down<R, MT, true, false>(a, p, st))
               : (vec ? launch_down<R, MT, false, true>(a, p, st) : launch_down<R, MT, false, false>(a, p, st));
-  constexpr auto kernel = ans_adapters_up_kernel<R, MT>;
-  if (rc == ANS_OK) rc = allow_smem<kernel>(S::kUpSmem);
-  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.parts), dim3(kAdThreads), S::kUpSmem, st, 1, a, p.sums) : rc;
+  if (rc != ANS_OK) return rc;
+  return a.rank == R && a.n_out % 32 == 0 && a.b_wide && a.y_wide ? launch_up<R, MT, true>(a, p, st) : launch_up<R, MT, false>(a, p, st);
 }
 static int launch_tiles_of(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
   switch (p.r) {
