@@ -18,7 +18,7 @@ namespace ansb {
 
 using namespace ten;
 
-constexpr uint32_t kPgThreads = 512;
+constexpr uint32_t kPgThreads = 512, kPgAhead = 8;   // rows of a thread whose pages are asked for together
 constexpr uint32_t kPgMost = 0x7FFFFFFFu;              // sums stop here, which no batch that fits reaches
 
 // sums that stop at kPgMost: associative for numbers up to it
@@ -38,6 +38,7 @@ __global__ void __launch_bounds__(kPgThreads) ans_page_tables_kernel(const ans_p
   extern __shared__ uint32_t smem[];
   uint32_t* const rows = smem;                         // [n + 1] sums of new tokens
   uint32_t* const more = rows + d.n_seqs + 1;          // [n + 1] sums of new pages
+  uint32_t* const had = more + d.n_seqs + 1;           // [n] cached tokens
   __shared__ uint32_t part[3][kPgThreads / 32];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, n = d.n_seqs;
   uint32_t blocks;
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(kPgThreads) ans_page_tables_kernel(const ans_p
       base[k] = plus(base[k], all[k]);
       x[k] = plus(x[k], before[k]);                    // with this request
     }
-    if (s < n) { rows[s + 1] = x[0]; more[s + 1] = x[1]; }
+    if (s < n) { rows[s + 1] = x[0]; more[s + 1] = x[1]; had[s] = cached; }
     my_cached = cached;
     my_end = x[2];
     __syncthreads();
@@ -104,28 +105,42 @@ __global__ void __launch_bounds__(kPgThreads) ans_page_tables_kernel(const ans_p
   // A request's own numbers are read again below; what overwrites them waits for the other blocks.
   const int32_t* const free_from = d.d_free + taken0;
 
-  // rows: a warp takes 32 at a time, and moves on in the sums from the request of the last ones
+  // rows: a warp takes 32 at a time, kPgAhead times together, and moves on in the sums from the request of the last ones
   const uint32_t warps = blocks * (kPgThreads / 32), each = (d.rows + 32 * warps - 1) / (32 * warps) * 32;
-  const uint64_t r0 = uint64_t(rank * (kPgThreads / 32) + warp) * each;
+  const uint64_t r0 = uint64_t(rank * (kPgThreads / 32) + warp) * each, r1 = min(r0 + each, uint64_t(d.rows));
   uint32_t s = 0;
-  for (uint64_t at = r0 + lane; at < min(r0 + each, uint64_t(d.rows)); at += 32) {
-    const uint32_t row = static_cast<uint32_t>(at);
-    int64_t slot = -1;
-    int32_t position = 0;
-    if (!bad && row < total) {
-      if (at < r0 + 32) s = place_in(rows, n, row);
-      else while (rows[s + 1] <= row) ++s;
-      const uint32_t c = d.d_cached[s], pos = c + (row - rows[s]), page = pos / d.page_size, held = (c + d.page_size - 1) / d.page_size;
-      const int32_t p = page < held ? d.d_tables[s * d.table_stride + page] : free_from[more[s] + (page - held)];
-      slot = int64_t(p) * d.page_size + (pos - page * d.page_size);
-      if (p < 0 || slot > int64_t(kPgMost)) {
-        slot = -1;
-        atomicOr(status, ANS_STATUS_BAD_PAGE);
+  for (uint64_t at = r0 + lane; at < r1; at += 32 * kPgAhead) {
+    int32_t page[kPgAhead];
+    uint32_t in[kPgAhead], position[kPgAhead];
+    bool live[kPgAhead];
+#pragma unroll
+    for (uint32_t k = 0; k < kPgAhead; ++k) {
+      const uint64_t mine = at + 32 * k;
+      const uint32_t row = static_cast<uint32_t>(mine);
+      live[k] = !bad && mine < r1 && row < total;
+      page[k] = -1;
+      in[k] = position[k] = 0;
+      if (live[k]) {
+        if (mine < r0 + 32) s = place_in(rows, n, row);
+        else while (rows[s + 1] <= row) ++s;
+        const uint32_t c = had[s], pos = c + (row - rows[s]), number = pos / d.page_size, held = (c + d.page_size - 1) / d.page_size;
+        page[k] = number < held ? d.d_tables[s * d.table_stride + number] : free_from[more[s] + (number - held)];
+        in[k] = pos - number * d.page_size;
+        position[k] = pos;
       }
-      position = static_cast<int32_t>(pos);
     }
-    d.d_slots[row] = slot;
-    d.d_positions[row] = position;
+#pragma unroll
+    for (uint32_t k = 0; k < kPgAhead; ++k) {
+      const uint64_t mine = at + 32 * k;
+      if (mine >= r1) break;
+      int64_t slot = int64_t(page[k]) * d.page_size + in[k];
+      if (page[k] < 0 || slot > int64_t(kPgMost)) {
+        slot = -1;
+        if (live[k]) atomicOr(status, ANS_STATUS_BAD_PAGE);
+      }
+      d.d_slots[mine] = slot;
+      d.d_positions[mine] = static_cast<int32_t>(position[k]);
+    }
   }
   // pages
   if (!bad) {
@@ -135,7 +150,7 @@ __global__ void __launch_bounds__(kPgThreads) ans_page_tables_kernel(const ans_p
       if (first) q = place_in(more, n, at);
       else while (more[q + 1] <= at) ++q;
       first = false;
-      const uint32_t held = (static_cast<uint32_t>(d.d_cached[q]) + d.page_size - 1) / d.page_size;
+      const uint32_t held = (had[q] + d.page_size - 1) / d.page_size;
       d.d_tables[q * d.table_stride + held + (at - more[q])] = free_from[at];
     }
   }
@@ -215,6 +230,8 @@ ANS_EXPORT int ans_page_tables(const ans_pages_desc* h_desc, uint32_t* d_status,
   if (reinterpret_cast<uintptr_t>(d.d_slots) & 7) return ANS_ERR_INVALID_ARG;
   const uint64_t work = std::max<uint64_t>(d.rows, d.n_seqs) / (2 * kPgThreads);
   const uint32_t blocks = work < 1 ? 1 : work < 2 ? 2 : work < 4 ? 4 : 8;
-  const size_t smem = 2 * (size_t(d.n_seqs) + 1) * sizeof(uint32_t);
+  const size_t smem = 3 * (size_t(d.n_seqs) + 1) * sizeof(uint32_t);
+  const int rc = allow_smem<ans_page_tables_kernel>(3 * (ANS_MAX_SEQS + 1) * sizeof(uint32_t));
+  if (rc != ANS_OK) return rc;
   return launch(ans_page_tables_kernel, dim3(blocks), dim3(kPgThreads), smem, static_cast<cudaStream_t>(stream), blocks, d, d_status);
 }
