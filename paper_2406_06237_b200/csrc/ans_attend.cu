@@ -33,8 +33,8 @@ struct ArShape {
   static constexpr uint32_t kRow = D + 4;                             // floats of a query's sums in shared memory
   static constexpr uint32_t kSums = kArWarps * kQueries * kRow * 4;
   static constexpr uint32_t kBody = kRing > kSums ? kRing : kSums;
-  // then: a stage's scales, the warps' maxima and sums, the sequences' first chunks
-  static constexpr uint32_t kMeta = kArWarps * kArStages * 16;
+  // then: where a warp's tiles lie and their scales, the warps' maxima and sums, the sequences' first chunks
+  static constexpr uint32_t kMeta = kArWarps * 64 * 16;
   static constexpr uint32_t kMl = kArWarps * kQueries * 8 + kQueries * 8 + kArWarps * kQueries * 4;
   static constexpr uint32_t kSmem = kBody + kMeta + kMl;              // + 4 (n + 1)
 };
@@ -104,14 +104,15 @@ __device__ __forceinline__ uint32_t ar_plus(uint32_t x, uint32_t y) { return min
 // The workspace: a record for each block, then for each block two slots of kQueries x (D sums, maximum, sum).
 struct ArRecord { uint32_t seq, unit, last, live; };
 
-template <int D, int NT>
+// EXACT: heads are of D dimensions, so that a tile's 16 pieces lie constants apart.
+template <int D, int NT, bool EXACT>
 __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_rows_kernel(const AttendArgs a) {
   using S = ArShape<D, NT>;
   constexpr uint32_t Q = S::kQueries;
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
   float* const sums = reinterpret_cast<float*>(smem);
-  float2* const meta = reinterpret_cast<float2*>(smem + S::kBody) + warp * kArStages * 2;       // {kscale, vscale}, {1 if used, -}
+  uint4* const tiles = reinterpret_cast<uint4*>(smem + S::kBody) + warp * 64;           // of chunk c: [c % 64] {place in the codes, kscale, log2 vscale}
   float2* const ml = reinterpret_cast<float2*>(smem + S::kBody + S::kMeta);            // [warp][query] {maximum, sum}
   float2* const total_ml = ml + kArWarps * Q;                                          // [query]
   float* const weight = reinterpret_cast<float*>(total_ml + Q);                        // [warp][query]
@@ -183,53 +184,50 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
     const int32_t* const table = a.b.tables + s * a.b.table_stride;
 
     // this warp's tokens: 16 of each chunk; where a tile begins in the codes, and its scales, for 32 chunks at a time
-    uint64_t where = 0;
-    float k_scale = 0.f, v_scale = 0.f;
-    uint32_t used = 0, known = c0;                     // chunks known .. known + 31
-    auto look = [&](uint32_t from) {
-      known = from;
-      used = 0;
-      const uint32_t c = from + lane, token = q.begin + c * kArChunk + warp * 16u;
+    uint32_t known = c0;                               // chunks before it are in the table
+    const uint32_t dim = EXACT ? D : a.c.dim;
+    auto look = [&]() {
+      const uint32_t c = known + lane, token = q.begin + c * kArChunk + warp * 16u;
+      uint64_t where = ~uint64_t(0);                   // not there
+      float ks = 0.f, e = 0.f;
       if (c < c1 && token < static_cast<uint32_t>(q.length)) {
         const uint32_t in = token / a.c.page_size;
         const int32_t page = table[in];
         if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {
           const uint64_t block = uint64_t(page) * a.c.heads + head;
-          where = (block * a.c.page_size + (token - in * a.c.page_size)) * a.c.dim;
-          k_scale = usable(a.c.scales[0][block]);
-          v_scale = usable(a.c.scales[1][block]);
-          used = 1;
+          where = (block * a.c.page_size + (token - in * a.c.page_size)) * dim;
+          ks = usable(a.c.scales[0][block]);
+          e = log2_near(usable(a.c.scales[1][block]));
         } else {
           atomicOr(a.status, ANS_STATUS_BAD_PAGE);
         }
       }
+      tiles[c % 64u] = make_uint4(static_cast<uint32_t>(where), static_cast<uint32_t>(where >> 32), __float_as_uint(ks), __float_as_uint(e));
+      known += 32u;
+      __syncwarp();
     };
+    // a lane's pieces of a tile: D / 32 of 16 codes of K and of V, kDown rows apart
+    constexpr uint32_t kDown = 512 / D;
+    const uint32_t row0 = lane / (D / 16), x0 = lane % (D / 16), lane_at = row0 * dim + x0 * 16u, in = x0 * 16u < dim ? 16u : 0u;
     auto fetch = [&](uint32_t c, uint32_t stage) {     // chunk c's tile into a stage
       if (c < c1) {
-        if (c - known >= 32u) look(c);
-        const uint32_t from = c - known;
-        const uint64_t p = __shfl_sync(kAll, where, from);
-        const float ks = __shfl_sync(kAll, k_scale, from), vs = __shfl_sync(kAll, v_scale, from);
-        const uint32_t u = __shfl_sync(kAll, used, from);
-        if (lane == 0) {
-          meta[2 * stage] = make_float2(ks, vs);
-          meta[2 * stage + 1].x = static_cast<float>(u);
-        }
-        if (u) {
+        if (c >= known) look();
+        const uint4 tile = tiles[c % 64u];
+        if ((tile.x & tile.y) != 0xFFFFFFFFu) {
+          const uint64_t at = (uint64_t(tile.y) << 32 | tile.x) + (EXACT || in ? lane_at : 0u);
+          const int8_t* const k = a.c.codes[0] + at;
+          const int8_t* const v = a.c.codes[1] + at;
           const uint32_t to = ring + stage * S::kStage;
 #pragma unroll
-          for (uint32_t i = 0; i < D / 32; ++i) {      // 16 rows of D / 16 pieces
-            const uint32_t piece = lane + 32u * i, row = piece / (D / 16), x = piece % (D / 16);
-            const uint32_t in = x * 16u < a.c.dim ? 16u : 0u;
-            const uint64_t from_at = in ? p + row * a.c.dim + x * 16u : 0u;
-            copy16(to + k_piece<D>(row, x), a.c.codes[0] + from_at, in);
-            copy16(to + 16u * D + v_piece<D>(row, x), a.c.codes[1] + from_at, in);
+          for (uint32_t i = 0; i < D / 32; ++i) {
+            const uint32_t row = row0 + kDown * i, far = EXACT || in ? kDown * i * dim : 0u;
+            copy16(to + k_piece<D>(row, x0), k + far, EXACT ? 16u : in);
+            copy16(to + 16u * D + v_piece<D>(row, x0), v + far, EXACT ? 16u : in);
           }
         }
       }
       copies_end();
     };
-    look(c0);
 #pragma unroll
     for (uint32_t i = 0; i + 1 < kArStages; ++i) fetch(c0 + i, i);
 
@@ -303,8 +301,8 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       copies_wait<kArStages - 1>();
       __syncwarp();
       const int32_t token = static_cast<int32_t>(q.begin + c * kArChunk + warp * 16u);
-      const float2 scales = meta[2 * stage];
-      if (meta[2 * stage + 1].x != 0.f && token < any_hi) {
+      const uint4 tile = tiles[c % 64u];
+      if ((tile.x & tile.y) != 0xFFFFFFFFu && token < any_hi) {
         const uint32_t keys = ring + stage * S::kStage, values = keys + 16u * D;
         float sc[NT][4];
 #pragma unroll
@@ -322,7 +320,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
             for (int m = 0; m < NT; ++m) mma16(sc[m], a0, a1, a2, a3, qf[m][4 * i + j][0], qf[m][4 * i + j][1]);
           }
         }
-        const float e = log2_near(scales.y), back = exp2_near(-e - kUp);
+        const float e = __uint_as_float(tile.w), back = exp2_near(-e - kUp);
         const bool inside = token >= all_lo && token + 16 <= all_hi;
         uint32_t p[NT][2];
 #pragma unroll
@@ -330,7 +328,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
           float best[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                // columns 2t + k: values k (token g) and k + 2 (token g + 8)
-            const float f = factor[m][k] * scales.x;
+            const float f = factor[m][k] * __uint_as_float(tile.z);
             sc[m][k] = fmaf(sc[m][k], f, e);
             sc[m][k + 2] = fmaf(sc[m][k + 2], f, e);
             if (!inside) {
@@ -543,11 +541,17 @@ static void plan_shape(const AttendArgs& a, uint32_t longest, int sms, ArPlan& p
 template <int D, int NT>
 static int launch_rows(const AttendArgs& a, const ArPlan& p, cudaStream_t st) {
   using S = ArShape<D, NT>;
-  constexpr auto kernel = ans_attend_rows_kernel<D, NT>;
   constexpr size_t most = S::kSmem + 4 * (ANS_MAX_SEQS + 1);
   static_assert(most <= 227 * 1024, "");
-  int rc = allow_smem<kernel>(most);
-  if (rc == ANS_OK) rc = launch(kernel, dim3(p.blocks), dim3(kArThreads), S::kSmem + 4 * (size_t(a.b.n_seqs) + 1), st, 1, a);
+  const size_t smem = S::kSmem + 4 * (size_t(a.b.n_seqs) + 1);
+  int rc;
+  if (a.c.dim == D) {
+    rc = allow_smem<ans_attend_rows_kernel<D, NT, true>>(most);
+    if (rc == ANS_OK) rc = launch(ans_attend_rows_kernel<D, NT, true>, dim3(p.blocks), dim3(kArThreads), smem, st, 1, a);
+  } else {
+    rc = allow_smem<ans_attend_rows_kernel<D, NT, false>>(most);
+    if (rc == ANS_OK) rc = launch(ans_attend_rows_kernel<D, NT, false>, dim3(p.blocks), dim3(kArThreads), smem, st, 1, a);
+  }
   if (rc == ANS_OK && p.join) rc = launch(ans_attend_join_kernel<D, NT>, dim3(p.blocks, S::kQueries / 8), dim3(128), 0, st, 1, a, p.blocks);
   return rc;
 }
