@@ -183,26 +183,36 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
     const uint32_t rows = q.fresh * a.share, r0 = group * Q, live = min(Q, rows - r0);
     const int32_t* const table = a.b.tables + s * a.b.table_stride;
 
-    // this warp's tokens: 16 of each chunk; where a tile begins in the codes, and its scales, for 32 chunks at a time
-    uint32_t known = c0;                               // chunks before it are in the table
+    // this warp's tokens: 16 of each chunk; where a tile begins in the codes, and its scales, for 32 chunks at a time: the places
+    // first, so that copies begin while the scales are on their way
+    uint32_t known = c0, scaled = c0;                  // chunks before them have their places, their scales in the table
     const uint32_t dim = EXACT ? D : a.c.dim;
+    float k_of = 0.f, v_of = 0.f;
+    auto scales = [&]() {
+      if (scaled == known) return;
+      float* const to = reinterpret_cast<float*>(tiles + (scaled + lane) % 64u);
+      to[2] = usable(k_of);
+      to[3] = log2_near(usable(v_of));
+      scaled = known;
+      __syncwarp();
+    };
     auto look = [&]() {
+      scales();
       const uint32_t c = known + lane, token = q.begin + c * kArChunk + warp * 16u;
       uint64_t where = ~uint64_t(0);                   // not there
-      float ks = 0.f, e = 0.f;
       if (c < c1 && token < static_cast<uint32_t>(q.length)) {
         const uint32_t in = token / a.c.page_size;
         const int32_t page = table[in];
         if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {
           const uint64_t block = uint64_t(page) * a.c.heads + head;
           where = (block * a.c.page_size + (token - in * a.c.page_size)) * dim;
-          ks = usable(a.c.scales[0][block]);
-          e = log2_near(usable(a.c.scales[1][block]));
+          k_of = a.c.scales[0][block];
+          v_of = a.c.scales[1][block];
         } else {
           atomicOr(a.status, ANS_STATUS_BAD_PAGE);
         }
       }
-      tiles[c % 64u] = make_uint4(static_cast<uint32_t>(where), static_cast<uint32_t>(where >> 32), __float_as_uint(ks), __float_as_uint(e));
+      *reinterpret_cast<uint2*>(tiles + c % 64u) = make_uint2(static_cast<uint32_t>(where), static_cast<uint32_t>(where >> 32));
       known += 32u;
       __syncwarp();
     };
@@ -212,7 +222,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
     auto fetch = [&](uint32_t c, uint32_t stage) {     // chunk c's tile into a stage
       if (c < c1) {
         if (c >= known) look();
-        const uint4 tile = tiles[c % 64u];
+        const uint2 tile = *reinterpret_cast<const uint2*>(tiles + c % 64u);
         if ((tile.x & tile.y) != 0xFFFFFFFFu) {
           const uint64_t at = (uint64_t(tile.y) << 32 | tile.x) + (EXACT || in ? lane_at : 0u);
           const int8_t* const k = a.c.codes[0] + at;
@@ -228,26 +238,34 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       }
       copies_end();
     };
+    // queries, on their way with the first tiles: column g of each 8; row r of the group is new token (r0 + r) / share, query head
+    // (r0 + r) % share of the head
+    uint4 qw[NT][D / 32];
+#pragma unroll
+    for (int m = 0; m < NT; ++m) {
+      const uint32_t r = 8u * m + g;
+      const uint32_t i = token_of(a, r0 + min(r, live - 1u)), j = (r0 + min(r, live - 1u)) - i * a.share;
+      const __nv_bfloat16* const from = a.q + (q.row + i) * a.q_token + (head * a.share + j) * a.q_head;
+#pragma unroll
+      for (uint32_t x = 0; x < D / 32; ++x) {          // 8 values: half x % 2 of dims 64 (x / 2) + 16 t
+        const uint32_t d = 64u * (x / 2) + 16u * t + 8u * (x % 2);
+        qw[m][x] = make_uint4(0, 0, 0, 0);
+        if (d < dim && r < live) qw[m][x] = *reinterpret_cast<const uint4*>(from + d);
+      }
+    }
 #pragma unroll
     for (uint32_t i = 0; i + 1 < kArStages; ++i) fetch(c0 + i, i);
 
-    // queries: column g of each 8; row r of the group is new token (r0 + r) / share, query head (r0 + r) % share of the head
     uint32_t qf[NT][D / 16][2];
     float factor[NT][2];                               // of the lane's columns 2t and 2t + 1 of S^T
     int32_t lo[NT][2], hi[NT][2];
     int32_t all_lo = 0, all_hi = 0x7FFFFFFF, any_hi = 0;     // tokens that all rows see, and end of those that one does
 #pragma unroll
     for (int m = 0; m < NT; ++m) {
-      const uint32_t r = 8u * m + g;
-      uint4 w[D / 32];
+      const uint4 (&w)[D / 32] = qw[m];
       uint32_t top = 0;
-      const uint32_t i = token_of(a, r0 + min(r, live - 1u)), j = (r0 + min(r, live - 1u)) - i * a.share;
-      const __nv_bfloat16* const from = a.q + (q.row + i) * a.q_token + (head * a.share + j) * a.q_head;
 #pragma unroll
-      for (uint32_t x = 0; x < D / 32; ++x) {          // 8 values: half x % 2 of dims 64 (x / 2) + 16 t
-        const uint32_t d = 64u * (x / 2) + 16u * t + 8u * (x % 2);
-        w[x] = make_uint4(0, 0, 0, 0);
-        if (d < a.c.dim && r < live) w[x] = *reinterpret_cast<const uint4*>(from + d);
+      for (uint32_t x = 0; x < D / 32; ++x) {
         const uint32_t* const e = &w[x].x;
 #pragma unroll
         for (int k = 0; k < 4; ++k) top = max(top, max((e[k] << 16) & 0x7FFFFFFFu, e[k] & 0x7FFF0000u));
@@ -298,6 +316,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
     uint32_t stage = 0;
     for (uint32_t c = c0; c < c1; ++c) {
       fetch(c + kArStages - 1u, stage == 0 ? kArStages - 1u : stage - 1u);
+      if (c >= scaled) scales();
       copies_wait<kArStages - 1>();
       __syncwarp();
       const int32_t token = static_cast<int32_t>(q.begin + c * kArChunk + warp * 16u);
@@ -471,57 +490,134 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
   if (a.parts && threadIdx.x == 0) *record = mine;
 }
 
-// Joins the parts of the units that begin in one block and end in another: block x has the unit that record x names.
-template <int D, int NT>
-__global__ void __launch_bounds__(128) ans_attend_join_kernel(const AttendArgs a, uint32_t blocks) {
-  constexpr uint32_t Q = 8 * NT;
+// Joins the parts of the units that begin in one block and end in another: blockIdx.x has the unit that this record names, blockIdx.y a row
+// of it, whose slots the block's warps share (ALONE: four rows, a warp each).
+constexpr uint32_t kAjWarps = 4;
+template <int D, int NT, bool ALONE>
+__global__ void __launch_bounds__(32 * kAjWarps) ans_attend_join_kernel(const AttendArgs a, uint32_t blocks) {
+  constexpr uint32_t Q = 8 * NT, kMany = 4, kTogether = D == 256 ? 4 : 8;
+  __shared__ float2 found[kAjWarps][32 * kMany];       // {slot's number, weight} of a warp
+  __shared__ float2 parts_ml[kAjWarps];
+  __shared__ __align__(16) float parts[kAjWarps][D];
   let_next_start();
   wait_for_previous();
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   const ArRecord rec = reinterpret_cast<const ArRecord*>(a.parts)[blockIdx.x];
   if (!rec.live) return;
+  const float* const slots = a.parts + blocks * (sizeof(ArRecord) / 4);
   bool unused = false;
   const ArSeq q = ar_sequence<Q>(a, rec.seq, unused);
-  const uint32_t head = rec.unit / q.groups, group = rec.unit - head * q.groups;
+  const uint32_t head = rec.unit / q.groups, group = rec.unit - head * q.groups, count = rec.last - blockIdx.x + 1u;
   const uint32_t rows = q.fresh * a.share, r0 = group * Q, live = min(Q, rows - r0);
-  const float* const slots = a.parts + blocks * (sizeof(ArRecord) / 4);
-  const uint32_t lane = threadIdx.x & 31u;
-  auto slot = [&](uint32_t b) { return slots + uint64_t(2u * b + (b == blockIdx.x ? 1u : 0u)) * Q * (D + 2); };
-  for (uint32_t r = blockIdx.y * 4u + (threadIdx.x >> 5); r < live; r += 4u * gridDim.y) {       // a warp a row
-    float most = kLowest, all = 0.f;
-    for (uint32_t b = blockIdx.x + lane; b <= rec.last; b += 32) most = fmaxf(most, slot(b)[Q * D + 2 * r]);
-    for (uint32_t step = 1; step < 32; step *= 2) most = fmaxf(most, __shfl_xor_sync(kAll, most, step));
-    float x[D / 32];
+  auto slot = [&](uint32_t b) { return 2u * (blockIdx.x + b) + (b == 0 ? 1u : 0u); };
+  constexpr uint32_t kShare = ALONE ? 1 : kAjWarps;  // warps of a row
+  const uint32_t part = ALONE ? 0u : warp;
+  for (uint32_t r = ALONE ? blockIdx.y * kAjWarps + warp : blockIdx.y; r < live; r += gridDim.y * (kAjWarps / kShare)) {
+    float most = kLowest, all = 0.f, x[D / 32];
 #pragma unroll
     for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
-#pragma unroll 4
-    for (uint32_t b = blockIdx.x; b <= rec.last; ++b) {
-      const float* const p = slot(b);
-      const float2 m = *reinterpret_cast<const float2*>(p + Q * D + 2 * r);
-      const float f = exp2_near(m.x - most);
-      all = fmaf(f, m.y, all);
+    const uint32_t b1 = count * (part + 1u) / kShare;
+    for (uint32_t b0 = count * part / kShare; b0 < b1; b0 += 32 * kMany) {
+      float2 m[kMany];
 #pragma unroll
-      for (int k = 0; k < D / 64; ++k) {
-        const float2 v = *reinterpret_cast<const float2*>(p + r * D + 64 * k + 2 * lane);
-        x[2 * k] = fmaf(f, v.x, x[2 * k]);
-        x[2 * k + 1] = fmaf(f, v.y, x[2 * k + 1]);
+      for (uint32_t k = 0; k < kMany; ++k) {
+        const uint32_t b = b0 + 32u * k + lane;
+        m[k] = b < b1 ? *reinterpret_cast<const float2*>(slots + uint64_t(slot(b)) * Q * (D + 2) + Q * D + 2 * r) : make_float2(kLowest, 0.f);
       }
+      float top = most;
+#pragma unroll
+      for (uint32_t k = 0; k < kMany; ++k) top = fmaxf(top, m[k].x);
+#pragma unroll
+      for (uint32_t step = 1; step < 32; step *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, step));
+      const float shrink = exp2_near(most - top);
+      most = top;
+      all *= shrink;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) x[k] *= shrink;
+      uint32_t have = 0;
+      float own = 0.f;
+#pragma unroll
+      for (uint32_t k = 0; k < kMany; ++k) {
+        const bool some = m[k].y != 0.f;             // a NaN counts
+        const uint32_t some_of = __ballot_sync(kAll, some);
+        const float f = exp2_near(m[k].x - most);
+        if (some) {
+          found[warp][have + __popc(some_of & ((1u << lane) - 1u))] = make_float2(__uint_as_float(slot(b0 + 32u * k + lane)), f);
+          own = fmaf(f, m[k].y, own);
+        }
+        have += __popc(some_of);
+      }
+#pragma unroll
+      for (uint32_t step = 1; step < 32; step *= 2) own += __shfl_xor_sync(kAll, own, step);
+      all += own;
+      __syncwarp();
+      for (uint32_t e = 0; e < have; e += kTogether) {
+        float v[kTogether][D / 32], w[kTogether];
+#pragma unroll
+        for (uint32_t z = 0; z < kTogether; ++z) {
+          const float2 of = found[warp][min(e + z, have - 1u)];
+          w[z] = of.y;
+          const float* const at = slots + uint64_t(__float_as_uint(of.x)) * Q * (D + 2) + r * D + 2 * lane;
+#pragma unroll
+          for (int k = 0; k < D / 64; ++k) {
+            const float2 y = *reinterpret_cast<const float2*>(at + 64 * k);
+            v[z][2 * k] = y.x;
+            v[z][2 * k + 1] = y.y;
+          }
+        }
+#pragma unroll
+        for (uint32_t z = 0; z < kTogether; ++z)
+          if (e + z < have)
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) x[k] = fmaf(w[z], v[z][k], x[k]);
+      }
+      __syncwarp();
     }
-    const float f = all == 0.f ? 0.f : exp2_near(-kUp) / all;
     const uint32_t row = token_of(a, r0 + r), j = (r0 + r) - row * a.share;
     __nv_bfloat16* const to = a.out + (q.row + row) * a.out_token + (head * a.share + j) * a.out_head;
+    if constexpr (ALONE) {
+      const float f = all == 0.f ? 0.f : exp2_near(-kUp) / all;
 #pragma unroll
-    for (int k = 0; k < D / 64; ++k) {
-      const uint32_t d = 64u * k + 2u * lane;
-      if (d < a.c.dim) *reinterpret_cast<__nv_bfloat162*>(to + d) = __floats2bfloat162_rn(x[2 * k] * f, x[2 * k + 1] * f);
+      for (int k = 0; k < D / 64; ++k) {
+        const uint32_t d = 64u * k + 2u * lane;
+        if (d < a.c.dim) *reinterpret_cast<__nv_bfloat162*>(to + d) = __floats2bfloat162_rn(x[2 * k] * f, x[2 * k + 1] * f);
+      }
+      continue;
     }
+    if (lane == 0) parts_ml[warp] = make_float2(most, all);
+#pragma unroll
+    for (int k = 0; k < D / 64; ++k) *reinterpret_cast<float2*>(&parts[warp][64 * k + 2 * lane]) = make_float2(x[2 * k], x[2 * k + 1]);
+    __syncthreads();
+    most = kLowest;
+    all = 0.f;
+#pragma unroll
+    for (uint32_t w = 0; w < kAjWarps; ++w) most = fmaxf(most, parts_ml[w].x);
+    float f[kAjWarps];
+#pragma unroll
+    for (uint32_t w = 0; w < kAjWarps; ++w) {
+      f[w] = exp2_near(parts_ml[w].x - most);
+      all = fmaf(f[w], parts_ml[w].y, all);
+    }
+    const float over = all == 0.f ? 0.f : exp2_near(-kUp) / all;
+    for (uint32_t d = 2u * threadIdx.x; d < a.c.dim; d += 64 * kAjWarps) {
+      float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+      for (uint32_t w = 0; w < kAjWarps; ++w) {
+        y0 = fmaf(f[w], parts[w][d], y0);
+        y1 = fmaf(f[w], parts[w][d + 1], y1);
+      }
+      *reinterpret_cast<__nv_bfloat162*>(to + d) = __floats2bfloat162_rn(y0 * over, y1 * over);
+    }
+    __syncthreads();
   }
-}
+  }
 
 // ---- host side -----------------------------------------------------------------------------
 struct ArPlan {
   uint32_t tiles;                                      // queries in eights
   uint32_t blocks;
   bool join;                                           // a unit may lie in several blocks
+  uint32_t units, rows;                                // by the caller's numbers: units, rows of a unit
   size_t room;
 };
 
@@ -535,6 +631,8 @@ static void plan_shape(const AttendArgs& a, uint32_t longest, int sms, ArPlan& p
   p.blocks = static_cast<uint32_t>(std::min<uint64_t>(all, uint64_t(sms) * (D * NT <= 128 ? 2 : 1)));
   p.join = chunks > 1;
   p.tiles = NT;
+  p.units = static_cast<uint32_t>(std::min<uint64_t>(groups * a.c.heads * a.b.n_seqs, 1u << 28));
+  p.rows = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(longest) * a.share, S::kQueries));
   p.room = p.join ? size_t(p.blocks) * (sizeof(ArRecord) + 2 * S::kQueries * (D + 2) * sizeof(float)) : 0;
 }
 
@@ -552,7 +650,10 @@ static int launch_rows(const AttendArgs& a, const ArPlan& p, cudaStream_t st) {
     rc = allow_smem<ans_attend_rows_kernel<D, NT, false>>(most);
     if (rc == ANS_OK) rc = launch(ans_attend_rows_kernel<D, NT, false>, dim3(p.blocks), dim3(kArThreads), smem, st, 1, a);
   }
-  if (rc == ANS_OK && p.join) rc = launch(ans_attend_join_kernel<D, NT>, dim3(p.blocks, S::kQueries / 8), dim3(128), 0, st, 1, a, p.blocks);
+  if (rc != ANS_OK || !p.join) return rc;
+  // a warp a row where units lie in few blocks, up to 8 on average
+  rc = p.blocks <= 8 * p.units ? launch(ans_attend_join_kernel<D, NT, true>, dim3(p.blocks, (p.rows + kAjWarps - 1) / kAjWarps), dim3(32 * kAjWarps), 0, st, 1, a, p.blocks)
+                               : launch(ans_attend_join_kernel<D, NT, false>, dim3(p.blocks, p.rows), dim3(32 * kAjWarps), 0, st, 1, a, p.blocks);
   return rc;
 }
 
