@@ -8,7 +8,8 @@
 // past a power of two.
 //
 // A block of threads has one (sequence, page, head) of the keys or of the values: the new values' largest magnitude, the scale,
-// the codes; the values are read again for the second pass (out of L1: 32 KB at most).  Bound by the bytes where prompts are written,
+// the codes.  The values are held in registers between the two, 64 a thread, which is all of a page of 64 tokens of 128 dimensions; what
+// a larger page has more is read again (7700 tokens of 8 heads of 128: 15.1 us held, 18.0 read again).  Bound by the bytes where prompts are written,
 // by latency (numbers of the sequence, page number, values, codes: four trips) for single tokens.
 #include <cmath>
 
@@ -26,31 +27,31 @@ struct BlockWriteArgs {
   uint32_t* status;
 };
 
-// Eight values from p on as fp32.
+// Eight values from p on, as they lie, and as fp32.
+template <typename T> struct Eight { uint32_t w[2 * sizeof(T)]; };
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, uint32_t wide, float (&v)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    uint32_t w[4];
-    if (wide) {
-      const uint4 u = *reinterpret_cast<const uint4*>(p);
-      w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-    } else {
-      const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
+__device__ __forceinline__ Eight<T> load8(const T* p, uint32_t wide) {
+  Eight<T> s;
+  if (wide) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = e[2 * i] | static_cast<uint32_t>(e[2 * i + 1]) << 16;
+    for (uint32_t h = 0; h < sizeof(T) / 2; ++h) {
+      const uint4 u = reinterpret_cast<const uint4*>(p)[h];
+      s.w[4 * h] = u.x; s.w[4 * h + 1] = u.y; s.w[4 * h + 2] = u.z; s.w[4 * h + 3] = u.w;
     }
+  } else if constexpr (sizeof(T) == 2) {
+    const uint16_t* e = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-  } else if (wide) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    for (int i = 0; i < 4; ++i) s.w[i] = e[2 * i] | static_cast<uint32_t>(e[2 * i + 1]) << 16;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p[i];
+    for (int i = 0; i < 8; ++i) s.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
   }
+  return s;
+}
+template <typename T>
+__device__ __forceinline__ float value_of(const Eight<T>& s, int i) {
+  if constexpr (sizeof(T) == 2) return __uint_as_float(i % 2 ? s.w[i / 2] & 0xFFFF0000u : s.w[i / 2] << 16);
+  else return __uint_as_float(s.w[i]);
 }
 
 // The scale for a largest magnitude, given as its bits; NaN for an infinity or a NaN.
@@ -105,14 +106,28 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   float* const scale_at = a.c.scales[which] + block;
   const float before = from ? *scale_at : 0.f;
 
+  // a thread's pieces of eight values: token t, values c .. c + 7, the next one kBwThreads pieces on
+  const uint32_t down = kBwThreads / across, right = kBwThreads % across, t0 = threadIdx.x / across, c0 = threadIdx.x % across;
+  auto move = [&](uint32_t& t, uint32_t& c) {
+    t += down;
+    c += right;
+    if (c >= across) { c -= across; ++t; }
+  };
+  constexpr uint32_t kHeld = 16 / sizeof(T);
+  Eight<T> held[kHeld];
   uint32_t top = 0;
-  for (uint32_t i = threadIdx.x; i < pieces; i += kBwThreads) {
-    const uint32_t t = i / across, c = (i - t * across) * 8u;
-    float v[8];
-    load8(x + t * a.token_stride[which] + c, a.wide[which], v);
+  auto look = [&](const Eight<T>& s) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7FFFFFFFu);
-  }
+    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(value_of<T>(s, k)) & 0x7FFFFFFFu);
+  };
+  uint32_t t = t0, c = c0;
+#pragma unroll
+  for (uint32_t n = 0; n < kHeld; ++n, move(t, c))
+    if (t < to - from) held[n] = load8(x + t * a.token_stride[which] + 8u * c, a.wide[which]);
+  for (; t < to - from; move(t, c)) look(load8(x + t * a.token_stride[which] + 8u * c, a.wide[which]));
+#pragma unroll
+  for (uint32_t n = 0; n < kHeld; ++n)
+    if (threadIdx.x + n * kBwThreads < pieces) look(held[n]);
   top = __reduce_max_sync(kAll, top);
   if (lane == 0) s_top[warp] = top;
   __syncthreads();                                     // the old scale is read
@@ -127,18 +142,21 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   const bool sound = !isnan(scale);
   const float per = 1.f / scale;                       // exact: a power of two, but for scales that others have written
   constexpr float kMagic = 12582912.f;                 // 1.5 * 2^23: rint(v) in the low bits of v + kMagic, |v| < 2^22
-  for (uint32_t i = threadIdx.x; i < pieces; i += kBwThreads) {
-    const uint32_t t = i / across, c = (i - t * across) * 8u;
-    float v[8];
-    load8(x + t * a.token_stride[which] + c, a.wide[which], v);
+  auto put = [&](const Eight<T>& s) {
     uint32_t w[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = sound ? __float_as_uint(fmaf(v[j], per, kMagic)) : 0u;
+    for (int k = 0; k < 8; ++k) w[k] = sound ? __float_as_uint(fmaf(value_of<T>(s, k), per, kMagic)) : 0u;
     uint2 out;
     out.x = __byte_perm(__byte_perm(w[0], w[1], 0x40), __byte_perm(w[2], w[3], 0x40), 0x5410);
     out.y = __byte_perm(__byte_perm(w[4], w[5], 0x40), __byte_perm(w[6], w[7], 0x40), 0x5410);
-    *reinterpret_cast<uint2*>(codes + (from + t) * dim + c) = out;
-  }
+    *reinterpret_cast<uint2*>(codes + (from + t) * dim + 8u * c) = out;
+  };
+  t = t0;
+  c = c0;
+#pragma unroll
+  for (uint32_t n = 0; n < kHeld; ++n, move(t, c))
+    if (t < to - from) put(held[n]);
+  for (; t < to - from; move(t, c)) put(load8(x + t * a.token_stride[which] + 8u * c, a.wide[which]));
   if (from && sound && scale > before) {               // the tokens before them, rounded to the larger scale
     const float shrink = before * per;
     for (uint32_t i = threadIdx.x; i < from * across; i += kBwThreads) {
