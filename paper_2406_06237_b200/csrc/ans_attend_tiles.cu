@@ -28,32 +28,26 @@ namespace blk {
 constexpr float kUpTile = 7.f, kSlack = 8.f;           // P <= 2^15
 constexpr float kLeastFactor = 1e-38f;                 // of S, so that -inf times it is -inf
 constexpr uint32_t kAtSoft = 8, kAtOpen = 4, kAtIssue = kAtSoft + kAtOpen, kAtScales = kAtIssue + 1;   // warps: softmax, converters, issuer, scales
-constexpr uint32_t kAtThreads = 32 * (kAtScales + 3);       // and two idle, as registers move by four warps
+constexpr uint32_t kAtThreads = 32 * (kAtScales + 1);
 
 template <int D>
 struct AtShape {
   static constexpr uint32_t kHalves = D <= 128 ? 2 : 1;
   static constexpr uint32_t kRows = 128 * kHalves;
-  static constexpr uint32_t kTokens = D <= 128 ? 128 : 64;             // of a block
+  static constexpr uint32_t kTokens = 64;                              // of a block
   static constexpr uint32_t kPanels = D / 64;                          // of 64 dimensions, 128 bytes
   static constexpr uint32_t kQPanel = 128 * 128, kPanel = kTokens * 128;
   static constexpr uint32_t kQ = kHalves * kPanels * kQPanel;
   static constexpr uint32_t kTile = kPanels * kPanel;                  // K or V of a block
-  static constexpr uint32_t kStages = 2;
+  static constexpr uint32_t kStages = D == 256 ? 2 : 4;
   static constexpr uint32_t kSubs = kTokens / 16;                      // runs of 16 tokens, each in one page
   static constexpr uint32_t kMeta = kStages * kSubs * 16;
-  static constexpr uint32_t kBars = 8 * (4 * kStages + 3 * kHalves + 2);
+  static constexpr uint32_t kBars = 8 * (4 * kStages + 4 * kHalves + 2);
   static constexpr uint32_t kSmem = 1024 + kQ + 2 * kStages * kTile + kMeta + kBars + 16;
   static constexpr uint32_t kOwn = kTokens / kAtOpen, kRuns = kOwn / 16;         // tokens and runs of a converter's warp
   static constexpr uint32_t kPieces = kOwn / 8 * kPanels;              // of 16 codes, of a converter's lane
-  static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory; halves 128 and D apart
+  static constexpr uint32_t kS = 0, kO = 256;                          // columns in tensor memory: a half's two blocks of S, 64 apart; O; halves 128 and D apart
 };
-
-// Registers a thread: the launch brings 128 for 512 threads.
-__device__ __forceinline__ void regs_soft() { asm volatile("setmaxnreg.inc.sync.aligned.u32 176;"); }
-__device__ __forceinline__ void regs_open() { asm volatile("setmaxnreg.dec.sync.aligned.u32 104;"); }
-__device__ __forceinline__ void regs_issue() { asm volatile("setmaxnreg.dec.sync.aligned.u32 56;"); }
-static_assert(256 * 176 + 128 * 104 + 128 * 56 <= kAtThreads * 128, "");
 
 __device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
 __device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -64,11 +58,6 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
-}
-__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-               :: "r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-                  "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]));
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
@@ -129,7 +118,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   const uint32_t q_at = base, k_at = q_at + S::kQ, v_at = k_at + S::kStages * S::kTile, meta = v_at + S::kStages * S::kTile;
   const uint32_t bars = meta + S::kMeta;
   const uint32_t k_full = bars, k_empty = k_full + 8 * S::kStages, v_full = k_empty + 8 * S::kStages, v_empty = v_full + 8 * S::kStages;
-  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 8 * S::kHalves, q_full = p_full + 16 * S::kHalves, o_full = q_full + 8;
+  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 16 * S::kHalves, o_done = p_full + 8 * S::kHalves, q_full = o_done + 8 * S::kHalves, o_full = q_full + 8;
   const uint32_t slot = o_full + 8;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   uint32_t bad = 0;
@@ -141,7 +130,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       bar_init(k_full + 8 * s, kAtOpen); bar_init(k_empty + 8 * s, 1);
       bar_init(v_full + 8 * s, kAtOpen + 1); bar_init(v_empty + 8 * s, 1);
     }
-    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 8 * h, 1); bar_init(p_full + 16 * h, 4); bar_init(p_full + 16 * h + 8, 4); }
+    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 16 * h, 1); bar_init(s_full + 16 * h + 8, 1); bar_init(p_full + 8 * h, 4); bar_init(o_done + 8 * h, 1); }
     bar_init(q_full, 4 * S::kHalves);
     bar_init(o_full, 1);
     bar_init_fence();
@@ -201,7 +190,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
 
   if (mine && warp < kAtSoft) {
     // ---- softmax: a row a thread
-    regs_soft();
     const uint32_t half = warp >> 2, row = T.r0 + threadIdx.x;
     if (half < halves) {
       const bool live = threadIdx.x < T.live;
@@ -249,11 +237,12 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       const Seen seen = seen_by(a, T.old, T.length, i);
       const int32_t all_lo = __reduce_max_sync(kAll, seen.first), all_hi = __reduce_min_sync(kAll, seen.end);
       const uint32_t lanes = (warp & 3u) << 21;        // this warp's 32 lanes of tensor memory
-      const uint32_t s_at = tmem + lanes + S::kS + half * 128u, o_at = tmem + lanes + S::kO + half * D;
+      const uint32_t s_both = tmem + lanes + S::kS + half * 128u, o_at = tmem + lanes + S::kO + half * D;
       float top = kLowest, sum = 0.f;
       for (uint32_t n = 0; n < blocks; ++n) {
         const uint32_t stage = n % S::kStages;
-        bar_wait(s_full + 8 * half, n & 1u, bad);
+        const uint32_t s_at = s_both + (n & 1u) * 64u;
+        bar_wait(s_full + 16 * half + 8 * (n & 1u), (n >> 1) & 1u, bad);
         bar_wait(v_full + 8 * stage, (n / S::kStages) & 1u, bad);      // the scales
         __syncwarp();
         fence_after();
@@ -286,6 +275,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           top = now;
           sum *= shrink;
           if (n) {
+            bar_wait(o_done + 8 * half, (n - 1u) & 1u, bad);           // the products before are done; the next ones wait for P
+            __syncwarp();
+            fence_after();
 #pragma unroll 1
             for (uint32_t c = 0; c < D; c += 32) {
               uint32_t o[32];
@@ -324,18 +316,14 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
             }
             const Two both = add2(part[0], part[1]);
             sum = fmaf(low(both) + high(both), back, sum);
-            if (b % (S::kSubs / 2) == S::kSubs / 2 - 1) {              // half of P is ready
-              constexpr uint32_t kHalf = S::kTokens / 4;               // columns of it
-              const uint32_t h = b / (S::kSubs / 2);
-              tmem_store(s_at + h * kHalf, *reinterpret_cast<uint32_t(*)[kHalf]>(v + h * kHalf));
-              tmem_stored();
-              fence_before();
-              __syncwarp();
-              if (lane == 0) arrive(p_full + 16 * half + 8 * h);
-            }
           }
         };
         if (inside) weigh(std::true_type{}); else weigh(std::false_type{});
+        tmem_store(s_at, *reinterpret_cast<uint32_t(*)[32]>(v));       // P over S, which has been read
+        tmem_stored();
+        fence_before();
+        __syncwarp();
+        if (lane == 0) arrive(p_full + 8 * half);
       }
       bar_wait(o_full, 0u, bad);
       __syncwarp();
@@ -416,7 +404,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     }
   } else if (mine && warp < kAtIssue) {
     // ---- converters: a warp has kOwn tokens of every block, one or two runs of 16
-    regs_open();
     // A lane has piece lane % 4 (16 codes) of each panel of every eighth token: the two chunks of 8 dimensions that it becomes have the
     // same places in every panel and every eight tokens, and four lanes by two tokens write to different banks.
     const uint32_t w = warp - kAtSoft, row0 = lane / 4u, c = lane % 4u;
@@ -493,7 +480,6 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     }
   } else if (mine && warp == kAtScales) {
     // ---- scales: lane b has run b of every block
-    regs_issue();
     float ks, e, back;
     auto look = [&](uint32_t block) {
       const uint32_t token = block * S::kTokens + lane * 16u;
@@ -521,55 +507,52 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       if (lane == 0) arrive(v_full + 8 * stage);
     }
   } else if (mine) {
-    regs_issue();
     if (warp == kAtIssue) {
       // ---- issuer: the whole warp waits, one lane issues
       const uint32_t me = elect();
       constexpr uint32_t is = instruction_half(S::kTokens, false), io = instruction_half(D, true);
-      auto scores = [&](uint32_t h, uint32_t stage) {
+      auto scores = [&](uint32_t h, uint32_t n) {
+        const uint32_t stage = n % S::kStages;
 #pragma unroll
         for (uint32_t p = 0; p < S::kPanels; ++p) {
           const uint64_t dq = operand(q_at + (h * S::kPanels + p) * S::kQPanel), dk = operand(k_at + stage * S::kTile + p * S::kPanel);
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) mma_smem(me, tmem + S::kS + h * 128u, dq + 2u * k, dk + 2u * k, is, p || k);
+          for (uint32_t k = 0; k < 4; ++k) mma_smem(me, tmem + S::kS + h * 128u + (n & 1u) * 64u, dq + 2u * k, dk + 2u * k, is, p || k);
         }
-        commit(me, s_full + 8 * h);
+        commit(me, s_full + 16 * h + 8 * (n & 1u));
       };
-      auto outputs = [&](uint32_t h, uint32_t part, uint32_t stage, bool more) {      // of half of the block's tokens
-        constexpr uint32_t kSteps = S::kTokens / 32;
-        const uint64_t dv = operand_across(v_at + stage * S::kTile, S::kPanel) + uint64_t(part * kSteps * 2048u >> 4);
-        const uint32_t p = tmem + S::kS + h * 128u + 8u * kSteps * part;
+      auto outputs = [&](uint32_t h, uint32_t n) {
+        const uint64_t dv = operand_across(v_at + n % S::kStages * S::kTile, S::kPanel);
+        const uint32_t p = tmem + S::kS + h * 128u + (n & 1u) * 64u;
 #pragma unroll
-        for (uint32_t k = 0; k < kSteps; ++k)
-          mma_tmem(me, tmem + S::kO + h * D, p + 8u * k, dv + uint64_t(k * 2048u >> 4), io, more || part || k);
+        for (uint32_t k = 0; k < S::kTokens / 16; ++k)
+          mma_tmem(me, tmem + S::kO + h * D, p + 8u * k, dv + uint64_t(k * 2048u >> 4), io, n || k);
+        commit(me, o_done + 8 * h);
       };
       for (uint32_t h = 0; h < S::kHalves; ++h)
         if (h >= halves) for (uint32_t i = 0; i < 4; ++i) { if (lane == 0) arrive(q_full); }            // a half without rows
       bar_wait(q_full, 0u, bad);
+      // S of the next block is made while the softmax of this one runs
+      if (blocks) {
+        bar_wait(k_full, 0u, bad);
+        fence_after();
+        for (uint32_t h = 0; h < halves; ++h) scores(h, 0);
+        commit(me, k_empty);
+      }
       for (uint32_t n = 0; n < blocks; ++n) {
-        const uint32_t stage = n % S::kStages, parity = (n / S::kStages) & 1u;
-        if (n == 0) {
-          bar_wait(k_full, 0u, bad);
-          fence_after();
-          for (uint32_t h = 0; h < halves; ++h) scores(h, 0);
-          commit(me, k_empty);
-        }
-        bar_wait(v_full + 8 * stage, parity, bad);
-        const uint32_t next = (n + 1) % S::kStages;
+        const uint32_t stage = n % S::kStages, next = (n + 1) % S::kStages;
         for (uint32_t h = 0; h < halves; ++h) {
-#pragma unroll
-          for (uint32_t part = 0; part < 2; ++part) {
-            bar_wait(p_full + 16 * h + 8 * part, n & 1u, bad);
-            fence_after();
-            outputs(h, part, stage, n > 0);
-          }
-          if (h + 1 == halves) commit(me, v_empty + 8 * stage);
           if (n + 1 < blocks) {
             if (h == 0) bar_wait(k_full + 8 * next, ((n + 1) / S::kStages) & 1u, bad);
             fence_after();
-            scores(h, next);
+            scores(h, n + 1);
             if (h + 1 == halves) commit(me, k_empty + 8 * next);
           }
+          if (h == 0) bar_wait(v_full + 8 * stage, (n / S::kStages) & 1u, bad);
+          bar_wait(p_full + 8 * h, n & 1u, bad);
+          fence_after();
+          outputs(h, n);
+          if (h + 1 == halves) commit(me, v_empty + 8 * stage);
         }
       }
       commit(me, o_full);
