@@ -637,6 +637,7 @@ static int launch_tiles_shape(const AttendArgs& a, const AtPlan& p, cudaStream_t
   using S = AtShape<D>;
   constexpr auto kernel = ans_attend_tiles_kernel<D>;
   static_assert(S::kSmem <= 227 * 1024, "");
+  if (uint64_t(a.c.heads) * p.tiles > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   int rc = allow_smem<kernel>(S::kSmem);
   if (rc == ANS_OK) rc = launch(kernel, dim3(a.c.heads * p.tiles, 1, p.splits), dim3(kAtThreads), S::kSmem, st, 1, a, p.splits);
   if (rc == ANS_OK && p.splits > 1) {

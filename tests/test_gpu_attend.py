@@ -110,6 +110,21 @@ def test_a_nan_block_is_seen_only_by_rows_that_see_it(new, which):
     assert got[sees][:, 2:].isnan().all() and torch.equal(got[:, :2], clean[:, :2]) and torch.equal(got[~sees], clean[~sees])
 
 
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_query_that_is_not_finite_stays_in_its_row(new, bad):
+    lengths = [100 + new, 300 + new]
+    tables, n_pages = tables_for(lengths, 16)
+    arrays = fill_cache(n_pages, 2, 16, 64)
+    cache, q = BlockCache.wrap(*arrays), queries(2 * new, 8, 64)
+    clean = cache.attend(q, tables, ints(lengths), ints([0, new, 2 * new]))
+    q[new // 2, 3, 5] = bad
+    got = cache.attend(q, tables, ints(lengths), ints([0, new, 2 * new]))
+    assert got[new // 2, 3].isnan().all()
+    got[new // 2, 3] = clean[new // 2, 3]
+    assert torch.equal(got, clean) and cache.read_status() == 0
+
+
 def test_strides_alignment_and_in_place():
     lengths, starts = [70, 300], [0, 5, 40]
     tables, n_pages = tables_for(lengths, 16)
