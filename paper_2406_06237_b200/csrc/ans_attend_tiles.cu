@@ -13,8 +13,9 @@
 // slots of each of the four schedulers, and opening the codes 320.
 // V is the operand as it lies in the cache, tokens x dimensions ("MN-major"), so nothing is transposed.
 //
-// S of the next block goes over P of this one: the products of one issuer are done in order, and P's was issued before.  For the same
-// reason O may be rescaled by whoever has seen S of the next block.  Where there are fewer tiles than SMs, several blocks have parts
+// A half has two places for S, in turn, with a barrier for S and one for P each: a warp whose rows need no rescaling may be a block ahead of
+// another of its half, and must not count for it.  S of block n + 2 goes over P of block n: the products of one issuer are done in
+// order, and P's was issued before.  O is rescaled when the products of the block before are done, which a barrier tells.  Where there are fewer tiles than SMs, several blocks have parts
 // of a tile's tokens and a second kernel joins them.
 #include <algorithm>
 #include <type_traits>
@@ -42,7 +43,7 @@ struct AtShape {
   static constexpr uint32_t kStages = D == 256 ? 2 : 4;
   static constexpr uint32_t kSubs = kTokens / 16;                      // runs of 16 tokens, each in one page
   static constexpr uint32_t kMeta = kStages * kSubs * 16;
-  static constexpr uint32_t kBars = 8 * (4 * kStages + 4 * kHalves + 2);
+  static constexpr uint32_t kBars = 8 * (4 * kStages + 5 * kHalves + 2);
   static constexpr uint32_t kSmem = 1024 + kQ + 2 * kStages * kTile + kMeta + kBars + 16;
   static constexpr uint32_t kOwn = kTokens / kAtOpen, kRuns = kOwn / 16;         // tokens and runs of a converter's warp
   static constexpr uint32_t kPieces = kOwn / 8 * kPanels;              // of 16 codes, of a converter's lane
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
   const uint32_t q_at = base, k_at = q_at + S::kQ, v_at = k_at + S::kStages * S::kTile, meta = v_at + S::kStages * S::kTile;
   const uint32_t bars = meta + S::kMeta;
   const uint32_t k_full = bars, k_empty = k_full + 8 * S::kStages, v_full = k_empty + 8 * S::kStages, v_empty = v_full + 8 * S::kStages;
-  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 16 * S::kHalves, o_done = p_full + 8 * S::kHalves, q_full = o_done + 8 * S::kHalves, o_full = q_full + 8;
+  const uint32_t s_full = v_empty + 8 * S::kStages, p_full = s_full + 16 * S::kHalves, o_done = p_full + 16 * S::kHalves, q_full = o_done + 8 * S::kHalves, o_full = q_full + 8;
   const uint32_t slot = o_full + 8;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
   uint32_t bad = 0;
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       bar_init(k_full + 8 * s, kAtOpen); bar_init(k_empty + 8 * s, 1);
       bar_init(v_full + 8 * s, kAtOpen + 1); bar_init(v_empty + 8 * s, 1);
     }
-    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 16 * h, 1); bar_init(s_full + 16 * h + 8, 1); bar_init(p_full + 8 * h, 4); bar_init(o_done + 8 * h, 1); }
+    for (uint32_t h = 0; h < S::kHalves; ++h) { bar_init(s_full + 16 * h, 1); bar_init(s_full + 16 * h + 8, 1); bar_init(p_full + 16 * h, 4); bar_init(p_full + 16 * h + 8, 4); bar_init(o_done + 8 * h, 1); }
     bar_init(q_full, 4 * S::kHalves);
     bar_init(o_full, 1);
     bar_init_fence();
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
         tmem_stored();
         fence_before();
         __syncwarp();
-        if (lane == 0) arrive(p_full + 8 * half);
+        if (lane == 0) arrive(p_full + 16 * half + 8 * (n & 1u));
       }
       bar_wait(o_full, 0u, bad);
       __syncwarp();
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
             if (h + 1 == halves) commit(me, k_empty + 8 * next);
           }
           if (h == 0) bar_wait(v_full + 8 * stage, (n / S::kStages) & 1u, bad);
-          bar_wait(p_full + 8 * h, n & 1u, bad);
+          bar_wait(p_full + 16 * h + 8 * (n & 1u), (n >> 1) & 1u, bad);
           fence_after();
           outputs(h, n);
           if (h + 1 == halves) commit(me, v_empty + 8 * stage);

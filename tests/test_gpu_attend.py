@@ -166,6 +166,25 @@ def test_results_do_not_vary_and_a_graph_serves_other_lengths():
     assert rounds_from(out, want, slack).all() and cache.read_status() == 0
 
 
+@pytest.mark.parametrize("dim,window", [(128, 1024), (64, 300), (256, 500), (128, 0)])
+def test_long_prompts_again_and_again(dim, window):
+    """Warps of a tile that are at different blocks: rows whose window hides a block rescale while others go on."""
+    new, page = [1635 - 62 * i for i in range(13)], 64
+    lengths, starts = [m + 2 * i for i, m in enumerate(new)], sums(new)
+    tables, n_pages = tables_for(lengths, page)
+    arrays = fill_cache(n_pages, 2, page, dim, spread=12)
+    cache, q = BlockCache.wrap(*arrays), queries(starts[-1], 14, dim, size=3.0)
+    a, b = ints(lengths), ints(starts)
+    want = cache.attend(q, tables, a, b, window=window)
+    for _ in range(40):
+        assert torch.equal(cache.attend(q, tables, a, b, window=window), want)
+    assert cache.read_status() == 0
+    for s in (0, 12):                                    # the first and the last of them against the definition
+        r0, r1 = starts[s], starts[s + 1]
+        exact, slack = attention(q[r0:r1], arrays, tables[s:s + 1], lengths[s:s + 1], [0, r1 - r0], window=window)
+        assert rounds_from(want[r0:r1], exact, slack).all()
+
+
 def test_pages_outside_the_cache_count_as_not_there():
     arrays = fill_cache(6, 2, 16, 64)
     cache, q = BlockCache.wrap(*arrays), queries(41, 4, 64)
