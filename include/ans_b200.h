@@ -644,8 +644,8 @@ int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_d
 /*
  * Attention of the batch's new tokens over the cache (which holds them already):
  *   out[t][j] = sum_i p_i v_i / sum_i p_i,   p_i = exp(scale * q[t][j] . k_i),   k, v of head j / (q_heads / heads),
- * over the tokens i that row t sees: with `causal` those up to its own position, with `window` > 0 only the last `window`
- * of these; without `causal` all of the sequence's tokens (the states of an encoder; window = 0).  A row that sees nothing is 0.
+ * over the tokens i that row t sees: with `causal` those up to its own position, without it all of the sequence's tokens (the
+ * states of an encoder); with `window` > 0 only the last `window` of these.  A row that sees nothing is 0.
  * q and out bf16, rows x q_heads x head_dim, the values of a head contiguous; d_q and its strides on 16 bytes, d_out on 4.
  * d_out may be d_q (same strides).  Sums and the softmax's maximum and sum are in fp32; p meets the codes as an
  * fp16 number scaled by a power of two (p_i times the scale of its block of values is off by 2^-11 of itself, or by 2^-32 of the largest such

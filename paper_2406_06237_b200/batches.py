@@ -241,7 +241,7 @@ class BlockCache(_Handle):
                causal: bool = True, window: int = 0, longest: int | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
         """Attention of the batch's new tokens over the cache, which holds them already.  q: [rows, query heads, head_dim] bf16,
         query heads a multiple of the cache's; scale: of the logits, head_dim ** -0.5 unless given.  causal: a token sees
-        itself and what is before it, the last `window` of these if that is not 0; else all of its sequence's tokens.
+        itself and what is before it, else all of its sequence's tokens; the last `window` of these if that is not 0.
         longest: the most new tokens of a request, if known on the host (results do not depend on it, time does).
         Returns out, bf16, of q's shape; the given buffer if there is one, which may be q.  Rows that see nothing are 0, rows
         behind the last request's are not written."""
@@ -278,7 +278,7 @@ class BlockCache(_Handle):
         _need(out.data_ptr() != q.data_ptr() or out.stride() == q.stride(), "out lies over q with other strides")
         _on_device(q, self.device, "q")
         _on_device(out, self.device, "out")
-        _need(window >= 0 and (causal or window == 0), "a window needs causal attention")
+        _need(window >= 0, "window must not be negative")
         _need(longest is None or longest > 0, "longest must be positive")
         self._batch(self._attend_batch, tables, lengths, starts, q.shape[0])
         d.q_token_stride, d.q_head_stride, d.out_token_stride, d.out_head_stride = *q.stride()[:2], *out.stride()[:2]

@@ -90,7 +90,7 @@ def attend(status=P, **kw):
 @pytest.mark.parametrize("kw,rc", CACHE_CASES + [
     (dict(d_q=None), INVALID), (dict(d_out=None), INVALID), (dict(d_q=P + 8), INVALID), (dict(d_out=P + 2), INVALID), (dict(q_token_stride=260), INVALID),
     (dict(q_head_stride=68), INVALID), (dict(out_head_stride=65), INVALID), (dict(q_heads=3), INVALID), (dict(q_heads=0), INVALID), (dict(q_heads=258), UNSUPPORTED),
-    (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(causal=0, window=5), INVALID), (dict(d_out=P, out_token_stride=512), INVALID),
+    (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(d_out=P, out_token_stride=512), INVALID),
     (dict(q_token_stride=FAR), UNSUPPORTED), (dict(rows=(1 << 31) - 1), UNSUPPORTED)])
 def test_attend(kw, rc):
     assert attend(**kw) == rc

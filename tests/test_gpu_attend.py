@@ -41,7 +41,7 @@ CASES = [                                                # heads, share, dim, pa
 
 
 @pytest.mark.parametrize("heads,share,dim,page,cached,new", CASES)
-@pytest.mark.parametrize("how", [dict(), dict(window=1), dict(window=100), dict(causal=False)])
+@pytest.mark.parametrize("how", [dict(), dict(window=1), dict(window=100), dict(causal=False), dict(causal=False, window=70)])
 def test_against_the_definition(heads, share, dim, page, cached, new, how):
     lengths, starts = [b + m for b, m in zip(cached, new)], sums(new)
     tables, n_pages = tables_for(lengths, page)
