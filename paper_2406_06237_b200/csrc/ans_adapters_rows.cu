@@ -4,6 +4,8 @@
 // the inputs and a part of the outputs; its part of B goes into shared memory (cp.async) while its part of A is multiplied out of registers.
 // One multiply-add an element on the plain units, in fp32: with one row the matrix instructions would work on 15 rows of zeros
 // and cost more instructions around them than they save.  The blocks' sums meet through distributed shared memory in the order of the ranks.
+// 64 rows of 8192 inputs and 8192 outputs at rank 16 (36 MB of adapters): 12.9 us, 6.3 of which an empty launch of the
+// same clusters takes; one row 5.0.
 #include <cuda_fp16.h>
 
 #include "ans_adapters.cuh"

@@ -1,22 +1,29 @@
 // Attention over the block-scaled cache for many queries a head of the cache (prompts, chunks of prompts), on the
 // fifth-generation tensor cores.
 //
-// A block of threads has a tile of rows (new tokens x query heads of one head of the cache), one or two halves of 128, and goes over
-// the tokens that they see, BN at a time.  Its warps:
-//   4 converters:   codes from global memory, opened to fp16, into shared memory as operands (two stages of K and V);
+// A block of threads has a tile of rows (new tokens x query heads of one head of the cache), one or two halves of 128, and
+// goes over the tokens that they see, 64 at a time.  Its warps:
+//   4 converters:   codes from global memory, opened to fp16, into shared memory as operands (four stages of K and V, two
+//                   for 256 dimensions);
 //   1 for scales:   of the runs of 16 tokens, as the softmax uses them;
 //   1 issuer:       S = Q K^T into tensor memory, then O += P V with P out of tensor memory;
-//   4 a half:       the softmax of a row a thread: S out of tensor memory, P over it as fp16, O rescaled there when the row's maximum
-//                   has grown by more than 2^kSlack since it was last.
-// While one half's softmax runs, the other half's products do: per BN = 128 tokens of D = 128 the two halves' four
-// products take 2048 clocks, their 32768 exponentials the same (16 a clock), the arithmetic around them 900 issue
-// slots of each of the four schedulers, and opening the codes 320.
+//   4 a half:       the softmax of a row a thread: S out of tensor memory, P over it as fp16, O rescaled there when the row's
+//                   maximum has grown by more than 2^kSlack since it was last.
 // V is the operand as it lies in the cache, tokens x dimensions ("MN-major"), so nothing is transposed.
 //
-// A half has two places for S, in turn, with a barrier for S and one for P each: a warp whose rows need no rescaling may be a block ahead of
-// another of its half, and must not count for it.  S of block n + 2 goes over P of block n: the products of one issuer are done in
-// order, and P's was issued before.  O is rescaled when the products of the block before are done, which a barrier tells.  Where there are fewer tiles than SMs, several blocks have parts
-// of a tile's tokens and a second kernel joins them.
+// For 64 tokens of 128 dimensions the two halves' four products take 1024 clocks of the tensor pipe and their 16384
+// exponentials as many (16 a clock).  What bounds is neither but a half's own chain, about 2100 clocks: S out of tensor
+// memory, the row's maximum, exponentials, P back, each waiting for the one before with one warp a scheduler and half.  A
+// prompt of 4096 (32 query heads on 8, D = 128) takes 172 us, 800 TFLOP/s of the products that causal order leaves; 1024 new
+// tokens behind 16 k to 64 k cached ones 875 us.  Blocks of 128 tokens with one place for S and two stages took 184 and
+// 938.  Measured and not taken: a part of the exponentials by a polynomial on the plain units (170 and 868 at best), 16
+// softmax warps with half a row a thread (a tenth slower), an issuer that takes whichever product is ready (the same).
+//
+// A half has two places for S, in turn, with a barrier for S and one for P each: a warp whose rows need no rescaling may be
+// a block ahead of another of its half, and must not count for it.  S of block n + 2 goes over P of block n: the products of
+// one issuer are done in order, and P's was issued before.  O is rescaled when the products of the block before are done,
+// which a barrier tells.  Where there are fewer tiles than SMs, several blocks have parts of a tile's tokens and a second
+// kernel joins them.
 #include <algorithm>
 #include <type_traits>
 
