@@ -5,7 +5,7 @@
 // part of the inputs, up to eight parts a tile, into the caller's room; the second adds the parts in their order and streams y through the product
 // with B.  With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64 rows: bound by the bytes, so the plain
 // matrix instructions are enough.  h meets B as the sum of two bf16 numbers, h = hi + lo, |h - hi - lo| <= 2^-17 |h|: a second
-// product, which costs less than the rounding of h to 8 bits would lose.  5005 rows of 8192 in e4m3, rank 32, 8192 outputs take
+// product, which costs less than the rounding of h to 8 bits would lose.  5507 rows of 8192 in e4m3, rank 32, 8192 outputs take
 // 80.5 us, 24 of them the first kernel and 57 the second (2.5 TB/s of y and out; bound by latency and by issue at 24 warps an SM, 47 %
 // of its issue slots used).  Rows without a ragged edge (EXACT) have a form without questions at each access, 180
 // instructions a tile of outputs where the general one has 600: 91 us without it.  One kernel with a cluster a tile, whose

@@ -14,8 +14,8 @@
 // evenly over the blocks that fit the GPU at once, and what a block has of a unit that others have parts of goes to a
 // workspace, which a second kernel joins in the order of the blocks: results do not depend on timing.
 //
-// Measured: one new token each of 64 requests with 1 k to 8 k cached (32 query heads on 8, D = 128; 149 MB) 40.5 us, 3.7 TB/s; one
-// request of 32768 tokens 21.8 us.  What bounds is the issue of instructions and their latency at 4 warps a scheduler: the
+// Measured: one new token each of 64 requests with 762 to 1500 cached (32 query heads on 8, D = 128; 149 MB) 40.5 us, 3.7 TB/s;
+// one request of 32768 tokens 21.8 us.  What bounds is the issue of instructions and their latency at 4 warps a scheduler: the
 // first takes 19 us with the copies alone, about as long with the arithmetic alone, and the beginnings and ends of
 // units 7 to 9; the join is 3 to 4 of both.  Not faster: two runs of 16 tokens at a time a warp (45.3 and 39.2: fewer bytes
 // under way), dealing over warps instead of blocks (42.5 and 23.4: more parts to join).

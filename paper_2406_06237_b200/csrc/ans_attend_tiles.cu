@@ -14,8 +14,8 @@
 // For 64 tokens of 128 dimensions the two halves' four products take 1024 clocks of the tensor pipe and their 16384
 // exponentials as many (16 a clock).  What bounds is neither but a half's own chain, about 2100 clocks: S out of tensor
 // memory, the row's maximum, exponentials, P back, each waiting for the one before with one warp a scheduler and half.  A
-// prompt of 4096 (32 query heads on 8, D = 128) takes 172 us, 800 TFLOP/s of the products that causal order leaves; 1024 new
-// tokens behind 16 k to 64 k cached ones 875 us.  Blocks of 128 tokens with one place for S and two stages took 184 and
+// prompt of 4096 (32 query heads on 8, D = 128) takes 172 us, 800 TFLOP/s of the products that causal order leaves; five chunks
+// of 1229 to 2048 behind 3601 to 6001 cached ones 875 us, 843.  Blocks of 128 tokens with one place for S and two stages took 184 and
 // 938.  Measured and not taken: a part of the exponentials by a polynomial on the plain units (170 and 868 at best), 16
 // softmax warps with half a row a thread (a tenth slower), an issuer that takes whichever product is ready (the same).
 //
