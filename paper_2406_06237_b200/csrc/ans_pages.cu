@@ -222,7 +222,6 @@ ANS_EXPORT int ans_page_tables(const ans_pages_desc* h_desc, uint32_t* d_status,
   if (d.n_seqs > ANS_MAX_SEQS || d.page_size > (1u << 20) || d.rows > kPgMost || d.n_free > kPgMost || d.table_pages > kPgMost ||
       d.table_stride > (uint64_t(1) << 40))
     return ANS_ERR_UNSUPPORTED;
-  if (d.n_seqs == 0 && d.rows == 0) return ANS_OK;
   if (d.n_seqs && (!d.d_cached || !d.d_new || !d.d_lengths || (!d.d_tables && d.table_pages) || (!d.d_free && d.n_free))) return ANS_ERR_INVALID_ARG;
   if (!d.d_taken || !d.d_taken_out || !d.d_starts || !d.d_ends || (d.rows && (!d.d_slots || !d.d_positions))) return ANS_ERR_INVALID_ARG;
   if (d.n_seqs > 1 && d.table_stride < d.table_pages) return ANS_ERR_INVALID_ARG;

@@ -29,7 +29,7 @@ def pages(status=P, **kw):
                                              "d_taken_out", "status")),
     *((dict([(f, P + 2)]), INVALID) for f in ("d_cached", "d_new", "d_free", "d_taken", "d_tables", "d_starts", "d_lengths", "d_ends", "d_positions", "d_taken_out")),
     (dict(d_slots=P + 4), INVALID), (dict(table_stride=7), INVALID), (dict(page_size=0), INVALID), (dict(page_size=(1 << 20) + 1), UNSUPPORTED),
-    (dict(n_seqs=4097), UNSUPPORTED), (dict(rows=1 << 31), UNSUPPORTED), (dict(table_stride=FAR), UNSUPPORTED), (dict(n_seqs=0, rows=0, d_starts=None), 0)])
+    (dict(n_seqs=4097), UNSUPPORTED), (dict(rows=1 << 31), UNSUPPORTED), (dict(table_stride=FAR), UNSUPPORTED), (dict(n_seqs=0, rows=0, d_starts=None), INVALID)])
 def test_page_tables(kw, rc):
     assert pages(**kw) == rc
 

@@ -134,3 +134,12 @@ def test_slots_and_ends_serve_the_paged_cache():
         e, m = int(got.ends[s + 1]), new[s]
         assert (back[e - m:e] - k[got.starts[s]:got.starts[s + 1]]).abs().max() < 0.05 if m else True
     assert cache.read_status() == 0
+
+
+def test_a_batch_without_requests_still_has_its_sums():
+    f = PageTables(16)
+    none, (starts, ends, taken) = ints([]), (ints([5]) for _ in range(3))
+    out = Batch(starts, none, ends, torch.empty(0, dtype=torch.int64, device="cuda"), none, taken)
+    f(torch.zeros(0, 4, dtype=INT, device="cuda"), none, none, ints([3, 1, 2]), ints([2]), out=out)
+    assert f.read_status() == 0
+    same(out, Batch([0], [], [0], [], [], [2]))
