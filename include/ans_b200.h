@@ -631,7 +631,8 @@ typedef struct ans_batch_desc {
  * contiguous, any alignment).  A block's scale is the least power of two, and at least 2^-40, that holds the largest
  * magnitude written to it in 127 steps, so that every code is a function of the values alone:
  *   code = rint(x / scale)  (to nearest even).
- * A block begins anew when its first token is written.  Where tokens are added behind others and need a larger scale,
+ * A block begins anew when its first token is written.  A scale that others have left there counts as at least 2^-40, as
+ * in the attention below.  Where tokens are added behind others and need a larger scale,
  * the codes before them are rounded to it, code' = rint(code * old / new).  Codes of the block's other places stay.
  * A NaN or an infinity makes its block's scale NaN (and the block's values of that head read as NaN) until it begins anew.
  * No two sequences may get new tokens in the same page.  A page number outside the cache, a sequence longer than its

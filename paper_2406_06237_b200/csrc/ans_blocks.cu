@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   const uint64_t block = uint64_t(page) * a.c.heads + head;
   int8_t* const codes = a.c.codes[which] + block * P * dim;
   float* const scale_at = a.c.scales[which] + block;
-  const float before = from ? *scale_at : 0.f;
+  const float before = from ? usable(*scale_at) : 0.f;
 
   // a thread's pieces of eight values: token t, values c .. c + 7, the next one kBwThreads pieces on
   const uint32_t down = kBwThreads / across, right = kBwThreads % across, t0 = threadIdx.x / across, c0 = threadIdx.x % across;

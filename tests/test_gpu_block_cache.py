@@ -75,6 +75,20 @@ def test_scales_of_others_are_kept_where_they_suffice():
     assert float(arrays[1][2, 0]) == pytest.approx(0.3) and float(arrays[3][2, 0]) == 2.0 ** -5
 
 
+@pytest.mark.parametrize("old", [2.0 ** -50, 0.0, -1.0])
+def test_scales_under_the_least_count_as_the_least(old):
+    arrays = fill_cache(2, 1, 16, 32)
+    codes = arrays[0][1, 0, :8].clone()
+    arrays[1][:] = old
+    cache = BlockCache.wrap(*arrays)
+    for top, keeps in ((2.0 ** -34, 1), (2.0 ** -33, 2)):                                  # 64 and 128 steps of 2^-40
+        x = torch.full((1, 1, 32), top, device="cuda")
+        cache.write(x, x, ints([[1]]), ints([9]), ints([0, 1]))
+        assert float(arrays[1][1, 0]) == keeps * 2.0 ** -40 and (arrays[0][1, 0, 8] == 64).all()
+        assert torch.equal(arrays[0][1, 0, :8], (codes.double() / keeps).round().to(torch.int8))
+    assert cache.read_status() == 0
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 def test_what_is_not_finite_makes_its_block_and_head_nan(bad):
     arrays = fill_cache(4, 2, 16, 32)
