@@ -712,7 +712,7 @@ static int plan_attend(const AttendArgs& a, uint32_t longest, AttendPlan& p) {
   if (longest == 0 || longest > a.b.rows) longest = a.b.rows;
   const uint64_t most = uint64_t(longest) * a.share;
   p.with_tiles = most > kBorder;
-  p.with_rows = !p.with_tiles || a.b.n_seqs > 1;
+  p.with_rows = !p.with_tiles || (a.b.n_seqs > 1 && a.share <= kBorder);          // a single token has `share` rows
   if (p.with_rows)                                     // beside the tiles, most others are single tokens
     rc = for_shape(a.c.dim, (p.with_tiles ? a.share : most) <= 8 ? 1 : 2, [&](auto d, auto nt) {
       plan_shape<d(), nt()>(a, p.with_tiles ? std::max(kBorder / a.share, 1u) : longest, sms, p.rows);

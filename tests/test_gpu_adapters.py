@@ -139,3 +139,16 @@ def test_graph_and_repeats():
     assert torch.equal(out, f(x, y, which, starts)) and not torch.equal(out, want)
     want, slack = definition(x, None, a, b, scales, y, [4, -1, 2], [0, 30, 31, 80])
     assert rounds_from(out, want, slack).all() and f.read_status() == 0
+
+
+def test_room_that_is_too_small_is_refused():
+    x, _, a, b, scales, y = make(3, 16, 512, 256, 40)
+    f = Adapters(a, b, scales)
+    f(x, y, ints([0, 2]), ints([0, 9, 40]))
+    torch.cuda.synchronize()
+    d = f._desc
+    for size, place in ((d.room_bytes - 1, d.d_room), (d.room_bytes, None)):
+        d.room_bytes, d.d_room = size, place
+        with pytest.raises(B.AnsError) as e:
+            B.ans_adapters(d, f._status)
+        assert e.value.code == B.ANS_ERR_BUFFER_TOO_SMALL

@@ -224,3 +224,29 @@ def test_another_stream():
         got = cache.attend(q, tables, lengths, starts)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [3, 90]])
+def test_room_that_is_too_small_is_refused(new):
+    lengths, starts = [3000, 4000], sums(new)
+    tables, n_pages = tables_for(lengths, 16)
+    cache = BlockCache.wrap(*fill_cache(n_pages, 2, 16, 128))
+    cache.attend(queries(starts[-1], 8, 128), tables, ints(lengths), ints(starts))
+    torch.cuda.synchronize()
+    d, b = cache._attend, cache._attend_batch
+    need = B.ans_attend_room_bytes(cache._desc, b, d)
+    assert need and d.room_bytes == need
+    d.room_bytes = need - 1
+    with pytest.raises(B.AnsError) as e:
+        B.ans_attend(cache._desc, b, d, cache._status)
+    assert e.value.code == B.ANS_ERR_BUFFER_TOO_SMALL
+    d.room_bytes, d.d_room = need, None
+    with pytest.raises(B.AnsError) as e:
+        B.ans_attend(cache._desc, b, d, cache._status)
+    assert e.value.code == B.ANS_ERR_BUFFER_TOO_SMALL
+
+
+def test_more_query_heads_than_the_border():
+    new, lengths = [1, 0, 7, 1], [500, 30, 7, 1]
+    tables, n_pages = tables_for(lengths, 32)
+    check(fill_cache(n_pages, 1, 32, 64), queries(sum(new), 40, 64), tables, lengths, sums(new))
