@@ -67,41 +67,76 @@ __device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, 
   return v;
 }
 
-// A tile of rows: tile numbers are dealt so that request s has starts[s] / rows + s and on, at least as many as it needs.
-struct AdTile {
-  uint64_t begin;                    // first row
-  uint32_t live;                     // rows; 0: none
-  int32_t which;                     // adapter, negative: none
-};
+// Tiles of ROWS rows, request by request, and what they consist of (inputs or outputs) in a row make a call's work, which is cut
+// into as many equal parts as there are blocks, so that none waits for the last wave: a block has the end of a tile and the
+// beginning of the next one, say.  first[s], in shared memory: tiles before request s's.  Returns all tiles.
 template <uint32_t ROWS>
-__device__ __forceinline__ AdTile ad_tile(const AdArgs& a, uint32_t tile, bool tell) {
-  __shared__ uint32_t s_seq;
-  if (threadIdx.x < 32) {
-    const uint32_t found = sequence_at(a.starts, a.n_seqs, 1u, ROWS, 1u, tile);
-    if (threadIdx.x == 0) s_seq = found;
+__device__ __forceinline__ uint32_t ad_tiles(const AdArgs& a, uint32_t* first, bool tell) {
+  __shared__ uint32_t part[kAdWarps];
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+  uint32_t total = 0;
+  bool bad = false;
+  for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += kAdThreads) {
+    const uint32_t s = s0 + threadIdx.x;
+    uint32_t x = 0;
+    if (s < a.n_seqs) {
+      const int32_t r0 = a.starts[s], r1 = a.starts[s + 1], i = a.which[s];
+      if (r0 < 0 || r1 < r0 || static_cast<uint32_t>(r1) > a.rows) {
+        bad = true;
+      } else {
+        const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
+        bad |= r1 > r0 && i >= 0 && none;
+        if (!none || a.out != a.y) x = (static_cast<uint32_t>(r1 - r0) + ROWS - 1) / ROWS;
+      }
+    }
+    const uint32_t own = x;
+#pragma unroll
+    for (uint32_t step = 1; step < 32; step *= 2) {
+      const uint32_t from = __shfl_up_sync(kAll, x, step);
+      if (lane >= step) x += from;
+    }
+    if (lane == 31) part[warp] = x;
+    __syncthreads();
+    uint32_t before = total;
+#pragma unroll
+    for (uint32_t w = 0; w < kAdWarps; ++w) {
+      if (w < warp) before += part[w];
+      total += part[w];
+    }
+    if (s < a.n_seqs) first[s] = before + x - own;
+    __syncthreads();
   }
+  if (threadIdx.x == 0) first[a.n_seqs] = total;
+  if (tell && bad) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
   __syncthreads();
-  const uint32_t s = s_seq;
-  const int32_t r0 = a.starts[s], r1 = a.starts[s + 1];
-  AdTile T{0, 0, a.which[s]};
-  if (tell) {                                          // what does not fit is found by one block
-    bool bad = false;
-    for (uint32_t k = threadIdx.x; k < a.n_seqs; k += kAdThreads)
-      bad |= a.starts[k] < 0 || a.starts[k + 1] < a.starts[k] || static_cast<uint32_t>(a.starts[k + 1]) > a.rows ||
-             (a.starts[k + 1] > a.starts[k] && a.which[k] >= 0 && static_cast<uint32_t>(a.which[k]) >= a.count);
-    if (bad) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
+  return total;
+}
+// the last request that has begun with or before the tile; first[0] <= tile < first[n]
+__device__ __forceinline__ uint32_t ad_request(const uint32_t* first, uint32_t n, uint32_t tile) {
+  uint32_t s = 0;
+  while (n - s > 1) {
+    const uint32_t mid = (s + n) / 2;
+    if (first[mid] <= tile) s = mid; else n = mid;
   }
-  const uint32_t place = static_cast<uint32_t>(max(r0, 0)) / ROWS + s;
-  if (r0 < 0 || r1 < r0 || static_cast<uint32_t>(r1) > a.rows || tile < place) return T;
-  T.begin = uint64_t(r0) + uint64_t(tile - place) * ROWS;
-  if (T.begin < static_cast<uint32_t>(r1)) T.live = static_cast<uint32_t>(min(uint64_t(ROWS), r1 - T.begin));
-  if (T.which >= 0 && static_cast<uint32_t>(T.which) >= a.count) T.which = -1;
-  return T;
+  return s;
+}
+// Block b's share of `all` pieces, `each` of them a tile: from piece `in` of `tile` on, `left` of them (fewer than 2^32: a piece has 512
+// elements of y, or of x, which is in memory).  And the block that has piece x.
+struct AdShare { uint32_t tile, in, left; };
+__device__ __forceinline__ AdShare ad_share(uint64_t all, uint32_t each, uint32_t blocks, uint32_t b) {
+  const uint64_t from = all * b / blocks, tile = from / each;
+  return {static_cast<uint32_t>(tile), static_cast<uint32_t>(from - tile * each), static_cast<uint32_t>(all * (b + 1u) / blocks - from)};
+}
+__device__ __forceinline__ uint32_t ad_block_of(uint64_t all, uint32_t blocks, uint64_t x) { return static_cast<uint32_t>(((x + 1u) * blocks + all - 1u) / all - 1u); }
+// Blocks that x A^T is dealt to: a tile's inputs then lie in `most` at most.  With shares of at least 1 / (most - 1) of a tile there are at
+// most most - 1 places between blocks behind a tile's first input.
+__device__ __forceinline__ uint32_t ad_down_blocks(uint32_t grid, uint32_t most, uint32_t tiles, uint32_t units) {
+  return static_cast<uint32_t>(min(uint64_t(grid), uint64_t(tiles) * min(most - 1u, units)));
 }
 
-// R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each.  blockIdx.y: the part of the inputs.
+// R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each; most: parts of a tile's sums.
 template <int R, int MT, bool F8, bool VEC>
-__global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapters_down_kernel(const AdArgs a) {
+__global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapters_down_kernel(const AdArgs a, const uint32_t most) {
   using S = AdShape<R, MT>;
   using X = std::conditional_t<F8, uint8_t, uint16_t>;
   constexpr uint32_t kUnit = F8 ? 64 : 32, kLane = kUnit / 4, kSteps = kUnit / 16;     // inputs of a unit, of a lane, products
@@ -112,18 +147,27 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
   let_next_start();
   wait_for_previous();
-  const AdTile T = ad_tile<S::kRows>(a, blockIdx.x, blockIdx.x == 0 && blockIdx.y == 0);
-  if (T.live == 0 || T.which < 0) return;
-  const uint32_t live = T.live, i = T.which;
-  const uint64_t begin = T.begin;
+  uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kDownSmem);             // [n_seqs + 1]
+  const uint32_t tiles = ad_tiles<S::kRows>(a, first, blockIdx.x == 0), units = (a.n_in + kUnit - 1) / kUnit;
+  const uint32_t blocks = ad_down_blocks(gridDim.x, most, tiles, units);
+  if (blockIdx.x >= blocks) return;
+  const uint64_t all = uint64_t(tiles) * units;
+  AdShare share = ad_share(all, units, blocks, blockIdx.x);
+  uint32_t s = ad_request(first, a.n_seqs, share.tile);
+  for (; share.left; ++share.tile, share.in = 0) {
+  const uint32_t tile = share.tile, u0 = share.in, u1 = u0 + min(units - u0, share.left);
+  share.left -= u1 - u0;
+  while (first[s + 1] <= tile) ++s;
+  const int32_t i = a.which[s];
+  if (i < 0 || static_cast<uint32_t>(i) >= a.count) continue;
+  const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
+  const uint64_t begin = uint64_t(a.starts[s]) + r0;
 
   float c[MT][NT][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
-  const uint32_t units = (a.n_in + kUnit - 1) / kUnit;
-  const uint32_t u0 = static_cast<uint32_t>(uint64_t(units) * blockIdx.y / gridDim.y), u1 = static_cast<uint32_t>(uint64_t(units) * (blockIdx.y + 1u) / gridDim.y);
   const X* x[MT][2];                                               // the lane's rows
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -182,7 +226,8 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
       *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
     }
   __syncthreads();
-  float* const h = a.room + (uint64_t(blockIdx.y) * a.rows + begin) * R;
+  const uint32_t part = blockIdx.x - ad_block_of(all, blocks, uint64_t(tile) * units);
+  float* const h = a.room + (uint64_t(part) * a.rows + begin) * R;
 #pragma unroll
   for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
     const uint32_t e = threadIdx.x + n * kAdThreads;
@@ -192,13 +237,15 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
     for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
     h[e] = sum;
   }
+  __syncthreads();                                     // the warps' sums are read
+  }
 }
 
-// blockIdx.y: the part of the outputs; `sums`: parts of the inputs.  EXACT: the rank is R, outputs come in whole groups of 32, and B, y
+// `most` and `down`: of the kernel before, its parts of a tile's sums and its grid.  EXACT: the rank is R, outputs come in whole groups of 32, and B, y
 // and out can be accessed 8 and 16 bytes at a time: addresses are then constants apart and nothing is asked (180 instructions a group
 // of 32 rows by 32 outputs where the general form takes 600).
 template <int R, int MT, bool EXACT>
-__global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_kernel(const AdArgs a, uint32_t sums) {
+__global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_kernel(const AdArgs a, const uint32_t most, const uint32_t down, const uint32_t down_units) {
   using S = AdShape<R, MT>;
   constexpr int KT = R / 16;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -208,19 +255,27 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
   uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + warp * S::kRing;
   let_next_start();
   wait_for_previous();
-  const AdTile T = ad_tile<S::kRows>(a, blockIdx.x, false);
-  const uint32_t live = T.live;
-  const int32_t i = T.which;
-  const uint64_t begin = T.begin;
-  const bool none = i < 0;
-  if (live == 0 || (none && a.out == a.y)) return;
+  uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kUpSmem);               // [n_seqs + 1]
+  const uint32_t tiles = ad_tiles<S::kRows>(a, first, false), groups = (a.n_out + 31u) / 32u;
+  const uint64_t all = uint64_t(tiles) * groups;
+  const uint32_t blocks = static_cast<uint32_t>(min(uint64_t(gridDim.x), (all + kAdWarps - 1) / kAdWarps));     // a group a warp at least
+  if (blockIdx.x >= blocks) return;
+  const uint32_t down_blocks = ad_down_blocks(down, most, tiles, down_units);
+  AdShare share = ad_share(all, groups, blocks, blockIdx.x);
+  uint32_t s = ad_request(first, a.n_seqs, share.tile);
+  for (; share.left; ++share.tile, share.in = 0) {
+  const uint32_t tile = share.tile, o0 = share.in, o1 = o0 + min(groups - o0, share.left);
+  share.left -= o1 - o0;
+  while (first[s + 1] <= tile) ++s;
+  const int32_t i = a.which[s];
+  const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
+  const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
+  const uint64_t begin = uint64_t(a.starts[s]) + r0;
 
-  const uint32_t groups = (a.n_out + 31u) / 32u;
-  const uint32_t o0 = static_cast<uint32_t>(uint64_t(groups) * blockIdx.y / gridDim.y), o1 = static_cast<uint32_t>(uint64_t(groups) * (blockIdx.y + 1u) / gridDim.y);
   // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
   // elements t R / 4 + 4 k and on of a row
   const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4), b_row = EXACT ? R : a.rank;
-  const __nv_bfloat16* const b_lane = a.b + (uint64_t(max(i, 0)) * a.n_out + b_out) * b_row + b_in;
+  const __nv_bfloat16* const b_lane = a.b + (uint64_t(none ? 0 : i) * a.n_out + b_out) * b_row + b_in;
   auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
     const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * b_row);
     const bool ours = o < o1 && !none;
@@ -285,9 +340,12 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
 #pragma unroll
   for (uint32_t n = 0; n < kBs; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
 
+  __syncthreads();                                     // the rows of h before are read
   if (!none) {
     const float scale = a.scales ? a.scales[i] : 1.f;
     const float* const h = a.room + begin * R;
+    const uint64_t all_units = uint64_t(tiles) * down_units, unit = uint64_t(tile) * down_units;
+    const uint32_t sums = ad_block_of(all_units, down_blocks, unit + down_units - 1u) - ad_block_of(all_units, down_blocks, unit) + 1u;
 #pragma unroll
     for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
       const uint32_t e = threadIdx.x + n * kAdThreads, row = e / R, k = e % R;
@@ -389,13 +447,15 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
       slot = slot + 1u == slots ? 0u : slot + 1u;
     }
   }
+  }
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // What a call with more rows than requests launches.
 struct AdPlan {
   int r, mt;                         // the rank as the kernels have it, and 16 rows each
-  uint32_t tiles, sums, parts;       // parts of the inputs and of the outputs
+  uint32_t down, up;                 // blocks
+  uint32_t most;                     // parts of a tile's sums
   size_t room;
 };
 static AdPlan plan_adapters(const ans_adapters_desc& d, int sms) {
@@ -403,14 +463,14 @@ static AdPlan plan_adapters(const ans_adapters_desc& d, int sms) {
   p.r = d.rank <= 16 ? 16 : d.rank <= 32 ? 32 : d.rank <= 64 ? 64 : 128;
   // tiles of 16 rows where requests have about as many, else of 32, if registers hold their sums
   p.mt = p.r == 128 || uint64_t(d.rows) <= 16ull * d.n_seqs ? 1 : 2;
-  p.tiles = d.rows / (16u * p.mt) + d.n_seqs;
-  // enough blocks for four an SM, as long as each warp has a unit of inputs, and four groups of outputs, to itself
-  const uint32_t units = (d.n_in + 63) / 64, groups = (d.n_out + 31) / 32, enough = 4u * sms;
-  p.sums = 1;
-  while (p.sums < 8 && uint64_t(p.tiles) * p.sums < enough && 2 * p.sums * kAdWarps <= units) p.sums *= 2;
-  p.parts = 1;
-  while (p.parts < 64 && uint64_t(p.tiles) * p.parts < enough && 2 * p.parts * kAdWarps <= groups) p.parts *= 2;
-  p.room = size_t(p.sums) * d.rows * p.r * sizeof(float);
+  const uint64_t tiles = d.rows / (16u * p.mt) + d.n_seqs;
+  // as many blocks as have their places on the GPU at once, as far as there is a group of outputs for each warp, and not
+  // more than 8 parts of a tile's inputs
+  p.up = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(sms) * (p.r <= 32 ? 3 : 2), (tiles * ((d.n_out + 31) / 32) + kAdWarps - 1) / kAdWarps));
+  p.down = uint64_t(sms) * (p.r * p.mt >= 128 ? 1 : 2);
+  p.most = static_cast<uint32_t>(std::min<uint64_t>(p.down / tiles + 2, 8));
+  p.down = static_cast<uint32_t>(std::min<uint64_t>(p.down, tiles * (p.most - 1)));
+  p.room = size_t(p.most) * d.rows * p.r * sizeof(float);
   return p;
 }
 
@@ -418,22 +478,23 @@ template <int R, int MT, bool F8, bool VEC>
 static int launch_down(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
   using S = AdShape<R, MT>;
   constexpr auto kernel = ans_adapters_down_kernel<R, MT, F8, VEC>;
-  const int rc = allow_smem<kernel>(S::kDownSmem);
-  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.sums), dim3(kAdThreads), S::kDownSmem, st, 1, a) : rc;
+  const int rc = allow_smem<kernel>(S::kDownSmem + 4 * (ANS_MAX_SEQS + 1));
+  return rc == ANS_OK ? launch(kernel, dim3(p.down), dim3(kAdThreads), S::kDownSmem + 4 * (a.n_seqs + 1), st, 1, a, p.most) : rc;
 }
 template <int R, int MT, bool EXACT>
-static int launch_up(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
+static int launch_up(const AdArgs& a, const AdPlan& p, uint32_t units, cudaStream_t st) {
   using S = AdShape<R, MT>;
   constexpr auto kernel = ans_adapters_up_kernel<R, MT, EXACT>;
-  const int rc = allow_smem<kernel>(S::kUpSmem);
-  return rc == ANS_OK ? launch(kernel, dim3(p.tiles, p.parts), dim3(kAdThreads), S::kUpSmem, st, 1, a, p.sums) : rc;
+  const int rc = allow_smem<kernel>(S::kUpSmem + 4 * (ANS_MAX_SEQS + 1));
+  return rc == ANS_OK ? launch(kernel, dim3(p.up), dim3(kAdThreads), S::kUpSmem + 4 * (a.n_seqs + 1), st, 1, a, p.most, p.down, units) : rc;
 }
 template <int R, int MT>
 static int launch_both(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
   const int rc = f8 ? (vec ? launch_down<R, MT, true, true>(a, p, st) : launch_down<R, MT, true, false>(a, p, st))
               : (vec ? launch_down<R, MT, false, true>(a, p, st) : launch_down<R, MT, false, false>(a, p, st));
   if (rc != ANS_OK) return rc;
-  return a.rank == R && a.n_out % 32 == 0 && a.b_wide && a.y_wide ? launch_up<R, MT, true>(a, p, st) : launch_up<R, MT, false>(a, p, st);
+  const uint32_t units = f8 ? (a.n_in + 63) / 64 : (a.n_in + 31) / 32;       // of inputs, as the first kernel has them
+  return a.rank == R && a.n_out % 32 == 0 && a.b_wide && a.y_wide ? launch_up<R, MT, true>(a, p, units, st) : launch_up<R, MT, false>(a, p, units, st);
 }
 static int launch_tiles_of(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
   switch (p.r) {
