@@ -30,8 +30,8 @@ struct AdShape {
   static constexpr uint32_t kSums = kRows * R;                       // of h
   static constexpr uint32_t kHRow = R + 8, kPart = kRows * (R + 8);  // elements of a row of h, of a warp's sums; + 8: eight rows in different banks
   static constexpr uint32_t kDownSmem = kAdWarps * kPart * 4;
-  // a warp's ring of groups of 32 outputs of y: two groups in bf16, one in fp32
-  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = 2 * kGroup;
+  // a warp's ring of groups of 32 outputs of y: four groups in bf16, two in fp32
+  static constexpr uint32_t kGroup = kRows * 32 * 2, kRing = 4 * kGroup;
   static constexpr uint32_t kUpSmem = 2 * kRows * kHRow * 2 + kAdWarps * kRing;
 };
 
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
 // and out can be accessed 8 and 16 bytes at a time: addresses are then constants apart and nothing is asked (180 instructions a group
 // of 32 rows by 32 outputs where the general form takes 600).
 template <int R, int MT, bool EXACT>
-__global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_kernel(const AdArgs a, const uint32_t most, const uint32_t down, const uint32_t down_units) {
+__global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const AdArgs a, const uint32_t most, const uint32_t down, const uint32_t down_units) {
   using S = AdShape<R, MT>;
   constexpr int KT = R / 16;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -363,6 +363,21 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
     __syncthreads();
   }
 
+  // h as the operand, in registers where they hold it
+  constexpr bool kHeld = MT * R <= 64;
+  uint2 held[kHeld ? MT : 1][kHeld ? KT : 1][4];
+  auto operand_of = [&](uint32_t m, uint32_t k, uint2 (&v)[4]) {
+    const uint32_t up = (16u * m + g) * S::kHRow + t * (R / 4) + 4u * k, dn = up + 8u * S::kHRow;
+    v[0] = *reinterpret_cast<const uint2*>(low + up); v[1] = *reinterpret_cast<const uint2*>(low + dn);
+    v[2] = *reinterpret_cast<const uint2*>(high + up); v[3] = *reinterpret_cast<const uint2*>(high + dn);
+  };
+  if constexpr (kHeld)
+    if (!none)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) operand_of(m, k, held[m][k]);
+
   uint32_t slot = 0;
   uint8_t* out_lane = out + (g * a.out_stride + 8u * t) * y_size + uint64_t(32u * y_size) * (o0 + warp);
   const uint64_t out_down = 8u * a.out_stride * y_size;
@@ -374,8 +389,8 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
       if (o >= o1) break;
       const uint32_t at = 32u * o + 8u * t;                          // the lane's outputs: at .. at + 7
       const bool wide = EXACT || (a.y_wide && at + 8 <= a.n_out);
-      if (slots == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else asm volatile("cp.async.wait_group 1;" ::: "memory");
       __syncwarp();
       const uint8_t* const staged = ring + slot * slot_bytes;
 #pragma unroll
@@ -386,13 +401,17 @@ __global__ void __launch_bounds__(kAdThreads, R <= 32 ? 3 : 2) ans_adapters_up_k
         if (!none) {
 #pragma unroll
           for (uint32_t k = 0; k < KT; ++k) {
-            const uint32_t e = t * (R / 4) + 4u * k, up = (16u * m + g) * S::kHRow + e, dn = up + 8u * S::kHRow;
-            const uint2 lu = *reinterpret_cast<const uint2*>(low + up), ld = *reinterpret_cast<const uint2*>(low + dn);
-            const uint2 hu = *reinterpret_cast<const uint2*>(high + up), hd = *reinterpret_cast<const uint2*>(high + dn);
+            uint2 v[4];
+            if constexpr (kHeld) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_bf16(d[j], lu.x, ld.x, lu.y, ld.y, bf[n][j][k][0], bf[n][j][k][1]);
+              for (int q = 0; q < 4; ++q) v[q] = held[m][k][q];
+            } else {
+              operand_of(m, k, v);
+            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_bf16(d[j], hu.x, hd.x, hu.y, hd.y, bf[n][j][k][0], bf[n][j][k][1]);
+            for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[2].x, v[3].x, v[2].y, v[3].y, bf[n][j][k][0], bf[n][j][k][1]);
           }
         }
 #pragma unroll
@@ -466,7 +485,7 @@ static AdPlan plan_adapters(const ans_adapters_desc& d, int sms) {
   const uint64_t tiles = d.rows / (16u * p.mt) + d.n_seqs;
   // as many blocks as have their places on the GPU at once, as far as there is a group of outputs for each warp, and not
   // more than 8 parts of a tile's inputs
-  p.up = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(sms) * (p.r <= 32 ? 3 : 2), (tiles * ((d.n_out + 31) / 32) + kAdWarps - 1) / kAdWarps));
+  p.up = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(sms) * 2, (tiles * ((d.n_out + 31) / 32) + kAdWarps - 1) / kAdWarps));
   p.down = uint64_t(sms) * (p.r * p.mt >= 128 ? 1 : 2);
   p.most = static_cast<uint32_t>(std::min<uint64_t>(p.down / tiles + 2, 8));
   p.down = static_cast<uint32_t>(std::min<uint64_t>(p.down, tiles * (p.most - 1)));
