@@ -39,6 +39,10 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_bf16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {       // onto zeros
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -396,8 +400,6 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         float d[4][4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
         if (!none) {
 #pragma unroll
           for (uint32_t k = 0; k < KT; ++k) {
@@ -409,7 +411,10 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
               operand_of(m, k, v);
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
+            for (int j = 0; j < 4; ++j) {
+              if (k == 0) mma_bf16_first(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
+              else mma_bf16(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[2].x, v[3].x, v[2].y, v[3].y, bf[n][j][k][0], bf[n][j][k][1]);
           }
