@@ -73,16 +73,17 @@ __device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, 
 
 // Tiles of ROWS rows, request by request, and what they consist of (inputs or outputs) in a row make a call's work, which is cut
 // into as many equal parts as there are blocks, so that none waits for the last wave: a block has the end of a tile and the
-// beginning of the next one, say.  first[s], in shared memory: tiles before request s's.  Returns all tiles.
+// beginning of the next one, say.  first[s], in shared memory: tiles before request s's, and returned all of them; x: those that have
+// an adapter, which are the first kernel's; y: those that get outputs, the second one's.  The first kernel has no place for y's.
 template <uint32_t ROWS>
-__device__ __forceinline__ uint32_t ad_tiles(const AdArgs& a, uint32_t* first, bool tell) {
-  __shared__ uint32_t part[kAdWarps];
+__device__ __forceinline__ uint2 ad_tiles(const AdArgs& a, uint32_t* first_x, uint32_t* first_y, bool tell) {
+  __shared__ uint2 part[kAdWarps];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
-  uint32_t total = 0;
+  uint2 total = make_uint2(0, 0);
   bool bad = false;
   for (uint32_t s0 = 0; s0 < a.n_seqs; s0 += kAdThreads) {
     const uint32_t s = s0 + threadIdx.x;
-    uint32_t x = 0;
+    uint2 own = make_uint2(0, 0);
     if (s < a.n_seqs) {
       const int32_t r0 = a.starts[s], r1 = a.starts[s + 1], i = a.which[s];
       if (r0 < 0 || r1 < r0 || static_cast<uint32_t>(r1) > a.rows) {
@@ -90,27 +91,36 @@ __device__ __forceinline__ uint32_t ad_tiles(const AdArgs& a, uint32_t* first, b
       } else {
         const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
         bad |= r1 > r0 && i >= 0 && none;
-        if (!none || a.out != a.y) x = (static_cast<uint32_t>(r1 - r0) + ROWS - 1) / ROWS;
+        const uint32_t tiles = (static_cast<uint32_t>(r1 - r0) + ROWS - 1) / ROWS;
+        own = make_uint2(none ? 0u : tiles, none && a.out == a.y ? 0u : tiles);
       }
     }
-    const uint32_t own = x;
+    uint2 x = own;
 #pragma unroll
     for (uint32_t step = 1; step < 32; step *= 2) {
-      const uint32_t from = __shfl_up_sync(kAll, x, step);
-      if (lane >= step) x += from;
+      const uint2 from = make_uint2(__shfl_up_sync(kAll, x.x, step), __shfl_up_sync(kAll, x.y, step));
+      if (lane >= step) { x.x += from.x; x.y += from.y; }
     }
     if (lane == 31) part[warp] = x;
     __syncthreads();
-    uint32_t before = total;
+    uint2 before = total;
 #pragma unroll
     for (uint32_t w = 0; w < kAdWarps; ++w) {
-      if (w < warp) before += part[w];
-      total += part[w];
+      const uint2 of = part[w];
+      if (w < warp) { before.x += of.x; before.y += of.y; }
+      total.x += of.x;
+      total.y += of.y;
     }
-    if (s < a.n_seqs) first[s] = before + x - own;
+    if (s < a.n_seqs) {
+      first_x[s] = before.x + x.x - own.x;
+      if (first_y) first_y[s] = before.y + x.y - own.y;
+    }
     __syncthreads();
   }
-  if (threadIdx.x == 0) first[a.n_seqs] = total;
+  if (threadIdx.x == 0) {
+    first_x[a.n_seqs] = total.x;
+    if (first_y) first_y[a.n_seqs] = total.y;
+  }
   if (tell && bad) atomicOr(a.status, ANS_STATUS_BAD_PAGE);
   __syncthreads();
   return total;
@@ -152,7 +162,7 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   let_next_start();
   wait_for_previous();
   uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kDownSmem);             // [n_seqs + 1]
-  const uint32_t tiles = ad_tiles<S::kRows>(a, first, blockIdx.x == 0), units = (a.n_in + kUnit - 1) / kUnit;
+  const uint32_t tiles = ad_tiles<S::kRows>(a, first, nullptr, blockIdx.x == 0).x, units = (a.n_in + kUnit - 1) / kUnit;
   const uint32_t blocks = ad_down_blocks(gridDim.x, most, tiles, units);
   if (blockIdx.x >= blocks) return;
   const uint64_t all = uint64_t(tiles) * units;
@@ -162,8 +172,7 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   const uint32_t tile = share.tile, u0 = share.in, u1 = u0 + min(units - u0, share.left);
   share.left -= u1 - u0;
   while (first[s + 1] <= tile) ++s;
-  const int32_t i = a.which[s];
-  if (i < 0 || static_cast<uint32_t>(i) >= a.count) continue;
+  const uint32_t i = a.which[s];
   const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
   const uint64_t begin = uint64_t(a.starts[s]) + r0;
 
@@ -259,12 +268,14 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
   uint8_t* const ring = reinterpret_cast<uint8_t*>(low + S::kRows * S::kHRow) + warp * S::kRing;
   let_next_start();
   wait_for_previous();
-  uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kUpSmem);               // [n_seqs + 1]
-  const uint32_t tiles = ad_tiles<S::kRows>(a, first, false), groups = (a.n_out + 31u) / 32u;
+  uint32_t* const first_down = reinterpret_cast<uint32_t*>(smem + S::kUpSmem);          // [n_seqs + 1]
+  uint32_t* const first = first_down + a.n_seqs + 1;                                   // [n_seqs + 1]
+  const uint2 counts = ad_tiles<S::kRows>(a, first_down, first, false);
+  const uint32_t tiles = counts.y, groups = (a.n_out + 31u) / 32u;
   const uint64_t all = uint64_t(tiles) * groups;
   const uint32_t blocks = static_cast<uint32_t>(min(uint64_t(gridDim.x), (all + kAdWarps - 1) / kAdWarps));     // a group a warp at least
   if (blockIdx.x >= blocks) return;
-  const uint32_t down_blocks = ad_down_blocks(down, most, tiles, down_units);
+  const uint32_t down_blocks = ad_down_blocks(down, most, counts.x, down_units);
   AdShare share = ad_share(all, groups, blocks, blockIdx.x);
   uint32_t s = ad_request(first, a.n_seqs, share.tile);
   for (; share.left; ++share.tile, share.in = 0) {
@@ -348,7 +359,7 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
   if (!none) {
     const float scale = a.scales ? a.scales[i] : 1.f;
     const float* const h = a.room + begin * R;
-    const uint64_t all_units = uint64_t(tiles) * down_units, unit = uint64_t(tile) * down_units;
+    const uint64_t all_units = uint64_t(counts.x) * down_units, unit = uint64_t(first_down[s] + (tile - first[s])) * down_units;
     const uint32_t sums = ad_block_of(all_units, down_blocks, unit + down_units - 1u) - ad_block_of(all_units, down_blocks, unit) + 1u;
 #pragma unroll
     for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
@@ -509,8 +520,8 @@ template <int R, int MT, bool EXACT>
 static int launch_up(const AdArgs& a, const AdPlan& p, uint32_t units, cudaStream_t st) {
   using S = AdShape<R, MT>;
   constexpr auto kernel = ans_adapters_up_kernel<R, MT, EXACT>;
-  const int rc = allow_smem<kernel>(S::kUpSmem + 4 * (ANS_MAX_SEQS + 1));
-  return rc == ANS_OK ? launch(kernel, dim3(p.up), dim3(kAdThreads), S::kUpSmem + 4 * (a.n_seqs + 1), st, 1, a, p.most, p.down, units) : rc;
+  const int rc = allow_smem<kernel>(S::kUpSmem + 8 * (ANS_MAX_SEQS + 1));
+  return rc == ANS_OK ? launch(kernel, dim3(p.up), dim3(kAdThreads), S::kUpSmem + 8 * (a.n_seqs + 1), st, 1, a, p.most, p.down, units) : rc;
 }
 template <int R, int MT>
 static int launch_both(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
