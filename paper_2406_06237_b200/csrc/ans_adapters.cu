@@ -1,16 +1,21 @@
 // Low-rank adapters of many requests beside a projection that they share:
 //   out[t] = y[t] + scales[i] * x_scales[t] * (x[t] A_i^T) B_i^T,   i the adapter of row t's request.
 //
-// For more rows than requests two kernels, both over tiles of 16 or 32 rows of one request: the first sums h = x A^T (mma.sync, fp32) over a
-// part of the inputs, up to eight parts a tile, into the caller's room; the second adds the parts in their order and streams y through the product
-// with B.  With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64 rows: bound by the bytes, so the plain
-// matrix instructions are enough.  h meets B as the sum of two bf16 numbers, h = hi + lo, |h - hi - lo| <= 2^-17 |h|: a second
-// product, which costs less than the rounding of h to 8 bits would lose.  5507 rows of 8192 in e4m3, rank 32, 8192 outputs take
-// 80.5 us, 24 of them the first kernel and 57 the second (2.5 TB/s of y and out; bound by latency and by issue at 24 warps an SM, 47 %
-// of its issue slots used).  Rows without a ragged edge (EXACT) have a form without questions at each access, 180
-// instructions a tile of outputs where the general one has 600: 91 us without it.  One kernel with a cluster a tile, whose
-// blocks exchange h through shared memory, took 118: 54 us of it were the blocks' starts, barriers and exchanges, eight times
-// as many as there are tiles.
+// For more rows than requests two kernels, both over tiles of 16 or 32 rows of one request: the first sums h = x A^T (mma.sync,
+// fp32) over a part of the inputs, up to eight parts a tile, into the caller's room; the second adds the parts in their order and
+// streams y through the product with B.  With a rank of 16 there are 2 operations a byte or so for a single row and 32 for 64
+// rows: bound by the bytes, so the plain matrix instructions are enough.  h meets B as the sum of two bf16 numbers, h = hi + lo,
+// |h - hi - lo| <= 2^-17 |h|: a second product, which costs less than the rounding of h to 8 bits would lose.
+//
+// 5507 rows of 8192 in e4m3, rank 32, 8192 outputs take 62 us, 19 of them the first kernel and 43 the second (4.2 TB/s of y and out;
+// bound by latency and by issue at 16 warps an SM, 45 % of its issue slots used).  What made it that:
+//   equal shares of the work for as many blocks as fit the GPU (80.5 us with a block for each tile and part: waves that end
+//   half filled; rows without an adapter counted in both kernels: 65.3), at a cost of 1 us where there are a few rows;
+//   h as an operand in registers and four groups of y on their way (75.4 with h read from shared memory for every group, three
+//   blocks an SM and two groups of y);
+//   a form without questions at each access for rows without a ragged edge (EXACT; 91 to 81 us when it came).
+// One kernel with a cluster a tile, whose blocks exchange h through shared memory, took 118: 54 us of it were the blocks'
+// starts, barriers and exchanges, eight times as many as there are tiles.
 //
 // The order of the inputs in a product is free, so a lane takes 16 bytes of a row at once; the columns of a product with B stand
 // for outputs such that a lane has 8 neighbouring ones.
@@ -71,8 +76,9 @@ __device__ __forceinline__ uint4 piece_of(const T* row, uint32_t e, uint32_t n, 
   return v;
 }
 
-// Tiles of ROWS rows, request by request, and what they consist of (inputs or outputs) in a row make a call's work, which is cut
-// into as many equal parts as there are blocks, so that none waits for the last wave: a block has the end of a tile and the
+// Tiles of ROWS rows, request by request, and the steps that each takes, of a unit of inputs or a group of outputs for each
+// warp, make a call's work in a row, which is cut into equal parts for as many blocks as there are, so that none waits for
+// a last wave: a block has the end of a tile and the
 // beginning of the next one, say.  first[s], in shared memory: tiles before request s's, and returned all of them; x: those that have
 // an adapter, which are the first kernel's; y: those that get outputs, the second one's.  The first kernel has no place for y's.
 template <uint32_t ROWS>
@@ -115,7 +121,7 @@ __device__ __forceinline__ uint2 ad_tiles(const AdArgs& a, uint32_t* first_x, ui
       first_x[s] = before.x + x.x - own.x;
       if (first_y) first_y[s] = before.y + x.y - own.y;
     }
-    __syncthreads();
+    if (s0 + kAdThreads < a.n_seqs) __syncthreads();   // the warps' sums are read
   }
   if (threadIdx.x == 0) {
     first_x[a.n_seqs] = total.x;
@@ -134,18 +140,19 @@ __device__ __forceinline__ uint32_t ad_request(const uint32_t* first, uint32_t n
   }
   return s;
 }
-// Block b's share of `all` pieces, `each` of them a tile: from piece `in` of `tile` on, `left` of them (fewer than 2^32: a piece has 512
-// elements of y, or of x, which is in memory).  And the block that has piece x.
+// Block b's share of `all` steps, `each` of them a tile: from step `in` of `tile` on, `left` of them (fewer than 2^32: a step has 4096
+// elements of y, or of x, which are in memory).  And the block that has step x.
 struct AdShare { uint32_t tile, in, left; };
 __device__ __forceinline__ AdShare ad_share(uint64_t all, uint32_t each, uint32_t blocks, uint32_t b) {
   const uint64_t from = all * b / blocks, tile = from / each;
   return {static_cast<uint32_t>(tile), static_cast<uint32_t>(from - tile * each), static_cast<uint32_t>(all * (b + 1u) / blocks - from)};
 }
 __device__ __forceinline__ uint32_t ad_block_of(uint64_t all, uint32_t blocks, uint64_t x) { return static_cast<uint32_t>(((x + 1u) * blocks + all - 1u) / all - 1u); }
-// Blocks that x A^T is dealt to: a tile's inputs then lie in `most` at most.  With shares of at least 1 / (most - 1) of a tile there are at
-// most most - 1 places between blocks behind a tile's first input.
-__device__ __forceinline__ uint32_t ad_down_blocks(uint32_t grid, uint32_t most, uint32_t tiles, uint32_t units) {
-  return static_cast<uint32_t>(min(uint64_t(grid), uint64_t(tiles) * min(most - 1u, units)));
+// Blocks that x A^T is dealt to, so that a tile's steps lie in `most` blocks at most: as many for each tile, or else shares of at
+// least 1 / (most - 1) of a tile, which begin in at most most - 1 places behind a tile's first step.
+__device__ __forceinline__ uint32_t ad_down_blocks(uint32_t grid, uint32_t most, uint32_t tiles, uint32_t steps) {
+  const uint64_t even = uint64_t(tiles) * min(most, steps);
+  return static_cast<uint32_t>(even <= grid ? even : min(uint64_t(grid), uint64_t(tiles) * (most - 1u)));
 }
 
 // R: the rank, rounded up to 16, 32, 64 or 128; MT: 16 rows each; most: parts of a tile's sums.
@@ -163,14 +170,15 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   wait_for_previous();
   uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kDownSmem);             // [n_seqs + 1]
   const uint32_t tiles = ad_tiles<S::kRows>(a, first, nullptr, blockIdx.x == 0).x, units = (a.n_in + kUnit - 1) / kUnit;
-  const uint32_t blocks = ad_down_blocks(gridDim.x, most, tiles, units);
+  const uint32_t steps = (units + kAdWarps - 1) / kAdWarps, blocks = ad_down_blocks(gridDim.x, most, tiles, steps);
   if (blockIdx.x >= blocks) return;
-  const uint64_t all = uint64_t(tiles) * units;
-  AdShare share = ad_share(all, units, blocks, blockIdx.x);
+  const uint64_t all = uint64_t(tiles) * steps;
+  AdShare share = ad_share(all, steps, blocks, blockIdx.x);
   uint32_t s = ad_request(first, a.n_seqs, share.tile);
   for (; share.left; ++share.tile, share.in = 0) {
-  const uint32_t tile = share.tile, u0 = share.in, u1 = u0 + min(units - u0, share.left);
-  share.left -= u1 - u0;
+  const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
+  const uint32_t u0 = kAdWarps * share.in, u1 = min(units, u0 + kAdWarps * count);
+  share.left -= count;
   while (first[s + 1] <= tile) ++s;
   const uint32_t i = a.which[s];
   const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
@@ -239,7 +247,7 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
       *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
     }
   __syncthreads();
-  const uint32_t part = blockIdx.x - ad_block_of(all, blocks, uint64_t(tile) * units);
+  const uint32_t part = blockIdx.x - ad_block_of(all, blocks, uint64_t(tile) * steps);
   float* const h = a.room + (uint64_t(part) * a.rows + begin) * R;
 #pragma unroll
   for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
@@ -255,10 +263,9 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
 }
 
 // `most` and `down`: of the kernel before, its parts of a tile's sums and its grid.  EXACT: the rank is R, outputs come in whole groups of 32, and B, y
-// and out can be accessed 8 and 16 bytes at a time: addresses are then constants apart and nothing is asked (180 instructions a group
-// of 32 rows by 32 outputs where the general form takes 600).
+// and out can be accessed 8 and 16 bytes at a time: addresses are then constants apart and nothing is asked.
 template <int R, int MT, bool EXACT>
-__global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const AdArgs a, const uint32_t most, const uint32_t down, const uint32_t down_units) {
+__global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const AdArgs a, const uint32_t most, const uint32_t down, const uint32_t down_steps) {
   using S = AdShape<R, MT>;
   constexpr int KT = R / 16;
   extern __shared__ __align__(16) uint8_t smem[];
@@ -272,15 +279,17 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
   uint32_t* const first = first_down + a.n_seqs + 1;                                   // [n_seqs + 1]
   const uint2 counts = ad_tiles<S::kRows>(a, first_down, first, false);
   const uint32_t tiles = counts.y, groups = (a.n_out + 31u) / 32u;
-  const uint64_t all = uint64_t(tiles) * groups;
-  const uint32_t blocks = static_cast<uint32_t>(min(uint64_t(gridDim.x), (all + kAdWarps - 1) / kAdWarps));     // a group a warp at least
+  const uint32_t steps = (groups + kAdWarps - 1) / kAdWarps;
+  const uint64_t all = uint64_t(tiles) * steps;
+  const uint32_t blocks = static_cast<uint32_t>(min(uint64_t(gridDim.x), all));
   if (blockIdx.x >= blocks) return;
-  const uint32_t down_blocks = ad_down_blocks(down, most, counts.x, down_units);
-  AdShare share = ad_share(all, groups, blocks, blockIdx.x);
+  const uint32_t down_blocks = ad_down_blocks(down, most, counts.x, down_steps);
+  AdShare share = ad_share(all, steps, blocks, blockIdx.x);
   uint32_t s = ad_request(first, a.n_seqs, share.tile);
   for (; share.left; ++share.tile, share.in = 0) {
-  const uint32_t tile = share.tile, o0 = share.in, o1 = o0 + min(groups - o0, share.left);
-  share.left -= o1 - o0;
+  const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
+  const uint32_t o0 = kAdWarps * share.in, o1 = min(groups, o0 + kAdWarps * count);
+  share.left -= count;
   while (first[s + 1] <= tile) ++s;
   const int32_t i = a.which[s];
   const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
@@ -359,8 +368,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
   if (!none) {
     const float scale = a.scales ? a.scales[i] : 1.f;
     const float* const h = a.room + begin * R;
-    const uint64_t all_units = uint64_t(counts.x) * down_units, unit = uint64_t(first_down[s] + (tile - first[s])) * down_units;
-    const uint32_t sums = ad_block_of(all_units, down_blocks, unit + down_units - 1u) - ad_block_of(all_units, down_blocks, unit) + 1u;
+    const uint64_t all_steps = uint64_t(counts.x) * down_steps, step = uint64_t(first_down[s] + (tile - first[s])) * down_steps;
+    const uint32_t sums = ad_block_of(all_steps, down_blocks, step + down_steps - 1u) - ad_block_of(all_steps, down_blocks, step) + 1u;
 #pragma unroll
     for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
       const uint32_t e = threadIdx.x + n * kAdThreads, row = e / R, k = e % R;
@@ -499,12 +508,12 @@ static AdPlan plan_adapters(const ans_adapters_desc& d, int sms) {
   // tiles of 16 rows where requests have about as many, else of 32, if registers hold their sums
   p.mt = p.r == 128 || uint64_t(d.rows) <= 16ull * d.n_seqs ? 1 : 2;
   const uint64_t tiles = d.rows / (16u * p.mt) + d.n_seqs;
-  // as many blocks as have their places on the GPU at once, as far as there is a group of outputs for each warp, and not
-  // more than 8 parts of a tile's inputs
-  p.up = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(sms) * 2, (tiles * ((d.n_out + 31) / 32) + kAdWarps - 1) / kAdWarps));
+  // as many blocks as have their places on the GPU at once, as far as there are steps for them and not more than 8 parts of
+  // a tile's inputs
+  p.up = static_cast<uint32_t>(std::min<uint64_t>(uint64_t(sms) * 2, tiles * ((d.n_out + 32 * kAdWarps - 1) / (32 * kAdWarps))));
   p.down = uint64_t(sms) * (p.r * p.mt >= 128 ? 1 : 2);
   p.most = static_cast<uint32_t>(std::min<uint64_t>(p.down / tiles + 2, 8));
-  p.down = static_cast<uint32_t>(std::min<uint64_t>(p.down, tiles * (p.most - 1)));
+  p.down = static_cast<uint32_t>(std::min<uint64_t>(p.down, tiles * p.most));
   p.room = size_t(p.most) * d.rows * p.r * sizeof(float);
   return p;
 }
@@ -517,19 +526,19 @@ static int launch_down(const AdArgs& a, const AdPlan& p, cudaStream_t st) {
   return rc == ANS_OK ? launch(kernel, dim3(p.down), dim3(kAdThreads), S::kDownSmem + 4 * (a.n_seqs + 1), st, 1, a, p.most) : rc;
 }
 template <int R, int MT, bool EXACT>
-static int launch_up(const AdArgs& a, const AdPlan& p, uint32_t units, cudaStream_t st) {
+static int launch_up(const AdArgs& a, const AdPlan& p, uint32_t steps, cudaStream_t st) {
   using S = AdShape<R, MT>;
   constexpr auto kernel = ans_adapters_up_kernel<R, MT, EXACT>;
   const int rc = allow_smem<kernel>(S::kUpSmem + 8 * (ANS_MAX_SEQS + 1));
-  return rc == ANS_OK ? launch(kernel, dim3(p.up), dim3(kAdThreads), S::kUpSmem + 8 * (a.n_seqs + 1), st, 1, a, p.most, p.down, units) : rc;
+  return rc == ANS_OK ? launch(kernel, dim3(p.up), dim3(kAdThreads), S::kUpSmem + 8 * (a.n_seqs + 1), st, 1, a, p.most, p.down, steps) : rc;
 }
 template <int R, int MT>
 static int launch_both(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
   const int rc = f8 ? (vec ? launch_down<R, MT, true, true>(a, p, st) : launch_down<R, MT, true, false>(a, p, st))
               : (vec ? launch_down<R, MT, false, true>(a, p, st) : launch_down<R, MT, false, false>(a, p, st));
   if (rc != ANS_OK) return rc;
-  const uint32_t units = f8 ? (a.n_in + 63) / 64 : (a.n_in + 31) / 32;       // of inputs, as the first kernel has them
-  return a.rank == R && a.n_out % 32 == 0 && a.b_wide && a.y_wide ? launch_up<R, MT, true>(a, p, units, st) : launch_up<R, MT, false>(a, p, units, st);
+  const uint32_t inputs = (f8 ? 64u : 32u) * kAdWarps, steps = (a.n_in + inputs - 1) / inputs;       // as the first kernel has them
+  return a.rank == R && a.n_out % 32 == 0 && a.b_wide && a.y_wide ? launch_up<R, MT, true>(a, p, steps, st) : launch_up<R, MT, false>(a, p, steps, st);
 }
 static int launch_tiles_of(const AdArgs& a, const AdPlan& p, bool f8, bool vec, cudaStream_t st) {
   switch (p.r) {
