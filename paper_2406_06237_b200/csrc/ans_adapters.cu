@@ -176,89 +176,89 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
   AdShare share = ad_share(all, steps, blocks, blockIdx.x);
   uint32_t s = ad_request(first, a.n_seqs, share.tile);
   for (; share.left; ++share.tile, share.in = 0) {
-  const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
-  const uint32_t u0 = kAdWarps * share.in, u1 = min(units, u0 + kAdWarps * count);
-  share.left -= count;
-  while (first[s + 1] <= tile) ++s;
-  const uint32_t i = a.which[s];
-  const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
-  const uint64_t begin = uint64_t(a.starts[s]) + r0;
+    const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
+    const uint32_t u0 = kAdWarps * share.in, u1 = min(units, u0 + kAdWarps * count);
+    share.left -= count;
+    while (first[s + 1] <= tile) ++s;
+    const uint32_t i = a.which[s];
+    const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
+    const uint64_t begin = uint64_t(a.starts[s]) + r0;
 
-  float c[MT][NT][4];
+    float c[MT][NT][4];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
-  const X* x[MT][2];                                               // the lane's rows
+      for (int n = 0; n < NT; ++n) c[m][n][0] = c[m][n][1] = c[m][n][2] = c[m][n][3] = 0.f;
+    const X* x[MT][2];                                               // the lane's rows
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (uint32_t h = 0; h < 2; ++h) x[m][h] = reinterpret_cast<const X*>(a.x) + (begin + min(16u * m + 8u * h + g, live - 1u)) * a.x_stride;
-  const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + (uint64_t(i) * a.rank + min(g, a.rank - 1u)) * a.n_in;
-  for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
-    uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
+      for (uint32_t h = 0; h < 2; ++h) x[m][h] = reinterpret_cast<const X*>(a.x) + (begin + min(16u * m + 8u * h + g, live - 1u)) * a.x_stride;
+    const uint16_t* const down = reinterpret_cast<const uint16_t*>(a.a) + (uint64_t(i) * a.rank + min(g, a.rank - 1u)) * a.n_in;
+    for (uint32_t u = u0 + warp; u < u1; u += kAdWarps * kAhead) {
+      uint4 xf[kAhead][MT][2], af[kAhead][NT][kLane / 8];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const uint32_t now = u + kAdWarps * k, e = now * kUnit + t * kLane;
-      const bool in = now < u1;
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t now = u + kAdWarps * k, e = now * kUnit + t * kLane;
+        const bool in = now < u1;
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (uint32_t h = 0; h < kLane / 8; ++h)
-          af[k][n][h] = piece_of<uint16_t, VEC>(down + 8u * n * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) xf[k][m][h] = piece_of<X, VEC>(x[m][h], e, a.n_in, in && 16u * m + 8u * h + g < live);
-    }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-#pragma unroll
-      for (uint32_t j = 0; j < kSteps; ++j) {
-        uint32_t xw[MT][4];
+          for (uint32_t h = 0; h < kLane / 8; ++h)
+            af[k][n][h] = piece_of<uint16_t, VEC>(down + 8u * n * a.n_in, e + 8u * h, a.n_in, in && 8u * n + g < a.rank);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t* const w = &xf[k][m][h].x;
-            if constexpr (F8) {
-              xw[m][h] = open_e4m3(w[j] & 0xFFFFu);
-              xw[m][h + 2] = open_e4m3(w[j] >> 16);
-            } else {
-              xw[m][h] = w[2 * j];
-              xw[m][h + 2] = w[2 * j + 1];
-            }
-          }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          const uint32_t* const w = &af[k][n][j / 2].x;
-          const uint32_t b0 = w[2 * (j % 2)], b1 = w[2 * (j % 2) + 1];
-#pragma unroll
-          for (int m = 0; m < MT; ++m) mma_bf16(c[m][n], xw[m][0], xw[m][1], xw[m][2], xw[m][3], b0, b1);
-        }
+          for (uint32_t h = 0; h < 2; ++h) xf[k][m][h] = piece_of<X, VEC>(x[m][h], e, a.n_in, in && 16u * m + 8u * h + g < live);
       }
-  }
-  float* const to = parts + warp * S::kPart;
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+      for (int k = 0; k < kAhead; ++k)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      *reinterpret_cast<float2*>(to + (16 * m + g) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
-      *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
+        for (uint32_t j = 0; j < kSteps; ++j) {
+          uint32_t xw[MT][4];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t* const w = &xf[k][m][h].x;
+              if constexpr (F8) {
+                xw[m][h] = open_e4m3(w[j] & 0xFFFFu);
+                xw[m][h + 2] = open_e4m3(w[j] >> 16);
+              } else {
+                xw[m][h] = w[2 * j];
+                xw[m][h + 2] = w[2 * j + 1];
+              }
+            }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const uint32_t* const w = &af[k][n][j / 2].x;
+            const uint32_t b0 = w[2 * (j % 2)], b1 = w[2 * (j % 2) + 1];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma_bf16(c[m][n], xw[m][0], xw[m][1], xw[m][2], xw[m][3], b0, b1);
+          }
+        }
     }
-  __syncthreads();
-  const uint32_t part = blockIdx.x - ad_block_of(all, blocks, uint64_t(tile) * steps);
-  float* const h = a.room + (uint64_t(part) * a.rows + begin) * R;
+    float* const to = parts + warp * S::kPart;
 #pragma unroll
-  for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
-    const uint32_t e = threadIdx.x + n * kAdThreads;
-    if (e / R >= live) break;
-    float sum = 0.f;
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
-    h[e] = sum;
-  }
-  __syncthreads();                                     // the warps' sums are read
+      for (int n = 0; n < NT; ++n) {
+        *reinterpret_cast<float2*>(to + (16 * m + g) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][0], c[m][n][1]);
+        *reinterpret_cast<float2*>(to + (16 * m + g + 8) * (R + 8) + 8 * n + 2 * t) = make_float2(c[m][n][2], c[m][n][3]);
+      }
+    __syncthreads();
+    const uint32_t part = blockIdx.x - ad_block_of(all, blocks, uint64_t(tile) * steps);
+    float* const h = a.room + (uint64_t(part) * a.rows + begin) * R;
+#pragma unroll
+    for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
+      const uint32_t e = threadIdx.x + n * kAdThreads;
+      if (e / R >= live) break;
+      float sum = 0.f;
+#pragma unroll
+      for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
+      h[e] = sum;
+    }
+    __syncthreads();                                     // the warps' sums are read
   }
 }
 
@@ -287,210 +287,210 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
   AdShare share = ad_share(all, steps, blocks, blockIdx.x);
   uint32_t s = ad_request(first, a.n_seqs, share.tile);
   for (; share.left; ++share.tile, share.in = 0) {
-  const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
-  const uint32_t o0 = kAdWarps * share.in, o1 = min(groups, o0 + kAdWarps * count);
-  share.left -= count;
-  while (first[s + 1] <= tile) ++s;
-  const int32_t i = a.which[s];
-  const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
-  const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
-  const uint64_t begin = uint64_t(a.starts[s]) + r0;
+    const uint32_t tile = share.tile, count = min(steps - share.in, share.left);
+    const uint32_t o0 = kAdWarps * share.in, o1 = min(groups, o0 + kAdWarps * count);
+    share.left -= count;
+    while (first[s + 1] <= tile) ++s;
+    const int32_t i = a.which[s];
+    const bool none = i < 0 || static_cast<uint32_t>(i) >= a.count;
+    const uint32_t r0 = (tile - first[s]) * S::kRows, live = min(S::kRows, static_cast<uint32_t>(a.starts[s + 1] - a.starts[s]) - r0);
+    const uint64_t begin = uint64_t(a.starts[s]) + r0;
 
-  // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
-  // elements t R / 4 + 4 k and on of a row
-  const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4), b_row = EXACT ? R : a.rank;
-  const __nv_bfloat16* const b_lane = a.b + (uint64_t(none ? 0 : i) * a.n_out + b_out) * b_row + b_in;
-  auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
-    const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * b_row);
-    const bool ours = o < o1 && !none;
-    const uint32_t left = ours ? a.n_out - 32u * o : 0u;             // outputs from the group's first on
+    // rows of B for group o: column g of product j stands for output 32 o + 8 (g / 2) + 2 j + g % 2, and products k take
+    // elements t R / 4 + 4 k and on of a row
+    const uint32_t b_out = 8u * (g >> 1) + (g & 1u), b_in = t * (R / 4), b_row = EXACT ? R : a.rank;
+    const __nv_bfloat16* const b_lane = a.b + (uint64_t(none ? 0 : i) * a.n_out + b_out) * b_row + b_in;
+    auto load_b = [&](uint32_t o, uint32_t (&f)[4][KT][2]) {
+      const __nv_bfloat16* const rows = b_lane + uint64_t(o) * (32u * b_row);
+      const bool ours = o < o1 && !none;
+      const uint32_t left = ours ? a.n_out - 32u * o : 0u;             // outputs from the group's first on
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-      const __nv_bfloat16* const row = rows + 2u * j * b_row;
+      for (uint32_t j = 0; j < 4; ++j) {
+        const __nv_bfloat16* const row = rows + 2u * j * b_row;
 #pragma unroll
-      for (uint32_t k = 0; k < KT; ++k) {
-        if constexpr (EXACT) {
-          if (ours) {
-            const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
-            f[j][k][0] = u.x; f[j][k][1] = u.y;
-          }
-        } else {
-          const bool in = b_out + 2u * j < left;
-          f[j][k][0] = f[j][k][1] = 0u;
-          if (a.b_wide) {
-            if (in && b_in + 4u * k < a.rank) {
+        for (uint32_t k = 0; k < KT; ++k) {
+          if constexpr (EXACT) {
+            if (ours) {
               const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
               f[j][k][0] = u.x; f[j][k][1] = u.y;
             }
           } else {
-#pragma unroll
-            for (uint32_t h = 0; h < 4; ++h)
-              if (in && b_in + 4u * k + h < a.rank)
-                f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[4u * k + h]) << (16 * (h % 2));
-          }
-        }
-      }
-    }
-  };
-  // groups of y: 16 bytes a lane and copy, a group ring slot a commit
-  const uint32_t y_shift = a.y_f32 ? 3u : 2u, y_size = a.y_f32 ? 4u : 2u;        // 2^y_shift pieces of 16 bytes a row
-  const uint32_t slot_bytes = S::kRows << (y_shift + 4u), slots = S::kRing / slot_bytes;
-  const uint8_t* const y = static_cast<const uint8_t*>(a.y) + begin * a.y_stride * y_size;
-  uint8_t* const out = static_cast<uint8_t*>(a.out) + begin * a.out_stride * y_size;
-  const uint32_t y_row = lane >> y_shift, y_at = 16u * (lane & ((1u << y_shift) - 1u)), y_rows = 32u >> y_shift;
-  const uint64_t y_down = y_rows * a.y_stride * y_size;
-  const uint8_t* const y_lane = y + y_row * a.y_stride * y_size + y_at;
-  const uint32_t ring_lane = smem_addr(ring) + lane * 16u;
-  const bool whole = live == S::kRows;
-  auto fetch_y = [&](uint32_t o, uint32_t slot) {
-    const uint64_t across = uint64_t(32u * y_size) * o;
-    if ((EXACT || a.y_wide) && o < o1 && (EXACT || across + y_at + 16u <= uint64_t(a.n_out) * y_size)) {
-      const uint8_t* from = y_lane + across;
-      uint32_t to = ring_lane + slot * slot_bytes;
-      if (EXACT && whole && y_shift == 2) {
-#pragma unroll
-        for (uint32_t n = 0; n < S::kRows / 8; ++n, from += y_down, to += 512u)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
-      } else {
-        for (uint32_t row = y_row; row < live; row += y_rows, from += y_down, to += 512u)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
-  constexpr uint32_t kBs = R <= 32 ? 2 : 1;                          // groups whose rows of B are loaded ahead
-  uint32_t bf[kBs][4][KT][2];
-#pragma unroll
-  for (uint32_t n = 0; n < kBs; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
-
-  __syncthreads();                                     // the rows of h before are read
-  if (!none) {
-    const float scale = a.scales ? a.scales[i] : 1.f;
-    const float* const h = a.room + begin * R;
-    const uint64_t all_steps = uint64_t(counts.x) * down_steps, step = uint64_t(first_down[s] + (tile - first[s])) * down_steps;
-    const uint32_t sums = ad_block_of(all_steps, down_blocks, step + down_steps - 1u) - ad_block_of(all_steps, down_blocks, step) + 1u;
-#pragma unroll
-    for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
-      const uint32_t e = threadIdx.x + n * kAdThreads, row = e / R, k = e % R;
-      float v[8], sum = 0.f;                                         // of all parts, under way together
-#pragma unroll
-      for (uint32_t p = 0; p < 8; ++p) v[p] = p < sums && row < live ? h[uint64_t(p) * a.rows * R + e] : 0.f;
-#pragma unroll
-      for (uint32_t p = 0; p < 8; ++p) sum += v[p];
-      sum *= a.x_scales && row < live ? a.x_scales[begin + row] * scale : scale;
-      const __nv_bfloat16 hi = __float2bfloat16_rn(sum);
-      const float rest = sum - __bfloat162float(hi);
-      high[row * S::kHRow + k] = hi;
-      low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
-    }
-    __syncthreads();
-  }
-
-  // h as the operand, in registers where they hold it
-  constexpr bool kHeld = MT * R <= 64;
-  uint2 held[kHeld ? MT : 1][kHeld ? KT : 1][4];
-  auto operand_of = [&](uint32_t m, uint32_t k, uint2 (&v)[4]) {
-    const uint32_t up = (16u * m + g) * S::kHRow + t * (R / 4) + 4u * k, dn = up + 8u * S::kHRow;
-    v[0] = *reinterpret_cast<const uint2*>(low + up); v[1] = *reinterpret_cast<const uint2*>(low + dn);
-    v[2] = *reinterpret_cast<const uint2*>(high + up); v[3] = *reinterpret_cast<const uint2*>(high + dn);
-  };
-  if constexpr (kHeld)
-    if (!none)
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int k = 0; k < KT; ++k) operand_of(m, k, held[m][k]);
-
-  uint32_t slot = 0;
-  uint8_t* out_lane = out + (g * a.out_stride + 8u * t) * y_size + uint64_t(32u * y_size) * (o0 + warp);
-  const uint64_t out_down = 8u * a.out_stride * y_size;
-#pragma unroll 1
-  for (uint32_t first = o0 + warp; first < o1; first += kAdWarps * kBs) {
-#pragma unroll
-    for (uint32_t n = 0; n < kBs; ++n, out_lane += 32u * y_size * kAdWarps) {
-      const uint32_t o = first + kAdWarps * n;
-      if (o >= o1) break;
-      const uint32_t at = 32u * o + 8u * t;                          // the lane's outputs: at .. at + 7
-      const bool wide = EXACT || (a.y_wide && at + 8 <= a.n_out);
-      if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
-      else asm volatile("cp.async.wait_group 1;" ::: "memory");
-      __syncwarp();
-      const uint8_t* const staged = ring + slot * slot_bytes;
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        float d[4][4];
-        if (!none) {
-#pragma unroll
-          for (uint32_t k = 0; k < KT; ++k) {
-            uint2 v[4];
-            if constexpr (kHeld) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) v[q] = held[m][k][q];
-            } else {
-              operand_of(m, k, v);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (k == 0) mma_bf16_first(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
-              else mma_bf16(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[2].x, v[3].x, v[2].y, v[3].y, bf[n][j][k][0], bf[n][j][k][1]);
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t r = 16u * m + 8u * h + g;
-          if (r >= live) continue;
-          float v[8];
-          uint8_t* const p = out_lane + (2 * m + h) * out_down;
-          if (wide) {
-            const uint4* const q = reinterpret_cast<const uint4*>(staged) + ((r * 4u + t) << (y_shift - 2u));
-            if (a.y_f32) {
-              const uint4 w = q[0], z = q[1];
-              v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
-              v[4] = __uint_as_float(z.x); v[5] = __uint_as_float(z.y); v[6] = __uint_as_float(z.z); v[7] = __uint_as_float(z.w);
-            } else {
-              const uint4 u = q[0];
-              const uint32_t* const w = &u.x;
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                v[2 * k] = __uint_as_float(w[k] << 16);
-                v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+            const bool in = b_out + 2u * j < left;
+            f[j][k][0] = f[j][k][1] = 0u;
+            if (a.b_wide) {
+              if (in && b_in + 4u * k < a.rank) {
+                const uint2 u = *reinterpret_cast<const uint2*>(row + 4u * k);
+                f[j][k][0] = u.x; f[j][k][1] = u.y;
               }
+            } else {
+#pragma unroll
+              for (uint32_t h = 0; h < 4; ++h)
+                if (in && b_in + 4u * k + h < a.rank)
+                  f[j][k][h / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(row)[4u * k + h]) << (16 * (h % 2));
             }
-            if (!none)
+          }
+        }
+      }
+    };
+    // groups of y: 16 bytes a lane and copy, a group ring slot a commit
+    const uint32_t y_shift = a.y_f32 ? 3u : 2u, y_size = a.y_f32 ? 4u : 2u;        // 2^y_shift pieces of 16 bytes a row
+    const uint32_t slot_bytes = S::kRows << (y_shift + 4u), slots = S::kRing / slot_bytes;
+    const uint8_t* const y = static_cast<const uint8_t*>(a.y) + begin * a.y_stride * y_size;
+    uint8_t* const out = static_cast<uint8_t*>(a.out) + begin * a.out_stride * y_size;
+    const uint32_t y_row = lane >> y_shift, y_at = 16u * (lane & ((1u << y_shift) - 1u)), y_rows = 32u >> y_shift;
+    const uint64_t y_down = y_rows * a.y_stride * y_size;
+    const uint8_t* const y_lane = y + y_row * a.y_stride * y_size + y_at;
+    const uint32_t ring_lane = smem_addr(ring) + lane * 16u;
+    const bool whole = live == S::kRows;
+    auto fetch_y = [&](uint32_t o, uint32_t slot) {
+      const uint64_t across = uint64_t(32u * y_size) * o;
+      if ((EXACT || a.y_wide) && o < o1 && (EXACT || across + y_at + 16u <= uint64_t(a.n_out) * y_size)) {
+        const uint8_t* from = y_lane + across;
+        uint32_t to = ring_lane + slot * slot_bytes;
+        if (EXACT && whole && y_shift == 2) {
+#pragma unroll
+          for (uint32_t n = 0; n < S::kRows / 8; ++n, from += y_down, to += 512u)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+        } else {
+          for (uint32_t row = y_row; row < live; row += y_rows, from += y_down, to += 512u)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (uint32_t n = 0; n < slots; ++n) fetch_y(o0 + warp + kAdWarps * n, n);
+    constexpr uint32_t kBs = R <= 32 ? 2 : 1;                          // groups whose rows of B are loaded ahead
+    uint32_t bf[kBs][4][KT][2];
+#pragma unroll
+    for (uint32_t n = 0; n < kBs; ++n) load_b(o0 + warp + kAdWarps * n, bf[n]);
+
+    __syncthreads();                                     // the rows of h before are read
+    if (!none) {
+      const float scale = a.scales ? a.scales[i] : 1.f;
+      const float* const h = a.room + begin * R;
+      const uint64_t all_steps = uint64_t(counts.x) * down_steps, step = uint64_t(first_down[s] + (tile - first[s])) * down_steps;
+      const uint32_t sums = ad_block_of(all_steps, down_blocks, step + down_steps - 1u) - ad_block_of(all_steps, down_blocks, step) + 1u;
+#pragma unroll
+      for (uint32_t n = 0; n < S::kSums / kAdThreads; ++n) {
+        const uint32_t e = threadIdx.x + n * kAdThreads, row = e / R, k = e % R;
+        float v[8], sum = 0.f;                                         // of all parts, under way together
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p) v[p] = p < sums && row < live ? h[uint64_t(p) * a.rows * R + e] : 0.f;
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p) sum += v[p];
+        sum *= a.x_scales && row < live ? a.x_scales[begin + row] * scale : scale;
+        const __nv_bfloat16 hi = __float2bfloat16_rn(sum);
+        const float rest = sum - __bfloat162float(hi);
+        high[row * S::kHRow + k] = hi;
+        low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);
+      }
+      __syncthreads();
+    }
+
+    // h as the operand, in registers where they hold it
+    constexpr bool kHeld = MT * R <= 64;
+    uint2 held[kHeld ? MT : 1][kHeld ? KT : 1][4];
+    auto operand_of = [&](uint32_t m, uint32_t k, uint2 (&v)[4]) {
+      const uint32_t up = (16u * m + g) * S::kHRow + t * (R / 4) + 4u * k, dn = up + 8u * S::kHRow;
+      v[0] = *reinterpret_cast<const uint2*>(low + up); v[1] = *reinterpret_cast<const uint2*>(low + dn);
+      v[2] = *reinterpret_cast<const uint2*>(high + up); v[3] = *reinterpret_cast<const uint2*>(high + dn);
+    };
+    if constexpr (kHeld)
+      if (!none)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int k = 0; k < KT; ++k) operand_of(m, k, held[m][k]);
+
+    uint32_t slot = 0;
+    uint8_t* out_lane = out + (g * a.out_stride + 8u * t) * y_size + uint64_t(32u * y_size) * (o0 + warp);
+    const uint64_t out_down = 8u * a.out_stride * y_size;
+#pragma unroll 1
+    for (uint32_t first = o0 + warp; first < o1; first += kAdWarps * kBs) {
+#pragma unroll
+      for (uint32_t n = 0; n < kBs; ++n, out_lane += 32u * y_size * kAdWarps) {
+        const uint32_t o = first + kAdWarps * n;
+        if (o >= o1) break;
+        const uint32_t at = 32u * o + 8u * t;                          // the lane's outputs: at .. at + 7
+        const bool wide = EXACT || (a.y_wide && at + 8 <= a.n_out);
+        if (slots == 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+        else asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        const uint8_t* const staged = ring + slot * slot_bytes;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float d[4][4];
+          if (!none) {
+#pragma unroll
+            for (uint32_t k = 0; k < KT; ++k) {
+              uint2 v[4];
+              if constexpr (kHeld) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = held[m][k][q];
+              } else {
+                operand_of(m, k, v);
+              }
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                v[2 * j] += d[j][2 * h];
-                v[2 * j + 1] += d[j][2 * h + 1];
+                if (k == 0) mma_bf16_first(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
+                else mma_bf16(d[j], v[0].x, v[1].x, v[0].y, v[1].y, bf[n][j][k][0], bf[n][j][k][1]);
               }
-            if (a.y_f32) {
-              reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-              reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
-              *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-            }
-          } else {
-            const uint8_t* const q = y + (r * a.y_stride + at) * y_size;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (at + k < a.n_out) {
-                float u = a.y_f32 ? reinterpret_cast<const float*>(q)[k] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[k]);
-                if (!none) u += d[k / 2][2 * h + k % 2];
-                if (a.y_f32) reinterpret_cast<float*>(p)[k] = u;
-                else reinterpret_cast<__nv_bfloat16*>(p)[k] = __float2bfloat16_rn(u);
+              for (int j = 0; j < 4; ++j) mma_bf16(d[j], v[2].x, v[3].x, v[2].y, v[3].y, bf[n][j][k][0], bf[n][j][k][1]);
+            }
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t r = 16u * m + 8u * h + g;
+            if (r >= live) continue;
+            float v[8];
+            uint8_t* const p = out_lane + (2 * m + h) * out_down;
+            if (wide) {
+              const uint4* const q = reinterpret_cast<const uint4*>(staged) + ((r * 4u + t) << (y_shift - 2u));
+              if (a.y_f32) {
+                const uint4 w = q[0], z = q[1];
+                v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+                v[4] = __uint_as_float(z.x); v[5] = __uint_as_float(z.y); v[6] = __uint_as_float(z.z); v[7] = __uint_as_float(z.w);
+              } else {
+                const uint4 u = q[0];
+                const uint32_t* const w = &u.x;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  v[2 * k] = __uint_as_float(w[k] << 16);
+                  v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+                }
               }
+              if (!none)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  v[2 * j] += d[j][2 * h];
+                  v[2 * j + 1] += d[j][2 * h + 1];
+                }
+              if (a.y_f32) {
+                reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+              } else {
+                *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+              }
+            } else {
+              const uint8_t* const q = y + (r * a.y_stride + at) * y_size;
+#pragma unroll
+              for (int k = 0; k < 8; ++k)
+                if (at + k < a.n_out) {
+                  float u = a.y_f32 ? reinterpret_cast<const float*>(q)[k] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[k]);
+                  if (!none) u += d[k / 2][2 * h + k % 2];
+                  if (a.y_f32) reinterpret_cast<float*>(p)[k] = u;
+                  else reinterpret_cast<__nv_bfloat16*>(p)[k] = __float2bfloat16_rn(u);
+                }
+            }
           }
         }
+        __syncwarp();
+        load_b(o + kAdWarps * kBs, bf[n]);
+        fetch_y(o + kAdWarps * slots, slot);
+        slot = slot + 1u == slots ? 0u : slot + 1u;
       }
-      __syncwarp();
-      load_b(o + kAdWarps * kBs, bf[n]);
-      fetch_y(o + kAdWarps * slots, slot);
-      slot = slot + 1u == slots ? 0u : slot + 1u;
     }
-  }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
