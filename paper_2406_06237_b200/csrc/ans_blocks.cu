@@ -9,8 +9,8 @@
 //
 // A block of threads has one (sequence, page, head) of the keys or of the values: the new values' largest magnitude, the scale,
 // the codes.  The values are held in registers between the two, 64 a thread, which is all of a page of 64 tokens of 128 dimensions; what
-// a larger page has more is read again (8194 tokens of 8 heads of 128: 15.1 us held, 18.0 read again).  Bound by the bytes where prompts are written,
-// by latency (numbers of the sequence, page number, values, codes: four trips) for single tokens.
+// a larger page has more is read again (8194 tokens of 8 heads of 128: 15.1 us held, 18.0 read again).  Bound by issue (54 % of the slots) and the
+// blocks' own beginnings where prompts are written, by latency (numbers of the sequence, page number, values, codes: four trips) for single tokens.
 #include <cmath>
 
 #include "ans_blocks.cuh"

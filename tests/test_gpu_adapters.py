@@ -152,3 +152,18 @@ def test_room_that_is_too_small_is_refused():
         with pytest.raises(B.AnsError) as e:
             B.ans_adapters(d, f._status)
         assert e.value.code == B.ANS_ERR_BUFFER_TOO_SMALL
+
+
+@pytest.mark.parametrize("rank,n_in,n_out", [(16, 512, 1024), (32, 1100, 300), (100, 64, 512)])
+@pytest.mark.parametrize("seqs", [3, 256, 257, 700])
+def test_shares_of_ragged_requests(rank, n_in, n_out, seqs):
+    """Blocks have parts of several requests' tiles: requests of many sizes, without rows, without adapters, out beside y and over it."""
+    new = [(7 * s * s + 3 * s) % (1 + 4000 // seqs) for s in range(seqs)]
+    new[seqs // 2] += 300
+    which = [(5 * s) % 9 - 1 if s % 4 else -1 for s in range(seqs)]
+    x, _, a, b, scales, y = make(8, rank, n_in, n_out, sum(new) + 40)
+    got = check(x, None, a, b, scales, y, which, sums(new))
+    for _ in range(3):
+        over = y.clone()
+        assert check(x, None, a, b, scales, over, which, sums(new), out=over) is over
+        assert torch.equal(over[:sum(new)], got[:sum(new)]) and torch.equal(over[sum(new):], y[sum(new):])
