@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   const uint64_t block = uint64_t(page) * a.c.heads + head;
   int8_t* const codes = a.c.codes[which] + block * P * dim;
   float* const scale_at = a.c.scales[which] + block;
-  const float before = from ? usable(*scale_at) : 0.f;
+  const float lay = from ? *scale_at : 0.f;           // looked at behind the values, so as not to be waited for here
 
   // a thread's pieces of eight values: token t, values c .. c + 7, the next one kBwThreads pieces on
   const uint32_t down = kBwThreads / across, right = kBwThreads % across, t0 = threadIdx.x / across, c0 = threadIdx.x % across;
@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
 #pragma unroll
   for (uint32_t i = 0; i < kBwThreads / 32; ++i) top = max(top, s_top[i]);
   float scale = scale_for(top);
+  const float before = usable(lay);
   if (from) {
     if (isnan(before)) scale = before;
     else if (before > scale) scale = before;
