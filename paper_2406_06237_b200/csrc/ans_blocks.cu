@@ -8,10 +8,14 @@
 // past a power of two.
 //
 // A block of threads has one (sequence, page, head) of the keys or of the values: the new values' largest magnitude, the scale,
-// the codes.  The values are held in registers between the two, 64 a thread, which is all of a page of 64 tokens of 128 dimensions; what
-// a larger page has more is read again (8194 tokens of 8 heads of 128: 15.1 us held, 18.0 read again).  Bound by issue (54 % of the slots) and the
-// blocks' own beginnings where prompts are written, by latency (numbers of the sequence, page number, values, codes: four trips) for single tokens.
+// the codes.  The values are held in registers between the two, 64 a thread (32 in fp32), by as many threads as that takes for a
+// page, 128 to 512; what a larger page has more is read again.  8194 tokens of 8 heads of 128 in pages of 64: 15.1 us held, 18.0 read
+// again; 8000 in pages of 128: 14.4 and 20; 1750 of 4 heads of 256 in fp32 in pages of 128: 6.7 and 17.1.  Bound by issue (54 %
+// of the slots) and the blocks' own beginnings where prompts are written, by latency (numbers of the sequence, page number,
+// values, codes: four trips) for single tokens.  Both keys and values by one block took 16.5 for the 15.1.
+#include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ans_blocks.cuh"
 
@@ -61,14 +65,13 @@ __device__ __forceinline__ float scale_for(uint32_t top) {
   return __uint_as_float(static_cast<uint32_t>(max(e, 127 - 40)) << 23);
 }
 
-constexpr uint32_t kBwThreads = 128;
-
 // gridDim.x: at least the pages that can get tokens: sequence s has places starts[s] / P + 2 s and on, of which there are at
 // least m / P + 2 before the next one's, and m new tokens lie in at most m / P + 2 pages.
-template <typename T>
-__global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const BlockWriteArgs a) {
+// THREADS: so that a page is held, if 512 can.
+template <typename T, uint32_t THREADS>
+__global__ void __launch_bounds__(THREADS) ans_block_write_kernel(const BlockWriteArgs a) {
   let_next_start();
-  __shared__ uint32_t s_top[kBwThreads / 32], s_seq;
+  __shared__ uint32_t s_top[THREADS / 32], s_seq;
   const uint32_t P = a.c.page_size, head = blockIdx.y, which = blockIdx.z, lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   wait_for_previous();
   if (warp == 0) {
@@ -81,7 +84,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   const bool first = blockIdx.x == 0 && head == 0 && which == 0;
   if (first) {                                         // what does not fit is found by one block
     bool bad = false;
-    for (uint32_t i = threadIdx.x; i < a.b.n_seqs; i += kBwThreads) {
+    for (uint32_t i = threadIdx.x; i < a.b.n_seqs; i += THREADS) {
       const Range q = range_of(a.b, i);
       bad |= !q.fits || q.fresh > q.length || q.length > uint64_t(a.b.table_pages) * P;
     }
@@ -106,8 +109,8 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   float* const scale_at = a.c.scales[which] + block;
   const float lay = from ? *scale_at : 0.f;           // looked at behind the values, so as not to be waited for here
 
-  // a thread's pieces of eight values: token t, values c .. c + 7, the next one kBwThreads pieces on
-  const uint32_t down = kBwThreads / across, right = kBwThreads % across, t0 = threadIdx.x / across, c0 = threadIdx.x % across;
+  // a thread's pieces of eight values: token t, values c .. c + 7, the next one THREADS pieces on
+  const uint32_t down = THREADS / across, right = THREADS % across, t0 = threadIdx.x / across, c0 = threadIdx.x % across;
   auto move = [&](uint32_t& t, uint32_t& c) {
     t += down;
     c += right;
@@ -127,12 +130,12 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   for (; t < to - from; move(t, c)) look(load8(x + t * a.token_stride[which] + 8u * c, a.wide[which]));
 #pragma unroll
   for (uint32_t n = 0; n < kHeld; ++n)
-    if (threadIdx.x + n * kBwThreads < pieces) look(held[n]);
+    if (threadIdx.x + n * THREADS < pieces) look(held[n]);
   top = __reduce_max_sync(kAll, top);
   if (lane == 0) s_top[warp] = top;
   __syncthreads();                                     // the old scale is read
 #pragma unroll
-  for (uint32_t i = 0; i < kBwThreads / 32; ++i) top = max(top, s_top[i]);
+  for (uint32_t i = 0; i < THREADS / 32; ++i) top = max(top, s_top[i]);
   float scale = scale_for(top);
   const float before = usable(lay);
   if (from) {
@@ -160,7 +163,7 @@ __global__ void __launch_bounds__(kBwThreads) ans_block_write_kernel(const Block
   for (; t < to - from; move(t, c)) put(load8(x + t * a.token_stride[which] + 8u * c, a.wide[which]));
   if (from && sound && scale > before) {               // the tokens before them, rounded to the larger scale
     const float shrink = before * per;
-    for (uint32_t i = threadIdx.x; i < from * across; i += kBwThreads) {
+    for (uint32_t i = threadIdx.x; i < from * across; i += THREADS) {
       uint32_t* const p = reinterpret_cast<uint32_t*>(codes + i * 8u);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -232,6 +235,15 @@ ANS_EXPORT int ans_block_cache_write(const ans_block_cache_desc* h_cache, const 
   if (places > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
   const dim3 grid(static_cast<unsigned>(places), a.c.heads, 2);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return dtype == ANS_BF16 ? launch(ans_block_write_kernel<__nv_bfloat16>, grid, dim3(kBwThreads), 0, st, 1, a)
-                           : launch(ans_block_write_kernel<float>, grid, dim3(kBwThreads), 0, st, 1, a);
+  // what a block writes if the sequences share the rows evenly: single tokens into large pages need few threads (64 in pages of
+  // 128 x 256: 6.2 us, with 512 threads 26)
+  const uint32_t values = std::min(a.c.page_size, a.b.rows / a.b.n_seqs) * a.c.dim, per_thread = dtype == ANS_BF16 ? 64u : 32u;
+  auto go = [&](auto threads) {
+    constexpr uint32_t kThreads = threads();
+    return dtype == ANS_BF16 ? launch(ans_block_write_kernel<__nv_bfloat16, kThreads>, grid, dim3(kThreads), 0, st, 1, a)
+                             : launch(ans_block_write_kernel<float, kThreads>, grid, dim3(kThreads), 0, st, 1, a);
+  };
+  if (values <= 128u * per_thread) return go(std::integral_constant<uint32_t, 128>{});
+  if (values <= 256u * per_thread) return go(std::integral_constant<uint32_t, 256>{});
+  return go(std::integral_constant<uint32_t, 512>{});
 }
