@@ -10,7 +10,7 @@
 // A block of threads has one (sequence, page, head) of the keys or of the values: the new values' largest magnitude, the scale,
 // the codes.  The values are held in registers between the two, 64 a thread (32 in fp32), by as many threads as that takes for a
 // page, 128 to 512; what a larger page has more is read again.  8194 tokens of 8 heads of 128 in pages of 64: 15.1 us held, 18.0 read
-// again; 8000 in pages of 128: 14.4 and 20; 1750 of 4 heads of 256 in fp32 in pages of 128: 6.7 and 17.1.  Bound by issue (54 %
+// again; 8000 in pages of 128: 14.4, and 23.0 by 128 threads that also waited for the old scale first; 1750 of 4 heads of 256 in fp32 in pages of 128: 6.7 and 17.1.  Bound by issue (54 %
 // of the slots) and the blocks' own beginnings where prompts are written, by latency (numbers of the sequence, page number,
 // values, codes: four trips) for single tokens.  Both keys and values by one block took 16.5 for the 15.1.
 #include <algorithm>
