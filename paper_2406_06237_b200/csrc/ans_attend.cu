@@ -17,7 +17,7 @@
 // Measured: one new token each of 64 requests with 762 to 1500 cached (32 query heads on 8, D = 128; 149 MB) 40.5 us, 3.7 TB/s;
 // one request of 32768 tokens 21.8 us.  What bounds is the issue of instructions and their latency at 4 warps a scheduler: the
 // first takes 19 us with the copies alone, about as long with the arithmetic alone, and the beginnings and ends of
-// units 7 to 9; the join is 3 to 4 of both.  Not faster: two runs of 16 tokens at a time a warp (45.3 and 39.2: fewer bytes
+// units 7 to 9; the join is 3 to 4 of both.  That a tile may count apart in the sum (ans_attend.cuh) costs 1 of the first.  Not faster: two runs of 16 tokens at a time a warp (45.3 and 39.2: fewer bytes
 // under way), dealing over warps instead of blocks (42.5 and 23.4: more parts to join).
 #include <cmath>
 
@@ -118,12 +118,13 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
   extern __shared__ __align__(128) uint8_t smem[];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, g = lane >> 2, t = lane & 3u;
   float* const sums = reinterpret_cast<float*>(smem);
-  uint4* const tiles = reinterpret_cast<uint4*>(smem + S::kBody) + warp * 64;           // of chunk c: [c % 64] {place in the codes, kscale, log2 vscale}
+  uint4* const tiles = reinterpret_cast<uint4*>(smem + S::kBody) + warp * 64;           // of chunk c: [c % 64] {place in the codes, kscale, log2 vscale}; kscale < 0: counts apart
   float2* const ml = reinterpret_cast<float2*>(smem + S::kBody + S::kMeta);            // [warp][query] {maximum, sum}
   float2* const total_ml = ml + kArWarps * Q;                                          // [query]
   float* const weight = reinterpret_cast<float*>(total_ml + Q);                        // [warp][query]
   uint32_t* const first = reinterpret_cast<uint32_t*>(smem + S::kSmem);                // [n + 1]
   __shared__ uint32_t part[kArWarps];
+  __shared__ float highest[kArWarps];                  // of a warp's unit: the largest log2 vscale so far
   const uint32_t ring = smem_addr(smem) + warp * kArStages * S::kStage;
   const uint32_t n = a.b.n_seqs;
   let_next_start();
@@ -194,11 +195,18 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
     uint32_t known = c0, scaled = c0;                  // chunks before them have their places, their scales in the table
     const uint32_t dim = EXACT ? D : a.c.dim;
     float k_of = 0.f, v_of = 0.f;
+    highest[warp] = -INFINITY;
+    __syncwarp();
     auto scales = [&]() {
       if (scaled == known) return;
       float* const to = reinterpret_cast<float*>(tiles + (scaled + lane) % 64u);
-      to[2] = usable(k_of);
-      to[3] = log2_near(usable(v_of));
+      const float k = usable(k_of), e = log2_near(usable(v_of));
+      float top = fmaxf(e, highest[warp]);
+#pragma unroll
+      for (uint32_t step = 1; step < 32; step *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, step));
+      highest[warp] = top;
+      to[2] = e + kApart < top ? -k : k;
+      to[3] = e;
       scaled = known;
       __syncwarp();
     };
@@ -345,7 +353,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
             for (int m = 0; m < NT; ++m) mma16(sc[m], a0, a1, a2, a3, qf[m][4 * i + j][0], qf[m][4 * i + j][1]);
           }
         }
-        const float e = __uint_as_float(tile.w), back = exp2_near(-e - kUp);
+        const float e = __uint_as_float(tile.w), back = __uint_as_float(tile.z) < 0.f ? 0.f : exp2_near(kSum - e);
         const bool inside = token >= all_lo && token + 16 <= all_hi;
         uint32_t p[NT][2];
 #pragma unroll
@@ -353,7 +361,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
           float best[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                // columns 2t + k: values k (token g) and k + 2 (token g + 8)
-            const float f = factor[m][k] * __uint_as_float(tile.z);
+            const float f = factor[m][k] * fabsf(__uint_as_float(tile.z));
             sc[m][k] = fmaf(sc[m][k], f, e);
             sc[m][k + 2] = fmaf(sc[m][k + 2], f, e);
             if (!inside) {
@@ -371,9 +379,9 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
           if (__any_sync(kAll, best[0] > top[m][0] || best[1] > top[m][1])) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const float now = fmaxf(top[m][k], best[k]), shrink = exp2_near(top[m][k] - now);
+              const float now = fmaxf(top[m][k], best[k]), half = exp2_near(0.5f * (top[m][k] - now)), shrink = half * half;
               top[m][k] = now;
-              sum[m][k] *= shrink;
+              sum[m][k] = sum[m][k] * half * half;
 #pragma unroll
               for (int d = 0; d < D / 16; ++d) {
                 o[m][d][k] *= shrink;
@@ -392,6 +400,12 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
           }
           p[m][0] = transpose8(pack_half(pr[0], pr[1]));
           p[m][1] = transpose8(pack_half(pr[2], pr[3]));
+        }
+        if (__any_sync(kAll, __uint_as_float(tile.z) < 0.f)) {         // the same for all lanes, which the vote tells the compiler
+#pragma unroll
+          for (int m = 0; m < NT; ++m)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) sum[m][k] += exp2_near(sc[m][k] - e + (kUp + kSum - top[m][k])) + exp2_near(sc[m][k + 2] - e + (kUp + kSum - top[m][k]));
         }
         // values: rows 2t, 2t + 1, 2t + 8, 2t + 9
         constexpr int kWords = D / 32;                 // of a row, for this lane
@@ -453,9 +467,9 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       for (uint32_t w = 0; w < kArWarps; ++w) most = fmaxf(most, ml[w * Q + threadIdx.x].x);
       for (uint32_t w = 0; w < kArWarps; ++w) {
         const float2 x = ml[w * Q + threadIdx.x];
-        const float f = exp2_near(x.x - most);
-        weight[w * Q + threadIdx.x] = f;
-        all = fmaf(f, x.y, all);
+        const float half = exp2_near(0.5f * (x.x - most));
+        weight[w * Q + threadIdx.x] = half * half;
+        all = fmaf(half, half * x.y, all);
       }
       total_ml[threadIdx.x] = make_float2(most, all);
     }
@@ -473,7 +487,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       }
       if (whole) {
         if (d < a.c.dim) {
-          const float l = total_ml[r].y, f = l == 0.f ? 0.f : exp2_near(-kUp) / l;
+          const float l = total_ml[r].y, f = l == 0.f ? 0.f : kFromSum / l;
           const uint32_t row = token_of(a, r0 + r), j = (r0 + r) - row * a.share;
           __nv_bfloat162* const to = reinterpret_cast<__nv_bfloat162*>(a.out + (q.row + row) * a.out_token + (head * a.share + j) * a.out_head + d);
           to[0] = __floats2bfloat162_rn(x.x * f, x.y * f);
@@ -535,9 +549,9 @@ __global__ void __launch_bounds__(32 * kAjWarps) ans_attend_join_kernel(const At
       for (uint32_t k = 0; k < kMany; ++k) top = fmaxf(top, m[k].x);
 #pragma unroll
       for (uint32_t step = 1; step < 32; step *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, step));
-      const float shrink = exp2_near(most - top);
+      const float half = exp2_near(0.5f * (most - top)), shrink = half * half;
       most = top;
-      all *= shrink;
+      all = all * half * half;
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) x[k] *= shrink;
       uint32_t have = 0;
@@ -546,10 +560,10 @@ __global__ void __launch_bounds__(32 * kAjWarps) ans_attend_join_kernel(const At
       for (uint32_t k = 0; k < kMany; ++k) {
         const bool some = m[k].y != 0.f;             // a NaN counts
         const uint32_t some_of = __ballot_sync(kAll, some);
-        const float f = exp2_near(m[k].x - most);
+        const float half = exp2_near(0.5f * (m[k].x - most));
         if (some) {
-          found[warp][have + __popc(some_of & ((1u << lane) - 1u))] = make_float2(__uint_as_float(slot(b0 + 32u * k + lane)), f);
-          own = fmaf(f, m[k].y, own);
+          found[warp][have + __popc(some_of & ((1u << lane) - 1u))] = make_float2(__uint_as_float(slot(b0 + 32u * k + lane)), half * half);
+          own = fmaf(half, half * m[k].y, own);
         }
         have += __popc(some_of);
       }
@@ -582,7 +596,7 @@ __global__ void __launch_bounds__(32 * kAjWarps) ans_attend_join_kernel(const At
     const uint32_t row = token_of(a, r0 + r), j = (r0 + r) - row * a.share;
     __nv_bfloat16* const to = a.out + (q.row + row) * a.out_token + (head * a.share + j) * a.out_head;
     if constexpr (ALONE) {
-      const float f = all == 0.f ? 0.f : exp2_near(-kUp) / all;
+      const float f = all == 0.f ? 0.f : kFromSum / all;
 #pragma unroll
       for (int k = 0; k < D / 64; ++k) {
         const uint32_t d = 64u * k + 2u * lane;
@@ -601,10 +615,11 @@ __global__ void __launch_bounds__(32 * kAjWarps) ans_attend_join_kernel(const At
     float f[kAjWarps];
 #pragma unroll
     for (uint32_t w = 0; w < kAjWarps; ++w) {
-      f[w] = exp2_near(parts_ml[w].x - most);
-      all = fmaf(f[w], parts_ml[w].y, all);
+      const float half = exp2_near(0.5f * (parts_ml[w].x - most));
+      f[w] = half * half;
+      all = fmaf(half, half * parts_ml[w].y, all);
     }
-    const float over = all == 0.f ? 0.f : exp2_near(-kUp) / all;
+    const float over = all == 0.f ? 0.f : kFromSum / all;
     for (uint32_t d = 2u * threadIdx.x; d < a.c.dim; d += 64 * kAjWarps) {
       float y0 = 0.f, y1 = 0.f;
 #pragma unroll

@@ -3,10 +3,16 @@
 // With s_i = scale * log2(e) * (q . k_i), k_i = kscale_i * kcode_i, v_i = vscale_i * vcode_i, the output is
 //   sum_i 2^(s_i) vscale_i vcode_i / sum_i 2^(s_i).
 // The scales of values go into the exponent: e_i = log2(vscale_i), M = max_i (s_i + e_i), and
-//   P_i = 2^(s_i + e_i - M + kUp),   out = 2^-kUp * sum_i P_i vcode_i / L,   L = sum_i 2^(s_i - M) = sum_i P_i 2^(-e_i - kUp),
+//   P_i = 2^(s_i + e_i - M + kUp),   out = 2^kSum * sum_i P_i vcode_i / L,   L = 2^(kUp + kSum) * sum_i 2^(s_i - M) = sum_i P_i 2^(kSum - e_i),
 // so that the matrix instructions meet small integers (codes, exact in fp16) with P_i <= 2^kUp in fp16, whose relative error of
 // 2^-11 then reaches down to 2^-(14 + kUp) of the largest term, and no product with a scale is rounded on its own.  Scales that
 // the cache's write makes are powers of two, so e_i is an integer and the terms of L are exact multiples of P_i.
+// L adds the P_i before they are rounded to fp16.
+//
+// e_i is -40 to 128.  2^(kSum - e_i) is then a normal number, and L one of 2^-101 to 2^105 (2^30 tokens).  As a P_i below fp32's range
+// may still count in L, where the largest e is far above its own (a block of zeros beside values of 1e30), blocks whose e is kApart below the
+// largest one met so far add 2^(s_i - M + kUp + kSum) to L by an exponential of their own: what is lost elsewhere is under 2^-40 of the largest
+// term of L.  For the same reason L goes to another M by two factors of half the exponent.
 // A block of 16 tokens lies in one page, so both scales are constants of such a block.
 #pragma once
 
@@ -16,6 +22,8 @@ namespace ansb {
 namespace blk {
 
 constexpr float kUp = 14.f;
+constexpr float kSum = 20.f, kFromSum = 1048576.f;     // 2^kSum
+constexpr float kApart = 90.f;
 constexpr float kLowest = -3.402823466e38f;
 
 struct AttendArgs {

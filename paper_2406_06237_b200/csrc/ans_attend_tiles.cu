@@ -67,6 +67,9 @@ __device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32
                   "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
                   "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]));
 }
+__device__ __forceinline__ void tmem_load4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // operand of tokens x dimensions with the dimensions contiguous: 64 of them in 128 bytes, 8 tokens in 1024, panels `panel` bytes apart
 __device__ __forceinline__ uint64_t operand_across(uint32_t addr, uint32_t panel) {
@@ -279,9 +282,9 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           best = fmaxf(best, fmaf(fmaxf(m, __uint_as_float(v[16 * b + 15])), f, e));
         }
         if (__any_sync(kAll, best > top + kSlack)) {
-          const float now = fmaxf(top, best), shrink = exp2_near(top - now);
+          const float now = fmaxf(top, best), by_half = exp2_near(0.5f * (top - now)), shrink = by_half * by_half;
           top = now;
-          sum *= shrink;
+          sum = sum * by_half * by_half;
           if (n) {
             bar_wait(o_done + 8 * half, (n - 1u) & 1u, bad);           // the products before are done; the next ones wait for P
             __syncwarp();
@@ -295,6 +298,22 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
               for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * shrink);
               tmem_store(o_at + c, o);
             }
+          }
+        }
+        // Runs that count in the sum by exponentials of their own, a few columns of S at a time: out of the registers of v this would cost heads
+        // of 256 dimensions their registers (1500 rows 69.8 us, so 49.4).
+        if (__any_sync(kAll, scales[stage * S::kSubs].w != 0.f)) {
+#pragma unroll 1
+          for (uint32_t c = 0; c < S::kTokens; c += 4) {
+            const float4 m = scales[stage * S::kSubs + c / 16u];
+            if (m.w < 2.f) continue;
+            uint32_t now[4];
+            tmem_load4(s_at + c, now);
+            tmem_wait();
+            hide(now, lo - static_cast<int32_t>(c), hi - static_cast<int32_t>(c));
+            const float f = fmaxf(factor * m.x, kLeastFactor), less = kUpTile + kSum - top;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) sum += exp2_near(fmaf(__uint_as_float(now[k]), f, less));
           }
         }
         // one stretch of code without branches, so that the runs' chains of instructions run beside each other
@@ -336,7 +355,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
       bar_wait(o_full, 0u, bad);
       __syncwarp();
       fence_after();
-      const float f = sum == 0.f ? 0.f : exp2_near(-kUpTile) / sum;
+      const float f = sum == 0.f ? 0.f : kFromSum / sum;
       const uint32_t heads = a.share * a.c.heads;
       const uint64_t part = (uint64_t(blockIdx.z) * a.b.rows + T.row + i) * heads + head * a.share + j;
       if (splits > 1 && live) reinterpret_cast<float2*>(a.parts + uint64_t(splits) * a.b.rows * heads * D)[part] = make_float2(top, sum);
@@ -488,7 +507,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     }
   } else if (mine && warp == kAtScales) {
     // ---- scales: lane b has run b of every block
-    float ks, e, back;
+    float ks, e, back, high = -INFINITY;               // high: the largest e so far
     auto look = [&](uint32_t block) {
       const uint32_t token = block * S::kTokens + lane * 16u;
       ks = 1.f; e = -INFINITY; back = 0.f;             // not there: not seen
@@ -499,7 +518,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           ks = usable(a.c.scales[0][at]);
           e = log2_near(usable(a.c.scales[1][at]));
           if (isnan(ks)) e = ks;
-          back = isnan(e) ? 1.f : exp2_near(-e - kUpTile);             // where e is NaN, so is what is summed
+          back = isnan(e) ? 1.f : exp2_near(kSum - e);                 // where e is NaN, so is what is summed
         } else {
           atomicOr(a.status, ANS_STATUS_BAD_PAGE);
         }
@@ -508,9 +527,16 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
     for (uint32_t n = 0; n < blocks; ++n) {
       const uint32_t stage = n % S::kStages, round = n / S::kStages;
       look(first + n);
+      float top = e;
+#pragma unroll
+      for (uint32_t step = 1; step < S::kSubs; step *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, step));
+      high = fmaxf(high, top);
+      const bool apart = e + kApart < high && e > kLowest;
+      if (apart) back = 0.f;
+      const float how = (__any_sync(kAll, apart) ? 1.f : 0.f) + (apart ? 1.f : 0.f);          // 1: a run of the block is, 2: this one
       if (round) bar_wait(v_empty + 8 * stage, (round - 1u) & 1u, bad);
       if (lane < S::kSubs)
-        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(meta + (stage * S::kSubs + lane) * 16u), "f"(ks), "f"(e), "f"(back), "f"(0.f) : "memory");
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"(meta + (stage * S::kSubs + lane) * 16u), "f"(ks), "f"(e), "f"(back), "f"(how) : "memory");
       __syncwarp();
       if (lane == 0) arrive(v_full + 8 * stage);
     }
@@ -604,8 +630,8 @@ __global__ void __launch_bounds__(256) ans_attend_tiles_join_kernel(const Attend
 #pragma unroll 2
   for (uint32_t z = 0; z < splits; ++z) {
     const float2 m = ml[z * all + at];
-    const float f = exp2_near(m.x - most);
-    sum = fmaf(f, m.y, sum);
+    const float half = exp2_near(0.5f * (m.x - most)), f = half * half;
+    sum = fmaf(half, half * m.y, sum);
 #pragma unroll
     for (int k = 0; k < D / 64; ++k) {
       const float2 v = *reinterpret_cast<const float2*>(a.parts + (z * all + at) * D + 64 * k + 2 * lane);
@@ -613,7 +639,7 @@ __global__ void __launch_bounds__(256) ans_attend_tiles_join_kernel(const Attend
       x[2 * k + 1] = fmaf(f, v.y, x[2 * k + 1]);
     }
   }
-  const float f = sum == 0.f ? 0.f : exp2_near(-kUpTile) / sum;
+  const float f = sum == 0.f ? 0.f : kFromSum / sum;
   __nv_bfloat16* const to = a.out + row * a.out_token + head * a.out_head;
 #pragma unroll
   for (int k = 0; k < D / 64; ++k) {
