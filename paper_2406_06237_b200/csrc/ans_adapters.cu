@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kAdThreads, R * MT >= 128 ? 1 : 2) ans_adapter
       float sum = 0.f;
 #pragma unroll
       for (uint32_t w = 0; w < kAdWarps; ++w) sum += parts[w * S::kPart + (e / R) * (R + 8) + e % R];
-      h[e] = sum;
+      h[e] = e % R < a.rank ? sum : 0.f;                 // not what the zeros behind the rank make of an infinity
     }
     __syncthreads();                                     // the warps' sums are read
   }
