@@ -160,7 +160,7 @@ class Adapters(_Handle):
         _vector_of(which, n, dev, "which")
         _vector_of(starts, n + 1, dev, "starts")
         d.x_stride, d.y_stride, d.out_stride = _rows(x, "x"), _rows(y, "y"), _rows(out, "out")
-        _need(out.data_ptr() != y.data_ptr() or d.out_stride == d.y_stride, "out lies over y with other strides")
+        _need(rows <= 1 or not y.numel() or out.data_ptr() != y.data_ptr() or d.out_stride == d.y_stride, "out lies over y with other strides")
         d.rows, d.n_seqs, d.x_dtype, d.y_dtype = rows, n, _ELEMENT[x.dtype], _ELEMENT[y.dtype]
 
 
@@ -275,7 +275,7 @@ class BlockCache(_Handle):
         _need(q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16, "q and out must be bf16")
         _need(out.shape == q.shape and out.stride(2) == 1, "out must be of q's shape, the values of a head contiguous")
         _need(out.data_ptr() % 4 == 0 and out.stride(0) % 2 == 0 and out.stride(1) % 2 == 0, "the heads of out must start on 4 bytes")
-        _need(out.data_ptr() != q.data_ptr() or out.stride() == q.stride(), "out lies over q with other strides")
+        _need(not q.numel() or out.data_ptr() != q.data_ptr() or out.stride() == q.stride(), "out lies over q with other strides")
         _on_device(q, self.device, "q")
         _on_device(out, self.device, "out")
         _need(window >= 0, "window must not be negative")
