@@ -31,6 +31,11 @@ def _check_tables(tables: torch.Tensor, device) -> tuple[int, int, int]:
     return n, pages, tables.stride(0)
 
 
+def _steps(t: torch.Tensor) -> tuple[int, int]:
+    """Strides of rows and heads, 0 for the one row or head that has no next one."""
+    return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
+
+
 class Batch(NamedTuple):
     """What PageTables makes: starts, ends (sums of the lengths: what PagedCache.read takes as starts), lengths,
     slots (for PagedCache.write), positions, and the number of entries of the free list that are taken."""
@@ -247,7 +252,8 @@ class BlockCache(_Handle):
         behind the last request's are not written."""
         st, b, d = self._enter(), self._attend_batch, self._attend
         if q.dim() == 3 and (q.data_ptr() % 16 or q.stride(2) != 1 or q.stride(0) % 8 or q.stride(1) % 8):
-            q = q.contiguous() if not q.is_contiguous() else q.clone()
+            if q.data_ptr() % 16 or q.stride(2) != 1 or any(step % 8 for step in _steps(q)):
+                q = q.clone(memory_format=torch.contiguous_format)
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
         at = self._seen.places(q, out, tables, lengths, starts)
@@ -274,13 +280,14 @@ class BlockCache(_Handle):
         _need(q.shape[1] > 0 and q.shape[1] % self.heads == 0, "the query heads must be a multiple of the cache's heads")
         _need(q.dtype is torch.bfloat16 and out.dtype is torch.bfloat16, "q and out must be bf16")
         _need(out.shape == q.shape and out.stride(2) == 1, "out must be of q's shape, the values of a head contiguous")
-        _need(out.data_ptr() % 4 == 0 and out.stride(0) % 2 == 0 and out.stride(1) % 2 == 0, "the heads of out must start on 4 bytes")
-        _need(not q.numel() or out.data_ptr() != q.data_ptr() or out.stride() == q.stride(), "out lies over q with other strides")
+        qs, outs = _steps(q), _steps(out)
+        _need(out.data_ptr() % 4 == 0 and outs[0] % 2 == 0 and outs[1] % 2 == 0, "the heads of out must start on 4 bytes")
+        _need(not q.numel() or out.data_ptr() != q.data_ptr() or outs == qs, "out lies over q with other strides")
         _on_device(q, self.device, "q")
         _on_device(out, self.device, "out")
         _need(window >= 0, "window must not be negative")
         _need(longest is None or longest > 0, "longest must be positive")
         self._batch(self._attend_batch, tables, lengths, starts, q.shape[0])
-        d.q_token_stride, d.q_head_stride, d.out_token_stride, d.out_head_stride = *q.stride()[:2], *out.stride()[:2]
+        d.q_token_stride, d.q_head_stride, d.out_token_stride, d.out_head_stride = *qs, *outs
         d.q_heads, d.longest, d.window, d.causal = q.shape[1], min(longest or 0, q.shape[0]), min(window, 2 ** 31 - 1), int(causal)
         d.scale = self.head_dim ** -0.5 if scale is None else scale

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from batch_helpers import BF16, ints
+from batch_helpers import BF16, attention, fill_cache, ints
+from operator_helpers import rounds_from
 from paper_2406_06237_b200.runtime import Adapters, BlockCache
 
 pytestmark = pytest.mark.gpu
@@ -16,3 +17,25 @@ def test_a_batch_without_rows_out_of_wider_buffers():
     wide = torch.zeros(5, 100, dtype=BF16, device="cuda")
     assert f(wide[:0, :32], wide[:0, 40:64], ints([0]), ints([0, 0])).shape == (0, 24)
     assert cache.read_status() == 0 and f.read_status() == 0
+
+
+@pytest.mark.parametrize("heads", [1, 2])
+@pytest.mark.parametrize("off", [0, 1])
+def test_one_token_out_of_a_row_of_any_length(heads, off):
+    """With one token (and one head) the distance to the next one is no one's concern."""
+    arrays = fill_cache(4, heads, 16, 64)
+    cache, tables = BlockCache.wrap(*arrays), ints([[0, 1, 2, 3]])
+    flat = torch.randn(128 * heads + 200, device="cuda").to(BF16)
+    q = flat.as_strided((1, 2 * heads, 64), (128 * heads + 3, 64, 1), off)
+    out = torch.zeros(300 * heads, dtype=BF16, device="cuda").as_strided((1, 2 * heads, 64), (128 * heads + 5, 64, 1), 2 * off)
+    want, slack = attention(q, arrays, tables, [50], [0, 1])
+    assert rounds_from(cache.attend(q, tables, ints([50]), ints([0, 1])), want, slack).all()
+    assert rounds_from(cache.attend(q, tables, ints([50]), ints([0, 1]), out=out), want, slack).all()
+    alone = flat.as_strided((3, 1, 64), (64, 67, 1), 0)
+    one = BlockCache.wrap(*(t[:, :1].contiguous() for t in arrays))
+    want, slack = attention(alone, (one.k_codes, one.k_scales, one.v_codes, one.v_scales), tables, [50], [0, 3])
+    assert rounds_from(one.attend(alone, tables, ints([50]), ints([0, 3])), want, slack).all()
+    own = flat.as_strided((1, 2 * heads, 64), (128 * heads + 3, 64, 1), 0)
+    want, slack = attention(own.clone(), arrays, tables, [50], [0, 1])
+    assert cache.attend(own, tables, ints([50]), ints([0, 1]), out=flat[:128 * heads].view(1, 2 * heads, 64)) is not own       # over q
+    assert rounds_from(own, want, slack).all() and cache.read_status() == 0
