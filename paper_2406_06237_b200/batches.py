@@ -260,13 +260,12 @@ class BlockCache(_Handle):
         if at is None or (scale, causal, window, longest) != self._attend_args:
             self._seen.keep()
             self._check_attend(q, out, tables, lengths, starts, scale, causal, window, longest)
-            self._seen.keep(q, out, tables, lengths, starts)
-            self._attend_args = (scale, causal, window, longest)
-            at = self._seen.places(q, out, tables, lengths, starts)
+            at = tuple(t.data_ptr() for t in (q, out, tables, lengths, starts))
             d.d_q, d.d_out, b.d_tables, b.d_lengths, b.d_starts = at
             self._room_bytes = B.ans_attend_room_bytes(self._desc, b, d)
-        else:
-            d.d_q, d.d_out, b.d_tables, b.d_lengths, b.d_starts = at
+            self._seen.keep(q, out, tables, lengths, starts)           # nothing is left to refuse
+            self._attend_args = (scale, causal, window, longest)
+        d.d_q, d.d_out, b.d_tables, b.d_lengths, b.d_starts = at
         d.room_bytes = self._room_bytes
         if self._room_bytes:
             room = torch.empty(self._room_bytes, dtype=torch.uint8, device=self.device)

@@ -4,6 +4,7 @@ import torch
 
 from batch_helpers import BF16, attention, fill_cache, ints
 from operator_helpers import rounds_from
+from paper_2406_06237_b200 import binding as B
 from paper_2406_06237_b200.runtime import Adapters, BlockCache
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,12 @@ def test_one_token_out_of_a_row_of_any_length(heads, off):
     want, slack = attention(own.clone(), arrays, tables, [50], [0, 1])
     assert cache.attend(own, tables, ints([50]), ints([0, 1]), out=flat[:128 * heads].view(1, 2 * heads, 64)) is not own       # over q
     assert rounds_from(own, want, slack).all() and cache.read_status() == 0
+
+
+@pytest.mark.parametrize("change", [dict(scale=float("inf")), dict(share=129)])
+def test_what_is_refused_is_refused_again(change):
+    cache = BlockCache(4, 16, 1, 16)
+    q = torch.zeros(2, change.pop("share", 4), 16, dtype=BF16, device="cuda")
+    for _ in range(2):
+        with pytest.raises(B.AnsError):
+            cache.attend(q, ints([[0]]), ints([5]), ints([0, 2]), **change)
