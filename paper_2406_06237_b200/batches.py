@@ -22,10 +22,16 @@ def _vector_of(t: torch.Tensor, n: int, device, what: str, dtype=_INT) -> None:
     _on_device(t, device, what)
 
 
+def _counts(*sizes: int) -> None:
+    """The library counts in 32 bits."""
+    _need(max(sizes) < 2 ** 31, "sizes must be under 2^31")
+
+
 def _check_tables(tables: torch.Tensor, device) -> tuple[int, int, int]:
     """(sequences, pages, row stride)"""
     _need(tables.dtype is _INT and tables.dim() == 2 and (tables.shape[1] <= 1 or tables.stride(1) == 1), "tables must be int32 [sequences, pages]")
     n, pages = tables.shape
+    _counts(n, pages)
     _need(n <= 1 or tables.stride(0) >= pages, "the rows of tables overlap")
     _on_device(tables, device, "tables")
     return n, pages, tables.stride(0)
@@ -52,7 +58,7 @@ class PageTables(_Handle):
 
     def __init__(self, page_size: int, device="cuda"):
         super().__init__(device)
-        _need(page_size > 0, "page_size must be positive")
+        _need(0 < page_size <= 1 << 20, "page_size must be 1 to 2^20")
         self.page_size = page_size
         self._form = self._new_form()
         self._desc = d = B.ans_pages_desc()
@@ -98,6 +104,7 @@ class PageTables(_Handle):
         rows = out.slots.shape[0]
         _vector_of(out.slots, rows, dev, "out.slots", torch.int64)
         _vector_of(out.positions, rows, dev, "out.positions")
+        _counts(free.shape[0], rows)
         d.n_seqs, d.n_free, d.rows = n, free.shape[0], rows
 
 
@@ -116,6 +123,7 @@ class Adapters(_Handle):
         _need(a.dtype is torch.bfloat16 and b.dtype is torch.bfloat16, "a and b must be bf16")
         _need(a.is_contiguous() and b.is_contiguous(), "a and b must be contiguous")
         _need(0 < rank <= 128 and n_in > 0, "rank must be 1 to 128, in features positive")
+        _counts(count, n_in, b.shape[1])
         _on_device(b, self.device, "b")
         if scales is not None:
             _vector_of(scales, count, self.device, "scales", torch.float32)
@@ -166,6 +174,7 @@ class Adapters(_Handle):
         _vector_of(starts, n + 1, dev, "starts")
         d.x_stride, d.y_stride, d.out_stride = _rows(x, "x"), _rows(y, "y"), _rows(out, "out")
         _need(rows <= 1 or not y.numel() or out.data_ptr() != y.data_ptr() or d.out_stride == d.y_stride, "out lies over y with other strides")
+        _counts(rows, n)
         d.rows, d.n_seqs, d.x_dtype, d.y_dtype = rows, n, _ELEMENT[x.dtype], _ELEMENT[y.dtype]
 
 
@@ -199,6 +208,7 @@ class BlockCache(_Handle):
             _on_device(t, self.device, what)
         for size, what in ((self.page_size, "page_size"), (self.head_dim, "head_dim")):
             _need(size % 16 == 0 and 0 < size <= 256, f"{what} must be a multiple of 16 up to 256")
+        _counts(self.n_pages, self.heads)
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
         self._wrote, self._seen = self._new_form(), self._new_form()
         self._desc = d = B.ans_block_cache_desc()
@@ -210,6 +220,7 @@ class BlockCache(_Handle):
 
     def _batch(self, b, tables, lengths, starts, rows):
         n, b.table_pages, b.table_stride = _check_tables(tables, self.device)
+        _counts(rows)
         b.n_seqs = n
         _vector_of(lengths, n, self.device, "lengths")
         _vector_of(starts, n + 1, self.device, "starts")

@@ -2,10 +2,10 @@
 import pytest
 import torch
 
-from batch_helpers import BF16, attention, fill_cache, ints
+from batch_helpers import BF16, INT, attention, fill_cache, ints
 from operator_helpers import rounds_from
 from paper_2406_06237_b200 import binding as B
-from paper_2406_06237_b200.runtime import Adapters, BlockCache
+from paper_2406_06237_b200.runtime import Adapters, BlockCache, PageTables
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,20 @@ def test_what_is_refused_is_refused_again(change):
     for _ in range(2):
         with pytest.raises(B.AnsError):
             cache.attend(q, ints([[0]]), ints([5]), ints([0, 2]), **change)
+
+
+def test_sizes_that_32_bits_do_not_hold():
+    for page_size in (0, -1, (1 << 20) + 1, (1 << 32) + 16):
+        with pytest.raises(ValueError):
+            PageTables(page_size)
+    many = (1 << 32) + 1
+    one, none = ints([0]), ints([])
+    with pytest.raises(ValueError):
+        PageTables(16)(ints([[0]]), one, one, torch.empty(many, dtype=INT, device="cuda"), one, rows=4)
+    f = Adapters(torch.zeros(1, 1, 1, dtype=BF16, device="cuda"), torch.zeros(1, 1, 1, dtype=BF16, device="cuda"))
+    x = torch.empty(many, 1, dtype=BF16, device="cuda")
+    with pytest.raises(ValueError):
+        f(x, x, one, ints([0, 0]), out=x)
+    with pytest.raises(ValueError):
+        Adapters(torch.empty(1, 1, many, dtype=BF16, device="cuda"), torch.zeros(1, 1, 1, dtype=BF16, device="cuda"))
+    assert none.numel() == 0
