@@ -42,6 +42,25 @@ def _steps(t: torch.Tensor) -> tuple[int, int]:
     return t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0
 
 
+def _overlaps(t: torch.Tensor) -> bool:
+    """Whether two heads of [rows, heads, dim], the values of a head contiguous, share an element."""
+    (rows, heads, dim), (row, head) = t.shape, _steps(t)
+    if not t.numel():
+        return False
+    if heads == 1 or head >= dim:                          # the usual forms: heads within rows, or rows within heads
+        if rows == 1 or row >= head * (heads - 1) + dim:
+            return False
+    if rows > 1 and row < dim:
+        return True
+    if heads > 1 and head >= row * (rows - 1) + dim:
+        return False
+    for h in range(heads):                                 # heads h apart: the two numbers of rows that bring them nearest
+        for r in ((-(h * head // row), -(h * head // row) - 1) if rows > 1 else (0,)):
+            if (r or h) and -rows < r and abs(r * row + h * head) < dim:
+                return True
+    return False
+
+
 class Batch(NamedTuple):
     """What PageTables makes: starts, ends (sums of the lengths: what PagedCache.read takes as starts), lengths,
     slots (for PagedCache.write), positions, and the number of entries of the free list that are taken."""
@@ -293,6 +312,7 @@ class BlockCache(_Handle):
         qs, outs = _steps(q), _steps(out)
         _need(out.data_ptr() % 4 == 0 and outs[0] % 2 == 0 and outs[1] % 2 == 0, "the heads of out must start on 4 bytes")
         _need(not q.numel() or out.data_ptr() != q.data_ptr() or outs == qs, "out lies over q with other strides")
+        _need(not _overlaps(out), "the heads of out lie over each other")
         _on_device(q, self.device, "q")
         _on_device(out, self.device, "out")
         _need(window >= 0, "window must not be negative")

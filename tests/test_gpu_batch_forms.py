@@ -66,3 +66,15 @@ def test_sizes_that_32_bits_do_not_hold():
     with pytest.raises(ValueError):
         Adapters(torch.empty(1, 1, many, dtype=BF16, device="cuda"), torch.zeros(1, 1, 1, dtype=BF16, device="cuda"))
     assert none.numel() == 0
+
+
+def test_an_output_whose_rows_lie_over_each_other():
+    cache = BlockCache(4, 16, 2, 64)
+    q = torch.zeros(3, 4, 64, dtype=BF16, device="cuda")
+    flat = torch.zeros(4096, dtype=BF16, device="cuda")
+    for strides in ((0, 64, 1), (256, 0, 1), (256, 32, 1), (128, 64, 1), (64, 128, 1)):
+        with pytest.raises(ValueError):
+            cache.attend(q, ints([[0]]), ints([5]), ints([0, 3]), out=flat.as_strided((3, 4, 64), strides))
+    for strides in ((256, 64, 1), (64, 192, 1), (64, 200, 1), (300, 66, 1)):
+        cache.attend(q, ints([[0]]), ints([5]), ints([0, 3]), out=flat.as_strided((3, 4, 64), strides))
+    assert cache.read_status() == 0
