@@ -655,7 +655,8 @@ int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_d
  * Scales are taken as they are if they are at least 2^-40 (less counts as 2^-40).  Logits of about 1e38 and more are not supported.
  * `longest`: the most new tokens of a sequence, if the caller knows it (0: no knowledge): choosing the kernels by it
  * saves time, results do not depend on its being right.
- * Pages outside the cache, or tokens past table_pages pages or 2^30 tokens, count as not there and are flagged ANS_STATUS_BAD_PAGE.
+ * Pages outside the cache, or tokens past table_pages pages or 2^30 tokens, count as not there and are flagged ANS_STATUS_BAD_PAGE.  Entries
+ * of pages of which no row sees a token, as the window has left them behind, may hold anything.
  * d_room: 16-byte aligned, ans_attend_room_bytes() bytes, free again when the call's work is done.
  */
 typedef struct ans_attend_desc {

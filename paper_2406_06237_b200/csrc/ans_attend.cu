@@ -84,7 +84,7 @@ template <int D> __device__ __forceinline__ uint32_t v_piece(uint32_t row, uint3
 struct ArSeq {
   uint32_t row, fresh;
   int32_t old, length;                                 // old: tokens before the new ones (negative: some rows see nothing)
-  uint32_t begin, chunks, groups;                      // first token (a multiple of a chunk's), chunks of a unit, groups of queries
+  uint32_t first, begin, chunks, groups;               // first token that a row sees, and its chunk's, chunks of a unit, groups of queries
 };
 template <uint32_t QUERIES>
 __device__ __forceinline__ ArSeq ar_sequence(const AttendArgs& a, uint32_t s, bool& bad) {
@@ -98,7 +98,8 @@ __device__ __forceinline__ ArSeq ar_sequence(const AttendArgs& a, uint32_t s, bo
   q.old = static_cast<int32_t>(r.length) - static_cast<int32_t>(r.fresh);
   const uint64_t rows = uint64_t(r.fresh) * a.share;
   q.groups = rows >= a.least && rows <= a.most ? static_cast<uint32_t>((rows + QUERIES - 1) / QUERIES) : 0u;
-  q.begin = static_cast<uint32_t>(max(seen_by(a, q.old, q.length, 0).first, 0)) / kArChunk * kArChunk;
+  q.first = static_cast<uint32_t>(max(seen_by(a, q.old, q.length, 0).first, 0));
+  q.begin = q.first / kArChunk * kArChunk;
   const uint32_t tokens = q.length > static_cast<int32_t>(q.begin) ? q.length - q.begin : 0u;
   q.chunks = max((tokens + kArChunk - 1) / kArChunk, 1u);
   return q;
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(kArThreads, D * NT <= 128 ? 2 : 1) ans_attend_
       scales();
       const uint32_t c = known + lane, token = q.begin + c * kArChunk + warp * 16u;
       uint64_t where = ~uint64_t(0);                   // not there
-      if (c < c1 && token < static_cast<uint32_t>(q.length)) {
+      if (c < c1 && token < static_cast<uint32_t>(q.length) && token + 16u > q.first) {          // what the window has left need not be there
         const uint32_t in = token / a.c.page_size;
         const int32_t page = table[in];
         if (page >= 0 && static_cast<uint32_t>(page) < a.c.n_pages) {

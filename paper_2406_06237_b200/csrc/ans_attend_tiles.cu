@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(kAtThreads, 1) ans_attend_tiles_kernel(const A
           e = log2_near(usable(a.c.scales[1][at]));
           if (isnan(ks)) e = ks;
           back = isnan(e) ? 1.f : exp2_near(kSum - e);                 // where e is NaN, so is what is summed
-        } else {
+        } else if (token + 16u > static_cast<uint32_t>(seen_by(a, T.old, T.length, token_of(a, T.r0)).first)) {       // what the window has left need not be there
           atomicOr(a.status, ANS_STATUS_BAD_PAGE);
         }
       }
