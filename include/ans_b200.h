@@ -652,7 +652,8 @@ int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_d
  * fp16 number scaled by a power of two (p_i times the scale of its block of values is off by 2^-11 of itself, or by 2^-32 of the largest such
  * product of the row where that is more), q as fp16 scaled likewise, row by row (exact, but for values
  * under 2^-14 of the row's largest, which are off by at most 2^-25 of it).
- * Scales are taken as they are if they are at least 2^-40 (less counts as 2^-40).  Logits of about 1e38 and more are not supported.
+ * Scales are taken as they are if they are at least 2^-40 (less counts as 2^-40).  Logits of about 1e38 and more are not
+ * supported, nor are products of that size of `scale` and a value of q.
  * `longest`: the most new tokens of a sequence, if the caller knows it (0: no knowledge): choosing the kernels by it
  * saves time, results do not depend on its being right.
  * Pages outside the cache, or tokens past table_pages pages or 2^30 tokens, count as not there and are flagged ANS_STATUS_BAD_PAGE.  Entries
@@ -665,7 +666,7 @@ typedef struct ans_attend_desc {
   uint32_t q_heads;               /* a multiple of the cache's heads, up to 128 times them   */
   uint32_t longest, window;
   int32_t causal;
-  float scale;                    /* finite                                                  */
+  float scale;                    /* finite, times log2(e) too                               */
   void* d_room; uint64_t room_bytes;
 } ans_attend_desc;
 int ans_attend(const ans_block_cache_desc* h_cache, const ans_batch_desc* h_batch, const ans_attend_desc* h_desc, uint32_t* d_status, void* stream);

@@ -685,7 +685,8 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   if (rc != ANS_OK) return rc;
   if (d.q_heads == 0 || d.q_heads % a.c.heads) return ANS_ERR_INVALID_ARG;
   if (d.q_heads / a.c.heads > 128 || uint64_t(a.b.rows) * (d.q_heads / a.c.heads) > 0x7FFFFFFFull) return ANS_ERR_UNSUPPORTED;
-  if (!std::isfinite(d.scale)) return ANS_ERR_INVALID_ARG;
+  a.scale2 = static_cast<float>(d.scale * 1.4426950408889634);
+  if (!std::isfinite(a.scale2)) return ANS_ERR_INVALID_ARG;
   if (a.b.n_seqs == 0 || a.b.rows == 0) return ANS_OK;
   if (!d.d_q || !d.d_out || (reinterpret_cast<uintptr_t>(d.d_q) & 15) || (reinterpret_cast<uintptr_t>(d.d_out) & 3)) return ANS_ERR_INVALID_ARG;
   if ((d.q_token_stride | d.q_head_stride) & 7 || (d.out_token_stride | d.out_head_stride) & 1) return ANS_ERR_INVALID_ARG;
@@ -702,7 +703,6 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   a.window = std::min<uint32_t>(d.window, 0x7FFFFFFFu);
   a.causal = d.causal != 0;
   a.out_wide = !((reinterpret_cast<uintptr_t>(d.d_out) | (d.out_token_stride | d.out_head_stride) * 2) & 15);
-  a.scale2 = static_cast<float>(d.scale * 1.4426950408889634);
   return ANS_OK;
 }
 
