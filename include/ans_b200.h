@@ -635,8 +635,8 @@ typedef struct ans_batch_desc {
  * in the attention below.  Where tokens are added behind others and need a larger scale,
  * the codes before them are rounded to it, code' = rint(code * old / new).  Codes of the block's other places stay.
  * A NaN or an infinity makes its block's scale NaN (and the block's values of that head read as NaN) until it begins anew.
- * No two sequences may get new tokens in the same page.  A page number outside the cache, a sequence longer than its
- * table, or rows that do not fit are left out and flagged ANS_STATUS_BAD_PAGE.
+ * No two sequences may get new tokens in the same page.  Tokens whose page is outside the cache or past table_pages pages are
+ * left out, as are sequences whose rows do not fit or that have fewer tokens than new ones, and flagged ANS_STATUS_BAD_PAGE.
  */
 int ans_block_cache_write(const ans_block_cache_desc* h_cache, const ans_batch_desc* h_batch, const void* d_k, const void* d_v,
                           int dtype, uint64_t k_token_stride, uint64_t k_head_stride, uint64_t v_token_stride,

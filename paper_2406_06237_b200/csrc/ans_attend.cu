@@ -14,11 +14,12 @@
 // evenly over the blocks that fit the GPU at once, and what a block has of a unit that others have parts of goes to a
 // workspace, which a second kernel joins in the order of the blocks: results do not depend on timing.
 //
-// Measured: one new token each of 64 requests with 762 to 1500 cached (32 query heads on 8, D = 128; 149 MB) 40.5 us, 3.7 TB/s;
-// one request of 32768 tokens 21.8 us.  What bounds is the issue of instructions and their latency at 4 warps a scheduler: the
-// first takes 19 us with the copies alone, about as long with the arithmetic alone, and the beginnings and ends of
-// units 7 to 9; the join is 3 to 4 of both.  That a tile may count apart in the sum (ans_attend.cuh) costs 1 of the first.  Not faster: two runs of 16 tokens at a time a warp (45.3 and 39.2: fewer bytes
-// under way), dealing over warps instead of blocks (42.5 and 23.4: more parts to join).
+// Measured: one new token each of 64 requests with 762 to 1500 cached (32 query heads on 8, D = 128; 149 MB) 41.8 us, 3.6 TB/s;
+// one request of 32768 tokens 21.9 us.  What bounds is the issue of instructions and their latency at 4 warps a scheduler (52 % of the issue
+// slots): over inputs that pass L2 several times the two take 39.6 and 19.9 us without the copies, 32.7 and 18.1 without the
+// arithmetic, 21.4 and 10.6 without both (the requests' numbers, tables, scales, the units' beginnings and ends), 37.9 and 17.2 without the join.
+// That a tile may count apart in the sum (ans_attend.cuh) costs 1 of the first.  Not faster: two runs of 16 tokens at a time a warp
+// (45.3 and 39.2 when the first was 44.3: fewer bytes under way), dealing over warps instead of blocks (42.5 and 23.4: more parts to join).
 #include <cmath>
 
 #include <algorithm>
@@ -706,8 +707,13 @@ static int check_attend(const ans_block_cache_desc& c, const ans_batch_desc& b, 
   return ANS_OK;
 }
 
-// What a call launches: the kernel of this file for sequences of up to `border` rows (new tokens x share), the tiles for
-// the others; one of them alone where the caller's numbers say that no sequence needs the other.
+// What a call launches: the kernel of this file for sequences of up to kBorder rows (new tokens x share), the tiles for
+// the others; one of them alone where the caller's numbers say that no sequence needs the other.  The two by the rows of a head, us, this kernel
+// and the tiles; 16 sequences of 2000 tokens, 64 of 500, one of 16000, 8 heads:
+//   D = 64:   16 rows  23  51    28  51    18  25      32 rows   33  53    44  53   23  25      64 rows   55  56    77  58   33  26
+//   D = 128:  16 rows  30  64    41  62    21  29      32 rows   49  66    67  63   29  29      64 rows   87  70   128  70   43  31
+//   D = 256:  16 rows  58 100    77  99    33  44      32 rows  102 104   140 104   52  44      64 rows  186  86   274 114   87  47
+// So 32 is the last number of rows at which this kernel is as fast or nearly so for D = 64 and 128; for D = 256, whose groups have 8 queries, 16 would be.
 constexpr uint32_t kBorder = 32;
 struct AttendPlan {
   bool with_rows, with_tiles;
@@ -729,6 +735,8 @@ static int plan_attend(const AttendArgs& a, uint32_t longest, AttendPlan& p) {
   const uint64_t most = uint64_t(longest) * a.share;
   p.with_tiles = most > kBorder;
   p.with_rows = !p.with_tiles || (a.b.n_seqs > 1 && a.share <= kBorder);          // a single token has `share` rows
+  // Groups of 8 queries or of 16: 16 queries in one group and in two take, for the sequences above, 23 and 25, 28 and 32, 18 and 17 us (D = 64), 30 and
+  // 34, 41 and 45, 21 and 22 (D = 128); 4 queries in a group of 16 and of 8 21 and 17, 25 and 20, 14 and 12; 28 and 24, 37 and 27, 19 and 15.
   if (p.with_rows)                                     // beside the tiles, most others are single tokens
     rc = for_shape(a.c.dim, (p.with_tiles ? a.share : most) <= 8 ? 1 : 2, [&](auto d, auto nt) {
       plan_shape<d(), nt()>(a, p.with_tiles ? std::max(kBorder / a.share, 1u) : longest, sms, p.rows);

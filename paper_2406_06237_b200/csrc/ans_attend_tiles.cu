@@ -14,9 +14,11 @@
 // For 64 tokens of 128 dimensions the two halves' four products take 1024 clocks of the tensor pipe and their 16384
 // exponentials as many (16 a clock).  What bounds is neither but a half's own chain, about 2100 clocks: S out of tensor
 // memory, the row's maximum, exponentials, P back, each waiting for the one before with one warp a scheduler and half.  A
-// prompt of 4096 (32 query heads on 8, D = 128) takes 172 us, 800 TFLOP/s of the products that causal order leaves; five chunks
-// of 1229 to 2048 behind 3601 to 6001 cached ones 875 us, 843.  Blocks of 128 tokens with one place for S and two stages took 184 and
-// 938.  Measured and not taken: a part of the exponentials by a polynomial on the plain units (170 and 868 at best), 16
+// prompt of 4096 (32 query heads on 8, D = 128) takes 176 us, 780 TFLOP/s of the products that causal order leaves; five chunks
+// of 1229 to 2048 behind 3601 to 6001 cached ones 900 us, 820 (172 and 875 before runs could count apart in the sum, ans_attend.cuh).  The prompt
+// takes 144 with D = 64 and 400 with D = 256, whose one half has nothing beside its chain and whose registers spill (492 bytes a thread; 12
+// with D = 128, none with 64).  Blocks of 128 tokens with one place for S and two stages took 184 and
+// 938 for 172 and 875.  Measured and not taken: a part of the exponentials by a polynomial on the plain units (170 and 868 for the 172 and 875 at best), 16
 // softmax warps with half a row a thread (a tenth slower), an issuer that takes whichever product is ready (the same).
 //
 // A half has two places for S, in turn, with a barrier for S and one for P each: a warp whose rows need no rescaling may be
@@ -654,7 +656,9 @@ static void plan_tiles_shape(const AttendArgs& a, int sms, AtPlan& p) {
   using S = AtShape<D>;
   const uint64_t rows = uint64_t(a.b.rows) * a.share;
   p.tiles = static_cast<uint32_t>(rows / S::kRows + a.b.n_seqs);
-  // parts: as many as there are SMs for, of 512 tokens at least
+  // Parts: as many as there are SMs for, of 512 tokens at least, 16 at most.  100 tokens (4 query heads a head, D = 128) behind 700, 1500 and 3000 of 2
+  // heads take 25, 25 and 25 us, undivided 25, 40 and 67; with parts of 128 tokens 17, 20 and 21, of 1024 25, 40 and 33.  Behind 64000 of 8, 2 and 1
+  // heads 155, 93 and 90 us; with up to 8 parts 172, 163 and 159, with up to 37 155, 58 and 54.
   const uint64_t units = std::max<uint64_t>((rows + S::kRows - 1) / S::kRows * a.c.heads, 1);
   const uint64_t most = uint64_t(a.b.table_pages) * a.c.page_size / 512;
   p.splits = static_cast<uint32_t>(std::max<uint64_t>(std::min<uint64_t>({uint64_t(sms) / units, most, 16}), 1));

@@ -9,10 +9,10 @@
 //
 // A block of threads has one (sequence, page, head) of the keys or of the values: the new values' largest magnitude, the scale,
 // the codes.  The values are held in registers between the two, 64 a thread (32 in fp32), by as many threads as that takes for a
-// page, 128 to 512; what a larger page has more is read again.  8194 tokens of 8 heads of 128 in pages of 64: 15.1 us held, 18.0 read
-// again; 8000 in pages of 128: 14.4, and 23.0 by 128 threads that also waited for the old scale first; 1750 of 4 heads of 256 in fp32 in pages of 128: 6.7 and 17.1.  Bound by issue (54 %
-// of the slots) and the blocks' own beginnings where prompts are written, by latency (numbers of the sequence, page number,
-// values, codes: four trips) for single tokens.  Both keys and values by one block took 16.5 for the 15.1.
+// page, 128 to 512; what a larger page has more is read again.  8194 tokens of 8 heads of 128 in pages of 64: 15.0 us held, 18.0 read
+// again when held it was 15.1; 8000 in pages of 128 14.4, and 23.0 by 128 threads that also waited for the old scale first; 1750 of 4 heads of 256 in fp32 in pages of
+// 128 6.7 and 17.1.  Bound by issue (61 % of the slots) and the blocks' own beginnings where prompts are written, by latency (numbers of
+// the sequence, page number, values, codes: four trips) for single tokens.  Both keys and values by one block took 16.5 for the 15.1.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -85,7 +85,7 @@ __device__ __forceinline__ uint32_t code_of(float x, float scale, float per) {
 // gridDim.x: at least the pages that can get tokens: sequence s has places starts[s] / P + 2 s and on, of which there are at
 // least m / P + 2 before the next one's, and m new tokens lie in at most m / P + 2 pages.
 // THREADS: so that a page is held, if 512 can.  Blocks an SM: registers for all loads of the held values at once; left to the compiler,
-// 1750 rows of 4 x 256 in fp32 take 8.6 us, so 6.7, 8194 tokens of 8 x 128 16.1 and 15.0.
+// 1600 rows of 4 x 256 in fp32 take 8.6 us, so 6.7, 8194 tokens of 8 x 128 16.1 and 15.0.
 template <typename T, uint32_t THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 7 : THREADS == 256 ? 4 : 1) ans_block_write_kernel(const BlockWriteArgs a) {
   let_next_start();

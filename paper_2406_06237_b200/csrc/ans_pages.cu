@@ -8,8 +8,9 @@
 // Each block makes the sums by itself (they are what a row's search needs, in shared memory) and takes a part of the rows and of the
 // pages.  Where lengths lie over cached, or taken over taken, something has to stand between the last read of the requests'
 // numbers and the first write: the blocks are then one cluster of up to 8 with its barrier; no workspace, no second launch.  A small
-// call is bound by latency (3.2 us: launch, one trip for the numbers, the sums, one trip for the pages, the stores), a large one by
-// instructions, about 100 a row (158 thousand rows of 700 requests 5.8 us on all SMs, 37.8 on a cluster of 8).
+// call is bound by latency (3.1 us: launch, one trip for the numbers, the sums, one trip for the pages, the stores), and so is a large one: two
+// trips of the sums, ten steps of the search, the pages (158 thousand rows of 700 requests 5.8 us on all SMs, 36 % of the issue slots used;
+// in place 36, as eight SMs do the work).
 #include <algorithm>
 #include <initializer_list>
 
