@@ -379,7 +379,8 @@ __global__ void __launch_bounds__(kAdThreads, 2) ans_adapters_up_kernel(const Ad
 #pragma unroll
         for (uint32_t p = 0; p < 8; ++p) sum += v[p];
         sum *= a.x_scales && row < live ? a.x_scales[begin + row] * scale : scale;
-        const __nv_bfloat16 hi = __float2bfloat16_rn(sum);
+        constexpr float kMost = 3.3895313892515355e38f;                // the largest bf16 number: what is finite stays so
+        const __nv_bfloat16 hi = __float2bfloat16_rn(isfinite(sum) ? fminf(fmaxf(sum, -kMost), kMost) : sum);
         const float rest = sum - __bfloat162float(hi);
         high[row * S::kHRow + k] = hi;
         low[row * S::kHRow + k] = __float2bfloat16_rn(isfinite(rest) ? rest : 0.f);

@@ -30,3 +30,17 @@ def test_an_infinity_gives_what_the_definition_gives(rank, new, n_in, n_out):
     odd = ~want.isfinite()
     assert torch.equal(got.to(F64)[odd].nan_to_num(7.0, 5.0, -5.0), want[odd].nan_to_num(7.0, 5.0, -5.0))
     assert got[~odd].isfinite().all() and f.read_status() == 0
+
+
+@pytest.mark.parametrize("new", [[1, 1], [20, 7]])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_sum_above_the_largest_bf16_number_stays_finite(new, sign):
+    """h = 3.3895e38 + 1e36 is an fp32 number that bf16 rounds to infinity; out is h 2^-100 within 2^-17 of it and one rounding to fp32."""
+    rows, starts = sums(new)[-1], sums(new)
+    a, b = torch.zeros(1, 16, 64, dtype=BF16, device="cuda"), torch.zeros(1, 32, 16, dtype=BF16, device="cuda")
+    a[0, 3, :2], b[0, :, 3] = 1, 2.0 ** -100
+    x = torch.zeros(rows, 64, dtype=BF16, device="cuda")
+    x[:, 0], x[:, 1] = sign * torch.finfo(BF16).max, sign * 1e36
+    got = Adapters(a, b)(x, torch.zeros(rows, 32, device="cuda"), ints([0, 0]), ints(starts)).to(F64)
+    want = x[:, :2].to(F64).sum(1, keepdim=True) * 2.0 ** -100
+    assert ((got - want).abs() <= (2.0 ** -17 + 2.0 ** -24) * want.abs()).all()
